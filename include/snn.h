@@ -275,6 +275,101 @@ const char *snn_last_error(const snn_ctx *ctx); /* never NULL; "" if none */
 void snn_destroy(snn_ctx *ctx);
 
 /*
+ * ---- Operators of token sequence models ---------------------------------------------------------------------------
+ * Layers and a loss that train or run beside the networks above, on arrays that the caller owns: a recurrence whose leak depends on
+ * the input, activations kept in 8 bits for the backward pass, and the cross entropy of a readout over a whole vocabulary.
+ *
+ * Every array is in the memory of snn_launch.device (SNN_E_INVAL otherwise, NULL where it is not optional included), aligned
+ * to its elements; an array of outputs overlaps no other array of the call unless said otherwise.  The calls queue their kernels on
+ * snn_launch.stream and return: they wait for nothing, allocate nothing, keep nothing and may be captured into a HIP graph.
+ * Arguments are checked before anything is queued.  The workspace belongs to a call until its kernels have run, is not read before it is written, and
+ * needs to be aligned to 256 bytes; calls that may run at the same time (two streams, two graphs) need one each.  Two calls with the same
+ * arguments give the same bits.  Calls may come from any thread, for any device, whatever the current one is.
+ */
+typedef enum { SNN_F32 = 0, SNN_BF16 = 1 } snn_dtype; /* type of activations, weights and their gradients */
+
+typedef struct {
+  int32_t device;  /* HIP device ordinal */
+  void *stream;    /* hipStream_t of that device; NULL: its default stream */
+  void *workspace; /* of at least the bytes that the operator's _workspace function says; may be NULL where that is 0 */
+  size_t workspace_bytes;
+} snn_launch;
+
+/* Text of the last operator call of this thread that did not return SNN_OK; never NULL, "" if there was none. */
+const char *snn_launch_error(void);
+
+/* Gated linear recurrence over time-major sequences [T][batch][n], each channel by itself:
+ *   a_t = sigmoid(z_t) ;  h_t = a_t h_{t-1} + (1 - a_t) x_t ,  t = 1..T
+ * Computed as h + sigmoid(-z) (x - h) in fp32 whatever the type: a state or drive that is not finite gives NaN from its step on. */
+typedef struct {
+  int32_t T, batch, n;        /* T >= 0 (0: h_last = h0), at most 2^30 steps and 2^30 channels batch * n */
+  int32_t dtype;              /* snn_dtype of z, x, h, dh, dz, dx */
+  int64_t ld_z, ld_x, ld_h;   /* elements between consecutive rows (t, b) of z, of x, of h and dh; 0: n.  z and x may be the halves of
+                                 one projection [T][batch][2 n], and dz and dx those of its gradient */
+  int64_t ld_dz, ld_dx;       /* the same of dz, dx (not used by the forward pass) */
+  const int32_t *lengths;     /* [batch] or NULL (T each): sequence b has steps 1..lengths[b]; a number outside 0..T counts as the nearer
+                                 end.  Later steps are read by nothing; h, dz and dx are zeros there */
+} snn_glr;
+
+/* Bytes of workspace for snn_glr_forward and both snn_glr_backward calls of this shape (0 for an invalid one too). */
+size_t snn_glr_workspace(const snn_glr *p);
+
+/* h0 [batch][n] fp32 or NULL (zeros); h; h_last [batch][n] fp32 or NULL: the state after a sequence's last step, may be h0 itself
+ * (serving: T = 1, state in and out); kept [ceil(T / 128)][batch][n] fp32 or NULL: the states before the steps 1, 129, 257, ..., which the
+ * backward pass recomputes h from. */
+snn_status snn_glr_forward(const snn_launch *at, const snn_glr *p, const void *z, const void *x, const float *h0, void *h, float *h_last,
+                           float *kept);
+
+/* Gradients of z, x and h0 from those of h and, where dh_last [batch][n] fp32 is not NULL, of h_last; h itself is not needed.
+ * dh0 [batch][n] fp32 may be NULL; it may be dh_last itself. */
+snn_status snn_glr_backward(const snn_launch *at, const snn_glr *p, const void *z, const void *x, const float *kept, const void *dh,
+                            const float *dh_last, void *dz, void *dx, float *dh0);
+
+/* Activations in 8 bits: blocks of 32 consecutive elements of a row (the last one of a row may be shorter) share a step, the smallest power of
+ * two, 2^-126 at least, with which no code exceeds 127 after rounding to nearest (ties to even).  An element is its code times the step, off by
+ * half a step at most (from 127.5 * 2^121 on, where the next multiple is no float, it is 127 * 2^121).  exps holds the step's exponent + 127, 0 for a block of zeros, 255 for a block with an infinity or NaN, which
+ * comes back as NaN throughout. */
+typedef struct {
+  const int8_t *codes; /* [rows][n] */
+  const uint8_t *exps; /* [rows][ceil(n / 32)] */
+  int64_t ld, ld_exps; /* elements between consecutive rows; 0: packed */
+} snn_packed;
+
+/* x: rows of cols elements, ld from one to the next (0: cols) -> codes [rows][cols], exps [rows][ceil(cols / 32)] */
+snn_status snn_pack(const snn_launch *at, int dtype, int64_t rows, int32_t cols, int64_t ld, const void *x, int8_t *codes, uint8_t *exps);
+/* and back: x = code * step, rounded to dtype */
+snn_status snn_unpack(const snn_launch *at, int dtype, int64_t rows, int32_t cols, int64_t ld, const int8_t *codes, const uint8_t *exps,
+                      void *x);
+
+/* snn_glr_backward from z and x as snn_pack left them ([T * batch] rows of n, or columns of wider rows that begin at a multiple of 32),
+ * whose distances between rows stand for ld_z and ld_x. */
+snn_status snn_glr_backward_packed(const snn_launch *at, const snn_glr *p, const snn_packed *z, const snn_packed *x, const float *kept,
+                                   const void *dh, const float *dh_last, void *dz, void *dx, float *dh0);
+
+/* Softmax cross entropy of rows h [rows][d] against a vocabulary w [vocab][d] (a row per entry, the layout of an embedding table):
+ *   logits_r = w h_r ;  loss_r = log sum_v exp(logits_rv) - logits_r,target
+ * Logits are never in memory as a whole.  bf16 products are summed in fp32; in fp32 they keep 24 bits. */
+typedef struct {
+  int32_t rows, d, vocab; /* rows 0..2^22, d 1..2^16, vocab 1..2^24 */
+  int32_t dtype;          /* snn_dtype of h, w, dh, dw */
+  int64_t ld_h, ld_w;     /* elements between rows of h and of w (0: d; at most 2^22); dh and dw are packed */
+} snn_vocab;
+
+/* Bytes of workspace for snn_vocab_loss (gradients = 0) or snn_vocab_loss_grad; 0 for an invalid shape too. */
+size_t snn_vocab_workspace(const snn_vocab *p, int32_t gradients);
+
+/* targets [rows]; one outside 0..vocab-1 (-1: padding) makes a row that has a loss of 0, no gradient and no part in a mean.
+ * loss [rows] fp32; state [rows][3] fp32: largest logit, 1 / sum of exp(logit - largest), 1 - softmax of the target.  The third is a
+ * sum of the other entries, so that loss and gradient of a target that is nearly certain keep their digits. */
+snn_status snn_vocab_loss(const snn_launch *at, const snn_vocab *p, const void *h, const void *w, const int32_t *targets, float *loss,
+                          float *state);
+
+/* Gradients dh [rows][d] and dw [vocab][d] (every row of it written) of sum_r dloss_r loss_r; dloss [rows] fp32, or NULL: of the mean over
+ * the rows that have a target.  h, w, targets: as snn_vocab_loss had them, state: what it gave. */
+snn_status snn_vocab_loss_grad(const snn_launch *at, const snn_vocab *p, const void *h, const void *w, const int32_t *targets,
+                               const float *state, const float *dloss, void *dh, void *dw);
+
+/*
  * Test hooks.  The library chooses its kernels from the layer shapes, the batch size, the state size and the
  * firing rates of the previous step; every choice by the rates gives the same bits.  The parity tests force each
  * flavour through environment variables, read by the library at the points noted.  They are not part of the

@@ -11,6 +11,10 @@ import os
 
 import numpy as np
 
+from . import ops
+from .ops import (Packed, snn_glr_backward, snn_glr_forward, snn_pack, snn_unpack, snn_vocab_loss,  # noqa: F401
+                  snn_vocab_loss_grad)
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsnn_mi355x.so")
 
@@ -25,7 +29,9 @@ OP_NAMES = {1: "SAVE_LOCAL", 2: "SAVE_REMOTE", 3: "LOAD_REMOTE", 4: "REFWD1", 5:
 EXPORTS = ["snn_init", "snn_set_weights", "snn_forward", "snn_bptt", "snn_bind_inputs", "snn_grads",
            "snn_get_spikes", "snn_get_readout", "snn_debug_states", "snn_bytes_required",
            "snn_state_slots", "snn_schedule", "snn_last_error", "snn_destroy", "snn_debug_copy", "snn_debug_die_exchanges",
-           "snn_suggest_intervals", "snn_debug_currents", "snn_get_state", "snn_forward_noalloc"]
+           "snn_suggest_intervals", "snn_debug_currents", "snn_get_state", "snn_forward_noalloc", "snn_launch_error",
+           "snn_glr_workspace", "snn_glr_forward", "snn_glr_backward", "snn_glr_backward_packed", "snn_pack", "snn_unpack",
+           "snn_vocab_workspace", "snn_vocab_loss", "snn_vocab_loss_grad"]
 
 
 class snn_config(C.Structure):
@@ -108,6 +114,7 @@ def lib() -> C.CDLL:
                      "snn_get_spikes", "snn_get_readout", "snn_debug_states", "snn_debug_copy", "snn_debug_currents",
                      "snn_get_state", "snn_forward_noalloc", "snn_debug_die_exchanges"):
             getattr(L, name).restype = C.c_int
+        ops.declare(L)
         _lib = L
     return _lib
 

@@ -7,7 +7,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsnn_mi355x.so")
-SOURCES = ["snn_kernels.hip", "snn_api.cpp", "snn_schedule.cpp"]
+SOURCES = ["snn_kernels.hip", "snn_api.cpp", "snn_schedule.cpp", "snn_ops.cpp", "snn_glr.hip", "snn_pack.hip",
+           "snn_vocab.hip"]
 
 # -ffp-contract=off: the forward/recompute arithmetic must not fuse multiply-adds (bit-exact spike
 # trains); packed fp32 instructions are disabled for the whole library.

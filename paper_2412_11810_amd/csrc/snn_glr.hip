@@ -1,0 +1,476 @@
+// Gated linear recurrence over [T][batch][n] and its backward pass.
+//
+//   b_t = sigmoid(-z_t);  h_t = h_{t-1} + b_t (x_t - h_{t-1})                       (a_t = 1 - b_t is what the state retains)
+//   g_t = dh_t + G_{t+1};  G_t = g_t - b_t g_t;  dx_t = b_t g_t;  dz_t = (1 - b_t) dx_t (h_{t-1} - x_t)
+//
+// Every channel (b, i) is a recurrence of its own.  16 steps of one channel are a map h -> h - Q h + B, and two maps in a row are one
+// again: Q = Q1 + Q2 (1 - Q1), B = B1 + (B2 - Q2 B1).  Q = 1 - product(a) is what is carried, not the product: b is
+// accurate relative to itself however small, where 1 - b rounds, so long memories (b of 1e-4 and less) keep their weight
+// against the drive.  A wavefront holds 16 steps of 64 lanes in registers, the eight wavefronts of a workgroup hold 128 steps in a row,
+// exchange their maps through LDS and then know the state that each of them starts from: one read of z and x, one write of h.
+// The state before every 128 steps is what the forward pass keeps; the backward pass gets h_{t-1} from there by
+// the same exchange, beside that of the gradient, which runs the other way.
+#include "snn_ops.h"
+
+namespace {
+
+constexpr int STEPS = 16; // steps of a wavefront
+constexpr int WAVES = SNN_GLR_INTERVAL / STEPS;
+
+// VEC consecutive elements of a row as they are in memory
+template <typename T, int VEC> struct Raw;
+template <> struct Raw<float, 1> { typedef uint32_t type; };
+template <> struct Raw<__bf16, 1> { typedef uint16_t type; };
+template <> struct Raw<__bf16, 2> { typedef uint32_t type; };
+template <> struct Raw<int8_t, 1> { typedef uint8_t type; };
+template <> struct Raw<int8_t, 2> { typedef uint16_t type; };
+
+template <typename T, int VEC> __device__ __forceinline__ void widen(typename Raw<T, VEC>::type r, float (&v)[VEC]) {
+  if constexpr (sizeof(T) == 4) v[0] = __uint_as_float(r);
+  else if constexpr (sizeof(T) == 2) {
+    v[0] = __uint_as_float((uint32_t)r << 16);
+    if constexpr (VEC == 2) v[1] = __uint_as_float(r & 0xffff0000u);
+  } else {
+    v[0] = (float)(int8_t)(r & 0xff);
+    if constexpr (VEC == 2) v[1] = (float)((int16_t)r >> 8);
+  }
+}
+template <typename T, int VEC> __device__ __forceinline__ typename Raw<T, VEC>::type narrow(const float (&v)[VEC]) {
+  if constexpr (sizeof(T) == 4) return __float_as_uint(v[0]);
+  else {
+    uint32_t r = __builtin_bit_cast(uint16_t, (__bf16)v[0]); // to nearest, ties to even
+    if constexpr (VEC == 2) r |= (uint32_t) __builtin_bit_cast(uint16_t, (__bf16)v[1]) << 16;
+    return (typename Raw<T, VEC>::type)r;
+  }
+}
+
+// sigmoid(-z).  The bound keeps 1 + e^z finite; a NaN passes it.
+__device__ __forceinline__ float moved(float z) {
+  float v = z * 1.44269504f;
+  v = v > 126.f ? 126.f : v;
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v));
+}
+
+__device__ __forceinline__ void lds_barrier() { // of the LDS alone: loads from memory stay in flight
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+struct Args {
+  const void *z, *x, *dh;
+  void *h, *dz, *dx;
+  const uint8_t *ze, *xe;
+  const int *lengths;
+  const float *from;  // forward: h0, backward: dh_last (NULL: zeros)
+  float *to;          // forward: h_last, backward: dh0 (NULL: not wanted)
+  float *kept;        // [tiles][channels]
+  float2 *maps;       // [segments + 1][channels], entry 0: `from`
+  long long ld_z, ld_x, ld_h, ld_ze, ld_xe, ld_dz, ld_dx; // elements from one row (t, b) to the next
+  int T, batch, n, channels, tiles, seg_tiles, segments;
+};
+
+// What a lane works on: VEC channels from c on
+template <int VEC> struct Lane {
+  int c, b, i, len;
+  bool on;
+  __device__ __forceinline__ Lane(const Args &a) {
+    c = (blockIdx.x * 64 + threadIdx.x) * VEC;
+    on = c < a.channels;
+    if (!on) c = 0;
+    b = c / a.n;
+    i = c - b * a.n;
+    len = a.T;
+    if (a.lengths) len = min(max(a.lengths[b], 0), a.T);
+  }
+};
+
+// An array [T][batch][ld] of elements of `size` bytes as a lane sees it: the offset of its element inside a step is kept in 32 bits
+// (a step has less than 4 GB), that of the step in scalar registers.
+struct Rows {
+  char *base;
+  long long step;
+  unsigned at;
+  __device__ __forceinline__ Rows(const void *p, int size, long long ld, int batch, int b, int i)
+      : base((char *)p), step((long long)size * ld * batch), at((unsigned)((size_t)size * (b * ld + i))) {}
+  template <typename R> __device__ __forceinline__ R &of(int t) const { return *(R *)(base + t * step + at); }
+  // 16 steps from t0 on.  Steps at and past T are those of the last one again (and not used).
+  template <typename R> __device__ __forceinline__ void load(R (&r)[STEPS], int t0, int T) const {
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) r[j] = of<const R>(min(t0 + j, T - 1));
+  }
+};
+
+// LDS of a workgroup: the maps of its wavefronts, for even and odd tiles (a tile's are read while the next one's are written)
+template <int VEC, int N> struct Maps { float v[2][N][WAVES][VEC][64]; };
+
+// Forward pass of one segment (blockIdx.y) of tiles.  MAPS: only the segment's map into maps[segment + 1], nothing stored; else the
+// state at its beginning comes from the maps before it.  NW = 1: sequences of up to 16 steps, one wavefront each.
+template <typename T, int VEC, int NW, bool MAPS>
+__global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
+  __shared__ Maps<VEC, 2> maps;
+  typedef typename Raw<T, VEC>::type R;
+  const Lane<VEC> me(a);
+  const Rows pz(a.z, sizeof(T), a.ld_z, a.batch, me.b, me.i), px(a.x, sizeof(T), a.ld_x, a.batch, me.b, me.i);
+  const Rows ph(a.h, sizeof(T), a.ld_h, a.batch, me.b, me.i);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.y), seg = blockIdx.y;
+  const int k0 = seg * a.seg_tiles, k1 = min(k0 + a.seg_tiles, a.tiles);
+  float h[VEC], q[VEC]; // the state (MAPS: from zero), and Q of the segment so far
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    h[v] = 0.f;
+    q[v] = 0.f;
+    if (MAPS || a.segments == 1) {
+      const float f = a.from && me.on ? a.from[me.c + v] : 0.f;
+      if (!MAPS) h[v] = f;
+      else if (seg == 0 && w == 0 && me.on) a.maps[me.c + v] = make_float2(0.f, f);
+    } else {
+      h[v] = a.maps[me.c + v].y;
+      for (int k = 1; k <= seg; ++k) {
+        const float2 m = a.maps[(size_t)k * a.channels + me.c + v];
+        h[v] += m.y - m.x * h[v];
+      }
+    }
+  }
+  // (a state that `to` may take the place of is read by every wavefront before the first one may write it)
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) asm volatile("" ::"v"(h[v]));
+  R rz[STEPS], rx[STEPS];
+  int t0 = (k0 * NW + w) * STEPS;
+  if (k0 < k1) {
+    pz.load(rz, t0, a.T);
+    px.load(rx, t0, a.T);
+  }
+  for (int k = k0; k < k1; ++k, t0 += NW * STEPS) {
+    float b[STEPS][VEC], x[STEPS][VEC];
+    const int live = me.len - t0; // steps of these 16 that the sequence has
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+      float z[VEC];
+      widen<T, VEC>(rz[j], z);
+      widen<T, VEC>(rx[j], x[j]);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        b[j][v] = j < live ? moved(z[v]) : 0.f;
+        x[j][v] = j < live ? x[j][v] : 0.f;
+      }
+    }
+    if (k + 1 < k1) {
+      pz.load(rz, t0 + NW * STEPS, a.T);
+      px.load(rx, t0 + NW * STEPS, a.T);
+    }
+    float start[VEC];
+    if (NW > 1) {
+      float Q[VEC] = {}, B[VEC] = {};
+#pragma unroll
+      for (int j = 0; j < STEPS; ++j)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          B[v] = fmaf(b[j][v], x[j][v] - B[v], B[v]);
+          Q[v] = fmaf(b[j][v], 1.f - Q[v], Q[v]);
+        }
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        maps.v[k & 1][0][w][v][threadIdx.x] = Q[v];
+        maps.v[k & 1][1][w][v][threadIdx.x] = B[v];
+      }
+      lds_barrier();
+      if (!MAPS && w == 0 && a.kept && me.on)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) a.kept[(size_t)k * a.channels + me.c + v] = h[v];
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          if (i == w) start[v] = h[v];
+          const float Qi = maps.v[k & 1][0][i][v][threadIdx.x], Bi = maps.v[k & 1][1][i][v][threadIdx.x];
+          h[v] += fmaf(-Qi, h[v], Bi);
+          if (MAPS) q[v] = fmaf(Qi, 1.f - q[v], q[v]);
+        }
+    } else {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        start[v] = h[v];
+        if (a.kept && me.on) a.kept[me.c + v] = h[v];
+      }
+    }
+    if (!MAPS) {
+#pragma unroll
+      for (int j = 0; j < STEPS; ++j) {
+        float out[VEC];
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          start[v] = fmaf(b[j][v], x[j][v] - start[v], start[v]);
+          out[v] = j < live ? start[v] : 0.f;
+        }
+        if (t0 + j < a.T && me.on) ph.of<R>(t0 + j) = narrow<T, VEC>(out);
+      }
+      if (NW == 1)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) h[v] = start[v];
+    }
+  }
+  if (w == 0 && me.on)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      if (MAPS) a.maps[(size_t)(seg + 1) * a.channels + me.c + v] = make_float2(q[v], h[v]);
+      else if (a.to && seg == a.segments - 1) a.to[me.c + v] = h[v];
+    }
+}
+
+// Backward pass of one segment, last tile first.  P: the type of z and x in memory (int8_t: codes of blocks, with their exponent
+// bytes).  MAPS: only the map of the segment's gradient, G at its end -> G at its beginning, which takes no x and no state; segment s
+// writes maps[segments - s].
+template <typename T, typename P, int VEC, bool MAPS>
+__global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
+  constexpr bool PACKED = sizeof(P) == 1;
+  __shared__ Maps<VEC, 3> maps;
+  typedef typename Raw<T, VEC>::type R;
+  const Lane<VEC> me(a);
+  const Rows pz(a.z, sizeof(P), a.ld_z, a.batch, me.b, me.i), px(a.x, sizeof(P), a.ld_x, a.batch, me.b, me.i);
+  const Rows pze(a.ze, 1, a.ld_ze, a.batch, me.b, me.i / SNN_PACK_BLOCK), pxe(a.xe, 1, a.ld_xe, a.batch, me.b, me.i / SNN_PACK_BLOCK);
+  const Rows pd(a.dh, sizeof(T), a.ld_h, a.batch, me.b, me.i);
+  const Rows pdz(a.dz, sizeof(T), a.ld_dz, a.batch, me.b, me.i), pdx(a.dx, sizeof(T), a.ld_dx, a.batch, me.b, me.i);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.y), seg = blockIdx.y + (MAPS ? 1 : 0);
+  const int k0 = seg * a.seg_tiles, k1 = min(k0 + a.seg_tiles, a.tiles);
+  float g[VEC], q[VEC]; // G (MAPS: from zero), and Q of the segment so far
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    g[v] = 0.f;
+    q[v] = 0.f;
+    if (MAPS || a.segments == 1) {
+      const float f = a.from && me.on ? a.from[me.c + v] : 0.f;
+      if (!MAPS) g[v] = f;
+      else if (seg == 1 && w == 0 && me.on) a.maps[me.c + v] = make_float2(0.f, f);
+    } else {
+      g[v] = a.maps[me.c + v].y;
+      for (int k = 1; k < a.segments - seg; ++k) {
+        const float2 m = a.maps[(size_t)k * a.channels + me.c + v];
+        g[v] += m.y - m.x * g[v];
+      }
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) asm volatile("" ::"v"(g[v])); // (as in the forward pass)
+  typename Raw<P, VEC>::type rz[STEPS], rx[STEPS];
+  R rd[STEPS];
+  uint8_t ez[STEPS], ex[STEPS];
+  float kept[VEC];
+  auto fetch = [&](int k) {
+    const int t = (k * WAVES + w) * STEPS;
+    pz.load(rz, t, a.T);
+    pd.load(rd, t, a.T);
+    if (!MAPS) px.load(rx, t, a.T);
+    if (PACKED) {
+      pze.load(ez, t, a.T);
+      if (!MAPS) pxe.load(ex, t, a.T);
+    }
+    if (!MAPS)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) kept[v] = a.kept[(size_t)k * a.channels + me.c + v];
+  };
+  if (k0 < k1) fetch(k1 - 1);
+  for (int k = k1 - 1; k >= k0; --k) {
+    const int t0 = (k * WAVES + w) * STEPS;
+    float b[STEPS][VEC], x[STEPS][VEC], d[STEPS][VEC];
+    const int live = me.len - t0;
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+      float z[VEC];
+      widen<P, VEC>(rz[j], z);
+      if (!MAPS) widen<P, VEC>(rx[j], x[j]);
+      widen<T, VEC>(rd[j], d[j]);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        if (PACKED) {
+          z[v] *= __uint_as_float((uint32_t)ez[j] << 23);
+          if (!MAPS) x[j][v] *= __uint_as_float((uint32_t)ex[j] << 23);
+        }
+        b[j][v] = j < live ? moved(z[v]) : 0.f;
+        if (!MAPS) x[j][v] = j < live ? x[j][v] : 0.f;
+        d[j][v] = j < live ? d[j][v] : 0.f;
+      }
+    }
+    float Q[VEC] = {}, B[VEC] = {}, G[VEC] = {}, h[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) h[v] = kept[v];
+    if (k > k0) fetch(k - 1);
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        if (!MAPS) B[v] = fmaf(b[j][v], x[j][v] - B[v], B[v]);
+        Q[v] = fmaf(b[j][v], 1.f - Q[v], Q[v]);
+      }
+#pragma unroll
+    for (int j = STEPS - 1; j >= 0; --j)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float s = d[j][v] + G[v];
+        G[v] = fmaf(-b[j][v], s, s);
+      }
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      maps.v[k & 1][0][w][v][threadIdx.x] = Q[v];
+      maps.v[k & 1][1][w][v][threadIdx.x] = G[v];
+      if (!MAPS) maps.v[k & 1][2][w][v][threadIdx.x] = B[v];
+    }
+    lds_barrier();
+    float from[VEC];
+#pragma unroll
+    for (int i = WAVES - 1; i >= 0; --i)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        if (i == w) from[v] = g[v];
+        const float Qi = maps.v[k & 1][0][i][v][threadIdx.x];
+        g[v] += fmaf(-Qi, g[v], maps.v[k & 1][1][i][v][threadIdx.x]);
+        if (MAPS) q[v] = fmaf(Qi, 1.f - q[v], q[v]);
+      }
+    if (MAPS) continue;
+#pragma unroll
+    for (int i = 0; i < WAVES - 1; ++i)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v)
+        if (i < w) h[v] += fmaf(-maps.v[k & 1][0][i][v][threadIdx.x], h[v], maps.v[k & 1][2][i][v][threadIdx.x]);
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float off = x[j][v] - h[v];
+        h[v] = fmaf(b[j][v], off, h[v]);
+        x[j][v] = off;
+      }
+#pragma unroll
+    for (int j = STEPS - 1; j >= 0; --j) {
+      float dz[VEC], dx[VEC];
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float s = d[j][v] + from[v];
+        dx[v] = b[j][v] * s;
+        from[v] = fmaf(-b[j][v], s, s);
+        dz[v] = j < live ? (b[j][v] - 1.f) * dx[v] * x[j][v] : 0.f; // (0 whatever the state)
+      }
+      if (t0 + j < a.T && me.on) {
+        pdz.of<R>(t0 + j) = narrow<T, VEC>(dz);
+        pdx.of<R>(t0 + j) = narrow<T, VEC>(dx);
+      }
+    }
+  }
+  if (w == 0 && me.on)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      if (MAPS) a.maps[(size_t)(a.segments - seg) * a.channels + me.c + v] = make_float2(q[v], g[v]);
+      else if (a.to && seg == 0) a.to[me.c + v] = g[v];
+    }
+}
+
+// Tiles of 128 steps per segment.  One workgroup per group of channels walks the whole sequence, unless that leaves compute units
+// without work: the sequence is then cut so that each has two workgroups, at the price of a launch before that finds the
+// segments' maps (z and x, or dh, are read twice).
+constexpr int WORKGROUPS = 512;
+void cut(Args *a, int vec) {
+  const int groups = (a->channels + 64 * vec - 1) / (64 * vec);
+  const int want = (WORKGROUPS + groups - 1) / groups;
+  a->tiles = (a->T + SNN_GLR_INTERVAL - 1) / SNN_GLR_INTERVAL;
+  a->seg_tiles = a->tiles ? (a->tiles + want - 1) / want : 1;
+  a->segments = a->tiles ? (a->tiles + a->seg_tiles - 1) / a->seg_tiles : 1;
+}
+
+Args shape_args(const GlrShape &p) {
+  Args a = {};
+  a.lengths = p.lengths;
+  a.T = p.T;
+  a.batch = p.batch;
+  a.n = p.n;
+  a.channels = p.batch * p.n;
+  a.ld_z = p.ld_z;
+  a.ld_x = p.ld_x;
+  a.ld_dz = p.ld_dz;
+  a.ld_dx = p.ld_dx;
+  a.ld_h = p.ld_h;
+  return a;
+}
+
+bool pairs(const void *p, size_t size, long long ld) { return (ld & 1) == 0 && (uintptr_t)p % (2 * size) == 0; }
+
+template <typename T, int VEC> hipError_t forward(Args a, hipStream_t s) {
+  const dim3 groups((a.channels + 64 * VEC - 1) / (64 * VEC));
+  if (a.T <= STEPS) {
+    a.tiles = a.T > 0;
+    a.seg_tiles = a.segments = 1;
+    k_glr_forward<T, VEC, 1, false><<<groups, dim3(64, 1), 0, s>>>(a);
+    return hipGetLastError();
+  }
+  cut(&a, VEC);
+  if (a.segments > 1) {
+    k_glr_forward<T, VEC, WAVES, true><<<dim3(groups.x, a.segments - 1), dim3(64, WAVES), 0, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  k_glr_forward<T, VEC, WAVES, false><<<dim3(groups.x, a.segments), dim3(64, WAVES), 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, typename P, int VEC> hipError_t backward(Args a, hipStream_t s) {
+  const dim3 groups((a.channels + 64 * VEC - 1) / (64 * VEC));
+  cut(&a, VEC);
+  if (a.segments > 1) {
+    k_glr_backward<T, P, VEC, true><<<dim3(groups.x, a.segments - 1), dim3(64, WAVES), 0, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  k_glr_backward<T, P, VEC, false><<<dim3(groups.x, a.segments), dim3(64, WAVES), 0, s>>>(a);
+  return hipGetLastError();
+}
+
+} // namespace
+
+size_t glr_workspace(const GlrShape &p) {
+  Args a = shape_args(p);
+  cut(&a, p.bf16 ? 2 : 1); // (one element per lane: no more segments than with two)
+  return a.segments > 1 ? (size_t)(a.segments + 1) * a.channels * sizeof(float2) : 0;
+}
+
+hipError_t launch_glr_forward(const GlrShape &p, const void *z, const void *x, const float *h0, void *h, float *h_last, float *kept,
+                              void *work, hipStream_t s) {
+  Args a = shape_args(p);
+  a.z = z;
+  a.x = x;
+  a.from = h0;
+  a.h = h;
+  a.to = h_last;
+  a.kept = kept;
+  a.maps = (float2 *)work;
+  if (!p.bf16) return forward<float, 1>(a, s);
+  const bool two = (p.n & 1) == 0 && pairs(z, 2, p.ld_z) && pairs(x, 2, p.ld_x) && pairs(h, 2, p.ld_h);
+  return two ? forward<__bf16, 2>(a, s) : forward<__bf16, 1>(a, s);
+}
+
+hipError_t launch_glr_backward(const GlrShape &p, const GlrInputs &in, const float *kept, const void *dh, const float *dh_last,
+                               void *dz, void *dx, float *dh0, void *work, hipStream_t s) {
+  Args a = shape_args(p);
+  a.z = in.z;
+  a.x = in.x;
+  a.kept = const_cast<float *>(kept);
+  a.dh = dh;
+  a.from = dh_last;
+  a.dz = dz;
+  a.dx = dx;
+  a.to = dh0;
+  a.maps = (float2 *)work;
+  const bool packed = in.ze != nullptr;
+  if (packed) {
+    a.ze = in.ze;
+    a.xe = in.xe;
+    a.ld_z = in.ld_z;
+    a.ld_x = in.ld_x;
+    a.ld_ze = in.ld_ze;
+    a.ld_xe = in.ld_xe;
+  }
+  if (!p.bf16) return packed ? backward<float, int8_t, 1>(a, s) : backward<float, float, 1>(a, s);
+  const size_t size = packed ? 1 : 2;
+  const bool two = (p.n & 1) == 0 && pairs(in.z, size, a.ld_z) && pairs(in.x, size, a.ld_x) && pairs(dh, 2, p.ld_h) &&
+                   pairs(dz, 2, p.ld_dz) && pairs(dx, 2, p.ld_dx);
+  if (packed) return two ? backward<__bf16, int8_t, 2>(a, s) : backward<__bf16, int8_t, 1>(a, s);
+  return two ? backward<__bf16, __bf16, 2>(a, s) : backward<__bf16, __bf16, 1>(a, s);
+}

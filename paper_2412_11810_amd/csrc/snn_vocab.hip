@@ -1,0 +1,476 @@
+// Softmax cross entropy of rows h [rows][d] against a vocabulary w [vocab][d], and its gradients, without a matrix of logits.
+//
+//   l_rv = h_r . w_v;  M_r = max_v l_rv;  S_r = sum_v exp(l_rv - M_r);  miss_r = sum_{v != y} exp(l_rv - M_r) / S_r = 1 - p_ry
+//   loss_r = -log1p(-miss_r), or M_r - l_ry + log S_r where miss_r is not small
+//   G_rv = dloss_r exp(l_rv - M_r) / S_r;  G_ry = -dloss_r miss_r;  dh = G w;  dw = G^T h
+//
+// miss_r is summed without the target, never formed as 1 - p: a target that the model is sure of keeps its loss and gradient.
+//
+// All four products are one kernel, C = A B^T with the sums along the rows of both operands, on the bf16 matrix cores with fp32
+// accumulators; what differs is what happens to the accumulators.  Operands of 32 bits go in as three bf16 parts of 8 bits
+// each, which hold all 24 bits of a float: the six products of parts whose weight is above 2^-24 are further steps of the same sum.
+// The logits are computed twice, for the loss (kept: one maximum and one sum for 128 of them) and for G, one piece of the
+// vocabulary after the other, whose G is all that is ever in memory; a second product of 2 rows d vocab operations costs less
+// than 4 bytes of logit written and read for each.
+#include "snn_ops.h"
+
+namespace {
+
+typedef __bf16 frag __attribute__((ext_vector_type(8)));
+typedef float tile32 __attribute__((ext_vector_type(16)));
+
+constexpr int BK = 64;    // elements of a row in LDS: 128 bytes
+constexpr int PAD = 256;  // rows of G are padded to whole tiles
+constexpr float LOG2E = 1.44269504f;
+
+// ---- C = A B^T ----------------------------------------------------------------------------
+// Operands: rows of ksteps * 64 bf16 each, in `parts` parts.  Rows past the last one are the last one again (not used by the epilogues).
+struct Product {
+  const __bf16 *a, *b;
+  long long lda, ldb, part_a, part_b; // elements from row to row, from part to part
+  int rows_a, rows_b, ksteps;
+  int tiles_a, tiles_b;
+};
+
+__device__ __forceinline__ void load_lds(const char *base, unsigned off, char *lds) {
+  // one wavefront: 64 * 16 bytes, lane after lane, to lds
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)0xffffffff, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)lds, 16, (int)off, 0, 0, 0);
+}
+
+// One tile of BM rows of A by BN rows of B by eight wavefronts, two along A and four along B.  A row's 64 elements are eight
+// 16-byte chunks in LDS; chunk c of row r is at place c ^ (r % 8), so that the lanes of a fragment, which read one chunk of
+// 32 rows, use all banks.  Loads go past the registers; the next 64 elements arrive while these are multiplied.
+template <int BM, int BN, int PARTS, class Epilogue>
+__global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
+  constexpr int MI = BM / 64, NI = BN / 128, LA = BM / 64, LB = BN / 64;
+  __shared__ __align__(16) char a0[BM * 128], b0[BN * 128], a1[BM * 128], b1[BN * 128];
+  // tiles in the order of the dies: consecutive workgroups are on different ones, each die takes a run of tiles, in groups of eight
+  // along A that share the rows of B
+  const unsigned n = p.tiles_a * p.tiles_b, per = n / 8, rest = n % 8;
+  const unsigned die = blockIdx.x % 8, at = blockIdx.x / 8;
+  const unsigned id = n < 8 ? blockIdx.x : die * per + min(die, rest) + at;
+  const unsigned group = id / (8 * p.tiles_b), first = group * 8, wide = min(8u, p.tiles_a - first), in = id - group * 8 * p.tiles_b;
+  const int ta = first + in % wide, tb = in / wide;
+
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wa = w >> 2, wb = w & 3;
+  const char *base_a = (const char *)(p.a + (long long)ta * BM * p.lda), *base_b = (const char *)(p.b + (long long)tb * BN * p.ldb);
+  unsigned off_a[LA], off_b[LB];
+  const int row8 = w * 8 + (lane >> 3), chunk = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+  for (int i = 0; i < LA; ++i) off_a[i] = (unsigned)min(i * 64 + row8, p.rows_a - 1 - ta * BM) * (unsigned)(p.lda * 2) + chunk * 16;
+#pragma unroll
+  for (int i = 0; i < LB; ++i) off_b[i] = (unsigned)min(i * 64 + row8, p.rows_b - 1 - tb * BN) * (unsigned)(p.ldb * 2) + chunk * 16;
+
+  tile32 acc[MI][NI] = {};
+  int k = 0, seg = 0;
+  constexpr int SEGS = PARTS == 1 ? 1 : 6;
+  auto fetch = [&](char *la, char *lb) {
+    // parts of A 0 1 2 0 1 0 with parts of B 2 1 0 1 0 0: the smallest products first
+    const int pa = PARTS == 1 ? 0 : (0x010210 >> (4 * seg)) & 15, pb = PARTS == 1 ? 0 : (0x001012 >> (4 * seg)) & 15;
+    const char *ga = base_a + pa * p.part_a * 2 + (long long)k * 128, *gb = base_b + pb * p.part_b * 2 + (long long)k * 128;
+#pragma unroll
+    for (int i = 0; i < LA; ++i) load_lds(ga, off_a[i], la + (i * 64 + w * 8) * 128);
+#pragma unroll
+    for (int i = 0; i < LB; ++i) load_lds(gb, off_b[i], lb + (i * 64 + w * 8) * 128);
+    if (++k == p.ksteps) { k = 0; ++seg; }
+  };
+  const int r = lane & 31, half = lane >> 5;
+  auto multiply = [&](const char *la, const char *lb) {
+#pragma unroll
+    for (int s = 0; s < BK / 16; ++s) {
+      frag fa[MI], fb[NI];
+      const int place = ((2 * s + half) ^ (r & 7)) * 16;
+#pragma unroll
+      for (int i = 0; i < MI; ++i) fa[i] = *(const frag *)(la + (wa * (BM / 2) + i * 32 + r) * 128 + place);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fb[i] = *(const frag *)(lb + (wb * (BN / 4) + i * 32 + r) * 128 + place);
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+    }
+  };
+  auto arrived = [&]() {
+    __builtin_amdgcn_s_waitcnt(0x0f70); // every load of this wavefront, then those of the others
+    __syncthreads();
+  };
+  const int steps = p.ksteps * SEGS;
+  fetch(a0, b0);
+  arrived();
+  for (int it = 0; it < steps; it += 2) {
+    if (it + 1 < steps) fetch(a1, b1);
+    multiply(a0, b0);
+    arrived();
+    if (it + 1 == steps) break;
+    if (it + 2 < steps) fetch(a0, b0);
+    multiply(a1, b1);
+    arrived();
+  }
+  // element e of a tile: row 8 (e / 4) + 4 half + e % 4 of A, row r of B
+  ep.template finish<BM, BN, MI, NI>(acc, ta * BM + wa * (BM / 2), tb * BN + wb * (BN / 4), r, half);
+}
+
+// x in parts of 8 bits each, cut off and not rounded: what is left is exact, and the third part has the last bits of 24
+template <int PARTS, int N = 1> __device__ __forceinline__ void split(float x, uint16_t (&part)[PARTS][N], int e = 0) {
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    const uint32_t bits = __float_as_uint(x) & 0xffff0000u;
+    part[k][e] = (uint16_t)(bits >> 16);
+    x -= __uint_as_float(bits);
+  }
+}
+
+// Row m's target, counted from entry v0 on; -1: none, or one before v0
+__device__ __forceinline__ int entry(const int *targets, int m, bool on, int vocab, int v0) {
+  const int y = on ? targets[m] : -1;
+  return y >= v0 && y < vocab ? y - v0 : -1;
+}
+
+// Logits, A = vocabulary (a piece of it from `first` on), B = rows of h.  A lane has the logits of one row with 16 MI entries of the
+// vocabulary: their maximum and sum, the target left out, and the target's logit go to memory.
+struct LossEpilogue {
+  const int *targets;
+  float2 *part;  // [blocks of BM / 2 entries][rows]
+  float *picked; // [rows]: the target's logit
+  int first, vocab, rows;
+  template <int BM, int BN, int MI, int NI>
+  __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int v0, int m0, int r, int half) const {
+    const int block = (first + v0) / (BM / 2);
+    v0 += first + 4 * half;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int m = m0 + j * 32 + r;
+      const bool on = m < rows;
+      const int y = entry(targets, m, on, vocab, v0); // the target's entry, counted as below
+      if (__any(((unsigned)y < 32u * MI && !(y & 4)) || v0 + 32 * MI > vocab)) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int v = 32 * i + 8 * (e >> 2) + (e & 3);
+            if (v == y && on) picked[m] = acc[i][j][e];
+            if (v == y || v0 + v >= vocab) acc[i][j][e] = -INFINITY;
+          }
+      }
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float from = top == -INFINITY ? 0.f : top; // nothing here: all terms are 0
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - from) * LOG2E);
+      sum += __shfl_xor(sum, 32);
+      if (half == 0 && on) part[(size_t)block * rows + m] = make_float2(top, sum);
+    }
+  }
+};
+
+// The same logits again, turned into G: as rows of h by entries of the vocabulary (gm) and the other way round (gt), in parts.
+template <int PARTS> struct GradEpilogue {
+  const int *targets;
+  const float *state, *scale; // scale [rows padded]: dloss, 0 for rows without a target
+  __bf16 *gm, *gt;            // [PARTS][rows padded][width], [PARTS][width][rows padded]
+  int first, vocab, rows, width, padded;
+  template <int BM, int BN, int MI, int NI>
+  __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int v0, int m0, int r, int half) const {
+    // (scalar addresses; what depends on the lane is one offset for each array)
+    const unsigned lane_m = (unsigned)(r * width + 4 * half) * 2, lane_t = (unsigned)(4 * half * padded + r) * 2;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int m = m0 + j * 32 + r;
+      const bool on = m < rows;
+      const int y = entry(targets, m, on, vocab, first + v0 + 4 * half), left = vocab - first - v0 - 4 * half;
+      const float g = on ? scale[m] : 0.f, top = on ? state[3 * m] : 0.f, per = on ? state[3 * m + 1] * g : 0.f;
+      const float miss = on ? state[3 * m + 2] : 0.f;
+      const bool none = g == 0.f; // no part in the gradients, whatever its logits
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int vq = 32 * i + 8 * q;
+          uint16_t parts[PARTS][4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = __builtin_amdgcn_exp2f((acc[i][j][4 * q + e] - top) * LOG2E) * per;
+            if (vq + e == y) x = -miss * g;
+            if (none || vq + e >= left) x = 0.f;
+            if constexpr (PARTS == 1) parts[0][e] = __builtin_bit_cast(uint16_t, (__bf16)x);
+            else split(x, parts, e);
+          }
+#pragma unroll
+          for (int k = 0; k < PARTS; ++k) {
+            uint2 four;
+            four.x = parts[k][0] | (uint32_t)parts[k][1] << 16;
+            four.y = parts[k][2] | (uint32_t)parts[k][3] << 16;
+            *(uint2 *)((char *)(gm + ((size_t)k * padded + m0 + j * 32) * width + v0 + vq) + lane_m) = four;
+            char *const t = (char *)(gt + ((size_t)k * width + v0 + vq) * padded + m0 + j * 32);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *(uint16_t *)(t + (size_t)e * padded * 2 + lane_t) = parts[k][e];
+          }
+        }
+    }
+  }
+};
+
+// C itself, [rows_a][rows_b] with ld elements per row, as T; or added to a sum in 32 bits (add: not the first part of it).
+template <typename T> struct StoreEpilogue {
+  T *out;
+  long long ld;
+  int rows_a, rows_b;
+  bool add;
+  template <int BM, int BN, int MI, int NI>
+  __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int ra, int rb, int r, int half) const {
+    const unsigned lane = (unsigned)(4 * half * ld + r) * sizeof(T);
+    const int left = rows_a - ra - 4 * half;
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+      if (rb + j * 32 + r < rows_b)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int a = 32 * i + 8 * (e >> 2) + (e & 3);
+            T *const to = (T *)((char *)(out + (ra + a) * ld + rb + j * 32) + lane);
+            if (a < left) {
+              if constexpr (sizeof(T) == 4) *to = add ? *to + acc[i][j][e] : acc[i][j][e];
+              else *to = (T)acc[i][j][e];
+            }
+          }
+  }
+};
+
+template <int PARTS, class Epilogue> hipError_t product(Product p, const Epilogue &ep, hipStream_t s) {
+  constexpr int B = 256;
+  p.tiles_a = (p.rows_a + B - 1) / B;
+  p.tiles_b = (p.rows_b + B - 1) / B;
+  k_product<B, B, PARTS, Epilogue><<<p.tiles_a * p.tiles_b, 512, 0, s>>>(p, ep);
+  return hipGetLastError();
+}
+
+// ---- operands -------------------------------------------------------------------------------
+// to[part][row][padded cols] = parts of from[row][cols]; zeros behind a row's end
+template <typename T, int PARTS>
+__global__ __launch_bounds__(256) void k_rows(const T *from, long long ld, int rows, int cols, __bf16 *to, int padded) {
+  const int c = blockIdx.x * 256 + threadIdx.x, r = blockIdx.y + blockIdx.z * 65535;
+  if (c >= padded || r >= rows) return;
+  uint16_t part[PARTS][1];
+  split(c < cols ? (float)from[r * ld + c] : 0.f, part);
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) *(uint16_t *)(to + ((size_t)k * rows + r) * padded + c) = part[k][0];
+}
+// to[part][col][padded rows] = parts of from[row][col]; zeros behind the last row and, where `scale` is given, for the rows whose
+// scale is 0: what they hold (padding: anything) would else meet the zeros of G as 0 * NaN
+template <typename T, int PARTS>
+__global__ __launch_bounds__(256) void k_columns(const T *from, long long ld, int rows, int cols, const float *scale, __bf16 *to, int padded) {
+  __shared__ T tile[64][65];
+  const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 64, l = threadIdx.x & 63, g = threadIdx.x >> 6;
+  for (int i = g; i < 64; i += 4) tile[i][l] = r0 + i < rows && c0 + l < cols && !(scale && scale[r0 + i] == 0.f) ? from[(r0 + i) * ld + c0 + l] : (T)0.f;
+  __syncthreads();
+  for (int i = g; i < 64; i += 4) {
+    if (c0 + i >= cols || r0 + l >= padded) continue;
+    uint16_t part[PARTS][1];
+    split((float)tile[l][i], part);
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) *(uint16_t *)(to + ((size_t)k * cols + c0 + i) * padded + r0 + l) = part[k][0];
+  }
+}
+
+// One wavefront per row: the blocks' maxima and sums joined, in an order that depends on nothing but their number.
+__global__ __launch_bounds__(256) void k_join(const float2 *part, const float *picked, const int *targets, int blocks, int rows, int vocab,
+                                              float *loss, float *state) {
+  const int m = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (m >= rows) return;
+  const int y = targets[m];
+  const bool has = y >= 0 && y < vocab;
+  float top = has ? picked[m] : -INFINITY;
+  const float own = top;
+  for (int b = lane; b < blocks; b += 64) top = fmaxf(top, part[(size_t)b * rows + m].x);
+#pragma unroll
+  for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+  float sum = 0.f;
+  for (int b = lane; b < blocks; b += 64) {
+    const float2 q = part[(size_t)b * rows + m];
+    sum += q.x == -INFINITY ? q.y : q.y * expf(q.x - top); // (an empty block has a sum of 0, or one of NaN)
+  }
+#pragma unroll
+  for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
+  if (lane) return;
+  const float mine = has ? expf(own - top) : 0.f, total = sum + mine, miss = sum / total;
+  loss[m] = !has ? 0.f : miss < 0.5f ? -log1pf(-miss) : top - own + logf(total);
+  state[3 * m] = top;
+  state[3 * m + 1] = 1.f / total;
+  state[3 * m + 2] = miss;
+}
+
+// scale[m] = the gradient of row m's loss, without one given that of their mean: 0 for rows without a target and for the padding
+__global__ __launch_bounds__(1024) void k_scale(const int *targets, const float *dloss, int rows, int padded, int vocab, float *scale) {
+  __shared__ int counts[16];
+  int count = 0;
+  if (!dloss) {
+    for (int m = threadIdx.x; m < rows; m += 1024) count += targets[m] >= 0 && targets[m] < vocab;
+#pragma unroll
+    for (int k = 32; k; k >>= 1) count += __shfl_xor(count, k);
+    if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = count;
+    __syncthreads();
+    count = 0;
+    for (int i = 0; i < 16; ++i) count += counts[i];
+  }
+  for (int m = threadIdx.x; m < padded; m += 1024) {
+    const bool has = m < rows && targets[m] >= 0 && targets[m] < vocab;
+    scale[m] = !has ? 0.f : dloss ? dloss[m] : 1.f / count;
+  }
+}
+
+template <typename T> __global__ __launch_bounds__(256) void k_narrow(const float *from, T *to, size_t n) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) to[i] = (T)from[i];
+}
+__global__ __launch_bounds__(256) void k_clear(uint16_t *to, size_t n) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) to[i] = 0;
+}
+
+// ---- workspace ------------------------------------------------------------------------------
+struct Space {
+  int parts, dp, padded, width; // width: entries of a piece of the vocabulary
+  size_t h, w, part, picked, scale, ht, wt, gm, gt, sum, bytes;
+  Space(const VocabShape &p, bool grad) {
+    parts = p.bf16 ? 1 : 3;
+    dp = (p.d + BK - 1) / BK * BK;
+    padded = (p.rows + PAD - 1) / PAD * PAD;
+    // G of a piece has about 2^27 elements, and a piece of w no more
+    const long long all = ((long long)p.vocab + PAD - 1) / PAD * PAD, most = grad ? (padded > dp ? padded : dp) : dp;
+    long long fit = (1ll << 27) / (most > 0 ? most : 1) / PAD * PAD;
+    if (fit < 2048) fit = 2048;
+    width = (int)(fit < all ? fit : all);
+    size_t at = 0;
+    auto take = [&](size_t n) { const size_t was = at; at += (n + 255) / 256 * 256; return was; };
+    h = take((size_t)2 * parts * p.rows * dp);
+    w = take((size_t)2 * parts * width * dp);
+    if (!grad) {
+      part = take(sizeof(float2) * (size_t)(all / 128) * p.rows);
+      picked = take(sizeof(float) * (size_t)p.rows);
+    } else {
+      scale = take(sizeof(float) * (size_t)padded);
+      ht = take((size_t)2 * parts * p.d * padded);
+      wt = take((size_t)2 * parts * p.d * width);
+      gm = take((size_t)2 * parts * padded * width);
+      gt = take((size_t)2 * parts * padded * width);
+      sum = take(width < p.vocab ? sizeof(float) * (size_t)p.rows * p.d : 0);
+    }
+    bytes = at;
+  }
+};
+
+#define TRY(call)                                 \
+  do {                                            \
+    const hipError_t e_ = (call);                 \
+    if (e_ != hipSuccess) return e_;              \
+  } while (0)
+
+// Rows as the products take them: where they are, if they are bf16, aligned and whole; else copied into `to`.
+template <typename T, int PARTS>
+hipError_t rows_of(const T *from, long long ld, int rows, int cols, int padded, __bf16 *to, const __bf16 **out, long long *out_ld,
+                   hipStream_t s) {
+  if (sizeof(T) == 2 && cols % BK == 0 && ld % 8 == 0 && (uintptr_t)from % 16 == 0) {
+    *out = (const __bf16 *)from;
+    *out_ld = ld;
+    return hipSuccess;
+  }
+  *out = to;
+  *out_ld = padded;
+  const dim3 grid((padded + 255) / 256, rows < 65535 ? rows : 65535, (rows + 65534) / 65535);
+  k_rows<T, PARTS><<<grid, 256, 0, s>>>(from, ld, rows, cols, to, padded);
+  return hipGetLastError();
+}
+template <typename T, int PARTS>
+hipError_t columns_of(const T *from, long long ld, int rows, int cols, int padded, const float *scale, __bf16 *to, hipStream_t s) {
+  k_columns<T, PARTS><<<dim3((cols + 63) / 64, (padded + 63) / 64), 256, 0, s>>>(from, ld, rows, cols, scale, to, padded);
+  return hipGetLastError();
+}
+
+template <typename T, int PARTS>
+hipError_t loss(const VocabShape &p, const T *h, const T *w, const int *targets, float *loss, float *state, char *work, hipStream_t s) {
+  const Space sp(p, false);
+  Product q = {};
+  q.rows_b = p.rows;
+  q.ksteps = sp.dp / BK;
+  TRY((rows_of<T, PARTS>(h, p.ld_h, p.rows, p.d, sp.dp, (__bf16 *)(work + sp.h), &q.b, &q.ldb, s)));
+  q.part_b = (long long)p.rows * sp.dp;
+  const bool direct = sizeof(T) == 2 && p.d % BK == 0 && p.ld_w % 8 == 0 && (uintptr_t)w % 16 == 0;
+  const int width = direct ? p.vocab : sp.width;
+  LossEpilogue ep = {targets, (float2 *)(work + sp.part), (float *)(work + sp.picked), 0, p.vocab, p.rows};
+  for (long long v = 0; v < p.vocab; v += width) {
+    ep.first = (int)v;
+    q.rows_a = (int)(p.vocab - v < width ? p.vocab - v : width);
+    TRY((rows_of<T, PARTS>(w + v * p.ld_w, p.ld_w, q.rows_a, p.d, sp.dp, (__bf16 *)(work + sp.w), &q.a, &q.lda, s)));
+    q.part_a = (long long)q.rows_a * sp.dp;
+    TRY((product<PARTS>(q, ep, s)));
+  }
+  const int blocks = (p.vocab + 255) / 256 * 2;
+  k_join<<<(p.rows + 3) / 4, 256, 0, s>>>(ep.part, ep.picked, targets, blocks, p.rows, p.vocab, loss, state);
+  return hipGetLastError();
+}
+
+template <typename T, int PARTS>
+hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *targets, const float *state, const float *dloss, T *dh, T *dw,
+                     char *work, hipStream_t s) {
+  const Space sp(p, true);
+  float *scale = (float *)(work + sp.scale), *sum = (float *)(work + sp.sum);
+  __bf16 *ht = (__bf16 *)(work + sp.ht), *wt = (__bf16 *)(work + sp.wt), *gm = (__bf16 *)(work + sp.gm), *gt = (__bf16 *)(work + sp.gt);
+  k_scale<<<1, 1024, 0, s>>>(targets, dloss, p.rows, sp.padded, p.vocab, scale);
+  TRY(hipGetLastError());
+  Product q = {}; // G from w and h
+  q.rows_b = sp.padded;
+  q.ksteps = sp.dp / BK;
+  TRY((rows_of<T, PARTS>(h, p.ld_h, p.rows, p.d, sp.dp, (__bf16 *)(work + sp.h), &q.b, &q.ldb, s)));
+  q.part_b = (long long)p.rows * sp.dp;
+  TRY((columns_of<T, PARTS>(h, p.ld_h, p.rows, p.d, sp.padded, scale, ht, s)));
+  for (long long v = 0; v < p.vocab; v += sp.width) {
+    const int entries = (int)(p.vocab - v < sp.width ? p.vocab - v : sp.width), width = (entries + PAD - 1) / PAD * PAD;
+    TRY((rows_of<T, PARTS>(w + v * p.ld_w, p.ld_w, entries, p.d, sp.dp, (__bf16 *)(work + sp.w), &q.a, &q.lda, s)));
+    q.rows_a = entries;
+    q.rows_b = p.rows;
+    q.part_a = (long long)entries * sp.dp;
+    GradEpilogue<PARTS> ep = {targets, state, scale, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded};
+    TRY((product<PARTS>(q, ep, s)));
+    TRY((columns_of<T, PARTS>(w + v * p.ld_w, p.ld_w, entries, p.d, width, nullptr, wt, s)));
+    Product dhq = {gm, wt, width, width, (long long)sp.padded * width, (long long)p.d * width, p.rows, p.d, width / BK, 0, 0};
+    if (sp.width >= p.vocab) TRY((product<PARTS>(dhq, StoreEpilogue<T>{dh, p.d, p.rows, p.d, false}, s)));
+    else TRY((product<PARTS>(dhq, StoreEpilogue<float>{sum, p.d, p.rows, p.d, v > 0}, s)));
+    Product dwq = {gt, ht, sp.padded, sp.padded, (long long)sp.padded * width, (long long)p.d * sp.padded, entries, p.d, sp.padded / BK, 0, 0};
+    TRY((product<PARTS>(dwq, StoreEpilogue<T>{dw + v * p.d, p.d, entries, p.d, false}, s)));
+  }
+  if (sp.width < p.vocab) {
+    const size_t n = (size_t)p.rows * p.d;
+    k_narrow<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum, dh, n);
+  }
+  return hipGetLastError();
+}
+
+} // namespace
+
+size_t vocab_workspace(const VocabShape &p, bool grad) { return Space(p, grad).bytes; }
+
+hipError_t launch_vocab_loss(const VocabShape &p, const void *h, const void *w, const int *targets, float *loss_, float *state,
+                             void *work, hipStream_t s) {
+  if (!p.rows) return hipSuccess;
+  return p.bf16 ? loss<__bf16, 1>(p, (const __bf16 *)h, (const __bf16 *)w, targets, loss_, state, (char *)work, s)
+                : loss<float, 3>(p, (const float *)h, (const float *)w, targets, loss_, state, (char *)work, s);
+}
+
+hipError_t launch_vocab_grad(const VocabShape &p, const void *h, const void *w, const int *targets, const float *state,
+                             const float *dloss, void *dh, void *dw, void *work, hipStream_t s) {
+  if (!p.rows) {
+    const size_t n = (size_t)p.vocab * p.d * (p.bf16 ? 1 : 2);
+    k_clear<<<(unsigned)(n < (1u << 28) ? (n + 255) / 256 : 1u << 20), 256, 0, s>>>((uint16_t *)dw, n);
+    return hipGetLastError();
+  }
+  return p.bf16 ? gradients<__bf16, 1>(p, (const __bf16 *)h, (const __bf16 *)w, targets, state, dloss, (__bf16 *)dh, (__bf16 *)dw, (char *)work, s)
+                : gradients<float, 3>(p, (const float *)h, (const float *)w, targets, state, dloss, (float *)dh, (float *)dw, (char *)work, s);
+}

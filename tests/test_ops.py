@@ -1,0 +1,597 @@
+"""Operators of token sequence models (snn_glr_*, snn_pack / snn_unpack, snn_vocab_*) against plain implementations in 64 bits on the
+CPU, through the Python binding.  Refusals that need no GPU run everywhere.
+
+Tolerances count roundings.  E32 = 2^-23 covers the two or three roundings and the last-place errors of the hardware's exponential
+and reciprocal that a step makes; results in bf16 are off by half a step, 2^-8 of the value, on top."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+import paper_2412_11810_amd as snn
+from paper_2412_11810_amd import ops
+
+torch = pytest.importorskip("torch")
+gpu = pytest.mark.gpu
+E32 = 2.0 ** -23
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+
+
+# ---- plain implementations ------------------------------------------------------------------------
+def glr_forward(z, x, h0, lengths):
+    T, B, n = z.shape
+    h, state, kept = torch.zeros(T, B, n, dtype=torch.float64), h0.clone(), []
+    for t in range(T):
+        if t % 128 == 0:
+            kept.append(state.clone())
+        on = (t < lengths)[:, None]
+        a = 1 / (1 + torch.exp(-z[t]))
+        new = a * state + x[t] / (1 + torch.exp(z[t]))
+        state = torch.where(on, new, state)
+        h[t] = torch.where(on, new, 0.0)
+    return h, state, torch.stack(kept) if kept else torch.zeros(0, B, n, dtype=torch.float64)
+
+
+def glr_backward(z, x, h0, lengths, dh, dh_last):
+    T, B, n = z.shape
+    before, state = torch.zeros(T, B, n, dtype=torch.float64), h0.clone()
+    a, c = 1 / (1 + torch.exp(-z)), 1 / (1 + torch.exp(z))
+    for t in range(T):
+        before[t] = state
+        state = torch.where((t < lengths)[:, None], a[t] * state + c[t] * x[t], state)
+    dz, dx, g, most = torch.zeros_like(z), torch.zeros_like(z), dh_last.clone(), dh_last.abs().max().item()
+    for t in reversed(range(T)):
+        on = (t < lengths)[:, None]
+        g = torch.where(on, g + dh[t], g)
+        most = max(most, g.abs().max().item())
+        dx[t] = torch.where(on, c[t] * g, 0.0)
+        dz[t] = torch.where(on, a[t] * c[t] * (before[t] - x[t]) * g, 0.0)
+        g = torch.where(on, a[t] * g, g)
+    return dz, dx, g, most
+
+
+def to_bytes(x):
+    """Codes and exponents of rows of numpy floats, block by block."""
+    rows, n = x.shape
+    codes, exps = np.zeros((rows, n), np.int8), np.zeros((rows, -(-n // 32)), np.uint8)
+    for r in range(rows):
+        for b in range(exps.shape[1]):
+            v = x[r, 32 * b:32 * b + 32].astype(np.float64)
+            if not np.all(np.isfinite(v)):
+                exps[r, b] = 255
+            elif np.any(v):
+                k = -126
+                while k < 121 and np.abs(np.round(np.ldexp(v, -k))).max() > 127:
+                    k += 1
+                codes[r, 32 * b:32 * b + 32], exps[r, b] = np.clip(np.round(np.ldexp(v, -k)), -127, 127), k + 127
+    return codes, exps
+
+
+def from_bytes(codes, exps):
+    step = np.where(exps == 255, np.nan, np.where(exps == 0, 0.0, np.ldexp(1.0, exps.astype(int) - 127)))
+    return codes.astype(np.float64) * np.repeat(step, 32, -1)[..., :codes.shape[-1]]
+
+
+def vocab_loss(h, w, target):
+    rows = len(target)
+    logits = h @ w.T
+    on = (target >= 0) & (target < w.shape[0])
+    y = torch.where(on, target, 0)
+    lse = torch.logsumexp(logits, 1)
+    others = logits.clone()
+    others[torch.arange(rows), y] = -math.inf
+    miss = torch.exp(torch.logsumexp(others, 1) - lse)  # 1 - softmax of the target, as a sum
+    loss = torch.where(on, torch.where(miss < 0.5, -torch.log1p(-miss), lse - logits[torch.arange(rows), y]), 0.0)
+    return logits, lse, miss, on, y, loss
+
+
+def vocab_grads(h, w, target, dloss):
+    logits, lse, miss, on, y, _ = vocab_loss(h, w, target)
+    G = torch.exp(logits - lse[:, None])
+    G[torch.arange(len(y)), y] = -miss
+    G = torch.where(on[:, None], G * dloss[:, None], 0.0)
+    return G, G @ w, G.T @ h
+
+
+def near(got, want, tol, what):
+    """|got - want| <= tol + half a step of got's type, everywhere."""
+    got_, want = got.double().cpu(), want.double()
+    assert got_.shape == want.shape, what
+    off = (got_ - want).abs() - (tol + HALF[got.dtype] * want.abs())
+    assert not torch.isnan(off).any() and off.max().item() <= 0 if off.numel() else True, (what, off.max().item())
+
+
+# ---- gated linear recurrence ------------------------------------------------------------------------
+def glr_inputs(T, B, n, dtype, ragged, seed=1, halves=False):
+    g = torch.Generator().manual_seed(seed)
+    z = (2 + 1.5 * torch.randn(T, B, n, generator=g)).clamp(-6, 6).to(dtype)
+    x, dh = torch.randn(T, B, n, generator=g).to(dtype), torch.randn(T, B, n, generator=g).to(dtype)
+    h0, dlast = torch.randn(B, n, generator=g), torch.randn(B, n, generator=g)
+    lengths = torch.randint(0, T + 1, (B,), generator=g, dtype=torch.int32) if ragged else torch.full((B,), T, dtype=torch.int32)
+    if ragged:
+        lengths[0] = T
+        lengths[-1] = 0
+        pad = torch.arange(T)[:, None] >= lengths[None, :]
+        for a in (z, x, dh):
+            a[pad] = math.nan  # nothing may read these
+    if halves:
+        zx = torch.cat([z, x], -1).cuda()
+        return zx[..., :n], zx[..., n:], dh.cuda(), h0.cuda(), dlast.cuda(), lengths.cuda()
+    return z.cuda(), x.cuda(), dh.cuda(), h0.cuda(), dlast.cuda(), lengths.cuda()
+
+
+def bounds(z, x, h0, lengths):
+    """Largest |z|, least b = sigmoid(-z), largest |x| or |h0| of what is read."""
+    live = torch.arange(z.shape[0])[:, None] < lengths[None, :]
+    z, x = z[live], x[live]
+    if not z.numel():
+        return 0.0, 0.5, max(h0.abs().max().item(), 1e-30)
+    return z.abs().max().item(), 1 / (1 + math.exp(z.max().item())), max(x.abs().max().item(), h0.abs().max().item())
+
+
+GLR = [(0, 2, 5, False), (1, 1, 1, False), (1, 64, 130, False), (2, 3, 7, True), (15, 2, 64, False), (16, 3, 66, True), (17, 2, 33, True),
+       (127, 1, 10, False), (128, 2, 128, True), (129, 5, 31, True), (300, 3, 75, True), (1000, 1, 2, False), (300, 33, 1024, False),
+       (700, 1, 12800, False), (260, 64, 1024, True)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,B,n,ragged", GLR)
+def test_glr_forward(T, B, n, ragged, dtype):
+    z, x, _, h0, _, lengths = glr_inputs(T, B, n, dtype, ragged, halves=n % 2 == 1)
+    h, last, kept = snn.snn_glr_forward(z, x, h0, lengths=lengths if ragged else None, keep=True)
+    zc, xc, hc, lc = z.double().cpu(), x.double().cpu(), h0.double().cpu(), lengths.cpu()
+    want = glr_forward(zc, xc, hc, lc)
+    zmax, bmin, M = bounds(zc, xc, hc, lc)
+    # e_t <= (1 - b) e_{t-1} + 2 M E32 (b (|z| + 4) + 1), and the joins of 16-step maps as much again
+    tol = 4 * M * E32 * (zmax + 4 + 1 / bmin)
+    for got, ref, what in zip((h, last, kept), want, ("h", "last", "kept")):
+        near(got, ref, tol, what)
+    if T:
+        near(snn.snn_glr_forward(z, x, None, lengths=lengths if ragged else None)[0], glr_forward(zc, xc, 0 * hc, lc)[0], tol, "from zero")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,B,n,ragged", GLR)
+@pytest.mark.parametrize("packed", [False, True])
+def test_glr_backward(T, B, n, ragged, dtype, packed):
+    z, x, dh, h0, dlast, lengths = glr_inputs(T, B, n, dtype, ragged, seed=2, halves=n % 2 == 1)
+    zc, xc = z.double().cpu(), x.double().cpu()
+    zi, xi = z, x
+    if packed:
+        zi, xi = snn.snn_pack(z), snn.snn_pack(x)
+        zc = torch.from_numpy(from_bytes(zi.codes.cpu().numpy(), zi.exps.cpu().numpy()))
+        xc = torch.from_numpy(from_bytes(xi.codes.cpu().numpy(), xi.exps.cpu().numpy()))
+    hc, dc, lc = h0.double().cpu(), dlast.double().cpu(), lengths.cpu()
+    kept = glr_forward(zc, xc, hc, lc)[2].float().cuda()
+    dhc = dh.double().cpu()
+    wide = torch.full((T, B, 2 * n), 7.0, dtype=dtype, device="cuda")
+    dz, dx, dh0 = snn.snn_glr_backward(zi, xi, kept, dh, dlast, lengths=lengths if ragged else None, dz=wide[..., :n], dx=wide[..., n:])
+    want = glr_backward(zc, xc, hc, lc, dhc, dc)
+    zmax, bmin, M = bounds(zc, xc, hc, lc)
+    G = max(want[3], 1e-30)
+    e_h, e_g = 4 * M * E32 * (zmax + 4 + 1 / bmin), 4 * G * E32 * (zmax + 4 + 1 / bmin)
+    near(dx, want[1], e_g + G * (zmax + 4) * E32, "dx")
+    near(dz, want[0], 0.25 * (2 * M * e_g + G * e_h) + 2 * M * G * (zmax + 6) * E32, "dz")
+    near(dh0, want[2], e_g, "dh0")
+    none = snn.snn_glr_backward(zi, xi, kept, dh, None, lengths=lengths if ragged else None)
+    zero = glr_backward(zc, xc, hc, lc, dhc, 0 * dc)
+    near(none[1], zero[1], e_g + G * (zmax + 4) * E32, "dx without dh_last")
+    near(none[2], zero[2], e_g, "dh0 without dh_last")
+
+
+@gpu
+def test_glr_state_in_place_is_a_sequence_cut_anywhere():
+    z, x, dh, h0, _, _ = glr_inputs(300, 3, 50, torch.float32, False)
+    whole, last, _ = snn.snn_glr_forward(z, x, h0)
+    state = h0.clone()
+    parts = [snn.snn_glr_forward(z[a:b], x[a:b], state, h_last=state)[0] for a, b in ((0, 1), (1, 2), (2, 150), (150, 300))]
+    tol = 4 * 5 * E32 * (10 + 500)  # |x|, |h0| < 5, |z| <= 6: as above
+    near(torch.cat(parts), whole.cpu(), tol, "h")
+    near(state, last.cpu(), tol, "state")
+
+
+@gpu
+def test_glr_long_memory_keeps_its_drive():
+    # gates so near one that 1 - a in 32 bits would be off by 30 %: the state still tends to its drive, 1
+    T = 4096
+    z, x = torch.full((T, 1, 64), 15.0, device="cuda"), torch.ones((T, 1, 64), device="cuda")
+    h = snn.snn_glr_forward(z, x)[0]
+    b = 1 / (1 + math.exp(15.0))
+    want = 1 - (1 - b) ** T
+    # b is off by (15 + 4) E32 of itself, a step's rounding by 2^-24 of h <= want
+    assert abs(h[-1].double().cpu() - want).max().item() <= want * (20 * E32 + T * 2.0 ** -24)
+
+
+@gpu
+def test_glr_saturated_gates_and_values_that_are_not_finite():
+    inf, nan = math.inf, math.nan
+    z = torch.tensor([200.0, -200.0, inf, -inf, nan, 0.0, 0.0], device="cuda").repeat(20, 1, 1)
+    x = torch.tensor([1.0, 3.0, 1.0, 3.0, 1.0, nan, inf], device="cuda").repeat(20, 1, 1)
+    h0 = torch.full((1, 7), 2.0, device="cuda")
+    h, last, kept = snn.snn_glr_forward(z, x, h0, keep=True)
+    assert h[:, 0, :4].cpu().tolist() == [[2.0, 3.0, 2.0, 3.0]] * 20 and torch.isnan(h[1:, 0, 4:]).all()
+    dz, dx, dh0 = snn.snn_glr_backward(z, x, kept, torch.ones_like(z))
+    assert torch.isfinite(dz[:, 0, :4]).all() and torch.isfinite(dx[:, 0, :4]).all()
+    assert dh0[0, :4].cpu().tolist() == [20.0, 0.0, 20.0, 0.0]
+
+
+# ---- 8 bits -------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,n", [(1, 1), (3, 7), (2, 8), (5, 31), (4, 32), (3, 33), (9, 75), (300, 264), (2, 5001)])
+def test_pack_and_unpack(rows, n, dtype):
+    g = torch.Generator().manual_seed(n)
+    x = (torch.randn(rows, n, generator=g) * torch.exp(3 * torch.randn(rows, 1, generator=g))).to(dtype)
+    wide = torch.full((rows, n + 3), math.nan, dtype=dtype)
+    wide[:, 1:n + 1] = x
+    codes, exps = to_bytes(x.float().numpy())
+    for given in (x.cuda(), wide.cuda()[:, 1:n + 1]):
+        p = snn.snn_pack(given)
+        assert np.array_equal(p.codes.cpu().numpy(), codes) and np.array_equal(p.exps.cpu().numpy(), exps)
+    for out in (torch.float32, torch.bfloat16):  # a code has 7 bits: exact in both
+        assert np.array_equal(snn.snn_unpack(p, out).double().cpu().numpy(), from_bytes(codes, exps))
+
+
+@gpu
+def test_pack_borders():
+    top = torch.finfo(torch.float32).max
+    rows = [[0.0] * 40, [127.0, 1.0] * 20, [127.49, -127.4, 0.5, 1.5, 2.5] * 8, [127.5] * 40, [255.0, 1.0] * 20, [top, -top, 1.0, 0.0] * 10,
+            [1e-45, -3e-39] * 20, [2.0 ** -126 * 127] * 40, [2.0 ** -126 * 128, 0.0] * 20, [-0.0] * 40, [math.inf] + [1.0] * 39,
+            [1.0] * 35 + [math.nan] * 5]
+    x = torch.tensor(rows, dtype=torch.float32)
+    codes, exps = to_bytes(x.numpy())
+    p = snn.snn_pack(x.cuda())
+    assert np.array_equal(p.codes.cpu().numpy(), codes) and np.array_equal(p.exps.cpu().numpy(), exps)
+    back = snn.snn_unpack(p).double().cpu().numpy()
+    assert np.array_equal(back, from_bytes(codes, exps), equal_nan=True)
+    assert np.isnan(back[10, :32]).all() and np.isfinite(back[10, 32:]).all() and np.isnan(back[11, 32:]).all()
+    step = np.repeat(np.ldexp(1.0, exps[:10].astype(int) - 127), 32, -1)[:, :40]
+    # the largest float, 2^128 less 2^104, would be 128 of the largest step, 2^121, whose product is no float: 127 of them are less than one step off
+    limit = np.where(np.arange(10) == 5, 1.0, 0.5)[:, None]
+    assert (np.abs(back[:10] - x[:10].double().numpy()) <= limit * step).all()
+
+
+# ---- cross entropy over a vocabulary --------------------------------------------------------------
+def vocab_inputs(rows, d, vocab, dtype, seed=3, spread=3.0):
+    g = torch.Generator().manual_seed(seed)
+    h, w = torch.randn(rows, d, generator=g).to(dtype), (spread / math.sqrt(d) * torch.randn(vocab, d, generator=g)).to(dtype)
+    t = torch.randint(0, vocab, (rows,), generator=g, dtype=torch.int32)
+    t[torch.rand(rows, generator=g) < 0.1] = -1
+    return h, w, t, torch.rand(rows, generator=g) + 0.1
+
+
+def check_vocab(h, w, t, dloss, given_h=None, given_w=None):
+    """Losses and gradients against 64 bits.  A logit is a sum of d (fp32: 6 d) products in some order: off by at most that many roundings of
+    the sum of their magnitudes."""
+    rows, d = h.shape
+    dtype, vocab = h.dtype, w.shape[0]
+    gh, gw, gt = (h.cuda() if given_h is None else given_h), (w.cuda() if given_w is None else given_w), t.cuda()
+    loss, state = snn.snn_vocab_loss(gh, gw, gt)
+    H, W, t64 = h.double(), w.double(), t.long()
+    logits, lse, miss, on, y, want = vocab_loss(H, W, t64)
+    terms = (1 if dtype == torch.bfloat16 else 6) * d + 8
+    e_l = terms * E32 * (H.abs() @ W.abs().T).amax(1) + 4 * E32 * logits.abs().amax(1)  # of each row's logits
+    # a loss moves by no more than its logits do; the sum of vocab exponentials adds vocab roundings of one, at worst
+    count = 64 + vocab / 64  # of the longest chain of additions: 64 in a lane, then one per block
+    near(loss, want, (2 * e_l + count * E32) * torch.where(miss < 0.5, 2 * miss, 1.0) + 8 * E32 * want.abs() + 1e-30, "loss")
+    assert (loss.cpu()[~on] == 0).all()
+    for given in (None, dloss):
+        scale = torch.where(on, 1.0 / max(1, int(on.sum())), 0.0).double() if given is None else given.double()
+        dh, dw = snn.snn_vocab_loss_grad(gh, gw, gt, state, None if given is None else given.cuda())
+        G, want_h, want_w = vocab_grads(H, W, t64, scale)
+        rel = 4 * e_l + (count + 16) * E32 + (2.0 ** -8 if dtype == torch.bfloat16 else 0)  # of an element of G, to itself
+        A = G.abs() * rel[:, None]
+        sums = (1 if dtype == torch.bfloat16 else 6) * E32
+        near(dh, want_h, A @ W.abs() + sums * (vocab + 8) * (G.abs() @ W.abs()) + 1e-30, "dh")
+        near(dw, want_w, A.T @ H.abs() + sums * (rows + 8) * (G.abs().T @ H.abs()) + 1e-30, "dw")
+    return loss, state
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,d,vocab", [(1, 1, 1), (1, 64, 2), (3, 5, 7), (2, 64, 1000), (33, 100, 129), (257, 128, 513), (300, 72, 1025),
+                                          (64, 256, 128), (31, 1000, 300), (600, 320, 2500)])
+def test_vocab(rows, d, vocab, dtype):
+    check_vocab(*vocab_inputs(rows, d, vocab, dtype))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_vocab_in_several_pieces(dtype):
+    check_vocab(*vocab_inputs(66000, 24, 4500, dtype))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 70])
+def test_vocab_rows_of_wider_arrays(d, dtype):
+    h, w, t, dloss = vocab_inputs(100, d, 300, dtype)
+    wide_h, wide_w = torch.full((100, d + 5), math.nan, dtype=dtype), torch.full((300, d + 8), math.nan, dtype=dtype)
+    wide_h[:, 3:3 + d], wide_w[:, 8:] = h, w
+    check_vocab(h, w, t, dloss, wide_h.cuda()[:, 3:3 + d], wide_w.cuda()[:, 8:])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_vocab_nearly_certain_and_hopeless_targets(dtype):
+    # the targets' logits stand out by up to 60 either way: losses from 1e-24 to 60
+    h = torch.eye(64).to(dtype)
+    w = torch.zeros(300, 64).to(dtype)
+    t = torch.arange(64, dtype=torch.int32) * 4
+    for r in range(64):
+        w[4 * r, r] = 60.0 * (r - 31) / 32
+    loss, _ = check_vocab(h, w, t, torch.rand(64) + 0.5)
+    assert 0 < loss[63].item() < 1e-20 and loss[0].item() > 50
+
+
+@gpu
+def test_vocab_without_targets_and_targets_outside():
+    h, w, t, dloss = vocab_inputs(40, 64, 100, torch.bfloat16)
+    t[:] = -1
+    t[::3], t[1::3] = 100, 2 ** 31 - 1
+    loss, state = snn.snn_vocab_loss(h.cuda(), w.cuda(), t.cuda())
+    dh, dw = snn.snn_vocab_loss_grad(h.cuda(), w.cuda(), t.cuda(), state)
+    assert not loss.any() and not dh.any() and not dw.any()
+    h[5] = math.nan  # a row that has no target takes no part, whatever it holds
+    t[0] = 3
+    loss, state = snn.snn_vocab_loss(h.cuda(), w.cuda(), t.cuda())
+    dh, dw = snn.snn_vocab_loss_grad(h.cuda(), w.cuda(), t.cuda(), state)
+    assert loss[0] > 0 and not loss[1:].any() and dh[0].any() and not dh[1:].any() and torch.isfinite(dw).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_vocab_no_rows(dtype):
+    h, w, t = torch.zeros(0, 8, dtype=dtype, device="cuda"), torch.ones(5, 8, dtype=dtype, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")
+    loss, state = snn.snn_vocab_loss(h, w, t)
+    dh, dw = snn.snn_vocab_loss_grad(h, w, t, state)
+    assert loss.numel() == 0 and dh.shape == (0, 8) and dw.shape == (5, 8) and not dw.any()
+
+
+@gpu
+def test_vocab_values_that_are_not_finite_show():
+    h, w, t, _ = vocab_inputs(300, 64, 700, torch.float32)
+    t[:] = torch.arange(300, dtype=torch.int32)
+    h[7] = math.inf
+    h[9, 3] = math.nan
+    loss, state = snn.snn_vocab_loss(h.cuda(), w.cuda(), t.cuda())
+    dh, dw = snn.snn_vocab_loss_grad(h.cuda(), w.cuda(), t.cuda(), state)
+    bad = torch.zeros(300, dtype=torch.bool)
+    bad[[7, 9]] = True
+    assert torch.equal(torch.isnan(loss).cpu(), bad) and torch.equal(torch.isnan(dh).all(1).cpu(), bad)
+    assert torch.isfinite(dh.cpu()[~bad]).all() and torch.isnan(dw).any(1).all()
+
+
+# ---- together ---------------------------------------------------------------------------------
+def model_loss(p, tokens, targets, h0):
+    """Losses of a one-layer model in 64 bits: an embedding, gate and drive by one projection, the recurrence, the vocabulary again."""
+    zx = p["embed"][tokens] @ p["project"].T
+    n = zx.shape[-1] // 2
+    state, h = h0, []
+    for t in range(zx.shape[0]):
+        state = state + torch.sigmoid(-zx[t, :, :n]) * (zx[t, :, n:] - state)
+        h.append(state)
+    logits = torch.stack(h).flatten(0, 1) @ p["embed"].T
+    return torch.nn.functional.cross_entropy(logits, targets.flatten(), ignore_index=-1)
+
+
+@gpu
+@pytest.mark.parametrize("packed", [False, True])
+def test_a_training_step_of_a_model(packed):
+    """Gradients of an embedding that is also the readout, and of the projection between, against autograd in 64 bits and against differences."""
+    T, B, n, vocab = 150, 3, 48, 333
+    g = torch.Generator().manual_seed(5)
+    p64 = {"embed": torch.randn(vocab, n, generator=g, dtype=torch.float64) * 0.5,
+           "project": torch.randn(2 * n, n, generator=g, dtype=torch.float64) * 0.3}
+    p64 = {k: v.float().double().requires_grad_() for k, v in p64.items()}
+    tokens, targets = torch.randint(0, vocab, (T, B), generator=g), torch.randint(-1, vocab, (T, B), generator=g)
+    h0 = torch.randn(B, n, generator=g, dtype=torch.float64).float().double()
+    want = model_loss(p64, tokens, targets, h0)
+    want.backward()
+
+    embed, project = (p64[k].detach().float().cuda() for k in ("embed", "project"))
+    tk, tg = tokens.cuda(), targets.to(torch.int32).cuda().flatten()
+    e = embed[tk]
+    zx = (e.flatten(0, 1) @ project.T).view(T, B, 2 * n)
+    h, _, kept = snn.snn_glr_forward(zx[..., :n], zx[..., n:], h0.float().cuda(), keep=True)
+    saved = (snn.snn_pack(zx[..., :n]), snn.snn_pack(zx[..., n:])) if packed else (zx[..., :n], zx[..., n:])
+    loss, state = snn.snn_vocab_loss(h.flatten(0, 1), embed, tg)
+    dh, d_embed = snn.snn_vocab_loss_grad(h.flatten(0, 1), embed, tg, state)
+    dzx = torch.empty_like(zx)
+    snn.snn_glr_backward(*saved, kept, dh.view(T, B, n), dz=dzx[..., :n], dx=dzx[..., n:])
+    flat = dzx.flatten(0, 1)
+    d_project = flat.T @ e.flatten(0, 1)
+    d_embed = d_embed.index_add(0, tk.flatten(), flat @ project)
+    mean = loss.sum() / (tg >= 0).sum()
+    assert abs(mean.item() - want.item()) < 1e-5 * want.item()
+    # in 32 bits the sums of up to 450 terms are off by 1e-5 of the largest gradient at most; 8 bits move z and x by 2^-7 of
+    # a block's largest, 4 here, hence a gradient by a few hundredths of the largest
+    tol = 0.05 if packed else 1e-5
+    for got, k in ((d_embed, "embed"), (d_project, "project")):
+        ref = p64[k].grad
+        assert (got.double().cpu() - ref).abs().max() <= tol * ref.abs().max(), k
+        direction = torch.randn(ref.shape, generator=g, dtype=torch.float64)
+        with torch.no_grad():
+            ends = [model_loss({**p64, k: p64[k] + s * direction}, tokens, targets, h0) for s in (1e-5, -1e-5)]
+        slope = ((ends[0] - ends[1]) / 2e-5).item()
+        assert abs((got.double().cpu() * direction).sum().item() - slope) <= tol * (ref.abs().max() * direction.abs().sum()).item() + 1e-6
+
+
+# ---- calls ------------------------------------------------------------------------------------
+def every_operator(seed=7):
+    """A function that runs every operator once, and its inputs."""
+    z, x, dh, h0, dlast, lengths = glr_inputs(400, 3, 70, torch.bfloat16, True, seed=seed)
+    live = torch.arange(400, device="cuda")[:, None] < lengths[None, :]
+    z, x, dh = (torch.where(live[..., None], a, 0.0) for a in (z, x, dh))
+    h, w, t, dloss = (a.cuda() for a in vocab_inputs(200, 96, 1500, torch.float32, seed=seed))
+
+    def run():
+        out, last, kept = snn.snn_glr_forward(z, x, h0, lengths=lengths, keep=True)
+        pz, px = snn.snn_pack(z), snn.snn_pack(x)
+        loss, state = snn.snn_vocab_loss(h, w, t)
+        return [out, last, kept, *snn.snn_glr_backward(z, x, kept, dh, dlast, lengths=lengths),
+                *snn.snn_glr_backward(pz, px, kept, dh, dlast, lengths=lengths), snn.snn_unpack(pz), loss, state,
+                *snn.snn_vocab_loss_grad(h, w, t, state, dloss)]
+    return run, [z, x, dh, h0, dlast, h, w, dloss]
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b)) and len(a) == len(b)
+
+
+@gpu
+def test_calls_on_other_streams_give_the_same_bits():
+    run, _ = every_operator()
+    other, _ = every_operator(seed=8)
+    want, want_other = run(), other()
+    assert same(run(), want)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(3):  # both at once
+        for s, f, to in zip(streams, (run, other), got):
+            with torch.cuda.stream(s):
+                to.append(f())
+    torch.cuda.synchronize()
+    assert all(same(a, want) for a in got[0]) and all(same(a, want_other) for a in got[1])
+
+
+@gpu
+def test_calls_in_a_graph():
+    run, inputs = every_operator()
+    want = run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for _ in range(3):
+        for o in got:
+            o.fill_(-1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(got, want)
+        inputs[0].mul_(0.5)  # other values in the same arrays
+        want = run()
+        torch.cuda.synchronize()
+
+
+# ---- refusals -----------------------------------------------------------------------------------
+def refused(call, text):
+    with pytest.raises(snn.SnnError) as e:
+        call()
+    assert e.value.status == snn.SNN_E_INVAL and text in str(e.value), str(e.value)
+
+
+def test_c_entry_points_refuse_what_they_cannot_run():
+    """No GPU needed: shapes and pointers are looked at before anything else happens."""
+    L, at = snn.lib(), ops.snn_launch(0, None, None, 0)
+    here = C.cast(C.create_string_buffer(4096), C.c_void_p).value
+
+    def glr(**k):
+        p = dict(T=10, batch=2, n=8, dtype=0)
+        return C.byref(ops.snn_glr(**{**p, **k}))
+
+    def forward(p, launch=C.byref(at), z=here):
+        ops._run("snn_glr_forward", launch, p, z, here, None, here, None, None)
+
+    refused(lambda: forward(glr(), None), "no device")
+    refused(lambda: forward(None), "no shape")
+    refused(lambda: forward(glr(dtype=7)), "unknown type 7")
+    refused(lambda: forward(glr(T=-1)), "T = -1")
+    refused(lambda: forward(glr(batch=0)), "batch 0")
+    refused(lambda: forward(glr(batch=1 << 16, n=1 << 16)), "channels")
+    refused(lambda: forward(glr(ld_z=7)), "7 elements")
+    refused(lambda: forward(glr(ld_dx=-8)), "-8 elements")
+    refused(lambda: forward(glr(ld_h=1 << 40)), "at most")
+    refused(lambda: forward(glr(), z=None), "z is NULL")
+    refused(lambda: forward(glr(), z=here + 1), "z is not aligned")
+    refused(lambda: forward(glr()), "not in device memory" if not torch.cuda.is_available() else "not in")
+    assert L.snn_glr_workspace(glr(n=0)) == 0 and L.snn_glr_workspace(glr()) == 0 and L.snn_glr_workspace(glr(T=4096)) > 0
+    packed = ops.snn_packed(here, here, 0, 0)
+
+    def backward_packed(p, z=packed):
+        ops._run("snn_glr_backward_packed", C.byref(at), p, C.byref(z) if z else None, C.byref(packed), *[here] * 6)
+
+    refused(lambda: backward_packed(glr(), None), "without codes")
+    refused(lambda: backward_packed(glr(), ops.snn_packed(here, None, 0, 0)), "without codes")
+    refused(lambda: backward_packed(glr(), ops.snn_packed(here, here, 7, 0)), "7 codes")
+    refused(lambda: backward_packed(glr(n=33), ops.snn_packed(here, here, 0, 1)), "1 codes or exponents")
+    refused(lambda: backward_packed(glr(n=-5)), "n -5")
+    for name in ("snn_pack", "snn_unpack"):
+        def pack(dtype=0, rows=2, cols=8, ld=0, x=here):
+            ops._run(name, C.byref(at), dtype, rows, cols, ld, x, here, here)
+        refused(lambda: pack(dtype=2), "unknown type")
+        refused(lambda: pack(rows=-1), "rows")
+        refused(lambda: pack(cols=0), "rows of 0")
+        refused(lambda: pack(rows=1 << 30, cols=1 << 30), "rows of")
+        refused(lambda: pack(ld=7), "fewer")
+        refused(lambda: pack(), "not in")
+
+    def vocab(**k):
+        return C.byref(ops.snn_vocab(**{**dict(rows=4, d=8, vocab=10, dtype=0), **k}))
+
+    def loss(p):
+        ops._run("snn_vocab_loss", C.byref(at), p, *[here] * 5)
+
+    refused(lambda: loss(None), "no shape")
+    refused(lambda: loss(vocab(dtype=-1)), "unknown type")
+    for bad in (dict(rows=-1), dict(d=0), dict(vocab=0), dict(rows=1 << 23), dict(d=1 << 17), dict(vocab=1 << 25)):
+        refused(lambda: loss(vocab(**bad)), "2^22")
+    refused(lambda: loss(vocab(ld_w=7)), "7 elements")
+    refused(lambda: loss(vocab()), "not in")
+    assert L.snn_vocab_workspace(vocab(vocab=0), 0) == 0 and L.snn_vocab_workspace(vocab(), 1) > L.snn_vocab_workspace(vocab(), 0) > 0
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    f = torch.zeros
+    for call, kind in (
+            (lambda: snn.snn_glr_forward(f(4, 2, 3), f(4, 2, 3)), ValueError),                          # on the CPU
+            (lambda: snn.snn_glr_forward(f(4, 3), f(4, 3)), ValueError),
+            (lambda: snn.snn_glr_forward(f(4, 2, 3, dtype=torch.float64), f(4, 2, 3, dtype=torch.float64)), TypeError),
+            (lambda: snn.snn_glr_forward(f(4, 2, 3), f(4, 2, 3, dtype=torch.bfloat16)), TypeError),
+            (lambda: snn.snn_glr_forward(f(4, 2, 3), f(4, 2, 4)), ValueError),
+            (lambda: snn.snn_glr_forward(f(4, 2, 3), f(4, 3, 2).mT), ValueError),
+            (lambda: snn.snn_glr_forward(f(4, 1, 3).expand(4, 2, 3), f(4, 2, 3)), ValueError),
+            (lambda: snn.snn_glr_forward(f(2, 4, 3).transpose(0, 1), f(4, 2, 3)), ValueError),
+            (lambda: snn.snn_glr_forward(f(4, 2, 3), f(4, 2, 3), f(2, 3, dtype=torch.bfloat16)), TypeError),
+            (lambda: snn.snn_glr_forward(f(4, 2, 3), f(4, 2, 3), lengths=f(2, dtype=torch.int64)), TypeError),
+            (lambda: snn.snn_glr_backward(f(4, 2, 3), f(4, 2, 3), f(2, 2, 3), f(4, 2, 3)), ValueError),
+            (lambda: snn.snn_glr_backward(snn.Packed(f(4, 2, 3), f(4, 2, 1)), f(4, 2, 3), f(1, 2, 3), f(4, 2, 3)), TypeError),
+            (lambda: snn.snn_pack(f(())), ValueError),
+            (lambda: snn.snn_pack(f(4, 0)), ValueError),
+            (lambda: snn.snn_pack(f(4, 3, dtype=torch.int32)), TypeError),
+            (lambda: snn.snn_pack(f(4, 8)[:, ::2]), ValueError),
+            (lambda: snn.snn_unpack(snn.Packed(f(4, 33, dtype=torch.int8), f(4, 1, dtype=torch.uint8))), ValueError),
+            (lambda: snn.snn_vocab_loss(f(4, 3), f(5, 4), f(4, dtype=torch.int32)), ValueError),
+            (lambda: snn.snn_vocab_loss(f(4, 3), f(5, 3), f(4, dtype=torch.int64)), TypeError),
+            (lambda: snn.snn_vocab_loss(f(4, 3), f(5, 3), f(3, dtype=torch.int32)), ValueError),
+            (lambda: snn.snn_vocab_loss_grad(f(4, 3), f(5, 3), f(4, dtype=torch.int32), f(4, 2)), ValueError)):
+        with pytest.raises(kind):
+            call()
+
+
+@gpu
+def test_workspaces_and_host_arrays_are_checked():
+    z = torch.zeros(1000, 1, 64, device="cuda")
+    p = ops.snn_glr(1000, 1, 64, 0, 0, 0, 0, 0, 0, None)
+    need = snn.lib().snn_glr_workspace(C.byref(p))
+    assert need > 0
+    space = torch.empty(need + 512, dtype=torch.uint8, device="cuda")
+    args = [z.data_ptr(), z.data_ptr(), None, torch.empty_like(z).data_ptr(), None, None]
+
+    def call(work, size, device=0, arrays=args):
+        ops._run("snn_glr_forward", C.byref(ops.snn_launch(device, None, work, size)), C.byref(p), *arrays)
+
+    call(space.data_ptr(), need)
+    torch.cuda.synchronize()
+    refused(lambda: call(space.data_ptr(), need - 1), f"{need} are needed")
+    refused(lambda: call(None, need), "workspace has 0")
+    refused(lambda: call(space.data_ptr() + 4, need), "aligned")
+    refused(lambda: call(space.data_ptr(), need, device=1), "device 1")
+    host = torch.zeros(1000, 1, 64)
+    refused(lambda: call(space.data_ptr(), need, arrays=[host.data_ptr(), *args[1:]]), "z is not in")
+    pinned = torch.zeros(1000, 1, 64, pin_memory=True)
+    refused(lambda: call(space.data_ptr(), need, arrays=[pinned.data_ptr(), *args[1:]]), "z is not in")
