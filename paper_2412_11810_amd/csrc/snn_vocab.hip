@@ -29,7 +29,7 @@ struct Product {
   const __bf16 *a, *b;
   long long lda, ldb, part_a, part_b; // elements from row to row, from part to part
   int rows_a, rows_b, ksteps;
-  int tiles_a, tiles_b;
+  int tiles_a, tiles_b, slices, slice_steps; // slices along the sums: blockIdx.y, slice_steps * 64 elements each
 };
 
 __device__ __forceinline__ void load_lds(const char *base, unsigned off, char *lds) {
@@ -38,12 +38,24 @@ __device__ __forceinline__ void load_lds(const char *base, unsigned off, char *l
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)lds, 16, (int)off, 0, 0, 0);
 }
 
-// One tile of BM rows of A by BN rows of B by eight wavefronts, two along A and four along B.  A row's 64 elements are eight
+// What an epilogue has of LDS for its wavefront, to turn accumulators into rows that leave in whole lines.  A wavefront's accesses to LDS are
+// in order, so that turn() only has to keep the compiler from changing that.
+struct Stage {
+  char *first, *second; // 4 KB each
+  int lane, r, half;
+  static __device__ __forceinline__ void turn() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+  }
+};
+
+// One tile of BM rows of A by BN rows of B by eight wavefronts, WA along A and WB along B.  A row's 64 elements are eight
 // 16-byte chunks in LDS; chunk c of row r is at place c ^ (r % 8), so that the lanes of a fragment, which read one chunk of
 // 32 rows, use all banks.  Loads go past the registers; the next 64 elements arrive while these are multiplied.
-template <int BM, int BN, int PARTS, class Epilogue>
+template <int BM, int BN, int WA, int WB, int PARTS, class Epilogue>
 __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
-  constexpr int MI = BM / 64, NI = BN / 128, LA = BM / 64, LB = BN / 64;
+  constexpr int MI = BM / WA / 32, NI = BN / WB / 32, LA = BM / 64, LB = BN / 64;
   __shared__ __align__(16) char a0[BM * 128], b0[BN * 128], a1[BM * 128], b1[BN * 128];
   // tiles in the order of the dies: consecutive workgroups are on different ones, each die takes a run of tiles, in groups of eight
   // along A that share the rows of B
@@ -54,7 +66,7 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
   const int ta = first + in % wide, tb = in / wide;
 
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wa = w >> 2, wb = w & 3;
+  const int wa = w / WB, wb = w % WB;
   const char *base_a = (const char *)(p.a + (long long)ta * BM * p.lda), *base_b = (const char *)(p.b + (long long)tb * BN * p.ldb);
   unsigned off_a[LA], off_b[LB];
   const int row8 = w * 8 + (lane >> 3), chunk = (lane & 7) ^ (lane >> 3);
@@ -64,7 +76,8 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
   for (int i = 0; i < LB; ++i) off_b[i] = (unsigned)min(i * 64 + row8, p.rows_b - 1 - tb * BN) * (unsigned)(p.ldb * 2) + chunk * 16;
 
   tile32 acc[MI][NI] = {};
-  int k = 0, seg = 0;
+  const int slice = blockIdx.y, k_first = slice * p.slice_steps, k_end = min(k_first + p.slice_steps, p.ksteps);
+  int k = k_first, seg = 0;
   constexpr int SEGS = PARTS == 1 ? 1 : 6;
   auto fetch = [&](char *la, char *lb) {
     // parts of A 0 1 2 0 1 0 with parts of B 2 1 0 1 0 0: the smallest products first
@@ -74,7 +87,7 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
     for (int i = 0; i < LA; ++i) load_lds(ga, off_a[i], la + (i * 64 + w * 8) * 128);
 #pragma unroll
     for (int i = 0; i < LB; ++i) load_lds(gb, off_b[i], lb + (i * 64 + w * 8) * 128);
-    if (++k == p.ksteps) { k = 0; ++seg; }
+    if (++k == k_end) { k = k_first; ++seg; }
   };
   const int r = lane & 31, half = lane >> 5;
   auto multiply = [&](const char *la, const char *lb) {
@@ -83,9 +96,9 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
       frag fa[MI], fb[NI];
       const int place = ((2 * s + half) ^ (r & 7)) * 16;
 #pragma unroll
-      for (int i = 0; i < MI; ++i) fa[i] = *(const frag *)(la + (wa * (BM / 2) + i * 32 + r) * 128 + place);
+      for (int i = 0; i < MI; ++i) fa[i] = *(const frag *)(la + (wa * (BM / WA) + i * 32 + r) * 128 + place);
 #pragma unroll
-      for (int i = 0; i < NI; ++i) fb[i] = *(const frag *)(lb + (wb * (BN / 4) + i * 32 + r) * 128 + place);
+      for (int i = 0; i < NI; ++i) fb[i] = *(const frag *)(lb + (wb * (BN / WB) + i * 32 + r) * 128 + place);
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -96,30 +109,27 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
     __builtin_amdgcn_s_waitcnt(0x0f70); // every load of this wavefront, then those of the others
     __syncthreads();
   };
-  const int steps = p.ksteps * SEGS;
   fetch(a0, b0);
   arrived();
-  for (int it = 0; it < steps; it += 2) {
-    if (it + 1 < steps) fetch(a1, b1);
+  int left = (k_end - k_first) * SEGS;
+  for (; left > 2; left -= 2) {
+    fetch(a1, b1);
     multiply(a0, b0);
     arrived();
-    if (it + 1 == steps) break;
-    if (it + 2 < steps) fetch(a0, b0);
+    fetch(a0, b0);
     multiply(a1, b1);
     arrived();
   }
-  // element e of a tile: row 8 (e / 4) + 4 half + e % 4 of A, row r of B
-  ep.template finish<BM, BN, MI, NI>(acc, ta * BM + wa * (BM / 2), tb * BN + wb * (BN / 4), r, half);
-}
-
-// x in parts of 8 bits each, cut off and not rounded: what is left is exact, and the third part has the last bits of 24
-template <int PARTS, int N = 1> __device__ __forceinline__ void split(float x, uint16_t (&part)[PARTS][N], int e = 0) {
-#pragma unroll
-  for (int k = 0; k < PARTS; ++k) {
-    const uint32_t bits = __float_as_uint(x) & 0xffff0000u;
-    part[k][e] = (uint16_t)(bits >> 16);
-    x -= __uint_as_float(bits);
+  if (left == 2) fetch(a1, b1);
+  multiply(a0, b0);
+  arrived();
+  if (left == 2) {
+    multiply(a1, b1);
+    arrived();
   }
+  // element e of a tile: row 8 (e / 4) + 4 half + e % 4 of A, row r of B.  Every wavefront is through with LDS: 4 KB each, twice
+  const Stage stage = {(BM >= BN ? a0 : b0) + w * 4096, (BM >= BN ? a1 : b1) + w * 4096, lane, r, half};
+  ep.template finish<MI, NI>(acc, ta * BM + wa * (BM / WA), tb * BN + wb * (BN / WB), slice, stage);
 }
 
 // Row m's target, counted from entry v0 on; -1: none, or one before v0
@@ -131,13 +141,13 @@ __device__ __forceinline__ int entry(const int *targets, int m, bool on, int voc
 // Logits, A = vocabulary (a piece of it from `first` on), B = rows of h.  A lane has the logits of one row with 16 MI entries of the
 // vocabulary: their maximum and sum, the target left out, and the target's logit go to memory.
 struct LossEpilogue {
+  static constexpr bool LOGITS = true;
   const int *targets;
-  float2 *part;  // [blocks of BM / 2 entries][rows]
+  float2 *part;  // [blocks of 32 MI entries][rows]
   float *picked; // [rows]: the target's logit
   int first, vocab, rows;
-  template <int BM, int BN, int MI, int NI>
-  __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int v0, int m0, int r, int half) const {
-    const int block = (first + v0) / (BM / 2);
+  template <int MI, int NI> __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int v0, int m0, int, const Stage &st) const {
+    const int r = st.r, half = st.half, block = (first + v0) / (32 * MI);
     v0 += first + 4 * half;
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
@@ -173,14 +183,14 @@ struct LossEpilogue {
 
 // The same logits again, turned into G: as rows of h by entries of the vocabulary (gm) and the other way round (gt), in parts.
 template <int PARTS> struct GradEpilogue {
+  static constexpr bool LOGITS = true;
   const int *targets;
   const float *state, *scale; // scale [rows padded]: dloss, 0 for rows without a target
   __bf16 *gm, *gt;            // [PARTS][rows padded][width], [PARTS][width][rows padded]
   int first, vocab, rows, width, padded;
-  template <int BM, int BN, int MI, int NI>
-  __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int v0, int m0, int r, int half) const {
-    // (scalar addresses; what depends on the lane is one offset for each array)
-    const unsigned lane_m = (unsigned)(r * width + 4 * half) * 2, lane_t = (unsigned)(4 * half * padded + r) * 2;
+  template <int MI, int NI> __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int v0, int m0, int, const Stage &st) const {
+    static_assert(NI == 2, "a wavefront has 64 rows of h");
+    const int r = st.r, half = st.half, lane = st.lane;
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int m = m0 + j * 32 + r;
@@ -192,77 +202,164 @@ template <int PARTS> struct GradEpilogue {
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int vq = 32 * i + 8 * q;
-          uint16_t parts[PARTS][4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = __builtin_amdgcn_exp2f((acc[i][j][4 * q + e] - top) * LOG2E) * per;
-            if (vq + e == y) x = -miss * g;
-            if (none || vq + e >= left) x = 0.f;
-            if constexpr (PARTS == 1) parts[0][e] = __builtin_bit_cast(uint16_t, (__bf16)x);
-            else split(x, parts, e);
-          }
-#pragma unroll
-          for (int k = 0; k < PARTS; ++k) {
-            uint2 four;
-            four.x = parts[k][0] | (uint32_t)parts[k][1] << 16;
-            four.y = parts[k][2] | (uint32_t)parts[k][3] << 16;
-            *(uint2 *)((char *)(gm + ((size_t)k * padded + m0 + j * 32) * width + v0 + vq) + lane_m) = four;
-            char *const t = (char *)(gt + ((size_t)k * width + v0 + vq) * padded + m0 + j * 32);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) *(uint16_t *)(t + (size_t)e * padded * 2 + lane_t) = parts[k][e];
-          }
+        for (int e = 0; e < 16; ++e) {
+          const int v = 32 * i + 8 * (e >> 2) + (e & 3);
+          float x = __builtin_amdgcn_exp2f((acc[i][j][e] - top) * LOG2E) * per;
+          if (v == y) x = -miss * g;
+          acc[i][j][e] = none || v >= left ? 0.f : x;
         }
     }
+    // 32 entries by 64 rows at a time.  first: [64 rows][32 entries], second: [32 entries][64 rows] (16-byte chunks at places that are
+    // exchanged by the row, so that a wavefront's writes use all banks)
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        Stage::turn();
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            uint16_t b[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float x = acc[i][j][4 * q + e];
+              if constexpr (PARTS == 1) b[e] = __builtin_bit_cast(uint16_t, (__bf16)x);
+              else {
+                const uint32_t bits = __float_as_uint(x) & 0xffff0000u;
+                b[e] = (uint16_t)(bits >> 16);
+                acc[i][j][4 * q + e] = x - __uint_as_float(bits);
+              }
+              const int v = 8 * q + 4 * half + e;
+              *(uint16_t *)(st.second + v * 128 + (((j * 4 + (r >> 3)) ^ (v & 7)) * 16) + (r & 7) * 2) = b[e];
+            }
+            uint2 four;
+            four.x = b[0] | (uint32_t)b[1] << 16;
+            four.y = b[2] | (uint32_t)b[3] << 16;
+            *(uint2 *)(st.first + (j * 32 + r) * 64 + ((q ^ ((r >> 1) & 3)) * 16) + half * 8) = four;
+          }
+        Stage::turn();
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const int m = n * 16 + (lane >> 2), v = n * 8 + (lane >> 3);
+          const uint4 of_m = *(const uint4 *)(st.first + m * 64 + (((lane & 3) ^ ((m >> 1) & 3)) * 16));
+          const uint4 of_v = *(const uint4 *)(st.second + v * 128 + (((lane & 7) ^ (v & 7)) * 16));
+          *(uint4 *)(gm + ((size_t)k * padded + m0 + m) * width + v0 + 32 * i + (lane & 3) * 8) = of_m;
+          *(uint4 *)(gt + ((size_t)k * width + v0 + 32 * i + v) * padded + m0 + (lane & 7) * 8) = of_v;
+        }
+      }
   }
 };
 
-// C itself, [rows_a][rows_b] with ld elements per row, as T; or added to a sum in 32 bits (add: not the first part of it).
+// C as T, [rows_a][rows_b] with ld elements per row; or in 32 bits, a slice each, added to what is there (add: it is not the first).
+// Rows may begin at any element.
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef words4 words4_any __attribute__((aligned(4)));
+typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+typedef words2 words2_any __attribute__((aligned(2)));
 template <typename T> struct StoreEpilogue {
+  static constexpr bool LOGITS = false;
   T *out;
-  long long ld;
+  long long ld, per_slice;
   int rows_a, rows_b;
   bool add;
-  template <int BM, int BN, int MI, int NI>
-  __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int ra, int rb, int r, int half) const {
-    const unsigned lane = (unsigned)(4 * half * ld + r) * sizeof(T);
-    const int left = rows_a - ra - 4 * half;
+  template <int MI, int NI> __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int ra, int rb, int slice, const Stage &st) const {
+    constexpr int COLS = 32 * NI, LANES = COLS / 4, ROWS = 64 / LANES; // four columns per lane, ROWS rows at once
+    T *const to = out + slice * per_slice;
+    const int c = rb + st.lane % LANES * 4;
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
-      if (rb + j * 32 + r < rows_b)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+      for (int part = 0; part < 2; ++part) { // 16 rows
+        Stage::turn();
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int a = 32 * i + 8 * (e >> 2) + (e & 3);
-            T *const to = (T *)((char *)(out + (ra + a) * ld + rb + j * 32) + lane);
-            if (a < left) {
-              if constexpr (sizeof(T) == 4) *to = add ? *to + acc[i][j][e] : acc[i][j][e];
-              else *to = (T)acc[i][j][e];
-            }
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            *(float *)(st.first + ((8 * (e >> 2) + 4 * st.half + (e & 3)) * COLS + j * 32 + st.r) * 4) = acc[i][j][8 * part + e];
+        Stage::turn();
+#pragma unroll
+        for (int n = 0; n < 16 / ROWS; ++n) {
+          const int row = n * ROWS + st.lane / LANES, a = ra + 32 * i + 16 * part + row;
+          float4 v = *(const float4 *)(st.first + row * COLS * 4 + st.lane % LANES * 16);
+          if (a >= rows_a) continue;
+          T *const at = to + a * ld + c;
+          if (c + 4 <= rows_b) {
+            if constexpr (sizeof(T) == 4) {
+              if (add) {
+                const words4 was = *(const words4_any *)at;
+                v.x += __uint_as_float(was[0]);
+                v.y += __uint_as_float(was[1]);
+                v.z += __uint_as_float(was[2]);
+                v.w += __uint_as_float(was[3]);
+              }
+              *(words4_any *)at = words4{__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
+            } else
+              *(words2_any *)at = words2{__builtin_bit_cast(uint16_t, (T)v.x) | (uint32_t)__builtin_bit_cast(uint16_t, (T)v.y) << 16,
+                                         __builtin_bit_cast(uint16_t, (T)v.z) | (uint32_t)__builtin_bit_cast(uint16_t, (T)v.w) << 16};
+          } else {
+            const float u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (c + x < rows_b) {
+                if (sizeof(T) == 4 && add) at[x] = (T)((float)at[x] + u[x]);
+                else at[x] = (T)u[x];
+              }
           }
+        }
+      }
   }
 };
 
+// Tiles: 256 by 256, or 64 along a side that has no more than 64 rows (the epilogues that work on logits: along that of h only).
+bool few(int rows) { return rows <= 64; }
+int tiles(int rows_a, int rows_b) { return (few(rows_a) ? 1 : (rows_a + 255) / 256) * (few(rows_b) ? 1 : (rows_b + 255) / 256); }
 template <int PARTS, class Epilogue> hipError_t product(Product p, const Epilogue &ep, hipStream_t s) {
-  constexpr int B = 256;
-  p.tiles_a = (p.rows_a + B - 1) / B;
-  p.tiles_b = (p.rows_b + B - 1) / B;
-  k_product<B, B, PARTS, Epilogue><<<p.tiles_a * p.tiles_b, 512, 0, s>>>(p, ep);
+  const bool few_a = few(p.rows_a) && !Epilogue::LOGITS, few_b = few(p.rows_b) && !few_a;
+  p.tiles_a = few_a ? 1 : (p.rows_a + 255) / 256;
+  p.tiles_b = few_b ? 1 : (p.rows_b + 255) / 256;
+  if (!p.slices) {
+    p.slices = 1;
+    p.slice_steps = p.ksteps;
+  }
+  const dim3 grid(p.tiles_a * p.tiles_b, p.slices);
+  if (few_b) k_product<256, 64, 8, 1, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  else if (!few_a) k_product<256, 256, 2, 4, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  else if constexpr (!Epilogue::LOGITS) k_product<64, 256, 1, 8, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
   return hipGetLastError();
 }
 
+// A product with fewer tiles than half the compute units is cut along its sums, eight steps of 64 or more each; the slices are added up
+// afterwards, in order.
+struct Slices {
+  int count, steps;
+  Slices(int rows_a, int rows_b, int ksteps, int at_most = 256) {
+    const int most = 256 / tiles(rows_a, rows_b), fit = ksteps / 8, n = most < fit ? most : fit;
+    count = n < 1 ? 1 : n < at_most ? n : at_most;
+    steps = (ksteps + count - 1) / count;
+    count = (ksteps + steps - 1) / steps;
+  }
+};
+
 // ---- operands -------------------------------------------------------------------------------
+// x in parts of 8 bits each, cut off and not rounded: what is left is exact, and the third part has the last bits of 24
+template <int PARTS> __device__ __forceinline__ void split(float x, uint16_t (&part)[PARTS]) {
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    const uint32_t bits = __float_as_uint(x) & 0xffff0000u;
+    part[k] = (uint16_t)(bits >> 16);
+    x -= __uint_as_float(bits);
+  }
+}
 // to[part][row][padded cols] = parts of from[row][cols]; zeros behind a row's end
 template <typename T, int PARTS>
 __global__ __launch_bounds__(256) void k_rows(const T *from, long long ld, int rows, int cols, __bf16 *to, int padded) {
   const int c = blockIdx.x * 256 + threadIdx.x, r = blockIdx.y + blockIdx.z * 65535;
   if (c >= padded || r >= rows) return;
-  uint16_t part[PARTS][1];
+  uint16_t part[PARTS];
   split(c < cols ? (float)from[r * ld + c] : 0.f, part);
 #pragma unroll
-  for (int k = 0; k < PARTS; ++k) *(uint16_t *)(to + ((size_t)k * rows + r) * padded + c) = part[k][0];
+  for (int k = 0; k < PARTS; ++k) *(uint16_t *)(to + ((size_t)k * rows + r) * padded + c) = part[k];
 }
 // to[part][col][padded rows] = parts of from[row][col]; zeros behind the last row and, where `scale` is given, for the rows whose
 // scale is 0: what they hold (padding: anything) would else meet the zeros of G as 0 * NaN
@@ -274,34 +371,49 @@ __global__ __launch_bounds__(256) void k_columns(const T *from, long long ld, in
   __syncthreads();
   for (int i = g; i < 64; i += 4) {
     if (c0 + i >= cols || r0 + l >= padded) continue;
-    uint16_t part[PARTS][1];
+    uint16_t part[PARTS];
     split((float)tile[l][i], part);
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k) *(uint16_t *)(to + ((size_t)k * cols + c0 + i) * padded + r0 + l) = part[k][0];
+    for (int k = 0; k < PARTS; ++k) *(uint16_t *)(to + ((size_t)k * cols + c0 + i) * padded + r0 + l) = part[k];
   }
 }
 
-// One wavefront per row: the blocks' maxima and sums joined, in an order that depends on nothing but their number.
-__global__ __launch_bounds__(256) void k_join(const float2 *part, const float *picked, const int *targets, int blocks, int rows, int vocab,
-                                              float *loss, float *state) {
-  const int m = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (m >= rows) return;
+// The blocks' maxima and sums joined, 16 rows per workgroup (whole lines of `part`), 64 threads each, in an order that depends on nothing but
+// the number of blocks.  A block without a maximum has no terms: its sum is 0, or NaN where a logit was.
+struct Terms {
+  float top, sum;
+  __device__ __forceinline__ void join(Terms o) {
+    const float t = fmaxf(top, o.top);
+    sum = (top == t ? sum : sum * expf(top - t)) + (o.top == t ? o.sum : o.sum * expf(o.top - t));
+    top = t;
+  }
+};
+__global__ __launch_bounds__(1024) void k_join(const float2 *part, const float *picked, const int *targets, int blocks, int rows, int vocab,
+                                               float *loss, float *state) {
+  __shared__ Terms all[64][16];
+  const int r = threadIdx.x & 15, at = threadIdx.x >> 4, m = blockIdx.x * 16 + r;
+  Terms t = {-INFINITY, 0.f};
+  if (m < rows)
+#pragma unroll 4
+    for (int b = at; b < blocks; b += 64) {
+      const float2 q = part[(size_t)b * rows + m];
+      t.join(Terms{q.x, q.y});
+    }
+  all[at][r] = t;
+#pragma unroll
+  for (int n = 32; n; n >>= 1) {
+    __syncthreads();
+    if (at < n) {
+      t.join(all[at + n][r]);
+      all[at][r] = t;
+    }
+  }
+  if (at || m >= rows) return;
   const int y = targets[m];
   const bool has = y >= 0 && y < vocab;
-  float top = has ? picked[m] : -INFINITY;
-  const float own = top;
-  for (int b = lane; b < blocks; b += 64) top = fmaxf(top, part[(size_t)b * rows + m].x);
-#pragma unroll
-  for (int k = 32; k; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-  float sum = 0.f;
-  for (int b = lane; b < blocks; b += 64) {
-    const float2 q = part[(size_t)b * rows + m];
-    sum += q.x == -INFINITY ? q.y : q.y * expf(q.x - top); // (an empty block has a sum of 0, or one of NaN)
-  }
-#pragma unroll
-  for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
-  if (lane) return;
-  const float mine = has ? expf(own - top) : 0.f, total = sum + mine, miss = sum / total;
+  const float own = has ? picked[m] : -INFINITY, top = fmaxf(own, t.top);
+  const float others = t.top == top ? t.sum : t.sum * expf(t.top - top);
+  const float total = others + (has ? expf(own - top) : 0.f), miss = others / total;
   loss[m] = !has ? 0.f : miss < 0.5f ? -log1pf(-miss) : top - own + logf(total);
   state[3 * m] = top;
   state[3 * m + 1] = 1.f / total;
@@ -327,9 +439,13 @@ __global__ __launch_bounds__(1024) void k_scale(const int *targets, const float 
   }
 }
 
-template <typename T> __global__ __launch_bounds__(256) void k_narrow(const float *from, T *to, size_t n) {
+// to = the sum of the slices, each n elements
+template <typename T> __global__ __launch_bounds__(256) void k_sum(const float *from, int slices, size_t n, T *to) {
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) to[i] = (T)from[i];
+  if (i >= n) return;
+  float sum = from[i];
+  for (int k = 1; k < slices; ++k) sum += from[k * n + i];
+  to[i] = (T)sum;
 }
 __global__ __launch_bounds__(256) void k_clear(uint16_t *to, size_t n) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) to[i] = 0;
@@ -338,11 +454,11 @@ __global__ __launch_bounds__(256) void k_clear(uint16_t *to, size_t n) {
 // ---- workspace ------------------------------------------------------------------------------
 struct Space {
   int parts, dp, padded, width; // width: entries of a piece of the vocabulary
-  size_t h, w, part, picked, scale, ht, wt, gm, gt, sum, bytes;
+  size_t h, w, part, picked, scale, ht, wt, gm, gt, sum_h, sum_w, bytes;
   Space(const VocabShape &p, bool grad) {
     parts = p.bf16 ? 1 : 3;
     dp = (p.d + BK - 1) / BK * BK;
-    padded = (p.rows + PAD - 1) / PAD * PAD;
+    padded = few(p.rows) ? 64 : (p.rows + PAD - 1) / PAD * PAD;
     // G of a piece has about 2^27 elements, and a piece of w no more
     const long long all = ((long long)p.vocab + PAD - 1) / PAD * PAD, most = grad ? (padded > dp ? padded : dp) : dp;
     long long fit = (1ll << 27) / (most > 0 ? most : 1) / PAD * PAD;
@@ -353,7 +469,7 @@ struct Space {
     h = take((size_t)2 * parts * p.rows * dp);
     w = take((size_t)2 * parts * width * dp);
     if (!grad) {
-      part = take(sizeof(float2) * (size_t)(all / 128) * p.rows);
+      part = take(sizeof(float2) * (size_t)(all / (few(p.rows) ? 32 : 128)) * p.rows);
       picked = take(sizeof(float) * (size_t)p.rows);
     } else {
       scale = take(sizeof(float) * (size_t)padded);
@@ -361,7 +477,10 @@ struct Space {
       wt = take((size_t)2 * parts * p.d * width);
       gm = take((size_t)2 * parts * padded * width);
       gt = take((size_t)2 * parts * padded * width);
-      sum = take(width < p.vocab ? sizeof(float) * (size_t)p.rows * p.d : 0);
+      const Slices sh(p.rows, p.d, width / BK), sw(width < p.vocab ? width : p.vocab, p.d, padded / BK);
+      sum_h = take(width < p.vocab || sh.count > 1 ? sizeof(float) * (size_t)sh.count * p.rows * p.d : 0);
+      // (the last piece may be so much narrower that it is cut further: no more than 256 tiles in all)
+      sum_w = take(sw.count > 1 || width < p.vocab ? sizeof(float) * 256 * (size_t)256 * 256 : 0);
     }
     bytes = at;
   }
@@ -412,8 +531,8 @@ hipError_t loss(const VocabShape &p, const T *h, const T *w, const int *targets,
     q.part_a = (long long)q.rows_a * sp.dp;
     TRY((product<PARTS>(q, ep, s)));
   }
-  const int blocks = (p.vocab + 255) / 256 * 2;
-  k_join<<<(p.rows + 3) / 4, 256, 0, s>>>(ep.part, ep.picked, targets, blocks, p.rows, p.vocab, loss, state);
+  const int blocks = (p.vocab + 255) / 256 * (few(p.rows) ? 8 : 2);
+  k_join<<<(p.rows + 15) / 16, 1024, 0, s>>>(ep.part, ep.picked, targets, blocks, p.rows, p.vocab, loss, state);
   return hipGetLastError();
 }
 
@@ -421,7 +540,9 @@ template <typename T, int PARTS>
 hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *targets, const float *state, const float *dloss, T *dh, T *dw,
                      char *work, hipStream_t s) {
   const Space sp(p, true);
-  float *scale = (float *)(work + sp.scale), *sum = (float *)(work + sp.sum);
+  float *scale = (float *)(work + sp.scale), *sum_h = (float *)(work + sp.sum_h), *sum_w = (float *)(work + sp.sum_w);
+  const bool summed = sp.width < p.vocab || Slices(p.rows, p.d, sp.width / BK).count > 1;
+  int slices_h = 1;
   __bf16 *ht = (__bf16 *)(work + sp.ht), *wt = (__bf16 *)(work + sp.wt), *gm = (__bf16 *)(work + sp.gm), *gt = (__bf16 *)(work + sp.gt);
   k_scale<<<1, 1024, 0, s>>>(targets, dloss, p.rows, sp.padded, p.vocab, scale);
   TRY(hipGetLastError());
@@ -440,15 +561,25 @@ hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *tar
     GradEpilogue<PARTS> ep = {targets, state, scale, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded};
     TRY((product<PARTS>(q, ep, s)));
     TRY((columns_of<T, PARTS>(w + v * p.ld_w, p.ld_w, entries, p.d, width, nullptr, wt, s)));
-    Product dhq = {gm, wt, width, width, (long long)sp.padded * width, (long long)p.d * width, p.rows, p.d, width / BK, 0, 0};
-    if (sp.width >= p.vocab) TRY((product<PARTS>(dhq, StoreEpilogue<T>{dh, p.d, p.rows, p.d, false}, s)));
-    else TRY((product<PARTS>(dhq, StoreEpilogue<float>{sum, p.d, p.rows, p.d, v > 0}, s)));
-    Product dwq = {gt, ht, sp.padded, sp.padded, (long long)sp.padded * width, (long long)p.d * sp.padded, entries, p.d, sp.padded / BK, 0, 0};
-    TRY((product<PARTS>(dwq, StoreEpilogue<T>{dw + v * p.d, p.d, entries, p.d, false}, s)));
+    const Slices sh(p.rows, p.d, width / BK, v ? slices_h : 256), sw(entries, p.d, sp.padded / BK);
+    if (!v) slices_h = sh.count;
+    Product dhq = {gm, wt, width, width, (long long)sp.padded * width, (long long)p.d * width, p.rows, p.d, width / BK, 0, 0, sh.count, sh.steps};
+    if (!summed) TRY((product<PARTS>(dhq, StoreEpilogue<T>{dh, p.d, 0, p.rows, p.d, false}, s)));
+    else TRY((product<PARTS>(dhq, StoreEpilogue<float>{sum_h, p.d, (long long)p.rows * p.d, p.rows, p.d, v > 0}, s)));
+    Product dwq = {gt, ht, sp.padded, sp.padded, (long long)sp.padded * width, (long long)p.d * sp.padded, entries, p.d, sp.padded / BK, 0, 0,
+                   sw.count, sw.steps};
+    T *const to = dw + v * p.d;
+    if (sw.count == 1) TRY((product<PARTS>(dwq, StoreEpilogue<T>{to, p.d, 0, entries, p.d, false}, s)));
+    else {
+      const size_t n = (size_t)entries * p.d;
+      TRY((product<PARTS>(dwq, StoreEpilogue<float>{sum_w, p.d, (long long)n, entries, p.d, false}, s)));
+      k_sum<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum_w, sw.count, n, to);
+      TRY(hipGetLastError());
+    }
   }
-  if (sp.width < p.vocab) {
+  if (summed) {
     const size_t n = (size_t)p.rows * p.d;
-    k_narrow<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum, dh, n);
+    k_sum<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum_h, slices_h, n, dh);
   }
   return hipGetLastError();
 }
