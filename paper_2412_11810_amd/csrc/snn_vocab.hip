@@ -50,12 +50,15 @@ struct Stage {
   }
 };
 
-// One tile of BM rows of A by BN rows of B by eight wavefronts, WA along A and WB along B.  A row's 64 elements are eight
-// 16-byte chunks in LDS; chunk c of row r is at place c ^ (r % 8), so that the lanes of a fragment, which read one chunk of
-// 32 rows, use all banks.  Loads go past the registers; the next 64 elements arrive while these are multiplied.
+// One tile of BM rows of A by BN rows of B by eight wavefronts, WA along A and WB along B.  LDS holds two steps of 64 elements (whole
+// lines of a row, eight chunks; chunk c of row r is at place c ^ (r / 2 % 8), so that 16 lanes of a fragment, which read one
+// chunk of as many rows, use all 64 banks).  Loads go past the registers, a step ahead.  The fragments of the next quarter of a step are
+// on their way while those of this one are multiplied, also across the barrier between two steps: matrix instructions wait for nothing
+// but loads that take longer than a step.
 template <int BM, int BN, int WA, int WB, int PARTS, class Epilogue>
 __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
-  constexpr int MI = BM / WA / 32, NI = BN / WB / 32, LA = BM / 64, LB = BN / 64;
+  constexpr int MI = BM / WA / 32, NI = BN / WB / 32, LA = BM / 64, LB = BN / 64, QUARTERS = BK / 16;
+  constexpr int SEGS = PARTS == 1 ? 1 : 6;
   __shared__ __align__(16) char a0[BM * 128], b0[BN * 128], a1[BM * 128], b1[BN * 128];
   // tiles in the order of the dies: consecutive workgroups are on different ones, each die takes a run of tiles, in groups of eight
   // along A that share the rows of B
@@ -69,16 +72,14 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
   const int wa = w / WB, wb = w % WB;
   const char *base_a = (const char *)(p.a + (long long)ta * BM * p.lda), *base_b = (const char *)(p.b + (long long)tb * BN * p.ldb);
   unsigned off_a[LA], off_b[LB];
-  const int row8 = w * 8 + (lane >> 3), chunk = (lane & 7) ^ (lane >> 3);
+  const int row8 = w * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row8 >> 1) & 7);
 #pragma unroll
   for (int i = 0; i < LA; ++i) off_a[i] = (unsigned)min(i * 64 + row8, p.rows_a - 1 - ta * BM) * (unsigned)(p.lda * 2) + chunk * 16;
 #pragma unroll
   for (int i = 0; i < LB; ++i) off_b[i] = (unsigned)min(i * 64 + row8, p.rows_b - 1 - tb * BN) * (unsigned)(p.ldb * 2) + chunk * 16;
 
-  tile32 acc[MI][NI] = {};
   const int slice = blockIdx.y, k_first = slice * p.slice_steps, k_end = min(k_first + p.slice_steps, p.ksteps);
   int k = k_first, seg = 0;
-  constexpr int SEGS = PARTS == 1 ? 1 : 6;
   auto fetch = [&](char *la, char *lb) {
     // parts of A 0 1 2 0 1 0 with parts of B 2 1 0 1 0 0: the smallest products first
     const int pa = PARTS == 1 ? 0 : (0x010210 >> (4 * seg)) & 15, pb = PARTS == 1 ? 0 : (0x001012 >> (4 * seg)) & 15;
@@ -89,46 +90,61 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
     for (int i = 0; i < LB; ++i) load_lds(gb, off_b[i], lb + (i * 64 + w * 8) * 128);
     if (++k == k_end) { k = k_first; ++seg; }
   };
+  tile32 acc[MI][NI] = {};
+  frag fa[2][MI], fb[2][NI];
   const int r = lane & 31, half = lane >> 5;
-  auto multiply = [&](const char *la, const char *lb) {
+  auto read = [&](int s, const char *la, const char *lb) {
+    const int place = ((2 * s + half) ^ ((r >> 1) & 7)) * 16;
 #pragma unroll
-    for (int s = 0; s < BK / 16; ++s) {
-      frag fa[MI], fb[NI];
-      const int place = ((2 * s + half) ^ (r & 7)) * 16;
+    for (int i = 0; i < MI; ++i) fa[s & 1][i] = *(const frag *)(la + (wa * (BM / WA) + i * 32 + r) * 128 + place);
 #pragma unroll
-      for (int i = 0; i < MI; ++i) fa[i] = *(const frag *)(la + (wa * (BM / WA) + i * 32 + r) * 128 + place);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) fb[i] = *(const frag *)(lb + (wb * (BN / WB) + i * 32 + r) * 128 + place);
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-    }
+    for (int i = 0; i < NI; ++i) fb[s & 1][i] = *(const frag *)(lb + (wb * (BN / WB) + i * 32 + r) * 128 + place);
+    __builtin_amdgcn_sched_barrier(0); // (left alone the compiler reads right before it multiplies, into the same registers)
   };
+  auto multiply = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s & 1][i], fb[s & 1][j], acc[i][j], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // every load of every wavefront is in LDS, and every wavefront has what it read before
   auto arrived = [&]() {
-    __builtin_amdgcn_s_waitcnt(0x0f70); // every load of this wavefront, then those of the others
-    __syncthreads();
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    asm volatile("" ::: "memory"); // (the compiler knows of no store to LDS here)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  int left = (k_end - k_first) * SEGS;
+  auto step = [&](char *la, char *lb, const char *na, const char *nb, bool more) {
+#pragma unroll
+    for (int s = 0; s < QUARTERS - 1; ++s) {
+      read(s + 1, la, lb);
+      multiply(s);
+    }
+    if (more || left > 1) {
+      arrived();
+      if (more || left > 2) fetch(la, lb);
+      read(0, na, nb);
+    }
+    multiply(QUARTERS - 1);
+    --left;
   };
   fetch(a0, b0);
+  if (left > 1) fetch(a1, b1);
   arrived();
-  int left = (k_end - k_first) * SEGS;
-  for (; left > 2; left -= 2) {
-    fetch(a1, b1);
-    multiply(a0, b0);
-    arrived();
-    fetch(a0, b0);
-    multiply(a1, b1);
-    arrived();
+  read(0, a0, b0);
+  while (left > 3) {
+    step(a0, b0, a1, b1, true);
+    step(a1, b1, a0, b0, true);
   }
-  if (left == 2) fetch(a1, b1);
-  multiply(a0, b0);
-  arrived();
-  if (left == 2) {
-    multiply(a1, b1);
-    arrived();
-  }
-  // element e of a tile: row 8 (e / 4) + 4 half + e % 4 of A, row r of B.  Every wavefront is through with LDS: 4 KB each, twice
-  const Stage stage = {(BM >= BN ? a0 : b0) + w * 4096, (BM >= BN ? a1 : b1) + w * 4096, lane, r, half};
+  step(a0, b0, a1, b1, false);
+  if (left) step(a1, b1, a0, b0, false);
+  if (left) step(a0, b0, a1, b1, false);
+  __syncthreads();
+  // element e of a tile: row 8 (e / 4) + 4 half + e % 4 of A, row r of B.  Every wavefront is through with the tiles in LDS
+  constexpr bool OF_A = BM >= BN;
+  const Stage stage = {(OF_A ? a0 : b0) + w * 4096, (OF_A ? a1 : b1) + w * 4096, lane, r, half};
   ep.template finish<MI, NI>(acc, ta * BM + wa * (BM / WA), tb * BN + wb * (BN / WB), slice, stage);
 }
 
