@@ -359,8 +359,8 @@ typedef struct {
 size_t snn_vocab_workspace(const snn_vocab *p, int32_t gradients);
 
 /* targets [rows]; one outside 0..vocab-1 (-1: padding) makes a row that has a loss of 0, no gradient and no part in a mean.
- * loss [rows] fp32; state [rows][3] fp32: largest logit, 1 / sum of exp(logit - largest), 1 - softmax of the target.  The third is a
- * sum of the other entries, so that loss and gradient of a target that is nearly certain keep their digits. */
+ * loss [rows] fp32; state [rows][3] fp32: a power M of two of the size of the largest exp(logit), as log2 M; 1 / sum of exp(logit) / M;
+ * 1 - softmax of the target, as a sum of the other entries, so that loss and gradient of a target that is nearly certain keep their digits. */
 snn_status snn_vocab_loss(const snn_launch *at, const snn_vocab *p, const void *h, const void *w, const int32_t *targets, float *loss,
                           float *state);
 

@@ -1,15 +1,17 @@
 // Softmax cross entropy of rows h [rows][d] against a vocabulary w [vocab][d], and its gradients, without a matrix of logits.
 //
-//   l_rv = h_r . w_v;  M_r = max_v l_rv;  S_r = sum_v exp(l_rv - M_r);  miss_r = sum_{v != y} exp(l_rv - M_r) / S_r = 1 - p_ry
-//   loss_r = -log1p(-miss_r), or M_r - l_ry + log S_r where miss_r is not small
-//   G_rv = dloss_r exp(l_rv - M_r) / S_r;  G_ry = -dloss_r miss_r;  dh = G w;  dw = G^T h
+//   l_rv = h_r . w_v log2(e);  M_r = max_v ceil(l_rv);  S_r = sum_v 2^(l_rv - M_r);  miss_r = sum_{v != y} 2^(l_rv - M_r) / S_r = 1 - p_ry
+//   loss_r = -log1p(-miss_r), or (log2 S_r - (l_ry - M_r)) log(2) where miss_r is not small
+//   G_rv = dloss_r 2^(l_rv - M_r) / S_r;  G_ry = -dloss_r miss_r;  dh = G w;  dw = G^T h
 //
 // miss_r is summed without the target, never formed as 1 - p: a target that the model is sure of keeps its loss and gradient.
+// The subtrahends are whole numbers: l - M is one fused multiply-add, rounded once to its own size, and sums over different M are brought
+// together exactly.
 //
 // All four products are one kernel, C = A B^T with the sums along the rows of both operands, on the bf16 matrix cores with fp32
 // accumulators; what differs is what happens to the accumulators.  Operands of 32 bits go in as three bf16 parts of 8 bits
 // each, which hold all 24 bits of a float: the six products of parts whose weight is above 2^-24 are further steps of the same sum.
-// The logits are computed twice, for the loss (kept: one maximum and one sum for 128 of them) and for G, one piece of the
+// The logits are computed twice, for the loss (kept: one exponent and one sum for 128 of them) and for G, one piece of the
 // vocabulary after the other, whose G is all that is ever in memory; a second product of 2 rows d vocab operations costs less
 // than 4 bytes of logit written and read for each.
 #include "snn_ops.h"
@@ -155,7 +157,8 @@ __device__ __forceinline__ int entry(const int *targets, int m, bool on, int voc
 }
 
 // Logits, A = vocabulary (a piece of it from `first` on), B = rows of h.  A lane has the logits of one row with 16 MI entries of the
-// vocabulary: their maximum and sum, the target left out, and the target's logit go to memory.
+// vocabulary: the exponent M of the largest and the
+// sum of the powers above it, the target left out, and the target's logit go to memory.
 struct LossEpilogue {
   static constexpr bool LOGITS = true;
   const int *targets;
@@ -180,19 +183,21 @@ struct LossEpilogue {
             if (v == y || v0 + v >= vocab) acc[i][j][e] = -INFINITY;
           }
       }
-      float top = -INFINITY, sum = 0.f;
+      float most[2] = {-INFINITY, -INFINITY}, sum[2] = {};
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
-      top = fmaxf(top, __shfl_xor(top, 32));
+        for (int e = 0; e < 16; e += 2) most[e >> 1 & 1] = fmaxf(fmaxf(most[e >> 1 & 1], acc[i][j][e]), acc[i][j][e + 1]);
+      float top = fmaxf(most[0], most[1]);
+      top = ceilf(fmaxf(top, __shfl_xor(top, 32)) * LOG2E);
       const float from = top == -INFINITY ? 0.f : top; // nothing here: all terms are 0
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - from) * LOG2E);
-      sum += __shfl_xor(sum, 32);
-      if (half == 0 && on) part[(size_t)block * rows + m] = make_float2(top, sum);
+        for (int e = 0; e < 16; ++e) sum[e & 1] += __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -from));
+      sum[0] += sum[1];
+      sum[0] += __shfl_xor(sum[0], 32);
+      if (half == 0 && on) part[(size_t)block * rows + m] = make_float2(top, sum[0]);
     }
   }
 };
@@ -220,7 +225,7 @@ template <int PARTS> struct GradEpilogue {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int v = 32 * i + 8 * (e >> 2) + (e & 3);
-          float x = __builtin_amdgcn_exp2f((acc[i][j][e] - top) * LOG2E) * per;
+          float x = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -top)) * per;
           if (v == y) x = -miss * g;
           acc[i][j][e] = none || v >= left ? 0.f : x;
         }
@@ -394,13 +399,14 @@ __global__ __launch_bounds__(256) void k_columns(const T *from, long long ld, in
   }
 }
 
-// The blocks' maxima and sums joined, 16 rows per workgroup (whole lines of `part`), 64 threads each, in an order that depends on nothing but
-// the number of blocks.  A block without a maximum has no terms: its sum is 0, or NaN where a logit was.
+// The blocks' exponents and sums joined, 16 rows per workgroup (whole lines of `part`), 64 threads each, in an order that depends on
+// nothing but the number of blocks.  A block without a logit has no terms: its sum is 0, or NaN where a logit was.
 struct Terms {
   float top, sum;
+  __device__ __forceinline__ float at(float t) const { return top == t ? sum : sum * exp2f(top - t); }
   __device__ __forceinline__ void join(Terms o) {
     const float t = fmaxf(top, o.top);
-    sum = (top == t ? sum : sum * expf(top - t)) + (o.top == t ? o.sum : o.sum * expf(o.top - t));
+    sum = at(t) + o.at(t);
     top = t;
   }
 };
@@ -427,10 +433,10 @@ __global__ __launch_bounds__(1024) void k_join(const float2 *part, const float *
   if (at || m >= rows) return;
   const int y = targets[m];
   const bool has = y >= 0 && y < vocab;
-  const float own = has ? picked[m] : -INFINITY, top = fmaxf(own, t.top);
-  const float others = t.top == top ? t.sum : t.sum * expf(t.top - top);
-  const float total = others + (has ? expf(own - top) : 0.f), miss = others / total;
-  loss[m] = !has ? 0.f : miss < 0.5f ? -log1pf(-miss) : top - own + logf(total);
+  const float own = has ? picked[m] : -INFINITY, top = fmaxf(ceilf(own * LOG2E), t.top);
+  const float others = t.at(top), mine = fmaf(own, LOG2E, -top);
+  const float total = others + (has ? exp2f(mine) : 0.f), miss = others / total;
+  loss[m] = !has ? 0.f : miss < 0.5f ? -log1pf(-miss) : (log2f(total) - mine) * 0.693147181f;
   state[3 * m] = top;
   state[3 * m + 1] = 1.f / total;
   state[3 * m + 2] = miss;
