@@ -302,10 +302,10 @@ const char *snn_launch_error(void);
  *   a_t = sigmoid(z_t) ;  h_t = a_t h_{t-1} + (1 - a_t) x_t ,  t = 1..T
  * Computed as h + sigmoid(-z) (x - h) in fp32 whatever the type: a state or drive that is not finite gives NaN from its step on. */
 typedef struct {
-  int32_t T, batch, n;        /* T >= 0 (0: h_last = h0), at most 2^30 steps and 2^30 channels batch * n */
+  int32_t T, batch, n;        /* T >= 0 (0: h_last = h0), at most 2^30 steps and 2^25 channels batch * n */
   int32_t dtype;              /* snn_dtype of z, x, h, dh, dz, dx */
-  int64_t ld_z, ld_x, ld_h;   /* elements between consecutive rows (t, b) of z, of x, of h and dh; 0: n.  z and x may be the halves of
-                                 one projection [T][batch][2 n], and dz and dx those of its gradient */
+  int64_t ld_z, ld_x, ld_h;   /* elements between consecutive rows (t, b) of z, of x, of h and dh; 0: n, at most 2^27 bytes
+                                 per step.  z and x may be the halves of one projection [T][batch][2 n], and dz and dx those of its gradient */
   int64_t ld_dz, ld_dx;       /* the same of dz, dx (not used by the forward pass) */
   const int32_t *lengths;     /* [batch] or NULL (T each): sequence b has steps 1..lengths[b]; a number outside 0..T counts as the nearer
                                  end.  Later steps are read by nothing; h, dz and dx are zeros there */

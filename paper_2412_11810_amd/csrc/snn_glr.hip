@@ -44,11 +44,15 @@ template <typename T, int VEC> __device__ __forceinline__ typename Raw<T, VEC>::
   }
 }
 
-// sigmoid(-z).  The bound keeps 1 + e^z finite; a NaN passes it.
-__device__ __forceinline__ float moved(float z) {
-  float v = z * 1.44269504f;
-  v = v > 126.f ? 126.f : v;
-  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v));
+// sigmoid(-z) from z / log(2): 0 from where 1 + e^z is infinite
+constexpr float LOG2E = 1.44269504f;
+__device__ __forceinline__ float moved(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z)); }
+
+// f(whole) for a wavefront's steps, `whole` known to the compiler: whether every lane's sequence has all of them, as nearly always
+template <bool B> struct Known { static constexpr bool value = B; };
+template <class F> __device__ __forceinline__ void either(bool whole, F f) {
+  if (whole) f(Known<true>());
+  else f(Known<false>());
 }
 
 __device__ __forceinline__ void lds_barrier() { // of the LDS alone: loads from memory stay in flight
@@ -85,19 +89,34 @@ template <int VEC> struct Lane {
   }
 };
 
-// An array [T][batch][ld] of elements of `size` bytes as a lane sees it: the offset of its element inside a step is kept in 32 bits
-// (a step has less than 4 GB), that of the step in scalar registers.
+// An array [T][batch][ld] of elements of `size` bytes as a lane sees it.  Sixteen steps are reached from a 64-bit scalar address, a
+// 32-bit scalar offset for the step (a step has 2^27 bytes at most) and a 32-bit one for the lane: no vector arithmetic for
+// addresses.
 struct Rows {
   char *base;
-  long long step;
-  unsigned at;
+  unsigned step, at;
   __device__ __forceinline__ Rows(const void *p, int size, long long ld, int batch, int b, int i)
-      : base((char *)p), step((long long)size * ld * batch), at((unsigned)((size_t)size * (b * ld + i))) {}
-  template <typename R> __device__ __forceinline__ R &of(int t) const { return *(R *)(base + t * step + at); }
+      : base((char *)p), step((unsigned)(size * ld * batch)), at((unsigned)(size * (b * ld + i))) {}
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t from(int t) const {
+    return __builtin_amdgcn_make_buffer_rsrc(base + (unsigned long long)t * step, 0, (int)0xffffffff, 0x00020000);
+  }
   // 16 steps from t0 on.  Steps at and past T are those of the last one again (and not used).
   template <typename R> __device__ __forceinline__ void load(R (&r)[STEPS], int t0, int T) const {
+    const int first = min(t0, T - 1), last = T - 1 - first;
+    const __amdgpu_buffer_rsrc_t from_first = from(first);
 #pragma unroll
-    for (int j = 0; j < STEPS; ++j) r[j] = of<const R>(min(t0 + j, T - 1));
+    for (int j = 0; j < STEPS; ++j) {
+      const int at_step = (int)(min(j, last) * step);
+      if constexpr (sizeof(R) == 4) r[j] = __builtin_amdgcn_raw_buffer_load_b32(from_first, (int)at, at_step, 0);
+      else if constexpr (sizeof(R) == 2) r[j] = __builtin_amdgcn_raw_buffer_load_b16(from_first, (int)at, at_step, 0);
+      else r[j] = __builtin_amdgcn_raw_buffer_load_b8(from_first, (int)at, at_step, 0);
+    }
+  }
+  // Step j of those, not to be kept in the caches (results are not read again here, z and x are)
+  template <typename R> __device__ __forceinline__ void store(const __amdgpu_buffer_rsrc_t &from_first, int j, R r) const {
+    constexpr int NT = 2;
+    if constexpr (sizeof(R) == 4) __builtin_amdgcn_raw_buffer_store_b32(r, from_first, (int)at, (int)(j * step), NT);
+    else __builtin_amdgcn_raw_buffer_store_b16(r, from_first, (int)at, (int)(j * step), NT);
   }
 };
 
@@ -135,29 +154,36 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
   // (a state that `to` may take the place of is read by every wavefront before the first one may write it)
 #pragma unroll
   for (int v = 0; v < VEC; ++v) asm volatile("" ::"v"(h[v]));
+  // (the map of a segment is put together from its end, its states are found from its beginning: what was read last is read first again)
   R rz[STEPS], rx[STEPS];
-  int t0 = (k0 * NW + w) * STEPS;
+  constexpr int STRIDE = MAPS ? -NW * STEPS : NW * STEPS;
+  int t0 = ((MAPS ? k1 - 1 : k0) * NW + w) * STEPS;
   if (k0 < k1) {
     pz.load(rz, t0, a.T);
     px.load(rx, t0, a.T);
   }
-  for (int k = k0; k < k1; ++k, t0 += NW * STEPS) {
+  int n = k1 - k0, k = MAPS ? k1 - 1 : k0;
+  for (; n > 0; --n, MAPS ? --k : ++k, t0 += STRIDE) {
     float b[STEPS][VEC], x[STEPS][VEC];
     const int live = me.len - t0; // steps of these 16 that the sequence has
+    const bool whole = __all(live >= STEPS);
+    either(whole, [&](auto known) {
+      constexpr bool ALL = decltype(known)::value;
 #pragma unroll
-    for (int j = 0; j < STEPS; ++j) {
-      float z[VEC];
-      widen<T, VEC>(rz[j], z);
-      widen<T, VEC>(rx[j], x[j]);
+      for (int j = 0; j < STEPS; ++j) {
+        float z[VEC];
+        widen<T, VEC>(rz[j], z);
+        widen<T, VEC>(rx[j], x[j]);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        b[j][v] = j < live ? moved(z[v]) : 0.f;
-        x[j][v] = j < live ? x[j][v] : 0.f;
+        for (int v = 0; v < VEC; ++v) {
+          b[j][v] = ALL || j < live ? moved(z[v] * LOG2E) : 0.f;
+          x[j][v] = ALL || j < live ? x[j][v] : 0.f;
+        }
       }
-    }
-    if (k + 1 < k1) {
-      pz.load(rz, t0 + NW * STEPS, a.T);
-      px.load(rx, t0 + NW * STEPS, a.T);
+    });
+    if (n > 1) {
+      pz.load(rz, t0 + STRIDE, a.T);
+      px.load(rx, t0 + STRIDE, a.T);
     }
     float start[VEC];
     if (NW > 1) {
@@ -182,10 +208,15 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
       for (int i = 0; i < WAVES; ++i)
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
-          if (i == w) start[v] = h[v];
-          const float Qi = maps.v[k & 1][0][i][v][threadIdx.x], Bi = maps.v[k & 1][1][i][v][threadIdx.x];
-          h[v] += fmaf(-Qi, h[v], Bi);
-          if (MAPS) q[v] = fmaf(Qi, 1.f - q[v], q[v]);
+          const int wave = MAPS ? WAVES - 1 - i : i;
+          const float Qi = maps.v[k & 1][0][wave][v][threadIdx.x], Bi = maps.v[k & 1][1][wave][v][threadIdx.x];
+          if (MAPS) { // an earlier map, then the one so far
+            h[v] += fmaf(-q[v], Bi, Bi);
+            q[v] = fmaf(q[v], 1.f - Qi, Qi);
+          } else {
+            if (i == w) start[v] = h[v];
+            h[v] += fmaf(-Qi, h[v], Bi);
+          }
         }
     } else {
 #pragma unroll
@@ -194,17 +225,21 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
         if (a.kept && me.on) a.kept[me.c + v] = h[v];
       }
     }
-    if (!MAPS) {
+    if (!MAPS && me.on) {
+      const __amdgpu_buffer_rsrc_t to = ph.from(t0);
+      either(whole, [&](auto known) {
+        constexpr bool ALL = decltype(known)::value;
 #pragma unroll
-      for (int j = 0; j < STEPS; ++j) {
-        float out[VEC];
+        for (int j = 0; j < STEPS; ++j) {
+          float out[VEC];
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          start[v] = fmaf(b[j][v], x[j][v] - start[v], start[v]);
-          out[v] = j < live ? start[v] : 0.f;
+          for (int v = 0; v < VEC; ++v) {
+            start[v] = fmaf(b[j][v], x[j][v] - start[v], start[v]);
+            out[v] = ALL || j < live ? start[v] : 0.f;
+          }
+          if (ALL || t0 + j < a.T) ph.store(to, j, narrow<T, VEC>(out));
         }
-        if (t0 + j < a.T && me.on) ph.of<R>(t0 + j) = narrow<T, VEC>(out);
-      }
+      });
       if (NW == 1)
 #pragma unroll
         for (int v = 0; v < VEC; ++v) h[v] = start[v];
@@ -269,32 +304,37 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
 #pragma unroll
       for (int v = 0; v < VEC; ++v) kept[v] = a.kept[(size_t)k * a.channels + me.c + v];
   };
-  if (k0 < k1) fetch(k1 - 1);
-  for (int k = k1 - 1; k >= k0; --k) {
+  // (as in the forward pass: the map of a segment is put together from its beginning)
+  if (k0 < k1) fetch(MAPS ? k0 : k1 - 1);
+  int n = k1 - k0, k = MAPS ? k0 : k1 - 1;
+  for (; n > 0; --n, MAPS ? ++k : --k) {
     const int t0 = (k * WAVES + w) * STEPS;
-    float b[STEPS][VEC], x[STEPS][VEC], d[STEPS][VEC];
+    float b[STEPS][VEC], x[STEPS][VEC];
+    R d[STEPS]; // (as it is in memory: half the registers)
     const int live = me.len - t0;
+    const bool whole = __all(live >= STEPS);
+    either(whole, [&](auto known) {
+      constexpr bool ALL = decltype(known)::value;
 #pragma unroll
-    for (int j = 0; j < STEPS; ++j) {
-      float z[VEC];
-      widen<P, VEC>(rz[j], z);
-      if (!MAPS) widen<P, VEC>(rx[j], x[j]);
-      widen<T, VEC>(rd[j], d[j]);
+      for (int j = 0; j < STEPS; ++j) {
+        float z[VEC];
+        widen<P, VEC>(rz[j], z);
+        if (!MAPS) widen<P, VEC>(rx[j], x[j]);
+        d[j] = ALL || j < live ? rd[j] : (R)0;
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        if (PACKED) {
-          z[v] *= __uint_as_float((uint32_t)ez[j] << 23);
-          if (!MAPS) x[j][v] *= __uint_as_float((uint32_t)ex[j] << 23);
+        for (int v = 0; v < VEC; ++v) {
+          // (a step is a power of two: its product with log2(e) is exact)
+          z[v] *= PACKED ? __uint_as_float((uint32_t)ez[j] << 23) * LOG2E : LOG2E;
+          if (PACKED && !MAPS) x[j][v] *= __uint_as_float((uint32_t)ex[j] << 23);
+          b[j][v] = ALL || j < live ? moved(z[v]) : 0.f;
+          if (!MAPS) x[j][v] = ALL || j < live ? x[j][v] : 0.f;
         }
-        b[j][v] = j < live ? moved(z[v]) : 0.f;
-        if (!MAPS) x[j][v] = j < live ? x[j][v] : 0.f;
-        d[j][v] = j < live ? d[j][v] : 0.f;
       }
-    }
+    });
     float Q[VEC] = {}, B[VEC] = {}, G[VEC] = {}, h[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) h[v] = kept[v];
-    if (k > k0) fetch(k - 1);
+    if (n > 1) fetch(MAPS ? k + 1 : k - 1);
 #pragma unroll
     for (int j = 0; j < STEPS; ++j)
 #pragma unroll
@@ -303,12 +343,15 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
         Q[v] = fmaf(b[j][v], 1.f - Q[v], Q[v]);
       }
 #pragma unroll
-    for (int j = STEPS - 1; j >= 0; --j)
+    for (int j = STEPS - 1; j >= 0; --j) {
+      float dh[VEC];
+      widen<T, VEC>(d[j], dh);
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        const float s = d[j][v] + G[v];
+        const float s = dh[v] + G[v];
         G[v] = fmaf(-b[j][v], s, s);
       }
+    }
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       maps.v[k & 1][0][w][v][threadIdx.x] = Q[v];
@@ -318,13 +361,18 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
     lds_barrier();
     float from[VEC];
 #pragma unroll
-    for (int i = WAVES - 1; i >= 0; --i)
+    for (int i = 0; i < WAVES; ++i)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        if (i == w) from[v] = g[v];
-        const float Qi = maps.v[k & 1][0][i][v][threadIdx.x];
-        g[v] += fmaf(-Qi, g[v], maps.v[k & 1][1][i][v][threadIdx.x]);
-        if (MAPS) q[v] = fmaf(Qi, 1.f - q[v], q[v]);
+        const int wave = MAPS ? i : WAVES - 1 - i;
+        const float Qi = maps.v[k & 1][0][wave][v][threadIdx.x], Gi = maps.v[k & 1][1][wave][v][threadIdx.x];
+        if (MAPS) { // the map of later steps comes first
+          g[v] += fmaf(-q[v], Gi, Gi);
+          q[v] = fmaf(q[v], 1.f - Qi, Qi);
+        } else {
+          if (wave == w) from[v] = g[v];
+          g[v] += fmaf(-Qi, g[v], Gi);
+        }
       }
     if (MAPS) continue;
 #pragma unroll
@@ -340,20 +388,27 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
         h[v] = fmaf(b[j][v], off, h[v]);
         x[j][v] = off;
       }
+    if (me.on) {
+      const __amdgpu_buffer_rsrc_t to_dz = pdz.from(t0), to_dx = pdx.from(t0);
+      either(whole, [&](auto known) {
+        constexpr bool ALL = decltype(known)::value;
 #pragma unroll
-    for (int j = STEPS - 1; j >= 0; --j) {
-      float dz[VEC], dx[VEC];
+        for (int j = STEPS - 1; j >= 0; --j) {
+          float dh[VEC], dz[VEC], dx[VEC];
+          widen<T, VEC>(d[j], dh);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        const float s = d[j][v] + from[v];
-        dx[v] = b[j][v] * s;
-        from[v] = fmaf(-b[j][v], s, s);
-        dz[v] = j < live ? (b[j][v] - 1.f) * dx[v] * x[j][v] : 0.f; // (0 whatever the state)
-      }
-      if (t0 + j < a.T && me.on) {
-        pdz.of<R>(t0 + j) = narrow<T, VEC>(dz);
-        pdx.of<R>(t0 + j) = narrow<T, VEC>(dx);
-      }
+          for (int v = 0; v < VEC; ++v) {
+            const float s = dh[v] + from[v];
+            dx[v] = b[j][v] * s;
+            from[v] = fmaf(-b[j][v], s, s);
+            dz[v] = ALL || j < live ? (b[j][v] - 1.f) * dx[v] * x[j][v] : 0.f; // (0 whatever the state)
+          }
+          if (ALL || t0 + j < a.T) {
+            pdz.store(to_dz, j, narrow<T, VEC>(dz));
+            pdx.store(to_dx, j, narrow<T, VEC>(dx));
+          }
+        }
+      });
     }
   }
   if (w == 0 && me.on)
@@ -364,16 +419,23 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
     }
 }
 
-// Tiles of 128 steps per segment.  One workgroup per group of channels walks the whole sequence, unless that leaves compute units
-// without work: the sequence is then cut so that each has two workgroups, at the price of a launch before that finds the
-// segments' maps (z and x, or dh, are read twice).
-constexpr int WORKGROUPS = 512;
+// From WHOLE groups of channels on, one workgroup per group walks the whole sequence: z and x are read once.  Fewer would leave too many
+// compute units without work: the sequence is then cut into segments so that there are WORKGROUPS in all, at the price of a launch before
+// that finds the segments' maps (z and x, or dh, are read twice).
+constexpr int WHOLE = 160, WORKGROUPS = 512;
+int groups_of(int channels, int vec) { return (channels + 64 * vec - 1) / (64 * vec); }
 void cut(Args *a, int vec) {
-  const int groups = (a->channels + 64 * vec - 1) / (64 * vec);
-  const int want = (WORKGROUPS + groups - 1) / groups;
+  const int groups = groups_of(a->channels, vec);
+  const int want = groups >= WHOLE ? 1 : (WORKGROUPS + groups - 1) / groups;
   a->tiles = (a->T + SNN_GLR_INTERVAL - 1) / SNN_GLR_INTERVAL;
   a->seg_tiles = a->tiles ? (a->tiles + want - 1) / want : 1;
   a->segments = a->tiles ? (a->tiles + a->seg_tiles - 1) / a->seg_tiles : 1;
+}
+// Two channels per lane in bf16, unless one per lane makes enough groups to walk the sequence whole and two do not
+// (16384 channels, 4096 steps: 84 us instead of 111).
+bool two_per_lane(const GlrShape &p) {
+  const int channels = p.batch * p.n;
+  return p.bf16 && p.n % 2 == 0 && (groups_of(channels, 2) >= WHOLE || groups_of(channels, 1) < WHOLE);
 }
 
 Args shape_args(const GlrShape &p) {
@@ -427,7 +489,7 @@ template <typename T, typename P, int VEC> hipError_t backward(Args a, hipStream
 
 size_t glr_workspace(const GlrShape &p) {
   Args a = shape_args(p);
-  cut(&a, p.bf16 ? 2 : 1); // (one element per lane: no more segments than with two)
+  cut(&a, two_per_lane(p) ? 2 : 1); // (arrays not aligned to pairs take one per lane all the same: no more segments than with two)
   return a.segments > 1 ? (size_t)(a.segments + 1) * a.channels * sizeof(float2) : 0;
 }
 
@@ -442,7 +504,7 @@ hipError_t launch_glr_forward(const GlrShape &p, const void *z, const void *x, c
   a.kept = kept;
   a.maps = (float2 *)work;
   if (!p.bf16) return forward<float, 1>(a, s);
-  const bool two = (p.n & 1) == 0 && pairs(z, 2, p.ld_z) && pairs(x, 2, p.ld_x) && pairs(h, 2, p.ld_h);
+  const bool two = two_per_lane(p) && pairs(z, 2, p.ld_z) && pairs(x, 2, p.ld_x) && pairs(h, 2, p.ld_h);
   return two ? forward<__bf16, 2>(a, s) : forward<__bf16, 1>(a, s);
 }
 
@@ -469,7 +531,7 @@ hipError_t launch_glr_backward(const GlrShape &p, const GlrInputs &in, const flo
   }
   if (!p.bf16) return packed ? backward<float, int8_t, 1>(a, s) : backward<float, float, 1>(a, s);
   const size_t size = packed ? 1 : 2;
-  const bool two = (p.n & 1) == 0 && pairs(in.z, size, a.ld_z) && pairs(in.x, size, a.ld_x) && pairs(dh, 2, p.ld_h) &&
+  const bool two = two_per_lane(p) && pairs(in.z, size, a.ld_z) && pairs(in.x, size, a.ld_x) && pairs(dh, 2, p.ld_h) &&
                    pairs(dz, 2, p.ld_dz) && pairs(dx, 2, p.ld_dx);
   if (packed) return two ? backward<__bf16, int8_t, 2>(a, s) : backward<__bf16, int8_t, 1>(a, s);
   return two ? backward<__bf16, __bf16, 2>(a, s) : backward<__bf16, __bf16, 1>(a, s);

@@ -72,18 +72,18 @@ bool dtype_ok(int dtype) { return dtype == SNN_F32 || dtype == SNN_BF16; }
     if (s_ != SNN_OK) return s_;       \
   } while (0)
 
-// Steps have less than 2^31 channels and rows less than 2^32 bytes apart from the first to the last of a step.
+constexpr long long STEP_BYTES = 1 << 27; // of one step of an array, so that offsets inside 16 steps fit 32 bits
 snn_status glr_shape(const char *what, const snn_glr *p, GlrShape *g) {
   if (!p) return refuse(SNN_E_INVAL, "%s: no shape", what);
   if (!dtype_ok(p->dtype)) return refuse(SNN_E_INVAL, "%s: unknown type %d", what, p->dtype);
   if (p->T < 0 || p->T > (1 << 30)) return refuse(SNN_E_INVAL, "%s: T = %d", what, p->T);
-  if (p->batch < 1 || p->n < 1 || (long long)p->batch * p->n > (1 << 30))
-    return refuse(SNN_E_INVAL, "%s: batch %d, n %d: 1 .. 2^30 channels in all", what, p->batch, p->n);
+  if (p->batch < 1 || p->n < 1 || (long long)p->batch * p->n > STEP_BYTES / 4)
+    return refuse(SNN_E_INVAL, "%s: batch %d, n %d: 1 .. 2^25 channels in all", what, p->batch, p->n);
   *g = GlrShape{p->T, p->batch, p->n, p->dtype == SNN_BF16, p->ld_z, p->ld_x, p->ld_h, p->ld_dz, p->ld_dx, p->lengths};
   for (long long *ld : {&g->ld_z, &g->ld_x, &g->ld_h, &g->ld_dz, &g->ld_dx}) {
     if (!*ld) *ld = p->n;
-    if (*ld < p->n || *ld > (1ll << 31) / p->batch / (long long)size_of(p->dtype))
-      return refuse(SNN_E_INVAL, "%s: %lld elements from row to row: n or more, and 2^31 bytes per step at most", what, *ld);
+    if (*ld < p->n || *ld > STEP_BYTES / p->batch / (long long)size_of(p->dtype))
+      return refuse(SNN_E_INVAL, "%s: %lld elements from row to row: n or more, and 2^27 bytes per step at most", what, *ld);
   }
   return SNN_OK;
 }
@@ -173,7 +173,7 @@ snn_status snn_glr_backward_packed(const snn_launch *at, const snn_glr *p, const
   for (long long *ld : {&in.ld_z, &in.ld_x, &in.ld_ze, &in.ld_xe}) {
     const int64_t least = ld == &in.ld_z || ld == &in.ld_x ? p->n : bytes;
     if (!*ld) *ld = least;
-    if (*ld < least || (p->batch > 0 && *ld > (1ll << 31) / p->batch))
+    if (*ld < least || (p->batch > 0 && *ld > STEP_BYTES / p->batch))
       return refuse(SNN_E_INVAL, "%s: %lld codes or exponents from row to row", what, *ld);
   }
   if (p->T <= 0) in = GlrInputs{};
