@@ -100,12 +100,12 @@ struct Rows {
   __device__ __forceinline__ __amdgpu_buffer_rsrc_t from(int t) const {
     return __builtin_amdgcn_make_buffer_rsrc(base + (unsigned long long)t * step, 0, (int)0xffffffff, 0x00020000);
   }
-  // 16 steps from t0 on.  Steps at and past T are those of the last one again (and not used).
-  template <typename R> __device__ __forceinline__ void load(R (&r)[STEPS], int t0, int T) const {
+  // N steps from t0 on.  Steps at and past T are those of the last one again (and not used).
+  template <typename R, int N> __device__ __forceinline__ void load(R (&r)[N], int t0, int T) const {
     const int first = min(t0, T - 1), last = T - 1 - first;
     const __amdgpu_buffer_rsrc_t from_first = from(first);
 #pragma unroll
-    for (int j = 0; j < STEPS; ++j) {
+    for (int j = 0; j < N; ++j) {
       const int at_step = (int)(min(j, last) * step);
       if constexpr (sizeof(R) == 4) r[j] = __builtin_amdgcn_raw_buffer_load_b32(from_first, (int)at, at_step, 0);
       else if constexpr (sizeof(R) == 2) r[j] = __builtin_amdgcn_raw_buffer_load_b16(from_first, (int)at, at_step, 0);
@@ -124,8 +124,9 @@ struct Rows {
 template <int VEC, int N> struct Maps { float v[2][N][WAVES][VEC][64]; };
 
 // Forward pass of one segment (blockIdx.y) of tiles.  MAPS: only the segment's map into maps[segment + 1], nothing stored; else the
-// state at its beginning comes from the maps before it.  NW = 1: sequences of up to 16 steps, one wavefront each.
-template <typename T, int VEC, int NW, bool MAPS>
+// state at its beginning comes from the maps before it.  NW = 1: sequences of up to
+// S steps, one wavefront each.
+template <typename T, int VEC, int NW, int S, bool MAPS>
 __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
   __shared__ Maps<VEC, 2> maps;
   typedef typename Raw<T, VEC>::type R;
@@ -155,22 +156,22 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
 #pragma unroll
   for (int v = 0; v < VEC; ++v) asm volatile("" ::"v"(h[v]));
   // (the map of a segment is put together from its end, its states are found from its beginning: what was read last is read first again)
-  R rz[STEPS], rx[STEPS];
-  constexpr int STRIDE = MAPS ? -NW * STEPS : NW * STEPS;
-  int t0 = ((MAPS ? k1 - 1 : k0) * NW + w) * STEPS;
+  R rz[S], rx[S];
+  constexpr int STRIDE = MAPS ? -NW * S : NW * S;
+  int t0 = ((MAPS ? k1 - 1 : k0) * NW + w) * S;
   if (k0 < k1) {
     pz.load(rz, t0, a.T);
     px.load(rx, t0, a.T);
   }
   int n = k1 - k0, k = MAPS ? k1 - 1 : k0;
   for (; n > 0; --n, MAPS ? --k : ++k, t0 += STRIDE) {
-    float b[STEPS][VEC], x[STEPS][VEC];
+    float b[S][VEC], x[S][VEC];
     const int live = me.len - t0; // steps of these 16 that the sequence has
-    const bool whole = __all(live >= STEPS);
+    const bool whole = __all(live >= S);
     either(whole, [&](auto known) {
       constexpr bool ALL = decltype(known)::value;
 #pragma unroll
-      for (int j = 0; j < STEPS; ++j) {
+      for (int j = 0; j < S; ++j) {
         float z[VEC];
         widen<T, VEC>(rz[j], z);
         widen<T, VEC>(rx[j], x[j]);
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
     if (NW > 1) {
       float Q[VEC] = {}, B[VEC] = {};
 #pragma unroll
-      for (int j = 0; j < STEPS; ++j)
+      for (int j = 0; j < S; ++j)
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
           B[v] = fmaf(b[j][v], x[j][v] - B[v], B[v]);
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
       either(whole, [&](auto known) {
         constexpr bool ALL = decltype(known)::value;
 #pragma unroll
-        for (int j = 0; j < STEPS; ++j) {
+        for (int j = 0; j < S; ++j) {
           float out[VEC];
 #pragma unroll
           for (int v = 0; v < VEC; ++v) {
@@ -460,16 +461,17 @@ template <typename T, int VEC> hipError_t forward(Args a, hipStream_t s) {
   if (a.T <= STEPS) {
     a.tiles = a.T > 0;
     a.seg_tiles = a.segments = 1;
-    k_glr_forward<T, VEC, 1, false><<<groups, dim3(64, 1), 0, s>>>(a);
+    if (a.T == 1) k_glr_forward<T, VEC, 1, 1, false><<<groups, 64, 0, s>>>(a);
+    else k_glr_forward<T, VEC, 1, STEPS, false><<<groups, 64, 0, s>>>(a);
     return hipGetLastError();
   }
   cut(&a, VEC);
   if (a.segments > 1) {
-    k_glr_forward<T, VEC, WAVES, true><<<dim3(groups.x, a.segments - 1), dim3(64, WAVES), 0, s>>>(a);
+    k_glr_forward<T, VEC, WAVES, STEPS, true><<<dim3(groups.x, a.segments - 1), dim3(64, WAVES), 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  k_glr_forward<T, VEC, WAVES, false><<<dim3(groups.x, a.segments), dim3(64, WAVES), 0, s>>>(a);
+  k_glr_forward<T, VEC, WAVES, STEPS, false><<<dim3(groups.x, a.segments), dim3(64, WAVES), 0, s>>>(a);
   return hipGetLastError();
 }
 

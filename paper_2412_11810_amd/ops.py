@@ -59,17 +59,22 @@ def declare(L):
         getattr(L, name).restype = C.c_int
 
 
-def _lib():
-    from . import lib
-    return lib()
+_functions = {}  # entry points, by name
+
+
+def _entry(name):
+    f = _functions.get(name)
+    if f is None:
+        from . import lib
+        f = _functions[name] = getattr(lib(), name)
+    return f
 
 
 def _run(name, *args):
-    from . import SNN_OK, SnnError
-    L = _lib()
-    st = getattr(L, name)(*args)
-    if st != SNN_OK:
-        raise SnnError(st, L.snn_launch_error().decode())
+    st = _entry(name)(*args)
+    if st:
+        from . import SnnError
+        raise SnnError(st, _entry("snn_launch_error")().decode())
 
 
 def _type(x, name):
@@ -100,6 +105,8 @@ def _packed_rows(x, name):
 
 def _ld(x, name):
     """Elements between consecutive rows of [..., n], if every row follows the one before at the same distance."""
+    if x.is_contiguous():
+        return x.shape[-1]
     ld = None
     rows = 1
     if x.shape[-1] > 1 and x.stride(-1) != 1:
@@ -121,8 +128,11 @@ def _launch(device, work=0):
     import torch
     if device.type != "cuda":
         raise ValueError(f"the operators run on a GPU, got tensors on {device}")
-    space = torch.empty(work, dtype=torch.uint8, device=device) if work else None
-    return snn_launch(device.index, torch.cuda.current_stream(device).cuda_stream, space.data_ptr() if work else None, work), space
+    stream = torch._C._cuda_getCurrentRawStream(device.index)  # (torch.cuda.current_stream makes an object first)
+    if not work:
+        return snn_launch(device.index, stream, None, 0), None
+    space = torch.empty(work, dtype=torch.uint8, device=device)
+    return snn_launch(device.index, stream, space.data_ptr(), work), space
 
 
 def _at(x):
@@ -139,7 +149,7 @@ def _out(x, name, like):
     """x as the result `name`, or a new tensor for it."""
     import torch
     if x is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
     return _same(x, name, like.dtype, like.shape, like.device)
 
 
@@ -163,7 +173,7 @@ def snn_glr_forward(z, x, h0=None, lengths=None, keep=False, h=None, h_last=None
         _packed_rows(_same(h0, "h0", torch.float32, (batch, n), device), "h0")
     h = _out(h, "h", z)
     p = _glr_shape(dtype, T, batch, n, (_ld(z, "z"), _ld(x, "x"), _ld(h, "h"), 0, 0), lengths, device)
-    at, space = _launch(device, _lib().snn_glr_workspace(C.byref(p)))
+    at, space = _launch(device, _entry("snn_glr_workspace")(C.byref(p)))
     if h_last is None:
         h_last = torch.empty((batch, n), dtype=torch.float32, device=device)
     else:
@@ -199,7 +209,7 @@ def snn_glr_backward(z, x, kept, dh, dh_last=None, lengths=None, dz=None, dx=Non
     dz, dx = _out(dz, "dz", dh), _out(dx, "dx", dh)
     dh0 = torch.empty((batch, n), dtype=torch.float32, device=device)
     p = _glr_shape(dtype, T, batch, n, (*lds, _ld(dh, "dh"), _ld(dz, "dz"), _ld(dx, "dx")), lengths, device)
-    at, space = _launch(device, _lib().snn_glr_workspace(C.byref(p)))
+    at, space = _launch(device, _entry("snn_glr_workspace")(C.byref(p)))
     _run("snn_glr_backward_packed" if packed else "snn_glr_backward", C.byref(at), C.byref(p), *inputs, _at(kept), _at(dh), _at(dh_last),
          _at(dz), _at(dx), _at(dh0))
     return dz, dx, dh0
@@ -250,7 +260,7 @@ def snn_vocab_loss(h, w, targets):
     Returns the losses [rows] (float32) and the state [rows][3] that snn_vocab_loss_grad takes."""
     import torch
     p = _vocab_shape(h, w, targets)
-    at, space = _launch(h.device, _lib().snn_vocab_workspace(C.byref(p), 0))
+    at, space = _launch(h.device, _entry("snn_vocab_workspace")(C.byref(p), 0))
     loss = torch.empty(p.rows, dtype=torch.float32, device=h.device)
     state = torch.empty((p.rows, 3), dtype=torch.float32, device=h.device)
     _run("snn_vocab_loss", C.byref(at), C.byref(p), _at(h), _at(w), _at(targets), _at(loss), _at(state))
@@ -264,7 +274,7 @@ def snn_vocab_loss_grad(h, w, targets, state, dloss=None):
     _packed_rows(_same(state, "state", torch.float32, (p.rows, 3), h.device), "state")
     if dloss is not None:
         _packed_rows(_same(dloss, "dloss", torch.float32, (p.rows,), h.device), "dloss")
-    at, space = _launch(h.device, _lib().snn_vocab_workspace(C.byref(p), 1))
+    at, space = _launch(h.device, _entry("snn_vocab_workspace")(C.byref(p), 1))
     dh = torch.empty((p.rows, p.d), dtype=h.dtype, device=h.device)
     dw = torch.empty((p.vocab, p.d), dtype=h.dtype, device=h.device)
     _run("snn_vocab_loss_grad", C.byref(at), C.byref(p), _at(h), _at(w), _at(targets), _at(state), _at(dloss), _at(dh), _at(dw))
