@@ -56,12 +56,14 @@ struct Stage {
 // lines of a row, eight chunks; chunk c of row r is at place c ^ (r / 2 % 8), so that 16 lanes of a fragment, which read one
 // chunk of as many rows, use all 64 banks).  Loads go past the registers, a step ahead.  The fragments of the next quarter of a step are
 // on their way while those of this one are multiplied, also across the barrier between two steps: matrix instructions wait for nothing
-// but loads that take longer than a step.
+// but loads that take longer than a step.  (Tiles with 64 rows on a side, of which there are few and which are soon multiplied, hold four
+// steps: their loads are three ahead.)
 template <int BM, int BN, int WA, int WB, int PARTS, class Epilogue>
 __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
   constexpr int MI = BM / WA / 32, NI = BN / WB / 32, LA = BM / 64, LB = BN / 64, QUARTERS = BK / 16;
-  constexpr int SEGS = PARTS == 1 ? 1 : 6;
+  constexpr int SEGS = PARTS == 1 ? 1 : 6, HELD = BM == 64 || BN == 64 ? 4 : 2;
   __shared__ __align__(16) char a0[BM * 128], b0[BN * 128], a1[BM * 128], b1[BN * 128];
+  __shared__ __align__(16) char a2[HELD > 2 ? BM * 128 : 16], b2[HELD > 2 ? BN * 128 : 16], a3[HELD > 2 ? BM * 128 : 16], b3[HELD > 2 ? BN * 128 : 16];
   // tiles in the order of the dies: consecutive workgroups are on different ones, each die takes a run of tiles, in groups of eight
   // along A that share the rows of B
   const unsigned n = p.tiles_a * p.tiles_b, per = n / 8, rest = n % 8;
@@ -110,9 +112,12 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
       for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s & 1][i], fb[s & 1][j], acc[i][j], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
-  // every load of every wavefront is in LDS, and every wavefront has what it read before
-  auto arrived = [&]() {
-    __builtin_amdgcn_s_waitcnt(0x0070);
+  // the next step is in LDS for every wavefront, and every wavefront has what it read before; `later`: the steps behind it may be under way
+  auto arrived = [&](bool later) {
+    constexpr int LATER = (HELD - 2) * (LA + LB);
+    static_assert(LATER < 16, "the count of loads under way");
+    if (later) __builtin_amdgcn_s_waitcnt(0x0070 | LATER);
+    else __builtin_amdgcn_s_waitcnt(0x0070);
     asm volatile("" ::: "memory"); // (the compiler knows of no store to LDS here)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -125,8 +130,8 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
       multiply(s);
     }
     if (more || left > 1) {
-      arrived();
-      if (more || left > 2) fetch(la, lb);
+      arrived(more || left >= HELD);
+      if (more || left > HELD) fetch(la, lb);
       read(0, na, nb);
     }
     multiply(QUARTERS - 1);
@@ -134,15 +139,38 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
   };
   fetch(a0, b0);
   if (left > 1) fetch(a1, b1);
-  arrived();
-  read(0, a0, b0);
-  while (left > 3) {
-    step(a0, b0, a1, b1, true);
-    step(a1, b1, a0, b0, true);
+  if constexpr (HELD > 2) {
+    if (left > 2) fetch(a2, b2);
+    if (left > 3) fetch(a3, b3);
   }
-  step(a0, b0, a1, b1, false);
-  if (left) step(a1, b1, a0, b0, false);
-  if (left) step(a0, b0, a1, b1, false);
+  arrived(false);
+  read(0, a0, b0);
+  if constexpr (HELD > 2) {
+    while (left > 7) {
+      step(a0, b0, a1, b1, true);
+      step(a1, b1, a2, b2, true);
+      step(a2, b2, a3, b3, true);
+      step(a3, b3, a0, b0, true);
+    }
+    for (;;) {
+      step(a0, b0, a1, b1, false);
+      if (!left) break;
+      step(a1, b1, a2, b2, false);
+      if (!left) break;
+      step(a2, b2, a3, b3, false);
+      if (!left) break;
+      step(a3, b3, a0, b0, false);
+      if (!left) break;
+    }
+  } else {
+    while (left > 3) {
+      step(a0, b0, a1, b1, true);
+      step(a1, b1, a0, b0, true);
+    }
+    step(a0, b0, a1, b1, false);
+    if (left) step(a1, b1, a0, b0, false);
+    if (left) step(a0, b0, a1, b1, false);
+  }
   __syncthreads();
   // element e of a tile: row 8 (e / 4) + 4 half + e % 4 of A, row r of B.  Every wavefront is through with the tiles in LDS
   constexpr bool OF_A = BM >= BN;
@@ -150,6 +178,7 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
   ep.template finish<MI, NI>(acc, ta * BM + wa * (BM / WA), tb * BN + wb * (BN / WB), slice, stage);
 }
 
+__device__ __forceinline__ bool has_target(const int *targets, int m, bool on, int vocab) { return on && targets[m] >= 0 && targets[m] < vocab; }
 // Row m's target, counted from entry v0 on; -1: none, or one before v0
 __device__ __forceinline__ int entry(const int *targets, int m, bool on, int vocab, int v0) {
   const int y = on ? targets[m] : -1;
@@ -206,7 +235,7 @@ struct LossEpilogue {
 template <int PARTS> struct GradEpilogue {
   static constexpr bool LOGITS = true;
   const int *targets;
-  const float *state, *scale; // scale [rows padded]: dloss, 0 for rows without a target
+  const float *state, *dloss, *mean; // dloss [rows], or NULL: mean[0] for each row with a target
   __bf16 *gm, *gt;            // [PARTS][rows padded][width], [PARTS][width][rows padded]
   int first, vocab, rows, width, padded;
   template <int MI, int NI> __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int v0, int m0, int, const Stage &st) const {
@@ -217,7 +246,7 @@ template <int PARTS> struct GradEpilogue {
       const int m = m0 + j * 32 + r;
       const bool on = m < rows;
       const int y = entry(targets, m, on, vocab, first + v0 + 4 * half), left = vocab - first - v0 - 4 * half;
-      const float g = on ? scale[m] : 0.f, top = on ? state[3 * m] : 0.f, per = on ? state[3 * m + 1] * g : 0.f;
+      const float g = has_target(targets, m, on, vocab) ? (dloss ? dloss[m] : *mean) : 0.f, top = on ? state[3 * m] : 0.f, per = on ? state[3 * m + 1] * g : 0.f;
       const float miss = on ? state[3 * m + 2] : 0.f;
       const bool none = g == 0.f; // no part in the gradients, whatever its logits
 #pragma unroll
@@ -350,12 +379,12 @@ template <int PARTS, class Epilogue> hipError_t product(Product p, const Epilogu
   return hipGetLastError();
 }
 
-// A product with fewer tiles than half the compute units is cut along its sums, eight steps of 64 or more each; the slices are added up
-// afterwards, in order.
+// A product with fewer tiles than half the compute units is cut along its sums, eight steps of 64 (of which parts take six each) or more;
+// the slices are added up afterwards, in order.
 struct Slices {
   int count, steps;
-  Slices(int rows_a, int rows_b, int ksteps, int at_most = 256) {
-    const int most = 256 / tiles(rows_a, rows_b), fit = ksteps / 8, n = most < fit ? most : fit;
+  Slices(int rows_a, int rows_b, int ksteps, int parts, int at_most = 256) {
+    const int most = 256 / tiles(rows_a, rows_b), fit = ksteps * (parts == 1 ? 1 : 6) / 8, n = most < fit ? most : fit;
     count = n < 1 ? 1 : n < at_most ? n : at_most;
     steps = (ksteps + count - 1) / count;
     count = (ksteps + steps - 1) / steps;
@@ -372,30 +401,85 @@ template <int PARTS> __device__ __forceinline__ void split(float x, uint16_t (&p
     x -= __uint_as_float(bits);
   }
 }
-// to[part][row][padded cols] = parts of from[row][cols]; zeros behind a row's end
-template <typename T, int PARTS>
-__global__ __launch_bounds__(256) void k_rows(const T *from, long long ld, int rows, int cols, __bf16 *to, int padded) {
-  const int c = blockIdx.x * 256 + threadIdx.x, r = blockIdx.y + blockIdx.z * 65535;
-  if (c >= padded || r >= rows) return;
-  uint16_t part[PARTS];
-  split(c < cols ? (float)from[r * ld + c] : 0.f, part);
+// One matrix on its way into products: its rows in parts [PARTS][rows][padded cols], zeros behind their ends, and its columns in parts
+// [PARTS][cols][padded rows], zeros behind the last row (either may be NULL).  With targets, rows that have none or whose dloss is 0 are
+// zeros in the columns: what they hold (padding: anything) would else meet the zeros of G as 0 * NaN.
+struct Operand {
+  const void *from;
+  long long ld;
+  int rows, cols, padded_cols, padded_rows;
+  __bf16 *to_rows, *to_cols;
+  const int *targets;
+  const float *dloss;
+  int vocab, tiles_c;
+  unsigned tiles;
+};
+// 64 by 64 elements per workgroup, four in a row per thread, through LDS for the columns.  The last workgroup finds 1 / number of rows with a
+// target, where that is asked for.
+template <typename T, int PARTS> __global__ __launch_bounds__(256) void k_operands(Operand x, Operand y, const int *targets, int rows, int vocab, float *mean) {
+  __shared__ float tile[64][65];
+  unsigned id = blockIdx.x;
+  if (id >= x.tiles + y.tiles) {
+    int count = 0;
+    for (int m = threadIdx.x; m < rows; m += 256) count += has_target(targets, m, true, vocab);
+    int *const counts = (int *)tile;
 #pragma unroll
-  for (int k = 0; k < PARTS; ++k) *(uint16_t *)(to + ((size_t)k * rows + r) * padded + c) = part[k];
-}
-// to[part][col][padded rows] = parts of from[row][col]; zeros behind the last row and, where `scale` is given, for the rows whose
-// scale is 0: what they hold (padding: anything) would else meet the zeros of G as 0 * NaN
-template <typename T, int PARTS>
-__global__ __launch_bounds__(256) void k_columns(const T *from, long long ld, int rows, int cols, const float *scale, __bf16 *to, int padded) {
-  __shared__ T tile[64][65];
-  const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 64, l = threadIdx.x & 63, g = threadIdx.x >> 6;
-  for (int i = g; i < 64; i += 4) tile[i][l] = r0 + i < rows && c0 + l < cols && !(scale && scale[r0 + i] == 0.f) ? from[(r0 + i) * ld + c0 + l] : (T)0.f;
+    for (int k = 32; k; k >>= 1) count += __shfl_xor(count, k);
+    if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = count;
+    __syncthreads();
+    if (threadIdx.x == 0) *mean = 1.f / (counts[0] + counts[1] + counts[2] + counts[3]);
+    return;
+  }
+  const bool second = id >= x.tiles;
+  if (second) id -= x.tiles;
+  const Operand &m = second ? y : x;
+  const int c0 = (int)(id % (unsigned)m.tiles_c) * 64, r0 = (int)(id / (unsigned)m.tiles_c) * 64, four = (threadIdx.x & 15) * 4, line = threadIdx.x >> 4;
+  const T *const from = (const T *)m.from;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = r0 + i * 16 + line, c = c0 + four;
+    float v[4] = {};
+    if (r < m.rows) {
+      const T *const at = from + r * m.ld + c;
+      if (c + 4 <= m.cols) {
+        if constexpr (sizeof(T) == 4) {
+          const words4 q = *(const words4_any *)at;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(q[e]);
+        } else {
+          const words2 q = *(const words2_any *)at;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(e & 1 ? q[e >> 1] & 0xffff0000u : q[e >> 1] << 16);
+        }
+      } else
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < m.cols) v[e] = (float)at[e];
+    }
+    if (m.to_rows && r < m.rows && c < m.padded_cols) {
+      uint16_t part[4][PARTS];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) split(v[e], part[e]);
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k)
+        *(uint2 *)(m.to_rows + ((size_t)k * m.rows + r) * m.padded_cols + c) = make_uint2(part[0][k] | (uint32_t)part[1][k] << 16, part[2][k] | (uint32_t)part[3][k] << 16);
+    }
+    const bool none = m.targets && r < m.rows && (!has_target(m.targets, r, true, m.vocab) || (m.dloss && m.dloss[r] == 0.f));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tile[i * 16 + line][four + e] = none ? 0.f : v[e];
+  }
+  if (!m.to_cols) return;
   __syncthreads();
-  for (int i = g; i < 64; i += 4) {
-    if (c0 + i >= cols || r0 + l >= padded) continue;
-    uint16_t part[PARTS];
-    split((float)tile[l][i], part);
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k) *(uint16_t *)(to + ((size_t)k * cols + c0 + i) * padded + r0 + l) = part[k];
+  for (int i = 0; i < 4; ++i) {
+    const int c = c0 + i * 16 + line, r = r0 + four;
+    if (c >= m.cols || r >= m.padded_rows) continue;
+    uint16_t part[4][PARTS];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) split(tile[four + e][i * 16 + line], part[e]);
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k)
+      *(uint2 *)(m.to_cols + ((size_t)k * m.cols + c) * m.padded_rows + r) = make_uint2(part[0][k] | (uint32_t)part[1][k] << 16, part[2][k] | (uint32_t)part[3][k] << 16);
   }
 }
 
@@ -442,25 +526,6 @@ __global__ __launch_bounds__(1024) void k_join(const float2 *part, const float *
   state[3 * m + 2] = miss;
 }
 
-// scale[m] = the gradient of row m's loss, without one given that of their mean: 0 for rows without a target and for the padding
-__global__ __launch_bounds__(1024) void k_scale(const int *targets, const float *dloss, int rows, int padded, int vocab, float *scale) {
-  __shared__ int counts[16];
-  int count = 0;
-  if (!dloss) {
-    for (int m = threadIdx.x; m < rows; m += 1024) count += targets[m] >= 0 && targets[m] < vocab;
-#pragma unroll
-    for (int k = 32; k; k >>= 1) count += __shfl_xor(count, k);
-    if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = count;
-    __syncthreads();
-    count = 0;
-    for (int i = 0; i < 16; ++i) count += counts[i];
-  }
-  for (int m = threadIdx.x; m < padded; m += 1024) {
-    const bool has = m < rows && targets[m] >= 0 && targets[m] < vocab;
-    scale[m] = !has ? 0.f : dloss ? dloss[m] : 1.f / count;
-  }
-}
-
 // to = the sum of the slices, each n elements
 template <typename T> __global__ __launch_bounds__(256) void k_sum(const float *from, int slices, size_t n, T *to) {
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
@@ -476,7 +541,7 @@ __global__ __launch_bounds__(256) void k_clear(uint16_t *to, size_t n) {
 // ---- workspace ------------------------------------------------------------------------------
 struct Space {
   int parts, dp, padded, width; // width: entries of a piece of the vocabulary
-  size_t h, w, part, picked, scale, ht, wt, gm, gt, sum_h, sum_w, bytes;
+  size_t h, w, part, picked, mean, ht, wt, gm, gt, sum_h, sum_w, bytes;
   Space(const VocabShape &p, bool grad) {
     parts = p.bf16 ? 1 : 3;
     dp = (p.d + BK - 1) / BK * BK;
@@ -494,12 +559,12 @@ struct Space {
       part = take(sizeof(float2) * (size_t)(all / (few(p.rows) ? 32 : 128)) * p.rows);
       picked = take(sizeof(float) * (size_t)p.rows);
     } else {
-      scale = take(sizeof(float) * (size_t)padded);
+      mean = take(sizeof(float));
       ht = take((size_t)2 * parts * p.d * padded);
       wt = take((size_t)2 * parts * p.d * width);
       gm = take((size_t)2 * parts * padded * width);
       gt = take((size_t)2 * parts * padded * width);
-      const Slices sh(p.rows, p.d, width / BK), sw(width < p.vocab ? width : p.vocab, p.d, padded / BK);
+      const Slices sh(p.rows, p.d, width / BK, parts), sw(width < p.vocab ? width : p.vocab, p.d, padded / BK, parts);
       sum_h = take(width < p.vocab || sh.count > 1 ? sizeof(float) * (size_t)sh.count * p.rows * p.d : 0);
       // (the last piece may be so much narrower that it is cut further: no more than 256 tiles in all)
       sum_w = take(sw.count > 1 || width < p.vocab ? sizeof(float) * 256 * (size_t)256 * 256 : 0);
@@ -514,43 +579,45 @@ struct Space {
     if (e_ != hipSuccess) return e_;              \
   } while (0)
 
-// Rows as the products take them: where they are, if they are bf16, aligned and whole; else copied into `to`.
-template <typename T, int PARTS>
-hipError_t rows_of(const T *from, long long ld, int rows, int cols, int padded, __bf16 *to, const __bf16 **out, long long *out_ld,
-                   hipStream_t s) {
-  if (sizeof(T) == 2 && cols % BK == 0 && ld % 8 == 0 && (uintptr_t)from % 16 == 0) {
-    *out = (const __bf16 *)from;
-    *out_ld = ld;
-    return hipSuccess;
-  }
-  *out = to;
-  *out_ld = padded;
-  const dim3 grid((padded + 255) / 256, rows < 65535 ? rows : 65535, (rows + 65534) / 65535);
-  k_rows<T, PARTS><<<grid, 256, 0, s>>>(from, ld, rows, cols, to, padded);
-  return hipGetLastError();
+// Whether rows can go into products from where they are: bf16, aligned and whole.
+template <typename T> bool direct(const T *from, long long ld, int cols) { return sizeof(T) == 2 && cols % BK == 0 && ld % 8 == 0 && (uintptr_t)from % 16 == 0; }
+
+template <typename T> Operand operand(const T *from, long long ld, int rows, int cols, int padded_cols, __bf16 *to_rows, int padded_rows, __bf16 *to_cols) {
+  Operand m = {from, ld, rows, cols, padded_cols, padded_rows, to_rows, to_cols, nullptr, nullptr, 0, 0, 0};
+  m.tiles_c = (padded_cols + 63) / 64;
+  m.tiles = to_rows || to_cols ? (unsigned)m.tiles_c * ((unsigned)((to_cols ? padded_rows : rows) + 63) / 64u) : 0;
+  return m;
 }
-template <typename T, int PARTS>
-hipError_t columns_of(const T *from, long long ld, int rows, int cols, int padded, const float *scale, __bf16 *to, hipStream_t s) {
-  k_columns<T, PARTS><<<dim3((cols + 63) / 64, (padded + 63) / 64), 256, 0, s>>>(from, ld, rows, cols, scale, to, padded);
+template <typename T, int PARTS> hipError_t lay_out(const Operand &x, const Operand &y, const int *targets, int rows, int vocab, float *mean, hipStream_t s) {
+  const unsigned blocks = x.tiles + y.tiles + (mean != nullptr);
+  if (!blocks) return hipSuccess;
+  k_operands<T, PARTS><<<blocks, 256, 0, s>>>(x, y, targets, rows, vocab, mean);
   return hipGetLastError();
 }
 
 template <typename T, int PARTS>
 hipError_t loss(const VocabShape &p, const T *h, const T *w, const int *targets, float *loss, float *state, char *work, hipStream_t s) {
   const Space sp(p, false);
+  __bf16 *const hr = (__bf16 *)(work + sp.h), *const wr = (__bf16 *)(work + sp.w);
+  const bool h_direct = direct(h, p.ld_h, p.d), w_direct = direct(w, p.ld_w, p.d);
   Product q = {};
   q.rows_b = p.rows;
   q.ksteps = sp.dp / BK;
-  TRY((rows_of<T, PARTS>(h, p.ld_h, p.rows, p.d, sp.dp, (__bf16 *)(work + sp.h), &q.b, &q.ldb, s)));
+  q.b = h_direct ? (const __bf16 *)h : hr;
+  q.ldb = h_direct ? p.ld_h : sp.dp;
   q.part_b = (long long)p.rows * sp.dp;
-  const bool direct = sizeof(T) == 2 && p.d % BK == 0 && p.ld_w % 8 == 0 && (uintptr_t)w % 16 == 0;
-  const int width = direct ? p.vocab : sp.width;
+  q.lda = w_direct ? p.ld_w : sp.dp;
+  const int width = w_direct ? p.vocab : sp.width;
   LossEpilogue ep = {targets, (float2 *)(work + sp.part), (float *)(work + sp.picked), 0, p.vocab, p.rows};
   for (long long v = 0; v < p.vocab; v += width) {
+    const int entries = (int)(p.vocab - v < width ? p.vocab - v : width);
+    const T *const piece = w + v * p.ld_w;
+    TRY((lay_out<T, PARTS>(operand(h, p.ld_h, p.rows, p.d, sp.dp, h_direct || v ? nullptr : hr, 0, nullptr),
+                           operand(piece, p.ld_w, entries, p.d, sp.dp, w_direct ? nullptr : wr, 0, nullptr), nullptr, 0, 0, nullptr, s)));
     ep.first = (int)v;
-    q.rows_a = (int)(p.vocab - v < width ? p.vocab - v : width);
-    TRY((rows_of<T, PARTS>(w + v * p.ld_w, p.ld_w, q.rows_a, p.d, sp.dp, (__bf16 *)(work + sp.w), &q.a, &q.lda, s)));
-    q.part_a = (long long)q.rows_a * sp.dp;
+    q.rows_a = entries;
+    q.a = w_direct ? (const __bf16 *)piece : wr;
+    q.part_a = (long long)entries * sp.dp;
     TRY((product<PARTS>(q, ep, s)));
   }
   const int blocks = (p.vocab + 255) / 256 * (few(p.rows) ? 8 : 2);
@@ -562,28 +629,24 @@ template <typename T, int PARTS>
 hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *targets, const float *state, const float *dloss, T *dh, T *dw,
                      char *work, hipStream_t s) {
   const Space sp(p, true);
-  float *scale = (float *)(work + sp.scale), *sum_h = (float *)(work + sp.sum_h), *sum_w = (float *)(work + sp.sum_w);
-  const bool summed = sp.width < p.vocab || Slices(p.rows, p.d, sp.width / BK).count > 1;
+  float *const mean = (float *)(work + sp.mean), *const sum_h = (float *)(work + sp.sum_h), *const sum_w = (float *)(work + sp.sum_w);
+  __bf16 *const hr = (__bf16 *)(work + sp.h), *const wr = (__bf16 *)(work + sp.w), *const ht = (__bf16 *)(work + sp.ht), *const wt = (__bf16 *)(work + sp.wt);
+  __bf16 *const gm = (__bf16 *)(work + sp.gm), *const gt = (__bf16 *)(work + sp.gt);
+  const bool h_direct = direct(h, p.ld_h, p.d), w_direct = direct(w, p.ld_w, p.d);
+  const bool summed = sp.width < p.vocab || Slices(p.rows, p.d, sp.width / BK, PARTS).count > 1;
   int slices_h = 1;
-  __bf16 *ht = (__bf16 *)(work + sp.ht), *wt = (__bf16 *)(work + sp.wt), *gm = (__bf16 *)(work + sp.gm), *gt = (__bf16 *)(work + sp.gt);
-  k_scale<<<1, 1024, 0, s>>>(targets, dloss, p.rows, sp.padded, p.vocab, scale);
-  TRY(hipGetLastError());
-  Product q = {}; // G from w and h
-  q.rows_b = sp.padded;
-  q.ksteps = sp.dp / BK;
-  TRY((rows_of<T, PARTS>(h, p.ld_h, p.rows, p.d, sp.dp, (__bf16 *)(work + sp.h), &q.b, &q.ldb, s)));
-  q.part_b = (long long)p.rows * sp.dp;
-  TRY((columns_of<T, PARTS>(h, p.ld_h, p.rows, p.d, sp.padded, scale, ht, s)));
   for (long long v = 0; v < p.vocab; v += sp.width) {
     const int entries = (int)(p.vocab - v < sp.width ? p.vocab - v : sp.width), width = (entries + PAD - 1) / PAD * PAD;
-    TRY((rows_of<T, PARTS>(w + v * p.ld_w, p.ld_w, entries, p.d, sp.dp, (__bf16 *)(work + sp.w), &q.a, &q.lda, s)));
-    q.rows_a = entries;
-    q.rows_b = p.rows;
-    q.part_a = (long long)entries * sp.dp;
-    GradEpilogue<PARTS> ep = {targets, state, scale, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded};
-    TRY((product<PARTS>(q, ep, s)));
-    TRY((columns_of<T, PARTS>(w + v * p.ld_w, p.ld_w, entries, p.d, width, nullptr, wt, s)));
-    const Slices sh(p.rows, p.d, width / BK, v ? slices_h : 256), sw(entries, p.d, sp.padded / BK);
+    const T *const piece = w + v * p.ld_w;
+    Operand oh = operand(h, p.ld_h, p.rows, p.d, sp.dp, h_direct || v ? nullptr : hr, sp.padded, v ? nullptr : ht);
+    oh.targets = targets;
+    oh.dloss = dloss;
+    oh.vocab = p.vocab;
+    TRY((lay_out<T, PARTS>(oh, operand(piece, p.ld_w, entries, p.d, sp.dp, w_direct ? nullptr : wr, width, wt), targets, p.rows, p.vocab, v ? nullptr : mean, s)));
+    Product q = {w_direct ? (const __bf16 *)piece : wr, h_direct ? (const __bf16 *)h : hr, w_direct ? p.ld_w : sp.dp, h_direct ? p.ld_h : sp.dp,
+                 (long long)entries * sp.dp, (long long)p.rows * sp.dp, entries, p.rows, sp.dp / BK, 0, 0, 0, 0};
+    TRY((product<PARTS>(q, GradEpilogue<PARTS>{targets, state, dloss, mean, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded}, s)));
+    const Slices sh(p.rows, p.d, width / BK, PARTS, v ? slices_h : 256), sw(entries, p.d, sp.padded / BK, PARTS);
     if (!v) slices_h = sh.count;
     Product dhq = {gm, wt, width, width, (long long)sp.padded * width, (long long)p.d * width, p.rows, p.d, width / BK, 0, 0, sh.count, sh.steps};
     if (!summed) TRY((product<PARTS>(dhq, StoreEpilogue<T>{dh, p.d, 0, p.rows, p.d, false}, s)));
