@@ -231,6 +231,12 @@ struct LossEpilogue {
   }
 };
 
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef float two __attribute__((ext_vector_type(2)));
+  typedef __bf16 two_bf16 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(two{a, b}, two_bf16));
+}
+
 // The same logits again, turned into G: as rows of h by entries of the vocabulary (gm) and the other way round (gt), in parts.
 template <int PARTS> struct GradEpilogue {
   static constexpr bool LOGITS = true;
@@ -253,14 +259,25 @@ template <int PARTS> struct GradEpilogue {
       for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int v = 32 * i + 8 * (e >> 2) + (e & 3);
-          float x = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -top)) * per;
-          if (v == y) x = -miss * g;
-          acc[i][j][e] = none || v >= left ? 0.f : x;
+          const float x = __builtin_amdgcn_exp2f(fmaf(acc[i][j][e], LOG2E, -top)) * per;
+          acc[i][j][e] = none ? 0.f : x;
         }
+      if (__any(((unsigned)y < 32u * MI && !(y & 4)) || left < 32 * MI)) { // targets here, or the vocabulary's end
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int v = 32 * i + 8 * (e >> 2) + (e & 3);
+            if (v == y) acc[i][j][e] = none ? 0.f : -miss * g;
+            if (v >= left) acc[i][j][e] = 0.f;
+          }
+      }
     }
     // 32 entries by 64 rows at a time.  first: [64 rows][32 entries], second: [32 entries][64 rows] (16-byte chunks at places that are
-    // exchanged by the row, so that a wavefront's writes use all banks)
+    // exchanged by the row, so that a wavefront's writes use all banks).  Two neighbouring lanes exchange one of two entries each, so that a
+    // lane writes an entry for two rows at once: an even one entries 0 and 2 of four, an odd one entries 1 and 3.
+    const uint32_t pair = lane & 1 ? 0x03020706u : 0x05040100u;
+    const int odd = lane & 1;
 #pragma unroll
     for (int k = 0; k < PARTS; ++k)
 #pragma unroll
@@ -270,22 +287,26 @@ template <int PARTS> struct GradEpilogue {
         for (int j = 0; j < NI; ++j)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            uint16_t b[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float x = acc[i][j][4 * q + e];
-              if constexpr (PARTS == 1) b[e] = __builtin_bit_cast(uint16_t, (__bf16)x);
-              else {
-                const uint32_t bits = __float_as_uint(x) & 0xffff0000u;
-                b[e] = (uint16_t)(bits >> 16);
-                acc[i][j][4 * q + e] = x - __uint_as_float(bits);
-              }
-              const int v = 8 * q + 4 * half + e;
-              *(uint16_t *)(st.second + v * 128 + (((j * 4 + (r >> 3)) ^ (v & 7)) * 16) + (r & 7) * 2) = b[e];
-            }
             uint2 four;
-            four.x = b[0] | (uint32_t)b[1] << 16;
-            four.y = b[2] | (uint32_t)b[3] << 16;
+            if constexpr (PARTS == 1) {
+              four.x = bf16_pair(acc[i][j][4 * q], acc[i][j][4 * q + 1]);
+              four.y = bf16_pair(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+            } else {
+              uint32_t b[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                b[e] = __float_as_uint(acc[i][j][4 * q + e]) & 0xffff0000u;
+                acc[i][j][4 * q + e] -= __uint_as_float(b[e]);
+              }
+              four.x = b[0] >> 16 | b[1];
+              four.y = b[2] >> 16 | b[3];
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t mine = e ? four.y : four.x, other = (uint32_t)__builtin_amdgcn_mov_dpp((int)mine, 0xb1, 0xf, 0xf, false);
+              const int v = 8 * q + 4 * half + 2 * e + odd;
+              *(uint32_t *)(st.second + v * 128 + (((j * 4 + (r >> 3)) ^ (v & 7)) * 16) + (r & 6) * 2) = __builtin_amdgcn_perm(other, mine, pair);
+            }
             *(uint2 *)(st.first + (j * 32 + r) * 64 + ((q ^ ((r >> 1) & 3)) * 16) + half * 8) = four;
           }
         Stage::turn();
@@ -345,8 +366,7 @@ template <typename T> struct StoreEpilogue {
               }
               *(words4_any *)at = words4{__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
             } else
-              *(words2_any *)at = words2{__builtin_bit_cast(uint16_t, (T)v.x) | (uint32_t)__builtin_bit_cast(uint16_t, (T)v.y) << 16,
-                                         __builtin_bit_cast(uint16_t, (T)v.z) | (uint32_t)__builtin_bit_cast(uint16_t, (T)v.w) << 16};
+              *(words2_any *)at = words2{bf16_pair(v.x, v.y), bf16_pair(v.z, v.w)};
           } else {
             const float u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
