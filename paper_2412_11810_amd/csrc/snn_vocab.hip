@@ -10,7 +10,8 @@
 //
 // All four products are one kernel, C = A B^T with the sums along the rows of both operands, on the bf16 matrix cores with fp32
 // accumulators; what differs is what happens to the accumulators.  Operands of 32 bits go in as three bf16 parts of 8 bits
-// each, which hold all 24 bits of a float: the six products of parts whose weight is above 2^-24 are further steps of the same sum.
+// each, which hold all 24 bits of a float; of the nine products of parts the six whose weight is above 2^-24 are made, the one of the
+// first parts in accumulators of its own.
 // The logits are computed twice, for the loss (kept: one exponent and one sum for 128 of them) and for G, one piece of the
 // vocabulary after the other, whose G is all that is ever in memory; a second product of 2 rows d vocab operations costs less
 // than 4 bytes of logit written and read for each.
@@ -21,17 +22,26 @@ namespace {
 typedef __bf16 frag __attribute__((ext_vector_type(8)));
 typedef float tile32 __attribute__((ext_vector_type(16)));
 
-constexpr int BK = 64;    // elements of a row in LDS: 128 bytes
-constexpr int PAD = 256;  // rows of G are padded to whole tiles
 constexpr float LOG2E = 1.44269504f;
 
+// Rows of operands lie in blocks of 32 elements, a block's parts one after the other; the products take KS elements of a row at a time, STEP
+// bytes.
+template <int PARTS> constexpr int KS = PARTS == 1 ? 64 : 32;
+template <int PARTS> constexpr int STEP = KS<PARTS> * PARTS * 2;
+template <int PARTS> __device__ __forceinline__ size_t place_of(size_t row, int c, int part, int padded) {
+  return (row * padded + (c & ~31)) * PARTS + part * 32 + (c & 31);
+}
+// Tiles: 256 rows of A by 256 of B, or, in parts, by 128; 64 along a side that has no more.
+bool few(int rows) { return rows <= 64; }
+int tile_b(int parts) { return parts == 1 ? 256 : 128; }
+
 // ---- C = A B^T ----------------------------------------------------------------------------
-// Operands: rows of ksteps * 64 bf16 each, in `parts` parts.  Rows past the last one are the last one again (not used by the epilogues).
+// Operands: rows of ksteps * STEP bytes.  Rows past the last one are the last one again (not used by the epilogues).
 struct Product {
   const __bf16 *a, *b;
-  long long lda, ldb, part_a, part_b; // elements from row to row, from part to part
+  long long lda, ldb; // elements from row to row, of all parts
   int rows_a, rows_b, ksteps;
-  int tiles_a, tiles_b, slices, slice_steps; // slices along the sums: blockIdx.y, slice_steps * 64 elements each
+  int tiles_a, tiles_b, slices, slice_steps; // slices along the sums: blockIdx.y, slice_steps each
 };
 
 __device__ __forceinline__ void load_lds(const char *base, unsigned off, char *lds) {
@@ -52,18 +62,21 @@ struct Stage {
   }
 };
 
-// One tile of BM rows of A by BN rows of B by eight wavefronts, WA along A and WB along B.  LDS holds two steps of 64 elements (whole
-// lines of a row, eight chunks; chunk c of row r is at place c ^ (r / 2 % 8), so that 16 lanes of a fragment, which read one
-// chunk of as many rows, use all 64 banks).  Loads go past the registers, a step ahead.  The fragments of the next quarter of a step are
-// on their way while those of this one are multiplied, also across the barrier between two steps: matrix instructions wait for nothing
-// but loads that take longer than a step.  (Tiles with 64 rows on a side, of which there are few and which are soon multiplied, hold four
-// steps: their loads are three ahead.)
+// One tile of BM rows of A by BN rows of B by eight wavefronts, WA along A and WB along B.  LDS holds two steps of 64 elements (128 bytes of
+// a row), or of 32 in three parts (192 bytes); its 16-byte chunks are exchanged in a way that depends on the row, so that 16
+// lanes of a fragment, which read one chunk of as many rows, use all 64 banks.  Loads go past the registers, a step ahead.  The fragments of
+// the next 16 elements are on their way while those of these are multiplied, also across the barrier between two steps: matrix instructions
+// wait for nothing but loads that take longer than a step.  (Tiles with 64 rows on a side, of which there are few and which are
+// soon multiplied, hold four steps: their loads are three ahead.)
 template <int BM, int BN, int WA, int WB, int PARTS, class Epilogue>
 __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
-  constexpr int MI = BM / WA / 32, NI = BN / WB / 32, LA = BM / 64, LB = BN / 64, QUARTERS = BK / 16;
-  constexpr int SEGS = PARTS == 1 ? 1 : 6, HELD = BM == 64 || BN == 64 ? 4 : 2;
-  __shared__ __align__(16) char a0[BM * 128], b0[BN * 128], a1[BM * 128], b1[BN * 128];
-  __shared__ __align__(16) char a2[HELD > 2 ? BM * 128 : 16], b2[HELD > 2 ? BN * 128 : 16], a3[HELD > 2 ? BM * 128 : 16], b3[HELD > 2 ? BN * 128 : 16];
+  constexpr int ROW = STEP<PARTS>, CHUNKS = ROW / 16, TIMES = KS<PARTS> / 16;
+  constexpr int MI = BM / WA / 32, NI = BN / WB / 32, LA = (BM * CHUNKS + 511) / 512, LB = (BN * CHUNKS + 511) / 512;
+  constexpr int HELD = PARTS == 1 && (BM == 64 || BN == 64) ? 4 : 2;
+  __shared__ __align__(16) char a0[BM * ROW], b0[BN * ROW], a1[BM * ROW], b1[BN * ROW];
+  __shared__ __align__(16) char a2[HELD > 2 ? BM * ROW : 16], b2[HELD > 2 ? BN * ROW : 16], a3[HELD > 2 ? BM * ROW : 16], b3[HELD > 2 ? BN * ROW : 16];
+  // where chunk c of a row is, and which one is at place c
+  auto exchanged = [](int row, int c) { return PARTS == 1 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3); };
   // tiles in the order of the dies: consecutive workgroups are on different ones, each die takes a run of tiles, in groups of eight
   // along A that share the rows of B
   const unsigned n = p.tiles_a * p.tiles_b, per = n / 8, rest = n % 8;
@@ -75,41 +88,57 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wa = w / WB, wb = w % WB;
   const char *base_a = (const char *)(p.a + (long long)ta * BM * p.lda), *base_b = (const char *)(p.b + (long long)tb * BN * p.ldb);
+  // load i of a wavefront: 64 chunks of the tile from number (8 i + w) * 64 on, from the beginning again where it has no more
   unsigned off_a[LA], off_b[LB];
-  const int row8 = w * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row8 >> 1) & 7);
 #pragma unroll
-  for (int i = 0; i < LA; ++i) off_a[i] = (unsigned)min(i * 64 + row8, p.rows_a - 1 - ta * BM) * (unsigned)(p.lda * 2) + chunk * 16;
+  for (int i = 0; i < LA; ++i) {
+    const int q = ((8 * i + w) * 64) % (BM * CHUNKS) + lane, row = q / CHUNKS;
+    off_a[i] = (unsigned)min(row, p.rows_a - 1 - ta * BM) * (unsigned)(p.lda * 2) + exchanged(row, q % CHUNKS) * 16;
+  }
 #pragma unroll
-  for (int i = 0; i < LB; ++i) off_b[i] = (unsigned)min(i * 64 + row8, p.rows_b - 1 - tb * BN) * (unsigned)(p.ldb * 2) + chunk * 16;
+  for (int i = 0; i < LB; ++i) {
+    const int q = ((8 * i + w) * 64) % (BN * CHUNKS) + lane, row = q / CHUNKS;
+    off_b[i] = (unsigned)min(row, p.rows_b - 1 - tb * BN) * (unsigned)(p.ldb * 2) + exchanged(row, q % CHUNKS) * 16;
+  }
 
   const int slice = blockIdx.y, k_first = slice * p.slice_steps, k_end = min(k_first + p.slice_steps, p.ksteps);
-  int k = k_first, seg = 0;
+  base_a += (long long)k_first * ROW;
+  base_b += (long long)k_first * ROW;
   auto fetch = [&](char *la, char *lb) {
-    // parts of A 0 1 2 0 1 0 with parts of B 2 1 0 1 0 0: the smallest products first
-    const int pa = PARTS == 1 ? 0 : (0x010210 >> (4 * seg)) & 15, pb = PARTS == 1 ? 0 : (0x001012 >> (4 * seg)) & 15;
-    const char *ga = base_a + pa * p.part_a * 2 + (long long)k * 128, *gb = base_b + pb * p.part_b * 2 + (long long)k * 128;
 #pragma unroll
-    for (int i = 0; i < LA; ++i) load_lds(ga, off_a[i], la + (i * 64 + w * 8) * 128);
+    for (int i = 0; i < LA; ++i) load_lds(base_a, off_a[i], la + ((8 * i + w) * 64) % (BM * CHUNKS) * 16);
 #pragma unroll
-    for (int i = 0; i < LB; ++i) load_lds(gb, off_b[i], lb + (i * 64 + w * 8) * 128);
-    if (++k == k_end) { k = k_first; ++seg; }
+    for (int i = 0; i < LB; ++i) load_lds(base_b, off_b[i], lb + ((8 * i + w) * 64) % (BN * CHUNKS) * 16);
+    base_a += ROW;
+    base_b += ROW;
   };
-  tile32 acc[MI][NI] = {};
-  frag fa[2][MI], fb[2][NI];
+  tile32 acc[MI][NI] = {}, low[PARTS == 1 ? 1 : MI][PARTS == 1 ? 1 : NI] = {};
+  frag fa[2][PARTS][MI], fb[2][PARTS][NI];
   const int r = lane & 31, half = lane >> 5;
   auto read = [&](int s, const char *la, const char *lb) {
-    const int place = ((2 * s + half) ^ ((r >> 1) & 7)) * 16;
 #pragma unroll
-    for (int i = 0; i < MI; ++i) fa[s & 1][i] = *(const frag *)(la + (wa * (BM / WA) + i * 32 + r) * 128 + place);
+    for (int k = 0; k < PARTS; ++k) {
+      const int place = exchanged(r, 4 * k + 2 * s + half) * 16; // (tiles of 32 rows begin at multiples of 32)
 #pragma unroll
-    for (int i = 0; i < NI; ++i) fb[s & 1][i] = *(const frag *)(lb + (wb * (BN / WB) + i * 32 + r) * 128 + place);
+      for (int i = 0; i < MI; ++i) fa[s & 1][k][i] = *(const frag *)(la + (wa * (BM / WA) + i * 32 + r) * ROW + place);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fb[s & 1][k][i] = *(const frag *)(lb + (wb * (BN / WB) + i * 32 + r) * ROW + place);
+    }
     __builtin_amdgcn_sched_barrier(0); // (left alone the compiler reads right before it multiplies, into the same registers)
   };
   auto multiply = [&](int s) {
 #pragma unroll
+    for (int k = PARTS - 1; k > 0; --k) // parts of A and of B whose numbers add up to k
+#pragma unroll
+      for (int n = 0; n <= k; ++n)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NI; ++j) low[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s & 1][n][i], fb[s & 1][k - n][j], low[i][j], 0, 0, 0);
+#pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s & 1][i], fb[s & 1][j], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s & 1][0][i], fb[s & 1][0][j], acc[i][j], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
   // the next step is in LDS for every wavefront, and every wavefront has what it read before; `later`: the steps behind it may be under way
@@ -122,10 +151,10 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  int left = (k_end - k_first) * SEGS;
+  int left = k_end - k_first;
   auto step = [&](char *la, char *lb, const char *na, const char *nb, bool more) {
 #pragma unroll
-    for (int s = 0; s < QUARTERS - 1; ++s) {
+    for (int s = 0; s < TIMES - 1; ++s) {
       read(s + 1, la, lb);
       multiply(s);
     }
@@ -134,7 +163,7 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
       if (more || left > HELD) fetch(la, lb);
       read(0, na, nb);
     }
-    multiply(QUARTERS - 1);
+    multiply(TIMES - 1);
     --left;
   };
   fetch(a0, b0);
@@ -172,6 +201,11 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
     if (left) step(a0, b0, a1, b1, false);
   }
   __syncthreads();
+  if constexpr (PARTS > 1)
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) acc[i][j] += low[i][j];
   // element e of a tile: row 8 (e / 4) + 4 half + e % 4 of A, row r of B.  Every wavefront is through with the tiles in LDS
   constexpr bool OF_A = BM >= BN;
   const Stage stage = {(OF_A ? a0 : b0) + w * 4096, (OF_A ? a1 : b1) + w * 4096, lane, r, half};
@@ -242,7 +276,7 @@ template <int PARTS> struct GradEpilogue {
   static constexpr bool LOGITS = true;
   const int *targets;
   const float *state, *dloss, *mean; // dloss [rows], or NULL: mean[0] for each row with a target
-  __bf16 *gm, *gt;            // [PARTS][rows padded][width], [PARTS][width][rows padded]
+  __bf16 *gm, *gt;                    // [rows padded][width], [width][rows padded], in parts
   int first, vocab, rows, width, padded;
   template <int MI, int NI> __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int v0, int m0, int, const Stage &st) const {
     static_assert(NI == 2, "a wavefront has 64 rows of h");
@@ -315,8 +349,8 @@ template <int PARTS> struct GradEpilogue {
           const int m = n * 16 + (lane >> 2), v = n * 8 + (lane >> 3);
           const uint4 of_m = *(const uint4 *)(st.first + m * 64 + (((lane & 3) ^ ((m >> 1) & 3)) * 16));
           const uint4 of_v = *(const uint4 *)(st.second + v * 128 + (((lane & 7) ^ (v & 7)) * 16));
-          *(uint4 *)(gm + ((size_t)k * padded + m0 + m) * width + v0 + 32 * i + (lane & 3) * 8) = of_m;
-          *(uint4 *)(gt + ((size_t)k * width + v0 + 32 * i + v) * padded + m0 + (lane & 7) * 8) = of_v;
+          *(uint4 *)(gm + place_of<PARTS>(m0 + m, v0 + 32 * i + (lane & 3) * 8, k, width)) = of_m;
+          *(uint4 *)(gt + place_of<PARTS>(v0 + 32 * i + v, m0 + (lane & 7) * 8, k, padded)) = of_v;
         }
       }
   }
@@ -381,30 +415,32 @@ template <typename T> struct StoreEpilogue {
   }
 };
 
-// Tiles: 256 by 256, or 64 along a side that has no more than 64 rows (the epilogues that work on logits: along that of h only).
-bool few(int rows) { return rows <= 64; }
-int tiles(int rows_a, int rows_b) { return (few(rows_a) ? 1 : (rows_a + 255) / 256) * (few(rows_b) ? 1 : (rows_b + 255) / 256); }
+int tiles(int rows_a, int rows_b, int parts) {
+  return (few(rows_a) ? 1 : (rows_a + 255) / 256) * (few(rows_b) ? 1 : (rows_b + tile_b(parts) - 1) / tile_b(parts));
+}
+// (the epilogues that work on logits: 64 rows along that of h only)
 template <int PARTS, class Epilogue> hipError_t product(Product p, const Epilogue &ep, hipStream_t s) {
+  constexpr int BN = PARTS == 1 ? 256 : 128, WA = PARTS == 1 ? 2 : 4, WB = 8 / WA; // 64 rows of B to a wavefront
   const bool few_a = few(p.rows_a) && !Epilogue::LOGITS, few_b = few(p.rows_b) && !few_a;
   p.tiles_a = few_a ? 1 : (p.rows_a + 255) / 256;
-  p.tiles_b = few_b ? 1 : (p.rows_b + 255) / 256;
+  p.tiles_b = few_b ? 1 : (p.rows_b + (few_a ? 255 : BN - 1)) / (few_a ? 256 : BN);
   if (!p.slices) {
     p.slices = 1;
     p.slice_steps = p.ksteps;
   }
   const dim3 grid(p.tiles_a * p.tiles_b, p.slices);
   if (few_b) k_product<256, 64, 8, 1, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
-  else if (!few_a) k_product<256, 256, 2, 4, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  else if (!few_a) k_product<256, BN, WA, WB, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
   else if constexpr (!Epilogue::LOGITS) k_product<64, 256, 1, 8, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
   return hipGetLastError();
 }
 
-// A product with fewer tiles than half the compute units is cut along its sums, eight steps of 64 (of which parts take six each) or more;
-// the slices are added up afterwards, in order.
+// A product with fewer tiles than half the compute units is cut along its sums, eight steps (in parts: four) or more each; the slices are
+// added up afterwards, in order.
 struct Slices {
   int count, steps;
   Slices(int rows_a, int rows_b, int ksteps, int parts, int at_most = 256) {
-    const int most = 256 / tiles(rows_a, rows_b), fit = ksteps * (parts == 1 ? 1 : 6) / 8, n = most < fit ? most : fit;
+    const int most = 256 / tiles(rows_a, rows_b, parts), fit = ksteps / (parts == 1 ? 8 : 4), n = most < fit ? most : fit;
     count = n < 1 ? 1 : n < at_most ? n : at_most;
     steps = (ksteps + count - 1) / count;
     count = (ksteps + steps - 1) / steps;
@@ -421,8 +457,8 @@ template <int PARTS> __device__ __forceinline__ void split(float x, uint16_t (&p
     x -= __uint_as_float(bits);
   }
 }
-// One matrix on its way into products: its rows in parts [PARTS][rows][padded cols], zeros behind their ends, and its columns in parts
-// [PARTS][cols][padded rows], zeros behind the last row (either may be NULL).  With targets, rows that have none or whose dloss is 0 are
+// One matrix on its way into products: its rows [rows][padded cols] in parts, zeros behind their ends, and its columns [cols][padded
+// rows] in parts, zeros behind the last row (either may be NULL).  With targets, rows that have none or whose dloss is 0 are
 // zeros in the columns: what they hold (padding: anything) would else meet the zeros of G as 0 * NaN.
 struct Operand {
   const void *from;
@@ -482,7 +518,7 @@ template <typename T, int PARTS> __global__ __launch_bounds__(256) void k_operan
       for (int e = 0; e < 4; ++e) split(v[e], part[e]);
 #pragma unroll
       for (int k = 0; k < PARTS; ++k)
-        *(uint2 *)(m.to_rows + ((size_t)k * m.rows + r) * m.padded_cols + c) = make_uint2(part[0][k] | (uint32_t)part[1][k] << 16, part[2][k] | (uint32_t)part[3][k] << 16);
+        *(uint2 *)(m.to_rows + place_of<PARTS>(r, c, k, m.padded_cols)) = make_uint2(part[0][k] | (uint32_t)part[1][k] << 16, part[2][k] | (uint32_t)part[3][k] << 16);
     }
     const bool none = m.targets && r < m.rows && (!has_target(m.targets, r, true, m.vocab) || (m.dloss && m.dloss[r] == 0.f));
 #pragma unroll
@@ -499,7 +535,7 @@ template <typename T, int PARTS> __global__ __launch_bounds__(256) void k_operan
     for (int e = 0; e < 4; ++e) split(tile[four + e][i * 16 + line], part[e]);
 #pragma unroll
     for (int k = 0; k < PARTS; ++k)
-      *(uint2 *)(m.to_cols + ((size_t)k * m.cols + c) * m.padded_rows + r) = make_uint2(part[0][k] | (uint32_t)part[1][k] << 16, part[2][k] | (uint32_t)part[3][k] << 16);
+      *(uint2 *)(m.to_cols + place_of<PARTS>(c, r, k, m.padded_rows)) = make_uint2(part[0][k] | (uint32_t)part[1][k] << 16, part[2][k] | (uint32_t)part[3][k] << 16);
   }
 }
 
@@ -559,16 +595,20 @@ __global__ __launch_bounds__(256) void k_clear(uint16_t *to, size_t n) {
 }
 
 // ---- workspace ------------------------------------------------------------------------------
+// Entries of the vocabulary that a wavefront has
+int block_of(const VocabShape &p) { return few(p.rows) ? 32 : p.bf16 ? 128 : 64; }
+
 struct Space {
   int parts, dp, padded, width; // width: entries of a piece of the vocabulary
   size_t h, w, part, picked, mean, ht, wt, gm, gt, sum_h, sum_w, bytes;
   Space(const VocabShape &p, bool grad) {
     parts = p.bf16 ? 1 : 3;
-    dp = (p.d + BK - 1) / BK * BK;
-    padded = few(p.rows) ? 64 : (p.rows + PAD - 1) / PAD * PAD;
+    const int ks = parts == 1 ? KS<1> : KS<3>, rows = few(p.rows) ? 64 : tile_b(parts);
+    dp = (p.d + ks - 1) / ks * ks;
+    padded = p.rows ? (p.rows + rows - 1) / rows * rows : rows;
     // G of a piece has about 2^27 elements, and a piece of w no more
-    const long long all = ((long long)p.vocab + PAD - 1) / PAD * PAD, most = grad ? (padded > dp ? padded : dp) : dp;
-    long long fit = (1ll << 27) / (most > 0 ? most : 1) / PAD * PAD;
+    const long long all = ((long long)p.vocab + 255) / 256 * 256, most = grad ? (padded > dp ? padded : dp) : dp;
+    long long fit = (1ll << 27) / (most > 0 ? most : 1) / 256 * 256;
     if (fit < 2048) fit = 2048;
     width = (int)(fit < all ? fit : all);
     size_t at = 0;
@@ -576,7 +616,7 @@ struct Space {
     h = take((size_t)2 * parts * p.rows * dp);
     w = take((size_t)2 * parts * width * dp);
     if (!grad) {
-      part = take(sizeof(float2) * (size_t)(all / (few(p.rows) ? 32 : 128)) * p.rows);
+      part = take(sizeof(float2) * (size_t)(all / block_of(p)) * p.rows);
       picked = take(sizeof(float) * (size_t)p.rows);
     } else {
       mean = take(sizeof(float));
@@ -584,7 +624,7 @@ struct Space {
       wt = take((size_t)2 * parts * p.d * width);
       gm = take((size_t)2 * parts * padded * width);
       gt = take((size_t)2 * parts * padded * width);
-      const Slices sh(p.rows, p.d, width / BK, parts), sw(width < p.vocab ? width : p.vocab, p.d, padded / BK, parts);
+      const Slices sh(p.rows, p.d, width / ks, parts), sw(width < p.vocab ? width : p.vocab, p.d, padded / ks, parts);
       sum_h = take(width < p.vocab || sh.count > 1 ? sizeof(float) * (size_t)sh.count * p.rows * p.d : 0);
       // (the last piece may be so much narrower that it is cut further: no more than 256 tiles in all)
       sum_w = take(sw.count > 1 || width < p.vocab ? sizeof(float) * 256 * (size_t)256 * 256 : 0);
@@ -600,7 +640,7 @@ struct Space {
   } while (0)
 
 // Whether rows can go into products from where they are: bf16, aligned and whole.
-template <typename T> bool direct(const T *from, long long ld, int cols) { return sizeof(T) == 2 && cols % BK == 0 && ld % 8 == 0 && (uintptr_t)from % 16 == 0; }
+template <typename T> bool direct(const T *from, long long ld, int cols) { return sizeof(T) == 2 && cols % 64 == 0 && ld % 8 == 0 && (uintptr_t)from % 16 == 0; }
 
 template <typename T> Operand operand(const T *from, long long ld, int rows, int cols, int padded_cols, __bf16 *to_rows, int padded_rows, __bf16 *to_cols) {
   Operand m = {from, ld, rows, cols, padded_cols, padded_rows, to_rows, to_cols, nullptr, nullptr, 0, 0, 0};
@@ -622,11 +662,10 @@ hipError_t loss(const VocabShape &p, const T *h, const T *w, const int *targets,
   const bool h_direct = direct(h, p.ld_h, p.d), w_direct = direct(w, p.ld_w, p.d);
   Product q = {};
   q.rows_b = p.rows;
-  q.ksteps = sp.dp / BK;
+  q.ksteps = sp.dp / KS<PARTS>;
   q.b = h_direct ? (const __bf16 *)h : hr;
-  q.ldb = h_direct ? p.ld_h : sp.dp;
-  q.part_b = (long long)p.rows * sp.dp;
-  q.lda = w_direct ? p.ld_w : sp.dp;
+  q.ldb = h_direct ? p.ld_h : sp.dp * PARTS;
+  q.lda = w_direct ? p.ld_w : sp.dp * PARTS;
   const int width = w_direct ? p.vocab : sp.width;
   LossEpilogue ep = {targets, (float2 *)(work + sp.part), (float *)(work + sp.picked), 0, p.vocab, p.rows};
   for (long long v = 0; v < p.vocab; v += width) {
@@ -637,10 +676,9 @@ hipError_t loss(const VocabShape &p, const T *h, const T *w, const int *targets,
     ep.first = (int)v;
     q.rows_a = entries;
     q.a = w_direct ? (const __bf16 *)piece : wr;
-    q.part_a = (long long)entries * sp.dp;
     TRY((product<PARTS>(q, ep, s)));
   }
-  const int blocks = (p.vocab + 255) / 256 * (few(p.rows) ? 8 : 2);
+  const int blocks = (p.vocab + 255) / 256 * (256 / block_of(p));
   k_join<<<(p.rows + 15) / 16, 1024, 0, s>>>(ep.part, ep.picked, targets, blocks, p.rows, p.vocab, loss, state);
   return hipGetLastError();
 }
@@ -653,26 +691,25 @@ hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *tar
   __bf16 *const hr = (__bf16 *)(work + sp.h), *const wr = (__bf16 *)(work + sp.w), *const ht = (__bf16 *)(work + sp.ht), *const wt = (__bf16 *)(work + sp.wt);
   __bf16 *const gm = (__bf16 *)(work + sp.gm), *const gt = (__bf16 *)(work + sp.gt);
   const bool h_direct = direct(h, p.ld_h, p.d), w_direct = direct(w, p.ld_w, p.d);
-  const bool summed = sp.width < p.vocab || Slices(p.rows, p.d, sp.width / BK, PARTS).count > 1;
+  const bool summed = sp.width < p.vocab || Slices(p.rows, p.d, sp.width / KS<PARTS>, PARTS).count > 1;
   int slices_h = 1;
   for (long long v = 0; v < p.vocab; v += sp.width) {
-    const int entries = (int)(p.vocab - v < sp.width ? p.vocab - v : sp.width), width = (entries + PAD - 1) / PAD * PAD;
+    const int entries = (int)(p.vocab - v < sp.width ? p.vocab - v : sp.width), width = (entries + 255) / 256 * 256;
     const T *const piece = w + v * p.ld_w;
     Operand oh = operand(h, p.ld_h, p.rows, p.d, sp.dp, h_direct || v ? nullptr : hr, sp.padded, v ? nullptr : ht);
     oh.targets = targets;
     oh.dloss = dloss;
     oh.vocab = p.vocab;
     TRY((lay_out<T, PARTS>(oh, operand(piece, p.ld_w, entries, p.d, sp.dp, w_direct ? nullptr : wr, width, wt), targets, p.rows, p.vocab, v ? nullptr : mean, s)));
-    Product q = {w_direct ? (const __bf16 *)piece : wr, h_direct ? (const __bf16 *)h : hr, w_direct ? p.ld_w : sp.dp, h_direct ? p.ld_h : sp.dp,
-                 (long long)entries * sp.dp, (long long)p.rows * sp.dp, entries, p.rows, sp.dp / BK, 0, 0, 0, 0};
+    Product q = {w_direct ? (const __bf16 *)piece : wr, h_direct ? (const __bf16 *)h : hr, w_direct ? p.ld_w : sp.dp * PARTS,
+                 h_direct ? p.ld_h : sp.dp * PARTS, entries, p.rows, sp.dp / KS<PARTS>, 0, 0, 0, 0};
     TRY((product<PARTS>(q, GradEpilogue<PARTS>{targets, state, dloss, mean, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded}, s)));
-    const Slices sh(p.rows, p.d, width / BK, PARTS, v ? slices_h : 256), sw(entries, p.d, sp.padded / BK, PARTS);
+    const Slices sh(p.rows, p.d, width / KS<PARTS>, PARTS, v ? slices_h : 256), sw(entries, p.d, sp.padded / KS<PARTS>, PARTS);
     if (!v) slices_h = sh.count;
-    Product dhq = {gm, wt, width, width, (long long)sp.padded * width, (long long)p.d * width, p.rows, p.d, width / BK, 0, 0, sh.count, sh.steps};
+    Product dhq = {gm, wt, (long long)width * PARTS, (long long)width * PARTS, p.rows, p.d, width / KS<PARTS>, 0, 0, sh.count, sh.steps};
     if (!summed) TRY((product<PARTS>(dhq, StoreEpilogue<T>{dh, p.d, 0, p.rows, p.d, false}, s)));
     else TRY((product<PARTS>(dhq, StoreEpilogue<float>{sum_h, p.d, (long long)p.rows * p.d, p.rows, p.d, v > 0}, s)));
-    Product dwq = {gt, ht, sp.padded, sp.padded, (long long)sp.padded * width, (long long)p.d * sp.padded, entries, p.d, sp.padded / BK, 0, 0,
-                   sw.count, sw.steps};
+    Product dwq = {gt, ht, (long long)sp.padded * PARTS, (long long)sp.padded * PARTS, entries, p.d, sp.padded / KS<PARTS>, 0, 0, sw.count, sw.steps};
     T *const to = dw + v * p.d;
     if (sw.count == 1) TRY((product<PARTS>(dwq, StoreEpilogue<T>{to, p.d, 0, entries, p.d, false}, s)));
     else {
