@@ -14,6 +14,8 @@ constexpr int LANE = 8; // elements of a lane
 constexpr int THREADS = 256;
 
 // Rows need not begin on whole words: these loads and stores may be at any address
+typedef float two __attribute__((ext_vector_type(2)));
+typedef __bf16 two_bf16 __attribute__((ext_vector_type(2)));
 typedef uint32_t words4 __attribute__((ext_vector_type(4)));
 typedef words4 words4_any __attribute__((aligned(2)));
 typedef uint32_t words2 __attribute__((ext_vector_type(2)));
@@ -43,7 +45,7 @@ template <typename T> __device__ __forceinline__ void write(T *p, int count, con
       words4 r;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        r[j] = __builtin_bit_cast(uint16_t, (__bf16)v[2 * j]) | (uint32_t) __builtin_bit_cast(uint16_t, (__bf16)v[2 * j + 1]) << 16;
+        r[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two{v[2 * j], v[2 * j + 1]}, two_bf16));
       *(words4_any *)p = r;
     } else {
 #pragma unroll

@@ -478,6 +478,85 @@ def test_calls_in_a_graph():
         torch.cuda.synchronize()
 
 
+@gpu
+def test_calls_from_two_threads():
+    import threading
+    runs = [every_operator(seed)[0] for seed in (11, 12)]
+    want = [f() for f in runs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(f, ref):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(5):
+                got = f()
+                torch.cuda.current_stream().synchronize()
+                if not same(got, ref):
+                    wrong.append(1)
+                try:  # a refusal of one thread's is not another's
+                    snn.snn_glr_forward(torch.zeros(2, 1, 1 << 26, device="cuda"), torch.zeros(2, 1, 1 << 26, device="cuda"))
+                except snn.SnnError as e:
+                    if "channels" not in str(e):
+                        wrong.append(str(e))
+
+    threads = [threading.Thread(target=work, args=a) for a in zip(runs, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
+# ---- offsets beyond 32 bits ---------------------------------------------------------------------
+@gpu
+def test_glr_arrays_beyond_4_gb():
+    T, n, tail = 70016, 32768, 256  # 4.6 GB each in bf16
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z = torch.empty((T, 1, n), dtype=torch.bfloat16, device="cuda").normal_(2.0, 1.0, generator=g)
+    x, dh = (torch.empty_like(z).normal_(generator=g) for _ in range(2))
+    h, last, kept = snn.snn_glr_forward(z, x, keep=True)
+    dz, dx, _ = snn.snn_glr_backward(z, x, kept, dh)
+    a = T - tail  # a multiple of 128: the last steps by themselves, from the state before them
+    part, part_last, _ = snn.snn_glr_forward(z[a:], x[a:], kept[a // 128])
+    part_dz, part_dx, _ = snn.snn_glr_backward(z[a:], x[a:], kept[a // 128:], dh[a:])
+    # in other groups, hence joined differently: a rounding of bf16, or of the states before it
+    for got, want in ((h[a:], part), (dz[a:], part_dz), (dx[a:], part_dx)):
+        assert ((got.float() - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + 1e-3).all()
+    assert (last - part_last).abs().max() < 1e-3 and h[a].abs().max() > 0.1 and dz[a].abs().max() > 0.01
+
+
+@gpu
+def test_pack_beyond_4_gb():
+    x = torch.empty((1 << 17, 33000), dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(2))
+    p = snn.snn_pack(x)
+    codes, exps = to_bytes(x[-2:].float().cpu().numpy())
+    assert np.array_equal(p.codes[-2:].cpu().numpy(), codes) and np.array_equal(p.exps[-2:].cpu().numpy(), exps)
+    assert np.array_equal(snn.snn_unpack(p, torch.bfloat16)[-2:].double().cpu().numpy(), from_bytes(codes, exps))
+
+
+@gpu
+def test_vocab_beyond_4_gb():
+    rows, d, vocab = 8, 2048, 1_200_000  # w and dw: 4.9 GB each
+    g = torch.Generator(device="cuda").manual_seed(3)
+    h = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    w = torch.empty((vocab, d), dtype=torch.bfloat16, device="cuda").normal_(0.0, 0.05, generator=g)
+    t = torch.arange(vocab - rows, vocab, dtype=torch.int32, device="cuda")
+    loss, state = snn.snn_vocab_loss(h, w, t)
+    dh, dw = snn.snn_vocab_loss_grad(h, w, t, state)
+    logits = torch.cat([h.float() @ w[a:a + 100000].float().T for a in range(0, vocab, 100000)], 1).double()
+    want = torch.logsumexp(logits, 1) - logits[torch.arange(rows), t.long()]
+    assert (loss.double() - want).abs().max() < 1e-4  # 2048 products in 32 bits, logits up to 12
+    G = torch.softmax(logits, 1)
+    G[torch.arange(rows), t.long()] -= 1
+    G /= rows
+    for a in (0, vocab - 64):  # an element of G is rounded to bf16, a sum of eight and the result too
+        ref = G[:, a:a + 64].T @ h.double()
+        assert ((dw[a:a + 64].double() - ref).abs() <= 2.0 ** -7 * (G[:, a:a + 64].abs().T @ h.double().abs()) + 1e-12).all()
+    ref = sum(G[:, a:a + 100000].float() @ w[a:a + 100000].float() for a in range(0, vocab, 100000)).double()
+    bound = sum(G[:, a:a + 100000].abs().float() @ w[a:a + 100000].abs().float() for a in range(0, vocab, 100000)).double()
+    assert ((dh.double() - ref).abs() <= 2.0 ** -7 * bound).all()
+
+
 # ---- refusals -----------------------------------------------------------------------------------
 def refused(call, text):
     with pytest.raises(snn.SnnError) as e:
