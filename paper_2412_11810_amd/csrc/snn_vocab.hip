@@ -31,9 +31,21 @@ template <int PARTS> constexpr int STEP = KS<PARTS> * PARTS * 2;
 template <int PARTS> __device__ __forceinline__ size_t place_of(size_t row, int c, int part, int padded) {
   return (row * padded + (c & ~31)) * PARTS + part * 32 + (c & 31);
 }
-// Tiles: 256 rows of A by 256 of B, or, in parts, by 128; 64 along a side that has no more.
-bool few(int rows) { return rows <= 64; }
-int tile_b(int parts) { return parts == 1 ? 256 : 128; }
+// Tiles: 256 rows of A by 256 of B, or, in parts, by 128; 64 by 256 where a side has no more than 64 rows (products that make logits: that of B
+// only); 128 by 128 where there would be fewer than 64 tiles, which are sooner done (300 x 512 x 1000 in bf16: 20 us -> 10 us a product).
+enum Tile { BIG, SMALL, FEW_A, FEW_B };
+int rows_of_a(Tile t) { return t == FEW_A ? 64 : t == SMALL ? 128 : 256; }
+int rows_of_b(Tile t, int parts) { return t == FEW_B ? 64 : t == FEW_A ? 256 : t == SMALL || parts > 1 ? 128 : 256; }
+int tiles(Tile t, int rows_a, int rows_b, int parts) {
+  const int a = rows_of_a(t), b = rows_of_b(t, parts);
+  return ((rows_a + a - 1) / a) * ((rows_b + b - 1) / b);
+}
+Tile tile_for(int rows_a, int rows_b, int parts, bool logits) {
+  if (rows_a <= 64 && !logits) return FEW_A;
+  if (rows_b <= 64) return FEW_B;
+  const int a = rows_of_a(BIG), b = rows_of_b(BIG, parts);
+  return (long long)((rows_a + a - 1) / a) * ((rows_b + b - 1) / b) < 64 ? SMALL : BIG;
+}
 
 // ---- C = A B^T ----------------------------------------------------------------------------
 // Operands: rows of ksteps * STEP bytes.  Rows past the last one are the last one again (not used by the epilogues).
@@ -66,13 +78,13 @@ struct Stage {
 // a row), or of 32 in three parts (192 bytes); its 16-byte chunks are exchanged in a way that depends on the row, so that 16
 // lanes of a fragment, which read one chunk of as many rows, use all 64 banks.  Loads go past the registers, a step ahead.  The fragments of
 // the next 16 elements are on their way while those of these are multiplied, also across the barrier between two steps: matrix instructions
-// wait for nothing but loads that take longer than a step.  (Tiles with 64 rows on a side, of which there are few and which are
-// soon multiplied, hold four steps: their loads are three ahead.)
+// wait for nothing but loads that take longer than a step.  (Smaller tiles, of which there are few and which are soon multiplied, hold
+// four steps where LDS has room for them: their loads are three ahead.)
 template <int BM, int BN, int WA, int WB, int PARTS, class Epilogue>
 __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
   constexpr int ROW = STEP<PARTS>, CHUNKS = ROW / 16, TIMES = KS<PARTS> / 16;
   constexpr int MI = BM / WA / 32, NI = BN / WB / 32, LA = (BM * CHUNKS + 511) / 512, LB = (BN * CHUNKS + 511) / 512;
-  constexpr int HELD = PARTS == 1 && (BM == 64 || BN == 64) ? 4 : 2;
+  constexpr int HELD = PARTS == 1 && BM * BN < 256 * 256 ? 4 : 2;
   __shared__ __align__(16) char a0[BM * ROW], b0[BN * ROW], a1[BM * ROW], b1[BN * ROW];
   __shared__ __align__(16) char a2[HELD > 2 ? BM * ROW : 16], b2[HELD > 2 ? BN * ROW : 16], a3[HELD > 2 ? BM * ROW : 16], b3[HELD > 2 ? BN * ROW : 16];
   // where chunk c of a row is, and which one is at place c
@@ -207,8 +219,10 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
 #pragma unroll
       for (int j = 0; j < NI; ++j) acc[i][j] += low[i][j];
   // element e of a tile: row 8 (e / 4) + 4 half + e % 4 of A, row r of B.  Every wavefront is through with the tiles in LDS
-  constexpr bool OF_A = BM >= BN;
-  const Stage stage = {(OF_A ? a0 : b0) + w * 4096, (OF_A ? a1 : b1) + w * 4096, lane, r, half};
+  constexpr bool HALVES = BM * ROW < 8 * 4096 && BN * ROW < 8 * 4096; // four wavefronts in each array
+  char *const first0 = HALVES ? (w < 4 ? a0 : b0) + w % 4 * 4096 : (BM >= BN ? a0 : b0) + w * 4096;
+  char *const second0 = HALVES ? (w < 4 ? a1 : b1) + w % 4 * 4096 : (BM >= BN ? a1 : b1) + w * 4096;
+  const Stage stage = {first0, second0, lane, r, half};
   ep.template finish<MI, NI>(acc, ta * BM + wa * (BM / WA), tb * BN + wb * (BN / WB), slice, stage);
 }
 
@@ -415,22 +429,19 @@ template <typename T> struct StoreEpilogue {
   }
 };
 
-int tiles(int rows_a, int rows_b, int parts) {
-  return (few(rows_a) ? 1 : (rows_a + 255) / 256) * (few(rows_b) ? 1 : (rows_b + tile_b(parts) - 1) / tile_b(parts));
-}
-// (the epilogues that work on logits: 64 rows along that of h only)
-template <int PARTS, class Epilogue> hipError_t product(Product p, const Epilogue &ep, hipStream_t s) {
+template <int PARTS, class Epilogue> hipError_t product(Tile t, Product p, const Epilogue &ep, hipStream_t s) {
   constexpr int BN = PARTS == 1 ? 256 : 128, WA = PARTS == 1 ? 2 : 4, WB = 8 / WA; // 64 rows of B to a wavefront
-  const bool few_a = few(p.rows_a) && !Epilogue::LOGITS, few_b = few(p.rows_b) && !few_a;
-  p.tiles_a = few_a ? 1 : (p.rows_a + 255) / 256;
-  p.tiles_b = few_b ? 1 : (p.rows_b + (few_a ? 255 : BN - 1)) / (few_a ? 256 : BN);
+  const int a = rows_of_a(t), b = rows_of_b(t, PARTS);
+  p.tiles_a = (p.rows_a + a - 1) / a;
+  p.tiles_b = (p.rows_b + b - 1) / b;
   if (!p.slices) {
     p.slices = 1;
     p.slice_steps = p.ksteps;
   }
   const dim3 grid(p.tiles_a * p.tiles_b, p.slices);
-  if (few_b) k_product<256, 64, 8, 1, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
-  else if (!few_a) k_product<256, BN, WA, WB, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  if (t == FEW_B) k_product<256, 64, 8, 1, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  else if (t == SMALL) k_product<128, 128, 4, 2, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  else if (t == BIG) k_product<256, BN, WA, WB, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
   else if constexpr (!Epilogue::LOGITS) k_product<64, 256, 1, 8, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
   return hipGetLastError();
 }
@@ -438,9 +449,11 @@ template <int PARTS, class Epilogue> hipError_t product(Product p, const Epilogu
 // A product with fewer tiles than half the compute units is cut along its sums, eight steps (in parts: four) or more each; the slices are
 // added up afterwards, in order.
 struct Slices {
+  Tile tile;
   int count, steps;
   Slices(int rows_a, int rows_b, int ksteps, int parts, int at_most = 256) {
-    const int most = 256 / tiles(rows_a, rows_b, parts), fit = ksteps / (parts == 1 ? 8 : 4), n = most < fit ? most : fit;
+    tile = tile_for(rows_a, rows_b, parts, false);
+    const int most = 256 / tiles(tile, rows_a, rows_b, parts), fit = ksteps / (parts == 1 ? 8 : 4), n = most < fit ? most : fit;
     count = n < 1 ? 1 : n < at_most ? n : at_most;
     steps = (ksteps + count - 1) / count;
     count = (ksteps + steps - 1) / steps;
@@ -595,19 +608,20 @@ __global__ __launch_bounds__(256) void k_clear(uint16_t *to, size_t n) {
 }
 
 // ---- workspace ------------------------------------------------------------------------------
-// Entries of the vocabulary that a wavefront has
-int block_of(const VocabShape &p) { return few(p.rows) ? 32 : p.bf16 ? 128 : 64; }
-
 struct Space {
-  int parts, dp, padded, width; // width: entries of a piece of the vocabulary
+  Tile logits; // of the products that make logits
+  int parts, dp, padded, width, block; // width: entries of a piece of the vocabulary; block: those of a wavefront
   size_t h, w, part, picked, mean, ht, wt, gm, gt, sum_h, sum_w, bytes;
   Space(const VocabShape &p, bool grad) {
     parts = p.bf16 ? 1 : 3;
-    const int ks = parts == 1 ? KS<1> : KS<3>, rows = few(p.rows) ? 64 : tile_b(parts);
+    logits = tile_for(p.vocab, p.rows, parts, true);
+    block = logits == BIG ? (parts == 1 ? 128 : 64) : 32;
+    const int ks = parts == 1 ? KS<1> : KS<3>, rows = rows_of_b(logits, parts);
     dp = (p.d + ks - 1) / ks * ks;
-    padded = p.rows ? (p.rows + rows - 1) / rows * rows : rows;
+    padded = (p.rows + rows - 1) / rows * rows;
     // G of a piece has about 2^27 elements, and a piece of w no more
-    const long long all = ((long long)p.vocab + 255) / 256 * 256, most = grad ? (padded > dp ? padded : dp) : dp;
+    const int tile_a = rows_of_a(logits);
+    const long long all = ((long long)p.vocab + tile_a - 1) / tile_a * tile_a, most = grad ? (padded > dp ? padded : dp) : dp;
     long long fit = (1ll << 27) / (most > 0 ? most : 1) / 256 * 256;
     if (fit < 2048) fit = 2048;
     width = (int)(fit < all ? fit : all);
@@ -616,7 +630,7 @@ struct Space {
     h = take((size_t)2 * parts * p.rows * dp);
     w = take((size_t)2 * parts * width * dp);
     if (!grad) {
-      part = take(sizeof(float2) * (size_t)(all / block_of(p)) * p.rows);
+      part = take(sizeof(float2) * (size_t)(all / block) * p.rows);
       picked = take(sizeof(float) * (size_t)p.rows);
     } else {
       mean = take(sizeof(float));
@@ -676,9 +690,9 @@ hipError_t loss(const VocabShape &p, const T *h, const T *w, const int *targets,
     ep.first = (int)v;
     q.rows_a = entries;
     q.a = w_direct ? (const __bf16 *)piece : wr;
-    TRY((product<PARTS>(q, ep, s)));
+    TRY((product<PARTS>(sp.logits, q, ep, s)));
   }
-  const int blocks = (p.vocab + 255) / 256 * (256 / block_of(p));
+  const int tile_a = rows_of_a(sp.logits), blocks = (p.vocab + tile_a - 1) / tile_a * (tile_a / sp.block);
   k_join<<<(p.rows + 15) / 16, 1024, 0, s>>>(ep.part, ep.picked, targets, blocks, p.rows, p.vocab, loss, state);
   return hipGetLastError();
 }
@@ -691,10 +705,11 @@ hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *tar
   __bf16 *const hr = (__bf16 *)(work + sp.h), *const wr = (__bf16 *)(work + sp.w), *const ht = (__bf16 *)(work + sp.ht), *const wt = (__bf16 *)(work + sp.wt);
   __bf16 *const gm = (__bf16 *)(work + sp.gm), *const gt = (__bf16 *)(work + sp.gt);
   const bool h_direct = direct(h, p.ld_h, p.d), w_direct = direct(w, p.ld_w, p.d);
+  const int tile_a = rows_of_a(sp.logits);
   const bool summed = sp.width < p.vocab || Slices(p.rows, p.d, sp.width / KS<PARTS>, PARTS).count > 1;
   int slices_h = 1;
   for (long long v = 0; v < p.vocab; v += sp.width) {
-    const int entries = (int)(p.vocab - v < sp.width ? p.vocab - v : sp.width), width = (entries + 255) / 256 * 256;
+    const int entries = (int)(p.vocab - v < sp.width ? p.vocab - v : sp.width), width = (entries + tile_a - 1) / tile_a * tile_a;
     const T *const piece = w + v * p.ld_w;
     Operand oh = operand(h, p.ld_h, p.rows, p.d, sp.dp, h_direct || v ? nullptr : hr, sp.padded, v ? nullptr : ht);
     oh.targets = targets;
@@ -703,18 +718,18 @@ hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *tar
     TRY((lay_out<T, PARTS>(oh, operand(piece, p.ld_w, entries, p.d, sp.dp, w_direct ? nullptr : wr, width, wt), targets, p.rows, p.vocab, v ? nullptr : mean, s)));
     Product q = {w_direct ? (const __bf16 *)piece : wr, h_direct ? (const __bf16 *)h : hr, w_direct ? p.ld_w : sp.dp * PARTS,
                  h_direct ? p.ld_h : sp.dp * PARTS, entries, p.rows, sp.dp / KS<PARTS>, 0, 0, 0, 0};
-    TRY((product<PARTS>(q, GradEpilogue<PARTS>{targets, state, dloss, mean, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded}, s)));
+    TRY((product<PARTS>(sp.logits, q, GradEpilogue<PARTS>{targets, state, dloss, mean, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded}, s)));
     const Slices sh(p.rows, p.d, width / KS<PARTS>, PARTS, v ? slices_h : 256), sw(entries, p.d, sp.padded / KS<PARTS>, PARTS);
     if (!v) slices_h = sh.count;
     Product dhq = {gm, wt, (long long)width * PARTS, (long long)width * PARTS, p.rows, p.d, width / KS<PARTS>, 0, 0, sh.count, sh.steps};
-    if (!summed) TRY((product<PARTS>(dhq, StoreEpilogue<T>{dh, p.d, 0, p.rows, p.d, false}, s)));
-    else TRY((product<PARTS>(dhq, StoreEpilogue<float>{sum_h, p.d, (long long)p.rows * p.d, p.rows, p.d, v > 0}, s)));
+    if (!summed) TRY((product<PARTS>(sh.tile, dhq, StoreEpilogue<T>{dh, p.d, 0, p.rows, p.d, false}, s)));
+    else TRY((product<PARTS>(sh.tile, dhq, StoreEpilogue<float>{sum_h, p.d, (long long)p.rows * p.d, p.rows, p.d, v > 0}, s)));
     Product dwq = {gt, ht, (long long)sp.padded * PARTS, (long long)sp.padded * PARTS, entries, p.d, sp.padded / KS<PARTS>, 0, 0, sw.count, sw.steps};
     T *const to = dw + v * p.d;
-    if (sw.count == 1) TRY((product<PARTS>(dwq, StoreEpilogue<T>{to, p.d, 0, entries, p.d, false}, s)));
+    if (sw.count == 1) TRY((product<PARTS>(sw.tile, dwq, StoreEpilogue<T>{to, p.d, 0, entries, p.d, false}, s)));
     else {
       const size_t n = (size_t)entries * p.d;
-      TRY((product<PARTS>(dwq, StoreEpilogue<float>{sum_w, p.d, (long long)n, entries, p.d, false}, s)));
+      TRY((product<PARTS>(sw.tile, dwq, StoreEpilogue<float>{sum_w, p.d, (long long)n, entries, p.d, false}, s)));
       k_sum<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum_w, sw.count, n, to);
       TRY(hipGetLastError());
     }
@@ -728,7 +743,7 @@ hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *tar
 
 } // namespace
 
-size_t vocab_workspace(const VocabShape &p, bool grad) { return Space(p, grad).bytes; }
+size_t vocab_workspace(const VocabShape &p, bool grad) { return p.rows ? Space(p, grad).bytes : 0; }
 
 hipError_t launch_vocab_loss(const VocabShape &p, const void *h, const void *w, const int *targets, float *loss_, float *state,
                              void *work, hipStream_t s) {
