@@ -32,7 +32,8 @@ template <int PARTS> __device__ __forceinline__ size_t place_of(size_t row, int 
   return (row * padded + (c & ~31)) * PARTS + part * 32 + (c & 31);
 }
 // Tiles: 256 rows of A by 256 of B, or, in parts, by 128; 64 by 256 where a side has no more than 64 rows (products that make logits: that of B
-// only); 128 by 128 where there would be fewer than 64 tiles, which are sooner done (300 x 512 x 1000 in bf16: 20 us -> 10 us a product).
+// only); 128 by 128 where there would be fewer than 128 tiles, half the compute units (loss and gradients in bf16, 300 x 512 x 1000: 82 us with
+// large tiles, 42 us with these; 2048 x 1024 x 4096: 144 and 122 us; 1024 x 1024 x 32000, 500 tiles: 347 and 349 us).
 enum Tile { BIG, SMALL, FEW_A, FEW_B };
 int rows_of_a(Tile t) { return t == FEW_A ? 64 : t == SMALL ? 128 : 256; }
 int rows_of_b(Tile t, int parts) { return t == FEW_B ? 64 : t == FEW_A ? 256 : t == SMALL || parts > 1 ? 128 : 256; }
@@ -44,7 +45,7 @@ Tile tile_for(int rows_a, int rows_b, int parts, bool logits) {
   if (rows_a <= 64 && !logits) return FEW_A;
   if (rows_b <= 64) return FEW_B;
   const int a = rows_of_a(BIG), b = rows_of_b(BIG, parts);
-  return (long long)((rows_a + a - 1) / a) * ((rows_b + b - 1) / b) < 64 ? SMALL : BIG;
+  return (long long)((rows_a + a - 1) / a) * ((rows_b + b - 1) / b) < 128 ? SMALL : BIG;
 }
 
 // ---- C = A B^T ----------------------------------------------------------------------------
