@@ -2,7 +2,10 @@
 //
 //   l_rv = h_r . w_v log2(e);  M_r = max_v ceil(l_rv);  S_r = sum_v 2^(l_rv - M_r);  miss_r = sum_{v != y} 2^(l_rv - M_r) / S_r = 1 - p_ry
 //   loss_r = -log1p(-miss_r), or (log2 S_r - (l_ry - M_r)) log(2) where miss_r is not small
-//   G_rv = dloss_r 2^(l_rv - M_r) / S_r;  G_ry = -dloss_r miss_r;  dh = G w;  dw = G^T h
+//   G_rv = dloss_r / c 2^(l_rv - M_r) / S_r;  G_ry = -dloss_r / c miss_r;  dh = c G w;  dw = c G^T h
+//
+// c is what the rows' dloss have in common (their largest magnitude, 1 / number of rows for a mean): rounded into G, a factor like 1 / 300
+// would be off by up to 2^-8 for all rows alike.
 //
 // miss_r is summed without the target, never formed as 1 - p: a target that the model is sure of keeps its loss and gradient.
 // The subtrahends are whole numbers: l - M is one fused multiply-add, rounded once to its own size, and sums over different M are brought
@@ -81,15 +84,17 @@ struct Stage {
 // the next 16 elements are on their way while those of these are multiplied, also across the barrier between two steps: matrix instructions
 // wait for nothing but loads that take longer than a step.  (Smaller tiles, of which there are few and which are soon multiplied, hold
 // four steps where LDS has room for them: their loads are three ahead.)
-template <int BM, int BN, int WA, int WB, int PARTS, class Epilogue>
+// WHOLE: the rows of A are floats as the caller has them (a multiple of 32 each, 128 bytes per step), whose parts are made in registers.
+template <int BM, int BN, int WA, int WB, int PARTS, bool WHOLE, class Epilogue>
 __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
-  constexpr int ROW = STEP<PARTS>, CHUNKS = ROW / 16, TIMES = KS<PARTS> / 16;
-  constexpr int MI = BM / WA / 32, NI = BN / WB / 32, LA = (BM * CHUNKS + 511) / 512, LB = (BN * CHUNKS + 511) / 512;
+  constexpr int ROW = STEP<PARTS>, CHUNKS = ROW / 16, TIMES = KS<PARTS> / 16, ROW_A = WHOLE ? 128 : ROW, CHUNKS_A = ROW_A / 16;
+  constexpr int MI = BM / WA / 32, NI = BN / WB / 32, LA = (BM * CHUNKS_A + 511) / 512, LB = (BN * CHUNKS + 511) / 512;
   constexpr int HELD = PARTS == 1 && BM * BN < 256 * 256 ? 4 : 2;
-  __shared__ __align__(16) char a0[BM * ROW], b0[BN * ROW], a1[BM * ROW], b1[BN * ROW];
-  __shared__ __align__(16) char a2[HELD > 2 ? BM * ROW : 16], b2[HELD > 2 ? BN * ROW : 16], a3[HELD > 2 ? BM * ROW : 16], b3[HELD > 2 ? BN * ROW : 16];
+  __shared__ __align__(16) char a0[BM * ROW_A], b0[BN * ROW], a1[BM * ROW_A], b1[BN * ROW];
+  __shared__ __align__(16) char a2[HELD > 2 ? BM * ROW_A : 16], b2[HELD > 2 ? BN * ROW : 16], a3[HELD > 2 ? BM * ROW_A : 16], b3[HELD > 2 ? BN * ROW : 16];
   // where chunk c of a row is, and which one is at place c
   auto exchanged = [](int row, int c) { return PARTS == 1 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3); };
+  auto exchanged_a = [&](int row, int c) { return WHOLE ? c ^ ((row >> 1) & 7) : exchanged(row, c); };
   // tiles in the order of the dies: consecutive workgroups are on different ones, each die takes a run of tiles, in groups of eight
   // along A that share the rows of B
   const unsigned n = p.tiles_a * p.tiles_b, per = n / 8, rest = n % 8;
@@ -105,8 +110,8 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
   unsigned off_a[LA], off_b[LB];
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
-    const int q = ((8 * i + w) * 64) % (BM * CHUNKS) + lane, row = q / CHUNKS;
-    off_a[i] = (unsigned)min(row, p.rows_a - 1 - ta * BM) * (unsigned)(p.lda * 2) + exchanged(row, q % CHUNKS) * 16;
+    const int q = ((8 * i + w) * 64) % (BM * CHUNKS_A) + lane, row = q / CHUNKS_A;
+    off_a[i] = (unsigned)min(row, p.rows_a - 1 - ta * BM) * (unsigned)(p.lda * 2) + exchanged_a(row, q % CHUNKS_A) * 16;
   }
 #pragma unroll
   for (int i = 0; i < LB; ++i) {
@@ -115,31 +120,58 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
   }
 
   const int slice = blockIdx.y, k_first = slice * p.slice_steps, k_end = min(k_first + p.slice_steps, p.ksteps);
-  base_a += (long long)k_first * ROW;
+  base_a += (long long)k_first * ROW_A;
   base_b += (long long)k_first * ROW;
   auto fetch = [&](char *la, char *lb) {
 #pragma unroll
-    for (int i = 0; i < LA; ++i) load_lds(base_a, off_a[i], la + ((8 * i + w) * 64) % (BM * CHUNKS) * 16);
+    for (int i = 0; i < LA; ++i) load_lds(base_a, off_a[i], la + ((8 * i + w) * 64) % (BM * CHUNKS_A) * 16);
 #pragma unroll
     for (int i = 0; i < LB; ++i) load_lds(base_b, off_b[i], lb + ((8 * i + w) * 64) % (BN * CHUNKS) * 16);
-    base_a += ROW;
+    base_a += ROW_A;
     base_b += ROW;
   };
   tile32 acc[MI][NI] = {}, low[PARTS == 1 ? 1 : MI][PARTS == 1 ? 1 : NI] = {};
-  frag fa[2][PARTS][MI], fb[2][PARTS][NI];
+  frag fa[2][WHOLE ? 1 : PARTS][MI], fb[2][PARTS][NI];
+  float4 whole[WHOLE ? 2 : 1][MI][2]; // 8 elements of A, not yet in parts
   const int r = lane & 31, half = lane >> 5;
   auto read = [&](int s, const char *la, const char *lb) {
 #pragma unroll
     for (int k = 0; k < PARTS; ++k) {
       const int place = exchanged(r, 4 * k + 2 * s + half) * 16; // (tiles of 32 rows begin at multiples of 32)
+      if constexpr (!WHOLE)
 #pragma unroll
-      for (int i = 0; i < MI; ++i) fa[s & 1][k][i] = *(const frag *)(la + (wa * (BM / WA) + i * 32 + r) * ROW + place);
+        for (int i = 0; i < MI; ++i) fa[s & 1][k][i] = *(const frag *)(la + (wa * (BM / WA) + i * 32 + r) * ROW + place);
 #pragma unroll
       for (int i = 0; i < NI; ++i) fb[s & 1][k][i] = *(const frag *)(lb + (wb * (BN / WB) + i * 32 + r) * ROW + place);
     }
+    if constexpr (WHOLE)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          whole[s & 1][i][c] = *(const float4 *)(la + (wa * (BM / WA) + i * 32 + r) * 128 + exchanged_a(r, 4 * s + 2 * half + c) * 16);
     __builtin_amdgcn_sched_barrier(0); // (left alone the compiler reads right before it multiplies, into the same registers)
   };
   auto multiply = [&](int s) {
+    frag a[PARTS][MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+      if constexpr (WHOLE) {
+        float x[8] = {whole[s & 1][i][0].x, whole[s & 1][i][0].y, whole[s & 1][i][0].z, whole[s & 1][i][0].w,
+                      whole[s & 1][i][1].x, whole[s & 1][i][1].y, whole[s & 1][i][1].z, whole[s & 1][i][1].w};
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+          uint32_t two[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) two[e] = __builtin_amdgcn_perm(__float_as_uint(x[2 * e + 1]), __float_as_uint(x[2 * e]), 0x07060302u); // upper halves
+          a[k][i] = __builtin_bit_cast(frag, *(const uint4 *)two);
+          if (k < PARTS - 1)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] -= __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
+        }
+      } else
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) a[k][i] = fa[s & 1][k][i];
 #pragma unroll
     for (int k = PARTS - 1; k > 0; --k) // parts of A and of B whose numbers add up to k
 #pragma unroll
@@ -147,11 +179,11 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-          for (int j = 0; j < NI; ++j) low[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s & 1][n][i], fb[s & 1][k - n][j], low[i][j], 0, 0, 0);
+          for (int j = 0; j < NI; ++j) low[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[n][i], fb[s & 1][k - n][j], low[i][j], 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s & 1][0][i], fb[s & 1][0][j], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0][i], fb[s & 1][0][j], acc[i][j], 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
   };
   // the next step is in LDS for every wavefront, and every wavefront has what it read before; `later`: the steps behind it may be under way
@@ -220,9 +252,9 @@ __global__ __launch_bounds__(512) void k_product(Product p, Epilogue ep) {
 #pragma unroll
       for (int j = 0; j < NI; ++j) acc[i][j] += low[i][j];
   // element e of a tile: row 8 (e / 4) + 4 half + e % 4 of A, row r of B.  Every wavefront is through with the tiles in LDS
-  constexpr bool HALVES = BM * ROW < 8 * 4096 && BN * ROW < 8 * 4096; // four wavefronts in each array
-  char *const first0 = HALVES ? (w < 4 ? a0 : b0) + w % 4 * 4096 : (BM >= BN ? a0 : b0) + w * 4096;
-  char *const second0 = HALVES ? (w < 4 ? a1 : b1) + w % 4 * 4096 : (BM >= BN ? a1 : b1) + w * 4096;
+  constexpr bool HALVES = BM * ROW_A < 8 * 4096 && BN * ROW < 8 * 4096; // four wavefronts in each array
+  char *const first0 = HALVES ? (w < 4 ? a0 : b0) + w % 4 * 4096 : (BM * ROW_A >= 8 * 4096 ? a0 : b0) + w * 4096;
+  char *const second0 = HALVES ? (w < 4 ? a1 : b1) + w % 4 * 4096 : (BM * ROW_A >= 8 * 4096 ? a1 : b1) + w * 4096;
   const Stage stage = {first0, second0, lane, r, half};
   ep.template finish<MI, NI>(acc, ta * BM + wa * (BM / WA), tb * BN + wb * (BN / WB), slice, stage);
 }
@@ -290,7 +322,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 template <int PARTS> struct GradEpilogue {
   static constexpr bool LOGITS = true;
   const int *targets;
-  const float *state, *dloss, *mean; // dloss [rows], or NULL: mean[0] for each row with a target
+  const float *state, *dloss, *common; // dloss [rows] is taken as multiples of common[0]; NULL: 1 for each row with a target
   __bf16 *gm, *gt;                    // [rows padded][width], [width][rows padded], in parts
   int first, vocab, rows, width, padded;
   template <int MI, int NI> __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int v0, int m0, int, const Stage &st) const {
@@ -301,9 +333,10 @@ template <int PARTS> struct GradEpilogue {
       const int m = m0 + j * 32 + r;
       const bool on = m < rows;
       const int y = entry(targets, m, on, vocab, first + v0 + 4 * half), left = vocab - first - v0 - 4 * half;
-      const float g = has_target(targets, m, on, vocab) ? (dloss ? dloss[m] : *mean) : 0.f, top = on ? state[3 * m] : 0.f, per = on ? state[3 * m + 1] * g : 0.f;
+      const float given = !has_target(targets, m, on, vocab) ? 0.f : dloss ? dloss[m] : 1.f;
+      const bool none = given == 0.f; // no part in the gradients, whatever its logits
+      const float g = dloss ? given / *common : given, top = on ? state[3 * m] : 0.f, per = on ? state[3 * m + 1] * g : 0.f;
       const float miss = on ? state[3 * m + 2] : 0.f;
-      const bool none = g == 0.f; // no part in the gradients, whatever its logits
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -371,7 +404,8 @@ template <int PARTS> struct GradEpilogue {
   }
 };
 
-// C as T, [rows_a][rows_b] with ld elements per row; or in 32 bits, a slice each, added to what is there (add: it is not the first).
+// C as T, times *factor, [rows_a][rows_b] with ld elements per row; or (factor NULL) in 32 bits, a slice each, added to what is there (add: it
+// is not the first).
 // Rows may begin at any element.
 typedef uint32_t words4 __attribute__((ext_vector_type(4)));
 typedef words4 words4_any __attribute__((aligned(4)));
@@ -380,12 +414,14 @@ typedef words2 words2_any __attribute__((aligned(2)));
 template <typename T> struct StoreEpilogue {
   static constexpr bool LOGITS = false;
   T *out;
+  const float *factor;
   long long ld, per_slice;
   int rows_a, rows_b;
   bool add;
   template <int MI, int NI> __device__ __forceinline__ void finish(tile32 (&acc)[MI][NI], int ra, int rb, int slice, const Stage &st) const {
     constexpr int COLS = 32 * NI, LANES = COLS / 4, ROWS = 64 / LANES; // four columns per lane, ROWS rows at once
     T *const to = out + slice * per_slice;
+    const float by = factor ? *factor : 1.f;
     const int c = rb + st.lane % LANES * 4;
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -403,6 +439,10 @@ template <typename T> struct StoreEpilogue {
           const int row = n * ROWS + st.lane / LANES, a = ra + 32 * i + 16 * part + row;
           float4 v = *(const float4 *)(st.first + row * COLS * 4 + st.lane % LANES * 16);
           if (a >= rows_a) continue;
+          v.x *= by;
+          v.y *= by;
+          v.z *= by;
+          v.w *= by;
           T *const at = to + a * ld + c;
           if (c + 4 <= rows_b) {
             if constexpr (sizeof(T) == 4) {
@@ -430,7 +470,7 @@ template <typename T> struct StoreEpilogue {
   }
 };
 
-template <int PARTS, class Epilogue> hipError_t product(Tile t, Product p, const Epilogue &ep, hipStream_t s) {
+template <int PARTS, bool WHOLE, class Epilogue> hipError_t product(Tile t, Product p, const Epilogue &ep, hipStream_t s) {
   constexpr int BN = PARTS == 1 ? 256 : 128, WA = PARTS == 1 ? 2 : 4, WB = 8 / WA; // 64 rows of B to a wavefront
   const int a = rows_of_a(t), b = rows_of_b(t, PARTS);
   p.tiles_a = (p.rows_a + a - 1) / a;
@@ -440,10 +480,10 @@ template <int PARTS, class Epilogue> hipError_t product(Tile t, Product p, const
     p.slice_steps = p.ksteps;
   }
   const dim3 grid(p.tiles_a * p.tiles_b, p.slices);
-  if (t == FEW_B) k_product<256, 64, 8, 1, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
-  else if (t == SMALL) k_product<128, 128, 4, 2, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
-  else if (t == BIG) k_product<256, BN, WA, WB, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
-  else if constexpr (!Epilogue::LOGITS) k_product<64, 256, 1, 8, PARTS, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  if (t == FEW_B) k_product<256, 64, 8, 1, PARTS, WHOLE, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  else if (t == SMALL) k_product<128, 128, 4, 2, PARTS, WHOLE, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  else if (t == BIG) k_product<256, BN, WA, WB, PARTS, WHOLE, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  else if constexpr (!Epilogue::LOGITS) k_product<64, 256, 1, 8, PARTS, WHOLE, Epilogue><<<grid, 512, 0, s>>>(p, ep);
   return hipGetLastError();
 }
 
@@ -484,20 +524,29 @@ struct Operand {
   int vocab, tiles_c;
   unsigned tiles;
 };
-// 64 by 64 elements per workgroup, four in a row per thread, through LDS for the columns.  The last workgroup finds 1 / number of rows with a
-// target, where that is asked for.
-template <typename T, int PARTS> __global__ __launch_bounds__(256) void k_operands(Operand x, Operand y, const int *targets, int rows, int vocab, float *mean) {
+// 64 by 64 elements per workgroup, four in a row per thread, through LDS for the columns.  The last workgroup finds what the rows' dloss have in
+// common, where that is asked for: their largest finite magnitude, or, without any, 1 / number of rows with a target.
+template <typename T, int PARTS> __global__ __launch_bounds__(256) void k_operands(Operand x, Operand y, const int *targets, const float *dloss, int rows, int vocab, float *common) {
   __shared__ float tile[64][65];
   unsigned id = blockIdx.x;
   if (id >= x.tiles + y.tiles) {
-    int count = 0;
-    for (int m = threadIdx.x; m < rows; m += 256) count += has_target(targets, m, true, vocab);
-    int *const counts = (int *)tile;
+    float all = 0.f; // (numbers of rows are exact)
+    for (int m = threadIdx.x; m < rows; m += 256)
+      if (has_target(targets, m, true, vocab)) {
+        const float g = dloss ? fabsf(dloss[m]) : 1.f;
+        all = !dloss ? all + g : g < INFINITY ? fmaxf(all, g) : all;
+      }
 #pragma unroll
-    for (int k = 32; k; k >>= 1) count += __shfl_xor(count, k);
-    if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = count;
+    for (int k = 32; k; k >>= 1) {
+      const float o = __shfl_xor(all, k);
+      all = dloss ? fmaxf(all, o) : all + o;
+    }
+    if ((threadIdx.x & 63) == 0) tile[0][threadIdx.x >> 6] = all;
     __syncthreads();
-    if (threadIdx.x == 0) *mean = 1.f / (counts[0] + counts[1] + counts[2] + counts[3]);
+    if (threadIdx.x == 0) {
+      const float count = tile[0][0] + tile[0][1] + tile[0][2] + tile[0][3];
+      *common = dloss ? fmaxf(fmaxf(tile[0][0], tile[0][1]), fmaxf(tile[0][2], tile[0][3])) : count > 0.f ? 1.f / count : 0.f;
+    }
     return;
   }
   const bool second = id >= x.tiles;
@@ -596,13 +645,13 @@ __global__ __launch_bounds__(1024) void k_join(const float2 *part, const float *
   state[3 * m + 2] = miss;
 }
 
-// to = the sum of the slices, each n elements
-template <typename T> __global__ __launch_bounds__(256) void k_sum(const float *from, int slices, size_t n, T *to) {
+// to = *factor times the sum of the slices, each n elements
+template <typename T> __global__ __launch_bounds__(256) void k_sum(const float *from, int slices, size_t n, const float *factor, T *to) {
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
   float sum = from[i];
   for (int k = 1; k < slices; ++k) sum += from[k * n + i];
-  to[i] = (T)sum;
+  to[i] = (T)(sum * *factor);
 }
 __global__ __launch_bounds__(256) void k_clear(uint16_t *to, size_t n) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) to[i] = 0;
@@ -612,7 +661,7 @@ __global__ __launch_bounds__(256) void k_clear(uint16_t *to, size_t n) {
 struct Space {
   Tile logits; // of the products that make logits
   int parts, dp, padded, width, block; // width: entries of a piece of the vocabulary; block: those of a wavefront
-  size_t h, w, part, picked, mean, ht, wt, gm, gt, sum_h, sum_w, bytes;
+  size_t h, w, part, picked, common, ht, wt, gm, gt, sum_h, sum_w, bytes;
   Space(const VocabShape &p, bool grad) {
     parts = p.bf16 ? 1 : 3;
     logits = tile_for(p.vocab, p.rows, parts, true);
@@ -634,7 +683,7 @@ struct Space {
       part = take(sizeof(float2) * (size_t)(all / block) * p.rows);
       picked = take(sizeof(float) * (size_t)p.rows);
     } else {
-      mean = take(sizeof(float));
+      common = take(sizeof(float));
       ht = take((size_t)2 * parts * p.d * padded);
       wt = take((size_t)2 * parts * p.d * width);
       gm = take((size_t)2 * parts * padded * width);
@@ -654,8 +703,15 @@ struct Space {
     if (e_ != hipSuccess) return e_;              \
   } while (0)
 
-// Whether rows can go into products from where they are: bf16, aligned and whole.
-template <typename T> bool direct(const T *from, long long ld, int cols) { return sizeof(T) == 2 && cols % 64 == 0 && ld % 8 == 0 && (uintptr_t)from % 16 == 0; }
+// Whether rows can go into products from where they are: whole steps, on 16 bytes.  (Floats as A of the products that make logits only.)
+template <typename T> bool direct(const T *from, long long ld, int cols) {
+  return cols % (sizeof(T) == 2 ? 64 : 32) == 0 && ld * sizeof(T) % 16 == 0 && (uintptr_t)from % 16 == 0;
+}
+template <int PARTS, class Epilogue> hipError_t logits(Tile t, bool w_direct, const Product &p, const Epilogue &ep, hipStream_t s) {
+  if constexpr (PARTS > 1)
+    if (w_direct) return product<PARTS, true>(t, p, ep, s);
+  return product<PARTS, false>(t, p, ep, s);
+}
 
 template <typename T> Operand operand(const T *from, long long ld, int rows, int cols, int padded_cols, __bf16 *to_rows, int padded_rows, __bf16 *to_cols) {
   Operand m = {from, ld, rows, cols, padded_cols, padded_rows, to_rows, to_cols, nullptr, nullptr, 0, 0, 0};
@@ -663,10 +719,10 @@ template <typename T> Operand operand(const T *from, long long ld, int rows, int
   m.tiles = to_rows || to_cols ? (unsigned)m.tiles_c * ((unsigned)((to_cols ? padded_rows : rows) + 63) / 64u) : 0;
   return m;
 }
-template <typename T, int PARTS> hipError_t lay_out(const Operand &x, const Operand &y, const int *targets, int rows, int vocab, float *mean, hipStream_t s) {
-  const unsigned blocks = x.tiles + y.tiles + (mean != nullptr);
+template <typename T, int PARTS> hipError_t lay_out(const Operand &x, const Operand &y, const int *targets, const float *dloss, int rows, int vocab, float *common, hipStream_t s) {
+  const unsigned blocks = x.tiles + y.tiles + (common != nullptr);
   if (!blocks) return hipSuccess;
-  k_operands<T, PARTS><<<blocks, 256, 0, s>>>(x, y, targets, rows, vocab, mean);
+  k_operands<T, PARTS><<<blocks, 256, 0, s>>>(x, y, targets, dloss, rows, vocab, common);
   return hipGetLastError();
 }
 
@@ -674,24 +730,24 @@ template <typename T, int PARTS>
 hipError_t loss(const VocabShape &p, const T *h, const T *w, const int *targets, float *loss, float *state, char *work, hipStream_t s) {
   const Space sp(p, false);
   __bf16 *const hr = (__bf16 *)(work + sp.h), *const wr = (__bf16 *)(work + sp.w);
-  const bool h_direct = direct(h, p.ld_h, p.d), w_direct = direct(w, p.ld_w, p.d);
+  const bool h_direct = PARTS == 1 && direct(h, p.ld_h, p.d), w_direct = direct(w, p.ld_w, p.d);
   Product q = {};
   q.rows_b = p.rows;
   q.ksteps = sp.dp / KS<PARTS>;
   q.b = h_direct ? (const __bf16 *)h : hr;
   q.ldb = h_direct ? p.ld_h : sp.dp * PARTS;
-  q.lda = w_direct ? p.ld_w : sp.dp * PARTS;
-  const int width = w_direct ? p.vocab : sp.width;
+  q.lda = w_direct ? p.ld_w * (sizeof(T) / 2) : sp.dp * PARTS;
+  const int width = !w_direct ? sp.width : p.vocab < (1 << 20) ? p.vocab : 1 << 20;
   LossEpilogue ep = {targets, (float2 *)(work + sp.part), (float *)(work + sp.picked), 0, p.vocab, p.rows};
   for (long long v = 0; v < p.vocab; v += width) {
     const int entries = (int)(p.vocab - v < width ? p.vocab - v : width);
     const T *const piece = w + v * p.ld_w;
     TRY((lay_out<T, PARTS>(operand(h, p.ld_h, p.rows, p.d, sp.dp, h_direct || v ? nullptr : hr, 0, nullptr),
-                           operand(piece, p.ld_w, entries, p.d, sp.dp, w_direct ? nullptr : wr, 0, nullptr), nullptr, 0, 0, nullptr, s)));
+                           operand(piece, p.ld_w, entries, p.d, sp.dp, w_direct ? nullptr : wr, 0, nullptr), nullptr, nullptr, 0, 0, nullptr, s)));
     ep.first = (int)v;
     q.rows_a = entries;
     q.a = w_direct ? (const __bf16 *)piece : wr;
-    TRY((product<PARTS>(sp.logits, q, ep, s)));
+    TRY((logits<PARTS>(sp.logits, w_direct, q, ep, s)));
   }
   const int tile_a = rows_of_a(sp.logits), blocks = (p.vocab + tile_a - 1) / tile_a * (tile_a / sp.block);
   k_join<<<(p.rows + 15) / 16, 1024, 0, s>>>(ep.part, ep.picked, targets, blocks, p.rows, p.vocab, loss, state);
@@ -702,10 +758,10 @@ template <typename T, int PARTS>
 hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *targets, const float *state, const float *dloss, T *dh, T *dw,
                      char *work, hipStream_t s) {
   const Space sp(p, true);
-  float *const mean = (float *)(work + sp.mean), *const sum_h = (float *)(work + sp.sum_h), *const sum_w = (float *)(work + sp.sum_w);
+  float *const common = (float *)(work + sp.common), *const sum_h = (float *)(work + sp.sum_h), *const sum_w = (float *)(work + sp.sum_w);
   __bf16 *const hr = (__bf16 *)(work + sp.h), *const wr = (__bf16 *)(work + sp.w), *const ht = (__bf16 *)(work + sp.ht), *const wt = (__bf16 *)(work + sp.wt);
   __bf16 *const gm = (__bf16 *)(work + sp.gm), *const gt = (__bf16 *)(work + sp.gt);
-  const bool h_direct = direct(h, p.ld_h, p.d), w_direct = direct(w, p.ld_w, p.d);
+  const bool h_direct = PARTS == 1 && direct(h, p.ld_h, p.d), w_direct = direct(w, p.ld_w, p.d);
   const int tile_a = rows_of_a(sp.logits);
   const bool summed = sp.width < p.vocab || Slices(p.rows, p.d, sp.width / KS<PARTS>, PARTS).count > 1;
   int slices_h = 1;
@@ -716,28 +772,28 @@ hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *tar
     oh.targets = targets;
     oh.dloss = dloss;
     oh.vocab = p.vocab;
-    TRY((lay_out<T, PARTS>(oh, operand(piece, p.ld_w, entries, p.d, sp.dp, w_direct ? nullptr : wr, width, wt), targets, p.rows, p.vocab, v ? nullptr : mean, s)));
-    Product q = {w_direct ? (const __bf16 *)piece : wr, h_direct ? (const __bf16 *)h : hr, w_direct ? p.ld_w : sp.dp * PARTS,
+    TRY((lay_out<T, PARTS>(oh, operand(piece, p.ld_w, entries, p.d, sp.dp, w_direct ? nullptr : wr, width, wt), targets, dloss, p.rows, p.vocab, v ? nullptr : common, s)));
+    Product q = {w_direct ? (const __bf16 *)piece : wr, h_direct ? (const __bf16 *)h : hr, w_direct ? p.ld_w * (long long)(sizeof(T) / 2) : sp.dp * PARTS,
                  h_direct ? p.ld_h : sp.dp * PARTS, entries, p.rows, sp.dp / KS<PARTS>, 0, 0, 0, 0};
-    TRY((product<PARTS>(sp.logits, q, GradEpilogue<PARTS>{targets, state, dloss, mean, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded}, s)));
+    TRY((logits<PARTS>(sp.logits, w_direct, q, GradEpilogue<PARTS>{targets, state, dloss, common, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded}, s)));
     const Slices sh(p.rows, p.d, width / KS<PARTS>, PARTS, v ? slices_h : 256), sw(entries, p.d, sp.padded / KS<PARTS>, PARTS);
     if (!v) slices_h = sh.count;
     Product dhq = {gm, wt, (long long)width * PARTS, (long long)width * PARTS, p.rows, p.d, width / KS<PARTS>, 0, 0, sh.count, sh.steps};
-    if (!summed) TRY((product<PARTS>(sh.tile, dhq, StoreEpilogue<T>{dh, p.d, 0, p.rows, p.d, false}, s)));
-    else TRY((product<PARTS>(sh.tile, dhq, StoreEpilogue<float>{sum_h, p.d, (long long)p.rows * p.d, p.rows, p.d, v > 0}, s)));
+    if (!summed) TRY((product<PARTS, false>(sh.tile, dhq, StoreEpilogue<T>{dh, common, p.d, 0, p.rows, p.d, false}, s)));
+    else TRY((product<PARTS, false>(sh.tile, dhq, StoreEpilogue<float>{sum_h, nullptr, p.d, (long long)p.rows * p.d, p.rows, p.d, v > 0}, s)));
     Product dwq = {gt, ht, (long long)sp.padded * PARTS, (long long)sp.padded * PARTS, entries, p.d, sp.padded / KS<PARTS>, 0, 0, sw.count, sw.steps};
     T *const to = dw + v * p.d;
-    if (sw.count == 1) TRY((product<PARTS>(sw.tile, dwq, StoreEpilogue<T>{to, p.d, 0, entries, p.d, false}, s)));
+    if (sw.count == 1) TRY((product<PARTS, false>(sw.tile, dwq, StoreEpilogue<T>{to, common, p.d, 0, entries, p.d, false}, s)));
     else {
       const size_t n = (size_t)entries * p.d;
-      TRY((product<PARTS>(sw.tile, dwq, StoreEpilogue<float>{sum_w, p.d, (long long)n, entries, p.d, false}, s)));
-      k_sum<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum_w, sw.count, n, to);
+      TRY((product<PARTS, false>(sw.tile, dwq, StoreEpilogue<float>{sum_w, nullptr, p.d, (long long)n, entries, p.d, false}, s)));
+      k_sum<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum_w, sw.count, n, common, to);
       TRY(hipGetLastError());
     }
   }
   if (summed) {
     const size_t n = (size_t)p.rows * p.d;
-    k_sum<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum_h, slices_h, n, dh);
+    k_sum<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum_h, slices_h, n, common, dh);
   }
   return hipGetLastError();
 }
