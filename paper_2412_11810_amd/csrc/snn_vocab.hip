@@ -650,6 +650,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_sum(const float *
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
   float sum = from[i];
+#pragma unroll 8
   for (int k = 1; k < slices; ++k) sum += from[k * n + i];
   to[i] = (T)(sum * *factor);
 }
