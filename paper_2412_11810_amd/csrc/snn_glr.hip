@@ -120,6 +120,20 @@ struct Rows {
   }
 };
 
+// The state behind the first `count` segments (in the backward pass: G, from the end): their maps applied one after the other, their loads
+// ahead of that.
+template <int VEC> __device__ __forceinline__ void through(const Args &a, int c, int count, float (&h)[VEC]) {
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) h[v] = a.maps[c + v].y;
+#pragma unroll 16
+  for (int k = 1; k <= count; ++k)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      const float2 m = a.maps[(size_t)k * a.channels + c + v];
+      h[v] += fmaf(-m.x, h[v], m.y);
+    }
+}
+
 // LDS of a workgroup: the maps of its wavefronts, for even and odd tiles (a tile's are read while the next one's are written)
 template <int VEC, int N> struct Maps { float v[2][N][WAVES][VEC][64]; };
 
@@ -144,14 +158,9 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
       const float f = a.from && me.on ? a.from[me.c + v] : 0.f;
       if (!MAPS) h[v] = f;
       else if (seg == 0 && w == 0 && me.on) a.maps[me.c + v] = make_float2(0.f, f);
-    } else {
-      h[v] = a.maps[me.c + v].y;
-      for (int k = 1; k <= seg; ++k) {
-        const float2 m = a.maps[(size_t)k * a.channels + me.c + v];
-        h[v] += m.y - m.x * h[v];
-      }
     }
   }
+  if (!MAPS && a.segments > 1) through<VEC>(a, me.c, seg, h);
   // (a state that `to` may take the place of is read by every wavefront before the first one may write it)
 #pragma unroll
   for (int v = 0; v < VEC; ++v) asm volatile("" ::"v"(h[v]));
@@ -278,14 +287,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
       const float f = a.from && me.on ? a.from[me.c + v] : 0.f;
       if (!MAPS) g[v] = f;
       else if (seg == 1 && w == 0 && me.on) a.maps[me.c + v] = make_float2(0.f, f);
-    } else {
-      g[v] = a.maps[me.c + v].y;
-      for (int k = 1; k < a.segments - seg; ++k) {
-        const float2 m = a.maps[(size_t)k * a.channels + me.c + v];
-        g[v] += m.y - m.x * g[v];
-      }
     }
   }
+  if (!MAPS && a.segments > 1) through<VEC>(a, me.c, a.segments - 1 - seg, g);
 #pragma unroll
   for (int v = 0; v < VEC; ++v) asm volatile("" ::"v"(g[v])); // (as in the forward pass)
   typename Raw<P, VEC>::type rz[STEPS], rx[STEPS];

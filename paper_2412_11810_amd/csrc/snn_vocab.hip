@@ -15,9 +15,12 @@
 // accumulators; what differs is what happens to the accumulators.  Operands of 32 bits go in as three bf16 parts of 8 bits
 // each, which hold all 24 bits of a float; of the nine products of parts the six whose weight is above 2^-24 are made, the one of the
 // first parts in accumulators of its own.
-// The logits are computed twice, for the loss (kept: one exponent and one sum for 128 of them) and for G, one piece of the
-// vocabulary after the other, whose G is all that is ever in memory; a second product of 2 rows d vocab operations costs less
-// than 4 bytes of logit written and read for each.
+// The logits are computed twice, for the loss (kept: an exponent and a sum for 32 to 128 of them) and for G, one piece of the vocabulary
+// after the other, whose G is all that is ever in memory.
+//
+// What bounds it: the matrix cores, at the clock that they leave.  8192 x 2048 x 128000 in bf16 takes 15.0 ms, four products of 4.3 TFLOP at
+// 1.15 PFLOP/s (a library product of the same shape: 1.20); the loss alone 1.17 to 1.24 PFLOP/s, matrix instructions in 69 % of
+// the cycles at 1.96 GHz.  Few rows are bound by w: 12 x 768 x 99960 in fp32, 307 MB, takes 93 us.
 #include "snn_ops.h"
 
 namespace {
@@ -267,8 +270,7 @@ __device__ __forceinline__ int entry(const int *targets, int m, bool on, int voc
 }
 
 // Logits, A = vocabulary (a piece of it from `first` on), B = rows of h.  A lane has the logits of one row with 16 MI entries of the
-// vocabulary: the exponent M of the largest and the
-// sum of the powers above it, the target left out, and the target's logit go to memory.
+// vocabulary: the exponent M of the largest and the sum of the powers above it, the target left out, and the target's logit go to memory.
 struct LossEpilogue {
   static constexpr bool LOGITS = true;
   const int *targets;
@@ -289,7 +291,7 @@ struct LossEpilogue {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int v = 32 * i + 8 * (e >> 2) + (e & 3);
-            if (v == y && on) picked[m] = acc[i][j][e];
+            if (v == y) picked[m] = acc[i][j][e];
             if (v == y || v0 + v >= vocab) acc[i][j][e] = -INFINITY;
           }
       }
@@ -405,8 +407,7 @@ template <int PARTS> struct GradEpilogue {
 };
 
 // C as T, times *factor, [rows_a][rows_b] with ld elements per row; or (factor NULL) in 32 bits, a slice each, added to what is there (add: it
-// is not the first).
-// Rows may begin at any element.
+// is not the first).  Rows may begin at any element.
 typedef uint32_t words4 __attribute__((ext_vector_type(4)));
 typedef words4 words4_any __attribute__((aligned(4)));
 typedef uint32_t words2 __attribute__((ext_vector_type(2)));
