@@ -10,6 +10,11 @@
 // exchange their maps through LDS and then know the state that each of them starts from: one read of z and x, one write of h.
 // The state before every 128 steps is what the forward pass keeps; the backward pass gets h_{t-1} from there by
 // the same exchange, beside that of the gradient, which runs the other way.
+//
+// What bounds it: memory, where there are channels or steps enough.  Forward, 4096 x 8 x 2048 in bf16: 94 us, 4.3 TB/s of z, x and h (a copy reaches
+// 5.1); backward, 1000 x 32 x 1024 in fp32: 123 us, 5.3 TB/s; 32768 x 1 x 1024 in bf16: 96 us, of which 26 for the maps of its
+// segments; from 8 bits, 4096 x 8 x 2048: 139 to 145 us, 3.8 TB/s, bound by the number of 1- and 2-byte loads.  One token of 64 x 2048: 3.3 us.
+// Short sequences are bound by the latency of a tile, some 5 us.
 #include "snn_ops.h"
 
 namespace {
@@ -81,7 +86,7 @@ template <int VEC> struct Lane {
   __device__ __forceinline__ Lane(const Args &a) {
     c = (blockIdx.x * 64 + threadIdx.x) * VEC;
     on = c < a.channels;
-    if (!on) c = 0;
+    if (!on) c = a.channels - VEC;
     b = c / a.n;
     i = c - b * a.n;
     len = a.T;
@@ -133,6 +138,32 @@ template <int VEC> __device__ __forceinline__ void through(const Args &a, int c,
       h[v] += fmaf(-m.x, h[v], m.y);
     }
 }
+
+// The exponent bytes of a wavefront's 16 steps where its channels lie in four blocks at most: one load, lane l has step l / 4 and the
+// block of number l % 4, and the lanes get theirs from there (512 x 64 x 2048: 118 us; a load for each step: 135 us).
+struct Exponents {
+  unsigned at; // of the block that the lane loads
+  int slot;    // of the four, the one that the lane's channels are in
+  __device__ __forceinline__ Exponents(const Rows &rows, int block) {
+    const int lane = threadIdx.x;
+    const int before = __shfl_up(block, 1); // (by every lane: none reads from one that takes no part)
+    const uint64_t firsts = __ballot(lane == 0 || before != block); // (blocks of neighbouring lanes are the same or the next)
+    slot = __popcll(firsts & (~0ull >> (63 - lane))) - 1;
+    uint64_t m = firsts;
+    const int want = min(lane & 3, __popcll(firsts) - 1);
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < want) m &= m - 1;
+    at = (unsigned)__shfl((int)rows.at, __ffsll((unsigned long long)m) - 1);
+  }
+  __device__ __forceinline__ uint32_t load(const Rows &rows, int t0, int T) const {
+    const int first = min(t0, T - 1), last = T - 1 - first;
+    return __builtin_amdgcn_raw_buffer_load_b8(rows.from(first), (int)(at + (unsigned)min((int)threadIdx.x >> 2, last) * rows.step), 0, 0);
+  }
+  __device__ __forceinline__ uint32_t of(uint32_t loaded, int j) const {
+    return (uint32_t)__builtin_amdgcn_ds_bpermute((4 * j + slot) * 4, (int)loaded);
+  }
+};
 
 // LDS of a workgroup: the maps of its wavefronts, for even and odd tiles (a tile's are read while the next one's are written)
 template <int VEC, int N> struct Maps { float v[2][N][WAVES][VEC][64]; };
@@ -264,9 +295,9 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
 }
 
 // Backward pass of one segment, last tile first.  P: the type of z and x in memory (int8_t: codes of blocks, with their exponent
-// bytes).  MAPS: only the map of the segment's gradient, G at its end -> G at its beginning, which takes no x and no state; segment s
+// bytes; SHARED: a wavefront's channels lie in four blocks at most).  MAPS: only the map of the segment's gradient, G at its end -> G at its beginning, which takes no x and no state; segment s
 // writes maps[segments - s].
-template <typename T, typename P, int VEC, bool MAPS>
+template <typename T, typename P, int VEC, bool SHARED, bool MAPS>
 __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
   constexpr bool PACKED = sizeof(P) == 1;
   __shared__ Maps<VEC, 3> maps;
@@ -294,6 +325,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
   for (int v = 0; v < VEC; ++v) asm volatile("" ::"v"(g[v])); // (as in the forward pass)
   typename Raw<P, VEC>::type rz[STEPS], rx[STEPS];
   R rd[STEPS];
+  const int block = me.b * ((a.n + SNN_PACK_BLOCK - 1) / SNN_PACK_BLOCK) + me.i / SNN_PACK_BLOCK;
+  const Exponents of_z(pze, SHARED ? block : 0), of_x(pxe, SHARED ? block : 0);
+  uint32_t shared_z = 0, shared_x = 0;
   uint8_t ez[STEPS], ex[STEPS];
   float kept[VEC];
   auto fetch = [&](int k) {
@@ -301,7 +335,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
     pz.load(rz, t, a.T);
     pd.load(rd, t, a.T);
     if (!MAPS) px.load(rx, t, a.T);
-    if (PACKED) {
+    if (PACKED && SHARED) {
+      shared_z = of_z.load(pze, t, a.T);
+      if (!MAPS) shared_x = of_x.load(pxe, t, a.T);
+    } else if (PACKED) {
       pze.load(ez, t, a.T);
       if (!MAPS) pxe.load(ex, t, a.T);
     }
@@ -326,11 +363,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
         widen<P, VEC>(rz[j], z);
         if (!MAPS) widen<P, VEC>(rx[j], x[j]);
         d[j] = ALL || j < live ? rd[j] : (R)0;
+        // (a step is a power of two: its product with log2(e) is exact)
+        const float step_z = PACKED ? __uint_as_float((SHARED ? of_z.of(shared_z, j) : (uint32_t)ez[j]) << 23) * LOG2E : LOG2E;
+        const float step_x = PACKED && !MAPS ? __uint_as_float((SHARED ? of_x.of(shared_x, j) : (uint32_t)ex[j]) << 23) : 1.f;
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
-          // (a step is a power of two: its product with log2(e) is exact)
-          z[v] *= PACKED ? __uint_as_float((uint32_t)ez[j] << 23) * LOG2E : LOG2E;
-          if (PACKED && !MAPS) x[j][v] *= __uint_as_float((uint32_t)ex[j] << 23);
+          z[v] *= step_z;
+          if (PACKED && !MAPS) x[j][v] *= step_x;
           b[j][v] = ALL || j < live ? moved(z[v]) : 0.f;
           if (!MAPS) x[j][v] = ALL || j < live ? x[j][v] : 0.f;
         }
@@ -479,15 +518,15 @@ template <typename T, int VEC> hipError_t forward(Args a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, typename P, int VEC> hipError_t backward(Args a, hipStream_t s) {
+template <typename T, typename P, int VEC, bool SHARED = false> hipError_t backward(Args a, hipStream_t s) {
   const dim3 groups((a.channels + 64 * VEC - 1) / (64 * VEC));
   cut(&a, VEC);
   if (a.segments > 1) {
-    k_glr_backward<T, P, VEC, true><<<dim3(groups.x, a.segments - 1), dim3(64, WAVES), 0, s>>>(a);
+    k_glr_backward<T, P, VEC, SHARED, true><<<dim3(groups.x, a.segments - 1), dim3(64, WAVES), 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  k_glr_backward<T, P, VEC, false><<<dim3(groups.x, a.segments), dim3(64, WAVES), 0, s>>>(a);
+  k_glr_backward<T, P, VEC, SHARED, false><<<dim3(groups.x, a.segments), dim3(64, WAVES), 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -535,10 +574,13 @@ hipError_t launch_glr_backward(const GlrShape &p, const GlrInputs &in, const flo
     a.ld_ze = in.ld_ze;
     a.ld_xe = in.ld_xe;
   }
-  if (!p.bf16) return packed ? backward<float, int8_t, 1>(a, s) : backward<float, float, 1>(a, s);
+  // 64 channels in a row begin in four blocks at most if there is no more than one row's end among them, 128 if rows are multiples of that
+  const bool shared = p.n >= 64;
+  if (!p.bf16) return !packed ? backward<float, float, 1>(a, s) : shared ? backward<float, int8_t, 1, true>(a, s) : backward<float, int8_t, 1>(a, s);
   const size_t size = packed ? 1 : 2;
   const bool two = two_per_lane(p) && pairs(in.z, size, a.ld_z) && pairs(in.x, size, a.ld_x) && pairs(dh, 2, p.ld_h) &&
                    pairs(dz, 2, p.ld_dz) && pairs(dx, 2, p.ld_dx);
-  if (packed) return two ? backward<__bf16, int8_t, 2>(a, s) : backward<__bf16, int8_t, 1>(a, s);
+  if (packed && two) return p.n % 128 == 0 ? backward<__bf16, int8_t, 2, true>(a, s) : backward<__bf16, int8_t, 2>(a, s);
+  if (packed) return shared ? backward<__bf16, int8_t, 1, true>(a, s) : backward<__bf16, int8_t, 1>(a, s);
   return two ? backward<__bf16, __bf16, 2>(a, s) : backward<__bf16, __bf16, 1>(a, s);
 }

@@ -183,6 +183,20 @@ def test_glr_backward(T, B, n, ragged, dtype, packed):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,B,n", [(1, 64, 130), (20, 40, 65), (33, 7, 97), (18, 9, 63), (40, 11, 64), (16, 300, 3), (40, 160, 130), (40, 170, 128),
+                                   (20, 200, 160)])
+def test_glr_backward_from_bytes_is_that_of_their_values(T, B, n, dtype):
+    # rows that end anywhere in a wavefront's channels; steps are powers of two: the same products, hence the same bits
+    z, x, dh, h0, dlast, _ = glr_inputs(T, B, n, dtype, False, seed=9)
+    z *= torch.exp(torch.randn(B, n, device="cuda")).to(dtype)
+    pz, px = snn.snn_pack(z), snn.snn_pack(x)
+    z, x = snn.snn_unpack(pz, dtype), snn.snn_unpack(px, dtype)
+    kept = snn.snn_glr_forward(z, x, h0, keep=True)[2]
+    assert same(snn.snn_glr_backward(pz, px, kept, dh, dlast), snn.snn_glr_backward(z, x, kept, dh, dlast))
+
+
+@gpu
 def test_glr_state_in_place_is_a_sequence_cut_anywhere():
     z, x, dh, h0, _, _ = glr_inputs(300, 3, 50, torch.float32, False)
     whole, last, _ = snn.snn_glr_forward(z, x, h0)
