@@ -208,6 +208,62 @@ def test_glr_state_in_place_is_a_sequence_cut_anywhere():
 
 
 @gpu
+def test_glr_lengths_outside_count_as_the_nearer_end():
+    z, x, dh, h0, _, _ = glr_inputs(200, 4, 70, torch.float32, False)
+    lengths = torch.tensor([-5, 207, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda")
+    inside = torch.tensor([0, 200, 200, 0], dtype=torch.int32, device="cuda")
+    got, want = (snn.snn_glr_forward(z, x, h0, lengths=v, keep=True) for v in (lengths, inside))
+    assert same(got, want) and same(*(snn.snn_glr_backward(z, x, want[2], dh, lengths=v) for v in (lengths, inside)))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T,B,n", [(40, 3, 66), (700, 2, 70)])
+def test_glr_rows_of_wider_arrays(T, B, n, dtype):
+    z, x, dh, h0, dlast, _ = glr_inputs(T, B, n, dtype, False, seed=4)
+    wide = torch.full((T, B, 5 * n + 2), math.nan, dtype=dtype, device="cuda")
+    parts = [wide[..., i * n:(i + 1) * n] for i in range(5)]
+    for to, v in zip(parts, (z, x, dh)):
+        to.copy_(v)
+    h, last, kept = snn.snn_glr_forward(z, x, h0, keep=True)
+    assert same(snn.snn_glr_forward(parts[0], parts[1], h0, keep=True, h=parts[3]), [h, last, kept])
+    want = snn.snn_glr_backward(z, x, kept, dh, dlast)
+    assert same(snn.snn_glr_backward(parts[0], parts[1], kept, parts[2], dlast, dz=parts[3], dx=parts[4]), want)
+    assert torch.isnan(wide[..., 5 * n:]).all()
+
+
+@gpu
+@pytest.mark.parametrize("T", [20, 1000])
+def test_glr_gradient_of_the_state_in_place(T):
+    z, x, dh, h0, dlast, _ = glr_inputs(T, 3, 50, torch.float32, False, seed=6)
+    kept = snn.snn_glr_forward(z, x, h0, keep=True)[2]
+    want = snn.snn_glr_backward(z, x, kept, dh, dlast)
+    dz, dx, state = torch.empty_like(z), torch.empty_like(z), dlast.clone()
+    p = ops.snn_glr(T, 3, 50, 0, 0, 0, 0, 0, 0, None)
+    work = snn.lib().snn_glr_workspace(C.byref(p))
+    space = torch.empty(max(work, 1), dtype=torch.uint8, device="cuda")
+    at = ops.snn_launch(0, torch.cuda.current_stream().cuda_stream, space.data_ptr(), work)
+    ops._run("snn_glr_backward", C.byref(at), C.byref(p), *(a.data_ptr() for a in (z, x, kept, dh, state, dz, dx, state)))
+    assert same([dz, dx, state], want)
+
+
+@gpu
+def test_glr_many_segments():
+    z, x, dh, h0, dlast, lengths = glr_inputs(20000, 1, 3, torch.float32, False, seed=8)
+    zc, xc, hc, lc = z.double().cpu(), x.double().cpu(), h0.double().cpu(), lengths.cpu()
+    h, last, kept = snn.snn_glr_forward(z, x, h0, keep=True)
+    want, back = glr_forward(zc, xc, hc, lc), glr_backward(zc, xc, hc, lc, dh.double().cpu(), dlast.double().cpu())
+    zmax, bmin, M = bounds(zc, xc, hc, lc)
+    tol = 4 * M * E32 * (zmax + 4 + 1 / bmin)
+    for got, ref, what in zip((h, last, kept), want, ("h", "last", "kept")):
+        near(got, ref, tol, what)
+    dx, dh0 = snn.snn_glr_backward(z, x, kept, dh, dlast)[1:]
+    e_g = 4 * back[3] * E32 * (zmax + 4 + 1 / bmin)
+    near(dx, back[1], e_g + back[3] * (zmax + 4) * E32, "dx")
+    near(dh0, back[2], e_g, "dh0")
+
+
+@gpu
 def test_glr_long_memory_keeps_its_drive():
     # gates so near one that 1 - a in 32 bits would be off by 30 %: the state still tends to its drive, 1
     T = 4096
@@ -307,7 +363,7 @@ def check_vocab(h, w, t, dloss, given_h=None, given_w=None):
 @gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("rows,d,vocab", [(1, 1, 1), (1, 64, 2), (3, 5, 7), (2, 64, 1000), (33, 100, 129), (257, 128, 513), (300, 72, 1025),
-                                          (64, 256, 128), (31, 1000, 300), (600, 320, 2500)])
+                                          (64, 256, 128), (31, 1000, 300), (600, 320, 2500), (700, 40, 3), (5000, 33, 17)])
 def test_vocab(rows, d, vocab, dtype):
     check_vocab(*vocab_inputs(rows, d, vocab, dtype))
 
@@ -326,6 +382,27 @@ def test_vocab_rows_of_wider_arrays(d, dtype):
     wide_h, wide_w = torch.full((100, d + 5), math.nan, dtype=dtype), torch.full((300, d + 8), math.nan, dtype=dtype)
     wide_h[:, 3:3 + d], wide_w[:, 8:] = h, w
     check_vocab(h, w, t, dloss, wide_h.cuda()[:, 3:3 + d], wide_w.cuda()[:, 8:])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_vocab_gradients_of_the_losses_of_any_size(dtype):
+    # rows' factors from 1e-12 to 1e6, of either sign, and none: relative to the largest of them nothing is lost
+    h, w, t, _ = vocab_inputs(130, 96, 400, dtype)
+    g = torch.Generator().manual_seed(1)
+    dloss = 10 ** (torch.rand(130, generator=g) * 18 - 12) * torch.sign(torch.randn(130, generator=g))
+    dloss[::7] = 0
+    h[7] = math.nan  # a row whose loss has no gradient takes no part
+    t[7] = 5
+    gh, gw, gt = h.cuda(), w.cuda(), t.cuda()
+    state = snn.snn_vocab_loss(gh, gw, gt)[1]
+    dh, dw = snn.snn_vocab_loss_grad(gh, gw, gt, state, dloss.cuda())
+    H = torch.where(dloss[:, None] == 0, 0.0, h.double())
+    G, want_h, want_w = vocab_grads(H, w.double(), t.long(), dloss.double())
+    # logits of 96 products (fp32: 6 each) of up to 12 in magnitude, then the roundings of G; sums of 400 and 130 terms
+    rel = 4 * 600 * E32 * (H.abs() @ w.double().abs().T).amax() + (2.0 ** -8 if dtype == torch.bfloat16 else 0)
+    near(dh, want_h, (rel + 6 * 408 * E32) * (G.abs() @ w.double().abs()) + 1e-36, "dh")
+    near(dw, want_w, (rel + 6 * 138 * E32) * (G.abs().T @ H.abs()) + 1e-36, "dw")
 
 
 @gpu
