@@ -38,20 +38,22 @@ template <int PARTS> __device__ __forceinline__ size_t place_of(size_t row, int 
   return (row * padded + (c & ~31)) * PARTS + part * 32 + (c & 31);
 }
 // Tiles: 256 rows of A by 256 of B, or, in parts, by 128; 64 by 256 where a side has no more than 64 rows (products that make logits: that of B
-// only); 128 by 128 where there would be fewer than 128 tiles, half the compute units (loss and gradients in bf16, 300 x 512 x 1000: 82 us with
-// large tiles, 42 us with these; 2048 x 1024 x 4096: 144 and 122 us; 1024 x 1024 x 32000, 500 tiles: 347 and 349 us).
+// only); 128 by 128 where 256 compute units are through with those sooner.  An element of a small tile takes 1.3 to 1.45 times as long
+// (the loss of 4096 x 2048 x 50021 in bf16 takes 721 us with large tiles and 909 us with small ones), in parts less than 1.12 times (2000 x 1024 x
+// 20011 in fp32 with gradients: 1.95 and 1.93 ms), but few large tiles leave units without work (loss and gradients in bf16, 300 x 512 x 1000: 82
+// and 42 us; 2048 x 1024 x 4096: 144 and 115 us).
 enum Tile { BIG, SMALL, FEW_A, FEW_B };
 int rows_of_a(Tile t) { return t == FEW_A ? 64 : t == SMALL ? 128 : 256; }
 int rows_of_b(Tile t, int parts) { return t == FEW_B ? 64 : t == FEW_A ? 256 : t == SMALL || parts > 1 ? 128 : 256; }
-int tiles(Tile t, int rows_a, int rows_b, int parts) {
+long long tiles(Tile t, int rows_a, int rows_b, int parts) {
   const int a = rows_of_a(t), b = rows_of_b(t, parts);
-  return ((rows_a + a - 1) / a) * ((rows_b + b - 1) / b);
+  return (long long)((rows_a + a - 1) / a) * ((rows_b + b - 1) / b);
 }
 Tile tile_for(int rows_a, int rows_b, int parts, bool logits) {
   if (rows_a <= 64 && !logits) return FEW_A;
   if (rows_b <= 64) return FEW_B;
-  const int a = rows_of_a(BIG), b = rows_of_b(BIG, parts);
-  return (long long)((rows_a + a - 1) / a) * ((rows_b + b - 1) / b) < 128 ? SMALL : BIG;
+  auto time = [&](Tile t, float each) { return (float)((tiles(t, rows_a, rows_b, parts) + 255) / 256) * rows_of_a(t) * rows_of_b(t, parts) * each; };
+  return time(SMALL, parts == 1 ? 1.45f : 1.12f) < time(BIG, 1.f) ? SMALL : BIG;
 }
 
 // ---- C = A B^T ----------------------------------------------------------------------------
@@ -495,7 +497,7 @@ struct Slices {
   int count, steps;
   Slices(int rows_a, int rows_b, int ksteps, int parts, int at_most = 256) {
     tile = tile_for(rows_a, rows_b, parts, false);
-    const int most = 256 / tiles(tile, rows_a, rows_b, parts), fit = ksteps / (parts == 1 ? 8 : 4), n = most < fit ? most : fit;
+    const int most = (int)(256 / tiles(tile, rows_a, rows_b, parts)), fit = ksteps / (parts == 1 ? 8 : 4), n = most < fit ? most : fit;
     count = n < 1 ? 1 : n < at_most ? n : at_most;
     steps = (ksteps + count - 1) / count;
     count = (ksteps + steps - 1) / steps;
