@@ -12,8 +12,8 @@
 // the same exchange, beside that of the gradient, which runs the other way.
 //
 // What bounds it: memory, where there are channels or steps enough.  Forward, 4096 x 8 x 2048 in bf16: 94 us, 4.3 TB/s of z, x and h (a copy reaches
-// 5.1); backward, 1000 x 32 x 1024 in fp32: 123 us, 5.3 TB/s; 32768 x 1 x 1024 in bf16: 96 us, of which 26 for the maps of its
-// segments; from 8 bits, 4096 x 8 x 2048: 139 to 145 us, 3.8 TB/s, bound by the number of 1- and 2-byte loads.  One token of 64 x 2048: 3.3 us.
+// 5.1); backward, 1000 x 32 x 1024 in fp32: 123 us, 5.3 TB/s; 32768 x 1 x 1024 in bf16: 97 us, of which 26 for the maps of its
+// segments; from 8 bits, 4096 x 8 x 2048: 146 us, 3.7 TB/s, bound by the number of 1- and 2-byte loads.  One token of 64 x 2048: 3.2 us.
 // Short sequences are bound by the latency of a tile, some 5 us.
 #include "snn_ops.h"
 

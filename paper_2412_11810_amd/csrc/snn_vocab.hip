@@ -18,8 +18,8 @@
 // The logits are computed twice, for the loss (kept: an exponent and a sum for 32 to 128 of them) and for G, one piece of the vocabulary
 // after the other, whose G is all that is ever in memory.
 //
-// What bounds it: the matrix cores, at the clock that they leave.  8192 x 2048 x 128000 in bf16 takes 15.0 ms, four products of 4.3 TFLOP at
-// 1.15 PFLOP/s (a library product of the same shape: 1.20); the loss alone 1.17 to 1.24 PFLOP/s, matrix instructions in 69 % of
+// What bounds it: the matrix cores, at the clock that they leave.  8192 x 2048 x 128000 in bf16 takes 15.2 ms, four products of 4.3 TFLOP at
+// 1.13 PFLOP/s (a library product with sums of 2048: 1.20); the loss of 4096 x 2048 x 50021 719 us, 1.17 PFLOP/s, matrix instructions in 69 % of
 // the cycles at 1.96 GHz.  Few rows are bound by w: 12 x 768 x 99960 in fp32, 307 MB, takes 93 us.
 #include "snn_ops.h"
 
