@@ -280,7 +280,7 @@ void snn_destroy(snn_ctx *ctx);
  * the input, activations kept in 8 bits for the backward pass, and the cross entropy of a readout over a whole vocabulary.
  *
  * Every array is in the memory of snn_launch.device (SNN_E_INVAL otherwise, NULL where it is not optional included), aligned
- * to its elements; an array of outputs overlaps no other array of the call unless said otherwise.  The calls queue their kernels on
+ * to its elements; no element of a result is one of another array of the call unless said otherwise.  The calls queue their kernels on
  * snn_launch.stream and return: they wait for nothing, allocate nothing, keep nothing and may be captured into a HIP graph.
  * Arguments are checked before anything is queued.  The workspace belongs to a call until its kernels have run, is not read before it is written, and
  * needs to be aligned to 256 bytes; calls that may run at the same time (two streams, two graphs) need one each.  Two calls with the same
@@ -308,7 +308,7 @@ typedef struct {
                                  per step.  z and x may be the halves of one projection [T][batch][2 n], and dz and dx those of its gradient */
   int64_t ld_dz, ld_dx;       /* the same of dz, dx (not used by the forward pass) */
   const int32_t *lengths;     /* [batch] or NULL (T each): sequence b has steps 1..lengths[b]; a number outside 0..T counts as the nearer
-                                 end.  Later steps are read by nothing; h, dz and dx are zeros there */
+                                 end.  What later steps hold does not matter; h, dz and dx are zeros there */
 } snn_glr;
 
 /* Bytes of workspace for snn_glr_forward and both snn_glr_backward calls of this shape (0 for an invalid one too). */
