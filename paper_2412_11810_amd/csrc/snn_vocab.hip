@@ -57,7 +57,8 @@ Tile tile_for(int rows_a, int rows_b, int parts, bool logits) {
 }
 
 // ---- C = A B^T ----------------------------------------------------------------------------
-// Operands: rows of ksteps * STEP bytes.  Rows past the last one are the last one again (not used by the epilogues).
+// Operands: rows of ksteps * STEP bytes.  Rows past the last one are the last one again (not used by the epilogues).  The bytes from a
+// tile's first row to the end of its last one fit 32 bits (vocab_shape() and Slices see to it).
 struct Product {
   const __bf16 *a, *b;
   long long lda, ldb; // elements from row to row, of all parts
@@ -491,12 +492,14 @@ template <int PARTS, bool WHOLE, class Epilogue> hipError_t product(Tile t, Prod
 }
 
 // A product with fewer tiles than half the compute units is cut along its sums, eight steps (in parts: four) or more each; the slices are
-// added up afterwards, in order.
+// added up afterwards, in order.  A tile's rows are reached by 32-bit offsets from its first one: where 256 of them would lie further apart
+// (dw in fp32, from 2.8 million rows of h on) a tile has 128, which do not at 2^22 rows of three parts either.
 struct Slices {
   Tile tile;
   int count, steps;
   Slices(int rows_a, int rows_b, int ksteps, int parts, int at_most = 256) {
-    tile = tile_for(rows_a, rows_b, parts, false);
+    const unsigned long long row = (unsigned long long)ksteps * (parts == 1 ? STEP<1> : STEP<3>); // bytes (of dw's operands: of all rows of h)
+    tile = 256 * row <= UINT32_MAX ? tile_for(rows_a, rows_b, parts, false) : SMALL;
     const int most = (int)(256 / tiles(tile, rows_a, rows_b, parts)), fit = ksteps / (parts == 1 ? 8 : 4), n = most < fit ? most : fit;
     count = n < 1 ? 1 : n < at_most ? n : at_most;
     steps = (ksteps + count - 1) / count;

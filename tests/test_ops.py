@@ -765,3 +765,26 @@ def test_workspaces_and_host_arrays_are_checked():
     refused(lambda: call(space.data_ptr(), need, arrays=[host.data_ptr(), *args[1:]]), "z is not in")
     pinned = torch.zeros(1000, 1, 64, pin_memory=True)
     refused(lambda: call(space.data_ptr(), need, arrays=[pinned.data_ptr(), *args[1:]]), "z is not in")
+
+
+# ---- as many rows as there may be -----------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("d,vocab", [(64, 300), (250, 60)])
+def test_vocab_weight_gradients_of_many_rows(d, vocab):
+    # rows of G the other way round are 6 * rows bytes in fp32: 256 of them in a tile are more than 4 GB
+    rows = 2_900_000
+    g = torch.Generator(device="cuda").manual_seed(4)
+    h = torch.empty((rows, d), device="cuda").normal_(generator=g).abs_()
+    w = torch.empty((vocab, d), device="cuda").normal_(0.0, 2 / math.sqrt(d), generator=g)
+    t = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    state = snn.snn_vocab_loss(h, w, t)[1]
+    dw = snn.snn_vocab_loss_grad(h, w, t, state)[1]
+    want, W = torch.zeros((vocab, d), dtype=torch.float64, device="cuda"), w.double()
+    for a in range(0, rows, 290_000):
+        H = h[a:a + 290_000].double()
+        G = torch.softmax(H @ W.T, 1)
+        G[:, 0] = -G[:, 1:].sum(1)
+        want += G.T @ H / rows
+    # every term of a sum has the sign of the others: 16 products at least are added at a time, hence rows / 16 roundings at most; logits
+    # of up to 6 d products of up to 5 * 10 / sqrt(d)
+    near(dw, want.cpu(), ((rows / 16 + 16) * E32 + 4 * (6 * d + 8) * E32) * want.abs().cpu(), "dw")
