@@ -335,7 +335,8 @@ typedef struct {
   int64_t ld, ld_exps; /* elements between consecutive rows; 0: packed */
 } snn_packed;
 
-/* x: rows of cols elements, ld from one to the next (0: cols) -> codes [rows][cols], exps [rows][ceil(cols / 32)] */
+/* x: rows of cols elements (2^31 - 1 rows, 2^30 of a row and 2^40 in all at most), ld from one row to the next (0: cols)
+ * -> codes [rows][cols], exps [rows][ceil(cols / 32)] */
 snn_status snn_pack(const snn_launch *at, int dtype, int64_t rows, int32_t cols, int64_t ld, const void *x, int8_t *codes, uint8_t *exps);
 /* and back: x = code * step, rounded to dtype */
 snn_status snn_unpack(const snn_launch *at, int dtype, int64_t rows, int32_t cols, int64_t ld, const int8_t *codes, const uint8_t *exps,

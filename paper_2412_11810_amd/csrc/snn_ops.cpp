@@ -110,7 +110,7 @@ snn_status glr_backward(const char *what, const snn_launch *at, const snn_glr *p
 snn_status pack_shape(const char *what, const snn_launch *at, int dtype, int64_t rows, int32_t cols, int64_t *ld) {
   CHECK(launch_ok(what, at));
   if (!dtype_ok(dtype)) return refuse(SNN_E_INVAL, "%s: unknown type %d", what, dtype);
-  if (rows < 0 || rows > INT32_MAX || cols < 1 || cols > (1 << 30) || (rows && cols > (1ll << 42) / rows))
+  if (rows < 0 || rows > INT32_MAX || cols < 1 || cols > (1 << 30) || (rows && cols > (1ll << 40) / rows))
     return refuse(SNN_E_INVAL, "%s: %lld rows of %d", what, (long long)rows, cols);
   if (!*ld) *ld = cols;
   if (*ld < cols) return refuse(SNN_E_INVAL, "%s: %lld elements from row to row, fewer than a row has", what, (long long)*ld);

@@ -64,13 +64,15 @@ template <typename T> __device__ __forceinline__ void write(T *p, int count, con
 }
 
 // The place of a thread: a row and the first of its 8 columns.  `across` threads (a power of two, whole blocks) lie side by side in a row.
+// A grid has fewer than 2^32 threads along x: the workgroups of more rows than that go on along y.
+constexpr unsigned GRID_X = 1u << 22;
 struct Place {
   long long row;
   int col;
   __device__ __forceinline__ Place(int across, int col_groups) {
     const int down = THREADS / across;
-    const unsigned group = blockIdx.x % (unsigned)col_groups;
-    row = (long long)(blockIdx.x / (unsigned)col_groups) * down + threadIdx.x / across;
+    const unsigned block = blockIdx.y * GRID_X + blockIdx.x, group = block % (unsigned)col_groups;
+    row = (long long)(block / (unsigned)col_groups) * down + threadIdx.x / across;
     col = (int)(group * across + threadIdx.x % across) * LANE;
   }
 };
@@ -132,14 +134,15 @@ template <typename T> __global__ __launch_bounds__(THREADS) void k_unpack(long l
 
 struct Grid {
   int across, col_groups;
-  unsigned blocks;
+  dim3 blocks;
   Grid(long long rows, int cols) {
     const int lanes = (cols + SNN_PACK_BLOCK - 1) / SNN_PACK_BLOCK * (SNN_PACK_BLOCK / LANE);
     across = SNN_PACK_BLOCK / LANE;
     while (across < lanes && across < THREADS) across *= 2;
     col_groups = (lanes + across - 1) / across;
     const int down = THREADS / across;
-    blocks = (unsigned)((rows + down - 1) / down * col_groups);
+    const unsigned all = (unsigned)((rows + down - 1) / down * col_groups); // (2^31 at most, of 2^40 elements)
+    blocks = all < GRID_X ? dim3(all) : dim3(GRID_X, (all + GRID_X - 1) / GRID_X);
   }
 };
 

@@ -788,3 +788,17 @@ def test_vocab_weight_gradients_of_many_rows(d, vocab):
     # every term of a sum has the sign of the others: 16 products at least are added at a time, hence rows / 16 roundings at most; logits
     # of up to 6 d products of up to 5 * 10 / sqrt(d)
     near(dw, want.cpu(), ((rows / 16 + 16) * E32 + 4 * (6 * d + 8) * E32) * want.abs().cpu(), "dw")
+
+
+@gpu
+def test_pack_more_rows_than_a_grid_has_threads():
+    rows = (1 << 30) + 77
+    x = torch.empty((rows, 1), dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(5))
+    p = snn.snn_pack(x)
+    back = snn.snn_unpack(p, torch.bfloat16)
+    for part in (slice(0, 1000), slice((1 << 29) - 500, (1 << 29) + 500), slice((1 << 30) - 500, rows)):
+        codes, exps = to_bytes(x[part].float().cpu().numpy())
+        assert np.array_equal(p.codes[part].cpu().numpy(), codes) and np.array_equal(p.exps[part].cpu().numpy(), exps)
+        assert np.array_equal(back[part].double().cpu().numpy(), from_bytes(codes, exps))
+    a = rows // 2  # (an element by itself keeps its 7 bits)
+    assert ((back[a:].float() - x[a:].float()).abs_() <= 2.0 ** -7 * x[a:].float().abs_()).all()
