@@ -351,7 +351,7 @@ snn_status snn_glr_backward_packed(const snn_launch *at, const snn_glr *p, const
  *   logits_r = w h_r ;  loss_r = log sum_v exp(logits_rv) - logits_r,target
  * Logits are never in memory as a whole.  bf16 products are summed in fp32; in fp32 they keep 24 bits. */
 typedef struct {
-  int32_t rows, d, vocab; /* rows 0..2^22, d 1..2^16, vocab 1..2^24 */
+  int32_t rows, d, vocab; /* rows 0..2^22, d 1..2^16 (rows * d 2^35 at most), vocab 1..2^24 */
   int32_t dtype;          /* snn_dtype of h, w, dh, dw */
   int64_t ld_h, ld_w;     /* elements between rows of h and of w (0: d; at most 2^22); dh and dw are packed */
 } snn_vocab;

@@ -122,6 +122,8 @@ snn_status vocab_shape(const char *what, const snn_vocab *p, VocabShape *v) {
   if (!dtype_ok(p->dtype)) return refuse(SNN_E_INVAL, "%s: unknown type %d", what, p->dtype);
   if (p->rows < 0 || p->rows > (1 << 22) || p->d < 1 || p->d > (1 << 16) || p->vocab < 1 || p->vocab > (1 << 24))
     return refuse(SNN_E_INVAL, "%s: rows %d (0 .. 2^22), d %d (1 .. 2^16), vocab %d (1 .. 2^24)", what, p->rows, p->d, p->vocab);
+  if ((long long)p->rows * p->d > 1ll << 35) // (what a grid of threads reaches)
+    return refuse(SNN_E_INVAL, "%s: %d rows of %d elements: 2^35 in all at most", what, p->rows, p->d);
   *v = VocabShape{p->rows, p->d, p->vocab, p->dtype == SNN_BF16, p->ld_h, p->ld_w};
   for (long long *ld : {&v->ld_h, &v->ld_w}) {
     if (!*ld) *ld = p->d;

@@ -653,21 +653,25 @@ __global__ __launch_bounds__(1024) void k_join(const float2 *part, const float *
 
 // to = *factor times the sum of the slices, each n elements
 template <typename T> __global__ __launch_bounds__(256) void k_sum(const float *from, int slices, size_t n, const float *factor, T *to) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  float sum = from[i];
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
+    float sum = from[i];
 #pragma unroll 8
-  for (int k = 1; k < slices; ++k) sum += from[k * n + i];
-  to[i] = (T)(sum * *factor);
+    for (int k = 1; k < slices; ++k) sum += from[k * n + i];
+    to[i] = (T)(sum * *factor);
+  }
 }
 __global__ __launch_bounds__(256) void k_clear(uint16_t *to, size_t n) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) to[i] = 0;
 }
 
+// Workgroups of 256 threads for n elements; a grid has fewer than 2^32 threads, the kernels go round
+unsigned groups_for(size_t n) { return n < (1u << 28) ? (unsigned)((n + 255) / 256) : 1u << 20; }
+
 // ---- workspace ------------------------------------------------------------------------------
 struct Space {
   Tile logits; // of the products that make logits
   int parts, dp, padded, width, block; // width: entries of a piece of the vocabulary; block: those of a wavefront
+  int at_once;                         // entries whose logits one launch makes at most
   size_t h, w, part, picked, common, ht, wt, gm, gt, sum_h, sum_w, bytes;
   Space(const VocabShape &p, bool grad) {
     parts = p.bf16 ? 1 : 3;
@@ -676,11 +680,14 @@ struct Space {
     const int ks = parts == 1 ? KS<1> : KS<3>, rows = rows_of_b(logits, parts);
     dp = (p.d + ks - 1) / ks * ks;
     padded = (p.rows + rows - 1) / rows * rows;
+    // 2^22 tiles of 512 threads (a grid has fewer than 2^32)
+    const int tile_a = rows_of_a(logits), tiles_b = padded / rows, fit_grid = (1 << 22) / (tiles_b > 0 ? tiles_b : 1);
+    at_once = fit_grid < (1 << 20) / tile_a ? fit_grid * tile_a : 1 << 20;
     // G of a piece has about 2^27 elements, and a piece of w no more
-    const int tile_a = rows_of_a(logits);
     const long long all = ((long long)p.vocab + tile_a - 1) / tile_a * tile_a, most = grad ? (padded > dp ? padded : dp) : dp;
     long long fit = (1ll << 27) / (most > 0 ? most : 1) / 256 * 256;
     if (fit < 2048) fit = 2048;
+    if (fit > at_once) fit = at_once;
     width = (int)(fit < all ? fit : all);
     size_t at = 0;
     auto take = [&](size_t n) { const size_t was = at; at += (n + 255) / 256 * 256; return was; };
@@ -744,7 +751,7 @@ hipError_t loss(const VocabShape &p, const T *h, const T *w, const int *targets,
   q.b = h_direct ? (const __bf16 *)h : hr;
   q.ldb = h_direct ? p.ld_h : sp.dp * PARTS;
   q.lda = w_direct ? p.ld_w * (sizeof(T) / 2) : sp.dp * PARTS;
-  const int width = !w_direct ? sp.width : p.vocab < (1 << 20) ? p.vocab : 1 << 20;
+  const int width = !w_direct ? sp.width : p.vocab < sp.at_once ? p.vocab : sp.at_once;
   LossEpilogue ep = {targets, (float2 *)(work + sp.part), (float *)(work + sp.picked), 0, p.vocab, p.rows};
   for (long long v = 0; v < p.vocab; v += width) {
     const int entries = (int)(p.vocab - v < width ? p.vocab - v : width);
@@ -794,13 +801,13 @@ hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *tar
     else {
       const size_t n = (size_t)entries * p.d;
       TRY((product<PARTS, false>(sw.tile, dwq, StoreEpilogue<float>{sum_w, nullptr, p.d, (long long)n, entries, p.d, false}, s)));
-      k_sum<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum_w, sw.count, n, common, to);
+      k_sum<T><<<groups_for(n), 256, 0, s>>>(sum_w, sw.count, n, common, to);
       TRY(hipGetLastError());
     }
   }
   if (summed) {
     const size_t n = (size_t)p.rows * p.d;
-    k_sum<T><<<(unsigned)((n + 255) / 256), 256, 0, s>>>(sum_h, slices_h, n, common, dh);
+    k_sum<T><<<groups_for(n), 256, 0, s>>>(sum_h, slices_h, n, common, dh);
   }
   return hipGetLastError();
 }
@@ -820,7 +827,7 @@ hipError_t launch_vocab_grad(const VocabShape &p, const void *h, const void *w, 
                              const float *dloss, void *dh, void *dw, void *work, hipStream_t s) {
   if (!p.rows) {
     const size_t n = (size_t)p.vocab * p.d * (p.bf16 ? 1 : 2);
-    k_clear<<<(unsigned)(n < (1u << 28) ? (n + 255) / 256 : 1u << 20), 256, 0, s>>>((uint16_t *)dw, n);
+    k_clear<<<groups_for(n), 256, 0, s>>>((uint16_t *)dw, n);
     return hipGetLastError();
   }
   return p.bf16 ? gradients<__bf16, 1>(p, (const __bf16 *)h, (const __bf16 *)w, targets, state, dloss, (__bf16 *)dh, (__bf16 *)dw, (char *)work, s)

@@ -802,3 +802,30 @@ def test_pack_more_rows_than_a_grid_has_threads():
         assert np.array_equal(back[part].double().cpu().numpy(), from_bytes(codes, exps))
     a = rows // 2  # (an element by itself keeps its 7 bits)
     assert ((back[a:].float() - x[a:].float()).abs_() <= 2.0 ** -7 * x[a:].float().abs_()).all()
+
+
+@gpu
+@pytest.mark.parametrize("d,vocab,gradients", [(64, 131072, False), (1024, 2100, True)])
+def test_vocab_more_tiles_and_elements_than_a_grid_has_threads(d, vocab, gradients):
+    rows = 1 << 22
+    g = torch.Generator(device="cuda").manual_seed(6)
+    h = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    w = torch.empty((vocab, d), dtype=torch.bfloat16, device="cuda").normal_(0.0, 2 / math.sqrt(d), generator=g)
+    t = torch.randint(0, vocab, (rows,), dtype=torch.int32, device="cuda", generator=g)
+    loss, state = snn.snn_vocab_loss(h, w, t)
+    some = torch.cat([torch.arange(0, 40), torch.arange(rows // 2, rows // 2 + 40), torch.arange(rows - 40, rows)]).cuda()
+    H, W, y = h[some].double().cpu(), w.double().cpu(), t[some].long().cpu()
+    logits, lse, miss, on, _, want = vocab_loss(H, W, y)
+    e_l = (d + 8) * E32 * (H.abs() @ W.abs().T).amax(1) + 4 * E32 * logits.abs().amax(1)
+    count = 64 + vocab / 64
+    near(loss[some], want, 2 * e_l + count * E32 + 8 * E32 * want, "loss")
+    if gradients:
+        dh = snn.snn_vocab_loss_grad(h, w, t, state, torch.ones(rows, device="cuda"))[0]
+        G, want_h, _ = vocab_grads(H, W, y, torch.ones(len(y), dtype=torch.float64))
+        A = G.abs() * (4 * e_l + (count + 16) * E32 + 2.0 ** -8)[:, None]
+        near(dh[some], want_h, A @ W.abs() + E32 * (vocab + 8) * (G.abs() @ W.abs()), "dh")
+
+
+def test_vocab_refuses_more_elements_than_a_grid_reaches():
+    with pytest.raises(snn.SnnError, match="2\\^35 in all"):
+        ops._run("snn_vocab_loss", C.byref(ops.snn_launch(0, None, None, 0)), C.byref(ops.snn_vocab(1 << 22, (1 << 13) + 1, 10, 1)), *[None] * 5)
