@@ -300,7 +300,8 @@ const char *snn_launch_error(void);
 
 /* Gated linear recurrence over time-major sequences [T][batch][n], each channel by itself:
  *   a_t = sigmoid(z_t) ;  h_t = a_t h_{t-1} + (1 - a_t) x_t ,  t = 1..T
- * Computed as h + sigmoid(-z) (x - h) in fp32 whatever the type: a state or drive that is not finite gives NaN from its step on. */
+ * Computed in fp32 whatever the type, from sigmoid(z) and sigmoid(-z), each accurate relative to itself down to 2^-126.  A state or drive that
+ * is not finite gives nothing finite from its step on. */
 typedef struct {
   int32_t T, batch, n;        /* T >= 0 (0: h_last = h0), at most 2^30 steps and 2^25 channels batch * n */
   int32_t dtype;              /* snn_dtype of z, x, h, dh, dz, dx */

@@ -1,19 +1,21 @@
 // Gated linear recurrence over [T][batch][n] and its backward pass.
 //
-//   b_t = sigmoid(-z_t);  h_t = h_{t-1} + b_t (x_t - h_{t-1})                       (a_t = 1 - b_t is what the state retains)
-//   g_t = dh_t + G_{t+1};  G_t = g_t - b_t g_t;  dx_t = b_t g_t;  dz_t = (1 - b_t) dx_t (h_{t-1} - x_t)
+//   a_t = sigmoid(z_t), b_t = sigmoid(-z_t);  h_t = a_t h_{t-1} + b_t x_t
+//   g_t = dh_t + G_{t+1};  G_t = a_t g_t;  dx_t = b_t g_t;  dz_t = a_t b_t g_t (h_{t-1} - x_t)
 //
-// Every channel (b, i) is a recurrence of its own.  16 steps of one channel are a map h -> h - Q h + B, and two maps in a row are one
-// again: Q = Q1 + Q2 (1 - Q1), B = B1 + (B2 - Q2 B1).  Q = 1 - product(a) is what is carried, not the product: b is
-// accurate relative to itself however small, where 1 - b rounds, so long memories (b of 1e-4 and less) keep their weight
-// against the drive.  A wavefront holds 16 steps of 64 lanes in registers, the eight wavefronts of a workgroup hold 128 steps in a row,
-// exchange their maps through LDS and then know the state that each of them starts from: one read of z and x, one write of h.
+// Every channel (b, i) is a recurrence of its own.  16 steps of one channel are a map h -> P h + B, P their product of a, and two maps in a
+// row are one again: P = P1 P2, B = P2 B1 + B2.
+// Digits: a and b are both computed, accurate relative to themselves, neither as 1 less the other, so that what a closed gate
+// (a of 1e-4 and less) lets through of a large state or gradient keeps its digits, and so does the drive of an open one (b of 1e-4 and less).  A P next to one
+// would lose those of its drive in its rounding, and over many steps that adds up: where P is the larger one a map holds Q = 1 - P
+// instead, found by itself (Q = P2 Q1 + Q2), and is h -> h - Q h + B.
+// A wavefront holds 16 steps of 64 lanes in registers, the eight wavefronts of a workgroup hold 128 steps in a row, exchange their maps through LDS and then know the state that each of them starts from: one read of z and x, one write of h.
 // The state before every 128 steps is what the forward pass keeps; the backward pass gets h_{t-1} from there by
 // the same exchange, beside that of the gradient, which runs the other way.
 //
-// What bounds it: memory, where there are channels or steps enough.  Forward, 4096 x 8 x 2048 in bf16: 94 us, 4.3 TB/s of z, x and h (a copy reaches
-// 5.1); backward, 1000 x 32 x 1024 in fp32: 123 us, 5.3 TB/s; 32768 x 1 x 1024 in bf16: 97 us, of which 26 for the maps of its
-// segments; from 8 bits, 4096 x 8 x 2048: 146 us, 3.7 TB/s, bound by the number of 1- and 2-byte loads.  One token of 64 x 2048: 3.2 us.
+// What bounds it: memory, where there are channels or steps enough.  Forward, 4096 x 8 x 2048 in bf16: 80 us, 5.1 TB/s of z, x and h (a copy reaches
+// 5.1); backward, 1000 x 32 x 1024 in fp32: 122 us, 5.4 TB/s; 32768 x 1 x 1024 in bf16: 100 us, of which 27 for the maps of its
+// segments; from 8 bits, 4096 x 8 x 2048: 147 us, 3.7 TB/s, bound by the number of 1- and 2-byte loads.  One token of 64 x 2048: 3.2 us.
 // Short sequences are bound by the latency of a tile, some 5 us.
 #include "snn_ops.h"
 
@@ -49,15 +51,51 @@ template <typename T, int VEC> __device__ __forceinline__ typename Raw<T, VEC>::
   }
 }
 
-// sigmoid(-z) from z / log(2): 0 from where 1 + e^z is infinite
+// sigmoid(z) and sigmoid(-z) from z / log(2); below 2^-126 they are 0, sigmoid(-z) (EVERY) 2^-126.  Where e^z is infinite sigmoid(z) is right
+// with EVERY and NaN without.
 constexpr float LOG2E = 1.44269504f;
-__device__ __forceinline__ float moved(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z)); }
+template <bool EVERY> __device__ __forceinline__ void gate(float z, float &a, float &b) {
+  const float e = __builtin_amdgcn_exp2f(EVERY && z > 126.f ? 126.f : z); // (NaN stays)
+  b = __builtin_amdgcn_rcpf(1.f + e);
+  a = e * b;
+}
+__device__ __forceinline__ float nan_if_infinite(float x) { return fmaf(x, 0.f, x); }
+// What a map retains: the smaller of P and Q, P as a negative number (its sign bit, as it may be 0)
+__device__ __forceinline__ float share(float p, float q) { return p <= 0.5f ? -p : q; }
+__device__ __forceinline__ bool is_p(float s) { return __float_as_int(s) < 0; }
+// The map applied to h
+__device__ __forceinline__ float mapped(float s, float h, float b) { return (is_p(s) ? 0.f : h) + fmaf(-s, h, b); }
+// and two of them as one
+__device__ __forceinline__ float both(float s, float r) {
+  return share((is_p(s) ? -s : 1.f - s) * (is_p(r) ? -r : 1.f - r), fmaf(s, 1.f - r, r));
+}
 
 // f(whole) for a wavefront's steps, `whole` known to the compiler: whether every lane's sequence has all of them, as nearly always
 template <bool B> struct Known { static constexpr bool value = B; };
 template <class F> __device__ __forceinline__ void either(bool whole, F f) {
   if (whole) f(Known<true>());
   else f(Known<false>());
+}
+// f(ordinary) as if all steps were there and every value an ordinary one, and once more where steps are missing, or `found` has found values
+// that are not (32768 x 1 x 1024 backwards: 99 us; with their tests in every step 106).  The second time begins from the elements as
+// they were read: `again` makes them values that the compiler knows nothing of, as it would else keep in registers what the first time made of them.
+template <class F, class G, class H> __device__ __forceinline__ void ordinarily(bool whole, F f, G found, H again) {
+  if (whole) {
+    f(Known<true>());
+    whole = !__any(found());
+  }
+  if (!whole) {
+    again();
+    f(Known<false>());
+  }
+}
+template <class R, int N> __device__ __forceinline__ void unknown(R (&r)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    uint32_t was = r[j];
+    asm volatile("" : "+v"(was));
+    r[j] = (R)was;
+  }
 }
 
 __device__ __forceinline__ void lds_barrier() { // of the LDS alone: loads from memory stay in flight
@@ -135,7 +173,7 @@ template <int VEC> __device__ __forceinline__ void through(const Args &a, int c,
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       const float2 m = a.maps[(size_t)k * a.channels + c + v];
-      h[v] += fmaf(-m.x, h[v], m.y);
+      h[v] = mapped(m.x, h[v], m.y);
     }
 }
 
@@ -160,8 +198,9 @@ struct Exponents {
     const int first = min(t0, T - 1), last = T - 1 - first;
     return __builtin_amdgcn_raw_buffer_load_b8(rows.from(first), (int)(at + (unsigned)min((int)threadIdx.x >> 2, last) * rows.step), 0, 0);
   }
-  __device__ __forceinline__ uint32_t of(uint32_t loaded, int j) const {
-    return (uint32_t)__builtin_amdgcn_ds_bpermute((4 * j + slot) * 4, (int)loaded);
+  // the lane's own value of step j, from what the lanes that loaded the bytes made of them
+  __device__ __forceinline__ float of(float loaded, int j) const {
+    return __int_as_float(__builtin_amdgcn_ds_bpermute((4 * j + slot) * 4, __float_as_int(loaded)));
   }
 };
 
@@ -180,11 +219,11 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
   const Rows ph(a.h, sizeof(T), a.ld_h, a.batch, me.b, me.i);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.y), seg = blockIdx.y;
   const int k0 = seg * a.seg_tiles, k1 = min(k0 + a.seg_tiles, a.tiles);
-  float h[VEC], q[VEC]; // the state (MAPS: from zero), and Q of the segment so far
+  float h[VEC], p[VEC]; // the state (MAPS: from zero), and the share that the segment so far retains
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
     h[v] = 0.f;
-    q[v] = 0.f;
+    p[v] = 0.f;
     if (MAPS || a.segments == 1) {
       const float f = a.from && me.on ? a.from[me.c + v] : 0.f;
       if (!MAPS) h[v] = f;
@@ -205,58 +244,78 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
   }
   int n = k1 - k0, k = MAPS ? k1 - 1 : k0;
   for (; n > 0; --n, MAPS ? --k : ++k, t0 += STRIDE) {
-    float b[S][VEC], x[S][VEC];
+    // Each step's state as P h + B of the one that these start from.  NW = 1: the smaller of a and b, a as a negative number, and the drive;
+    // a state that goes from call to call is moved by h + b (x - h) where a is next to one.
+    float P[S][VEC], B[S][VEC], Q[VEC];
     const int live = me.len - t0; // steps of these 16 that the sequence has
     const bool whole = __all(live >= S);
-    either(whole, [&](auto known) {
-      constexpr bool ALL = decltype(known)::value;
+    ordinarily(
+        NW > 1 && whole,
+        [&](auto known) {
+          constexpr bool ORDINARY = decltype(known)::value;
 #pragma unroll
-      for (int j = 0; j < S; ++j) {
-        float z[VEC];
-        widen<T, VEC>(rz[j], z);
-        widen<T, VEC>(rx[j], x[j]);
+          for (int j = 0; j < S; ++j) {
+            float z[VEC], x[VEC];
+            widen<T, VEC>(rz[j], z);
+            widen<T, VEC>(rx[j], x);
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          b[j][v] = ALL || j < live ? moved(z[v] * LOG2E) : 0.f;
-          x[j][v] = ALL || j < live ? x[j][v] : 0.f;
-        }
-      }
-    });
-    if (n > 1) {
+            for (int v = 0; v < VEC; ++v) {
+              float keep, move;
+              gate<!ORDINARY>(z[v] * LOG2E, keep, move);
+              if (!ORDINARY) {
+                x[v] = nan_if_infinite(x[v]);
+                if (j >= live) keep = 1.f, move = x[v] = 0.f;
+              }
+              if (NW == 1) {
+                P[j][v] = keep < move ? -keep : move;
+                B[j][v] = x[v];
+              } else {
+                P[j][v] = j ? P[j - 1][v] * keep : keep;
+                Q[v] = j ? fmaf(keep, Q[v], move) : move;
+                B[j][v] = j ? fmaf(keep, B[j - 1][v], move * x[v]) : move * x[v];
+              }
+            }
+          }
+        },
+        [&] {
+          bool bad = false;
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) bad |= !(P[S - 1][v] + fabsf(B[S - 1][v]) < INFINITY); // (once so, so to the end)
+          return bad;
+        },
+        [&] {
+          unknown(rz);
+          unknown(rx);
+        });
+    if (n > 1) { // (ahead of the arithmetic above: 104 us instead of 84 for 4096 x 8 x 2048 in bf16)
       pz.load(rz, t0 + STRIDE, a.T);
       px.load(rx, t0 + STRIDE, a.T);
     }
     float start[VEC];
     if (NW > 1) {
-      float Q[VEC] = {}, B[VEC] = {};
-#pragma unroll
-      for (int j = 0; j < S; ++j)
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          B[v] = fmaf(b[j][v], x[j][v] - B[v], B[v]);
-          Q[v] = fmaf(b[j][v], 1.f - Q[v], Q[v]);
-        }
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        maps.v[k & 1][0][w][v][threadIdx.x] = Q[v];
-        maps.v[k & 1][1][w][v][threadIdx.x] = B[v];
+        maps.v[k & 1][0][w][v][threadIdx.x] = share(P[S - 1][v], Q[v]);
+        maps.v[k & 1][1][w][v][threadIdx.x] = B[S - 1][v];
       }
       lds_barrier();
       if (!MAPS && w == 0 && a.kept && me.on)
 #pragma unroll
         for (int v = 0; v < VEC; ++v) a.kept[(size_t)k * a.channels + me.c + v] = h[v];
 #pragma unroll
+      for (int v = 0; v < VEC; ++v) h[v] = nan_if_infinite(h[v]);
+#pragma unroll
       for (int i = 0; i < WAVES; ++i)
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
           const int wave = MAPS ? WAVES - 1 - i : i;
-          const float Qi = maps.v[k & 1][0][wave][v][threadIdx.x], Bi = maps.v[k & 1][1][wave][v][threadIdx.x];
+          const float Pi = maps.v[k & 1][0][wave][v][threadIdx.x], Bi = maps.v[k & 1][1][wave][v][threadIdx.x];
           if (MAPS) { // an earlier map, then the one so far
-            h[v] += fmaf(-q[v], Bi, Bi);
-            q[v] = fmaf(q[v], 1.f - Qi, Qi);
+            h[v] = mapped(p[v], Bi, h[v]);
+            p[v] = both(p[v], Pi);
           } else {
             if (i == w) start[v] = h[v];
-            h[v] += fmaf(-Qi, h[v], Bi);
+            h[v] = mapped(Pi, h[v], Bi);
           }
         }
     } else {
@@ -275,8 +334,9 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
           float out[VEC];
 #pragma unroll
           for (int v = 0; v < VEC; ++v) {
-            start[v] = fmaf(b[j][v], x[j][v] - start[v], start[v]);
-            out[v] = ALL || j < live ? start[v] : 0.f;
+            const float state = NW > 1 ? fmaf(P[j][v], start[v], B[j][v]) : fmaf(P[j][v], B[j][v] - start[v], is_p(P[j][v]) ? B[j][v] : start[v]);
+            if (NW == 1) start[v] = state;
+            out[v] = ALL || j < live ? state : 0.f;
           }
           if (ALL || t0 + j < a.T) ph.store(to, j, narrow<T, VEC>(out));
         }
@@ -289,7 +349,7 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
   if (w == 0 && me.on)
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      if (MAPS) a.maps[(size_t)(seg + 1) * a.channels + me.c + v] = make_float2(q[v], h[v]);
+      if (MAPS) a.maps[(size_t)(seg + 1) * a.channels + me.c + v] = make_float2(p[v], h[v]);
       else if (a.to && seg == a.segments - 1) a.to[me.c + v] = h[v];
     }
 }
@@ -300,6 +360,8 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
 template <typename T, typename P, int VEC, bool SHARED, bool MAPS>
 __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
   constexpr bool PACKED = sizeof(P) == 1;
+  // dh is not loaded a tile ahead where registers would go to memory instead (512 x 64 x 2080: 149 us, 180 with the loads ahead)
+  constexpr bool LATE = PACKED && VEC == 2 && !SHARED;
   __shared__ Maps<VEC, 3> maps;
   typedef typename Raw<T, VEC>::type R;
   const Lane<VEC> me(a);
@@ -309,11 +371,11 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
   const Rows pdz(a.dz, sizeof(T), a.ld_dz, a.batch, me.b, me.i), pdx(a.dx, sizeof(T), a.ld_dx, a.batch, me.b, me.i);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.y), seg = blockIdx.y + (MAPS ? 1 : 0);
   const int k0 = seg * a.seg_tiles, k1 = min(k0 + a.seg_tiles, a.tiles);
-  float g[VEC], q[VEC]; // G (MAPS: from zero), and Q of the segment so far
+  float g[VEC], p[VEC]; // G (MAPS: from zero), and the share that the segment so far retains
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
     g[v] = 0.f;
-    q[v] = 0.f;
+    p[v] = 0.f;
     if (MAPS || a.segments == 1) {
       const float f = a.from && me.on ? a.from[me.c + v] : 0.f;
       if (!MAPS) g[v] = f;
@@ -333,9 +395,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
   auto fetch = [&](int k) {
     const int t = (k * WAVES + w) * STEPS;
     pz.load(rz, t, a.T);
-    pd.load(rd, t, a.T);
+    if (!LATE) pd.load(rd, t, a.T);
     if (!MAPS) px.load(rx, t, a.T);
-    if (PACKED && SHARED) {
+    if (SHARED) {
       shared_z = of_z.load(pze, t, a.T);
       if (!MAPS) shared_x = of_x.load(pxe, t, a.T);
     } else if (PACKED) {
@@ -351,57 +413,77 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
   int n = k1 - k0, k = MAPS ? k0 : k1 - 1;
   for (; n > 0; --n, MAPS ? ++k : --k) {
     const int t0 = (k * WAVES + w) * STEPS;
-    float b[STEPS][VEC], x[STEPS][VEC];
+    float keep[STEPS][VEC], move[STEPS][VEC], x[STEPS][VEC]; // a, b and b x
     R d[STEPS]; // (as it is in memory: half the registers)
     const int live = me.len - t0;
     const bool whole = __all(live >= STEPS);
-    either(whole, [&](auto known) {
-      constexpr bool ALL = decltype(known)::value;
+    float product[VEC], Q[VEC];
+    if (LATE) pd.load(d, t0, a.T);
+    // (a step is a power of two: its product with log2(e) is exact)
+    float steps_z = __uint_as_float(shared_z << 23) * LOG2E, steps_x = __uint_as_float(shared_x << 23);
+    ordinarily(
+        whole,
+        [&](auto known) {
+          constexpr bool ORDINARY = decltype(known)::value;
 #pragma unroll
-      for (int j = 0; j < STEPS; ++j) {
-        float z[VEC];
-        widen<P, VEC>(rz[j], z);
-        if (!MAPS) widen<P, VEC>(rx[j], x[j]);
-        d[j] = ALL || j < live ? rd[j] : (R)0;
-        // (a step is a power of two: its product with log2(e) is exact)
-        const float step_z = PACKED ? __uint_as_float((SHARED ? of_z.of(shared_z, j) : (uint32_t)ez[j]) << 23) * LOG2E : LOG2E;
-        const float step_x = PACKED && !MAPS ? __uint_as_float((SHARED ? of_x.of(shared_x, j) : (uint32_t)ex[j]) << 23) : 1.f;
+          for (int j = 0; j < STEPS; ++j) {
+            float z[VEC];
+            widen<P, VEC>(rz[j], z);
+            if (!MAPS) widen<P, VEC>(rx[j], x[j]);
+            if (!LATE) d[j] = ORDINARY || j < live ? rd[j] : (R)0;
+            const float step_z = SHARED ? of_z.of(steps_z, j) : PACKED ? __uint_as_float((uint32_t)ez[j] << 23) * LOG2E : LOG2E;
+            const float step_x = MAPS ? 1.f : SHARED ? of_x.of(steps_x, j) : PACKED ? __uint_as_float((uint32_t)ex[j] << 23) : 1.f;
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          z[v] *= step_z;
-          if (PACKED && !MAPS) x[j][v] *= step_x;
-          b[j][v] = ALL || j < live ? moved(z[v]) : 0.f;
-          if (!MAPS) x[j][v] = ALL || j < live ? x[j][v] : 0.f;
-        }
-      }
-    });
-    float Q[VEC] = {}, B[VEC] = {}, G[VEC] = {}, h[VEC];
+            for (int v = 0; v < VEC; ++v) {
+              gate<!ORDINARY>(z[v] * step_z, keep[j][v], move[j][v]);
+              if (PACKED && !MAPS) x[j][v] *= step_x;
+              if (!MAPS) x[j][v] *= move[j][v];
+              if (!ORDINARY && j >= live) keep[j][v] = 1.f, move[j][v] = x[j][v] = 0.f;
+              product[v] = j ? product[v] * keep[j][v] : keep[j][v];
+              Q[v] = j ? fmaf(keep[j][v], Q[v], move[j][v]) : move[j][v];
+            }
+          }
+        },
+        [&] {
+          bool bad = false;
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) bad |= product[v] != product[v];
+          return bad;
+        },
+        [&] {
+          unknown(rz);
+          if (!MAPS) unknown(rx);
+          if (SHARED) asm volatile("" : "+v"(steps_z), "+v"(steps_x));
+          else if (PACKED) {
+            unknown(ez);
+            if (!MAPS) unknown(ex);
+          }
+        });
+    float B[VEC] = {}, G[VEC] = {}, h[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) h[v] = kept[v];
-    if (n > 1) fetch(MAPS ? k + 1 : k - 1);
+    if (LATE && !whole)
 #pragma unroll
-    for (int j = 0; j < STEPS; ++j)
+      for (int j = 0; j < STEPS; ++j) d[j] = j < live ? d[j] : (R)0;
+    if (!MAPS)
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        if (!MAPS) B[v] = fmaf(b[j][v], x[j][v] - B[v], B[v]);
-        Q[v] = fmaf(b[j][v], 1.f - Q[v], Q[v]);
-      }
+      for (int j = 0; j < STEPS; ++j)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) B[v] = fmaf(keep[j][v], B[v], x[j][v]);
 #pragma unroll
     for (int j = STEPS - 1; j >= 0; --j) {
       float dh[VEC];
       widen<T, VEC>(d[j], dh);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        const float s = dh[v] + G[v];
-        G[v] = fmaf(-b[j][v], s, s);
-      }
+      for (int v = 0; v < VEC; ++v) G[v] = keep[j][v] * (dh[v] + G[v]);
     }
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      maps.v[k & 1][0][w][v][threadIdx.x] = Q[v];
+      maps.v[k & 1][0][w][v][threadIdx.x] = share(product[v], Q[v]);
       maps.v[k & 1][1][w][v][threadIdx.x] = G[v];
       if (!MAPS) maps.v[k & 1][2][w][v][threadIdx.x] = B[v];
     }
+    if (n > 1) fetch(MAPS ? k + 1 : k - 1); // (4096 x 8 x 2048 in bf16: 136 us; before the loops above 148)
     lds_barrier();
     float from[VEC];
 #pragma unroll
@@ -409,13 +491,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         const int wave = MAPS ? i : WAVES - 1 - i;
-        const float Qi = maps.v[k & 1][0][wave][v][threadIdx.x], Gi = maps.v[k & 1][1][wave][v][threadIdx.x];
+        const float Pi = maps.v[k & 1][0][wave][v][threadIdx.x], Gi = maps.v[k & 1][1][wave][v][threadIdx.x];
         if (MAPS) { // the map of later steps comes first
-          g[v] += fmaf(-q[v], Gi, Gi);
-          q[v] = fmaf(q[v], 1.f - Qi, Qi);
+          g[v] = mapped(p[v], Gi, g[v]);
+          p[v] = both(p[v], Pi);
         } else {
           if (wave == w) from[v] = g[v];
-          g[v] += fmaf(-Qi, g[v], Gi);
+          g[v] = mapped(Pi, g[v], Gi);
         }
       }
     if (MAPS) continue;
@@ -423,13 +505,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
     for (int i = 0; i < WAVES - 1; ++i)
 #pragma unroll
       for (int v = 0; v < VEC; ++v)
-        if (i < w) h[v] += fmaf(-maps.v[k & 1][0][i][v][threadIdx.x], h[v], maps.v[k & 1][2][i][v][threadIdx.x]);
+        if (i < w) h[v] = mapped(maps.v[k & 1][0][i][v][threadIdx.x], h[v], maps.v[k & 1][2][i][v][threadIdx.x]);
 #pragma unroll
     for (int j = 0; j < STEPS; ++j)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        const float off = x[j][v] - h[v];
-        h[v] = fmaf(b[j][v], off, h[v]);
+        const float off = fmaf(move[j][v], h[v], -x[j][v]); // b (h - x)
+        h[v] = fmaf(keep[j][v], h[v], x[j][v]);
         x[j][v] = off;
       }
     if (me.on) {
@@ -442,10 +524,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
           widen<T, VEC>(d[j], dh);
 #pragma unroll
           for (int v = 0; v < VEC; ++v) {
-            const float s = dh[v] + from[v];
-            dx[v] = b[j][v] * s;
-            from[v] = fmaf(-b[j][v], s, s);
-            dz[v] = ALL || j < live ? (b[j][v] - 1.f) * dx[v] * x[j][v] : 0.f; // (0 whatever the state)
+            const float g = dh[v] + from[v];
+            dx[v] = move[j][v] * g;
+            from[v] = keep[j][v] * g;
+            dz[v] = ALL || j < live ? from[v] * x[j][v] : 0.f; // (0 whatever the state)
           }
           if (ALL || t0 + j < a.T) {
             pdz.store(to_dz, j, narrow<T, VEC>(dz));
@@ -458,7 +540,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
   if (w == 0 && me.on)
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      if (MAPS) a.maps[(size_t)(a.segments - seg) * a.channels + me.c + v] = make_float2(q[v], g[v]);
+      if (MAPS) a.maps[(size_t)(a.segments - seg) * a.channels + me.c + v] = make_float2(p[v], g[v]);
       else if (a.to && seg == 0) a.to[me.c + v] = g[v];
     }
 }

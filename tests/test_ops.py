@@ -829,3 +829,74 @@ def test_vocab_more_tiles_and_elements_than_a_grid_has_threads(d, vocab, gradien
 def test_vocab_refuses_more_elements_than_a_grid_reaches():
     with pytest.raises(snn.SnnError, match="2\\^35 in all"):
         ops._run("snn_vocab_loss", C.byref(ops.snn_launch(0, None, None, 0)), C.byref(ops.snn_vocab(1 << 22, (1 << 13) + 1, 10, 1)), *[None] * 5)
+
+
+# ---- gates that are closed or nearly so -----------------------------------------------------------
+def relative_bounds(z, x, h0, dh, dlast):
+    """What h, dz, dx and dh0 may be off by, in terms of the magnitudes of what they are sums of: of each step's gate s = min(a, 1 - a), off
+    by (|z| + 8) E32 of itself and 2^-126, and of three roundings; twice that, for steps that are joined to maps before they are applied."""
+    T = z.shape[0]
+    a, c = torch.sigmoid(z), torch.sigmoid(-z)
+    e_s = torch.minimum(a, c) * (z.abs() + 8) * E32 + 2.0 ** -126
+    m, e, offs = h0.abs(), torch.zeros_like(h0), []
+    before_m, before_e = [], []
+    for t in range(T):
+        before_m.append(m)
+        before_e.append(e)
+        e = a[t] * e + e_s[t] * (m + x[t].abs())
+        m = a[t] * m + c[t] * x[t].abs()
+        e = e + 3 * E32 * m
+        offs.append(e)
+    gm, ge = dlast.abs(), torch.zeros_like(h0)
+    tol_z, tol_x = torch.zeros_like(z), torch.zeros_like(z)
+    for t in reversed(range(T)):
+        gm = gm + dh[t].abs()
+        ge = ge + E32 * gm
+        off = before_m[t] + x[t].abs()
+        tol_x[t] = c[t] * ge + (e_s[t] + 2 * E32 * c[t]) * gm
+        tol_z[t] = a[t] * c[t] * (off * ge + gm * (before_e[t] + 5 * E32 * off)) + 2 * e_s[t] * off * gm
+        ge = a[t] * ge + (e_s[t] + 2 * E32 * a[t]) * gm
+        gm = a[t] * gm
+    return [2 * v + 1e-36 for v in (torch.stack(offs), tol_z, tol_x, ge)]
+
+
+@gpu
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("T,low,high", [(1, -30, -5), (1, -40, 15), (3, -16, -10), (40, -25, 5), (128, -3, 0), (300, -25, 15), (300, -200, 200), (5000, -14, 14)])
+def test_glr_closed_gates_keep_their_digits(T, low, high, packed):
+    # a state and a gradient far above what drives them: what a closed gate lets through of them counts beside that
+    g = torch.Generator().manual_seed(T)
+    z = low + (high - low) * torch.rand(T, 2, 66, generator=g)
+    x, dh = 1e-3 * torch.randn(T, 2, 66, generator=g), 1e-3 * torch.randn(T, 2, 66, generator=g)
+    h0, dlast = 1e4 * torch.randn(2, 66, generator=g), 1e4 * torch.randn(2, 66, generator=g)
+    zg, xg, dhg, hg, dg = (v.cuda() for v in (z, x, dh, h0, dlast))
+    zi, xi = (snn.snn_pack(zg), snn.snn_pack(xg)) if packed else (zg, xg)
+    if packed:
+        zg, xg = snn.snn_unpack(zi), snn.snn_unpack(xi)
+        z, x = zg.cpu(), xg.cpu()
+    h, _, kept = snn.snn_glr_forward(zg, xg, hg, keep=True)
+    dz, dx, dh0 = snn.snn_glr_backward(zi, xi, kept, dhg, dg)
+    z, x, dh, h0, dlast = (v.double() for v in (z, x, dh, h0, dlast))
+    all_steps = torch.full((2,), T)
+    tol = relative_bounds(z, x, h0, dh, dlast)
+    near(h, glr_forward(z, x, h0, all_steps)[0], tol[0], "h")
+    for got, want, t, what in zip((dz, dx, dh0), glr_backward(z, x, h0, all_steps, dh, dlast), tol[1:], ("dz", "dx", "dh0")):
+        near(got, want, t, what)
+
+
+@gpu
+def test_glr_gates_shut_altogether():
+    z = torch.tensor([[[-200.0, -20.0]]], device="cuda")
+    h = snn.snn_glr_forward(z, torch.tensor([[[1.0, 1e-3]]], device="cuda"), torch.tensor([[1e8, 1e4]], device="cuda"))[0].cpu()
+    assert h[0, 0, 0] == 1 and abs(h[0, 0, 1].item() - (1e-3 + math.exp(-20) * 1e4)) < 1e-3 * 40 * E32
+
+
+@gpu
+@pytest.mark.parametrize("steps", [1, 16, 128])
+def test_glr_long_memory_from_call_to_call(steps):
+    z, x, state = torch.full((steps, 1, 64), 15.0, device="cuda"), torch.ones((steps, 1, 64), device="cuda"), torch.zeros((1, 64), device="cuda")
+    for _ in range(2048 // steps):
+        snn.snn_glr_forward(z, x, state, h_last=state)
+    want = 1 - (1 - 1 / (1 + math.exp(15.0))) ** 2048
+    # as for one call: the gate's digits, and a rounding of the state per step at most
+    assert abs(state.double().cpu() - want).max().item() <= want * (20 * E32 + 2048 * 2.0 ** -24)
