@@ -322,7 +322,8 @@ snn_status snn_glr_forward(const snn_launch *at, const snn_glr *p, const void *z
                            float *kept);
 
 /* Gradients of z, x and h0 from those of h and, where dh_last [batch][n] fp32 is not NULL, of h_last; h itself is not needed.
- * dh0 [batch][n] fp32 may be NULL; it may be dh_last itself. */
+ * dh0 [batch][n] fp32 may be NULL; it may be dh_last itself.  A gradient that is not finite gives nothing finite in its channel from its step
+ * back to the first. */
 snn_status snn_glr_backward(const snn_launch *at, const snn_glr *p, const void *z, const void *x, const float *kept, const void *dh,
                             const float *dh_last, void *dz, void *dx, float *dh0);
 

@@ -527,7 +527,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
             const float g = dh[v] + from[v];
             dx[v] = move[j][v] * g;
             from[v] = keep[j][v] * g;
-            dz[v] = ALL || j < live ? from[v] * x[j][v] : 0.f; // (0 whatever the state)
+            dz[v] = from[v] * x[j][v];
+            if (!ALL && j >= live) dz[v] = dx[v] = 0.f; // (whatever the state and its gradient)
           }
           if (ALL || t0 + j < a.T) {
             pdz.store(to_dz, j, narrow<T, VEC>(dz));

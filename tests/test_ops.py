@@ -900,3 +900,20 @@ def test_glr_long_memory_from_call_to_call(steps):
     want = 1 - (1 - 1 / (1 + math.exp(15.0))) ** 2048
     # as for one call: the gate's digits, and a rounding of the state per step at most
     assert abs(state.double().cpu() - want).max().item() <= want * (20 * E32 + 2048 * 2.0 ** -24)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("T", [30, 700])
+def test_glr_padded_steps_have_no_gradient_whatever_that_of_the_state(T, dtype):
+    z, x, dh, h0, dlast, _ = glr_inputs(T, 4, 66, dtype, False, seed=12)
+    lengths = torch.tensor([T, 0, T // 2, 1], dtype=torch.int32, device="cuda")
+    kept = snn.snn_glr_forward(z, x, h0, lengths=lengths, keep=True)[2]
+    want = snn.snn_glr_backward(z, x, kept, dh, dlast, lengths=lengths)
+    dlast[1:, ::2] = torch.tensor([math.inf, math.nan, -math.inf], device="cuda")[:, None]
+    dz, dx, dh0 = snn.snn_glr_backward(z, x, kept, dh, dlast, lengths=lengths)
+    held = torch.arange(T, device="cuda")[:, None] >= lengths[None, :]
+    assert not dz[held].any() and not dx[held].any()
+    assert not torch.isfinite(dx[0, 2:, ::2]).any() and not torch.isfinite(dh0[1:, ::2]).any()
+    for got, ref in zip((dz, dx, dh0), want):  # the other channels
+        assert torch.equal(got[..., 1::2], ref[..., 1::2]) and torch.equal(got[..., 0, :], ref[..., 0, :])
