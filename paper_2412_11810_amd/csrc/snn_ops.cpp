@@ -30,6 +30,10 @@ struct OnDevice {
     error = hipGetDevice(&before);
     if (error != hipSuccess || before == device) before = -1;
     else error = hipSetDevice(device);
+    if (error != hipSuccess) {
+      before = -1;
+      (void)hipGetLastError(); // (the call says so; the thread's next one of any kind shall not find it)
+    }
   }
   ~OnDevice() {
     if (before >= 0) (void)hipSetDevice(before);

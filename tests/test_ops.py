@@ -917,3 +917,12 @@ def test_glr_padded_steps_have_no_gradient_whatever_that_of_the_state(T, dtype):
     assert not torch.isfinite(dx[0, 2:, ::2]).any() and not torch.isfinite(dh0[1:, ::2]).any()
     for got, ref in zip((dz, dx, dh0), want):  # the other channels
         assert torch.equal(got[..., 1::2], ref[..., 1::2]) and torch.equal(got[..., 0, :], ref[..., 0, :])
+
+
+@gpu
+def test_a_refused_device_leaves_no_error_behind():
+    p = ops.snn_glr(0, 1, 8, 0, 0, 0, 0, 0, 0, None)
+    with pytest.raises(snn.SnnError):
+        ops._run("snn_glr_forward", C.byref(ops.snn_launch(63, None, None, 0)), C.byref(p), *[None] * 6)
+    assert (torch.zeros(3, device="cuda") + 1).sum().item() == 3 and torch.cuda.current_device() == 0
+    snn.snn_glr_forward(torch.zeros(1, 1, 8, device="cuda"), torch.zeros(1, 1, 8, device="cuda"))
