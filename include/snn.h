@@ -361,7 +361,8 @@ typedef struct {
 /* Bytes of workspace for snn_vocab_loss (gradients = 0) or snn_vocab_loss_grad; 0 for an invalid shape too. */
 size_t snn_vocab_workspace(const snn_vocab *p, int32_t gradients);
 
-/* targets [rows]; one outside 0..vocab-1 (-1: padding) makes a row that has a loss of 0, no gradient and no part in a mean.
+/* targets [rows]; one outside 0..vocab-1 (-1: padding) makes a row that has a loss of 0, no gradient and no part in a mean.  A row with a target
+ * that has a logit of NaN or +infinity, or whose largest one is 2^30 or more from 0, has a loss of NaN and such gradients.
  * loss [rows] fp32; state [rows][3] fp32: a power M of two of the size of the largest exp(logit), as log2 M; 1 / sum of exp(logit) / M;
  * 1 - softmax of the target, as a sum of the other entries, so that loss and gradient of a target that is nearly certain keep their digits. */
 snn_status snn_vocab_loss(const snn_launch *at, const snn_vocab *p, const void *h, const void *w, const int32_t *targets, float *loss,

@@ -642,7 +642,10 @@ __global__ __launch_bounds__(1024) void k_join(const float2 *part, const float *
   if (at || m >= rows) return;
   const int y = targets[m];
   const bool has = y >= 0 && y < vocab;
-  const float own = has ? picked[m] : -INFINITY, top = fmaxf(ceilf(own * LOG2E), t.top);
+  const float own = has ? picked[m] : -INFINITY;
+  float top = fmaxf(ceilf(own * LOG2E), t.top);
+  // (M is off by half its last place: 64 for a logit of 2^30, which sums bear; some way beyond, terms would be infinite or all be 0)
+  if (fabsf(top) >= 0x1p30f * LOG2E && top != -INFINITY) top = __builtin_nanf("");
   const float others = t.at(top), mine = fmaf(own, LOG2E, -top);
   const float total = others + (has ? exp2f(mine) : 0.f), miss = others / total;
   loss[m] = !has ? 0.f : miss < 0.5f ? -log1pf(-miss) : (log2f(total) - mine) * 0.693147181f;

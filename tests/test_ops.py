@@ -926,3 +926,20 @@ def test_a_refused_device_leaves_no_error_behind():
         ops._run("snn_glr_forward", C.byref(ops.snn_launch(63, None, None, 0)), C.byref(p), *[None] * 6)
     assert (torch.zeros(3, device="cuda") + 1).sum().item() == 3 and torch.cuda.current_device() == 0
     snn.snn_glr_forward(torch.zeros(1, 1, 8, device="cuda"), torch.zeros(1, 1, 8, device="cuda"))
+
+
+@gpu
+@pytest.mark.parametrize("sign", [1, -1])
+def test_vocab_logits_up_to_2_to_the_30(sign):
+    # of some rows one logit's neighbours, 2^-24 of it away, are much further off than 1: a loss is a difference of logits, each off by 2^-24
+    sizes = torch.tensor([1e3, 1e6, 3.1e7, 1.7e8, 5.5e8, 1.07e9, 1.08e9, 3.4e9, 1e10, 1.1e10, 1e30], dtype=torch.float32)
+    h, w = sizes[:, None], sign * torch.tensor([[1.0], [1.5], [0.5], [1.5]])
+    for y in range(4):
+        t = torch.full((11,), y, dtype=torch.int32)
+        loss, state = snn.snn_vocab_loss(h.cuda(), w.cuda(), t.cuda())
+        dh = snn.snn_vocab_loss_grad(h.cuda(), w.cuda(), t.cuda(), state, torch.ones(11, device="cuda"))[0].cpu()
+        _, _, _, _, _, want = vocab_loss(h.double(), w.double(), t.long())
+        beyond = (h[:, 0] * (1.5 if sign > 0 else 0.5)) >= 2.0 ** 30  # the largest logit's magnitude
+        assert torch.isnan(loss.cpu()[beyond]).all() and torch.isnan(dh[beyond]).all() and torch.isfinite(dh[~beyond]).all()
+        # (both logits times log2(e), their difference, times log(2); the logarithm of a sum of two)
+        near(loss[~beyond.cuda()], want[~beyond], 8 * E32 * (want[~beyond] + 1), "loss")
