@@ -275,7 +275,7 @@ __device__ __forceinline__ int entry(const int *targets, int m, bool on, int voc
 // Logits, A = vocabulary (a piece of it from `first` on), B = rows of h.  A lane has the logits of one row with 16 MI entries of the
 // vocabulary: the exponent M of the largest and the sum of the powers above it, the target left out, and the target's logit go to memory.
 struct LossEpilogue {
-  static constexpr bool LOGITS = true;
+  static constexpr bool LOGITS = true, FEW_ROWS = false;
   const int *targets;
   float2 *part;  // [blocks of 32 MI entries][rows]
   float *picked; // [rows]: the target's logit
@@ -323,9 +323,12 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(two{a, b}, two_bf16));
 }
 
-// The same logits again, turned into G: as rows of h by entries of the vocabulary (gm) and the other way round (gt), in parts.
-template <int PARTS> struct GradEpilogue {
-  static constexpr bool LOGITS = true;
+// The same logits again, turned into G: as rows of h by entries of the vocabulary (gm) and the other way round (gt), in parts.  TWICE (bf16, FEW
+// rows or fewer): rounded, and what the rounding left as G of as many rows more, from `rows` on in gm, from FEW on in gt, which have room for
+// them (in tiles of 64 rows, in sums of 64 terms).
+constexpr int FEW = 32;
+template <int PARTS, bool TWICE> struct GradEpilogue {
+  static constexpr bool LOGITS = true, FEW_ROWS = TWICE; // (of h: no other tile than FEW_B)
   const int *targets;
   const float *state, *dloss, *common; // dloss [rows] is taken as multiples of common[0]; NULL: 1 for each row with a target
   __bf16 *gm, *gt;                    // [rows padded][width], [width][rows padded], in parts
@@ -366,7 +369,7 @@ template <int PARTS> struct GradEpilogue {
     const uint32_t pair = lane & 1 ? 0x03020706u : 0x05040100u;
     const int odd = lane & 1;
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k)
+    for (int k = 0; k < (TWICE ? 2 : PARTS); ++k)
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         Stage::turn();
@@ -378,6 +381,12 @@ template <int PARTS> struct GradEpilogue {
             if constexpr (PARTS == 1) {
               four.x = bf16_pair(acc[i][j][4 * q], acc[i][j][4 * q + 1]);
               four.y = bf16_pair(acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+              if (TWICE && k == 0)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const uint32_t pair_of = e < 2 ? four.x : four.y;
+                  acc[i][j][4 * q + e] -= __uint_as_float(e & 1 ? pair_of & 0xffff0000u : pair_of << 16);
+                }
             } else {
               uint32_t b[4];
 #pragma unroll
@@ -402,8 +411,13 @@ template <int PARTS> struct GradEpilogue {
           const int m = n * 16 + (lane >> 2), v = n * 8 + (lane >> 3);
           const uint4 of_m = *(const uint4 *)(st.first + m * 64 + (((lane & 3) ^ ((m >> 1) & 3)) * 16));
           const uint4 of_v = *(const uint4 *)(st.second + v * 128 + (((lane & 7) ^ (v & 7)) * 16));
-          *(uint4 *)(gm + place_of<PARTS>(m0 + m, v0 + 32 * i + (lane & 3) * 8, k, width)) = of_m;
-          *(uint4 *)(gt + place_of<PARTS>(v0 + 32 * i + v, m0 + (lane & 7) * 8, k, padded)) = of_v;
+          if constexpr (TWICE) {
+            if (m < rows) *(uint4 *)(gm + place_of<1>(k * rows + m, v0 + 32 * i + (lane & 3) * 8, 0, width)) = of_m;
+            if ((lane & 7) * 8 < FEW) *(uint4 *)(gt + place_of<1>(v0 + 32 * i + v, k * FEW + (lane & 7) * 8, 0, padded)) = of_v;
+          } else {
+            *(uint4 *)(gm + place_of<PARTS>(m0 + m, v0 + 32 * i + (lane & 3) * 8, k, width)) = of_m;
+            *(uint4 *)(gt + place_of<PARTS>(v0 + 32 * i + v, m0 + (lane & 7) * 8, k, padded)) = of_v;
+          }
         }
       }
   }
@@ -416,7 +430,7 @@ typedef words4 words4_any __attribute__((aligned(4)));
 typedef uint32_t words2 __attribute__((ext_vector_type(2)));
 typedef words2 words2_any __attribute__((aligned(2)));
 template <typename T> struct StoreEpilogue {
-  static constexpr bool LOGITS = false;
+  static constexpr bool LOGITS = false, FEW_ROWS = false;
   T *out;
   const float *factor;
   long long ld, per_slice;
@@ -484,7 +498,8 @@ template <int PARTS, bool WHOLE, class Epilogue> hipError_t product(Tile t, Prod
     p.slice_steps = p.ksteps;
   }
   const dim3 grid(p.tiles_a * p.tiles_b, p.slices);
-  if (t == FEW_B) k_product<256, 64, 8, 1, PARTS, WHOLE, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  if (Epilogue::FEW_ROWS || t == FEW_B) k_product<256, 64, 8, 1, PARTS, WHOLE, Epilogue><<<grid, 512, 0, s>>>(p, ep);
+  else if constexpr (Epilogue::FEW_ROWS) return hipErrorInvalidValue;
   else if (t == SMALL) k_product<128, 128, 4, 2, PARTS, WHOLE, Epilogue><<<grid, 512, 0, s>>>(p, ep);
   else if (t == BIG) k_product<256, BN, WA, WB, PARTS, WHOLE, Epilogue><<<grid, 512, 0, s>>>(p, ep);
   else if constexpr (!Epilogue::LOGITS) k_product<64, 256, 1, 8, PARTS, WHOLE, Epilogue><<<grid, 512, 0, s>>>(p, ep);
@@ -529,6 +544,7 @@ struct Operand {
   const float *dloss;
   int vocab, tiles_c;
   unsigned tiles;
+  int again; // from here on the columns have the rows from the first one on again; 0: nowhere
 };
 // 64 by 64 elements per workgroup, four in a row per thread, through LDS for the columns.  The last workgroup finds what the rows' dloss have in
 // common, where that is asked for: their largest finite magnitude, or, without any, 1 / number of rows with a target.
@@ -564,8 +580,9 @@ template <typename T, int PARTS> __global__ __launch_bounds__(256) void k_operan
   for (int i = 0; i < 4; ++i) {
     const int r = r0 + i * 16 + line, c = c0 + four;
     float v[4] = {};
-    if (r < m.rows) {
-      const T *const at = from + r * m.ld + c;
+    const int of = m.again && r >= m.again ? r - m.again : r;
+    if (of < m.rows) {
+      const T *const at = from + of * m.ld + c;
       if (c + 4 <= m.cols) {
         if constexpr (sizeof(T) == 4) {
           const words4 q = *(const words4_any *)at;
@@ -589,7 +606,7 @@ template <typename T, int PARTS> __global__ __launch_bounds__(256) void k_operan
       for (int k = 0; k < PARTS; ++k)
         *(uint2 *)(m.to_rows + place_of<PARTS>(r, c, k, m.padded_cols)) = make_uint2(part[0][k] | (uint32_t)part[1][k] << 16, part[2][k] | (uint32_t)part[3][k] << 16);
     }
-    const bool none = m.targets && r < m.rows && (!has_target(m.targets, r, true, m.vocab) || (m.dloss && m.dloss[r] == 0.f));
+    const bool none = m.targets && of < m.rows && (!has_target(m.targets, of, true, m.vocab) || (m.dloss && m.dloss[of] == 0.f));
 #pragma unroll
     for (int e = 0; e < 4; ++e) tile[i * 16 + line][four + e] = none ? 0.f : v[e];
   }
@@ -674,6 +691,8 @@ unsigned groups_for(size_t n) { return n < (1u << 28) ? (unsigned)((n + 255) / 2
 struct Space {
   Tile logits; // of the products that make logits
   int parts, dp, padded, width, block; // width: entries of a piece of the vocabulary; block: those of a wavefront
+  bool twice;                          // G is rounded, and has what that left as more rows
+  int rows_g;                          // of G with those
   int at_once;                         // entries whose logits one launch makes at most
   size_t h, w, part, picked, common, ht, wt, gm, gt, sum_h, sum_w, bytes;
   Space(const VocabShape &p, bool grad) {
@@ -683,6 +702,8 @@ struct Space {
     const int ks = parts == 1 ? KS<1> : KS<3>, rows = rows_of_b(logits, parts);
     dp = (p.d + ks - 1) / ks * ks;
     padded = (p.rows + rows - 1) / rows * rows;
+    twice = p.bf16 && p.rows <= FEW;
+    rows_g = twice ? 2 * p.rows : p.rows;
     // 2^22 tiles of 512 threads (a grid has fewer than 2^32)
     const int tile_a = rows_of_a(logits), tiles_b = padded / rows, fit_grid = (1 << 22) / (tiles_b > 0 ? tiles_b : 1);
     at_once = fit_grid < (1 << 20) / tile_a ? fit_grid * tile_a : 1 << 20;
@@ -705,8 +726,8 @@ struct Space {
       wt = take((size_t)2 * parts * p.d * width);
       gm = take((size_t)2 * parts * padded * width);
       gt = take((size_t)2 * parts * padded * width);
-      const Slices sh(p.rows, p.d, width / ks, parts), sw(width < p.vocab ? width : p.vocab, p.d, padded / ks, parts);
-      sum_h = take(width < p.vocab || sh.count > 1 ? sizeof(float) * (size_t)sh.count * p.rows * p.d : 0);
+      const Slices sh(rows_g, p.d, width / ks, parts), sw(width < p.vocab ? width : p.vocab, p.d, padded / ks, parts);
+      sum_h = take(twice || width < p.vocab || sh.count > 1 ? sizeof(float) * (size_t)sh.count * rows_g * p.d : 0);
       // (the last piece may be so much narrower that it is cut further: no more than 256 tiles in all)
       sum_w = take(sw.count > 1 || width < p.vocab ? sizeof(float) * 256 * (size_t)256 * 256 : 0);
     }
@@ -731,7 +752,7 @@ template <int PARTS, class Epilogue> hipError_t logits(Tile t, bool w_direct, co
 }
 
 template <typename T> Operand operand(const T *from, long long ld, int rows, int cols, int padded_cols, __bf16 *to_rows, int padded_rows, __bf16 *to_cols) {
-  Operand m = {from, ld, rows, cols, padded_cols, padded_rows, to_rows, to_cols, nullptr, nullptr, 0, 0, 0};
+  Operand m = {from, ld, rows, cols, padded_cols, padded_rows, to_rows, to_cols, nullptr, nullptr, 0, 0, 0, 0};
   m.tiles_c = (padded_cols + 63) / 64;
   m.tiles = to_rows || to_cols ? (unsigned)m.tiles_c * ((unsigned)((to_cols ? padded_rows : rows) + 63) / 64u) : 0;
   return m;
@@ -780,7 +801,7 @@ hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *tar
   __bf16 *const gm = (__bf16 *)(work + sp.gm), *const gt = (__bf16 *)(work + sp.gt);
   const bool h_direct = PARTS == 1 && direct(h, p.ld_h, p.d), w_direct = direct(w, p.ld_w, p.d);
   const int tile_a = rows_of_a(sp.logits);
-  const bool summed = sp.width < p.vocab || Slices(p.rows, p.d, sp.width / KS<PARTS>, PARTS).count > 1;
+  const bool summed = sp.twice || sp.width < p.vocab || Slices(p.rows, p.d, sp.width / KS<PARTS>, PARTS).count > 1;
   int slices_h = 1;
   for (long long v = 0; v < p.vocab; v += sp.width) {
     const int entries = (int)(p.vocab - v < sp.width ? p.vocab - v : sp.width), width = (entries + tile_a - 1) / tile_a * tile_a;
@@ -789,15 +810,23 @@ hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *tar
     oh.targets = targets;
     oh.dloss = dloss;
     oh.vocab = p.vocab;
+    oh.again = sp.twice ? FEW : 0;
     TRY((lay_out<T, PARTS>(oh, operand(piece, p.ld_w, entries, p.d, sp.dp, w_direct ? nullptr : wr, width, wt), targets, dloss, p.rows, p.vocab, v ? nullptr : common, s)));
     Product q = {w_direct ? (const __bf16 *)piece : wr, h_direct ? (const __bf16 *)h : hr, w_direct ? p.ld_w * (long long)(sizeof(T) / 2) : sp.dp * PARTS,
                  h_direct ? p.ld_h : sp.dp * PARTS, entries, p.rows, sp.dp / KS<PARTS>, 0, 0, 0, 0};
-    TRY((logits<PARTS>(sp.logits, w_direct, q, GradEpilogue<PARTS>{targets, state, dloss, common, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded}, s)));
-    const Slices sh(p.rows, p.d, width / KS<PARTS>, PARTS, v ? slices_h : 256), sw(entries, p.d, sp.padded / KS<PARTS>, PARTS);
+    auto g = [&](auto ep) {
+      ep = {targets, state, dloss, common, gm, gt, (int)v, p.vocab, p.rows, width, sp.padded};
+      return logits<PARTS>(sp.logits, w_direct, q, ep, s);
+    };
+    if constexpr (PARTS == 1) {
+      if (sp.twice) TRY(g(GradEpilogue<1, true>()));
+      else TRY(g(GradEpilogue<1, false>()));
+    } else TRY(g(GradEpilogue<PARTS, false>()));
+    const Slices sh(sp.rows_g, p.d, width / KS<PARTS>, PARTS, v ? slices_h : 256), sw(entries, p.d, sp.padded / KS<PARTS>, PARTS);
     if (!v) slices_h = sh.count;
-    Product dhq = {gm, wt, (long long)width * PARTS, (long long)width * PARTS, p.rows, p.d, width / KS<PARTS>, 0, 0, sh.count, sh.steps};
+    Product dhq = {gm, wt, (long long)width * PARTS, (long long)width * PARTS, sp.rows_g, p.d, width / KS<PARTS>, 0, 0, sh.count, sh.steps};
     if (!summed) TRY((product<PARTS, false>(sh.tile, dhq, StoreEpilogue<T>{dh, common, p.d, 0, p.rows, p.d, false}, s)));
-    else TRY((product<PARTS, false>(sh.tile, dhq, StoreEpilogue<float>{sum_h, nullptr, p.d, (long long)p.rows * p.d, p.rows, p.d, v > 0}, s)));
+    else TRY((product<PARTS, false>(sh.tile, dhq, StoreEpilogue<float>{sum_h, nullptr, p.d, (long long)sp.rows_g * p.d, sp.rows_g, p.d, v > 0}, s)));
     Product dwq = {gt, ht, (long long)sp.padded * PARTS, (long long)sp.padded * PARTS, entries, p.d, sp.padded / KS<PARTS>, 0, 0, sw.count, sw.steps};
     T *const to = dw + v * p.d;
     if (sw.count == 1) TRY((product<PARTS, false>(sw.tile, dwq, StoreEpilogue<T>{to, common, p.d, 0, entries, p.d, false}, s)));
@@ -810,7 +839,7 @@ hipError_t gradients(const VocabShape &p, const T *h, const T *w, const int *tar
   }
   if (summed) {
     const size_t n = (size_t)p.rows * p.d;
-    k_sum<T><<<groups_for(n), 256, 0, s>>>(sum_h, slices_h, n, common, dh);
+    k_sum<T><<<groups_for(n), 256, 0, s>>>(sum_h, sp.twice ? 2 * slices_h : slices_h, n, common, dh);
   }
   return hipGetLastError();
 }

@@ -943,3 +943,22 @@ def test_vocab_logits_up_to_2_to_the_30(sign):
         assert torch.isnan(loss.cpu()[beyond]).all() and torch.isnan(dh[beyond]).all() and torch.isfinite(dh[~beyond]).all()
         # (both logits times log2(e), their difference, times log(2); the logarithm of a sum of two)
         near(loss[~beyond.cuda()], want[~beyond], 8 * E32 * (want[~beyond] + 1), "loss")
+
+
+@gpu
+@pytest.mark.parametrize("rows,d,vocab", [(1, 64, 7), (1, 512, 1000), (2, 70, 300), (31, 130, 1025), (32, 64, 129), (17, 200, 2500), (32, 96, 5003), (5, 24, 4100)])
+def test_vocab_gradients_of_few_rows_lose_nothing_but_their_own_rounding(rows, d, vocab):
+    # sums of few terms, or of few that count: each element of G is off by its logits and 2^-16, nothing of the size of a rounding to bf16
+    h, w, t, dloss = vocab_inputs(rows, d, vocab, torch.bfloat16, seed=rows)
+    t[0] = vocab // 2
+    gh, gw, gt = h.cuda(), w.cuda(), t.cuda()
+    state = snn.snn_vocab_loss(gh, gw, gt)[1]
+    H, W, t64 = h.double(), w.double(), t.long()
+    e_l = (d + 8) * E32 * (H.abs() @ W.abs().T).amax(1) + 4 * E32 * (H @ W.T).abs().amax(1)
+    for given in (None, dloss):
+        on = (t >= 0).double()
+        G, want_h, want_w = vocab_grads(H, W, t64, on / on.sum() if given is None else given.double())
+        dh, dw = snn.snn_vocab_loss_grad(gh, gw, gt, state, None if given is None else given.cuda())
+        A = G.abs() * (4 * e_l + (80 + vocab / 64) * E32 + 2.0 ** -16)[:, None]
+        near(dh, want_h, A @ W.abs() + (vocab + 8) * E32 * (G.abs() @ W.abs()) + 1e-30, "dh")
+        near(dw, want_w, A.T @ H.abs() + (rows + 8) * E32 * (G.abs().T @ H.abs()) + 1e-30, "dw")
