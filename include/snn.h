@@ -351,7 +351,9 @@ snn_status snn_glr_backward_packed(const snn_launch *at, const snn_glr *p, const
 
 /* Softmax cross entropy of rows h [rows][d] against a vocabulary w [vocab][d] (a row per entry, the layout of an embedding table):
  *   logits_r = w h_r ;  loss_r = log sum_v exp(logits_rv) - logits_r,target
- * Logits are never in memory as a whole.  bf16 products are summed in fp32; in fp32 they keep 24 bits. */
+ * Logits are never in memory as a whole.  Products are summed in fp32; in fp32 they keep 24 bits.  With bf16 and
+ * more than 32 rows the gradients' products take the rows' factors, softmax less 1 at the target times dloss, in bf16 too (each off by 2^-8 of
+ * itself at most), with up to 32 rows in 16 bits. */
 typedef struct {
   int32_t rows, d, vocab; /* rows 0..2^22, d 1..2^16 (rows * d 2^35 at most), vocab 1..2^24 */
   int32_t dtype;          /* snn_dtype of h, w, dh, dw */

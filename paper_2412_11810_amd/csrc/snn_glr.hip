@@ -14,9 +14,9 @@
 // the same exchange, beside that of the gradient, which runs the other way.
 //
 // What bounds it: memory, where there are channels or steps enough.  Forward, 4096 x 8 x 2048 in bf16: 80 us, 5.1 TB/s of z, x and h (a copy reaches
-// 5.1); backward, 1000 x 32 x 1024 in fp32: 122 us, 5.4 TB/s; 32768 x 1 x 1024 in bf16: 100 us, of which 27 for the maps of its
-// segments; from 8 bits, 4096 x 8 x 2048: 147 us, 3.7 TB/s, bound by the number of 1- and 2-byte loads.  One token of 64 x 2048: 3.2 us.
-// Short sequences are bound by the latency of a tile, some 5 us.
+// 5.1); backward, 1000 x 32 x 1024 in fp32: 122 us, 5.4 TB/s; 32768 x 1 x 1024 in bf16: 99 us, of which 26 for the maps of its
+// segments; from 8 bits, 4096 x 8 x 2048: 147 us, 3.7 TB/s, bound by the number of 1- and 2-byte loads.  One token of 64 x 2048: 2.8 us.
+// Short sequences are bound by the latency of a tile, some 5 us.  Outputs that lie behind a sequence's end are zeros; its steps are read all the same.
 #include "snn_ops.h"
 
 namespace {
@@ -548,7 +548,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
 
 // From WHOLE groups of channels on, one workgroup per group walks the whole sequence: z and x are read once.  Fewer would leave too many
 // compute units without work: the sequence is then cut into segments so that there are WORKGROUPS in all, at the price of a launch before
-// that finds the segments' maps (z and x, or dh, are read twice).
+// that finds the segments' maps (z and x, or dh, are read twice).  Forward passes of 4096 steps in bf16, one channel per lane, whole and cut:
+// 128 groups 66 and 60 us, 160 groups 66 and 74 us, 192 groups 67 and 93 us (backward 106 and 86, 106 and 111, 124 and 149); in fp32 128 groups
+// 77 and 104 us (backward 166 and 158).  16384 steps of 32 groups in bf16: 244 and 63 us.  A call of few steps is as long as its launches:
+// 4 us more where it is cut (333 x 13 x 75 in fp32: 14 and 18 us), which whole sequences of more than five tiles cost as well.
 constexpr int WHOLE = 160, WORKGROUPS = 512;
 int groups_of(int channels, int vec) { return (channels + 64 * vec - 1) / (64 * vec); }
 void cut(Args *a, int vec) {
@@ -558,8 +561,9 @@ void cut(Args *a, int vec) {
   a->seg_tiles = a->tiles ? (a->tiles + want - 1) / want : 1;
   a->segments = a->tiles ? (a->tiles + a->seg_tiles - 1) / a->seg_tiles : 1;
 }
-// Two channels per lane in bf16, unless one per lane makes enough groups to walk the sequence whole and two do not
-// (16384 channels, 4096 steps: 84 us instead of 111).
+// Two channels per lane in bf16, unless one per lane makes enough groups to walk the sequence whole and two do not.  4096 steps, one per lane and
+// two: 16384 channels (whole, cut) 74 and 112 us, backward 135 and 179; 24576 channels (whole both) 146 and 138 us, backward 245 and 256; 8192
+// channels (cut both) 60 and 60 us, backward 86 and 85.
 bool two_per_lane(const GlrShape &p) {
   const int channels = p.batch * p.n;
   return p.bf16 && p.n % 2 == 0 && (groups_of(channels, 2) >= WHOLE || groups_of(channels, 1) < WHOLE);
@@ -658,6 +662,7 @@ hipError_t launch_glr_backward(const GlrShape &p, const GlrInputs &in, const flo
     a.ld_xe = in.ld_xe;
   }
   // 64 channels in a row begin in four blocks at most if there is no more than one row's end among them, 128 if rows are multiples of that
+  // (other even rows load a step's exponents one by one: 512 x 64 x 2080 takes 143 us, x 2048 136)
   const bool shared = p.n >= 64;
   if (!p.bf16) return !packed ? backward<float, float, 1>(a, s) : shared ? backward<float, int8_t, 1, true>(a, s) : backward<float, int8_t, 1>(a, s);
   const size_t size = packed ? 1 : 2;

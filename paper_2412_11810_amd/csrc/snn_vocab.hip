@@ -6,6 +6,11 @@
 //
 // c is what the rows' dloss have in common (their largest magnitude, 1 / number of rows for a mean): rounded into G, a factor like 1 / 300
 // would be off by up to 2^-8 for all rows alike.
+// G itself is found in 32 bits and, where h and w are bf16, rounded to bf16 on its way into its two products: the matrix cores take both operands in
+// one type, and two parts of G would cost 7 ms beside the 15 of 8192 x 2048 x 128000.  Each element is off by 2^-8 of itself at most, each in its
+// own way; that adds 0 to 14 % to what dh and dw are off by for their own rounding (1.66e-3 of their norm; 33 x 512 x 1000 to 2000 x 512 x 5000,
+// logits spread over +-1 to +-12).  Sums of few terms would show more of it (one row of 512 with 1000 entries: 57 %): up to 32 rows, which leave half
+// of a tile empty, what the rounding leaves goes through the products as further rows.
 //
 // miss_r is summed without the target, never formed as 1 - p: a target that the model is sure of keeps its loss and gradient.
 // The subtrahends are whole numbers: l - M is one fused multiply-add, rounded once to its own size, and sums over different M are brought
@@ -19,8 +24,8 @@
 // after the other, whose G is all that is ever in memory.
 //
 // What bounds it: the matrix cores, at the clock that they leave.  8192 x 2048 x 128000 in bf16 takes 15.2 ms, four products of 4.3 TFLOP at
-// 1.13 PFLOP/s (a library product with sums of 2048: 1.20); the loss of 4096 x 2048 x 50021 719 us, 1.17 PFLOP/s, matrix instructions in 69 % of
-// the cycles at 1.96 GHz.  Few rows are bound by w: 12 x 768 x 99960 in fp32, 307 MB, takes 93 us.
+// 1.13 PFLOP/s (a library product with sums of 2048: 1.18 to 1.20); the loss of 4096 x 2048 x 50021 720 us, 1.16 PFLOP/s, matrix instructions in 69 % of
+// the cycles at 1.9 GHz.  (Machines differ: on another one 15.8 ms and 747 us.)  Few rows are bound by w: 12 x 768 x 99960 in fp32, 307 MB, takes 93 us.
 #include "snn_ops.h"
 
 namespace {
@@ -38,10 +43,11 @@ template <int PARTS> __device__ __forceinline__ size_t place_of(size_t row, int 
   return (row * padded + (c & ~31)) * PARTS + part * 32 + (c & 31);
 }
 // Tiles: 256 rows of A by 256 of B, or, in parts, by 128; 64 by 256 where a side has no more than 64 rows (products that make logits: that of B
-// only); 128 by 128 where 256 compute units are through with those sooner.  An element of a small tile takes 1.3 to 1.45 times as long
-// (the loss of 4096 x 2048 x 50021 in bf16 takes 721 us with large tiles and 909 us with small ones), in parts less than 1.12 times (2000 x 1024 x
-// 20011 in fp32 with gradients: 1.95 and 1.93 ms), but few large tiles leave units without work (loss and gradients in bf16, 300 x 512 x 1000: 82
-// and 42 us; 2048 x 1024 x 4096: 144 and 115 us).
+// only); 128 by 128 where 256 compute units are through with those sooner.  By the rounds that the units take, an element of a small tile takes
+// 1.2 to 1.45 times as long in bf16 (loss of 8192 x 1024 x 16384, 8 rounds of large tiles and 32 quarter ones: 284 and 355 us; of 1500 x 768 x
+// 12000, 2 rounds and 5 quarters: 58 and 53 us), in parts 1.01 to 1.12 times (2000 x 1024 x 20011: 435 and 446 us; 1500 x 768 x 12000: 193 and
+// 174 us).  The rule takes the upper end: at the lower one 2000 x 1024 x 20011 in bf16 would get small tiles, 117 us instead of 106.  Few
+// large tiles leave units without work (2048 x 1024 x 4096 in bf16: 39 and 31 us, with gradients 132 and 98; 300 x 512 x 1000: 27 and 17, 66 and 34).
 enum Tile { BIG, SMALL, FEW_A, FEW_B };
 int rows_of_a(Tile t) { return t == FEW_A ? 64 : t == SMALL ? 128 : 256; }
 int rows_of_b(Tile t, int parts) { return t == FEW_B ? 64 : t == FEW_A ? 256 : t == SMALL || parts > 1 ? 128 : 256; }

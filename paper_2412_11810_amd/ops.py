@@ -2,8 +2,9 @@
 
 Every call queues its kernels on the current stream of its tensors' device and returns; results and workspace are tensors of torch's
 allocator, so calls may be captured into a graph like torch's own.  Arguments that do not fit raise before anything is queued
-(TypeError: element types, ValueError: shapes, strides and devices, SnnError: what the library refuses).  Gradients come from the
-backward calls; nothing is recorded for torch.autograd.
+(TypeError: element types, ValueError: shapes, strides and devices, SnnError: what the library refuses).  No element of a result may be
+one of another tensor of the call, but where it is said so.  Gradients come from the backward calls: nothing is recorded for torch.autograd,
+and results have no history even where an argument requires a gradient.
 """
 from __future__ import annotations
 
