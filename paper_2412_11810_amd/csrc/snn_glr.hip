@@ -51,11 +51,11 @@ template <typename T, int VEC> __device__ __forceinline__ typename Raw<T, VEC>::
   }
 }
 
-// sigmoid(z) and sigmoid(-z) from z / log(2); below 2^-126 they are 0, sigmoid(-z) (EVERY) 2^-126.  Where e^z is infinite sigmoid(z) is right
-// with EVERY and NaN without.
-constexpr float LOG2E = 1.44269504f;
+// sigmoid(z) and sigmoid(-z) from z / log(2), which is LARGEST at most (the reciprocal gives no numbers below 2^-126) or, EVERY, taken to be: there
+// sigmoid(-z) is 2^-126.  sigmoid(z) below 2^-126 is 0.
+constexpr float LOG2E = 1.44269504f, LARGEST = 126.f;
 template <bool EVERY> __device__ __forceinline__ void gate(float z, float &a, float &b) {
-  const float e = __builtin_amdgcn_exp2f(EVERY && z > 126.f ? 126.f : z); // (NaN stays)
+  const float e = __builtin_amdgcn_exp2f(EVERY && z > LARGEST ? LARGEST : z); // (NaN stays)
   b = __builtin_amdgcn_rcpf(1.f + e);
   a = e * b;
 }
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
   for (; n > 0; --n, MAPS ? --k : ++k, t0 += STRIDE) {
     // Each step's state as P h + B of the one that these start from.  NW = 1: the smaller of a and b, a as a negative number, and the drive;
     // a state that goes from call to call is moved by h + b (x - h) where a is next to one.
-    float P[S][VEC], B[S][VEC], Q[VEC];
+    float P[S][VEC], B[S][VEC], Q[VEC], top = 0.f;
     const int live = me.len - t0; // steps of these 16 that the sequence has
     const bool whole = __all(live >= S);
     ordinarily(
@@ -261,7 +261,9 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
               float keep, move;
-              gate<!ORDINARY>(z[v] * LOG2E, keep, move);
+              z[v] *= LOG2E;
+              top = fmaxf(top, z[v]);
+              gate<!ORDINARY>(z[v], keep, move);
               if (!ORDINARY) {
                 x[v] = nan_if_infinite(x[v]);
                 if (j >= live) keep = 1.f, move = x[v] = 0.f;
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(64 * NW) void k_glr_forward(Args a) {
           }
         },
         [&] {
-          bool bad = false;
+          bool bad = top > LARGEST;
 #pragma unroll
           for (int v = 0; v < VEC; ++v) bad |= !(P[S - 1][v] + fabsf(B[S - 1][v]) < INFINITY); // (once so, so to the end)
           return bad;
@@ -417,7 +419,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
     R d[STEPS]; // (as it is in memory: half the registers)
     const int live = me.len - t0;
     const bool whole = __all(live >= STEPS);
-    float product[VEC], Q[VEC];
+    float product[VEC], Q[VEC], top = 0.f;
     if (LATE) pd.load(d, t0, a.T);
     // (a step is a power of two: its product with log2(e) is exact)
     float steps_z = __uint_as_float(shared_z << 23) * LOG2E, steps_x = __uint_as_float(shared_x << 23);
@@ -435,7 +437,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
             const float step_x = MAPS ? 1.f : SHARED ? of_x.of(steps_x, j) : PACKED ? __uint_as_float((uint32_t)ex[j] << 23) : 1.f;
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
-              gate<!ORDINARY>(z[v] * step_z, keep[j][v], move[j][v]);
+              z[v] *= step_z;
+              top = fmaxf(top, z[v]);
+              gate<!ORDINARY>(z[v], keep[j][v], move[j][v]);
               if (PACKED && !MAPS) x[j][v] *= step_x;
               if (!MAPS) x[j][v] *= move[j][v];
               if (!ORDINARY && j >= live) keep[j][v] = 1.f, move[j][v] = x[j][v] = 0.f;
@@ -445,7 +449,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_glr_backward(Args a) {
           }
         },
         [&] {
-          bool bad = false;
+          bool bad = top > LARGEST;
 #pragma unroll
           for (int v = 0; v < VEC; ++v) bad |= product[v] != product[v];
           return bad;
