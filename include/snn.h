@@ -375,6 +375,62 @@ snn_status snn_vocab_loss(const snn_launch *at, const snn_vocab *p, const void *
 snn_status snn_vocab_loss_grad(const snn_launch *at, const snn_vocab *p, const void *h, const void *w, const int32_t *targets,
                                const float *state, const float *dloss, void *dh, void *dw);
 
+/* Root-mean-square norm of rows, of the sum with what went past the layers before it:
+ *   s = x + residual (or x) ;  y = w s / sqrt(mean(s^2) + eps)
+ * Computed in fp32 from the sum before it is rounded to dtype.  Rows may hold numbers of any size.  A row with an infinity or NaN gives what the
+ * formula gives (NaN at these), one of zeros with eps = 0 NaN. */
+typedef struct {
+  int64_t rows;           /* >= 0; rows * n 2^40 at most */
+  int32_t n;              /* 1..2^15 */
+  int32_t dtype;          /* snn_dtype of all arrays */
+  float eps;              /* >= 0 */
+  int64_t ld_x, ld_residual, ld_total; /* elements between consecutive rows (0: n); total: of the backward pass too */
+  int64_t ld_y;           /* of y, of dy */
+  int64_t ld_dtotal, ld_dx;
+} snn_norm;
+
+/* Bytes of workspace for snn_norm_backward with dw; the forward calls, and the backward one without, take none. */
+size_t snn_norm_workspace(const snn_norm *p);
+
+/* w [n] or NULL (ones); residual [rows][n] or NULL, then total must be NULL too; total [rows][n] or NULL: s, which may take the place of x or of the residual
+ * (the same rows, equally far apart). */
+snn_status snn_norm_forward(const snn_launch *at, const snn_norm *p, const void *x, const void *residual, const void *w, void *total, void *y);
+/* The same with y in 8 bits, as snn_pack would give it of a y that had not been rounded: codes [rows][n], exps [rows][ceil(n / 32)], packed. */
+snn_status snn_norm_forward_packed(const snn_launch *at, const snn_norm *p, const void *x, const void *residual, const void *w, void *total,
+                                   int8_t *codes, uint8_t *exps);
+/* From total, as the forward pass gave it (or x, without a residual), and the gradients of y and, where dtotal is not NULL, of total: dx, which is the
+ * residual's gradient as well and may take the place of dy or dtotal, and dw [n] (NULL: not wanted). */
+snn_status snn_norm_backward(const snn_launch *at, const snn_norm *p, const void *total, const void *w, const void *dy, const void *dtotal, void *dx,
+                             void *dw);
+
+/* A step of AdamW over many tensors:
+ *   m = beta1 m + (1 - beta1) g ;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32, each element from its moments before they are rounded to 8 bits. */
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay; /* 0 <= beta < 1, eps >= 0 */
+  int64_t step;            /* t: 1, 2, ... */
+  int32_t *step_on_device; /* [1] or NULL: steps taken so far, which the call counts up, and then goes by in place of `step` (a step in a graph) */
+  const float *grad_scale; /* [1] or NULL: what the gradients are multiplied by first (1 / a loss scale, a clipping of their norm) */
+} snn_adamw;
+typedef struct {
+  void *p;                   /* [n] of dtype_p.  bf16 is rounded to nearest each time: a step of less than 2^-9 of an element leaves it as it is */
+  const void *g;             /* [n] of dtype_g */
+  void *m, *v;               /* [n] fp32; or, with exponents, int8 codes of m and of the root of v */
+  uint8_t *m_exps, *v_exps;  /* [ceil(n / 32)] both, or both NULL: steps of blocks of 32 elements in the format of snn_pack.  Codes are rounded up or
+                                down by a threshold that depends on the element's place and on t alone, such that roundings cancel over the
+                                steps; a root that is not 0 has a code of 1 or more.  A block with a moment that is not finite is NaN from then on */
+  void *copy;                /* [n] bf16 or NULL: p rounded, for the layers that compute in bf16 (p in fp32) */
+  int64_t n;                 /* 0..2^40 */
+  int32_t dtype_p, dtype_g;  /* snn_dtype */
+} snn_adamw_tensor;
+
+/* Bytes of workspace: none unless the step's number is on the device. */
+size_t snn_adamw_workspace(const snn_adamw *how);
+/* tensors: `count` descriptions in host memory, which are read before the call returns.  No two arrays that are written may share elements, nor may a
+ * gradient with one of them (SNN_E_INVAL). */
+snn_status snn_adamw_step(const snn_launch *at, const snn_adamw *how, const snn_adamw_tensor *tensors, int64_t count);
+
 /*
  * Test hooks.  The library chooses its kernels from the layer shapes, the batch size, the state size and the
  * firing rates of the previous step; every choice by the rates gives the same bits.  The parity tests force each

@@ -3,8 +3,13 @@
 #include "../../include/snn.h"
 #include "snn_ops.h"
 
+#include <algorithm>
+#include <cmath>
+#include <new>
 #include <stdarg.h>
 #include <stdio.h>
+#include <utility>
+#include <vector>
 
 namespace {
 
@@ -136,6 +141,71 @@ snn_status vocab_shape(const char *what, const snn_vocab *p, VocabShape *v) {
   return SNN_OK;
 }
 
+snn_status norm_shape(const char *what, const snn_norm *p, NormShape *n) {
+  if (!p) return refuse(SNN_E_INVAL, "%s: no shape", what);
+  if (!dtype_ok(p->dtype)) return refuse(SNN_E_INVAL, "%s: unknown type %d", what, p->dtype);
+  if (p->n < 1 || p->n > (1 << 15) || p->rows < 0 || p->rows > (1ll << 40) / p->n)
+    return refuse(SNN_E_INVAL, "%s: %lld rows of %d: 1 .. 2^15 elements, 2^40 in all at most", what, (long long)p->rows, p->n);
+  if (!(p->eps >= 0.f) || !(p->eps < 1e30f)) return refuse(SNN_E_INVAL, "%s: eps = %g", what, p->eps);
+  *n = NormShape{p->rows, p->n, p->dtype == SNN_BF16, p->eps, p->ld_x, p->ld_residual, p->ld_total, p->ld_y, p->ld_dtotal, p->ld_dx};
+  for (long long *ld : {&n->ld_x, &n->ld_residual, &n->ld_total, &n->ld_y, &n->ld_dtotal, &n->ld_dx}) {
+    if (!*ld) *ld = p->n;
+    if (*ld < p->n || *ld > (1ll << 40)) return refuse(SNN_E_INVAL, "%s: %lld elements from row to row: n .. 2^40", what, *ld);
+  }
+  return SNN_OK;
+}
+
+snn_status norm_forward(const char *what, const snn_launch *at, const snn_norm *p, const void *x, const void *residual, const void *w, void *total,
+                        void *y, int8_t *codes, uint8_t *exps, bool packed) {
+  NormShape n;
+  CHECK(launch_ok(what, at));
+  CHECK(norm_shape(what, p, &n));
+  if (!n.rows) return SNN_OK;
+  const size_t size = size_of(p->dtype);
+  const Array arrays[] = {{"x", x, size, true}, {"residual", residual, size, false}, {"w", w, size, false}, {"total", total, size, false},
+                          {"y", y, size, !packed}, {"the codes", codes, 1, packed}, {"the exponents", exps, 1, packed}};
+  CHECK(check(what, at, arrays));
+  if (total && !residual) return refuse(SNN_E_INVAL, "%s: a total without a residual", what);
+  const OnDevice on(at->device);
+  if (on.error != hipSuccess) return queued(on.error, what);
+  return queued(launch_norm(n, x, residual, w, total, y, codes, exps, (hipStream_t)at->stream), what);
+}
+
+// No two of the arrays that a step writes may share elements: it would change them twice, or at the same time.
+struct Written { uintptr_t from, to; };
+snn_status adamw_arrays(const char *what, const snn_launch *at, const snn_adamw_tensor *tensors, int64_t count, std::vector<AdamwTensor> &out) {
+  std::vector<Written> written;
+  out.reserve(count);
+  written.reserve(6 * count);
+  for (int64_t k = 0; k < count; ++k) {
+    const snn_adamw_tensor &x = tensors[k];
+    if (!dtype_ok(x.dtype_p) || !dtype_ok(x.dtype_g)) return refuse(SNN_E_INVAL, "%s: tensor %lld: unknown type", what, (long long)k);
+    if (x.n < 0 || x.n > (1ll << 40)) return refuse(SNN_E_INVAL, "%s: tensor %lld: %lld elements: 0 .. 2^40", what, (long long)k, (long long)x.n);
+    if (!x.m_exps != !x.v_exps) return refuse(SNN_E_INVAL, "%s: tensor %lld: one moment with exponents, one without", what, (long long)k);
+    if (x.copy && x.dtype_p != SNN_F32) return refuse(SNN_E_INVAL, "%s: tensor %lld: a copy in bf16 of what is in bf16", what, (long long)k);
+    if (!x.n) continue;
+    const bool eight = x.m_exps != nullptr;
+    const size_t size_p = size_of(x.dtype_p), size_m = eight ? 1 : 4;
+    const Array arrays[] = {{"p", x.p, size_p, true}, {"g", x.g, size_of(x.dtype_g), true}, {"m", x.m, size_m, true}, {"v", x.v, size_m, true},
+                            {"the exponents of m", x.m_exps, 1, eight}, {"the exponents of v", x.v_exps, 1, eight}, {"the copy", x.copy, 2, false}};
+    CHECK(check(what, at, arrays));
+    const size_t exps = (x.n + SNN_PACK_BLOCK - 1) / SNN_PACK_BLOCK;
+    const std::pair<const void *, size_t> to[] = {{x.p, x.n * size_p}, {x.m, x.n * size_m}, {x.v, x.n * size_m}, {x.m_exps, exps}, {x.v_exps, exps}, {x.copy, 2 * x.n}};
+    for (auto [p, bytes] : to)
+      if (p) written.push_back({(uintptr_t)p, (uintptr_t)p + bytes});
+    out.push_back(AdamwTensor{x.p, x.g, x.m, x.v, x.m_exps, x.v_exps, x.copy, x.n, x.dtype_p == SNN_BF16, x.dtype_g == SNN_BF16});
+  }
+  std::sort(written.begin(), written.end(), [](const Written &a, const Written &b) { return a.from < b.from; });
+  for (size_t i = 1; i < written.size(); ++i)
+    if (written[i].from < written[i - 1].to) return refuse(SNN_E_INVAL, "%s: two of the arrays that the step writes share elements", what);
+  for (const AdamwTensor &x : out) { // a gradient may be anywhere but in what is written
+    const uintptr_t from = (uintptr_t)x.g, to = from + x.n * (x.g16 ? 2 : 4);
+    const auto next = std::upper_bound(written.begin(), written.end(), from, [](uintptr_t v, const Written &w) { return v < w.to; });
+    if (next != written.end() && next->from < to) return refuse(SNN_E_INVAL, "%s: a gradient shares elements with an array that the step writes", what);
+  }
+  return SNN_OK;
+}
+
 } // namespace
 
 extern "C" {
@@ -245,6 +315,64 @@ snn_status snn_vocab_loss_grad(const snn_launch *at, const snn_vocab *p, const v
   const OnDevice on(at->device);
   if (on.error != hipSuccess) return queued(on.error, what);
   return queued(launch_vocab_grad(v, h, w, targets, state, dloss, dh, dw, at->workspace, (hipStream_t)at->stream), what);
+}
+
+size_t snn_norm_workspace(const snn_norm *p) {
+  NormShape n;
+  return norm_shape("snn_norm_workspace", p, &n) == SNN_OK ? norm_workspace(n) : 0;
+}
+
+snn_status snn_norm_forward(const snn_launch *at, const snn_norm *p, const void *x, const void *residual, const void *w, void *total, void *y) {
+  return norm_forward("snn_norm_forward", at, p, x, residual, w, total, y, nullptr, nullptr, false);
+}
+
+snn_status snn_norm_forward_packed(const snn_launch *at, const snn_norm *p, const void *x, const void *residual, const void *w, void *total,
+                                   int8_t *codes, uint8_t *exps) {
+  return norm_forward("snn_norm_forward_packed", at, p, x, residual, w, total, nullptr, codes, exps, true);
+}
+
+snn_status snn_norm_backward(const snn_launch *at, const snn_norm *p, const void *total, const void *w, const void *dy, const void *dtotal, void *dx,
+                             void *dw) {
+  static const char what[] = "snn_norm_backward";
+  NormShape n;
+  CHECK(launch_ok(what, at));
+  CHECK(norm_shape(what, p, &n));
+  const size_t size = size_of(p->dtype);
+  const bool some = n.rows > 0;
+  if (!some && !dw) return SNN_OK;
+  const Array arrays[] = {{"total", total, size, some}, {"w", w, size, dw != nullptr}, {"dy", dy, size, some}, {"dtotal", dtotal, size, false},
+                          {"dx", dx, size, some}, {"dw", dw, size, false}};
+  CHECK(check(what, at, arrays));
+  if (dw) CHECK(check_workspace(what, at, norm_workspace(n)));
+  const OnDevice on(at->device);
+  if (on.error != hipSuccess) return queued(on.error, what);
+  return queued(launch_norm_backward(n, total, w, dy, dtotal, dx, dw, (float *)at->workspace, (hipStream_t)at->stream), what);
+}
+
+size_t snn_adamw_workspace(const snn_adamw *how) { return how && how->step_on_device ? adamw_workspace() : 0; }
+
+snn_status snn_adamw_step(const snn_launch *at, const snn_adamw *how, const snn_adamw_tensor *tensors, int64_t count) {
+  static const char what[] = "snn_adamw_step";
+  CHECK(launch_ok(what, at));
+  if (!how || count < 0 || count > (1 << 24) || (count && !tensors)) return refuse(SNN_E_INVAL, "%s: no step, or no tensors", what);
+  if (!std::isfinite(how->lr) || !std::isfinite(how->weight_decay) || !(how->beta1 >= 0 && how->beta1 < 1) || !(how->beta2 >= 0 && how->beta2 < 1) ||
+      !(how->eps >= 0 && how->eps < 1e30))
+    return refuse(SNN_E_INVAL, "%s: lr %g, betas %g and %g (0 .. 1, less than 1), eps %g, weight decay %g", what, how->lr, how->beta1, how->beta2,
+                  how->eps, how->weight_decay);
+  if (!how->step_on_device && how->step < 1) return refuse(SNN_E_INVAL, "%s: step %lld: the first one is 1", what, (long long)how->step);
+  const Array arrays[] = {{"the step", how->step_on_device, 4, false}, {"the gradients' scale", how->grad_scale, 4, false}};
+  CHECK(check(what, at, arrays));
+  CHECK(check_workspace(what, at, snn_adamw_workspace(how)));
+  try {
+    std::vector<AdamwTensor> all;
+    CHECK(adamw_arrays(what, at, tensors, count, all));
+    const OnDevice on(at->device);
+    if (on.error != hipSuccess) return queued(on.error, what);
+    const AdamwStep step = {how->lr, how->beta1, how->beta2, how->eps, how->weight_decay, how->step, how->step_on_device, how->grad_scale};
+    return queued(launch_adamw(step, all.data(), (long long)all.size(), at->workspace, (hipStream_t)at->stream), what);
+  } catch (const std::bad_alloc &) {
+    return refuse(SNN_E_HOSTMEM, "%s: no memory for the descriptions of %lld tensors", what, (long long)count);
+  }
 }
 
 } // extern "C"

@@ -43,3 +43,38 @@ hipError_t launch_vocab_loss(const VocabShape &p, const void *h, const void *w, 
                              void *work, hipStream_t s);
 hipError_t launch_vocab_grad(const VocabShape &p, const void *h, const void *w, const int *targets, const float *state,
                              const float *dloss, void *dh, void *dw, void *work, hipStream_t s);
+
+// ---- root-mean-square norm (snn_norm.hip) ---------------------------------------------------
+struct NormShape {
+  long long rows;
+  int n;
+  bool bf16;
+  float eps;
+  long long ld_x, ld_residual, ld_total, ld_y, ld_dtotal, ld_dx; // elements between rows (ld_y: of y and dy)
+};
+size_t norm_workspace(const NormShape &p); // of the backward pass
+// y, or codes and exps, of x + residual (NULL: of x), which goes to total (NULL: nowhere); w may be NULL
+hipError_t launch_norm(const NormShape &p, const void *x, const void *residual, const void *w, void *total, void *y, int8_t *codes, uint8_t *exps,
+                       hipStream_t s);
+// dtotal, dw may be NULL
+hipError_t launch_norm_backward(const NormShape &p, const void *total, const void *w, const void *dy, const void *dtotal, void *dx, void *dw,
+                                float *sums, hipStream_t s);
+
+// ---- AdamW (snn_adamw.hip) ------------------------------------------------------------------
+struct AdamwStep {
+  double lr, beta1, beta2, eps, decay;
+  long long t;  // the step's number, or
+  int *count;   // where it is, less one, on the device
+  const float *scale; // of the gradients; NULL: 1
+};
+struct AdamwTensor {
+  void *p;
+  const void *g;
+  void *m, *v;                 // 32 bits, or codes where there are
+  uint8_t *m_exps, *v_exps;
+  void *copy;                  // bf16 or NULL
+  long long n;
+  bool p16, g16;
+};
+size_t adamw_workspace(); // where the count is on the device
+hipError_t launch_adamw(const AdamwStep &how, const AdamwTensor *tensors, long long count, void *work, hipStream_t s);

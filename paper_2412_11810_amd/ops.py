@@ -34,6 +34,21 @@ class snn_vocab(C.Structure):
                 ("ld_w", C.c_int64)]
 
 
+class snn_norm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float), ("ld_x", C.c_int64),
+                ("ld_residual", C.c_int64), ("ld_total", C.c_int64), ("ld_y", C.c_int64), ("ld_dtotal", C.c_int64), ("ld_dx", C.c_int64)]
+
+
+class snn_adamw(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("step", C.c_int64), ("step_on_device", C.c_void_p), ("grad_scale", C.c_void_p)]
+
+
+class snn_adamw_tensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_exps", C.c_void_p), ("v_exps", C.c_void_p),
+                ("copy", C.c_void_p), ("n", C.c_int64), ("dtype_p", C.c_int32), ("dtype_g", C.c_int32)]
+
+
 class Packed(NamedTuple):
     """Rows in 8 bits, as snn_pack gives them: codes int8 [..., n], exps uint8 [..., ceil(n / 32)]."""
     codes: object
@@ -55,8 +70,16 @@ def declare(L):
     L.snn_pack.argtypes = L.snn_unpack.argtypes = [at, C.c_int, i64, i32, i64] + [vp] * 3
     L.snn_vocab_loss.argtypes = [at, vocab] + [vp] * 5
     L.snn_vocab_loss_grad.argtypes = [at, vocab] + [vp] * 7
+    norm, adamw = C.POINTER(snn_norm), C.POINTER(snn_adamw)
+    L.snn_norm_workspace.argtypes = [norm]
+    L.snn_norm_workspace.restype = C.c_size_t
+    L.snn_norm_forward.argtypes = [at, norm] + [vp] * 5
+    L.snn_norm_forward_packed.argtypes = L.snn_norm_backward.argtypes = [at, norm] + [vp] * 6
+    L.snn_adamw_workspace.argtypes = [adamw]
+    L.snn_adamw_workspace.restype = C.c_size_t
+    L.snn_adamw_step.argtypes = [at, adamw, C.POINTER(snn_adamw_tensor), i64]
     for name in ("snn_glr_forward", "snn_glr_backward", "snn_glr_backward_packed", "snn_pack", "snn_unpack", "snn_vocab_loss",
-                 "snn_vocab_loss_grad"):
+                 "snn_vocab_loss_grad", "snn_norm_forward", "snn_norm_forward_packed", "snn_norm_backward", "snn_adamw_step"):
         getattr(L, name).restype = C.c_int
 
 
@@ -280,3 +303,158 @@ def snn_vocab_loss_grad(h, w, targets, state, dloss=None):
     dw = torch.empty((p.vocab, p.d), dtype=h.dtype, device=h.device)
     _run("snn_vocab_loss_grad", C.byref(at), C.byref(p), _at(h), _at(w), _at(targets), _at(state), _at(dloss), _at(dh), _at(dw))
     return dh, dw
+
+
+def _rows(x, name):
+    n = x.shape[-1] if x.dim() else 0
+    if n < 1:
+        raise ValueError(f"{name} must be rows of at least one element, got {tuple(x.shape)}")
+    return x.numel() // n, n
+
+
+def snn_norm_forward(x, w=None, residual=None, eps=1e-6, packed=False, y=None, total=None):
+    """y = w s / sqrt(mean(s^2) + eps) for rows s = x + residual (or x) [..., n]; w [n] (None: ones).
+
+    Returns y (packed: as Packed, in 8 bits) and s, which is what snn_norm_backward takes: x itself without a residual.  y and total: tensors
+    for the results; total may be x or residual itself, a sum that is updated in place."""
+    import torch
+    dtype, device, (rows, n) = _type(x, "x"), x.device, _rows(x, "x")
+    if w is not None:
+        _packed_rows(_same(w, "w", x.dtype, (n,), device), "w")
+    ld_r = ld_total = 0
+    if residual is None:
+        if total is not None:
+            raise ValueError("total without a residual: it would be x")
+    else:
+        ld_r = _ld(_same(residual, "residual", x.dtype, x.shape, device), "residual")
+        total = _out(total, "total", x)
+        ld_total = _ld(total, "total")
+    at, _ = _launch(device)
+    if packed:
+        if y is not None:
+            raise ValueError("y in 8 bits is a new Packed")
+        y = Packed(torch.empty(x.shape, dtype=torch.int8, device=device),
+                   torch.empty((*x.shape[:-1], -(-n // PACK_BLOCK)), dtype=torch.uint8, device=device))
+        to, ld_y = (_at(y.codes), _at(y.exps)), 0
+    else:
+        y = _out(y, "y", x)
+        to, ld_y = (_at(y),), _ld(y, "y")
+    p = snn_norm(rows, n, dtype, eps, _ld(x, "x"), ld_r, ld_total, ld_y, 0, 0)
+    _run("snn_norm_forward_packed" if packed else "snn_norm_forward", C.byref(at), C.byref(p), _at(x), _at(residual), _at(w), _at(total), *to)
+    return y, x if residual is None else total
+
+
+def snn_norm_backward(total, w, dy, dtotal=None, eps=1e-6, dx=None):
+    """Gradients of x (and of the residual: the same) and of w (None without one) from those of y and, if given, of s = total itself.
+    dx: a tensor for the result, which may be dy or dtotal itself."""
+    import torch
+    dtype, device, (rows, n) = _type(total, "total"), total.device, _rows(total, "total")
+    _same(dy, "dy", total.dtype, total.shape, device)
+    if w is not None:
+        _packed_rows(_same(w, "w", total.dtype, (n,), device), "w")
+    ld_dtotal = 0
+    if dtotal is not None:
+        ld_dtotal = _ld(_same(dtotal, "dtotal", total.dtype, total.shape, device), "dtotal")
+    dx = _out(dx, "dx", total)
+    dw = None if w is None else torch.empty((n,), dtype=total.dtype, device=device)
+    p = snn_norm(rows, n, dtype, eps, 0, 0, _ld(total, "total"), _ld(dy, "dy"), ld_dtotal, _ld(dx, "dx"))
+    at, space = _launch(device, _entry("snn_norm_workspace")(C.byref(p)) if w is not None else 0)
+    _run("snn_norm_backward", C.byref(at), C.byref(p), _at(total), _at(w), _at(dy), _at(dtotal), _at(dx), _at(dw))
+    return dx, dw
+
+
+class AdamwPlan:
+    """Tensors that snn_adamw_step moves, with their moments: params, m, v, copies as snn_adamw_plan was given them."""
+
+    def __init__(self, params, m, v, copies, tensors, device):
+        self.params, self.m, self.v, self.copies, self.tensors, self.device = params, m, v, copies, tensors, device
+
+
+def snn_adamw_moments(params, bits=32):
+    """m and v of tensors that have not been moved yet: zeros, float32 in their shapes, or (bits=8) Packed: codes in their shapes, an
+    exponent for 32 elements.  Each of the two is one array for all, of which the tensors' parts are views."""
+    import torch
+    if bits not in (8, 32):
+        raise ValueError(f"moments of 8 or 32 bits, not {bits}")
+    params = list(params)
+    counts = [p.numel() for p in params]
+    blocks = [-(-n // PACK_BLOCK) for n in counts]
+
+    def views(dtype, sizes):
+        whole = torch.zeros(sum(sizes), dtype=dtype, device=params[0].device if params else None)
+        return whole.split(sizes) if sizes else []
+
+    def moment():
+        values = views(torch.float32 if bits == 32 else torch.int8, [PACK_BLOCK * k for k in blocks])
+        values = [x[:n].view(p.shape) for x, n, p in zip(values, counts, params)]
+        return values if bits == 32 else [Packed(x, e) for x, e in zip(values, views(torch.uint8, blocks))]
+
+    return moment(), moment()
+
+
+def snn_adamw_plan(params, m, v, copies=None):
+    """What snn_adamw_step needs of its tensors, once for all steps: params (float32 or bfloat16, contiguous), their moments (snn_adamw_moments,
+    or tensors like those) and, if wanted, copies in bfloat16 of params in float32 (None in the list: no copy of that one).
+    The tensors are held, and changed in place by each step."""
+    import torch
+    params, m, v = list(params), list(m), list(v)
+    copies = [None] * len(params) if copies is None else list(copies)
+    if not len(params) == len(m) == len(v) == len(copies):
+        raise ValueError(f"{len(params)} params, {len(m)} m, {len(v)} v, {len(copies)} copies")
+    tensors = (snn_adamw_tensor * len(params))()
+    for i, (p, a, b, c, t) in enumerate(zip(params, m, v, copies, tensors)):
+        kind, device = _type(p, f"params[{i}]"), params[0].device
+        _packed_rows(_same(p, f"params[{i}]", p.dtype, p.shape, device), f"params[{i}]")
+        if isinstance(a, Packed) != isinstance(b, Packed):
+            raise TypeError(f"m[{i}] and v[{i}] must be tensors both, or Packed both")
+        for name, x in (("m", a), ("v", b)):
+            if isinstance(x, Packed):
+                if x.codes.numel() != p.numel():
+                    raise ValueError(f"the codes of {name}[{i}] must be as many as params[{i}] has elements")
+                _packed_rows(_same(x.codes, f"the codes of {name}[{i}]", torch.int8, x.codes.shape, device), f"the codes of {name}[{i}]")
+                _packed_rows(_same(x.exps, f"the exponents of {name}[{i}]", torch.uint8, (-(-p.numel() // PACK_BLOCK),), device),
+                             f"the exponents of {name}[{i}]")
+            else:
+                _packed_rows(_same(x, f"{name}[{i}]", torch.float32, p.shape, device), f"{name}[{i}]")
+        if isinstance(a, Packed):
+            t.m, t.m_exps, t.v, t.v_exps = _at(a.codes), _at(a.exps), _at(b.codes), _at(b.exps)
+        else:
+            t.m, t.v = _at(a), _at(b)
+        if c is not None:
+            if p.dtype != torch.float32:
+                raise TypeError(f"copies[{i}] is of params in {p.dtype}: only float32 has copies")
+            t.copy = _at(_packed_rows(_same(c, f"copies[{i}]", torch.bfloat16, p.shape, device), f"copies[{i}]"))
+        t.p, t.n, t.dtype_p = _at(p), p.numel(), kind
+    return AdamwPlan(params, m, v, copies, tensors, params[0].device if params else None)
+
+
+def snn_adamw_step(plan, grads, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None):
+    """One step of AdamW: params, moments and copies of the plan change in place.  grads: a gradient (float32 or bfloat16, contiguous) for each of
+    params.  step: 1, 2, ..., or an int32 tensor [1] on the device with the number of steps taken, which the call counts up (a step in a
+    graph).  grad_scale: float32 [1] that the gradients are multiplied by first."""
+    import torch
+    grads = list(grads)
+    if len(grads) != len(plan.params):
+        raise ValueError(f"{len(grads)} grads for {len(plan.params)} params")
+    if not grads:
+        return
+    device = plan.device
+    for i, (g, p, t) in enumerate(zip(grads, plan.params, plan.tensors)):
+        if g.dtype == torch.bfloat16:
+            t.dtype_g = SNN_BF16
+        elif g.dtype == torch.float32:
+            t.dtype_g = SNN_F32
+        else:
+            raise TypeError(f"grads[{i}] must be float32 or bfloat16, got {g.dtype}")
+        if g.shape != p.shape or g.device != device or not g.is_contiguous():
+            _packed_rows(_same(g, f"grads[{i}]", g.dtype, p.shape, device), f"grads[{i}]")
+        t.g = g.data_ptr()
+    how = snn_adamw(lr, betas[0], betas[1], eps, weight_decay, 0, None, None)
+    if isinstance(step, torch.Tensor):
+        how.step_on_device = _at(_same(step, "step", torch.int32, (1,), device))
+    else:
+        how.step = step
+    if grad_scale is not None:
+        how.grad_scale = _at(_same(grad_scale, "grad_scale", torch.float32, (1,), device))
+    at, space = _launch(device, _entry("snn_adamw_workspace")(C.byref(how)))
+    _run("snn_adamw_step", C.byref(at), C.byref(how), plan.tensors, len(grads))

@@ -1,0 +1,491 @@
+"""Norm, optimizer step and delta rule of token sequence models (snn_norm_*, snn_adamw_step, snn_delta_*) against plain implementations in 64 bits
+on the CPU, through the Python binding.  Refusals that need no GPU run everywhere.
+
+Tolerances count roundings: U = 2^-24 is what one in 32 bits is off by at most, relative to its result; results in bf16 are off by half
+a step, 2^-8 of the value, on top."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+import paper_2412_11810_amd as snn
+from paper_2412_11810_amd import ops
+
+torch = pytest.importorskip("torch")
+gpu = pytest.mark.gpu
+U = 2.0 ** -24
+HALF = {torch.float32: U, torch.bfloat16: 2.0 ** -8}
+TYPES = [torch.float32, torch.bfloat16]
+
+
+def near(got, want, tol, what):
+    """|got - want| <= tol + half a step of got's type, everywhere."""
+    got_, want = got.double().cpu(), want.double().cpu()
+    assert got_.shape == want.shape, what
+    off = (got_ - want).abs() - (tol + HALF[got.dtype] * want.abs())
+    assert not torch.isnan(off).any() and off.max().item() <= 0 if off.numel() else True, (what, off.max().item())
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def rows_of(shape, dtype, seed, wide=0, spread=0.5):
+    """Rows on the GPU, those of a wider array (NaN beside them) with `wide`."""
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(shape, generator=g) * torch.exp(spread * torch.randn(*shape[:-1], 1, generator=g))).to(dtype)
+    if wide:
+        w = torch.full((*shape[:-1], shape[-1] + wide), math.nan, dtype=dtype, device="cuda")
+        w[..., 1:shape[-1] + 1] = x.cuda()
+        return w[..., 1:shape[-1] + 1]
+    return x.cuda()
+
+
+# ---- norm ---------------------------------------------------------------------------------------
+NORM = [(1, 1), (3, 2), (5, 8), (70, 31), (64, 64), (9, 75), (1000, 128), (3, 500), (33, 513), (7, 1024), (5, 1501), (64, 2048), (3, 2049), (4, 4096),
+        (2, 8191), (3, 8200), (2, 16385), (1, 32768), (5000, 40), (2100, 1100)]
+ROUNDINGS = 64  # of a sum over a row: 32 elements in a lane, 6 exchanges, 16 wavefronts, and the square root, the quotient and three products
+
+
+def norm_plain(x, r, w, eps):
+    s = x.double().cpu() + (0 if r is None else r.double().cpu())
+    i = 1 / torch.sqrt((s * s).mean(-1, keepdim=True) + eps)
+    return s, i, s * i * (1 if w is None else w.double().cpu())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n", NORM)
+def test_norm_forward(rows, n, dtype):
+    x, r = rows_of((rows, n), dtype, 1, wide=n % 2 * 3), rows_of((rows, n), dtype, 2)
+    w = rows_of((1, n), dtype, 3)[0]
+    s, i, want = norm_plain(x, r, w, 1e-6)
+    y, total = snn.snn_norm_forward(x, w, residual=r, eps=1e-6)
+    near(total, s, U * s.abs(), "total")
+    near(y, want, ROUNDINGS * U * want.abs(), "y")
+    want = norm_plain(x, None, None, 0.25)[2]
+    y, total = snn.snn_norm_forward(x, eps=0.25)
+    assert total is x
+    near(y, want, ROUNDINGS * U * want.abs(), "y without residual and weights")
+    # in place, and into a part of a wider array
+    wide, stream = torch.full((rows, 2 * n), 7.0, dtype=dtype, device="cuda"), r.clone()
+    y2, total2 = snn.snn_norm_forward(x, w, residual=stream, eps=1e-6, y=wide[:, n:], total=stream)
+    assert total2 is stream
+    assert same([y2, total2], snn.snn_norm_forward(x, w, residual=r, eps=1e-6)) and (wide[:, :n] == 7).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n", NORM)
+def test_norm_forward_packed(rows, n, dtype):
+    x, r = rows_of((rows, n), dtype, 4, wide=n % 2), rows_of((rows, n), dtype, 5)
+    w = rows_of((1, n), dtype, 6)[0]
+    want = norm_plain(x, r, w, 1e-6)[2]
+    p, total = snn.snn_norm_forward(x, w, residual=r, eps=1e-6, packed=True)
+    assert same([total], snn.snn_norm_forward(x, w, residual=r, eps=1e-6)[1:])
+    blocks = torch.nn.functional.pad(want, (0, -n % 32)).unflatten(-1, (-1, 32))
+    off = ROUNDINGS * U
+    top, step = blocks.abs().amax(-1), torch.exp2(p.exps.cpu().double() - 127)
+    # the smallest step that fits, but for what the largest element may be off by
+    assert (top <= 127.5 * step * (1 + off)).all() and (top * (1 + off) > 127.5 * step / 2).all()
+    codes = torch.nn.functional.pad(p.codes.cpu().double(), (0, -n % 32)).unflatten(-1, (-1, 32))
+    assert ((codes * step[..., None] - blocks).abs() <= 0.5 * step[..., None] + off * blocks.abs()).all()
+    if dtype == torch.float32:  # y is not rounded before: its codes are those of snn_pack
+        assert same(p, snn.snn_pack(snn.snn_norm_forward(x, w, residual=r, eps=1e-6)[0]))
+
+
+def norm_back_plain(s, w, dy, ds, eps):
+    s, dy = s.double().cpu(), dy.double().cpu()
+    mine = dy if w is None else dy * w.double().cpu()
+    i = 1 / torch.sqrt((s * s).mean(-1, keepdim=True) + eps)
+    hat = s * i
+    dx = i * (mine - hat * (mine * hat).mean(-1, keepdim=True)) + (0 if ds is None else ds.double().cpu())
+    size = i * (mine.abs() + hat.abs() * (mine * hat).abs().mean(-1, keepdim=True))
+    return dx, size, (dy * hat).sum(0), (dy * hat).abs().sum(0)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n", NORM)
+def test_norm_backward(rows, n, dtype):
+    s, dy, ds = rows_of((rows, n), dtype, 7), rows_of((rows, n), dtype, 8, wide=n % 2 * 2), rows_of((rows, n), dtype, 9)
+    w = rows_of((1, n), dtype, 10)[0]
+    dx, size, dw, terms = norm_back_plain(s, w, dy, ds, 1e-6)
+    got, got_w = snn.snn_norm_backward(s, w, dy, dtotal=ds, eps=1e-6)
+    near(got, dx, 3 * ROUNDINGS * U * size + U * ds.double().cpu().abs(), "dx")
+    # a sum over rows: those of a lane one after the other (1024 workgroups take turns), then up to 1024 in 32 strands
+    near(got_w, dw, (ROUNDINGS + rows / 1024 + 80) * U * terms, "dw")
+    free, none = snn.snn_norm_backward(s, None, dy, eps=1e-6)
+    plain = norm_back_plain(s, None, dy, None, 1e-6)
+    assert none is None
+    near(free, plain[0], 3 * ROUNDINGS * U * plain[1], "dx without weights")
+    place = dy.clone()
+    assert same(snn.snn_norm_backward(s, w, place, dtotal=ds, eps=1e-6, dx=place), [got, got_w])
+    place = ds.clone()
+    assert same(snn.snn_norm_backward(s, w, dy, dtotal=place, eps=1e-6, dx=place), [got, got_w])
+
+
+@gpu
+def test_norm_gradients_are_differences():
+    s, dy, w = (rows_of(x, torch.float32, k) for k, x in enumerate(((5, 33), (5, 33), (1, 33))))
+    dx, dw = snn.snn_norm_backward(s, w[0], dy, eps=1e-3)
+    f = lambda a, b: (norm_plain(a, None, b, 1e-3)[2] * dy.double().cpu()).sum()  # noqa: E731
+    d, S, W = 1e-6, s.double().cpu(), w[0].double().cpu()
+    for r, c in ((0, 0), (2, 17), (4, 32)):
+        e = torch.zeros_like(S)
+        e[r, c] = d
+        # (a third derivative of size 30 d^2, and 1e-16 of f over d)
+        assert abs((f(S + e, W) - f(S - e, W)) / (2 * d) - dx[r, c].item()) < 1e-5 * max(1, dx.abs().max().item())
+        assert abs((f(S, W + e[r]) - f(S, W - e[r])) / (2 * d) - dw[c].item()) < 1e-5 * max(1, dw.abs().max().item())
+
+
+@gpu
+@pytest.mark.parametrize("n", [40, 600, 3000, 9000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_of_numbers_of_any_size(n, dtype):
+    x = rows_of((8, n), dtype, 11, spread=0)
+    scale = torch.tensor([1e36, 1e30, 1e25, 1.0, 1e-18, 1e-25, 1e-36, 0.0], device="cuda")[:, None]
+    x = (x.float() * scale).to(dtype)
+    w, dy = rows_of((1, n), dtype, 12)[0], rows_of((8, n), dtype, 13)
+    for eps in (0.0, 1e-6):
+        live = slice(0, 7) if eps == 0 else slice(0, 8)  # (0 / 0 is NaN)
+        y = snn.snn_norm_forward(x, w, eps=eps)[0]
+        want = norm_plain(x, None, w, eps)[2]
+        near(y[live], want[live], ROUNDINGS * U * want[live].abs() + 2.0 ** -133, "y")
+        got = snn.snn_norm_backward(x[live], w, dy[live], eps=eps)
+        dx, size, dw, terms = norm_back_plain(x[live], w, dy[live], None, eps)
+        fits = size.amax(1) < 1e37  # a row of 1e-36 has gradients of 1e36
+        near(got[0][fits.cuda()], dx[fits], (3 * ROUNDINGS * U * size + 2.0 ** -133)[fits], "dx")
+        near(got[1], dw, (ROUNDINGS + 80) * U * terms + 2.0 ** -133, "dw")
+        if eps == 0:
+            assert torch.isnan(y[7]).all()
+
+
+@gpu
+def test_norm_values_that_are_not_finite_stay_in_their_rows():
+    x = rows_of((6, 100), torch.float32, 14)
+    clean, w = x.clone(), torch.ones(100, device="cuda")
+    x[1, 3], x[4, 99] = math.inf, math.nan
+    y, p = snn.snn_norm_forward(x, w)[0], snn.snn_norm_forward(x, w, packed=True)[0]
+    want = snn.snn_norm_forward(clean, w)[0]
+    rest = [0, 2, 3, 5]
+    assert torch.equal(y[rest], want[rest]) and torch.isnan(y[4]).all() and torch.isnan(y[1, 3]) and (y[1, :3] == 0).all()
+    assert same([p.codes[rest], p.exps[rest]], [z[rest] for z in snn.snn_pack(want)])
+    assert (p.exps[4] == 255).all() and p.exps[1].tolist() == [255, 0, 0, 0]
+
+
+@gpu
+def test_norm_of_no_rows():
+    x, w = torch.zeros((0, 70), device="cuda"), torch.ones(70, device="cuda")
+    assert snn.snn_norm_forward(x, w, residual=x)[0].shape == (0, 70) and snn.snn_norm_forward(x, w, packed=True)[0].exps.shape == (0, 3)
+    dx, dw = snn.snn_norm_backward(x, w, x)
+    assert dx.shape == (0, 70) and (dw == 0).all()
+
+
+@gpu
+def test_norm_beyond_4_gb():
+    rows, n = 70000, 32768  # 4.6 GB in bf16
+    x = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(3))
+    y, total = snn.snn_norm_forward(x, None, residual=x)
+    at = slice(rows - 3, rows)
+    want = norm_plain(x[at], x[at], None, 1e-6)
+    near(y[at], want[2], ROUNDINGS * U * want[2].abs(), "y")
+    assert torch.equal(total, 2 * x)
+
+
+# ---- AdamW --------------------------------------------------------------------------------------
+C1, C2 = 0xC13FA9A9, 0x91E10DA5
+
+
+def adamw_plain(p, g, m, v, t, lr, betas, eps, decay):
+    """New p, m, v, and what they may be off by in 32 bits."""
+    a, b = betas
+    m1, v1 = a * m + (1 - a) * g, b * v + (1 - b) * g * g
+    em, ev = 4 * U * (a * m.abs() + (1 - a) * g.abs()), 5 * U * v1
+    root = torch.sqrt(v1 / (1 - b ** t)) + eps
+    move = lr * m1 / (1 - a ** t) / root
+    p1 = p * (1 - lr * decay) - move
+    # half of v's error, six factors and quotients
+    return p1, m1, v1, 2 * U * p.abs() + lr * em / (1 - a ** t) / root + 10 * U * move.abs(), em, ev
+
+
+def values(p):
+    return p.codes.cpu().double().flatten() * torch.exp2(p.exps.cpu().double() - 127).repeat_interleave(32)[:p.codes.numel()]
+
+
+def check_codes(p, want, tol, t, c1, c2, root):
+    """The codes of a moment in 8 bits: floor(x / step + u) of an x within tol of `want`."""
+    n = len(want)
+    pad = lambda x: torch.nn.functional.pad(x, (0, -n % 32)).view(-1, 32)  # noqa: E731
+    step = torch.exp2(p.exps.cpu().double() - 127)[:, None]
+    x, e, codes = pad(want), pad(tol), pad(p.codes.cpu().double().flatten())
+    top = x.abs().amax(1)
+    assert ((top - e.amax(1)) <= 127 * step[:, 0]).all()
+    assert ((top + e.amax(1) > 63.5 * step[:, 0]) | (p.exps.cpu() <= 1)).all()
+    assert ((p.exps.cpu() == 0) == (top == 0)).all()
+    i = torch.arange(x.numel()).view(x.shape)
+    u = (((i * c1 + t * c2) % 2 ** 32) // 2 ** 16).double() / 2 ** 16
+    at = x / step + u
+    lowest = torch.where(x > 0, 1.0, -127.0) if root else torch.full_like(x, -127.0)
+    assert (codes <= torch.maximum(at + e / step + 2.0 ** -16, lowest)).all() and (codes >= lowest).all()  # (x / step + u has 24 bits)
+    assert (codes > at - 1 - e / step - 2.0 ** -16).all()
+
+
+SHAPES = [(1,), (7, 5), (32,), (33,), (0,), (4, 64), (8192,), (8193,), (5, 3001), (1025, 64)]
+
+
+def adamw_inputs(shapes, bits, kinds, seed=1):
+    g = torch.Generator().manual_seed(seed)
+    params = [(0.1 * torch.randn(x, generator=g)).to(k).cuda() for x, (k, _) in zip(shapes, kinds)]
+    grads = [(0.01 * torch.exp(2 * torch.randn((), generator=g)) * torch.randn(x, generator=g)).to(k).cuda() for x, (_, k) in zip(shapes, kinds)]
+    copies = [torch.full(p.shape, 7.0, dtype=torch.bfloat16, device="cuda") if p.dtype == torch.float32 and i % 3 else None for i, p in enumerate(params)]
+    return params, grads, copies, *snn.snn_adamw_moments(params, bits)
+
+
+@gpu
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("many", [False, True])
+def test_adamw_steps(bits, many):
+    shapes = SHAPES * (9 if many else 1)  # more tensors than a launch takes
+    kinds = [(TYPES[i % 2], TYPES[i // 2 % 2]) for i in range(len(shapes))]
+    params, grads, copies, m, v = adamw_inputs(shapes, bits, kinds)
+    plan = snn.snn_adamw_plan(params, m, v, copies)
+    how = dict(lr=3e-3, betas=(0.85, 0.98), eps=1e-7, weight_decay=0.2)
+    for t in (1, 2, 3, 50, 1000003):
+        flat = lambda x: values(x) if bits == 8 else x.cpu().double().flatten()  # noqa: E731
+        before = [(p.cpu().double().flatten(), g.cpu().double().flatten(), flat(a), flat(b) ** (2 if bits == 8 else 1)) for p, g, a, b in zip(params, grads, m, v)]
+        snn.snn_adamw_step(plan, grads, t, **how)
+        for k, (x, p, a, b, c) in enumerate(zip(before, params, m, v, copies)):
+            p1, m1, v1, ep, em, ev = adamw_plain(*x, t, how["lr"], how["betas"], how["eps"], how["weight_decay"])
+            near(p.flatten(), p1, ep, ("p", k, t))
+            if c is not None:
+                assert torch.equal(c, p.to(torch.bfloat16))
+            if not len(p1):
+                continue
+            if bits == 32:
+                near(a.flatten(), m1, em, ("m", k, t))
+                near(b.flatten(), v1, ev, ("v", k, t))
+            else:
+                check_codes(a, m1, em, t, C1, C2, False)
+                root = torch.sqrt(v1)
+                check_codes(b, root, 4 * U * root, t, C2, C1, True)
+        grads = [g * 0.5 for g in grads]
+
+
+@gpu
+def test_adamw_in_8_bits_follows_moments_that_change_little_at_a_time():
+    # gradients that stop: a root changes by 1/2000 of itself at a time, a twentieth of a code at most
+    params = [torch.zeros(4096, device="cuda")]
+    m, v = snn.snn_adamw_moments(params, 8)
+    plan, g = snn.snn_adamw_plan(params, m, v), torch.linspace(0.5, 1.0, 4096, device="cuda")
+    for t in range(1, 101):
+        snn.snn_adamw_step(plan, [g], t)
+    for t in range(101, 1101):
+        snn.snn_adamw_step(plan, [0 * g], t)
+    want = g.double().cpu() * math.sqrt(1 - 0.999 ** 100) * 0.999 ** 500
+    step = torch.exp2(v[0].exps.cpu().double() - 127).repeat_interleave(32)
+    # a sum of N errors floor(x + u) - x over multiples of an irrational number grows with the logarithm of N: 3 + log2 N is more than any
+    assert ((values(v[0]) - want).abs() <= (3 + math.log2(1100)) * step).all()
+    # and cancels over the elements: their mean is off by a part of a step
+    assert abs((values(v[0]) - want).mean().item()) <= 0.25 * step.max().item()
+
+
+@gpu
+def test_adamw_first_steps_of_elements_of_very_different_sizes():
+    # a root that has no code of its own has the smallest: its element moves less than in 32 bits, never more
+    g = torch.full((64,), 1e-6, device="cuda")
+    g[::32] = 1.0
+    params = [torch.zeros(64, device="cuda")]
+    plan = snn.snn_adamw_plan(params, *snn.snn_adamw_moments(params, 8))
+    for t in range(1, 20):
+        before = params[0].clone()
+        snn.snn_adamw_step(plan, [g], t, lr=1.0, weight_decay=0.0)
+        # its m is at most rounded up to a step, 1 / 63.5 of the block's largest, its root 1 / 127 of that one's at least: a quotient of 2 and its
+        # own 1e-6; the largest element's is 1
+        assert ((params[0] - before).abs() <= 2.1).all()
+    assert (plan.v[0].codes > 0).all()
+
+
+@gpu
+def test_adamw_scale_of_gradients_and_step_on_the_device():
+    kinds = [(torch.float32, torch.bfloat16)] * len(SHAPES)
+    both = [adamw_inputs(SHAPES, 8, kinds) for _ in range(2)]
+    plans = [snn.snn_adamw_plan(x[0], x[3], x[4], x[2]) for x in both]
+    step, scale = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.full((1,), 0.25, device="cuda")
+    for t in (1, 2, 3):
+        snn.snn_adamw_step(plans[0], both[0][1], t)
+        snn.snn_adamw_step(plans[1], [g * 4 for g in both[1][1]], step, grad_scale=scale)
+        assert step.item() == t
+    for a, b in zip(both[0][0] + both[0][2], both[1][0] + both[1][2]):
+        # (the device's pow() and the host's may differ in their last bit of 64)
+        assert a is None or torch.allclose(a.float(), b.float(), rtol=4 * U if a.dtype == torch.float32 else 2.0 ** -7, atol=1e-9)
+
+
+@gpu
+def test_adamw_in_a_graph():
+    kinds = [(torch.float32, torch.float32)] * len(SHAPES)
+    (params, grads, copies, m, v), (other, _, _, om, ov) = (adamw_inputs(SHAPES, 32, kinds) for _ in range(2))
+    plan, eager = snn.snn_adamw_plan(params, m, v, copies), snn.snn_adamw_plan(other, om, ov)
+    step, eager_step = (torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        snn.snn_adamw_step(plan, grads, step)
+    for t in range(1, 5):
+        for g in grads:
+            g.mul_(0.9)
+        graph.replay()
+        torch.cuda.synchronize()
+        snn.snn_adamw_step(eager, grads, eager_step)
+        assert step.item() == t and same(params, other) and same(m, om) and same(v, ov)
+
+
+@gpu
+def test_adamw_of_more_elements_than_32_bits_count():
+    n = 2 ** 32 + 100
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 2 ** 31 - 1, 2 ** 31, 2 ** 32 - 1, 2 ** 32, n - 1], device="cuda")
+    g[at] = torch.arange(1, 7, device="cuda").to(torch.bfloat16)
+    m, v = snn.snn_adamw_moments([p], 8)
+    snn.snn_adamw_step(snn.snn_adamw_plan([p], m, v), [g], 1, lr=0.5, weight_decay=0.0)
+    assert (p[at] == -0.5).all() and p.count_nonzero().item() == 6
+    assert (v[0].codes[at] > 0).all() and v[0].codes.count_nonzero().item() == 6
+
+
+@gpu
+def test_adamw_refuses_arrays_that_share_elements():
+    x = torch.zeros(200, device="cuda")
+    m, v = snn.snn_adamw_moments([x, x])
+    g = [torch.ones(200, device="cuda")] * 2
+    for params, grads, moments in (([x, x], g, (m, v)), ([x[:100], x[99:199]], [g[0][:100]] * 2, ([y[:100] for y in m], [y[:100] for y in v])),
+                                   ([x], [x], (m[:1], v[:1])), ([x], g[:1], (m[:1], m[:1])), ([x], [m[0]], (m[:1], v[:1]))):
+        with pytest.raises(snn.SnnError) as e:
+            snn.snn_adamw_step(snn.snn_adamw_plan(params, *moments), grads, 1)
+        assert e.value.status == snn.SNN_E_INVAL and "shares" in str(e.value) or "share" in str(e.value)
+    assert (x == 0).all()
+    y = torch.zeros(100, device="cuda")
+    snn.snn_adamw_step(snn.snn_adamw_plan([x[:100], y], *snn.snn_adamw_moments([y, y])), [g[0][:100]] * 2, 1)  # one gradient for two is none
+
+
+@gpu
+def test_adamw_gradients_that_are_not_finite():
+    p = [torch.zeros(96, device="cuda")]
+    m, v = snn.snn_adamw_moments(p, 8)
+    g = torch.ones(96, device="cuda")
+    g[40] = math.nan
+    snn.snn_adamw_step(snn.snn_adamw_plan(p, m, v), [g], 1)
+    assert m[0].exps.tolist()[1] == v[0].exps.tolist()[1] == 255 and torch.isnan(p[0]).nonzero().tolist() == [[40]]
+    assert torch.isfinite(values(m[0])[:32]).all() and torch.isfinite(values(m[0])[64:]).all()
+
+
+@gpu
+def test_adamw_moves_the_weights_of_a_network():
+    import synth
+    w = synth.config(0)
+    d = synth.generate(w)
+    net = snn.from_workload(w, d, device=0)
+    kinds = [(snn.SNN_W_IN, 0), (snn.SNN_W_REC, 0), (snn.SNN_W_OUT, 0)]
+    params = [torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).cuda() for x in (d["W_in"][0], d["W_rec"][0], d["W_out"])]
+    plan = snn.snn_adamw_plan(params, *snn.snn_adamw_moments(params))
+    net.snn_bind_inputs(d["in_spikes"], d["labels"], w.T)
+    for t in (1, 2):
+        net.snn_bptt(snn.SNN_CHUNK, 0, 16)
+        grads = [net.snn_grads(*k) for k in kinds]
+        before = [p.cpu().double() for p in params]
+        moments = [(a.cpu().double(), b.cpu().double()) for a, b in zip(plan.m, plan.v)]
+        snn.snn_adamw_step(plan, [torch.from_numpy(g).cuda() for g in grads], t, lr=1e-4)
+        for p, x, g, (a, b), k in zip(params, before, grads, moments, kinds):
+            want = adamw_plain(x, torch.from_numpy(g).double(), a, b, t, 1e-4, (0.9, 0.999), 1e-8, 0.01)
+            near(p, want[0], want[3], "weights")
+            net.snn_set_weights(*k, p)
+    net.snn_bptt(snn.SNN_CHUNK, 0, 16)
+    assert not np.array_equal(net.snn_grads(*kinds[0]), grads[0])
+    net.snn_destroy()
+
+
+# ---- refusals -----------------------------------------------------------------------------------
+def refused(call, text):
+    with pytest.raises(snn.SnnError) as e:
+        call()
+    assert e.value.status == snn.SNN_E_INVAL and text in str(e.value), str(e.value)
+
+
+def test_c_entry_points_of_norm_and_adamw_refuse_what_they_cannot_run():
+    L, at = snn.lib(), ops.snn_launch(0, None, None, 0)
+    here = C.cast(C.create_string_buffer(4096), C.c_void_p).value
+
+    def norm(**k):
+        return C.byref(ops.snn_norm(**{**dict(rows=4, n=8, dtype=0, eps=1e-6), **k}))
+
+    for name, count in (("snn_norm_forward", 5), ("snn_norm_forward_packed", 6), ("snn_norm_backward", 6)):
+        def call(p, launch=C.byref(at), first=here):
+            ops._run(name, launch, p, first, *[here] * (count - 1))
+        refused(lambda: call(norm(), None), "no device")
+        refused(lambda: call(None), "no shape")
+        refused(lambda: call(norm(dtype=2)), "unknown type 2")
+        for bad in (dict(n=0), dict(n=32769), dict(rows=-1), dict(rows=1 << 40)):
+            refused(lambda: call(norm(**bad)), "2^15")
+        for bad in (-1.0, math.nan, math.inf):
+            refused(lambda: call(norm(eps=bad)), "eps")
+        refused(lambda: call(norm(ld_dx=7)), "7 elements")
+        refused(lambda: call(norm(), first=None), "is NULL")
+        refused(lambda: call(norm(), first=here + 2), "not aligned")
+        refused(lambda: call(norm()), "not in")
+    assert L.snn_norm_workspace(norm(n=0)) == 0 and L.snn_norm_workspace(norm()) > 0
+
+    def adamw(**k):
+        return C.byref(ops.snn_adamw(**{**dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.1, step=1), **k}))
+
+    def step(how, launch=C.byref(at), count=1, **k):
+        t = ops.snn_adamw_tensor(**{**dict(p=here, g=here, m=here, v=here, n=8), **k})
+        ops._run("snn_adamw_step", launch, how, C.byref(t), count)
+
+    refused(lambda: step(adamw(), None), "no device")
+    refused(lambda: step(None), "no step")
+    refused(lambda: step(adamw(), count=-1), "no tensors")
+    for bad in (dict(lr=math.nan), dict(beta1=1.0), dict(beta2=-0.1), dict(eps=-1.0), dict(weight_decay=math.inf)):
+        refused(lambda: step(adamw(**bad)), "betas")
+    refused(lambda: step(adamw(step=0)), "the first one is 1")
+    refused(lambda: step(adamw(), n=-1), "-1 elements")
+    refused(lambda: step(adamw(), dtype_g=3), "unknown type")
+    refused(lambda: step(adamw(), m_exps=here), "one without")
+    refused(lambda: step(adamw(), copy=here, dtype_p=1), "copy")
+    refused(lambda: step(adamw(), p=None), "p is NULL")
+    refused(lambda: step(adamw()), "not in")
+    assert L.snn_adamw_workspace(adamw()) == 0 < L.snn_adamw_workspace(adamw(step_on_device=here))
+
+
+def test_binding_of_norm_and_adamw_refuses_tensors_that_do_not_fit():
+    f, b = torch.zeros, torch.bfloat16
+    m, v = snn.snn_adamw_moments([f(40)], 8)
+    assert m[0].codes.shape == (40,) and v[0].exps.shape == (2,) and [x.shape for x in snn.snn_adamw_moments([f(3, 5)])[0]] == [(3, 5)]
+    plan = snn.snn_adamw_plan([f(40)], m, v)
+    for call, kind in (
+            (lambda: snn.snn_norm_forward(f(4, 8)), ValueError),                                # on the CPU
+            (lambda: snn.snn_norm_forward(f(())), ValueError),
+            (lambda: snn.snn_norm_forward(f(4, 8, dtype=torch.float16)), TypeError),
+            (lambda: snn.snn_norm_forward(f(4, 8), f(8, dtype=b)), TypeError),
+            (lambda: snn.snn_norm_forward(f(4, 8), f(7)), ValueError),
+            (lambda: snn.snn_norm_forward(f(4, 8), residual=f(4, 7)), ValueError),
+            (lambda: snn.snn_norm_forward(f(4, 8), residual=f(8, 4).T), ValueError),
+            (lambda: snn.snn_norm_forward(f(4, 8), total=f(4, 8)), ValueError),
+            (lambda: snn.snn_norm_backward(f(4, 8), f(8), f(4, 9)), ValueError),
+            (lambda: snn.snn_norm_backward(f(4, 8), f(8), f(4, 8), dtotal=f(4, 8, dtype=b)), TypeError),
+            (lambda: snn.snn_adamw_moments([f(4)], 16), ValueError),
+            (lambda: snn.snn_adamw_plan([f(4)], [f(4)], []), ValueError),
+            (lambda: snn.snn_adamw_plan([f(4)], [f(5)], [f(4)]), ValueError),
+            (lambda: snn.snn_adamw_plan([f(4)], [f(4, dtype=b)], [f(4)]), TypeError),
+            (lambda: snn.snn_adamw_plan([f(40)], m, [f(40)]), TypeError),
+            (lambda: snn.snn_adamw_plan([f(41)], m, v), ValueError),
+            (lambda: snn.snn_adamw_plan([f(40)], [snn.Packed(m[0].codes, f(1, dtype=torch.uint8))], v), ValueError),
+            (lambda: snn.snn_adamw_plan([f(4, dtype=b)], [f(4)], [f(4)], [f(4, dtype=b)]), TypeError),
+            (lambda: snn.snn_adamw_plan([f(4, 4).T[:2]], [f(2, 4)], [f(2, 4)]), ValueError),
+            (lambda: snn.snn_adamw_step(plan, [], 1), ValueError),
+            (lambda: snn.snn_adamw_step(plan, [f(40, dtype=torch.float64)], 1), TypeError),
+            (lambda: snn.snn_adamw_step(plan, [f(39)], 1), ValueError),
+            (lambda: snn.snn_adamw_step(plan, [f(80)[::2]], 1), ValueError),
+            (lambda: snn.snn_adamw_step(plan, [f(40)], f(1)), TypeError),
+            (lambda: snn.snn_adamw_step(plan, [f(40)], 1), ValueError)):                        # on the CPU
+        with pytest.raises(kind):
+            call()
