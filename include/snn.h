@@ -375,6 +375,39 @@ snn_status snn_vocab_loss(const snn_launch *at, const snn_vocab *p, const void *
 snn_status snn_vocab_loss_grad(const snn_launch *at, const snn_vocab *p, const void *h, const void *w, const int32_t *targets,
                                const float *state, const float *dloss, void *dh, void *dw);
 
+/* Gated delta rule over time-major sequences [T][batch][heads], each head with a state S [dk][dv] of its own:
+ *   S_t = a_t S_{t-1} + k_t u_t^T ,  u_t = beta_t (v_t - a_t S_{t-1}^T k_t) ,  o_t = scale S_t^T q_t ,  a_t = exp(g_t) ,  t = 1..T
+ * (k_t reads what the state holds for it, and beta_t of the difference to v_t is written in its place.)  Keys are taken as they are: with |k| = 1 and
+ * beta 0..1 the state stays bounded; g <= 0 as a rule, minus infinity forgets all (as -10^4 does).  Computed in fp32; products of bf16 arrays with
+ * what is computed on the way keep 16 bits of the latter, those of fp32 arrays 24.  A state or value that is not finite gives nothing
+ * finite in its head from its chunk of 64 steps on. */
+typedef struct {
+  int32_t T, batch;          /* T >= 0 (0: s_last = s0), at most 2^30 */
+  int32_t heads, key_heads;  /* heads a multiple of key_heads: head h has the queries and keys of h / (heads / key_heads).  batch * heads 2^20 at most */
+  int32_t dk, dv;            /* 1..128, 1..1024; batch * heads * dv 2^28 at most */
+  int32_t dtype;             /* snn_dtype of q, k, v, o and their gradients; gates and states are fp32 */
+  float scale;               /* of the queries, 1 / sqrt(dk) say */
+  int64_t ld_q, ld_k, ld_v, ld_o;  /* elements between consecutive rows (t, b), each of all heads one after the other (0: packed; at most 2^30); ld_o: of o and do.
+                                      q, k and v may be parts of one projection */
+  int64_t ld_dq, ld_dk, ld_dv;
+  const int32_t *lengths;    /* [batch] or NULL (T each): sequence b has steps 1..lengths[b]; a number outside 0..T counts as the nearer end.  What
+                                later steps hold does not matter; o and all gradients are zeros there */
+} snn_delta;
+
+/* Bytes of workspace for snn_delta_forward (gradients = 0; none for up to 16 steps) or snn_delta_backward; 0 for an invalid shape too.  Half a GB or what
+ * four chunks of 64 steps need, whichever is more, however long the sequences are. */
+size_t snn_delta_workspace(const snn_delta *p, int32_t gradients);
+
+/* q, k [T][batch][key_heads][dk], v, o [T][batch][heads][dv], g, beta [T][batch][heads] fp32; s0 [batch][heads][dk][dv] fp32 or NULL (zeros); s_last of the same
+ * shape or NULL, may be s0 itself (serving: T = 1, state in and out); kept [ceil(T / 256)][batch][heads][dk][dv] fp32 or NULL: the states before the
+ * steps 1, 257, 513, ..., which the backward pass recomputes the others from. */
+snn_status snn_delta_forward(const snn_launch *at, const snn_delta *p, const void *q, const void *k, const void *v, const float *g, const float *beta,
+                             const float *s0, void *o, float *s_last, float *kept);
+
+/* Gradients of q, k, v, g, beta and s0 from those of o and, where ds_last is not NULL, of s_last.  ds0 may be NULL; it may be ds_last itself. */
+snn_status snn_delta_backward(const snn_launch *at, const snn_delta *p, const void *q, const void *k, const void *v, const float *g, const float *beta,
+                              const float *kept, const void *dout, const float *ds_last, void *dq, void *dk, void *dv, float *dg, float *dbeta, float *ds0);
+
 /* Root-mean-square norm of rows, of the sum with what went past the layers before it:
  *   s = x + residual (or x) ;  y = w s / sqrt(mean(s^2) + eps)
  * Computed in fp32 from the sum before it is rounded to dtype.  Rows may hold numbers of any size.  A row with an infinity or NaN gives what the

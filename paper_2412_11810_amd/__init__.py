@@ -12,8 +12,8 @@ import os
 import numpy as np
 
 from . import ops
-from .ops import (Packed, snn_adamw_moments, snn_adamw_plan, snn_adamw_step, snn_glr_backward, snn_glr_forward,  # noqa: F401
-                  snn_norm_backward, snn_norm_forward, snn_pack, snn_unpack, snn_vocab_loss, snn_vocab_loss_grad)
+from .ops import (Packed, snn_adamw_moments, snn_adamw_plan, snn_adamw_step, snn_delta_backward,  # noqa: F401
+                  snn_delta_forward, snn_glr_backward, snn_glr_forward, snn_norm_backward, snn_norm_forward, snn_pack, snn_unpack, snn_vocab_loss, snn_vocab_loss_grad)
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsnn_mi355x.so")
@@ -32,7 +32,8 @@ EXPORTS = ["snn_init", "snn_set_weights", "snn_forward", "snn_bptt", "snn_bind_i
            "snn_suggest_intervals", "snn_debug_currents", "snn_get_state", "snn_forward_noalloc", "snn_launch_error",
            "snn_glr_workspace", "snn_glr_forward", "snn_glr_backward", "snn_glr_backward_packed", "snn_pack", "snn_unpack",
            "snn_vocab_workspace", "snn_vocab_loss", "snn_vocab_loss_grad", "snn_norm_workspace", "snn_norm_forward",
-           "snn_norm_forward_packed", "snn_norm_backward", "snn_adamw_workspace", "snn_adamw_step"]
+           "snn_norm_forward_packed", "snn_norm_backward", "snn_adamw_workspace", "snn_adamw_step",
+           "snn_delta_workspace", "snn_delta_forward", "snn_delta_backward"]
 
 
 class snn_config(C.Structure):

@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsnn_mi355x.so")
 SOURCES = ["snn_kernels.hip", "snn_api.cpp", "snn_schedule.cpp", "snn_ops.cpp", "snn_glr.hip", "snn_pack.hip",
-           "snn_vocab.hip", "snn_norm.hip", "snn_adamw.hip"]
+           "snn_vocab.hip", "snn_norm.hip", "snn_adamw.hip", "snn_delta.hip"]
 
 # -ffp-contract=off: the forward/recompute arithmetic must not fuse multiply-adds (bit-exact spike
 # trains); packed fp32 instructions are disabled for the whole library.

@@ -1,0 +1,1052 @@
+// Gated delta rule over [T][batch][heads]: a state S [dk][dv] per head, read and corrected by each step.
+//
+//   S_t = a_t S_{t-1} + k_t u_t^T,  u_t = beta_t (v_t - a_t S_{t-1}^T k_t),  o_t = scale S_t^T q_t,  a_t = exp(g_t)
+//
+// 64 steps are taken at once.  With G the sum of g from the chunk's first step on, gam = exp(G), D_tj = exp(G_t - G_j) for j <= t, S the state before
+// the chunk and L' = (K K^T D) strictly below the diagonal, its steps are
+//   E = V - gam K S,  w = A E with A = (1 + L' diag(beta))^-1,  u = beta w,  O = scale gam Q S + P u with P = scale Q K^T D,
+//   S' = gam_end S + K^T (gam_end / gam u)
+// and back, from dO and the gradient dS' of S':
+//   dU = P^T dO + gam_end / gam K dS',  dV = dE = A^T (beta dU),  dS = gam_end dS' + Q^T (scale gam dO) - K^T (gam dE)
+//   dP = (dO u^T) D scale,  M = -(dE u^T) D below the diagonal
+//   dQ = scale gam dO S^T + dP K,  dK = gam_end / gam u dS'^T - gam dE S^T + dP^T Q + (M + M^T) K
+//   dbeta_j = w_j . dU_j - sum_t L'_tj dE_t . w_j
+//   dg_t = gam_end <S, dS'> + sum_{j<t} k_j . (of dK_j the first part) + sum_{i>=t} (q_i, k_i . the parts of dQ_i, dK_i from S) + sum_{i>=t>j} Z_ij,
+//   Z = Q K^T dP + K K^T M: what was written before a decay and read after it.  (Sums of what belongs to a decay: nothing large is taken away again.)
+//
+// G and its differences are of 64 bits: behind a decay that forgets everything the next steps' ratios keep their digits.  A is found by substitution in
+// blocks of 16, in 32 bits, and by products of blocks, so that equal keys do no harm.
+// States and sums are of 32 bits.  Products go through the bf16 matrix cores: arrays of bf16 as they are, what is computed on the way (S, E, u, dU, dE, A, P) in two
+// bf16 parts, which leaves 16 bits of each factor (off by 2^-17 of itself at most; 3 products of parts, or 2 beside an operand that is bf16); with
+// arrays of 32 bits everything goes in three parts and six products, which keep 24.
+//
+// Four kernels: what is of a chunk alone (k_chunk: A, P, and the operands in the order in which a wavefront loads them); the walk over the chunks
+// with S in registers, its columns dealt to workgroups (k_walk; for the backward pass it starts at each kept state, every 4 chunks); the walk back
+// with dS (k_walk_back); and what needs S, dS', w and dE of a chunk (k_grads).  They go through the sequence in pieces whose intermediate arrays fit the caches
+// or nearly so.  Few steps are taken one after the other, by a kernel whose workgroup holds the whole state of a head (k_steps).
+#include "snn_rows.h"
+
+namespace {
+
+typedef __bf16 frag __attribute__((ext_vector_type(8)));
+typedef __bf16 four __attribute__((ext_vector_type(4)));
+typedef float tile __attribute__((ext_vector_type(4)));
+
+constexpr int C = 64;      // steps of a chunk
+constexpr int KEPT = SNN_DELTA_INTERVAL / C;
+constexpr int LINE = C + 8;  // elements from row to row in LDS: 16 lanes read 16 bytes of as many rows from all 64 banks
+constexpr int FLINE = C + 4; // the same of floats
+constexpr float LOG2E = 1.44269504f;
+
+template <class T> constexpr int GIVEN = sizeof(T) == 2 ? 1 : 3; // parts of what the caller's arrays hold
+template <class T> constexpr int MADE = sizeof(T) == 2 ? 2 : 3;  // and of what is computed
+
+struct Args {
+  const void *q, *k, *v, *dout;
+  const float *g, *beta, *from; // from: s0, kept (k_walk in the backward pass), ds_last; NULL: zeros
+  void *o, *dq, *dk_, *dv_;
+  float *to, *kept, *dg, *dbeta; // to: s_last, ds0
+  const int *lengths;
+  // a piece's intermediate arrays, by (chunk, batch, key head) or (chunk, batch, head)
+  __bf16 *kf, *qf, *ktf, *qtf; // operands: rows of steps, rows of channels
+  __bf16 *af, *pf, *atf, *ptf; // A, P and their transposes
+  float *gates;                // [3][64]: gam, gam_end / gam, beta
+  double *sums;                // [64]: G, as exponents of two
+  float *before, *after;       // S and dS' [dk padded][dvp]
+  float *w, *de;               // [64][dvp]
+  float *parts;                // [blocks][units][64]: w . dU of a block of columns
+  long long ld_q, ld_k, ld_v, ld_o, ld_dq, ld_dk, ld_dv;
+  int T, batch, heads, key_heads, dk, dv, dvp, blocks;
+  int first, chunks, all; // the piece's first chunk, its chunks, those of the sequence
+  float scale;
+};
+
+__device__ __forceinline__ int length_of(const Args &a, int b) { return a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T; }
+
+// ---- products ------------------------------------------------------------------------------
+// Matrix instructions of 16 x 16 with sums over 32.  Lane l has row (of B: column) l % 16 and sums 8 (l / 16) on of both operands, and elements 4 (l / 16) on of
+// the result's column l % 16.
+template <int P> struct Operand { frag p[P]; };
+
+template <int PA, int PB> __device__ __forceinline__ void multiply(tile &acc, const Operand<PA> &a, const Operand<PB> &b) {
+  constexpr int MOST = PA > PB ? PA : PB;
+#pragma unroll
+  for (int s = MOST - 1; s >= 0; --s) // parts whose numbers add up to s, the small ones first
+#pragma unroll
+    for (int i = 0; i <= s; ++i)
+      if (i < PA && s - i < PB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], acc, 0, 0, 0);
+}
+template <int P, int N> __device__ __forceinline__ void split(const float (&x)[N], __bf16 (&to)[P][N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    float left = x[j];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      to[i][j] = (__bf16)left;
+      left -= (float)to[i][j];
+    }
+  }
+}
+template <int P> __device__ __forceinline__ Operand<P> operand(const float (&x)[LANE]) {
+  __bf16 parts[P][LANE];
+  split<P, LANE>(x, parts);
+  Operand<P> r;
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+#pragma unroll
+    for (int j = 0; j < LANE; ++j) r.p[i][j] = parts[i][j];
+  return r;
+}
+// Operands in memory: one after the other, each its parts, each the lanes' 16 bytes
+template <int P> __device__ __forceinline__ Operand<P> fetch(const __bf16 *p, int number, int lane) {
+  Operand<P> r;
+#pragma unroll
+  for (int i = 0; i < P; ++i) r.p[i] = *(const frag *)(p + ((number * P + i) * 64 + lane) * LANE);
+  return r;
+}
+template <int P> __device__ __forceinline__ void leave(__bf16 *p, int number, int lane, const Operand<P> &x) {
+#pragma unroll
+  for (int i = 0; i < P; ++i) *(frag *)(p + ((number * P + i) * 64 + lane) * LANE) = x.p[i];
+}
+// and in LDS: planes of rows
+template <int P, int ROWS, int STRIDE> struct Planes {
+  __bf16 e[P][ROWS * STRIDE];
+  __device__ __forceinline__ Operand<P> get(int row, int col) const {
+    Operand<P> r;
+#pragma unroll
+    for (int i = 0; i < P; ++i) r.p[i] = *(const frag *)(e[i] + row * STRIDE + col);
+    return r;
+  }
+  // four elements of a row
+  __device__ __forceinline__ void put(int row, int col, const tile &x) {
+    const float v[4] = {x[0], x[1], x[2], x[3]};
+    __bf16 parts[P][4];
+    split<P, 4>(v, parts);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      four f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = parts[i][j];
+      *(four *)(e[i] + row * STRIDE + col) = f;
+    }
+  }
+};
+
+template <class T> __device__ __forceinline__ float element(const T *p, bool on) { return on ? (float)*p : 0.f; }
+
+// ---- a chunk by itself ------------------------------------------------------------------------
+template <class T, int DK, bool BACK> __global__ __launch_bounds__(256) void k_chunk(Args a) {
+  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32;
+  __shared__ __align__(16) Planes<PI, C, DK + 8> rows;
+  __shared__ __align__(16) float m[C][FLINE], x[C][FLINE];
+  __shared__ double sum[C];
+  __shared__ float rate[C];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
+  const int unit = blockIdx.x, kh = unit % a.key_heads, b = unit / a.key_heads % a.batch, c = unit / a.key_heads / a.batch;
+  const int t0 = (a.first + c) * C, len = length_of(a, b), group = a.heads / a.key_heads;
+  const int t = t0 + 16 * w + r;
+  constexpr int SIZE = DK * C * PI; // elements of one operand array of a unit
+  // rows of steps: to memory as operands, and those of k to LDS
+  Operand<PI> kf[KK], qf[KK];
+  auto load = [&](const void *p, long long ld, Operand<PI> (&f)[KK], __bf16 *to) {
+    const T *row = (const T *)p + ((long long)t * a.batch + b) * ld + kh * a.dk;
+#pragma unroll
+    for (int i = 0; i < KK; ++i) {
+      float e[LANE];
+      const int col = 32 * i + 8 * q4;
+      read(row + col, t < len ? a.dk - col : 0, e);
+      f[i] = operand<PI>(e);
+      leave<PI>(to + (long long)unit * SIZE, w * KK + i, lane, f[i]);
+    }
+  };
+  auto to_lds = [&](const Operand<PI> (&f)[KK]) {
+#pragma unroll
+    for (int i = 0; i < KK; ++i)
+#pragma unroll
+      for (int p = 0; p < PI; ++p) *(frag *)(rows.e[p] + (16 * w + r) * (DK + 8) + 32 * i + 8 * q4) = f[i].p[p];
+  };
+  auto turned = [&](__bf16 *to) { // rows of channels
+    for (int f = w; f < DK / 16 * 2; f += 4) {
+      Operand<PI> y;
+#pragma unroll
+      for (int p = 0; p < PI; ++p)
+#pragma unroll
+        for (int j = 0; j < LANE; ++j) y.p[p][j] = rows.e[p][(32 * (f & 1) + 8 * q4 + j) * (DK + 8) + 16 * (f >> 1) + r];
+      leave<PI>(to + (long long)unit * SIZE, f, lane, y);
+    }
+  };
+  load(a.k, a.ld_k, kf, a.kf);
+  load(a.q, a.ld_q, qf, a.qf);
+  to_lds(kf);
+  __syncthreads();
+  tile kk[4] = {}, qk[4] = {};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (j <= w)
+#pragma unroll
+      for (int i = 0; i < KK; ++i) {
+        const Operand<PI> y = rows.get(16 * j + r, 32 * i + 8 * q4);
+        multiply(kk[j], kf[i], y);
+        multiply(qk[j], qf[i], y);
+      }
+  turned(a.ktf);
+  if constexpr (BACK) {
+    __syncthreads();
+    to_lds(qf);
+    __syncthreads();
+    turned(a.qtf);
+  }
+  for (int i = 0; i < group; ++i) {
+    const int h = kh * group + i;
+    const long long of = ((long long)c * a.batch + b) * a.heads + h;
+    if (w == 0) {
+      const bool on = t0 + lane < len;
+      const long long at = ((long long)(t0 + lane) * a.batch + b) * a.heads + h;
+      float g = on ? a.g[at] : 0.f;
+      g = g < -1e4f ? -1e4f : g; // (minus infinity: forgotten all the same)
+      const float beta = on ? a.beta[at] : 0.f;
+      double G = (double)g * 1.4426950408889634;
+#pragma unroll
+      for (int s = 1; s < C; s *= 2) {
+        const double o = __shfl_up(G, s);
+        if (lane >= s) G += o;
+      }
+      sum[lane] = G;
+      rate[lane] = beta;
+      const double end = __shfl(G, C - 1);
+      float *to = a.gates + of * (3 * C);
+      to[lane] = __builtin_amdgcn_exp2f((float)G);
+      to[C + lane] = __builtin_amdgcn_exp2f((float)(end - G));
+      to[2 * C + lane] = beta;
+      if constexpr (BACK) a.sums[of * C + lane] = G;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = 16 * w + 4 * q4 + e, col = 16 * j + r;
+        float d = 0.f;
+        if (j <= w && col <= row) d = __builtin_amdgcn_exp2f((float)(sum[row] - sum[col]));
+        m[row][col] = col < row ? kk[j][e] * d * rate[col] : 0.f;
+        x[row][col] = col <= row ? qk[j][e] * d * a.scale : 0.f;
+      }
+    __syncthreads();
+    auto emit = [&](__bf16 *to, bool over) { // a matrix in x, or its transpose
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        float e[LANE];
+#pragma unroll
+        for (int j = 0; j < LANE; ++j) e[j] = over ? x[32 * s + 8 * q4 + j][16 * w + r] : x[16 * w + r][32 * s + 8 * q4 + j];
+        leave<PC>(to + of * (C * C * PC), 2 * w + s, lane, operand<PC>(e));
+      }
+    };
+    if constexpr (BACK) emit(a.ptf, true);
+    else emit(a.pf, false);
+    // column r of the inverse of the diagonal's block w
+    float y[16];
+#pragma unroll
+    for (int n = 0; n < 16; ++n) {
+      float s = n == r ? 1.f : 0.f;
+#pragma unroll
+      for (int j = 0; j < n; ++j) s = fmaf(-m[16 * w + n][16 * w + j], y[j], s);
+      y[n] = s;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j > w) x[16 * w + 4 * q4 + e][16 * j + r] = 0.f;
+#pragma unroll
+    for (int n = 0; n < 16; ++n)
+      if (n / 4 == q4) x[16 * w + n][16 * w + r] = y[n];
+    __syncthreads();
+    // column w of blocks, from the diagonal down: X_nw = -X_nn sum_j M_nj X_jw.  Four instructions of 16 x 16 with sums over 4 make a product; their sums
+    // are taken over elements e, 4 + e, .. of both operands, so that a result's registers are the next one's operand.
+    tile inv[4] = {};
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      if (n == w)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) inv[n][e] = x[16 * n + 4 * q4 + e][16 * w + r];
+      if (n > w) {
+        tile s = {}, z = {};
+#pragma unroll
+        for (int j = 0; j < n; ++j)
+          if (j >= w) {
+            const tile f = *(const tile *)&m[16 * n + r][16 * j + 4 * q4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(f[e], inv[j][e], s, 0, 0, 0);
+          }
+        const tile f = *(const tile *)&x[16 * n + r][16 * n + 4 * q4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z = __builtin_amdgcn_mfma_f32_16x16x4f32(-f[e], s[e], z, 0, 0, 0);
+        inv[n] = z;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[16 * n + 4 * q4 + e][16 * w + r] = z[e];
+      }
+    }
+    __syncthreads();
+    emit(a.af, false);
+    if constexpr (BACK) emit(a.atf, true);
+    __syncthreads();
+  }
+}
+
+// ---- the walk over the chunks -------------------------------------------------------------------
+// Workgroups of one head are on one die: they share what k_chunk left.
+struct Unit { int of, block; };
+__device__ __forceinline__ Unit unit_of(unsigned id, int units, int blocks) {
+  if (units % 8 == 0) return {(int)(id / 8 / blocks * 8 + id % 8), (int)(id / 8 % blocks)};
+  return {(int)(id / blocks), (int)(id % blocks)};
+}
+
+// REC: of the backward pass, from a kept state to the next; leaves S and w of each chunk.
+template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) void k_walk(Args a) {
+  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
+  __shared__ __align__(16) Planes<PC, BV, DK + 8> st;
+  __shared__ __align__(16) Planes<PC, BV, LINE> et, wt;
+  __shared__ __align__(16) Planes<REC ? 1 : PC, REC ? 1 : BV, LINE> ut;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
+  const int per = a.batch * a.heads;
+  const Unit u = unit_of(blockIdx.x % (per * a.blocks), per, a.blocks);
+  const int segment = blockIdx.x / (per * a.blocks); // REC: of KEPT chunks
+  const int h = u.of % a.heads, b = u.of / a.heads, kh = h / (a.heads / a.key_heads), v0 = u.block * BV;
+  const int len = length_of(a, b);
+  tile s[RT][NT] = {};
+  if (a.from) {
+    const float *from = a.from + ((REC ? (long long)(a.first / KEPT + segment) * per : 0) + u.of) * a.dk * a.dv;
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
+          s[i][n][e] = element(from + (long long)row * a.dv + col, row < a.dk && col < a.dv);
+        }
+  }
+  auto state_to = [&](float *to) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
+          if (row < a.dk && col < a.dv) to[(long long)row * a.dv + col] = s[i][n][e];
+        }
+  };
+  const int c0 = REC ? segment * KEPT : 0, c1 = REC ? min(c0 + KEPT, a.chunks) : a.chunks;
+  for (int c = c0; c < c1; ++c) {
+    const int t0 = (a.first + c) * C;
+    const long long of_k = ((long long)c * a.batch + b) * a.key_heads + kh, of = ((long long)c * a.batch + b) * a.heads + h;
+    const float *gates = a.gates + of * (3 * C);
+    if constexpr (!REC) {
+      if (a.kept && (a.first + c) % KEPT == 0) state_to(a.kept + ((long long)((a.first + c) / KEPT) * per + u.of) * a.dk * a.dv);
+    } else {
+      float *to = a.before + of * DK * a.dvp;
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
+            if (col < a.dvp) to[row * a.dvp + col] = s[i][n][e];
+          }
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) st.put(16 * n + r, 16 * (w * RT + i) + 4 * q4, s[i][n]);
+    float v[NT][4];
+    const int row0 = 16 * w + 4 * q4;
+    const T *vp = (const T *)a.v + ((long long)(t0 + row0) * a.batch + b) * a.ld_v + h * a.dv + v0 + r;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[n][e] = element(vp + (long long)e * a.batch * a.ld_v + 16 * n, t0 + row0 + e < len && v0 + 16 * n + r < a.dv);
+    const tile gam = *(const tile *)(gates + row0), tail = *(const tile *)(gates + C + row0), beta = *(const tile *)(gates + 2 * C + row0);
+    const float end = gates[C - 1];
+    __syncthreads();
+    tile e[NT] = {}, o[NT] = {};
+#pragma unroll
+    for (int i = 0; i < KK; ++i) {
+      const Operand<PI> k = fetch<PI>(a.kf + of_k * (DK * C * PI), w * KK + i, lane);
+      Operand<PI> q;
+      if constexpr (!REC) q = fetch<PI>(a.qf + of_k * (DK * C * PI), w * KK + i, lane);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const Operand<PC> y = st.get(16 * n + r, 32 * i + 8 * q4);
+        multiply(e[n], k, y);
+        if constexpr (!REC) multiply(o[n], q, y);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[n][i] = fmaf(-gam[i], e[n][i], v[n][i]);
+      et.put(16 * n + r, row0, e[n]);
+    }
+    __syncthreads();
+    tile x[NT] = {};
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (2 * j <= w) { // (A is lower triangular)
+        const Operand<PC> m = fetch<PC>(a.af + of * (C * C * PC), 2 * w + j, lane);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) multiply(x[n], m, et.get(16 * n + r, 32 * j + 8 * q4));
+      }
+    if constexpr (REC) {
+      float *to = a.w + (of * C + row0) * a.dvp + v0 + r;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (v0 + 16 * n + r < a.dvp) to[i * a.dvp + 16 * n] = x[n][i];
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const tile un = x[n] * beta;
+      if constexpr (!REC) ut.put(16 * n + r, row0, un);
+      wt.put(16 * n + r, row0, un * tail);
+    }
+    __syncthreads();
+    if constexpr (!REC) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[n] *= gam * a.scale;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (2 * j <= w) {
+          const Operand<PC> m = fetch<PC>(a.pf + of * (C * C * PC), 2 * w + j, lane);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) multiply(o[n], m, ut.get(16 * n + r, 32 * j + 8 * q4));
+        }
+      T *op = (T *)a.o + ((long long)(t0 + row0) * a.batch + b) * a.ld_o + h * a.dv + v0 + r;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (t0 + row0 + i < a.T && v0 + 16 * n + r < a.dv)
+            op[(long long)i * a.batch * a.ld_o + 16 * n] = (T)(t0 + row0 + i < len ? o[n][i] : 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[i][n] *= end;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const Operand<PI> k = fetch<PI>(a.ktf + of_k * (DK * C * PI), 2 * (w * RT + i) + j, lane);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) multiply(s[i][n], k, wt.get(16 * n + r, 32 * j + 8 * q4));
+      }
+  }
+  if constexpr (!REC)
+    if (a.to) state_to(a.to + (long long)u.of * a.dk * a.dv);
+}
+
+// ---- the walk back --------------------------------------------------------------------------------
+template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk_back(Args a) {
+  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
+  __shared__ __align__(16) Planes<PC, BV, DK + 8> st;
+  __shared__ __align__(16) Planes<PI, BV, LINE> ot;
+  __shared__ __align__(16) Planes<PC, BV, LINE> got, ut, et; // scale gam dO, beta dU, -gam dE
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
+  const int per = a.batch * a.heads;
+  const Unit u = unit_of(blockIdx.x, per, a.blocks);
+  const int h = u.of % a.heads, b = u.of / a.heads, kh = h / (a.heads / a.key_heads), v0 = u.block * BV;
+  const int len = length_of(a, b);
+  tile s[RT][NT] = {};
+  if (a.from)
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
+          s[i][n][e] = element(a.from + ((long long)u.of * a.dk + row) * a.dv + col, row < a.dk && col < a.dv);
+        }
+  for (int c = a.chunks - 1; c >= 0; --c) {
+    const int t0 = (a.first + c) * C, row0 = 16 * w + 4 * q4;
+    const long long of_k = ((long long)c * a.batch + b) * a.key_heads + kh, of = ((long long)c * a.batch + b) * a.heads + h;
+    const float *gates = a.gates + of * (3 * C);
+    const tile gam = *(const tile *)(gates + row0), tail = *(const tile *)(gates + C + row0), beta = *(const tile *)(gates + 2 * C + row0);
+    const float end = gates[C - 1];
+    {
+      float *to = a.after + of * DK * a.dvp;
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const int row = 16 * (w * RT + i) + 4 * q4, col = v0 + 16 * n + r;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (col < a.dvp) to[(row + e) * a.dvp + col] = s[i][n][e];
+          st.put(16 * n + r, row, s[i][n]);
+        }
+    }
+    const T *dp = (const T *)a.dout + ((long long)(t0 + row0) * a.batch + b) * a.ld_o + h * a.dv + v0 + r;
+    tile given[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        given[n][e] = element(dp + (long long)e * a.batch * a.ld_o + 16 * n, t0 + row0 + e < len && v0 + 16 * n + r < a.dv);
+      ot.put(16 * n + r, row0, given[n]);
+    }
+    __syncthreads(); // (and every wavefront is through with the last chunk)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) got.put(16 * n + r, row0, given[n] * (gam * a.scale));
+    tile d[NT] = {};
+#pragma unroll
+    for (int i = 0; i < KK; ++i) {
+      const Operand<PI> k = fetch<PI>(a.kf + of_k * (DK * C * PI), w * KK + i, lane);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) multiply(d[n], k, st.get(16 * n + r, 32 * i + 8 * q4));
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) d[n] *= tail;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (2 * j + 1 >= w) { // (P^T is upper triangular)
+        const Operand<PC> m = fetch<PC>(a.ptf + of * (C * C * PC), 2 * w + j, lane);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) multiply(d[n], m, ot.get(16 * n + r, 32 * j + 8 * q4));
+      }
+    {
+      const float *wp = a.w + (of * C + row0) * a.dvp + v0 + r;
+      tile dot = {};
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (v0 + 16 * n + r < a.dvp) dot[e] = fmaf(wp[e * a.dvp + 16 * n], d[n][e], dot[e]);
+        ut.put(16 * n + r, row0, d[n] * beta);
+      }
+#pragma unroll
+      for (int x = 1; x < 16; x *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dot[e] += __shfl_xor(dot[e], x);
+      if (r == 0) *(tile *)(a.parts + ((long long)u.block * a.chunks * per + of) * C + row0) = dot;
+    }
+    __syncthreads();
+    tile x[NT] = {};
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (2 * j + 1 >= w) {
+        const Operand<PC> m = fetch<PC>(a.atf + of * (C * C * PC), 2 * w + j, lane);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) multiply(x[n], m, ut.get(16 * n + r, 32 * j + 8 * q4));
+      }
+    T *vp = (T *)a.dv_ + ((long long)(t0 + row0) * a.batch + b) * a.ld_dv + h * a.dv + v0 + r;
+    float *ep = a.de + (of * C + row0) * a.dvp + v0 + r;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (t0 + row0 + e >= len) x[n][e] = 0.f;
+        if (v0 + 16 * n + r < a.dvp) ep[e * a.dvp + 16 * n] = x[n][e];
+        if (t0 + row0 + e < a.T && v0 + 16 * n + r < a.dv) vp[(long long)e * a.batch * a.ld_dv + 16 * n] = (T)x[n][e];
+      }
+      et.put(16 * n + r, row0, x[n] * -gam);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[i][n] *= end;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const Operand<PI> q = fetch<PI>(a.qtf + of_k * (DK * C * PI), 2 * (w * RT + i) + j, lane);
+        const Operand<PI> k = fetch<PI>(a.ktf + of_k * (DK * C * PI), 2 * (w * RT + i) + j, lane);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          multiply(s[i][n], q, got.get(16 * n + r, 32 * j + 8 * q4));
+          multiply(s[i][n], k, et.get(16 * n + r, 32 * j + 8 * q4));
+        }
+      }
+  }
+  if (a.to)
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
+          if (row < a.dk && col < a.dv) a.to[((long long)u.of * a.dk + row) * a.dv + col] = s[i][n][e];
+        }
+}
+
+// ---- gradients of a chunk's queries, keys and gates -----------------------------------------------
+template <class T, int DK> __global__ __launch_bounds__(256) void k_grads(Args a) {
+  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, NT = DK / 16;
+  constexpr int SLICE = 32 + 8; // a row's 32 columns in LDS
+  struct Sums { Planes<PC, DK, SLICE> before, after; Planes<PC, C, SLICE> w; };
+  struct Squares { float dp[C][FLINE], m[C][FLINE]; };
+  __shared__ __align__(16) char space[sizeof(Sums) > sizeof(Squares) ? sizeof(Sums) : sizeof(Squares)];
+  __shared__ float of_col[2][4][C], of_row[2][C], of_all[4];
+  Sums &sums = *(Sums *)space;
+  Squares &squares = *(Squares *)space;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
+  const int unit = blockIdx.x, kh = unit % a.key_heads, b = unit / a.key_heads % a.batch, c = unit / a.key_heads / a.batch;
+  const int t0 = (a.first + c) * C, len = length_of(a, b), group = a.heads / a.key_heads, row0 = 16 * w + 4 * q4;
+  const long long of_k = (long long)unit * (DK * C * PI);
+  tile qk[4] = {}, kk[4] = {};
+#pragma unroll
+  for (int i = 0; i < KK; ++i) {
+    const Operand<PI> q = fetch<PI>(a.qf + of_k, w * KK + i, lane), k = fetch<PI>(a.kf + of_k, w * KK + i, lane);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j <= w) {
+        const Operand<PI> y = fetch<PI>(a.kf + of_k, j * KK + i, lane);
+        multiply(qk[j], q, y);
+        multiply(kk[j], k, y);
+      }
+  }
+  tile gq[NT] = {}, gk[NT] = {};
+  for (int i = 0; i < group; ++i) {
+    const int h = kh * group + i;
+    const long long of = ((long long)c * a.batch + b) * a.heads + h;
+    const float *gates = a.gates + of * (3 * C);
+    const double *G = a.sums + of * C;
+    const float *before = a.before + of * DK * a.dvp, *after = a.after + of * DK * a.dvp, *wp = a.w + of * C * a.dvp, *ep = a.de + of * C * a.dvp;
+    const int t = t0 + 16 * w + r;
+    const T *dp = (const T *)a.dout + ((long long)t * a.batch + b) * a.ld_o + h * a.dv;
+    tile sq[NT] = {}, se[NT] = {}, su[NT] = {}, p[4] = {}, x[4] = {};
+    float both = 0.f; // <S, dS'>
+    for (int v = 0; v < a.dvp; v += 32) {
+      __syncthreads();
+#pragma unroll
+      for (int n = 0; n < DK / 64; ++n) {
+        const int o = n * 256 + threadIdx.x, row = o / 4, col = o % 4 * 8;
+        float y[LANE], z[LANE];
+        read(before + row * a.dvp + v + col, LANE, y);
+        read(after + row * a.dvp + v + col, LANE, z);
+#pragma unroll
+        for (int j = 0; j < LANE; ++j) both = fmaf(y[j], z[j], both);
+        const Operand<PC> fy = operand<PC>(y), fz = operand<PC>(z);
+#pragma unroll
+        for (int k = 0; k < PC; ++k) {
+          *(frag *)(sums.before.e[k] + row * SLICE + col) = fy.p[k];
+          *(frag *)(sums.after.e[k] + row * SLICE + col) = fz.p[k];
+        }
+      }
+      {
+        const int row = threadIdx.x / 4, col = threadIdx.x % 4 * 8;
+        float y[LANE];
+        read(wp + row * a.dvp + v + col, LANE, y);
+        const Operand<PC> f = operand<PC>(y);
+#pragma unroll
+        for (int k = 0; k < PC; ++k) *(frag *)(sums.w.e[k] + row * SLICE + col) = f.p[k];
+      }
+      float y[LANE];
+      read(dp + v + 8 * q4, t < len ? a.dv - v - 8 * q4 : 0, y);
+      const Operand<PI> d = operand<PI>(y);
+      read(ep + (16 * w + r) * a.dvp + v + 8 * q4, LANE, y);
+      const Operand<PC> e = operand<PC>(y);
+      __syncthreads();
+      const Operand<PC> mine = sums.w.get(16 * w + r, 8 * q4);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const Operand<PC> s = sums.before.get(16 * n + r, 8 * q4);
+        multiply(sq[n], d, s);
+        multiply(se[n], e, s);
+        multiply(su[n], mine, sums.after.get(16 * n + r, 8 * q4));
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j <= w) {
+          const Operand<PC> y = sums.w.get(16 * j + r, 8 * q4);
+          multiply(p[j], d, y);
+          multiply(x[j], e, y);
+        }
+    }
+    __syncthreads();
+    const tile gam = *(const tile *)(gates + row0), tail = *(const tile *)(gates + C + row0), beta = *(const tile *)(gates + 2 * C + row0);
+    tile of_mine = {}, wrote = {}; // what is read by a step and what a later step reads of it, what is left of it at the end
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int col = 16 * j + r;
+      const float beta_col = gates[2 * C + col];
+      float z_col = 0.f, l_col = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = row0 + e;
+        const bool low = j <= w && col <= row, below = j <= w && col < row;
+        const float d = low ? __builtin_amdgcn_exp2f((float)(G[row] - G[col])) : 0.f;
+        const float dpe = low ? p[j][e] * beta_col * d * a.scale : 0.f, me = below ? -x[j][e] * beta_col * d : 0.f;
+        const float z = low ? fmaf(qk[j][e], dpe, kk[j][e] * me) : 0.f;
+        of_mine[e] += z;
+        z_col += z;
+        l_col += below ? kk[j][e] * d * x[j][e] : 0.f;
+        squares.dp[row][col] = dpe;
+        if (below) squares.m[row][col] = squares.m[col][row] = me;
+        if (j == w && col == row) squares.m[row][col] = 0.f;
+      }
+#pragma unroll
+      for (int s = 16; s < 64; s *= 2) {
+        z_col += __shfl_xor(z_col, s);
+        l_col += __shfl_xor(l_col, s);
+      }
+      if (q4 == 0) {
+        of_col[0][w][col] = z_col;
+        of_col[1][w][col] = l_col;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      sq[n] *= gam * a.scale;
+      se[n] *= gam;
+      su[n] *= beta * tail;
+      const int col = 16 * n + r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const long long row = (long long)(t0 + row0 + e) * a.batch + b;
+        const bool on = t0 + row0 + e < len && col < a.dk;
+        const float qe = element((const T *)a.q + row * a.ld_q + kh * a.dk + col, on), ke = element((const T *)a.k + row * a.ld_k + kh * a.dk + col, on);
+        of_mine[e] += fmaf(qe, sq[n][e], -(ke * se[n][e]));
+        wrote[e] = fmaf(ke, su[n][e], wrote[e]);
+      }
+      gq[n] += sq[n];
+      gk[n] += su[n] - se[n];
+    }
+#pragma unroll
+    for (int s = 1; s < 16; s *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        of_mine[e] += __shfl_xor(of_mine[e], s);
+        wrote[e] += __shfl_xor(wrote[e], s);
+      }
+    if (r == 0) {
+      *(tile *)(of_row[0] + row0) = of_mine;
+      *(tile *)(of_row[1] + row0) = wrote;
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) both += __shfl_xor(both, s);
+    if (lane == 0) of_all[w] = both;
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      float y[LANE];
+      Operand<PC> dpf, dpt, m;
+#pragma unroll
+      for (int j = 0; j < LANE; ++j) y[j] = squares.dp[16 * w + r][32 * s + 8 * q4 + j];
+      dpf = operand<PC>(y);
+#pragma unroll
+      for (int j = 0; j < LANE; ++j) y[j] = squares.dp[32 * s + 8 * q4 + j][16 * w + r];
+      dpt = operand<PC>(y);
+#pragma unroll
+      for (int j = 0; j < LANE; ++j) y[j] = squares.m[16 * w + r][32 * s + 8 * q4 + j];
+      m = operand<PC>(y);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const Operand<PI> k = fetch<PI>(a.ktf + of_k, 2 * n + s, lane);
+        if (2 * s <= w) multiply(gq[n], dpf, k);
+        multiply(gk[n], m, k);
+        if (2 * s + 1 >= w) multiply(gk[n], dpt, fetch<PI>(a.qtf + of_k, 2 * n + s, lane));
+      }
+    }
+    if (w == 0) {
+      const float end = gates[C - 1];
+      double on = (double)of_row[0][lane] - ((of_col[0][0][lane] + of_col[0][1][lane]) + (of_col[0][2][lane] + of_col[0][3][lane]));
+      const float mine = of_row[1][lane];
+      double up = mine;
+#pragma unroll
+      for (int s = 1; s < C; s *= 2) {
+        const double o = __shfl_down(on, s), y = __shfl_up(up, s);
+        if (lane + s < C) on += o;
+        if (lane >= s) up += y;
+      }
+      const float all = end * ((of_all[0] + of_all[1]) + (of_all[2] + of_all[3]));
+      float db = -((of_col[1][0][lane] + of_col[1][1][lane]) + (of_col[1][2][lane] + of_col[1][3][lane]));
+      for (int n = 0; n < a.blocks; ++n) db += a.parts[((long long)n * a.chunks * a.batch * a.heads + of) * C + lane];
+      if (t0 + lane < a.T) {
+        const long long at = ((long long)(t0 + lane) * a.batch + b) * a.heads + h;
+        a.dg[at] = t0 + lane < len ? (float)(all + on + (up - mine)) : 0.f;
+        a.dbeta[at] = t0 + lane < len ? db : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int t = t0 + row0 + e, col = 16 * n + r;
+      if (t < a.T && col < a.dk) {
+        const long long row = (long long)t * a.batch + b;
+        ((T *)a.dq)[row * a.ld_dq + kh * a.dk + col] = (T)(t < len ? gq[n][e] : 0.f);
+        ((T *)a.dk_)[row * a.ld_dk + kh * a.dk + col] = (T)(t < len ? gk[n][e] : 0.f);
+      }
+    }
+}
+
+// ---- step after step ------------------------------------------------------------------------------
+// A workgroup has all of a head's rows and 4 LV columns, four of them and every (256 / LV)-th row a lane.  o_t = scale (q . a S + (q . k) u): both sums over the
+// rows are taken of the state as it was, at once.
+template <class T, int DK, int LV> __global__ __launch_bounds__(256) void k_steps(Args a) {
+  constexpr int GROUPS = 256 / LV, ROWS = DK / GROUPS;
+  __shared__ float qs[2][DK], ks[2][DK], sums[2][4][2][LV * 4], dots[2][4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = threadIdx.x % LV, first = threadIdx.x / LV;
+  const Unit u = unit_of(blockIdx.x, a.batch * a.heads, a.blocks);
+  const int h = u.of % a.heads, b = u.of / a.heads, kh = h / (a.heads / a.key_heads), col = u.block * (4 * LV) + 4 * at;
+  const int len = length_of(a, b), cols = min(4, a.dv - col);
+  typedef tile tile_any __attribute__((aligned(4)));
+  tile s[ROWS];
+  const long long base = (long long)u.of * a.dk * a.dv + col;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    const int row = first + GROUPS * i;
+    s[i] = tile{};
+    if (a.from && row < a.dk) {
+      const float *p = a.from + base + (long long)row * a.dv;
+      if (cols == 4) s[i] = *(const tile_any *)p;
+      else
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[i][e] = e < cols ? p[e] : 0.f;
+    }
+  }
+  auto state_to = [&](float *to) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int row = first + GROUPS * i;
+      if (row >= a.dk) continue;
+      float *p = to + base + (long long)row * a.dv;
+      if (cols == 4) *(tile_any *)p = s[i];
+      else
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < cols) p[e] = s[i][e];
+    }
+  };
+  if (a.kept && a.T) state_to(a.kept);
+  for (int t = 0; t < a.T; ++t) {
+    const long long row = (long long)t * a.batch + b;
+    T *op = (T *)a.o + row * a.ld_o + h * a.dv + col;
+    if (t >= len) {
+      if (first == 0)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < cols) op[e] = (T)0.f;
+      continue;
+    }
+    const int turn = t & 1; // (LDS of one step is read while that of the next is written)
+    if ((int)threadIdx.x < DK) {
+      const bool on = (int)threadIdx.x < a.dk;
+      const float q = element((const T *)a.q + row * a.ld_q + kh * a.dk + threadIdx.x, on), k = element((const T *)a.k + row * a.ld_k + kh * a.dk + threadIdx.x, on);
+      qs[turn][threadIdx.x] = q;
+      ks[turn][threadIdx.x] = k;
+      float d = q * k;
+#pragma unroll
+      for (int x = 1; x < 64; x *= 2) d += __shfl_xor(d, x);
+      if (lane == 0) dots[turn][wave] = d;
+    }
+    tile v = {};
+    const T *vp = (const T *)a.v + row * a.ld_v + h * a.dv + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = element(vp + e, e < cols);
+    const float hold = __builtin_amdgcn_exp2f(a.g[row * a.heads + h] * LOG2E), beta = a.beta[row * a.heads + h];
+    __syncthreads();
+    tile of_k = {}, of_q = {};
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const float k = ks[turn][first + GROUPS * i], q = qs[turn][first + GROUPS * i];
+      s[i] *= hold;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        of_k[e] = fmaf(s[i][e], k, of_k[e]);
+        of_q[e] = fmaf(s[i][e], q, of_q[e]);
+      }
+    }
+#pragma unroll
+    for (int x = LV; x < 64; x *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        of_k[e] += __shfl_xor(of_k[e], x);
+        of_q[e] += __shfl_xor(of_q[e], x);
+      }
+    if (lane < LV) {
+      *(tile *)(sums[turn][wave][0] + 4 * at) = of_k;
+      *(tile *)(sums[turn][wave][1] + 4 * at) = of_q;
+    }
+    __syncthreads();
+    of_k = of_q = tile{};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      of_k += *(const tile *)(sums[turn][x][0] + 4 * at);
+      of_q += *(const tile *)(sums[turn][x][1] + 4 * at);
+    }
+    float qk = 0.f;
+#pragma unroll
+    for (int x = 0; x < DK / 64; ++x) qk += dots[turn][x];
+    const tile un = (v - of_k) * beta;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const float k = ks[turn][first + GROUPS * i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[i][e] = fmaf(k, un[e], s[i][e]);
+    }
+    if (first == 0) {
+      const tile o = (of_q + un * qk) * a.scale;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < cols) op[e] = (T)o[e];
+    }
+  }
+  if (a.to) state_to(a.to);
+}
+
+// ---- launches -------------------------------------------------------------------------------------
+constexpr int STEPS_MOST = 16;            // steps that are taken one after the other
+constexpr size_t PIECE = (size_t)512 << 20; // bytes of a piece's intermediate arrays, at least 4 chunks
+
+size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+struct Plan {
+  int dk, bv, blocks, dvp, all, chunks, per, units; // units: of key heads
+  size_t bytes;
+  float *last = nullptr; // where the caller wants the last state, or ds0
+  Args a = {};
+  Plan(const DeltaShape &p, bool back, char *work) {
+    dk = p.dk <= 64 ? 64 : 128;
+    per = p.batch * p.heads, units = p.batch * p.key_heads;
+    bv = p.bf16 && p.dv > 32 && !back ? 64 : 32;
+    blocks = (p.dv + bv - 1) / bv;
+    dvp = (p.dv + 31) / 32 * 32;
+    all = (p.T + C - 1) / C;
+    const size_t pi = p.bf16 ? 1 : 3, pc = p.bf16 ? 2 : 3;
+    auto lay = [&](int n) {
+      size_t at = 0;
+      auto take = [&](auto *&to, size_t count) {
+        to = (std::remove_reference_t<decltype(to)>)(work ? work + at : nullptr);
+        at += rounded(count * sizeof *to);
+      };
+      const size_t nk = (size_t)n * units, nh = (size_t)n * per;
+      float *carry;
+      take(carry, (size_t)per * p.dk * p.dv);
+      a.to = carry;
+      for (__bf16 **x : {&a.kf, &a.qf, &a.ktf}) take(*x, nk * dk * C * pi);
+      take(a.af, nh * C * C * pc);
+      take(a.gates, nh * 3 * C);
+      if (!back) take(a.pf, nh * C * C * pc);
+      else {
+        take(a.qtf, nk * dk * C * pi);
+        take(a.ptf, nh * C * C * pc);
+        take(a.atf, nh * C * C * pc);
+        take(a.sums, nh * C);
+        take(a.before, nh * dk * dvp);
+        take(a.after, nh * dk * dvp);
+        take(a.w, nh * C * dvp);
+        take(a.de, nh * C * dvp);
+        take(a.parts, nh * C * blocks);
+      }
+      return at;
+    };
+    const size_t one = lay(KEPT) - lay(0);
+    const long long most = (long long)(PIECE / one) * KEPT;
+    chunks = (int)(most < KEPT ? KEPT : most > all ? all : most);
+    if (chunks > all) chunks = all;
+    bytes = lay(chunks);
+    a.lengths = p.lengths;
+    a.ld_q = p.ld_q, a.ld_k = p.ld_k, a.ld_v = p.ld_v, a.ld_o = p.ld_o, a.ld_dq = p.ld_dq, a.ld_dk = p.ld_dk, a.ld_dv = p.ld_dv;
+    a.T = p.T, a.batch = p.batch, a.heads = p.heads, a.key_heads = p.key_heads, a.dk = p.dk, a.dv = p.dv, a.dvp = dvp, a.blocks = blocks;
+    a.all = all, a.scale = p.scale;
+  }
+};
+
+template <class T, int DK> hipError_t forward(Plan &p, hipStream_t s) {
+  Args a = p.a;
+  float *const carry = a.to;
+  const float *from = a.from;
+  for (int first = 0; first < p.all; first += p.chunks) {
+    a.first = first;
+    a.chunks = p.all - first < p.chunks ? p.all - first : p.chunks;
+    a.from = from;
+    a.to = first + a.chunks < p.all ? carry : p.last;
+    k_chunk<T, DK, false><<<a.chunks * p.units, 256, 0, s>>>(a);
+    if (p.bv == 64) {
+      if constexpr (sizeof(T) == 2) k_walk<T, DK, 64, false><<<p.per * p.blocks, 256, 0, s>>>(a);
+    } else k_walk<T, DK, 32, false><<<p.per * p.blocks, 256, 0, s>>>(a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    from = carry;
+  }
+  return hipSuccess;
+}
+template <class T, int DK> hipError_t backward(Plan &p, const float *kept, const float *ds_last, hipStream_t s) {
+  Args a = p.a;
+  float *const carry = a.to;
+  const float *from = ds_last;
+  if (!p.all) {
+    a.from = ds_last;
+    a.to = p.last;
+    k_walk_back<T, DK, 32><<<p.per * p.blocks, 256, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  // pieces of whole kept intervals, from the last one on
+  for (int first = (p.all - 1) / p.chunks * p.chunks; first >= 0; first -= p.chunks) {
+    a.first = first;
+    a.chunks = p.all - first < p.chunks ? p.all - first : p.chunks;
+    k_chunk<T, DK, true><<<a.chunks * p.units, 256, 0, s>>>(a);
+    a.from = kept;
+    a.to = nullptr;
+    k_walk<T, DK, 32, true><<<(a.chunks + KEPT - 1) / KEPT * p.per * p.blocks, 256, 0, s>>>(a);
+    a.from = from;
+    a.to = first ? carry : p.last;
+    k_walk_back<T, DK, 32><<<p.per * p.blocks, 256, 0, s>>>(a);
+    k_grads<T, DK><<<a.chunks * p.units, 256, 0, s>>>(a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    from = carry;
+  }
+  return hipSuccess;
+}
+template <class T> hipError_t steps(Plan &p, hipStream_t s) {
+  Args a = p.a;
+  a.to = p.last;
+  const bool wide = a.dv > 64;
+  a.blocks = (a.dv + (wide ? 127 : 63)) / (wide ? 128 : 64);
+  const unsigned grid = (unsigned)p.per * a.blocks;
+  if (p.dk == 64) {
+    if (wide) k_steps<T, 64, 32><<<grid, 256, 0, s>>>(a);
+    else k_steps<T, 64, 16><<<grid, 256, 0, s>>>(a);
+  } else {
+    if (wide) k_steps<T, 128, 32><<<grid, 256, 0, s>>>(a);
+    else k_steps<T, 128, 16><<<grid, 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+} // namespace
+
+size_t delta_workspace(const DeltaShape &p, bool back) {
+  if (!p.T || (!back && p.T <= STEPS_MOST)) return 0;
+  return Plan(p, back, nullptr).bytes;
+}
+
+hipError_t launch_delta_forward(const DeltaShape &p, const void *q, const void *k, const void *v, const float *g, const float *beta, const float *s0,
+                                void *o, float *s_last, float *kept, void *work, hipStream_t s) {
+  Plan plan(p, false, (char *)work);
+  Args &a = plan.a;
+  a.q = q, a.k = k, a.v = v, a.g = g, a.beta = beta, a.from = s0, a.o = o, a.kept = kept;
+  plan.last = s_last;
+  if (p.T <= STEPS_MOST) return p.bf16 ? steps<__bf16>(plan, s) : steps<float>(plan, s);
+  if (plan.dk == 64) return p.bf16 ? forward<__bf16, 64>(plan, s) : forward<float, 64>(plan, s);
+  return p.bf16 ? forward<__bf16, 128>(plan, s) : forward<float, 128>(plan, s);
+}
+
+hipError_t launch_delta_backward(const DeltaShape &p, const void *q, const void *k, const void *v, const float *g, const float *beta, const float *kept,
+                                 const void *dout, const float *ds_last, void *dq, void *dk, void *dv, float *dg, float *dbeta, float *ds0, void *work,
+                                 hipStream_t s) {
+  Plan plan(p, true, (char *)work);
+  Args &a = plan.a;
+  a.q = q, a.k = k, a.v = v, a.g = g, a.beta = beta, a.dout = dout, a.dq = dq, a.dk_ = dk, a.dv_ = dv, a.dg = dg, a.dbeta = dbeta;
+  plan.last = ds0;
+  if (plan.dk == 64) return p.bf16 ? backward<__bf16, 64>(plan, kept, ds_last, s) : backward<float, 64>(plan, kept, ds_last, s);
+  return p.bf16 ? backward<__bf16, 128>(plan, kept, ds_last, s) : backward<float, 128>(plan, kept, ds_last, s);
+}

@@ -141,6 +141,28 @@ snn_status vocab_shape(const char *what, const snn_vocab *p, VocabShape *v) {
   return SNN_OK;
 }
 
+snn_status delta_shape(const char *what, const snn_delta *p, DeltaShape *d) {
+  if (!p) return refuse(SNN_E_INVAL, "%s: no shape", what);
+  if (!dtype_ok(p->dtype)) return refuse(SNN_E_INVAL, "%s: unknown type %d", what, p->dtype);
+  if (p->T < 0 || p->T > (1 << 30)) return refuse(SNN_E_INVAL, "%s: T = %d", what, p->T);
+  if (p->key_heads < 1 || p->heads < 1 || p->heads % p->key_heads)
+    return refuse(SNN_E_INVAL, "%s: %d heads, %d of keys: the first must be a multiple of the second", what, p->heads, p->key_heads);
+  if (p->dk < 1 || p->dk > 128 || p->dv < 1 || p->dv > 1024) return refuse(SNN_E_INVAL, "%s: dk %d (1 .. 128), dv %d (1 .. 1024)", what, p->dk, p->dv);
+  if (p->batch < 1 || (long long)p->batch * p->heads > 1 << 20 || (long long)p->batch * p->heads * p->dv > 1 << 28)
+    return refuse(SNN_E_INVAL, "%s: batch %d, %d heads, dv %d: 2^20 heads and 2^28 columns of states in all at most", what, p->batch, p->heads, p->dv);
+  if (!std::isfinite(p->scale)) return refuse(SNN_E_INVAL, "%s: scale = %g", what, p->scale);
+  *d = DeltaShape{p->T, p->batch, p->heads, p->key_heads, p->dk, p->dv, p->dtype == SNN_BF16, p->scale,
+                  p->ld_q, p->ld_k, p->ld_v, p->ld_o, p->ld_dq, p->ld_dk, p->ld_dv, p->lengths};
+  const int64_t of_keys = (int64_t)p->key_heads * p->dk, of_values = (int64_t)p->heads * p->dv;
+  const std::pair<long long *, int64_t> lds[] = {{&d->ld_q, of_keys}, {&d->ld_k, of_keys}, {&d->ld_v, of_values}, {&d->ld_o, of_values},
+                                                 {&d->ld_dq, of_keys}, {&d->ld_dk, of_keys}, {&d->ld_dv, of_values}};
+  for (auto [ld, least] : lds) {
+    if (!*ld) *ld = least;
+    if (*ld < least || *ld > (1 << 30)) return refuse(SNN_E_INVAL, "%s: %lld elements from row to row: those of all heads .. 2^30", what, *ld);
+  }
+  return SNN_OK;
+}
+
 snn_status norm_shape(const char *what, const snn_norm *p, NormShape *n) {
   if (!p) return refuse(SNN_E_INVAL, "%s: no shape", what);
   if (!dtype_ok(p->dtype)) return refuse(SNN_E_INVAL, "%s: unknown type %d", what, p->dtype);
@@ -315,6 +337,46 @@ snn_status snn_vocab_loss_grad(const snn_launch *at, const snn_vocab *p, const v
   const OnDevice on(at->device);
   if (on.error != hipSuccess) return queued(on.error, what);
   return queued(launch_vocab_grad(v, h, w, targets, state, dloss, dh, dw, at->workspace, (hipStream_t)at->stream), what);
+}
+
+size_t snn_delta_workspace(const snn_delta *p, int32_t gradients) {
+  DeltaShape d;
+  return delta_shape("snn_delta_workspace", p, &d) == SNN_OK ? delta_workspace(d, gradients != 0) : 0;
+}
+
+snn_status snn_delta_forward(const snn_launch *at, const snn_delta *p, const void *q, const void *k, const void *v, const float *g, const float *beta,
+                             const float *s0, void *o, float *s_last, float *kept) {
+  static const char what[] = "snn_delta_forward";
+  DeltaShape d;
+  CHECK(launch_ok(what, at));
+  CHECK(delta_shape(what, p, &d));
+  const bool some = d.T > 0;
+  const size_t size = size_of(p->dtype);
+  const Array arrays[] = {{"q", q, size, some}, {"k", k, size, some}, {"v", v, size, some}, {"g", g, 4, some}, {"beta", beta, 4, some}, {"s0", s0, 4, false},
+                          {"o", o, size, some}, {"s_last", s_last, 4, false}, {"kept", kept, 4, false}, {"lengths", d.lengths, 4, false}};
+  CHECK(check(what, at, arrays));
+  CHECK(check_workspace(what, at, delta_workspace(d, false)));
+  const OnDevice on(at->device);
+  if (on.error != hipSuccess) return queued(on.error, what);
+  return queued(launch_delta_forward(d, q, k, v, g, beta, s0, o, s_last, kept, at->workspace, (hipStream_t)at->stream), what);
+}
+
+snn_status snn_delta_backward(const snn_launch *at, const snn_delta *p, const void *q, const void *k, const void *v, const float *g, const float *beta,
+                              const float *kept, const void *dout, const float *ds_last, void *dq, void *dk, void *dv, float *dg, float *dbeta, float *ds0) {
+  static const char what[] = "snn_delta_backward";
+  DeltaShape d;
+  CHECK(launch_ok(what, at));
+  CHECK(delta_shape(what, p, &d));
+  const bool some = d.T > 0;
+  const size_t size = size_of(p->dtype);
+  const Array arrays[] = {{"q", q, size, some}, {"k", k, size, some}, {"v", v, size, some}, {"g", g, 4, some}, {"beta", beta, 4, some}, {"kept", kept, 4, some},
+                          {"do", dout, size, some}, {"ds_last", ds_last, 4, false}, {"dq", dq, size, some}, {"dk", dk, size, some}, {"dv", dv, size, some},
+                          {"dg", dg, 4, some}, {"dbeta", dbeta, 4, some}, {"ds0", ds0, 4, false}, {"lengths", d.lengths, 4, false}};
+  CHECK(check(what, at, arrays));
+  CHECK(check_workspace(what, at, delta_workspace(d, true)));
+  const OnDevice on(at->device);
+  if (on.error != hipSuccess) return queued(on.error, what);
+  return queued(launch_delta_backward(d, q, k, v, g, beta, kept, dout, ds_last, dq, dk, dv, dg, dbeta, ds0, at->workspace, (hipStream_t)at->stream), what);
 }
 
 size_t snn_norm_workspace(const snn_norm *p) {

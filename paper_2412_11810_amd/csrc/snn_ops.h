@@ -78,3 +78,20 @@ struct AdamwTensor {
 };
 size_t adamw_workspace(); // where the count is on the device
 hipError_t launch_adamw(const AdamwStep &how, const AdamwTensor *tensors, long long count, void *work, hipStream_t s);
+
+// ---- gated delta rule (snn_delta.hip) -------------------------------------------------------
+#define SNN_DELTA_INTERVAL 256 // steps between the states that the forward pass keeps
+
+struct DeltaShape {
+  int T, batch, heads, key_heads, dk, dv;
+  bool bf16;
+  float scale;
+  long long ld_q, ld_k, ld_v, ld_o, ld_dq, ld_dk, ld_dv; // elements between the rows (t, b) of an array (ld_o: of o and its gradient)
+  const int *lengths;                                    // NULL: T steps each
+};
+size_t delta_workspace(const DeltaShape &p, bool back);
+hipError_t launch_delta_forward(const DeltaShape &p, const void *q, const void *k, const void *v, const float *g, const float *beta, const float *s0,
+                                void *o, float *s_last, float *kept, void *work, hipStream_t s);
+hipError_t launch_delta_backward(const DeltaShape &p, const void *q, const void *k, const void *v, const float *g, const float *beta, const float *kept,
+                                 const void *dout, const float *ds_last, void *dq, void *dk, void *dv, float *dg, float *dbeta, float *ds0, void *work,
+                                 hipStream_t s);

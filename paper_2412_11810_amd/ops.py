@@ -13,6 +13,7 @@ from typing import NamedTuple
 
 SNN_F32, SNN_BF16 = 0, 1
 GLR_INTERVAL = 128  # steps between the states that snn_glr_forward keeps
+DELTA_INTERVAL = 256  # and snn_delta_forward
 PACK_BLOCK = 32     # elements of a row that share a step in 8 bits
 
 
@@ -32,6 +33,12 @@ class snn_packed(C.Structure):
 class snn_vocab(C.Structure):
     _fields_ = [("rows", C.c_int32), ("d", C.c_int32), ("vocab", C.c_int32), ("dtype", C.c_int32), ("ld_h", C.c_int64),
                 ("ld_w", C.c_int64)]
+
+
+class snn_delta(C.Structure):
+    _fields_ = [("T", C.c_int32), ("batch", C.c_int32), ("heads", C.c_int32), ("key_heads", C.c_int32), ("dk", C.c_int32), ("dv", C.c_int32),
+                ("dtype", C.c_int32), ("scale", C.c_float), ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_v", C.c_int64), ("ld_o", C.c_int64),
+                ("ld_dq", C.c_int64), ("ld_dk", C.c_int64), ("ld_dv", C.c_int64), ("lengths", C.c_void_p)]
 
 
 class snn_norm(C.Structure):
@@ -70,7 +77,11 @@ def declare(L):
     L.snn_pack.argtypes = L.snn_unpack.argtypes = [at, C.c_int, i64, i32, i64] + [vp] * 3
     L.snn_vocab_loss.argtypes = [at, vocab] + [vp] * 5
     L.snn_vocab_loss_grad.argtypes = [at, vocab] + [vp] * 7
-    norm, adamw = C.POINTER(snn_norm), C.POINTER(snn_adamw)
+    norm, adamw, delta = C.POINTER(snn_norm), C.POINTER(snn_adamw), C.POINTER(snn_delta)
+    L.snn_delta_workspace.argtypes = [delta, i32]
+    L.snn_delta_workspace.restype = C.c_size_t
+    L.snn_delta_forward.argtypes = [at, delta] + [vp] * 9
+    L.snn_delta_backward.argtypes = [at, delta] + [vp] * 14
     L.snn_norm_workspace.argtypes = [norm]
     L.snn_norm_workspace.restype = C.c_size_t
     L.snn_norm_forward.argtypes = [at, norm] + [vp] * 5
@@ -79,7 +90,8 @@ def declare(L):
     L.snn_adamw_workspace.restype = C.c_size_t
     L.snn_adamw_step.argtypes = [at, adamw, C.POINTER(snn_adamw_tensor), i64]
     for name in ("snn_glr_forward", "snn_glr_backward", "snn_glr_backward_packed", "snn_pack", "snn_unpack", "snn_vocab_loss",
-                 "snn_vocab_loss_grad", "snn_norm_forward", "snn_norm_forward_packed", "snn_norm_backward", "snn_adamw_step"):
+                 "snn_vocab_loss_grad", "snn_norm_forward", "snn_norm_forward_packed", "snn_norm_backward", "snn_adamw_step", "snn_delta_forward",
+                 "snn_delta_backward"):
         getattr(L, name).restype = C.c_int
 
 
@@ -303,6 +315,75 @@ def snn_vocab_loss_grad(h, w, targets, state, dloss=None):
     dw = torch.empty((p.vocab, p.d), dtype=h.dtype, device=h.device)
     _run("snn_vocab_loss_grad", C.byref(at), C.byref(p), _at(h), _at(w), _at(targets), _at(state), _at(dloss), _at(dh), _at(dw))
     return dh, dw
+
+
+def _ld_heads(x, name):
+    """Elements between consecutive rows of [T][batch][heads][d], a row being all its heads one after the other."""
+    T, batch, heads, d = x.shape
+    if x.is_contiguous():
+        return heads * d
+    if (d > 1 and x.stride(3) != 1) or (heads > 1 and x.stride(2) != d):
+        raise ValueError(f"{name}: the heads of a row must follow one another")
+    return _ld(x.as_strided((T, batch, heads * d), (x.stride(0), x.stride(1), 1)), name)
+
+
+def _delta_shape(q, k, v, g, beta, lengths, scale):
+    import torch
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError(f"q, k must be [T][batch][key_heads][dk] and v [T][batch][heads][dv], got {tuple(q.shape)} and {tuple(v.shape)}")
+    (T, batch, key_heads, dk), (heads, dv), dtype, device = q.shape, v.shape[2:], _type(q, "q"), q.device
+    _same(k, "k", q.dtype, q.shape, device)
+    _same(v, "v", q.dtype, (T, batch, heads, dv), device)
+    _packed_rows(_same(g, "g", torch.float32, (T, batch, heads), device), "g")
+    _packed_rows(_same(beta, "beta", torch.float32, (T, batch, heads), device), "beta")
+    if lengths is not None:
+        _packed_rows(_same(lengths, "lengths", torch.int32, (batch,), device), "lengths")
+    return snn_delta(T, batch, heads, key_heads, dk, dv, dtype, dk ** -0.5 if scale is None and dk else scale or 0.0, _ld_heads(q, "q"), _ld_heads(k, "k"),
+                     _ld_heads(v, "v"), 0, 0, 0, 0, _at(lengths)), (batch, heads, dk, dv)
+
+
+def snn_delta_forward(q, k, v, g, beta, s0=None, lengths=None, scale=None, keep=False, o=None, s_last=None):
+    """S_t = exp(g_t) S_{t-1} + k_t u_t^T with u_t = beta_t (v_t - exp(g_t) S_{t-1}^T k_t), and o_t = scale S_t^T q_t, over q, k [T][batch][key_heads][dk],
+    v [T][batch][heads][dv], g, beta [T][batch][heads] (float32) from the state s0 [batch][heads][dk][dv] (float32; None: zeros).
+    scale: 1 / sqrt(dk) unless given; consecutive heads share queries and keys where there are more of them than of keys.
+
+    Returns o, the last state and, with keep, the states that snn_delta_backward needs (else None).  o and s_last: tensors for the results;
+    s_last may be s0 itself, a state that is updated in place."""
+    import torch
+    p, state = _delta_shape(q, k, v, g, beta, lengths, scale)
+    device = q.device
+    if s0 is not None:
+        _packed_rows(_same(s0, "s0", torch.float32, state, device), "s0")
+    o = _out(o, "o", v)
+    p.ld_o = _ld_heads(o, "o")
+    at, space = _launch(device, _entry("snn_delta_workspace")(C.byref(p), 0))
+    if s_last is None:
+        s_last = torch.empty(state, dtype=torch.float32, device=device)
+    else:
+        _packed_rows(_same(s_last, "s_last", torch.float32, state, device), "s_last")
+    kept = torch.empty((-(-p.T // DELTA_INTERVAL), *state), dtype=torch.float32, device=device) if keep else None
+    _run("snn_delta_forward", C.byref(at), C.byref(p), _at(q), _at(k), _at(v), _at(g), _at(beta), _at(s0), _at(o), _at(s_last), _at(kept))
+    return o, s_last, kept
+
+
+def snn_delta_backward(q, k, v, g, beta, kept, do, ds_last=None, lengths=None, scale=None, dq=None, dk=None, dv=None):
+    """Gradients of q, k, v, g, beta and s0 from those of o (and of the last state); q to beta, lengths and scale as the forward pass had them.
+    dq, dk and dv: tensors for the results (the parts of a projection's gradient, say)."""
+    import torch
+    p, state = _delta_shape(q, k, v, g, beta, lengths, scale)
+    device = q.device
+    _packed_rows(_same(kept, "kept", torch.float32, (-(-p.T // DELTA_INTERVAL), *state), device), "kept")
+    _same(do, "do", v.dtype, v.shape, device)
+    if ds_last is not None:
+        _packed_rows(_same(ds_last, "ds_last", torch.float32, state, device), "ds_last")
+    dq, dk, dv = _out(dq, "dq", q), _out(dk, "dk", k), _out(dv, "dv", v)
+    p.ld_o, p.ld_dq, p.ld_dk, p.ld_dv = _ld_heads(do, "do"), _ld_heads(dq, "dq"), _ld_heads(dk, "dk"), _ld_heads(dv, "dv")
+    dg, dbeta = torch.empty_like(g), torch.empty_like(beta)
+    ds0 = torch.empty(state, dtype=torch.float32, device=device)
+    at, space = _launch(device, _entry("snn_delta_workspace")(C.byref(p), 1))
+    _run("snn_delta_backward", C.byref(at), C.byref(p), _at(q), _at(k), _at(v), _at(g), _at(beta), _at(kept), _at(do), _at(ds_last), _at(dq), _at(dk), _at(dv),
+         _at(dg), _at(dbeta), _at(ds0))
+    return dq, dk, dv, dg, dbeta, ds0
 
 
 def _rows(x, name):

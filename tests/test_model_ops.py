@@ -404,6 +404,405 @@ def test_adamw_moves_the_weights_of_a_network():
     net.snn_destroy()
 
 
+# ---- gated delta rule ---------------------------------------------------------------------------
+def delta_plain(q, k, v, g, beta, s0, lengths, scale):
+    """Step by step, differentiable."""
+    T, B, H = g.shape
+    heads = torch.arange(H) // (H // q.shape[2])
+    S, o, kept = s0, [], []
+    for t in range(T):
+        if t % 256 == 0:
+            kept.append(S)
+        on = (t < lengths)[:, None, None, None]
+        kt, qt = k[t][:, heads], q[t][:, heads]
+        held = torch.exp(g[t])[..., None, None] * S
+        u = beta[t][..., None] * (v[t] - (held * kt[..., None]).sum(-2))
+        S = torch.where(on, held + kt[..., None] * u[..., None, :], S)
+        o.append(torch.where(on[..., 0], scale * (S * qt[..., None]).sum(-2), 0.0))
+    return torch.stack(o) if T else torch.zeros_like(v), S, torch.stack(kept) if T else S[None][:0]
+
+
+def delta_inputs(T, B, H, K, dk, dv, dtype, ragged=False, seed=1):
+    g = torch.Generator().manual_seed(seed)
+    rand = lambda *x: torch.randn(x, generator=g)  # noqa: E731
+    q, k = rand(T, B, K, dk), rand(T, B, K, dk) + 0.5 * rand(1, B, K, dk)
+    q, k = ((x / x.norm(dim=-1, keepdim=True)).to(dtype) for x in (q, k))
+    x = dict(q=q, k=k, v=rand(T, B, H, dv).to(dtype), g=-torch.nn.functional.softplus(rand(T, B, H) - 1) * torch.exp(-3 * torch.rand(H, generator=g)),
+             beta=torch.sigmoid(rand(T, B, H)))
+    s0, do, ds = rand(B, H, dk, dv), rand(T, B, H, dv).to(dtype), rand(B, H, dk, dv)
+    lengths = torch.full((B,), T, dtype=torch.int32)
+    if ragged:
+        lengths = torch.randint(0, T + 1, (B,), generator=g, dtype=torch.int32)
+        lengths[0], lengths[-1] = T, 0
+        pad = torch.arange(T)[:, None] >= lengths[None, :]
+        for a in (*x.values(), do):
+            a[pad] = math.nan  # nothing may read these
+    return [a.cuda() for a in x.values()], s0.cuda(), do.cuda(), ds.cuda(), lengths.cuda()
+
+
+def clean(a, lengths):
+    """In 64 bits on the CPU, zeros behind the ends."""
+    a = a.cpu().double()
+    return torch.where((torch.arange(a.shape[0])[:, None] < lengths.cpu()[None, :]).view(*a.shape[:2], *[1] * (a.dim() - 2)), a, 0.0)
+
+
+def delta_tol(dtype, T, dk, times):
+    """What results may be off by, to their 2-norm.  Roundings of either sign add up as the root of their number: sums over dk and over 64 steps, twice
+    each, and those of up to 16 chunks that a state remembers; with bf16 also what two parts leave of a factor (2^-17 at most), of up to eight
+    factors in each of the chunks.  Four times that, for what adds up in one direction; `times` as much where such results are factors again."""
+    chunks = min(T / 64 + 1, 16)
+    return times * 4 * (U * math.sqrt(2 * (dk + 64) * chunks) + (0 if dtype == torch.float32 else 2.0 ** -18 * math.sqrt(8 * chunks)))
+
+
+def close(got, want, tol, what):
+    """To the 2-norm, and each element to 30 times the root mean square besides its own rounding."""
+    got_, want = got.double().cpu(), want.double()
+    assert got_.shape == want.shape, what
+    if not want.numel():
+        return
+    off, norm = (got_ - want).norm().item(), want.norm().item()
+    assert off <= (tol + HALF[got.dtype]) * norm, (what, off / max(norm, 1e-300), tol)
+    rest = ((got_ - want).abs() - HALF[got.dtype] * want.abs()).max().item()
+    assert rest <= 30 * tol * norm / math.sqrt(want.numel()), (what, rest, norm)
+
+
+DELTA = [(0, 2, 3, 3, 5, 7, False), (1, 2, 3, 3, 5, 7, False), (1, 64, 4, 2, 128, 128, False), (3, 2, 2, 1, 65, 130, True), (16, 2, 4, 4, 128, 64, True),
+         (17, 1, 2, 2, 16, 16, False), (63, 2, 1, 1, 1, 1, False), (64, 2, 2, 2, 64, 64, False), (65, 3, 3, 1, 48, 75, True), (130, 3, 2, 2, 33, 31, True),
+         (256, 1, 2, 2, 128, 128, False), (257, 3, 2, 1, 64, 100, True), (300, 5, 4, 2, 128, 40, True), (700, 1, 1, 1, 100, 256, False),
+         (200, 4, 6, 2, 72, 33, True), (128, 8, 8, 8, 32, 96, False)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,B,H,K,dk,dv,ragged", DELTA)
+def test_delta_forward(T, B, H, K, dk, dv, ragged, dtype):
+    x, s0, _, _, lengths = delta_inputs(T, B, H, K, dk, dv, dtype, ragged)
+    given = lengths if ragged else None
+    o, last, kept = snn.snn_delta_forward(*x, s0, lengths=given, keep=True)
+    c, tol = [clean(a, lengths) for a in x], delta_tol(dtype, T, dk, 1)
+    want = delta_plain(*c, s0.cpu().double(), lengths.cpu(), dk ** -0.5)
+    for got, ref, what in zip((o, last, kept), want, ("o", "last", "kept")):
+        close(got, ref, tol, what)
+    assert (o[torch.arange(T, device="cuda")[:, None] >= lengths[None, :]] == 0).all()
+    if T:
+        close(snn.snn_delta_forward(*x, None, lengths=given, scale=2.0)[0], delta_plain(*c, 0 * s0.cpu().double(), lengths.cpu(), 2.0)[0], tol, "from zero")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,B,H,K,dk,dv,ragged", DELTA)
+def test_delta_backward(T, B, H, K, dk, dv, ragged, dtype):
+    x, s0, do, ds, lengths = delta_inputs(T, B, H, K, dk, dv, dtype, ragged, seed=2)
+    given = lengths if ragged else None
+    c = [clean(a, lengths).requires_grad_() for a in x]
+    S = s0.cpu().double().requires_grad_()
+    o, last, kept = delta_plain(*c, S, lengths.cpu(), dk ** -0.5)
+    f = (o * clean(do, lengths)).sum()
+    got = snn.snn_delta_backward(*x, kept.detach().float().cuda(), do, ds, lengths=given)
+    want = torch.autograd.grad(f + (last * ds.cpu().double()).sum(), (*c, S), retain_graph=True, allow_unused=True)
+    tol = delta_tol(dtype, T, dk, 3)
+    for a, b, y, what in zip(got, want, (*c, S), ("dq", "dk", "dv", "dg", "dbeta", "ds0")):
+        close(a, torch.zeros_like(y) if b is None else b, tol, what)
+    behind = torch.arange(T, device="cuda")[:, None] >= lengths[None, :]
+    assert all((a[behind] == 0).all() for a in got[:5])
+    if T:
+        none = snn.snn_delta_backward(*x, kept.detach().float().cuda(), do, lengths=given)
+        for a, b, what in zip(none, torch.autograd.grad(f, (*c, S)), ("dq", "dk", "dv", "dg", "dbeta", "ds0")):
+            close(a, b, tol, what + " without ds_last")
+
+
+@gpu
+def test_delta_gradients_are_differences():
+    T, B, H, K, dk, dv = 70, 1, 2, 1, 6, 5
+    x, s0, do, ds, lengths = delta_inputs(T, B, H, K, dk, dv, torch.float32, seed=3)
+    c, S = [clean(a, lengths) for a in x], s0.cpu().double()
+    kept = snn.snn_delta_forward(*x, s0, keep=True)[2]
+    got = snn.snn_delta_backward(*x, kept, do, ds)
+
+    def f(*a):
+        o, last, _ = delta_plain(*a, lengths.cpu(), dk ** -0.5)
+        return ((o * do.cpu().double()).sum() + (last * ds.cpu().double()).sum()).item()
+
+    every, d = [*c, S], 1e-5
+    for i, a in enumerate(got):
+        for at in (0, every[i].numel() // 2, every[i].numel() - 1):
+            e = torch.zeros_like(every[i]).flatten()
+            e[at] = d
+            e = e.view(every[i].shape)
+            diff = (f(*every[:i], every[i] + e, *every[i + 1:]) - f(*every[:i], every[i] - e, *every[i + 1:])) / (2 * d)
+            # (a third derivative of up to 1e3 gradients times d^2, and 1e-14 of f over d)
+            assert abs(diff - a.flatten()[at].item()) <= 1e-5 * max(1.0, a.abs().max().item()), (i, at)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_delta_state_in_place_is_a_sequence_cut_anywhere(dtype):
+    x, s0, _, _, lengths = delta_inputs(300, 2, 4, 2, 72, 90, dtype, seed=4)
+    whole, last, _ = snn.snn_delta_forward(*x, s0)
+    state = s0.clone()
+    parts = [snn.snn_delta_forward(*[y[a:b].contiguous() for y in x], state, s_last=state)[0] for a, b in ((0, 1), (1, 2), (2, 20), (20, 100), (100, 300))]
+    tol = 2 * delta_tol(dtype, 300, 72, 1)
+    close(torch.cat(parts), whole.cpu(), tol + HALF[dtype], "o")
+    close(state, last.cpu(), tol, "state")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T", [5, 150])
+def test_delta_parts_of_a_projection(T, dtype):
+    B, H, K, dk, dv = 3, 4, 2, 24, 40
+    x, s0, do, ds, lengths = delta_inputs(T, B, H, K, dk, dv, dtype, seed=5)
+    want = snn.snn_delta_forward(*x, s0, keep=True)
+    back = snn.snn_delta_backward(*x, want[2], do, ds)
+    sizes = [K * dk, K * dk, H * dv, H * dv, 3]
+    wide, grads = (torch.full((T, B, sum(sizes)), math.nan, dtype=dtype, device="cuda") for _ in range(2))
+    part = lambda w: [p.view(T, B, n, -1) for p, n in zip(w.split(sizes, -1), (K, K, H, H))]  # noqa: E731
+    q, k, v, o = part(wide)
+    for to, y in zip((q, k, v), x):
+        to.copy_(y)
+    assert same(snn.snn_delta_forward(q, k, v, *x[3:], s0, keep=True, o=o), want)
+    dq, dk_, dv_, do_ = part(grads)
+    do_.copy_(do)
+    assert same(snn.snn_delta_backward(q, k, v, *x[3:], want[2], do_, ds, dq=dq, dk=dk_, dv=dv_), back)
+    assert torch.isnan(wide[..., -3:]).all() and torch.isnan(grads[..., -3:]).all()
+
+
+@gpu
+def test_delta_lengths_outside_count_as_the_nearer_end():
+    for T in (10, 100):
+        x, s0, do, ds, _ = delta_inputs(T, 4, 2, 2, 20, 30, torch.float32, seed=6)
+        lengths = torch.tensor([-5, T + 7, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda")
+        inside = torch.tensor([0, T, T, 0], dtype=torch.int32, device="cuda")
+        got, want = (snn.snn_delta_forward(*x, s0, lengths=v, keep=True) for v in (lengths, inside))
+        assert same(got, want) and same(*(snn.snn_delta_backward(*x, want[2], do, ds, lengths=v) for v in (lengths, inside)))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T", [12, 200])
+def test_delta_equal_keys(T, dtype):
+    # one key again and again with beta = 1: a step writes over what the last one wrote, and reads its own value
+    x, s0, _, _, lengths = delta_inputs(T, 2, 2, 2, 32, 48, dtype, seed=7)
+    key = torch.zeros(32, dtype=dtype, device="cuda")
+    key[:4] = 0.5
+    x[0][:], x[1][:] = key, key
+    x[3].zero_()
+    x[4].fill_(1.0)
+    o, last, _ = snn.snn_delta_forward(*x, None, scale=1.0)
+    # differences of neighbouring values, each off by a few roundings
+    near(o, x[2].cpu(), (16 * U if dtype == torch.float32 else 2.0 ** -15) * 2 * x[2].cpu().double().abs().max(), "o")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_delta_gates_at_their_ends(dtype):
+    # decays that forget all (minus infinity, and sums of them that 32 bits would round), none at all, beta 0 and 1
+    T = 150
+    x, s0, do, ds, lengths = delta_inputs(T, 2, 3, 3, 40, 40, dtype, seed=8)
+    g, beta = x[3], x[4]
+    g[::7] = -60.0
+    g[30], g[100, 0] = -math.inf, -math.inf
+    g[5:9], g[70:90] = 0.0, -1e-4
+    beta[::3], beta[1::5] = 0.0, 1.0
+    o, last, kept = snn.snn_delta_forward(*x, s0, keep=True)
+    c = [clean(a, lengths) for a in x]
+    tol = delta_tol(dtype, T, 40, 1)
+    want = delta_plain(*c, s0.cpu().double(), lengths.cpu(), 40 ** -0.5)
+    close(o, want[0], tol, "o")
+    close(last, want[1], tol, "last")
+    c[3] = c[3].clamp(min=-1e4)  # (exp of it is 0; the gradient of minus infinity would be 0 times infinity)
+    c = [a.requires_grad_() for a in c]
+    S = s0.cpu().double().requires_grad_()
+    o, last, _ = delta_plain(*c, S, lengths.cpu(), 40 ** -0.5)
+    want = torch.autograd.grad((o * do.cpu().double()).sum() + (last * ds.cpu().double()).sum(), (*c, S))
+    for a, b, what in zip(snn.snn_delta_backward(*x, kept, do, ds), want, ("dq", "dk", "dv", "dg", "dbeta", "ds0")):
+        close(a, b, 3 * tol, what)
+
+
+@gpu
+@pytest.mark.parametrize("T", [4, 90])
+def test_delta_values_that_are_not_finite_stay_in_their_heads(T):
+    x, s0, do, ds, _ = delta_inputs(T, 3, 4, 2, 20, 30, torch.float32, seed=9)
+    want = snn.snn_delta_forward(*x, s0, keep=True)
+    back = snn.snn_delta_backward(*x, want[2], do, ds)
+    x[2][2, 1, 3, 4] = math.nan
+    s0[0, 2, 3, 5] = math.inf
+    got = snn.snn_delta_forward(*x, s0, keep=True)
+    bad = torch.zeros(3, 4, dtype=torch.bool, device="cuda")
+    bad[1, 3] = bad[0, 2] = True
+    assert torch.equal(got[0][:, ~bad], want[0][:, ~bad]) and torch.equal(got[1][~bad], want[1][~bad])
+    assert not torch.isfinite(got[1][1, 3, :, 4]).any()
+    grads = snn.snn_delta_backward(*x, got[2], do, ds)
+    keys = ~bad.view(3, 2, 2).any(2)
+    assert all(torch.equal(a[:, keys], b[:, keys]) for a, b in zip(grads[:2], back[:2]))
+    assert all(torch.equal(a[:, ~bad], b[:, ~bad]) for a, b in zip(grads[2:5], back[2:5])) and torch.equal(grads[5][~bad], back[5][~bad])
+
+
+@gpu
+def test_delta_no_gradient_behind_an_end_whatever_that_of_the_state():
+    x, s0, do, ds, _ = delta_inputs(100, 2, 2, 2, 20, 30, torch.float32, seed=10)
+    lengths = torch.tensor([70, 0], dtype=torch.int32, device="cuda")
+    kept = snn.snn_delta_forward(*x, s0, lengths=lengths, keep=True)[2]
+    ds[:, 0] = math.inf
+    grads = snn.snn_delta_backward(*x, kept, do, ds, lengths=lengths)
+    assert all((a[70:, 0] == 0).all() and (a[:, 1] == 0).all() for a in grads[:5]) and torch.equal(grads[5][1], ds[1])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_delta_pieces_of_long_sequences(dtype):
+    # more than the workspace holds at once: the same bits as calls for parts of the sequence, which fit
+    T, B, H = 64 * 160, 2, 32
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *x: torch.randn(x, generator=g, device="cuda")  # noqa: E731
+    q, k = (torch.nn.functional.normalize(rand(T, B, H, 128), dim=-1).to(dtype) for _ in range(2))
+    x = [q, k, rand(T, B, H, 64).to(dtype), -0.1 * rand(T, B, H).abs(), torch.sigmoid(rand(T, B, H))]
+    do, ds = rand(T, B, H, 64).to(dtype), rand(B, H, 128, 64)
+    p = ops.snn_delta(T, B, H, H, 128, 64, ops.SNN_BF16 if dtype == torch.bfloat16 else ops.SNN_F32, 1.0)
+    half = ops.snn_delta(512, B, H, H, 128, 64, p.dtype, 1.0)
+    size = snn.lib().snn_delta_workspace
+    assert size(C.byref(p), 0) < 20 * size(C.byref(half), 0) and size(C.byref(p), 1) < 20 * size(C.byref(half), 1)
+    o, last, kept = snn.snn_delta_forward(*x, keep=True)
+    grads = snn.snn_delta_backward(*x, kept, do, ds)
+    cuts = list(range(0, T, 512))
+    state = None
+    for a in cuts:
+        part = [y[a:a + 512] for y in x]
+        oo, state, kk = snn.snn_delta_forward(*part, state, keep=True)
+        assert torch.equal(oo, o[a:a + 512]) and torch.equal(kk, kept[a // 256:a // 256 + 2]), a
+    assert torch.equal(state, last)
+    for a in reversed(cuts):
+        part = snn.snn_delta_backward(*[y[a:a + 512] for y in x], kept[a // 256:a // 256 + 2].contiguous(), do[a:a + 512], ds)
+        ds = part[5]
+        assert same(part[:5], [y[a:a + 512] for y in grads[:5]]), a
+    assert torch.equal(ds, grads[5])
+
+
+@gpu
+def test_delta_beyond_4_gb():
+    T, B, H, dv = 32768 + 16, 8, 64, 128  # 2^31 elements and more of v, of o
+    g = torch.Generator(device="cuda").manual_seed(4)
+    q, k = (torch.nn.functional.normalize(torch.randn((T, B, 1, 32), generator=g, device="cuda"), dim=-1).bfloat16() for _ in range(2))
+    v = torch.empty((T, B, H, dv), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    gates = -0.2 * torch.rand((T, B, H), generator=g, device="cuda")
+    beta = torch.rand((T, B, H), generator=g, device="cuda")
+    x = [q, k, v, gates, beta]
+    o, last, _ = snn.snn_delta_forward(*x)
+    # the last 16 steps by themselves, from a state 500 steps back: nothing that is older is left of it
+    first = [y[T - 516:T - 16] for y in x]
+    state = snn.snn_delta_forward(*first)[1]
+    end, state, _ = snn.snn_delta_forward(*[y[T - 16:] for y in x], state)
+    tol = 2 * delta_tol(torch.bfloat16, 500, 32, 1)
+    close(o[T - 16:], end.cpu(), tol + HALF[torch.bfloat16], "o")
+    close(last, state.cpu(), tol, "last")
+
+
+@gpu
+@pytest.mark.parametrize("T", [1, 100])
+def test_delta_in_a_graph(T):
+    x, s0, do, ds, lengths = delta_inputs(T, 3, 4, 2, 40, 50, torch.bfloat16, ragged=T > 1, seed=11)
+    state = s0.clone()
+
+    def run():
+        o, last, kept = snn.snn_delta_forward(*x, state, lengths=lengths, keep=True)
+        return o, last, kept, *snn.snn_delta_backward(*x, kept, do, ds, lengths=lengths)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for i in range(3):
+        state.mul_(0.5)
+        x[2].mul_(1.25)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(got, run())
+
+
+@gpu
+def test_delta_on_another_stream_and_from_two_threads():
+    import threading
+    cases = [delta_inputs(200, 2, 4, 4, 64, 64, torch.bfloat16, seed=s) for s in (12, 13)]
+
+    def run(case):
+        x, s0, do, ds, _ = case
+        o, last, kept = snn.snn_delta_forward(*x, s0, keep=True)
+        return o, last, *snn.snn_delta_backward(*x, kept, do, ds)
+
+    want, got = [run(c) for c in cases], [None, None]
+    torch.cuda.synchronize()
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(10):
+                got[i] = run(cases[i])
+        stream.synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert all(same(a, b) for a, b in zip(got, want))
+
+
+# ---- all of them together -------------------------------------------------------------------------
+@gpu
+def test_a_model_of_norms_delta_rule_and_vocabulary_takes_a_step():
+    T, B, H, dk, dv, d, vocab = 80, 2, 2, 16, 24, 40, 101
+    g = torch.Generator().manual_seed(5)
+    rand = lambda *x: torch.randn(x, generator=g)  # noqa: E731
+    sizes = [H * dk, H * dk, H * dv, H, H]
+    params = [p.cuda() for p in (rand(vocab, d), 1 + 0.1 * rand(d), rand(d, sum(sizes)) / d ** 0.5, rand(H * dv, d) / 7, 1 + 0.1 * rand(d))]
+    tokens = torch.randint(0, vocab, (T + 1, B), generator=g).cuda()
+    targets = tokens[1:].flatten().int()
+
+    def gates(z):
+        q, k, v, a, b = z.split(sizes, -1)
+        q, k = (torch.nn.functional.normalize(y.unflatten(-1, (H, dk)), dim=-1) for y in (q, k))
+        return q, k, v.unflatten(-1, (H, dv)), -torch.nn.functional.softplus(a), torch.sigmoid(b)
+
+    def plain(table, w1, up, down, w2):
+        norm = lambda s, w: w * s / torch.sqrt((s * s).mean(-1, keepdim=True) + 1e-6)  # noqa: E731
+        x = table[tokens[:-1].cpu()]
+        o = delta_plain(*gates(norm(x, w1) @ up), torch.zeros(B, H, dk, dv, dtype=torch.float64), torch.full((B,), T), dk ** -0.5)[0]
+        y = norm(x + o.flatten(2) @ down, w2).flatten(0, 1)
+        return torch.nn.functional.cross_entropy(y @ table.T, targets.cpu().long())
+
+    # the library's calls, and torch for the products between
+    table, w1, up, down, w2 = params
+    x = table[tokens[:-1]]
+    y1, _ = snn.snn_norm_forward(x, w1)
+    z = (y1 @ up).requires_grad_()
+    layer = gates(z)
+    held = [y.detach().contiguous() for y in layer]
+    o, _, kept = snn.snn_delta_forward(*held, keep=True)
+    y2, total = snn.snn_norm_forward(o.flatten(2) @ down, w2, residual=x)
+    loss, state = snn.snn_vocab_loss(y2.flatten(0, 1), table, targets)
+    dy2, dtable = snn.snn_vocab_loss_grad(y2.flatten(0, 1), table, targets, state)
+    dtotal, dw2 = snn.snn_norm_backward(total, w2, dy2.view_as(total))
+    ddown = o.flatten(2).flatten(0, 1).T @ dtotal.flatten(0, 1)
+    back = snn.snn_delta_backward(*held, kept, (dtotal @ down.T).view_as(o))
+    dz, = torch.autograd.grad(layer, z, back[:5])
+    dup = y1.flatten(0, 1).T @ dz.flatten(0, 1)
+    dx, dw1 = snn.snn_norm_backward(x, w1, dz @ up.T, dtotal=dtotal)
+    dtable = dtable.index_add(0, tokens[:-1].flatten(), dx.flatten(0, 1))
+    grads = [dtable, dw1, dup, ddown, dw2]
+    double = [p.cpu().double().requires_grad_() for p in params]
+    want = plain(*double)
+    assert abs(loss.double().mean().item() - want.item()) <= 2e-5 * want.item()  # (the root mean square of its logits' errors is 1e-6)
+    reference = torch.autograd.grad(want, double)
+    for a, b, what in zip(grads, reference, ("table", "w1", "up", "down", "w2")):
+        close(a, b, 3 * delta_tol(torch.float32, T, d, 3), what)
+    # and the step that they make
+    plan = snn.snn_adamw_plan(params, *snn.snn_adamw_moments(params))
+    before = [p.cpu().double() for p in params]
+    snn.snn_adamw_step(plan, grads, 1, lr=1e-2)
+    for p, x, a in zip(params, before, grads):
+        want = adamw_plain(x, a.cpu().double(), 0 * x, 0 * x, 1, 1e-2, (0.9, 0.999), 1e-8, 0.01)
+        near(p, want[0], want[3], "step")
+
+
 # ---- refusals -----------------------------------------------------------------------------------
 def refused(call, text):
     with pytest.raises(snn.SnnError) as e:
@@ -489,3 +888,50 @@ def test_binding_of_norm_and_adamw_refuses_tensors_that_do_not_fit():
             (lambda: snn.snn_adamw_step(plan, [f(40)], 1), ValueError)):                        # on the CPU
         with pytest.raises(kind):
             call()
+
+
+def test_c_entry_points_of_the_delta_rule_refuse_what_they_cannot_run():
+    L, at = snn.lib(), ops.snn_launch(0, None, None, 0)
+    here = C.cast(C.create_string_buffer(4096), C.c_void_p).value
+
+    def shape(**k):
+        return C.byref(ops.snn_delta(**{**dict(T=20, batch=2, heads=4, key_heads=2, dk=8, dv=8, dtype=0, scale=1.0), **k}))
+
+    for name, count in (("snn_delta_forward", 9), ("snn_delta_backward", 14)):
+        def call(p, launch=C.byref(at), first=here):
+            ops._run(name, launch, p, first, *[here] * (count - 1))
+        refused(lambda: call(shape(), None), "no device")
+        refused(lambda: call(None), "no shape")
+        refused(lambda: call(shape(dtype=2)), "unknown type 2")
+        refused(lambda: call(shape(T=-1)), "T = -1")
+        for bad in (dict(key_heads=3), dict(heads=0), dict(key_heads=0), dict(key_heads=-2)):
+            refused(lambda: call(shape(**bad)), "multiple")
+        for bad in (dict(dk=0), dict(dk=129), dict(dv=0), dict(dv=1025)):
+            refused(lambda: call(shape(**bad)), "1024")
+        for bad in (dict(batch=0), dict(batch=1 << 20), dict(batch=1 << 17, dv=1024)):
+            refused(lambda: call(shape(**bad)), "2^20")
+        refused(lambda: call(shape(scale=math.inf)), "scale")
+        for bad in (dict(ld_q=15), dict(ld_v=31), dict(ld_dv=-1), dict(ld_o=1 << 31)):
+            refused(lambda: call(shape(**bad)), "elements from row to row")
+        refused(lambda: call(shape(), first=None), "q is NULL")
+        refused(lambda: call(shape(), first=here + 2), "not aligned")
+        refused(lambda: call(shape()), "not in")
+    assert L.snn_delta_workspace(shape(dk=0), 0) == 0 and L.snn_delta_workspace(shape(), 1) > L.snn_delta_workspace(shape(), 0) > 0
+    assert L.snn_delta_workspace(shape(T=1), 0) == 0
+
+
+def test_binding_of_the_delta_rule_refuses_tensors_that_do_not_fit():
+    f = torch.zeros
+    x = dict(q=f(4, 2, 2, 8), k=f(4, 2, 2, 8), v=f(4, 2, 4, 6), g=f(4, 2, 4), beta=f(4, 2, 4))
+    wide = f(4, 2, 2, 16)[..., ::2]
+    for change, kind in ((dict(), ValueError), (dict(q=f(4, 2, 16)), ValueError), (dict(k=f(4, 2, 2, 7)), ValueError), (dict(v=f(4, 3, 4, 6)), ValueError),
+                         (dict(v=f(4, 2, 4, 6, dtype=torch.bfloat16)), TypeError), (dict(g=f(4, 2, 2)), ValueError),
+                         (dict(beta=f(4, 2, 4, dtype=torch.bfloat16)), TypeError), (dict(q=wide), ValueError), (dict(k=f(4, 2, 2, 16)[..., :8]), ValueError),
+                         (dict(q=f(2, 4, 2, 8).transpose(0, 1)), ValueError), (dict(s0=f(2, 4, 6, 8)), ValueError), (dict(s_last=f(2, 4, 8, 5)), ValueError),
+                         (dict(lengths=f(2)), TypeError), (dict(o=f(4, 2, 4, 7)), ValueError)):
+        with pytest.raises(kind):
+            snn.snn_delta_forward(**{**x, **change})
+    for change, kind in ((dict(), ValueError), (dict(kept=f(2, 2, 4, 8, 6)), ValueError), (dict(do=f(4, 2, 4, 5)), ValueError),
+                         (dict(ds_last=f(2, 4, 8, 6, dtype=torch.float64)), TypeError), (dict(dk=f(4, 2, 2, 9)), ValueError)):
+        with pytest.raises(kind):
+            snn.snn_delta_backward(**{**x, **dict(kept=f(1, 2, 4, 8, 6), do=f(4, 2, 4, 6)), **change})
