@@ -76,6 +76,17 @@ template <int PA, int PB> __device__ __forceinline__ void multiply(tile &acc, co
     for (int i = 0; i <= s; ++i)
       if (i < PA && s - i < PB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], acc, 0, 0, 0);
 }
+// Several columns' products in turn: none waits for the one before
+template <int PA, int PB, int N> __device__ __forceinline__ void multiply(tile (&acc)[N], const Operand<PA> &a, const Operand<PB> (&b)[N]) {
+  constexpr int MOST = PA > PB ? PA : PB;
+#pragma unroll
+  for (int s = MOST - 1; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i <= s; ++i)
+      if (i < PA && s - i < PB)
+#pragma unroll
+        for (int n = 0; n < N; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b[n].p[s - i], acc[n], 0, 0, 0);
+}
 template <int P, int N> __device__ __forceinline__ void split(const float (&x)[N], __bf16 (&to)[P][N]) {
 #pragma unroll
   for (int j = 0; j < N; ++j) {
@@ -117,6 +128,10 @@ template <int P, int ROWS, int STRIDE> struct Planes {
     for (int i = 0; i < P; ++i) r.p[i] = *(const frag *)(e[i] + row * STRIDE + col);
     return r;
   }
+  template <int N> __device__ __forceinline__ void get(int row, int col, Operand<P> (&r)[N]) const { // of every 16th row
+#pragma unroll
+    for (int n = 0; n < N; ++n) r[n] = get(row + 16 * n, col);
+  }
   // four elements of a row
   __device__ __forceinline__ void put(int row, int col, const tile &x) {
     const float v[4] = {x[0], x[1], x[2], x[3]};
@@ -132,7 +147,53 @@ template <int P, int ROWS, int STRIDE> struct Planes {
   }
 };
 
+__device__ __forceinline__ void lds_barrier() { // of the LDS alone: loads from memory stay in flight
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 template <class T> __device__ __forceinline__ float element(const T *p, bool on) { return on ? (float)*p : 0.f; }
+// Four rows of a chunk and every 16th column.  They are asked for as they are in memory and made values of when they are used, which is what waits for them.
+// What is beside the array is read from its last row and column instead, without a branch for each, and is zeros then.
+template <class T, int N> struct Values {
+  typedef typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type Bits;
+  Bits raw[4][N];
+  __device__ __forceinline__ void ask(const void *p, long long ld, const Args &a, int b, int t, int first, int col, int cols) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const Bits *row = (const Bits *)p + ((long long)min(t + e, a.T - 1) * a.batch + b) * ld + first;
+#pragma unroll
+      for (int n = 0; n < N; ++n) raw[e][n] = row[min(col + 16 * n, cols - 1)];
+    }
+  }
+  __device__ __forceinline__ tile get(int n, int t, int len, int col, int cols) const {
+    tile v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = sizeof(T) == 2 ? __uint_as_float((uint32_t)raw[e][n] << 16) : __uint_as_float((uint32_t)raw[e][n]);
+      v[e] = t + e < len && col + 16 * n < cols ? x : 0.f;
+    }
+    return v;
+  }
+};
+// and back; `whole`: all of them are there
+template <class T, int N> __device__ __forceinline__ void values_to(void *p, long long ld, const Args &a, int b, int t, int len, int first, int col, int cols, bool whole,
+                                                                    const tile (&v)[N]) {
+  T *to = (T *)p + ((long long)t * a.batch + b) * ld + first + col;
+  const long long step = (long long)a.batch * ld;
+  if (whole) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int n = 0; n < N; ++n) to[e * step + 16 * n] = (T)v[n][e];
+  } else
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        if (t + e < a.T && col + 16 * n < cols) to[e * step + 16 * n] = (T)(t + e < len ? v[n][e] : 0.f);
+}
 
 // ---- a chunk by itself ------------------------------------------------------------------------
 template <class T, int DK, bool BACK> __global__ __launch_bounds__(256) void k_chunk(Args a) {
@@ -339,14 +400,54 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) v
         }
   };
   const int c0 = REC ? segment * KEPT : 0, c1 = REC ? min(c0 + KEPT, a.chunks) : a.chunks;
+  const int row0 = 16 * w + 4 * q4;
+  // What the next chunk needs is on its way while this one is worked on: each part is asked for as soon as this chunk's has been used.
+  Operand<PI> k[KK], q[REC ? 1 : KK], kt[RT][2];
+  Operand<PC> am[2], pm[2];
+  Values<T, NT> v;
+  tile gam, tail, beta;
+  float end;
+  auto of_keys = [&](int c) { return (((long long)c * a.batch + b) * a.key_heads + kh) * (DK * C * PI); };
+  auto of_head = [&](int c) { return ((long long)c * a.batch + b) * a.heads + h; };
+  auto ask_rows = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < KK; ++i) {
+      k[i] = fetch<PI>(a.kf + of_keys(c), w * KK + i, lane);
+      if constexpr (!REC) q[i] = fetch<PI>(a.qf + of_keys(c), w * KK + i, lane);
+    }
+  };
+  auto ask_values = [&](int c) {
+    v.ask(a.v, a.ld_v, a, b, (a.first + c) * C + row0, h * a.dv, v0 + r, a.dv);
+  };
+  auto ask_squares = [&](const __bf16 *p, int c, Operand<PC> (&m)[2]) { // (lower triangular: the first two rows of blocks have zeros behind)
+    m[0] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w, lane);
+    if (w > 1) m[1] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w + 1, lane);
+  };
+  auto ask_columns = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) kt[i][j] = fetch<PI>(a.ktf + of_keys(c), 2 * (w * RT + i) + j, lane);
+  };
+  auto ask_gates = [&](int c) {
+    const float *gates = a.gates + of_head(c) * (3 * C);
+    gam = *(const tile *)(gates + row0), tail = *(const tile *)(gates + C + row0), beta = *(const tile *)(gates + 2 * C + row0);
+    end = gates[C - 1];
+  };
+  if (c0 < c1) {
+    ask_gates(c0);
+    ask_rows(c0);
+    ask_values(c0);
+    ask_squares(a.af, c0, am);
+    if constexpr (!REC) ask_squares(a.pf, c0, pm);
+    ask_columns(c0);
+  }
   for (int c = c0; c < c1; ++c) {
-    const int t0 = (a.first + c) * C;
-    const long long of_k = ((long long)c * a.batch + b) * a.key_heads + kh, of = ((long long)c * a.batch + b) * a.heads + h;
-    const float *gates = a.gates + of * (3 * C);
+    const int t0 = (a.first + c) * C, next = min(c + 1, c1 - 1);
     if constexpr (!REC) {
       if (a.kept && (a.first + c) % KEPT == 0) state_to(a.kept + ((long long)((a.first + c) / KEPT) * per + u.of) * a.dk * a.dv);
     } else {
-      float *to = a.before + of * DK * a.dvp;
+      float *to = a.before + of_head(c) * DK * a.dvp;
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -354,58 +455,48 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) v
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
-            if (col < a.dvp) to[row * a.dvp + col] = s[i][n][e];
+            if (v0 + 16 * n < a.dvp) to[row * a.dvp + col] = s[i][n][e];
           }
     }
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
       for (int n = 0; n < NT; ++n) st.put(16 * n + r, 16 * (w * RT + i) + 4 * q4, s[i][n]);
-    float v[NT][4];
-    const int row0 = 16 * w + 4 * q4;
-    const T *vp = (const T *)a.v + ((long long)(t0 + row0) * a.batch + b) * a.ld_v + h * a.dv + v0 + r;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[n][e] = element(vp + (long long)e * a.batch * a.ld_v + 16 * n, t0 + row0 + e < len && v0 + 16 * n + r < a.dv);
-    const tile gam = *(const tile *)(gates + row0), tail = *(const tile *)(gates + C + row0), beta = *(const tile *)(gates + 2 * C + row0);
-    const float end = gates[C - 1];
-    __syncthreads();
+    lds_barrier();
     tile e[NT] = {}, o[NT] = {};
 #pragma unroll
     for (int i = 0; i < KK; ++i) {
-      const Operand<PI> k = fetch<PI>(a.kf + of_k * (DK * C * PI), w * KK + i, lane);
-      Operand<PI> q;
-      if constexpr (!REC) q = fetch<PI>(a.qf + of_k * (DK * C * PI), w * KK + i, lane);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const Operand<PC> y = st.get(16 * n + r, 32 * i + 8 * q4);
-        multiply(e[n], k, y);
-        if constexpr (!REC) multiply(o[n], q, y);
-      }
+      Operand<PC> y[NT];
+      st.get(r, 32 * i + 8 * q4, y);
+      multiply(e, k[i], y);
+      if constexpr (!REC) multiply(o, q[i], y);
     }
+    ask_rows(next);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+      const tile vn = v.get(n, t0 + row0, len, v0 + r, a.dv);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e[n][i] = fmaf(-gam[i], e[n][i], v[n][i]);
+      for (int i = 0; i < 4; ++i) e[n][i] = fmaf(-gam[i], e[n][i], vn[i]);
       et.put(16 * n + r, row0, e[n]);
     }
-    __syncthreads();
+    ask_values(next);
+    lds_barrier();
     tile x[NT] = {};
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       if (2 * j <= w) { // (A is lower triangular)
-        const Operand<PC> m = fetch<PC>(a.af + of * (C * C * PC), 2 * w + j, lane);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) multiply(x[n], m, et.get(16 * n + r, 32 * j + 8 * q4));
+        Operand<PC> y[NT];
+        et.get(r, 32 * j + 8 * q4, y);
+        multiply(x, am[j], y);
       }
+    ask_squares(a.af, next, am);
     if constexpr (REC) {
-      float *to = a.w + (of * C + row0) * a.dvp + v0 + r;
+      float *to = a.w + (of_head(c) * C + row0) * a.dvp + v0 + r;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (v0 + 16 * n + r < a.dvp) to[i * a.dvp + 16 * n] = x[n][i];
+          if (v0 + 16 * n < a.dvp) to[i * a.dvp + 16 * n] = x[n][i];
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -413,37 +504,33 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) v
       if constexpr (!REC) ut.put(16 * n + r, row0, un);
       wt.put(16 * n + r, row0, un * tail);
     }
-    __syncthreads();
+    lds_barrier();
     if constexpr (!REC) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) o[n] *= gam * a.scale;
 #pragma unroll
       for (int j = 0; j < 2; ++j)
         if (2 * j <= w) {
-          const Operand<PC> m = fetch<PC>(a.pf + of * (C * C * PC), 2 * w + j, lane);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) multiply(o[n], m, ut.get(16 * n + r, 32 * j + 8 * q4));
+          Operand<PC> y[NT];
+          ut.get(r, 32 * j + 8 * q4, y);
+          multiply(o, pm[j], y);
         }
-      T *op = (T *)a.o + ((long long)(t0 + row0) * a.batch + b) * a.ld_o + h * a.dv + v0 + r;
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (t0 + row0 + i < a.T && v0 + 16 * n + r < a.dv)
-            op[(long long)i * a.batch * a.ld_o + 16 * n] = (T)(t0 + row0 + i < len ? o[n][i] : 0.f);
+      ask_squares(a.pf, next, pm);
+      values_to<T, NT>(a.o, a.ld_o, a, b, t0 + row0, len, h * a.dv, v0 + r, a.dv, t0 + C <= len && v0 + BV <= a.dv, o);
     }
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
       for (int n = 0; n < NT; ++n) s[i][n] *= end;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j) {
+      Operand<PC> y[NT];
+      wt.get(r, 32 * j + 8 * q4, y);
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        const Operand<PI> k = fetch<PI>(a.ktf + of_k * (DK * C * PI), 2 * (w * RT + i) + j, lane);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) multiply(s[i][n], k, wt.get(16 * n + r, 32 * j + 8 * q4));
-      }
+      for (int i = 0; i < RT; ++i) multiply(s[i], kt[i][j], y);
+    }
+    ask_columns(next);
+    ask_gates(next);
   }
   if constexpr (!REC)
     if (a.to) state_to(a.to + (long long)u.of * a.dk * a.dv);
@@ -471,12 +558,60 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
           const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
           s[i][n][e] = element(a.from + ((long long)u.of * a.dk + row) * a.dv + col, row < a.dk && col < a.dv);
         }
+  const int row0 = 16 * w + 4 * q4;
+  // (as in k_walk)
+  Operand<PI> k[KK], kt[RT][2], qt[RT][2];
+  Operand<PC> am[2], pm[2];
+  Values<T, NT> raw; // of dO
+  tile made[NT], gam, tail, beta; // w
+  float end;
+  auto of_keys = [&](int c) { return (((long long)c * a.batch + b) * a.key_heads + kh) * (DK * C * PI); };
+  auto of_head = [&](int c) { return ((long long)c * a.batch + b) * a.heads + h; };
+  auto ask_rows = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < KK; ++i) k[i] = fetch<PI>(a.kf + of_keys(c), w * KK + i, lane);
+  };
+  auto ask_values = [&](int c) {
+    raw.ask(a.dout, a.ld_o, a, b, (a.first + c) * C + row0, h * a.dv, v0 + r, a.dv);
+  };
+  auto ask_made = [&](int c) {
+    const float *wp = a.w + (of_head(c) * C + row0) * a.dvp + v0 + r;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) made[n][e] = wp[e * a.dvp + 16 * n]; // (dvp is a multiple of the 32 columns of this kernel)
+  };
+  auto ask_squares = [&](const __bf16 *p, int c, Operand<PC> (&m)[2]) { // (upper triangular: the last two rows of blocks begin with zeros)
+    if (w < 2) m[0] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w, lane);
+    m[1] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w + 1, lane);
+  };
+  auto ask_columns = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        qt[i][j] = fetch<PI>(a.qtf + of_keys(c), 2 * (w * RT + i) + j, lane);
+        kt[i][j] = fetch<PI>(a.ktf + of_keys(c), 2 * (w * RT + i) + j, lane);
+      }
+  };
+  auto ask_gates = [&](int c) {
+    const float *gates = a.gates + of_head(c) * (3 * C);
+    gam = *(const tile *)(gates + row0), tail = *(const tile *)(gates + C + row0), beta = *(const tile *)(gates + 2 * C + row0);
+    end = gates[C - 1];
+  };
+  if (a.chunks) {
+    const int c = a.chunks - 1;
+    ask_gates(c);
+    ask_values(c);
+    ask_rows(c);
+    ask_squares(a.ptf, c, pm);
+    ask_made(c);
+    ask_squares(a.atf, c, am);
+    ask_columns(c);
+  }
   for (int c = a.chunks - 1; c >= 0; --c) {
-    const int t0 = (a.first + c) * C, row0 = 16 * w + 4 * q4;
-    const long long of_k = ((long long)c * a.batch + b) * a.key_heads + kh, of = ((long long)c * a.batch + b) * a.heads + h;
-    const float *gates = a.gates + of * (3 * C);
-    const tile gam = *(const tile *)(gates + row0), tail = *(const tile *)(gates + C + row0), beta = *(const tile *)(gates + 2 * C + row0);
-    const float end = gates[C - 1];
+    const int t0 = (a.first + c) * C, next = max(c - 1, 0);
+    const long long of = of_head(c);
     {
       float *to = a.after + of * DK * a.dvp;
 #pragma unroll
@@ -486,92 +621,91 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
           const int row = 16 * (w * RT + i) + 4 * q4, col = v0 + 16 * n + r;
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (col < a.dvp) to[(row + e) * a.dvp + col] = s[i][n][e];
+            if (v0 + 16 * n < a.dvp) to[(row + e) * a.dvp + col] = s[i][n][e];
           st.put(16 * n + r, row, s[i][n]);
         }
     }
-    const T *dp = (const T *)a.dout + ((long long)(t0 + row0) * a.batch + b) * a.ld_o + h * a.dv + v0 + r;
     tile given[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        given[n][e] = element(dp + (long long)e * a.batch * a.ld_o + 16 * n, t0 + row0 + e < len && v0 + 16 * n + r < a.dv);
+      given[n] = raw.get(n, t0 + row0, len, v0 + r, a.dv);
       ot.put(16 * n + r, row0, given[n]);
     }
-    __syncthreads(); // (and every wavefront is through with the last chunk)
+    lds_barrier(); // (and every wavefront is through with the last chunk)
 #pragma unroll
     for (int n = 0; n < NT; ++n) got.put(16 * n + r, row0, given[n] * (gam * a.scale));
+    ask_values(next);
     tile d[NT] = {};
 #pragma unroll
     for (int i = 0; i < KK; ++i) {
-      const Operand<PI> k = fetch<PI>(a.kf + of_k * (DK * C * PI), w * KK + i, lane);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) multiply(d[n], k, st.get(16 * n + r, 32 * i + 8 * q4));
+      Operand<PC> y[NT];
+      st.get(r, 32 * i + 8 * q4, y);
+      multiply(d, k[i], y);
     }
+    ask_rows(next);
 #pragma unroll
     for (int n = 0; n < NT; ++n) d[n] *= tail;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       if (2 * j + 1 >= w) { // (P^T is upper triangular)
-        const Operand<PC> m = fetch<PC>(a.ptf + of * (C * C * PC), 2 * w + j, lane);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) multiply(d[n], m, ot.get(16 * n + r, 32 * j + 8 * q4));
+        Operand<PI> y[NT];
+        ot.get(r, 32 * j + 8 * q4, y);
+        multiply(d, pm[j], y);
       }
+    ask_squares(a.ptf, next, pm);
     {
-      const float *wp = a.w + (of * C + row0) * a.dvp + v0 + r;
       tile dot = {};
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (v0 + 16 * n + r < a.dvp) dot[e] = fmaf(wp[e * a.dvp + 16 * n], d[n][e], dot[e]);
+        for (int e = 0; e < 4; ++e) dot[e] = fmaf(made[n][e], d[n][e], dot[e]);
         ut.put(16 * n + r, row0, d[n] * beta);
       }
+      ask_made(next);
 #pragma unroll
       for (int x = 1; x < 16; x *= 2)
 #pragma unroll
         for (int e = 0; e < 4; ++e) dot[e] += __shfl_xor(dot[e], x);
       if (r == 0) *(tile *)(a.parts + ((long long)u.block * a.chunks * per + of) * C + row0) = dot;
     }
-    __syncthreads();
+    lds_barrier();
     tile x[NT] = {};
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       if (2 * j + 1 >= w) {
-        const Operand<PC> m = fetch<PC>(a.atf + of * (C * C * PC), 2 * w + j, lane);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) multiply(x[n], m, ut.get(16 * n + r, 32 * j + 8 * q4));
+        Operand<PC> y[NT];
+        ut.get(r, 32 * j + 8 * q4, y);
+        multiply(x, am[j], y);
       }
-    T *vp = (T *)a.dv_ + ((long long)(t0 + row0) * a.batch + b) * a.ld_dv + h * a.dv + v0 + r;
+    ask_squares(a.atf, next, am);
     float *ep = a.de + (of * C + row0) * a.dvp + v0 + r;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (t0 + row0 + e >= len) x[n][e] = 0.f;
-        if (v0 + 16 * n + r < a.dvp) ep[e * a.dvp + 16 * n] = x[n][e];
-        if (t0 + row0 + e < a.T && v0 + 16 * n + r < a.dv) vp[(long long)e * a.batch * a.ld_dv + 16 * n] = (T)x[n][e];
+        if (v0 + 16 * n < a.dvp) ep[e * a.dvp + 16 * n] = x[n][e];
       }
       et.put(16 * n + r, row0, x[n] * -gam);
     }
-    __syncthreads();
+    values_to<T, NT>(a.dv_, a.ld_dv, a, b, t0 + row0, len, h * a.dv, v0 + r, a.dv, t0 + C <= len && v0 + BV <= a.dv, x);
+    lds_barrier();
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
       for (int n = 0; n < NT; ++n) s[i][n] *= end;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j) {
+      Operand<PC> y[NT], z[NT];
+      got.get(r, 32 * j + 8 * q4, y);
+      et.get(r, 32 * j + 8 * q4, z);
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        const Operand<PI> q = fetch<PI>(a.qtf + of_k * (DK * C * PI), 2 * (w * RT + i) + j, lane);
-        const Operand<PI> k = fetch<PI>(a.ktf + of_k * (DK * C * PI), 2 * (w * RT + i) + j, lane);
+      for (int i = 0; i < RT; ++i) multiply(s[i], qt[i][j], y);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          multiply(s[i][n], q, got.get(16 * n + r, 32 * j + 8 * q4));
-          multiply(s[i][n], k, et.get(16 * n + r, 32 * j + 8 * q4));
-        }
-      }
+      for (int i = 0; i < RT; ++i) multiply(s[i], kt[i][j], z);
+    }
+    ask_columns(next);
+    ask_gates(next);
   }
   if (a.to)
 #pragma unroll
@@ -586,80 +720,126 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
 }
 
 // ---- gradients of a chunk's queries, keys and gates -----------------------------------------------
-template <class T, int DK> __global__ __launch_bounds__(256) void k_grads(Args a) {
-  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, NT = DK / 16;
+// Elements as they are in memory, asked for ahead of their use
+template <class T> struct Octet { // 8 of a row
+  words4 raw[sizeof(T) / 2];
+  __device__ __forceinline__ void ask(const T *p, int count) {
+    if (count >= LANE) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = *(const words4_any *)((const char *)p + 16 * i);
+    } else {
+      T x[LANE];
+#pragma unroll
+      for (int j = 0; j < LANE; ++j) x[j] = j < count ? p[j] : (T)0.f;
+      __builtin_memcpy(raw, x, sizeof x);
+    }
+  }
+  __device__ __forceinline__ void get(float (&v)[LANE]) const {
+    T x[LANE];
+    __builtin_memcpy(x, raw, sizeof x);
+#pragma unroll
+    for (int j = 0; j < LANE; ++j) v[j] = (float)x[j];
+  }
+};
+template <class T> struct Quad { // 4 of a row
+  T x[4];
+  typedef T any __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  __device__ __forceinline__ void ask(const T *p, int count) {
+    if (count >= 4) {
+      const any y = *(const any *)p;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = y[j];
+    } else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = j < count ? p[j] : (T)0.f;
+  }
+  static __device__ __forceinline__ void put(T *p, int count, const tile &v) {
+    if (count >= 4) {
+      any y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = (T)v[j];
+      *(any *)p = y;
+    } else
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < count) p[j] = (T)v[j];
+  }
+};
+
+// Sums over the state's columns go through LDS 32 at a time, the next ones on their way; results are [dk][t], so that a lane has four elements of one step's
+// row.  ONE: each head has queries and keys of its own.
+template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (sizeof(T) == 2 || DK == 64) ? 2 : 1) void k_grads(Args a) {
+  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, NT = DK / 16, NS = DK / 64;
   constexpr int SLICE = 32 + 8; // a row's 32 columns in LDS
   struct Sums { Planes<PC, DK, SLICE> before, after; Planes<PC, C, SLICE> w; };
   struct Squares { float dp[C][FLINE], m[C][FLINE]; };
   __shared__ __align__(16) char space[sizeof(Sums) > sizeof(Squares) ? sizeof(Sums) : sizeof(Squares)];
-  __shared__ float of_col[2][4][C], of_row[2][C], of_all[4];
+  __shared__ float of_col[2][4][C], of_row[3][C], of_all[4];
   Sums &sums = *(Sums *)space;
   Squares &squares = *(Squares *)space;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
   const int unit = blockIdx.x, kh = unit % a.key_heads, b = unit / a.key_heads % a.batch, c = unit / a.key_heads / a.batch;
-  const int t0 = (a.first + c) * C, len = length_of(a, b), group = a.heads / a.key_heads, row0 = 16 * w + 4 * q4;
-  const long long of_k = (long long)unit * (DK * C * PI);
-  tile qk[4] = {}, kk[4] = {};
-#pragma unroll
-  for (int i = 0; i < KK; ++i) {
-    const Operand<PI> q = fetch<PI>(a.qf + of_k, w * KK + i, lane), k = fetch<PI>(a.kf + of_k, w * KK + i, lane);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j <= w) {
-        const Operand<PI> y = fetch<PI>(a.kf + of_k, j * KK + i, lane);
-        multiply(qk[j], q, y);
-        multiply(kk[j], k, y);
-      }
-  }
+  const int t0 = (a.first + c) * C, len = length_of(a, b), group = ONE ? 1 : a.heads / a.key_heads, row0 = 16 * w + 4 * q4;
+  const int mine = 16 * w + r, t = t0 + mine; // a lane's step
+  const T *qp = (const T *)a.q + ((long long)t * a.batch + b) * a.ld_q + kh * a.dk, *kp = (const T *)a.k + ((long long)t * a.batch + b) * a.ld_k + kh * a.dk;
   tile gq[NT] = {}, gk[NT] = {};
   for (int i = 0; i < group; ++i) {
     const int h = kh * group + i;
     const long long of = ((long long)c * a.batch + b) * a.heads + h;
+    long long of_k = (long long)unit * (DK * C * PI);
+    if constexpr (!ONE) asm volatile("" : "+s"(of_k), "+v"(qp), "+v"(kp)); // (what is the same for all heads is read again for each: there are no registers to keep it)
     const float *gates = a.gates + of * (3 * C);
     const double *G = a.sums + of * C;
-    const float *before = a.before + of * DK * a.dvp, *after = a.after + of * DK * a.dvp, *wp = a.w + of * C * a.dvp, *ep = a.de + of * C * a.dvp;
-    const int t = t0 + 16 * w + r;
-    const T *dp = (const T *)a.dout + ((long long)t * a.batch + b) * a.ld_o + h * a.dv;
+    const float *before = a.before + of * DK * a.dvp, *after = a.after + of * DK * a.dvp, *wp = a.w + of * C * a.dvp, *ep = a.de + (of * C + mine) * a.dvp + 8 * q4;
+    const T *dp = (const T *)a.dout + ((long long)t * a.batch + b) * a.ld_o + h * a.dv + 8 * q4;
+    const int srow = threadIdx.x / 4, scol = threadIdx.x % 4 * 8; // of what a thread takes to LDS
+    Octet<float> rb[NS], ra[NS], rw, re;
+    Octet<T> rd;
+    auto ask = [&](int v) {
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        rb[n].ask(before + (64 * n + srow) * a.dvp + v + scol, LANE);
+        ra[n].ask(after + (64 * n + srow) * a.dvp + v + scol, LANE);
+      }
+      rw.ask(wp + srow * a.dvp + v + scol, LANE);
+      re.ask(ep + v, LANE);
+      rd.ask(dp + v, t < len ? a.dv - v - 8 * q4 : 0);
+    };
+    ask(0);
     tile sq[NT] = {}, se[NT] = {}, su[NT] = {}, p[4] = {}, x[4] = {};
     float both = 0.f; // <S, dS'>
     for (int v = 0; v < a.dvp; v += 32) {
-      __syncthreads();
+      lds_barrier();
+      float y[LANE], z[LANE];
+      auto to_lds = [&](const float (&from)[LANE], auto &planes, int row) {
+        const Operand<PC> f = operand<PC>(from);
 #pragma unroll
-      for (int n = 0; n < DK / 64; ++n) {
-        const int o = n * 256 + threadIdx.x, row = o / 4, col = o % 4 * 8;
-        float y[LANE], z[LANE];
-        read(before + row * a.dvp + v + col, LANE, y);
-        read(after + row * a.dvp + v + col, LANE, z);
+        for (int k = 0; k < PC; ++k) *(frag *)(planes.e[k] + row * SLICE + scol) = f.p[k];
+      };
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        rb[n].get(y);
+        ra[n].get(z);
 #pragma unroll
         for (int j = 0; j < LANE; ++j) both = fmaf(y[j], z[j], both);
-        const Operand<PC> fy = operand<PC>(y), fz = operand<PC>(z);
-#pragma unroll
-        for (int k = 0; k < PC; ++k) {
-          *(frag *)(sums.before.e[k] + row * SLICE + col) = fy.p[k];
-          *(frag *)(sums.after.e[k] + row * SLICE + col) = fz.p[k];
-        }
+        to_lds(y, sums.before, 64 * n + srow);
+        to_lds(z, sums.after, 64 * n + srow);
       }
-      {
-        const int row = threadIdx.x / 4, col = threadIdx.x % 4 * 8;
-        float y[LANE];
-        read(wp + row * a.dvp + v + col, LANE, y);
-        const Operand<PC> f = operand<PC>(y);
-#pragma unroll
-        for (int k = 0; k < PC; ++k) *(frag *)(sums.w.e[k] + row * SLICE + col) = f.p[k];
-      }
-      float y[LANE];
-      read(dp + v + 8 * q4, t < len ? a.dv - v - 8 * q4 : 0, y);
+      rw.get(y);
+      to_lds(y, sums.w, srow);
+      rd.get(y);
       const Operand<PI> d = operand<PI>(y);
-      read(ep + (16 * w + r) * a.dvp + v + 8 * q4, LANE, y);
+      re.get(y);
       const Operand<PC> e = operand<PC>(y);
-      __syncthreads();
-      const Operand<PC> mine = sums.w.get(16 * w + r, 8 * q4);
+      if (v + 32 < a.dvp) ask(v + 32);
+      lds_barrier();
+      const Operand<PC> wm = sums.w.get(mine, 8 * q4);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const Operand<PC> s = sums.before.get(16 * n + r, 8 * q4);
-        multiply(sq[n], d, s);
-        multiply(se[n], e, s);
-        multiply(su[n], mine, sums.after.get(16 * n + r, 8 * q4));
+        const Operand<PC> s = sums.before.get(16 * n + r, 8 * q4), s2 = sums.after.get(16 * n + r, 8 * q4);
+        multiply(sq[n], s, d);
+        multiply(se[n], s, e);
+        multiply(su[n], s2, wm);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -669,9 +849,27 @@ template <class T, int DK> __global__ __launch_bounds__(256) void k_grads(Args a
           multiply(x[j], e, y);
         }
     }
-    __syncthreads();
-    const tile gam = *(const tile *)(gates + row0), tail = *(const tile *)(gates + C + row0), beta = *(const tile *)(gates + 2 * C + row0);
-    tile of_mine = {}, wrote = {}; // what is read by a step and what a later step reads of it, what is left of it at the end
+    lds_barrier();
+    tile qk[4] = {}, kk[4] = {};
+#pragma unroll
+    for (int n = 0; n < KK; ++n) {
+      const Operand<PI> q = fetch<PI>(a.qf + of_k, w * KK + n, lane), k = fetch<PI>(a.kf + of_k, w * KK + n, lane);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j <= w) {
+          const Operand<PI> y = fetch<PI>(a.kf + of_k, j * KK + n, lane);
+          multiply(qk[j], q, y);
+          multiply(kk[j], k, y);
+        }
+    }
+    Quad<T> qe[NT], ke[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int col = 16 * n + 4 * q4, count = t < len ? a.dk - col : 0;
+      qe[n].ask(qp + col, count);
+      ke[n].ask(kp + col, count);
+    }
+    tile of_z = {};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int col = 16 * j + r;
@@ -684,7 +882,7 @@ template <class T, int DK> __global__ __launch_bounds__(256) void k_grads(Args a
         const float d = low ? __builtin_amdgcn_exp2f((float)(G[row] - G[col])) : 0.f;
         const float dpe = low ? p[j][e] * beta_col * d * a.scale : 0.f, me = below ? -x[j][e] * beta_col * d : 0.f;
         const float z = low ? fmaf(qk[j][e], dpe, kk[j][e] * me) : 0.f;
-        of_mine[e] += z;
+        of_z[e] += z;
         z_col += z;
         l_col += below ? kk[j][e] * d * x[j][e] : 0.f;
         squares.dp[row][col] = dpe;
@@ -701,64 +899,65 @@ template <class T, int DK> __global__ __launch_bounds__(256) void k_grads(Args a
         of_col[1][w][col] = l_col;
       }
     }
+    const float gam = gates[mine], left = gates[C + mine] * gates[2 * C + mine], end = gates[C - 1];
+    float read_by = 0.f, wrote = 0.f; // what a step reads of what was before, and what is left of its own at the end
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       sq[n] *= gam * a.scale;
       se[n] *= gam;
-      su[n] *= beta * tail;
-      const int col = 16 * n + r;
+      su[n] *= left;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const long long row = (long long)(t0 + row0 + e) * a.batch + b;
-        const bool on = t0 + row0 + e < len && col < a.dk;
-        const float qe = element((const T *)a.q + row * a.ld_q + kh * a.dk + col, on), ke = element((const T *)a.k + row * a.ld_k + kh * a.dk + col, on);
-        of_mine[e] += fmaf(qe, sq[n][e], -(ke * se[n][e]));
-        wrote[e] = fmaf(ke, su[n][e], wrote[e]);
+        const float q = (float)qe[n].x[e], k = (float)ke[n].x[e];
+        read_by += fmaf(q, sq[n][e], -(k * se[n][e]));
+        wrote = fmaf(k, su[n][e], wrote);
       }
       gq[n] += sq[n];
       gk[n] += su[n] - se[n];
     }
 #pragma unroll
+    for (int s = 16; s < 64; s *= 2) {
+      read_by += __shfl_xor(read_by, s);
+      wrote += __shfl_xor(wrote, s);
+    }
+#pragma unroll
     for (int s = 1; s < 16; s *= 2)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        of_mine[e] += __shfl_xor(of_mine[e], s);
-        wrote[e] += __shfl_xor(wrote[e], s);
-      }
-    if (r == 0) {
-      *(tile *)(of_row[0] + row0) = of_mine;
-      *(tile *)(of_row[1] + row0) = wrote;
+      for (int e = 0; e < 4; ++e) of_z[e] += __shfl_xor(of_z[e], s);
+    if (r == 0) *(tile *)(of_row[0] + row0) = of_z;
+    if (q4 == 0) {
+      of_row[1][mine] = read_by;
+      of_row[2][mine] = wrote;
     }
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) both += __shfl_xor(both, s);
     if (lane == 0) of_all[w] = both;
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       float y[LANE];
-      Operand<PC> dpf, dpt, m;
 #pragma unroll
-      for (int j = 0; j < LANE; ++j) y[j] = squares.dp[16 * w + r][32 * s + 8 * q4 + j];
-      dpf = operand<PC>(y);
+      for (int j = 0; j < LANE; ++j) y[j] = squares.dp[mine][32 * s + 8 * q4 + j];
+      const Operand<PC> dpf = operand<PC>(y);
 #pragma unroll
-      for (int j = 0; j < LANE; ++j) y[j] = squares.dp[32 * s + 8 * q4 + j][16 * w + r];
-      dpt = operand<PC>(y);
+      for (int j = 0; j < LANE; ++j) y[j] = squares.dp[32 * s + 8 * q4 + j][mine];
+      const Operand<PC> dpt = operand<PC>(y);
 #pragma unroll
-      for (int j = 0; j < LANE; ++j) y[j] = squares.m[16 * w + r][32 * s + 8 * q4 + j];
-      m = operand<PC>(y);
+      for (int j = 0; j < LANE; ++j) y[j] = squares.m[mine][32 * s + 8 * q4 + j];
+      const Operand<PC> m = operand<PC>(y);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const Operand<PI> k = fetch<PI>(a.ktf + of_k, 2 * n + s, lane);
-        if (2 * s <= w) multiply(gq[n], dpf, k);
-        multiply(gk[n], m, k);
-        if (2 * s + 1 >= w) multiply(gk[n], dpt, fetch<PI>(a.qtf + of_k, 2 * n + s, lane));
+        const Operand<PI> k = fetch<PI>(a.ktf + of_k, 2 * n + s, lane), q = fetch<PI>(a.qtf + of_k, 2 * n + s, lane);
+        if (2 * s <= w) multiply(gq[n], k, dpf);
+        multiply(gk[n], k, m);
+        if (2 * s + 1 >= w) multiply(gk[n], q, dpt);
       }
+      __builtin_amdgcn_sched_barrier(0); // (the operands of one half of the steps at a time)
     }
     if (w == 0) {
-      const float end = gates[C - 1];
-      double on = (double)of_row[0][lane] - ((of_col[0][0][lane] + of_col[0][1][lane]) + (of_col[0][2][lane] + of_col[0][3][lane]));
-      const float mine = of_row[1][lane];
-      double up = mine;
+      double on = (double)of_row[0][lane] + of_row[1][lane] - ((of_col[0][0][lane] + of_col[0][1][lane]) + (of_col[0][2][lane] + of_col[0][3][lane]));
+      const float own = of_row[2][lane];
+      double up = own;
 #pragma unroll
       for (int s = 1; s < C; s *= 2) {
         const double o = __shfl_down(on, s), y = __shfl_up(up, s);
@@ -770,22 +969,19 @@ template <class T, int DK> __global__ __launch_bounds__(256) void k_grads(Args a
       for (int n = 0; n < a.blocks; ++n) db += a.parts[((long long)n * a.chunks * a.batch * a.heads + of) * C + lane];
       if (t0 + lane < a.T) {
         const long long at = ((long long)(t0 + lane) * a.batch + b) * a.heads + h;
-        a.dg[at] = t0 + lane < len ? (float)(all + on + (up - mine)) : 0.f;
+        a.dg[at] = t0 + lane < len ? (float)(all + on + (up - own)) : 0.f;
         a.dbeta[at] = t0 + lane < len ? db : 0.f;
       }
     }
   }
+  if (t >= a.T) return;
+  T *dq = (T *)a.dq + ((long long)t * a.batch + b) * a.ld_dq + kh * a.dk, *dk = (T *)a.dk_ + ((long long)t * a.batch + b) * a.ld_dk + kh * a.dk;
 #pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int t = t0 + row0 + e, col = 16 * n + r;
-      if (t < a.T && col < a.dk) {
-        const long long row = (long long)t * a.batch + b;
-        ((T *)a.dq)[row * a.ld_dq + kh * a.dk + col] = (T)(t < len ? gq[n][e] : 0.f);
-        ((T *)a.dk_)[row * a.ld_dk + kh * a.dk + col] = (T)(t < len ? gk[n][e] : 0.f);
-      }
-    }
+  for (int n = 0; n < NT; ++n) {
+    const int col = 16 * n + 4 * q4;
+    Quad<T>::put(dq + col, a.dk - col, t < len ? gq[n] : tile{});
+    Quad<T>::put(dk + col, a.dk - col, t < len ? gk[n] : tile{});
+  }
 }
 
 // ---- step after step ------------------------------------------------------------------------------
@@ -1000,7 +1196,8 @@ template <class T, int DK> hipError_t backward(Plan &p, const float *kept, const
     a.from = from;
     a.to = first ? carry : p.last;
     k_walk_back<T, DK, 32><<<p.per * p.blocks, 256, 0, s>>>(a);
-    k_grads<T, DK><<<a.chunks * p.units, 256, 0, s>>>(a);
+    if (a.heads == a.key_heads) k_grads<T, DK, true><<<a.chunks * p.units, 256, 0, s>>>(a);
+    else k_grads<T, DK, false><<<a.chunks * p.units, 256, 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     from = carry;
   }
