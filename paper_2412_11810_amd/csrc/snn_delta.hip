@@ -10,7 +10,7 @@
 //   dU = P^T dO + gam_end / gam K dS',  dV = dE = A^T (beta dU),  dS = gam_end dS' + Q^T (scale gam dO) - K^T (gam dE)
 //   dP = (dO u^T) D scale,  M = -(dE u^T) D below the diagonal
 //   dQ = scale gam dO S^T + dP K,  dK = gam_end / gam u dS'^T - gam dE S^T + dP^T Q + (M + M^T) K
-//   dbeta_j = w_j . dU_j - sum_t L'_tj dE_t . w_j
+//   dbeta_j = sum_t (P_tj dO_t . w_j - L'_tj dE_t . w_j) + gam_end / gam_j k_j . dS' w_j
 //   dg_t = gam_end <S, dS'> + sum_{j<t} k_j . (of dK_j the first part) + sum_{i>=t} (q_i, k_i . the parts of dQ_i, dK_i from S) + sum_{i>=t>j} Z_ij,
 //   Z = Q K^T dP + K K^T M: what was written before a decay and read after it.  (Sums of what belongs to a decay: nothing large is taken away again.)
 //
@@ -54,7 +54,6 @@ struct Args {
   double *sums;                // [64]: G, as exponents of two
   float *before, *after;       // S and dS' [dk padded][dvp]
   float *w, *de;               // [64][dvp]
-  float *parts;                // [blocks][units][64]: w . dU of a block of columns
   long long ld_q, ld_k, ld_v, ld_o, ld_dq, ld_dk, ld_dv;
   int T, batch, heads, key_heads, dk, dv, dvp, blocks;
   int first, chunks, all; // the piece's first chunk, its chunks, those of the sequence
@@ -195,28 +194,111 @@ template <class T, int N> __device__ __forceinline__ void values_to(void *p, lon
         if (t + e < a.T && col + 16 * n < cols) to[e * step + 16 * n] = (T)(t + e < len ? v[n][e] : 0.f);
 }
 
+// Elements as they are in memory, asked for ahead of their use
+template <class T> struct Octet { // 8 of a row
+  words4 raw[sizeof(T) / 2];
+  __device__ __forceinline__ void ask(const T *p, int count) {
+    if (count >= LANE) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = *(const words4_any *)((const char *)p + 16 * i);
+    } else {
+      T x[LANE];
+#pragma unroll
+      for (int j = 0; j < LANE; ++j) x[j] = j < count ? p[j] : (T)0.f;
+      __builtin_memcpy(raw, x, sizeof x);
+    }
+  }
+  __device__ __forceinline__ void get(float (&v)[LANE]) const {
+    T x[LANE];
+    __builtin_memcpy(x, raw, sizeof x);
+#pragma unroll
+    for (int j = 0; j < LANE; ++j) v[j] = (float)x[j];
+  }
+  __device__ __forceinline__ Operand<GIVEN<T>> get() const {
+    if constexpr (sizeof(T) == 2) return Operand<1>{__builtin_bit_cast(frag, raw[0])};
+    else {
+      float v[LANE];
+      get(v);
+      return operand<3>(v);
+    }
+  }
+};
+template <class T> struct Quad { // 4 of a row
+  T x[4];
+  typedef T any __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  __device__ __forceinline__ void ask(const T *p, int count) {
+    if (count >= 4) {
+      const any y = *(const any *)p;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = y[j];
+    } else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = j < count ? p[j] : (T)0.f;
+  }
+  static __device__ __forceinline__ void put(T *p, int count, const tile &v) {
+    if (count >= 4) {
+      any y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = (T)v[j];
+      *(any *)p = y;
+    } else
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < count) p[j] = (T)v[j];
+  }
+};
+
 // ---- a chunk by itself ------------------------------------------------------------------------
-template <class T, int DK, bool BACK> __global__ __launch_bounds__(256) void k_chunk(Args a) {
+// ONE: each head has queries and keys of its own.
+template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256, ONE ? sizeof(T) == 2 || DK == 64 ? 4 : 3 : 2) void k_chunk(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32;
-  __shared__ __align__(16) Planes<PI, C, DK + 8> rows;
-  __shared__ __align__(16) float m[C][FLINE], x[C][FLINE];
+  typedef Planes<PI, C, DK + 8> Rows;
+  struct Squares { float m[C][FLINE], x[C][FLINE]; };
+  __shared__ __align__(16) char space[sizeof(Rows) > sizeof(Squares) ? sizeof(Rows) : sizeof(Squares)];
   __shared__ double sum[C];
   __shared__ float rate[C];
+  Rows &rows = *(Rows *)space;
+  auto &m = ((Squares *)space)->m, &x = ((Squares *)space)->x;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
   const int unit = blockIdx.x, kh = unit % a.key_heads, b = unit / a.key_heads % a.batch, c = unit / a.key_heads / a.batch;
-  const int t0 = (a.first + c) * C, len = length_of(a, b), group = a.heads / a.key_heads;
+  const int t0 = (a.first + c) * C, len = length_of(a, b), group = ONE ? 1 : a.heads / a.key_heads;
   const int t = t0 + 16 * w + r;
   constexpr int SIZE = DK * C * PI; // elements of one operand array of a unit
-  // rows of steps: to memory as operands, and those of k to LDS
-  Operand<PI> kf[KK], qf[KK];
-  auto load = [&](const void *p, long long ld, Operand<PI> (&f)[KK], __bf16 *to) {
+  Octet<T> kr[KK], qr[KK];
+  auto ask = [&](const void *p, long long ld, Octet<T> (&o)[KK]) {
     const T *row = (const T *)p + ((long long)t * a.batch + b) * ld + kh * a.dk;
 #pragma unroll
+    for (int i = 0; i < KK; ++i) o[i].ask(row + 32 * i + 8 * q4, t < len ? a.dk - 32 * i - 8 * q4 : 0);
+  };
+  // a head's gates, in the first wavefront, whose lanes are the chunk's steps
+  const bool on = t0 + lane < len;
+  auto gate = [&](const float *p, int h) { return on ? p[((long long)(t0 + lane) * a.batch + b) * a.heads + h] : 0.f; };
+  float g = w == 0 ? gate(a.g, kh * group) : 0.f, beta = w == 0 ? gate(a.beta, kh * group) : 0.f;
+  ask(a.k, a.ld_k, kr);
+  ask(a.q, a.ld_q, qr);
+  auto gates = [&](int h, int lane) {
+    const long long of = ((long long)c * a.batch + b) * a.heads + h;
+    double G = (double)(g < -1e4f ? -1e4f : g) * 1.4426950408889634; // (minus infinity: forgotten all the same)
+#pragma unroll
+    for (int s = 1; s < C; s *= 2) {
+      const double o = __shfl_up(G, s);
+      if (lane >= s) G += o;
+    }
+    sum[lane] = G;
+    rate[lane] = beta;
+    const double end = __shfl(G, C - 1);
+    float *to = a.gates + of * (3 * C);
+    to[lane] = __builtin_amdgcn_exp2f((float)G);
+    to[C + lane] = __builtin_amdgcn_exp2f((float)(end - G));
+    to[2 * C + lane] = beta;
+    if constexpr (BACK) a.sums[of * C + lane] = G;
+  };
+  if (w == 0) gates(kh * group, lane);
+  // rows of steps: to memory as operands, and those of k to LDS
+  auto give = [&](const Octet<T> (&o)[KK], Operand<PI> (&f)[KK], __bf16 *to) {
+#pragma unroll
     for (int i = 0; i < KK; ++i) {
-      float e[LANE];
-      const int col = 32 * i + 8 * q4;
-      read(row + col, t < len ? a.dk - col : 0, e);
-      f[i] = operand<PI>(e);
+      f[i] = o[i].get();
       leave<PI>(to + (long long)unit * SIZE, w * KK + i, lane, f[i]);
     }
   };
@@ -227,6 +309,7 @@ template <class T, int DK, bool BACK> __global__ __launch_bounds__(256) void k_c
       for (int p = 0; p < PI; ++p) *(frag *)(rows.e[p] + (16 * w + r) * (DK + 8) + 32 * i + 8 * q4) = f[i].p[p];
   };
   auto turned = [&](__bf16 *to) { // rows of channels
+#pragma unroll 1
     for (int f = w; f < DK / 16 * 2; f += 4) {
       Operand<PI> y;
 #pragma unroll
@@ -236,13 +319,14 @@ template <class T, int DK, bool BACK> __global__ __launch_bounds__(256) void k_c
       leave<PI>(to + (long long)unit * SIZE, f, lane, y);
     }
   };
-  load(a.k, a.ld_k, kf, a.kf);
-  load(a.q, a.ld_q, qf, a.qf);
+  Operand<PI> kf[KK], qf[KK];
+  give(kr, kf, a.kf);
   to_lds(kf);
+  give(qr, qf, a.qf);
   __syncthreads();
   tile kk[4] = {}, qk[4] = {};
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < 4; ++j) {
     if (j <= w)
 #pragma unroll
       for (int i = 0; i < KK; ++i) {
@@ -250,6 +334,8 @@ template <class T, int DK, bool BACK> __global__ __launch_bounds__(256) void k_c
         multiply(kk[j], kf[i], y);
         multiply(qk[j], qf[i], y);
       }
+    __builtin_amdgcn_sched_barrier(0);
+  }
   turned(a.ktf);
   if constexpr (BACK) {
     __syncthreads();
@@ -257,29 +343,17 @@ template <class T, int DK, bool BACK> __global__ __launch_bounds__(256) void k_c
     __syncthreads();
     turned(a.qtf);
   }
+  const int thread = lane;
+#pragma unroll 1
   for (int i = 0; i < group; ++i) {
-    const int h = kh * group + i;
+    // (What depends on the lane alone would be kept for all heads, masks and addresses, in twice the registers: 84 of them without)
+    int lane = thread;
+    asm volatile("" : "+v"(lane));
+    const int r = lane & 15, q4 = lane >> 4, h = kh * group + i;
     const long long of = ((long long)c * a.batch + b) * a.heads + h;
     if (w == 0) {
-      const bool on = t0 + lane < len;
-      const long long at = ((long long)(t0 + lane) * a.batch + b) * a.heads + h;
-      float g = on ? a.g[at] : 0.f;
-      g = g < -1e4f ? -1e4f : g; // (minus infinity: forgotten all the same)
-      const float beta = on ? a.beta[at] : 0.f;
-      double G = (double)g * 1.4426950408889634;
-#pragma unroll
-      for (int s = 1; s < C; s *= 2) {
-        const double o = __shfl_up(G, s);
-        if (lane >= s) G += o;
-      }
-      sum[lane] = G;
-      rate[lane] = beta;
-      const double end = __shfl(G, C - 1);
-      float *to = a.gates + of * (3 * C);
-      to[lane] = __builtin_amdgcn_exp2f((float)G);
-      to[C + lane] = __builtin_amdgcn_exp2f((float)(end - G));
-      to[2 * C + lane] = beta;
-      if constexpr (BACK) a.sums[of * C + lane] = G;
+      if (i) gates(h, lane);
+      if (i + 1 < group) g = gate(a.g, h + 1), beta = gate(a.beta, h + 1);
     }
     __syncthreads();
 #pragma unroll
@@ -293,9 +367,10 @@ template <class T, int DK, bool BACK> __global__ __launch_bounds__(256) void k_c
         x[row][col] = col <= row ? qk[j][e] * d * a.scale : 0.f;
       }
     __syncthreads();
-    auto emit = [&](__bf16 *to, bool over) { // a matrix in x, or its transpose
+    auto emit = [&](__bf16 *to, bool over) { // a lower triangular matrix in x, or its transpose; blocks of zeros, which nothing reads, are left out
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
+        if (over ? 2 * s + 1 < w : 2 * s > w) continue;
         float e[LANE];
 #pragma unroll
         for (int j = 0; j < LANE; ++j) e[j] = over ? x[32 * s + 8 * q4 + j][16 * w + r] : x[16 * w + r][32 * s + 8 * q4 + j];
@@ -304,14 +379,21 @@ template <class T, int DK, bool BACK> __global__ __launch_bounds__(256) void k_c
     };
     if constexpr (BACK) emit(a.ptf, true);
     else emit(a.pf, false);
-    // column r of the inverse of the diagonal's block w
+    // column r of the inverse of the diagonal's block w: a row of it after the other, the next row of m on its way
     float y[16];
+    tile now[4] = {}, then[4];
 #pragma unroll
     for (int n = 0; n < 16; ++n) {
-      float s = n == r ? 1.f : 0.f;
+      if (n < 15)
 #pragma unroll
-      for (int j = 0; j < n; ++j) s = fmaf(-m[16 * w + n][16 * w + j], y[j], s);
-      y[n] = s;
+        for (int j = 0; j <= n / 4; ++j) then[j] = *(const tile *)&m[16 * w + n + 1][16 * w + 4 * j];
+      float s[4] = {n == r ? 1.f : 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < n; ++j) s[j % 4] = fmaf(-now[j / 4][j % 4], y[j], s[j % 4]);
+      y[n] = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+      for (int j = 0; j <= n / 4; ++j) now[j] = then[j];
+      __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
 #pragma unroll
@@ -563,7 +645,7 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
   Operand<PI> k[KK], kt[RT][2], qt[RT][2];
   Operand<PC> am[2], pm[2];
   Values<T, NT> raw; // of dO
-  tile made[NT], gam, tail, beta; // w
+  tile gam, tail, beta;
   float end;
   auto of_keys = [&](int c) { return (((long long)c * a.batch + b) * a.key_heads + kh) * (DK * C * PI); };
   auto of_head = [&](int c) { return ((long long)c * a.batch + b) * a.heads + h; };
@@ -573,13 +655,6 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
   };
   auto ask_values = [&](int c) {
     raw.ask(a.dout, a.ld_o, a, b, (a.first + c) * C + row0, h * a.dv, v0 + r, a.dv);
-  };
-  auto ask_made = [&](int c) {
-    const float *wp = a.w + (of_head(c) * C + row0) * a.dvp + v0 + r;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) made[n][e] = wp[e * a.dvp + 16 * n]; // (dvp is a multiple of the 32 columns of this kernel)
   };
   auto ask_squares = [&](const __bf16 *p, int c, Operand<PC> (&m)[2]) { // (upper triangular: the last two rows of blocks begin with zeros)
     if (w < 2) m[0] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w, lane);
@@ -605,7 +680,6 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
     ask_values(c);
     ask_rows(c);
     ask_squares(a.ptf, c, pm);
-    ask_made(c);
     ask_squares(a.atf, c, am);
     ask_columns(c);
   }
@@ -653,21 +727,8 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
         multiply(d, pm[j], y);
       }
     ask_squares(a.ptf, next, pm);
-    {
-      tile dot = {};
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) dot[e] = fmaf(made[n][e], d[n][e], dot[e]);
-        ut.put(16 * n + r, row0, d[n] * beta);
-      }
-      ask_made(next);
-#pragma unroll
-      for (int x = 1; x < 16; x *= 2)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) dot[e] += __shfl_xor(dot[e], x);
-      if (r == 0) *(tile *)(a.parts + ((long long)u.block * a.chunks * per + of) * C + row0) = dot;
-    }
+    for (int n = 0; n < NT; ++n) ut.put(16 * n + r, row0, d[n] * beta);
     lds_barrier();
     tile x[NT] = {};
 #pragma unroll
@@ -720,61 +781,16 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
 }
 
 // ---- gradients of a chunk's queries, keys and gates -----------------------------------------------
-// Elements as they are in memory, asked for ahead of their use
-template <class T> struct Octet { // 8 of a row
-  words4 raw[sizeof(T) / 2];
-  __device__ __forceinline__ void ask(const T *p, int count) {
-    if (count >= LANE) {
-#pragma unroll
-      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = *(const words4_any *)((const char *)p + 16 * i);
-    } else {
-      T x[LANE];
-#pragma unroll
-      for (int j = 0; j < LANE; ++j) x[j] = j < count ? p[j] : (T)0.f;
-      __builtin_memcpy(raw, x, sizeof x);
-    }
-  }
-  __device__ __forceinline__ void get(float (&v)[LANE]) const {
-    T x[LANE];
-    __builtin_memcpy(x, raw, sizeof x);
-#pragma unroll
-    for (int j = 0; j < LANE; ++j) v[j] = (float)x[j];
-  }
-};
-template <class T> struct Quad { // 4 of a row
-  T x[4];
-  typedef T any __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-  __device__ __forceinline__ void ask(const T *p, int count) {
-    if (count >= 4) {
-      const any y = *(const any *)p;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = y[j];
-    } else
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = j < count ? p[j] : (T)0.f;
-  }
-  static __device__ __forceinline__ void put(T *p, int count, const tile &v) {
-    if (count >= 4) {
-      any y;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = (T)v[j];
-      *(any *)p = y;
-    } else
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (j < count) p[j] = (T)v[j];
-  }
-};
-
 // Sums over the state's columns go through LDS 32 at a time, the next ones on their way; results are [dk][t], so that a lane has four elements of one step's
-// row.  ONE: each head has queries and keys of its own.
+// row.
 template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (sizeof(T) == 2 || DK == 64) ? 2 : 1) void k_grads(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, NT = DK / 16, NS = DK / 64;
   constexpr int SLICE = 32 + 8; // a row's 32 columns in LDS
   struct Sums { Planes<PC, DK, SLICE> before, after; Planes<PC, C, SLICE> w; };
   struct Squares { float dp[C][FLINE], m[C][FLINE]; };
   __shared__ __align__(16) char space[sizeof(Sums) > sizeof(Squares) ? sizeof(Sums) : sizeof(Squares)];
-  __shared__ float of_col[2][4][C], of_row[3][C], of_all[4];
+  __shared__ float of_col[4][C], of_row[3][C], of_all[4], gates[3][C];
+  __shared__ double G[C];
   Sums &sums = *(Sums *)space;
   Squares &squares = *(Squares *)space;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
@@ -788,8 +804,6 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
     const long long of = ((long long)c * a.batch + b) * a.heads + h;
     long long of_k = (long long)unit * (DK * C * PI);
     if constexpr (!ONE) asm volatile("" : "+s"(of_k), "+v"(qp), "+v"(kp)); // (what is the same for all heads is read again for each: there are no registers to keep it)
-    const float *gates = a.gates + of * (3 * C);
-    const double *G = a.sums + of * C;
     const float *before = a.before + of * DK * a.dvp, *after = a.after + of * DK * a.dvp, *wp = a.w + of * C * a.dvp, *ep = a.de + (of * C + mine) * a.dvp + 8 * q4;
     const T *dp = (const T *)a.dout + ((long long)t * a.batch + b) * a.ld_o + h * a.dv + 8 * q4;
     const int srow = threadIdx.x / 4, scol = threadIdx.x % 4 * 8; // of what a thread takes to LDS
@@ -805,11 +819,17 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
       re.ask(ep + v, LANE);
       rd.ask(dp + v, t < len ? a.dv - v - 8 * q4 : 0);
     };
+    const float gate = threadIdx.x < 3 * C ? a.gates[of * (3 * C) + threadIdx.x] : 0.f;
+    const double sum = threadIdx.x < C ? a.sums[of * C + threadIdx.x] : 0.;
     ask(0);
     tile sq[NT] = {}, se[NT] = {}, su[NT] = {}, p[4] = {}, x[4] = {};
     float both = 0.f; // <S, dS'>
     for (int v = 0; v < a.dvp; v += 32) {
       lds_barrier();
+      if (v == 0) { // (every wavefront is through with the last head's)
+        if (threadIdx.x < 3 * C) gates[threadIdx.x / C][threadIdx.x % C] = gate;
+        if (threadIdx.x < C) G[threadIdx.x] = sum;
+      }
       float y[LANE], z[LANE];
       auto to_lds = [&](const float (&from)[LANE], auto &planes, int row) {
         const Operand<PC> f = operand<PC>(from);
@@ -850,18 +870,27 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
         }
     }
     lds_barrier();
-    tile qk[4] = {}, kk[4] = {};
+    // The rest's loads are asked for ahead, as many at a time as there are registers for
+    Operand<PI> q[KK], k[KK], y[4][KK];
 #pragma unroll
     for (int n = 0; n < KK; ++n) {
-      const Operand<PI> q = fetch<PI>(a.qf + of_k, w * KK + n, lane), k = fetch<PI>(a.kf + of_k, w * KK + n, lane);
+      q[n] = fetch<PI>(a.qf + of_k, w * KK + n, lane);
+      k[n] = fetch<PI>(a.kf + of_k, w * KK + n, lane);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (j <= w) {
-          const Operand<PI> y = fetch<PI>(a.kf + of_k, j * KK + n, lane);
-          multiply(qk[j], q, y);
-          multiply(kk[j], k, y);
-        }
+        if (j <= w) y[j][n] = fetch<PI>(a.kf + of_k, j * KK + n, lane);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    tile qk[4] = {}, kk[4] = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j <= w)
+#pragma unroll
+        for (int n = 0; n < KK; ++n) {
+          multiply(qk[j], q[n], y[j][n]);
+          multiply(kk[j], k[n], y[j][n]);
+        }
+    __builtin_amdgcn_sched_barrier(0);
     Quad<T> qe[NT], ke[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -869,43 +898,44 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
       qe[n].ask(qp + col, count);
       ke[n].ask(kp + col, count);
     }
+    Operand<PI> cols[NT];
+    auto columns = [&](const __bf16 *p, int s) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) cols[n] = fetch<PI>(p + of_k, 2 * n + s, lane);
+    };
+    if constexpr (PI == 1) columns(a.ktf, 0);
+    __builtin_amdgcn_sched_barrier(0);
     tile of_z = {};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int col = 16 * j + r;
-      const float beta_col = gates[2 * C + col];
-      float z_col = 0.f, l_col = 0.f;
+      const float beta_col = gates[2][col];
+      float z_col = 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int row = row0 + e;
         const bool low = j <= w && col <= row, below = j <= w && col < row;
         const float d = low ? __builtin_amdgcn_exp2f((float)(G[row] - G[col])) : 0.f;
-        const float dpe = low ? p[j][e] * beta_col * d * a.scale : 0.f, me = below ? -x[j][e] * beta_col * d : 0.f;
-        const float z = low ? fmaf(qk[j][e], dpe, kk[j][e] * me) : 0.f;
-        of_z[e] += z;
+        const float dps = low ? p[j][e] * d * a.scale : 0.f, me = below ? x[j][e] * d : 0.f; // beta of the column is left out
+        const float zq = low ? qk[j][e] * dps : 0.f, zk = below ? kk[j][e] * me : 0.f;
+        const float z = zq - zk; // of both w . dU less that of what it was taken from; times beta, of what decays lie between
+        of_z[e] = fmaf(z, beta_col, of_z[e]);
         z_col += z;
-        l_col += below ? kk[j][e] * d * x[j][e] : 0.f;
-        squares.dp[row][col] = dpe;
-        if (below) squares.m[row][col] = squares.m[col][row] = me;
+        squares.dp[row][col] = dps * beta_col;
+        if (below) squares.m[row][col] = squares.m[col][row] = -me * beta_col;
         if (j == w && col == row) squares.m[row][col] = 0.f;
       }
 #pragma unroll
-      for (int s = 16; s < 64; s *= 2) {
-        z_col += __shfl_xor(z_col, s);
-        l_col += __shfl_xor(l_col, s);
-      }
-      if (q4 == 0) {
-        of_col[0][w][col] = z_col;
-        of_col[1][w][col] = l_col;
-      }
+      for (int s = 16; s < 64; s *= 2) z_col += __shfl_xor(z_col, s);
+      if (q4 == 0) of_col[w][col] = z_col;
     }
-    const float gam = gates[mine], left = gates[C + mine] * gates[2 * C + mine], end = gates[C - 1];
-    float read_by = 0.f, wrote = 0.f; // what a step reads of what was before, and what is left of its own at the end
+    const float gam = gates[0][mine], tail = gates[1][mine], beta = gates[2][mine], end = gates[0][C - 1];
+    float read_by = 0.f, wrote = 0.f; // what a step reads of what was before, and what is left of its own at the end, but for beta
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       sq[n] *= gam * a.scale;
       se[n] *= gam;
-      su[n] *= left;
+      su[n] *= tail;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float q = (float)qe[n].x[e], k = (float)ke[n].x[e];
@@ -913,7 +943,7 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
         wrote = fmaf(k, su[n][e], wrote);
       }
       gq[n] += sq[n];
-      gk[n] += su[n] - se[n];
+      gk[n] += su[n] * beta - se[n];
     }
 #pragma unroll
     for (int s = 16; s < 64; s *= 2) {
@@ -945,18 +975,22 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
 #pragma unroll
       for (int j = 0; j < LANE; ++j) y[j] = squares.m[mine][32 * s + 8 * q4 + j];
       const Operand<PC> m = operand<PC>(y);
+      if (s || PI > 1) columns(a.ktf, s);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const Operand<PI> k = fetch<PI>(a.ktf + of_k, 2 * n + s, lane), q = fetch<PI>(a.qtf + of_k, 2 * n + s, lane);
-        if (2 * s <= w) multiply(gq[n], k, dpf);
-        multiply(gk[n], k, m);
-        if (2 * s + 1 >= w) multiply(gk[n], q, dpt);
+        if (2 * s <= w) multiply(gq[n], cols[n], dpf);
+        multiply(gk[n], cols[n], m);
       }
-      __builtin_amdgcn_sched_barrier(0); // (the operands of one half of the steps at a time)
+      if (2 * s + 1 >= w) {
+        columns(a.qtf, s);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) multiply(gk[n], cols[n], dpt);
+      }
     }
     if (w == 0) {
-      double on = (double)of_row[0][lane] + of_row[1][lane] - ((of_col[0][0][lane] + of_col[0][1][lane]) + (of_col[0][2][lane] + of_col[0][3][lane]));
-      const float own = of_row[2][lane];
+      const float beta = gates[2][lane], of_w = (of_col[0][lane] + of_col[1][lane]) + (of_col[2][lane] + of_col[3][lane]), left = of_row[2][lane];
+      const float own = left * beta;
+      double on = (double)of_row[0][lane] + of_row[1][lane] - (double)of_w * beta;
       double up = own;
 #pragma unroll
       for (int s = 1; s < C; s *= 2) {
@@ -965,12 +999,10 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
         if (lane >= s) up += y;
       }
       const float all = end * ((of_all[0] + of_all[1]) + (of_all[2] + of_all[3]));
-      float db = -((of_col[1][0][lane] + of_col[1][1][lane]) + (of_col[1][2][lane] + of_col[1][3][lane]));
-      for (int n = 0; n < a.blocks; ++n) db += a.parts[((long long)n * a.chunks * a.batch * a.heads + of) * C + lane];
       if (t0 + lane < a.T) {
         const long long at = ((long long)(t0 + lane) * a.batch + b) * a.heads + h;
         a.dg[at] = t0 + lane < len ? (float)(all + on + (up - own)) : 0.f;
-        a.dbeta[at] = t0 + lane < len ? db : 0.f;
+        a.dbeta[at] = t0 + lane < len ? of_w + left : 0.f;
       }
     }
   }
@@ -1101,7 +1133,7 @@ template <class T, int DK, int LV> __global__ __launch_bounds__(256) void k_step
 
 // ---- launches -------------------------------------------------------------------------------------
 constexpr int STEPS_MOST = 16;            // steps that are taken one after the other
-constexpr size_t PIECE = (size_t)512 << 20; // bytes of a piece's intermediate arrays, at least 4 chunks
+constexpr size_t PIECE = (size_t)256 << 20; // bytes of a piece's intermediate arrays, at least 4 chunks
 
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
@@ -1141,7 +1173,6 @@ struct Plan {
         take(a.after, nh * dk * dvp);
         take(a.w, nh * C * dvp);
         take(a.de, nh * C * dvp);
-        take(a.parts, nh * C * blocks);
       }
       return at;
     };
@@ -1166,7 +1197,8 @@ template <class T, int DK> hipError_t forward(Plan &p, hipStream_t s) {
     a.chunks = p.all - first < p.chunks ? p.all - first : p.chunks;
     a.from = from;
     a.to = first + a.chunks < p.all ? carry : p.last;
-    k_chunk<T, DK, false><<<a.chunks * p.units, 256, 0, s>>>(a);
+    if (a.heads == a.key_heads) k_chunk<T, DK, false, true><<<a.chunks * p.units, 256, 0, s>>>(a);
+    else k_chunk<T, DK, false, false><<<a.chunks * p.units, 256, 0, s>>>(a);
     if (p.bv == 64) {
       if constexpr (sizeof(T) == 2) k_walk<T, DK, 64, false><<<p.per * p.blocks, 256, 0, s>>>(a);
     } else k_walk<T, DK, 32, false><<<p.per * p.blocks, 256, 0, s>>>(a);
@@ -1189,7 +1221,8 @@ template <class T, int DK> hipError_t backward(Plan &p, const float *kept, const
   for (int first = (p.all - 1) / p.chunks * p.chunks; first >= 0; first -= p.chunks) {
     a.first = first;
     a.chunks = p.all - first < p.chunks ? p.all - first : p.chunks;
-    k_chunk<T, DK, true><<<a.chunks * p.units, 256, 0, s>>>(a);
+    if (a.heads == a.key_heads) k_chunk<T, DK, true, true><<<a.chunks * p.units, 256, 0, s>>>(a);
+    else k_chunk<T, DK, true, false><<<a.chunks * p.units, 256, 0, s>>>(a);
     a.from = kept;
     a.to = nullptr;
     k_walk<T, DK, 32, true><<<(a.chunks + KEPT - 1) / KEPT * p.per * p.blocks, 256, 0, s>>>(a);
