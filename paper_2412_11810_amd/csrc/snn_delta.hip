@@ -6,8 +6,9 @@
 // the chunk and L' = (K K^T D) strictly below the diagonal, its steps are
 //   E = V - gam K S,  w = A E with A = (1 + L' diag(beta))^-1,  u = beta w,  O = scale gam Q S + P u with P = scale Q K^T D,
 //   S' = gam_end S + K^T (gam_end / gam u)
+// With A1 = diag(gam_end / gam beta) A and B = P diag(beta) A, found for all chunks beforehand, that is O = scale gam Q S + B E, S' = gam_end S + K^T A1 E;
 // and back, from dO and the gradient dS' of S':
-//   dU = P^T dO + gam_end / gam K dS',  dV = dE = A^T (beta dU),  dS = gam_end dS' + Q^T (scale gam dO) - K^T (gam dE)
+//   dV = dE = B^T dO + A1^T K dS',  dS = gam_end dS' + Q^T (scale gam dO) - K^T (gam dE)
 //   dP = (dO u^T) D scale,  M = -(dE u^T) D below the diagonal
 //   dQ = scale gam dO S^T + dP K,  dK = gam_end / gam u dS'^T - gam dE S^T + dP^T Q + (M + M^T) K
 //   dbeta_j = sum_t (P_tj dO_t . w_j - L'_tj dE_t . w_j) + gam_end / gam_j k_j . dS' w_j
@@ -16,11 +17,11 @@
 //
 // G and its differences are of 64 bits: behind a decay that forgets everything the next steps' ratios keep their digits.  A is found by substitution in
 // blocks of 16, in 32 bits, and by products of blocks, so that equal keys do no harm.
-// States and sums are of 32 bits.  Products go through the bf16 matrix cores: arrays of bf16 as they are, what is computed on the way (S, E, u, dU, dE, A, P) in two
+// States and sums are of 32 bits.  Products go through the bf16 matrix cores: arrays of bf16 as they are, what is computed on the way (S, E, u, dE, A, B) in two
 // bf16 parts, which leaves 16 bits of each factor (off by 2^-17 of itself at most; 3 products of parts, or 2 beside an operand that is bf16); with
 // arrays of 32 bits everything goes in three parts and six products, which keep 24.
 //
-// Four kernels: what is of a chunk alone (k_chunk: A, P, and the operands in the order in which a wavefront loads them); the walk over the chunks
+// Four kernels: what is of a chunk alone (k_chunk: A, B, and the operands in the order in which a wavefront loads them); the walk over the chunks
 // with S in registers, its columns dealt to workgroups (k_walk; for the backward pass it starts at each kept state, every 4 chunks); the walk back
 // with dS (k_walk_back); and what needs S, dS', w and dE of a chunk (k_grads).  They go through the sequence in pieces whose intermediate arrays fit the caches
 // or nearly so.  Few steps are taken one after the other, by a kernel whose workgroup holds the whole state of a head (k_steps).
@@ -49,7 +50,7 @@ struct Args {
   const int *lengths;
   // a piece's intermediate arrays, by (chunk, batch, key head) or (chunk, batch, head)
   __bf16 *kf, *qf, *ktf, *qtf; // operands: rows of steps, rows of channels
-  __bf16 *af, *pf, *atf, *ptf; // A, P and their transposes
+  __bf16 *af, *bf, *at, *bt;   // A1 (in the backward pass A) and B; A1 and B transposed
   float *gates;                // [3][64]: gam, gam_end / gam, beta
   double *sums;                // [64]: G, as exponents of two
   float *before, *after;       // S and dS' [dk padded][dvp]
@@ -256,7 +257,7 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
   struct Squares { float m[C][FLINE], x[C][FLINE]; };
   __shared__ __align__(16) char space[sizeof(Rows) > sizeof(Squares) ? sizeof(Rows) : sizeof(Squares)];
   __shared__ double sum[C];
-  __shared__ float rate[C];
+  __shared__ float rate[C], left[C]; // beta; gam_end / gam beta
   Rows &rows = *(Rows *)space;
   auto &m = ((Squares *)space)->m, &x = ((Squares *)space)->x;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
@@ -289,7 +290,9 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
     const double end = __shfl(G, C - 1);
     float *to = a.gates + of * (3 * C);
     to[lane] = __builtin_amdgcn_exp2f((float)G);
-    to[C + lane] = __builtin_amdgcn_exp2f((float)(end - G));
+    const float tail = __builtin_amdgcn_exp2f((float)(end - G));
+    left[lane] = tail * beta;
+    to[C + lane] = tail;
     to[2 * C + lane] = beta;
     if constexpr (BACK) a.sums[of * C + lane] = G;
   };
@@ -367,18 +370,15 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
         x[row][col] = col <= row ? qk[j][e] * d * a.scale : 0.f;
       }
     __syncthreads();
-    auto emit = [&](__bf16 *to, bool over) { // a lower triangular matrix in x, or its transpose; blocks of zeros, which nothing reads, are left out
+    // P diag(beta): its rows of this wavefront's steps
+    Operand<PC> pm[2];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        if (over ? 2 * s + 1 < w : 2 * s > w) continue;
-        float e[LANE];
+    for (int s = 0; s < 2; ++s) {
+      float e[LANE];
 #pragma unroll
-        for (int j = 0; j < LANE; ++j) e[j] = over ? x[32 * s + 8 * q4 + j][16 * w + r] : x[16 * w + r][32 * s + 8 * q4 + j];
-        leave<PC>(to + of * (C * C * PC), 2 * w + s, lane, operand<PC>(e));
-      }
-    };
-    if constexpr (BACK) emit(a.ptf, true);
-    else emit(a.pf, false);
+      for (int j = 0; j < LANE; ++j) e[j] = x[16 * w + r][32 * s + 8 * q4 + j] * rate[32 * s + 8 * q4 + j];
+      pm[s] = operand<PC>(e);
+    }
     // column r of the inverse of the diagonal's block w: a row of it after the other, the next row of m on its way
     float y[16];
     tile now[4] = {}, then[4];
@@ -431,8 +431,41 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
       }
     }
     __syncthreads();
-    emit(a.af, false);
-    if constexpr (BACK) emit(a.atf, true);
+    // A lower triangular matrix in x, or its transpose, times a factor of its rows; blocks of zeros, which nothing reads, are left out
+    auto emit = [&](__bf16 *to, bool over, bool scaled) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (over ? 2 * s + 1 < w : 2 * s > w) continue;
+        float e[LANE];
+#pragma unroll
+        for (int j = 0; j < LANE; ++j) {
+          const int k = 32 * s + 8 * q4 + j;
+          e[j] = (over ? x[k][16 * w + r] : x[16 * w + r][k]) * (scaled ? left[over ? k : 16 * w + r] : 1.f);
+        }
+        leave<PC>(to + of * (C * C * PC), 2 * w + s, lane, operand<PC>(e));
+      }
+    };
+    emit(a.af, false, !BACK);
+    if constexpr (BACK) emit(a.at, true, true);
+    tile product[4] = {};
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        if (n <= w && 2 * s <= w && 2 * s + 1 >= n) {
+          float e[LANE];
+#pragma unroll
+          for (int j = 0; j < LANE; ++j) e[j] = x[32 * s + 8 * q4 + j][16 * n + r];
+          multiply(product[n], pm[s], operand<PC>(e));
+        }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[16 * w + 4 * q4 + e][16 * n + r] = product[n][e];
+    __syncthreads();
+    if constexpr (BACK) emit(a.bt, true, false);
+    else emit(a.bf, false, false);
     __syncthreads();
   }
 }
@@ -446,11 +479,10 @@ __device__ __forceinline__ Unit unit_of(unsigned id, int units, int blocks) {
 }
 
 // REC: of the backward pass, from a kept state to the next; leaves S and w of each chunk.
-template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) void k_walk(Args a) {
+template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
   __shared__ __align__(16) Planes<PC, BV, DK + 8> st;
   __shared__ __align__(16) Planes<PC, BV, LINE> et, wt;
-  __shared__ __align__(16) Planes<REC ? 1 : PC, REC ? 1 : BV, LINE> ut;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
   const int per = a.batch * a.heads;
   const Unit u = unit_of(blockIdx.x % (per * a.blocks), per, a.blocks);
@@ -485,9 +517,9 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) v
   const int row0 = 16 * w + 4 * q4;
   // What the next chunk needs is on its way while this one is worked on: each part is asked for as soon as this chunk's has been used.
   Operand<PI> k[KK], q[REC ? 1 : KK], kt[RT][2];
-  Operand<PC> am[2], pm[2];
+  Operand<PC> am[2], bm[2];
   Values<T, NT> v;
-  tile gam, tail, beta;
+  tile gam, left; // left: gam_end / gam beta
   float end;
   auto of_keys = [&](int c) { return (((long long)c * a.batch + b) * a.key_heads + kh) * (DK * C * PI); };
   auto of_head = [&](int c) { return ((long long)c * a.batch + b) * a.heads + h; };
@@ -513,7 +545,8 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) v
   };
   auto ask_gates = [&](int c) {
     const float *gates = a.gates + of_head(c) * (3 * C);
-    gam = *(const tile *)(gates + row0), tail = *(const tile *)(gates + C + row0), beta = *(const tile *)(gates + 2 * C + row0);
+    gam = *(const tile *)(gates + row0);
+    if constexpr (REC) left = *(const tile *)(gates + C + row0) * *(const tile *)(gates + 2 * C + row0);
     end = gates[C - 1];
   };
   if (c0 < c1) {
@@ -521,7 +554,7 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) v
     ask_rows(c0);
     ask_values(c0);
     ask_squares(a.af, c0, am);
-    if constexpr (!REC) ask_squares(a.pf, c0, pm);
+    if constexpr (!REC) ask_squares(a.bf, c0, bm);
     ask_columns(c0);
   }
   for (int c = c0; c < c1; ++c) {
@@ -564,14 +597,19 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) v
     ask_values(next);
     lds_barrier();
     tile x[NT] = {};
+    if constexpr (!REC)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[n] *= gam * a.scale;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
-      if (2 * j <= w) { // (A is lower triangular)
+      if (2 * j <= w) { // (A and B are lower triangular)
         Operand<PC> y[NT];
         et.get(r, 32 * j + 8 * q4, y);
         multiply(x, am[j], y);
+        if constexpr (!REC) multiply(o, bm[j], y);
       }
     ask_squares(a.af, next, am);
+    if constexpr (!REC) ask_squares(a.bf, next, bm);
     if constexpr (REC) {
       float *to = a.w + (of_head(c) * C + row0) * a.dvp + v0 + r;
 #pragma unroll
@@ -581,25 +619,9 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) v
           if (v0 + 16 * n < a.dvp) to[i * a.dvp + 16 * n] = x[n][i];
     }
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const tile un = x[n] * beta;
-      if constexpr (!REC) ut.put(16 * n + r, row0, un);
-      wt.put(16 * n + r, row0, un * tail);
-    }
+    for (int n = 0; n < NT; ++n) wt.put(16 * n + r, row0, REC ? x[n] * left : x[n]);
+    if constexpr (!REC) values_to<T, NT>(a.o, a.ld_o, a, b, t0 + row0, len, h * a.dv, v0 + r, a.dv, t0 + C <= len && v0 + BV <= a.dv, o);
     lds_barrier();
-    if constexpr (!REC) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) o[n] *= gam * a.scale;
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        if (2 * j <= w) {
-          Operand<PC> y[NT];
-          ut.get(r, 32 * j + 8 * q4, y);
-          multiply(o, pm[j], y);
-        }
-      ask_squares(a.pf, next, pm);
-      values_to<T, NT>(a.o, a.ld_o, a, b, t0 + row0, len, h * a.dv, v0 + r, a.dv, t0 + C <= len && v0 + BV <= a.dv, o);
-    }
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -619,11 +641,11 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256) v
 }
 
 // ---- the walk back --------------------------------------------------------------------------------
-template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk_back(Args a) {
+template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk_back(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
   __shared__ __align__(16) Planes<PC, BV, DK + 8> st;
   __shared__ __align__(16) Planes<PI, BV, LINE> ot;
-  __shared__ __align__(16) Planes<PC, BV, LINE> got, ut, et; // scale gam dO, beta dU, -gam dE
+  __shared__ __align__(16) Planes<PC, BV, LINE> got, ut, et; // scale gam dO, K dS', -gam dE
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
   const int per = a.batch * a.heads;
   const Unit u = unit_of(blockIdx.x, per, a.blocks);
@@ -643,9 +665,9 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
   const int row0 = 16 * w + 4 * q4;
   // (as in k_walk)
   Operand<PI> k[KK], kt[RT][2], qt[RT][2];
-  Operand<PC> am[2], pm[2];
+  Operand<PC> am[2], bm[2];
   Values<T, NT> raw; // of dO
-  tile gam, tail, beta;
+  tile gam;
   float end;
   auto of_keys = [&](int c) { return (((long long)c * a.batch + b) * a.key_heads + kh) * (DK * C * PI); };
   auto of_head = [&](int c) { return ((long long)c * a.batch + b) * a.heads + h; };
@@ -671,7 +693,7 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
   };
   auto ask_gates = [&](int c) {
     const float *gates = a.gates + of_head(c) * (3 * C);
-    gam = *(const tile *)(gates + row0), tail = *(const tile *)(gates + C + row0), beta = *(const tile *)(gates + 2 * C + row0);
+    gam = *(const tile *)(gates + row0);
     end = gates[C - 1];
   };
   if (a.chunks) {
@@ -679,8 +701,8 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
     ask_gates(c);
     ask_values(c);
     ask_rows(c);
-    ask_squares(a.ptf, c, pm);
-    ask_squares(a.atf, c, am);
+    ask_squares(a.bt, c, bm);
+    ask_squares(a.at, c, am);
     ask_columns(c);
   }
   for (int c = a.chunks - 1; c >= 0; --c) {
@@ -718,19 +740,17 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
     }
     ask_rows(next);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) d[n] *= tail;
+    for (int n = 0; n < NT; ++n) ut.put(16 * n + r, row0, d[n]);
+    tile x[NT] = {};
 #pragma unroll
     for (int j = 0; j < 2; ++j)
-      if (2 * j + 1 >= w) { // (P^T is upper triangular)
+      if (2 * j + 1 >= w) { // (transposed, A1 and B are upper triangular)
         Operand<PI> y[NT];
         ot.get(r, 32 * j + 8 * q4, y);
-        multiply(d, pm[j], y);
+        multiply(x, bm[j], y);
       }
-    ask_squares(a.ptf, next, pm);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) ut.put(16 * n + r, row0, d[n] * beta);
+    ask_squares(a.bt, next, bm);
     lds_barrier();
-    tile x[NT] = {};
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       if (2 * j + 1 >= w) {
@@ -738,7 +758,7 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256) void k_walk
         ut.get(r, 32 * j + 8 * q4, y);
         multiply(x, am[j], y);
       }
-    ask_squares(a.atf, next, am);
+    ask_squares(a.at, next, am);
     float *ep = a.de + (of * C + row0) * a.dvp + v0 + r;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -1163,11 +1183,11 @@ struct Plan {
       for (__bf16 **x : {&a.kf, &a.qf, &a.ktf}) take(*x, nk * dk * C * pi);
       take(a.af, nh * C * C * pc);
       take(a.gates, nh * 3 * C);
-      if (!back) take(a.pf, nh * C * C * pc);
+      if (!back) take(a.bf, nh * C * C * pc);
       else {
         take(a.qtf, nk * dk * C * pi);
-        take(a.ptf, nh * C * C * pc);
-        take(a.atf, nh * C * C * pc);
+        take(a.bt, nh * C * C * pc);
+        take(a.at, nh * C * C * pc);
         take(a.sums, nh * C);
         take(a.before, nh * dk * dvp);
         take(a.after, nh * dk * dvp);
