@@ -35,8 +35,7 @@ typedef float tile __attribute__((ext_vector_type(4)));
 
 constexpr int C = 64;      // steps of a chunk
 constexpr int KEPT = SNN_DELTA_INTERVAL / C;
-constexpr int LINE = C + 8;  // elements from row to row in LDS: 16 lanes read 16 bytes of as many rows from all 64 banks
-constexpr int FLINE = C + 4; // the same of floats
+constexpr int FLINE = C + 4; // floats from row to row of a matrix of a chunk's steps in LDS
 constexpr float LOG2E = 1.44269504f;
 
 template <class T> constexpr int GIVEN = sizeof(T) == 2 ? 1 : 3; // parts of what the caller's arrays hold
@@ -119,18 +118,29 @@ template <int P> __device__ __forceinline__ void leave(__bf16 *p, int number, in
 #pragma unroll
   for (int i = 0; i < P; ++i) *(frag *)(p + ((number * P + i) * 64 + lane) * LANE) = x.p[i];
 }
-// and in LDS: planes of rows
-template <int P, int ROWS, int STRIDE> struct Planes {
-  __bf16 e[P][ROWS * STRIDE];
+// and in LDS: planes of rows, whose 16-byte chunks are exchanged in a way that depends on the row.  A read of 16 bytes a lane takes the lanes in fours of
+// four, 0-3, 12-15, 20-23 and 24-27 the first, that is rows 0-3 and 12-15 of one chunk and 4-11 of the next: each of the four has all 64 banks to
+// itself then (4.3 cycles for a wavefront's; rows with 16 bytes between them 8, whole rows 24).
+template <int P, int ROWS, int COLS> struct Planes {
+  static_assert(COLS == 128 || COLS == 64 || COLS == 32, "rows of 256, 128 or 64 bytes");
+  __bf16 e[P][ROWS * COLS];
+  static __device__ __forceinline__ int place(int row, int col) {
+    const int chunk = col >> 3, other = COLS == 128 ? row & 15 : COLS == 64 ? row >> 1 & 7 : -(row >> 2) & 3;
+    return row * COLS + ((chunk ^ other) << 3) + (col & 7);
+  }
   __device__ __forceinline__ Operand<P> get(int row, int col) const {
     Operand<P> r;
 #pragma unroll
-    for (int i = 0; i < P; ++i) r.p[i] = *(const frag *)(e[i] + row * STRIDE + col);
+    for (int i = 0; i < P; ++i) r.p[i] = *(const frag *)(e[i] + place(row, col));
     return r;
   }
   template <int N> __device__ __forceinline__ void get(int row, int col, Operand<P> (&r)[N]) const { // of every 16th row
 #pragma unroll
     for (int n = 0; n < N; ++n) r[n] = get(row + 16 * n, col);
+  }
+  __device__ __forceinline__ void put(int row, int col, const Operand<P> &x) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) *(frag *)(e[i] + place(row, col)) = x.p[i];
   }
   // four elements of a row
   __device__ __forceinline__ void put(int row, int col, const tile &x) {
@@ -142,7 +152,7 @@ template <int P, int ROWS, int STRIDE> struct Planes {
       four f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) f[j] = parts[i][j];
-      *(four *)(e[i] + row * STRIDE + col) = f;
+      *(four *)(e[i] + place(row, col)) = f;
     }
   }
 };
@@ -154,45 +164,75 @@ __device__ __forceinline__ void lds_barrier() { // of the LDS alone: loads from 
 }
 
 template <class T> __device__ __forceinline__ float element(const T *p, bool on) { return on ? (float)*p : 0.f; }
-// Four rows of a chunk and every 16th column.  They are asked for as they are in memory and made values of when they are used, which is what waits for them.
-// What is beside the array is read from its last row and column instead, without a branch for each, and is zeros then.
+// Four rows of a chunk and every 16th column of an array of values, from a head's first value of the chunk's first step on: places in a chunk fit 32 bits.
+struct Part {
+  unsigned step;       // elements from step to step
+  int row, col, cols;  // the lane's first row and column, the columns that there are
+};
+// They are asked for as they are in memory and made values of when they are used, which is what waits for them.  `rows`: those from the chunk's first on that
+// are in the array; what is beside it is read from its last row and column instead, without a branch for each.
 template <class T, int N> struct Values {
   typedef typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type Bits;
   Bits raw[4][N];
-  __device__ __forceinline__ void ask(const void *p, long long ld, const Args &a, int b, int t, int first, int col, int cols) {
+  __device__ __forceinline__ void ask(const T *head, const Part &p, int rows, bool whole) {
+    const Bits *at = (const Bits *)head;
+    if (whole) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const Bits *row = (const Bits *)p + ((long long)min(t + e, a.T - 1) * a.batch + b) * ld + first;
+      for (int e = 0; e < 4; ++e) {
+        const unsigned off = (unsigned)(p.row + e) * p.step + p.col;
 #pragma unroll
-      for (int n = 0; n < N; ++n) raw[e][n] = row[min(col + 16 * n, cols - 1)];
-    }
+        for (int n = 0; n < N; ++n) raw[e][n] = (at + 16 * n)[off];
+      }
+    } else
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const unsigned off = (unsigned)min(p.row + e, rows - 1) * p.step;
+#pragma unroll
+        for (int n = 0; n < N; ++n) raw[e][n] = at[off + min(p.col + 16 * n, p.cols - 1)];
+      }
   }
-  __device__ __forceinline__ tile get(int n, int t, int len, int col, int cols) const {
+  // zeros behind the sequence's `live` rows and beside the array
+  __device__ __forceinline__ tile get(int n, const Part &p, int live, bool whole) const {
     tile v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float x = sizeof(T) == 2 ? __uint_as_float((uint32_t)raw[e][n] << 16) : __uint_as_float((uint32_t)raw[e][n]);
-      v[e] = t + e < len && col + 16 * n < cols ? x : 0.f;
-    }
+    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(sizeof(T) == 2 ? (uint32_t)raw[e][n] << 16 : (uint32_t)raw[e][n]);
+    if (!whole)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = p.row + e < live && p.col + 16 * n < p.cols ? v[e] : 0.f;
     return v;
   }
 };
-// and back; `whole`: all of them are there
-template <class T, int N> __device__ __forceinline__ void values_to(void *p, long long ld, const Args &a, int b, int t, int len, int first, int col, int cols, bool whole,
-                                                                    const tile (&v)[N]) {
-  T *to = (T *)p + ((long long)t * a.batch + b) * ld + first + col;
-  const long long step = (long long)a.batch * ld;
-  if (whole) {
+template <class T, int N> __device__ __forceinline__ void values_to(T *head, const Part &p, int rows, int live, bool whole, const tile (&v)[N]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const unsigned off = (unsigned)(p.row + e) * p.step + p.col;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (whole) (head + 16 * n)[off] = (T)v[n][e];
+      else if (p.row + e < rows && p.col + 16 * n < p.cols) (head + 16 * n)[off] = (T)(p.row + e < live ? v[n][e] : 0.f);
+  }
+}
+// Waits for all loads, where the compiler would else wait for what comes from before a loop in each of its turns, and for all that was asked for since
+__device__ __forceinline__ void loaded() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+// Tiles of a state between registers and memory: rows of the lane's wavefront from `row` on, RT tiles of them, every 16th column from col on
+template <int RT, int NT> __device__ __forceinline__ void state_from(const float *from, int row, int col, int rows, int cols, tile (&s)[RT][NT]) {
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        s[i][n][e] = element(from + (long long)(row + 16 * i + e) * cols + col + 16 * n, row + 16 * i + e < rows && col + 16 * n < cols);
+}
+template <int RT, int NT> __device__ __forceinline__ void state_to(float *to, int row, int col, int rows, int cols, bool whole, const tile (&s)[RT][NT]) {
+  const unsigned off = (unsigned)row * cols + col;
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int n = 0; n < N; ++n) to[e * step + 16 * n] = (T)v[n][e];
-  } else
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-        if (t + e < a.T && col + 16 * n < cols) to[e * step + 16 * n] = (T)(t + e < len ? v[n][e] : 0.f);
+      for (int n = 0; n < NT; ++n)
+        if (whole || (row + 16 * i + e < rows && col + 16 * n < cols)) (to + (16 * i + e) * cols + 16 * n)[off] = s[i][n][e];
 }
 
 // Elements as they are in memory, asked for ahead of their use
@@ -253,7 +293,7 @@ template <class T> struct Quad { // 4 of a row
 // ONE: each head has queries and keys of its own.
 template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256, ONE ? sizeof(T) == 2 || DK == 64 ? 4 : 3 : 2) void k_chunk(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32;
-  typedef Planes<PI, C, DK + 8> Rows;
+  typedef Planes<PI, C, DK> Rows;
   struct Squares { float m[C][FLINE], x[C][FLINE]; };
   __shared__ __align__(16) char space[sizeof(Rows) > sizeof(Squares) ? sizeof(Rows) : sizeof(Squares)];
   __shared__ double sum[C];
@@ -307,9 +347,7 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
   };
   auto to_lds = [&](const Operand<PI> (&f)[KK]) {
 #pragma unroll
-    for (int i = 0; i < KK; ++i)
-#pragma unroll
-      for (int p = 0; p < PI; ++p) *(frag *)(rows.e[p] + (16 * w + r) * (DK + 8) + 32 * i + 8 * q4) = f[i].p[p];
+    for (int i = 0; i < KK; ++i) rows.put(16 * w + r, 32 * i + 8 * q4, f[i]);
   };
   auto turned = [&](__bf16 *to) { // rows of channels
 #pragma unroll 1
@@ -318,7 +356,7 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
 #pragma unroll
       for (int p = 0; p < PI; ++p)
 #pragma unroll
-        for (int j = 0; j < LANE; ++j) y.p[p][j] = rows.e[p][(32 * (f & 1) + 8 * q4 + j) * (DK + 8) + 16 * (f >> 1) + r];
+        for (int j = 0; j < LANE; ++j) y.p[p][j] = rows.e[p][Rows::place(32 * (f & 1) + 8 * q4 + j, 16 * (f >> 1) + r)];
       leave<PI>(to + (long long)unit * SIZE, f, lane, y);
     }
   };
@@ -481,38 +519,19 @@ __device__ __forceinline__ Unit unit_of(unsigned id, int units, int blocks) {
 // REC: of the backward pass, from a kept state to the next; leaves S and w of each chunk.
 template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
-  __shared__ __align__(16) Planes<PC, BV, DK + 8> st;
-  __shared__ __align__(16) Planes<PC, BV, LINE> et, wt;
+  __shared__ __align__(16) Planes<PC, BV, DK> st;
+  __shared__ __align__(16) Planes<PC, BV, C> et, wt;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
   const int per = a.batch * a.heads;
   const Unit u = unit_of(blockIdx.x % (per * a.blocks), per, a.blocks);
   const int segment = blockIdx.x / (per * a.blocks); // REC: of KEPT chunks
   const int h = u.of % a.heads, b = u.of / a.heads, kh = h / (a.heads / a.key_heads), v0 = u.block * BV;
   const int len = length_of(a, b);
+  const int srow = 16 * w * RT + 4 * q4, col = v0 + r;
+  const bool cols = v0 + BV <= a.dv, all = cols && a.dk == DK; // the columns, the state are there
   tile s[RT][NT] = {};
-  if (a.from) {
-    const float *from = a.from + ((REC ? (long long)(a.first / KEPT + segment) * per : 0) + u.of) * a.dk * a.dv;
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
-          s[i][n][e] = element(from + (long long)row * a.dv + col, row < a.dk && col < a.dv);
-        }
-  }
-  auto state_to = [&](float *to) {
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
-          if (row < a.dk && col < a.dv) to[(long long)row * a.dv + col] = s[i][n][e];
-        }
-  };
+  if (a.from) state_from(a.from + ((REC ? (long long)(a.first / KEPT + segment) * per : 0) + u.of) * a.dk * a.dv, srow, col, a.dk, a.dv, s);
+  loaded();
   const int c0 = REC ? segment * KEPT : 0, c1 = REC ? min(c0 + KEPT, a.chunks) : a.chunks;
   const int row0 = 16 * w + 4 * q4;
   // What the next chunk needs is on its way while this one is worked on: each part is asked for as soon as this chunk's has been used.
@@ -530,8 +549,10 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
       if constexpr (!REC) q[i] = fetch<PI>(a.qf + of_keys(c), w * KK + i, lane);
     }
   };
+  const Part of_v = {(unsigned)(a.batch * a.ld_v), row0, col, a.dv}, of_o = {(unsigned)(a.batch * a.ld_o), row0, col, a.dv};
   auto ask_values = [&](int c) {
-    v.ask(a.v, a.ld_v, a, b, (a.first + c) * C + row0, h * a.dv, v0 + r, a.dv);
+    const int t0 = (a.first + c) * C;
+    v.ask((const T *)a.v + ((long long)t0 * a.batch + b) * a.ld_v + h * a.dv, of_v, a.T - t0, cols && t0 + C <= a.T);
   };
   auto ask_squares = [&](const __bf16 *p, int c, Operand<PC> (&m)[2]) { // (lower triangular: the first two rows of blocks have zeros behind)
     m[0] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w, lane);
@@ -550,29 +571,20 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
     end = gates[C - 1];
   };
   if (c0 < c1) {
-    ask_gates(c0);
     ask_rows(c0);
     ask_values(c0);
     ask_squares(a.af, c0, am);
     if constexpr (!REC) ask_squares(a.bf, c0, bm);
     ask_columns(c0);
+    ask_gates(c0);
   }
   for (int c = c0; c < c1; ++c) {
     const int t0 = (a.first + c) * C, next = min(c + 1, c1 - 1);
+    const bool whole = cols && t0 + C <= len;
     if constexpr (!REC) {
-      if (a.kept && (a.first + c) % KEPT == 0) state_to(a.kept + ((long long)((a.first + c) / KEPT) * per + u.of) * a.dk * a.dv);
-    } else {
-      float *to = a.before + of_head(c) * DK * a.dvp;
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
-            if (v0 + 16 * n < a.dvp) to[row * a.dvp + col] = s[i][n][e];
-          }
-    }
+      if (a.kept && (a.first + c) % KEPT == 0)
+        state_to(a.kept + ((long long)((a.first + c) / KEPT) * per + u.of) * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
+    } else state_to(a.before + of_head(c) * DK * a.dvp, srow, col, DK, a.dvp, true, s); // (dvp is a multiple of the 32 columns of a workgroup)
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -589,7 +601,7 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
     ask_rows(next);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const tile vn = v.get(n, t0 + row0, len, v0 + r, a.dv);
+      const tile vn = v.get(n, of_v, len - t0, whole);
 #pragma unroll
       for (int i = 0; i < 4; ++i) e[n][i] = fmaf(-gam[i], e[n][i], vn[i]);
       et.put(16 * n + r, row0, e[n]);
@@ -610,17 +622,10 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
       }
     ask_squares(a.af, next, am);
     if constexpr (!REC) ask_squares(a.bf, next, bm);
-    if constexpr (REC) {
-      float *to = a.w + (of_head(c) * C + row0) * a.dvp + v0 + r;
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (v0 + 16 * n < a.dvp) to[i * a.dvp + 16 * n] = x[n][i];
-    }
+    if constexpr (REC) state_to(a.w + of_head(c) * C * a.dvp, row0, col, C, a.dvp, true, (const tile (&)[1][NT])x);
 #pragma unroll
     for (int n = 0; n < NT; ++n) wt.put(16 * n + r, row0, REC ? x[n] * left : x[n]);
-    if constexpr (!REC) values_to<T, NT>(a.o, a.ld_o, a, b, t0 + row0, len, h * a.dv, v0 + r, a.dv, t0 + C <= len && v0 + BV <= a.dv, o);
+    if constexpr (!REC) values_to<T, NT>((T *)a.o + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv, of_o, a.T - t0, len - t0, whole, o);
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -637,31 +642,25 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
     ask_gates(next);
   }
   if constexpr (!REC)
-    if (a.to) state_to(a.to + (long long)u.of * a.dk * a.dv);
+    if (a.to) state_to(a.to + (long long)u.of * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
 }
 
 // ---- the walk back --------------------------------------------------------------------------------
 template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk_back(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
-  __shared__ __align__(16) Planes<PC, BV, DK + 8> st;
-  __shared__ __align__(16) Planes<PI, BV, LINE> ot;
-  __shared__ __align__(16) Planes<PC, BV, LINE> got, ut, et; // scale gam dO, K dS', -gam dE
+  __shared__ __align__(16) Planes<PC, BV, DK> st;
+  __shared__ __align__(16) Planes<PI, BV, C> ot;
+  __shared__ __align__(16) Planes<PC, BV, C> got, ut, et; // scale gam dO, K dS', -gam dE
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
   const int per = a.batch * a.heads;
   const Unit u = unit_of(blockIdx.x, per, a.blocks);
   const int h = u.of % a.heads, b = u.of / a.heads, kh = h / (a.heads / a.key_heads), v0 = u.block * BV;
   const int len = length_of(a, b);
+  const int srow = 16 * w * RT + 4 * q4, col = v0 + r;
+  const bool cols = v0 + BV <= a.dv, all = cols && a.dk == DK;
   tile s[RT][NT] = {};
-  if (a.from)
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
-          s[i][n][e] = element(a.from + ((long long)u.of * a.dk + row) * a.dv + col, row < a.dk && col < a.dv);
-        }
+  if (a.from) state_from(a.from + (long long)u.of * a.dk * a.dv, srow, col, a.dk, a.dv, s);
+  loaded();
   const int row0 = 16 * w + 4 * q4;
   // (as in k_walk)
   Operand<PI> k[KK], kt[RT][2], qt[RT][2];
@@ -675,8 +674,10 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
 #pragma unroll
     for (int i = 0; i < KK; ++i) k[i] = fetch<PI>(a.kf + of_keys(c), w * KK + i, lane);
   };
+  const Part of_o = {(unsigned)(a.batch * a.ld_o), row0, col, a.dv}, of_v = {(unsigned)(a.batch * a.ld_dv), row0, col, a.dv};
   auto ask_values = [&](int c) {
-    raw.ask(a.dout, a.ld_o, a, b, (a.first + c) * C + row0, h * a.dv, v0 + r, a.dv);
+    const int t0 = (a.first + c) * C;
+    raw.ask((const T *)a.dout + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv, of_o, a.T - t0, cols && t0 + C <= a.T);
   };
   auto ask_squares = [&](const __bf16 *p, int c, Operand<PC> (&m)[2]) { // (upper triangular: the last two rows of blocks begin with zeros)
     if (w < 2) m[0] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w, lane);
@@ -698,33 +699,26 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
   };
   if (a.chunks) {
     const int c = a.chunks - 1;
-    ask_gates(c);
     ask_values(c);
     ask_rows(c);
     ask_squares(a.bt, c, bm);
     ask_squares(a.at, c, am);
     ask_columns(c);
+    ask_gates(c);
   }
   for (int c = a.chunks - 1; c >= 0; --c) {
     const int t0 = (a.first + c) * C, next = max(c - 1, 0);
     const long long of = of_head(c);
-    {
-      float *to = a.after + of * DK * a.dvp;
+    const bool whole = cols && t0 + C <= len;
+    state_to(a.after + of * DK * a.dvp, srow, col, DK, a.dvp, true, s);
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const int row = 16 * (w * RT + i) + 4 * q4, col = v0 + 16 * n + r;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (v0 + 16 * n < a.dvp) to[(row + e) * a.dvp + col] = s[i][n][e];
-          st.put(16 * n + r, row, s[i][n]);
-        }
-    }
+      for (int n = 0; n < NT; ++n) st.put(16 * n + r, srow + 16 * i, s[i][n]);
     tile given[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      given[n] = raw.get(n, t0 + row0, len, v0 + r, a.dv);
+      given[n] = raw.get(n, of_o, len - t0, whole);
       ot.put(16 * n + r, row0, given[n]);
     }
     lds_barrier(); // (and every wavefront is through with the last chunk)
@@ -759,17 +753,15 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
         multiply(x, am[j], y);
       }
     ask_squares(a.at, next, am);
-    float *ep = a.de + (of * C + row0) * a.dvp + v0 + r;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+      if (!whole)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (t0 + row0 + e >= len) x[n][e] = 0.f;
-        if (v0 + 16 * n < a.dvp) ep[e * a.dvp + 16 * n] = x[n][e];
-      }
+        for (int e = 0; e < 4; ++e) x[n][e] = t0 + row0 + e < len ? x[n][e] : 0.f;
       et.put(16 * n + r, row0, x[n] * -gam);
     }
-    values_to<T, NT>(a.dv_, a.ld_dv, a, b, t0 + row0, len, h * a.dv, v0 + r, a.dv, t0 + C <= len && v0 + BV <= a.dv, x);
+    state_to(a.de + of * C * a.dvp, row0, col, C, a.dvp, true, (const tile (&)[1][NT])x);
+    values_to<T, NT>((T *)a.dv_ + ((long long)t0 * a.batch + b) * a.ld_dv + h * a.dv, of_v, a.T - t0, len - t0, whole, x);
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -788,16 +780,7 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
     ask_columns(next);
     ask_gates(next);
   }
-  if (a.to)
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = 16 * (w * RT + i) + 4 * q4 + e, col = v0 + 16 * n + r;
-          if (row < a.dk && col < a.dv) a.to[((long long)u.of * a.dk + row) * a.dv + col] = s[i][n][e];
-        }
+  if (a.to) state_to(a.to + (long long)u.of * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
 }
 
 // ---- gradients of a chunk's queries, keys and gates -----------------------------------------------
@@ -805,8 +788,7 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
 // row.
 template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (sizeof(T) == 2 || DK == 64) ? 2 : 1) void k_grads(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, NT = DK / 16, NS = DK / 64;
-  constexpr int SLICE = 32 + 8; // a row's 32 columns in LDS
-  struct Sums { Planes<PC, DK, SLICE> before, after; Planes<PC, C, SLICE> w; };
+  struct Sums { Planes<PC, DK, 32> before, after; Planes<PC, C, 32> w; };
   struct Squares { float dp[C][FLINE], m[C][FLINE]; };
   __shared__ __align__(16) char space[sizeof(Sums) > sizeof(Squares) ? sizeof(Sums) : sizeof(Squares)];
   __shared__ float of_col[4][C], of_row[3][C], of_all[4], gates[3][C];
@@ -852,9 +834,7 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
       }
       float y[LANE], z[LANE];
       auto to_lds = [&](const float (&from)[LANE], auto &planes, int row) {
-        const Operand<PC> f = operand<PC>(from);
-#pragma unroll
-        for (int k = 0; k < PC; ++k) *(frag *)(planes.e[k] + row * SLICE + scol) = f.p[k];
+        planes.put(row, scol, operand<PC>(from));
       };
 #pragma unroll
       for (int n = 0; n < NS; ++n) {

@@ -158,7 +158,8 @@ snn_status delta_shape(const char *what, const snn_delta *p, DeltaShape *d) {
                                                  {&d->ld_dq, of_keys}, {&d->ld_dk, of_keys}, {&d->ld_dv, of_values}};
   for (auto [ld, least] : lds) {
     if (!*ld) *ld = least;
-    if (*ld < least || *ld > (1 << 30)) return refuse(SNN_E_INVAL, "%s: %lld elements from row to row: those of all heads .. 2^30", what, *ld);
+    if (*ld < least || *ld > (1 << 25) / p->batch / (long long)size_of(p->dtype)) // (places in a chunk of 64 steps fit 32 bits)
+      return refuse(SNN_E_INVAL, "%s: %lld elements from row to row: those of all heads or more, and 2^25 bytes per step at most", what, *ld);
   }
   return SNN_OK;
 }

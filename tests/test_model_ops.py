@@ -911,7 +911,7 @@ def test_c_entry_points_of_the_delta_rule_refuse_what_they_cannot_run():
         for bad in (dict(batch=0), dict(batch=1 << 20), dict(batch=1 << 17, dv=1024)):
             refused(lambda: call(shape(**bad)), "2^20")
         refused(lambda: call(shape(scale=math.inf)), "scale")
-        for bad in (dict(ld_q=15), dict(ld_v=31), dict(ld_dv=-1), dict(ld_o=1 << 31)):
+        for bad in (dict(ld_q=15), dict(ld_v=31), dict(ld_dv=-1), dict(ld_o=(1 << 22) + 1), dict(batch=1 << 18, dv=16)):
             refused(lambda: call(shape(**bad)), "elements from row to row")
         refused(lambda: call(shape(), first=None), "q is NULL")
         refused(lambda: call(shape(), first=here + 2), "not aligned")
