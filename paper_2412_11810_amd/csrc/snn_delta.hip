@@ -138,6 +138,16 @@ template <int P, int ROWS, int COLS> struct Planes {
 #pragma unroll
     for (int n = 0; n < N; ++n) r[n] = get(row + 16 * n, col);
   }
+  __device__ __forceinline__ tile four_of(int row, int col) const {
+    tile r = {};
+#pragma unroll
+    for (int i = P - 1; i >= 0; --i) {
+      const four f = *(const four *)(e[i] + place(row, col));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r[j] += (float)f[j];
+    }
+    return r;
+  }
   __device__ __forceinline__ void put(int row, int col, const Operand<P> &x) {
 #pragma unroll
     for (int i = 0; i < P; ++i) *(frag *)(e[i] + place(row, col)) = x.p[i];
@@ -785,46 +795,48 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
 
 // ---- gradients of a chunk's queries, keys and gates -----------------------------------------------
 // Sums over the state's columns go through LDS 32 at a time, the next ones on their way; results are [dk][t], so that a lane has four elements of one step's
-// row.
-template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (sizeof(T) == 2 || DK == 64) ? 2 : 1) void k_grads(Args a) {
-  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, NT = DK / 16, NS = DK / 64;
+// row.  Eight wavefronts: four take 16 steps each, with one half of the channels, and of the chunk's steps before theirs, four with the other.
+template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k_grads(Args a) {
+  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, NT = DK / 32; // NT: tiles of a half of the channels
   struct Sums { Planes<PC, DK, 32> before, after; Planes<PC, C, 32> w; };
+  struct Rows { Planes<PI, C, DK> q, k; };
   struct Squares { float dp[C][FLINE], m[C][FLINE]; };
-  __shared__ __align__(16) char space[sizeof(Sums) > sizeof(Squares) ? sizeof(Sums) : sizeof(Squares)];
-  __shared__ float of_col[4][C], of_row[3][C], of_all[4], gates[3][C];
+  constexpr size_t FIRST = sizeof(Sums) > sizeof(Squares) ? sizeof(Sums) : sizeof(Squares);
+  __shared__ __align__(16) char space[sizeof(Rows) > FIRST ? sizeof(Rows) : FIRST];
+  __shared__ float of_col[4][C], of_row[3][2][C], of_all[8], gates[3][C];
   __shared__ double G[C];
   Sums &sums = *(Sums *)space;
+  Rows &rows = *(Rows *)space;
   Squares &squares = *(Squares *)space;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3, half = wave >> 2, r = lane & 15, q4 = lane >> 4;
   const int unit = blockIdx.x, kh = unit % a.key_heads, b = unit / a.key_heads % a.batch, c = unit / a.key_heads / a.batch;
   const int t0 = (a.first + c) * C, len = length_of(a, b), group = ONE ? 1 : a.heads / a.key_heads, row0 = 16 * w + 4 * q4;
   const int mine = 16 * w + r, t = t0 + mine; // a lane's step
-  const T *qp = (const T *)a.q + ((long long)t * a.batch + b) * a.ld_q + kh * a.dk, *kp = (const T *)a.k + ((long long)t * a.batch + b) * a.ld_k + kh * a.dk;
   tile gq[NT] = {}, gk[NT] = {};
   for (int i = 0; i < group; ++i) {
     const int h = kh * group + i;
     const long long of = ((long long)c * a.batch + b) * a.heads + h;
     long long of_k = (long long)unit * (DK * C * PI);
-    if constexpr (!ONE) asm volatile("" : "+s"(of_k), "+v"(qp), "+v"(kp)); // (what is the same for all heads is read again for each: there are no registers to keep it)
-    const float *before = a.before + of * DK * a.dvp, *after = a.after + of * DK * a.dvp, *wp = a.w + of * C * a.dvp, *ep = a.de + (of * C + mine) * a.dvp + 8 * q4;
-    const T *dp = (const T *)a.dout + ((long long)t * a.batch + b) * a.ld_o + h * a.dv + 8 * q4;
+    if constexpr (!ONE) asm volatile("" : "+s"(of_k)); // (what is the same for all heads is read again for each: there are no registers to keep it)
+    const float *before = a.before + of * DK * a.dvp, *after = a.after + of * DK * a.dvp, *wp = a.w + of * C * a.dvp, *ep = a.de + of * C * a.dvp;
+    const T *dp = (const T *)a.dout + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv;
     const int srow = threadIdx.x / 4, scol = threadIdx.x % 4 * 8; // of what a thread takes to LDS
-    Octet<float> rb[NS], ra[NS], rw, re;
+    Octet<float> rb, ra, rw, re;
     Octet<T> rd;
+    const unsigned off_s = srow * a.dvp + scol, off_e = mine * a.dvp + 8 * q4, off_d = (unsigned)mine * (unsigned)(a.batch * a.ld_o) + 8 * q4;
     auto ask = [&](int v) {
-#pragma unroll
-      for (int n = 0; n < NS; ++n) {
-        rb[n].ask(before + (64 * n + srow) * a.dvp + v + scol, LANE);
-        ra[n].ask(after + (64 * n + srow) * a.dvp + v + scol, LANE);
+      if (threadIdx.x < 4 * DK) {
+        rb.ask((before + v) + off_s, LANE);
+        ra.ask((after + v) + off_s, LANE);
       }
-      rw.ask(wp + srow * a.dvp + v + scol, LANE);
-      re.ask(ep + v, LANE);
-      rd.ask(dp + v, t < len ? a.dv - v - 8 * q4 : 0);
+      if (threadIdx.x < 4 * C) rw.ask((wp + v) + off_s, LANE);
+      re.ask((ep + v) + off_e, LANE);
+      rd.ask((dp + v) + off_d, t < len ? a.dv - v - 8 * q4 : 0);
     };
     const float gate = threadIdx.x < 3 * C ? a.gates[of * (3 * C) + threadIdx.x] : 0.f;
     const double sum = threadIdx.x < C ? a.sums[of * C + threadIdx.x] : 0.;
     ask(0);
-    tile sq[NT] = {}, se[NT] = {}, su[NT] = {}, p[4] = {}, x[4] = {};
+    tile sq[NT] = {}, se[NT] = {}, su[NT] = {}, p[2] = {}, x[2] = {};
     float both = 0.f; // <S, dS'>
     for (int v = 0; v < a.dvp; v += 32) {
       lds_barrier();
@@ -836,17 +848,18 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
       auto to_lds = [&](const float (&from)[LANE], auto &planes, int row) {
         planes.put(row, scol, operand<PC>(from));
       };
-#pragma unroll
-      for (int n = 0; n < NS; ++n) {
-        rb[n].get(y);
-        ra[n].get(z);
+      if (threadIdx.x < 4 * DK) {
+        rb.get(y);
+        ra.get(z);
 #pragma unroll
         for (int j = 0; j < LANE; ++j) both = fmaf(y[j], z[j], both);
-        to_lds(y, sums.before, 64 * n + srow);
-        to_lds(z, sums.after, 64 * n + srow);
+        to_lds(y, sums.before, srow);
+        to_lds(z, sums.after, srow);
       }
-      rw.get(y);
-      to_lds(y, sums.w, srow);
+      if (threadIdx.x < 4 * C) {
+        rw.get(y);
+        to_lds(y, sums.w, srow);
+      }
       rd.get(y);
       const Operand<PI> d = operand<PI>(y);
       re.get(y);
@@ -856,65 +869,88 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
       const Operand<PC> wm = sums.w.get(mine, 8 * q4);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const Operand<PC> s = sums.before.get(16 * n + r, 8 * q4), s2 = sums.after.get(16 * n + r, 8 * q4);
+        const int row = 16 * (half * NT + n) + r;
+        const Operand<PC> s = sums.before.get(row, 8 * q4), s2 = sums.after.get(row, 8 * q4);
         multiply(sq[n], s, d);
         multiply(se[n], s, e);
         multiply(su[n], s2, wm);
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (j <= w) {
-          const Operand<PC> y = sums.w.get(16 * j + r, 8 * q4);
+      for (int j = 0; j < 2; ++j)
+        if (2 * half + j <= w) {
+          const Operand<PC> y = sums.w.get(16 * (2 * half + j) + r, 8 * q4);
           multiply(p[j], d, y);
           multiply(x[j], e, y);
         }
     }
-    lds_barrier();
-    // The rest's loads are asked for ahead, as many at a time as there are registers for
-    Operand<PI> q[KK], k[KK], y[4][KK];
+    // queries and keys of the chunk: what its steps are to each other, and each step's with what came from the states
+    {
+      Operand<PI> q[KK / 2], k[KK / 2];
 #pragma unroll
-    for (int n = 0; n < KK; ++n) {
-      q[n] = fetch<PI>(a.qf + of_k, w * KK + n, lane);
-      k[n] = fetch<PI>(a.kf + of_k, w * KK + n, lane);
+      for (int n = 0; n < KK / 2; ++n) {
+        q[n] = fetch<PI>(a.qf + of_k, w * KK + half * (KK / 2) + n, lane);
+        k[n] = fetch<PI>(a.kf + of_k, w * KK + half * (KK / 2) + n, lane);
+      }
+      lds_barrier();
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (j <= w) y[j][n] = fetch<PI>(a.kf + of_k, j * KK + n, lane);
+      for (int n = 0; n < KK / 2; ++n) {
+        const int col = 32 * (half * (KK / 2) + n) + 8 * q4;
+        rows.q.put(mine, col, q[n]);
+        rows.k.put(mine, col, k[n]);
+      }
+      lds_barrier();
     }
-    __builtin_amdgcn_sched_barrier(0);
-    tile qk[4] = {}, kk[4] = {};
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j <= w)
-#pragma unroll
-        for (int n = 0; n < KK; ++n) {
-          multiply(qk[j], q[n], y[j][n]);
-          multiply(kk[j], k[n], y[j][n]);
-        }
-    __builtin_amdgcn_sched_barrier(0);
-    Quad<T> qe[NT], ke[NT];
+    const float gam = gates[0][mine], tail = gates[1][mine], beta = gates[2][mine], end = gates[0][C - 1];
+    float read_by = 0.f, wrote = 0.f; // what a step reads of what was before, and what is left of its own at the end, but for beta
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int col = 16 * n + 4 * q4, count = t < len ? a.dk - col : 0;
-      qe[n].ask(qp + col, count);
-      ke[n].ask(kp + col, count);
-    }
-    Operand<PI> cols[NT];
-    auto columns = [&](const __bf16 *p, int s) {
+      const int col = 16 * (half * NT + n) + 4 * q4;
+      const tile q = rows.q.four_of(mine, col), k = rows.k.four_of(mine, col);
+      sq[n] *= gam * a.scale;
+      se[n] *= gam;
+      su[n] *= tail;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) cols[n] = fetch<PI>(p + of_k, 2 * n + s, lane);
-    };
-    if constexpr (PI == 1) columns(a.ktf, 0);
+      for (int e = 0; e < 4; ++e) {
+        read_by += fmaf(q[e], sq[n][e], -(k[e] * se[n][e]));
+        wrote = fmaf(k[e], su[n][e], wrote);
+      }
+      gq[n] += sq[n];
+      gk[n] += su[n] * beta - se[n];
+    }
     __builtin_amdgcn_sched_barrier(0);
+    // (the columns that come last are asked for ahead, as many at a time as there are registers for)
+    Operand<PI> kt[2][NT], qt[2][NT];
+    auto columns = [&](int s) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        kt[s][n] = fetch<PI>(a.ktf + of_k, 2 * (half * NT + n) + s, lane);
+        if (2 * s + 1 >= w) qt[s][n] = fetch<PI>(a.qtf + of_k, 2 * (half * NT + n) + s, lane);
+      }
+    };
+    if constexpr (PI == 1) columns(0);
+    tile qk[2] = {}, kk[2] = {};
+#pragma unroll
+    for (int n = 0; n < KK; ++n) {
+      const Operand<PI> q = rows.q.get(mine, 32 * n + 8 * q4), k = rows.k.get(mine, 32 * n + 8 * q4);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (2 * half + j <= w) {
+          const Operand<PI> y = rows.k.get(16 * (2 * half + j) + r, 32 * n + 8 * q4);
+          multiply(qk[j], q, y);
+          multiply(kk[j], k, y);
+        }
+    }
+    lds_barrier();
     tile of_z = {};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int col = 16 * j + r;
+    for (int j = 0; j < 2; ++j) {
+      const int at = 2 * half + j, col = 16 * at + r;
       const float beta_col = gates[2][col];
       float z_col = 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int row = row0 + e;
-        const bool low = j <= w && col <= row, below = j <= w && col < row;
+        const bool low = at <= w && col <= row, below = at <= w && col < row;
         const float d = low ? __builtin_amdgcn_exp2f((float)(G[row] - G[col])) : 0.f;
         const float dps = low ? p[j][e] * d * a.scale : 0.f, me = below ? x[j][e] * d : 0.f; // beta of the column is left out
         const float zq = low ? qk[j][e] * dps : 0.f, zk = below ? kk[j][e] * me : 0.f;
@@ -923,27 +959,11 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
         z_col += z;
         squares.dp[row][col] = dps * beta_col;
         if (below) squares.m[row][col] = squares.m[col][row] = -me * beta_col;
-        if (j == w && col == row) squares.m[row][col] = 0.f;
+        if (at == w && col == row) squares.m[row][col] = 0.f;
       }
 #pragma unroll
       for (int s = 16; s < 64; s *= 2) z_col += __shfl_xor(z_col, s);
       if (q4 == 0) of_col[w][col] = z_col;
-    }
-    const float gam = gates[0][mine], tail = gates[1][mine], beta = gates[2][mine], end = gates[0][C - 1];
-    float read_by = 0.f, wrote = 0.f; // what a step reads of what was before, and what is left of its own at the end, but for beta
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      sq[n] *= gam * a.scale;
-      se[n] *= gam;
-      su[n] *= tail;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float q = (float)qe[n].x[e], k = (float)ke[n].x[e];
-        read_by += fmaf(q, sq[n][e], -(k * se[n][e]));
-        wrote = fmaf(k, su[n][e], wrote);
-      }
-      gq[n] += sq[n];
-      gk[n] += su[n] * beta - se[n];
     }
 #pragma unroll
     for (int s = 16; s < 64; s *= 2) {
@@ -954,14 +974,16 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
     for (int s = 1; s < 16; s *= 2)
 #pragma unroll
       for (int e = 0; e < 4; ++e) of_z[e] += __shfl_xor(of_z[e], s);
-    if (r == 0) *(tile *)(of_row[0] + row0) = of_z;
+    if (r == 0) *(tile *)(of_row[0][half] + row0) = of_z;
     if (q4 == 0) {
-      of_row[1][mine] = read_by;
-      of_row[2][mine] = wrote;
+      of_row[1][half][mine] = read_by;
+      of_row[2][half][mine] = wrote;
     }
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) both += __shfl_xor(both, s);
-    if (lane == 0) of_all[w] = both;
+    if (lane == 0) of_all[wave] = both;
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (PI == 1) columns(1);
     lds_barrier();
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -975,22 +997,19 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
 #pragma unroll
       for (int j = 0; j < LANE; ++j) y[j] = squares.m[mine][32 * s + 8 * q4 + j];
       const Operand<PC> m = operand<PC>(y);
-      if (s || PI > 1) columns(a.ktf, s);
+      if constexpr (PI > 1) columns(s);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        if (2 * s <= w) multiply(gq[n], cols[n], dpf);
-        multiply(gk[n], cols[n], m);
+        if (2 * s <= w) multiply(gq[n], kt[s][n], dpf);
+        multiply(gk[n], kt[s][n], m);
+        if (2 * s + 1 >= w) multiply(gk[n], qt[s][n], dpt);
       }
-      if (2 * s + 1 >= w) {
-        columns(a.qtf, s);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) multiply(gk[n], cols[n], dpt);
-      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (w == 0) {
-      const float beta = gates[2][lane], of_w = (of_col[0][lane] + of_col[1][lane]) + (of_col[2][lane] + of_col[3][lane]), left = of_row[2][lane];
+    if (wave == 0) {
+      const float beta = gates[2][lane], of_w = (of_col[0][lane] + of_col[1][lane]) + (of_col[2][lane] + of_col[3][lane]), left = of_row[2][0][lane] + of_row[2][1][lane];
       const float own = left * beta;
-      double on = (double)of_row[0][lane] + of_row[1][lane] - (double)of_w * beta;
+      double on = ((double)of_row[0][0][lane] + of_row[0][1][lane]) + ((double)of_row[1][0][lane] + of_row[1][1][lane]) - (double)of_w * beta;
       double up = own;
 #pragma unroll
       for (int s = 1; s < C; s *= 2) {
@@ -998,7 +1017,7 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
         if (lane + s < C) on += o;
         if (lane >= s) up += y;
       }
-      const float all = end * ((of_all[0] + of_all[1]) + (of_all[2] + of_all[3]));
+      const float all = end * (((of_all[0] + of_all[1]) + (of_all[2] + of_all[3])) + ((of_all[4] + of_all[5]) + (of_all[6] + of_all[7])));
       if (t0 + lane < a.T) {
         const long long at = ((long long)(t0 + lane) * a.batch + b) * a.heads + h;
         a.dg[at] = t0 + lane < len ? (float)(all + on + (up - own)) : 0.f;
@@ -1010,7 +1029,7 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(256, ONE && (s
   T *dq = (T *)a.dq + ((long long)t * a.batch + b) * a.ld_dq + kh * a.dk, *dk = (T *)a.dk_ + ((long long)t * a.batch + b) * a.ld_dk + kh * a.dk;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int col = 16 * n + 4 * q4;
+    const int col = 16 * (half * NT + n) + 4 * q4;
     Quad<T>::put(dq + col, a.dk - col, t < len ? gq[n] : tile{});
     Quad<T>::put(dk + col, a.dk - col, t < len ? gk[n] : tile{});
   }
@@ -1229,8 +1248,8 @@ template <class T, int DK> hipError_t backward(Plan &p, const float *kept, const
     a.from = from;
     a.to = first ? carry : p.last;
     k_walk_back<T, DK, 32><<<p.per * p.blocks, 256, 0, s>>>(a);
-    if (a.heads == a.key_heads) k_grads<T, DK, true><<<a.chunks * p.units, 256, 0, s>>>(a);
-    else k_grads<T, DK, false><<<a.chunks * p.units, 256, 0, s>>>(a);
+    if (a.heads == a.key_heads) k_grads<T, DK, true><<<a.chunks * p.units, 512, 0, s>>>(a);
+    else k_grads<T, DK, false><<<a.chunks * p.units, 512, 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     from = carry;
   }
