@@ -174,77 +174,6 @@ __device__ __forceinline__ void lds_barrier() { // of the LDS alone: loads from 
 }
 
 template <class T> __device__ __forceinline__ float element(const T *p, bool on) { return on ? (float)*p : 0.f; }
-// Four rows of a chunk and every 16th column of an array of values, from a head's first value of the chunk's first step on: places in a chunk fit 32 bits.
-struct Part {
-  unsigned step;       // elements from step to step
-  int row, col, cols;  // the lane's first row and column, the columns that there are
-};
-// They are asked for as they are in memory and made values of when they are used, which is what waits for them.  `rows`: those from the chunk's first on that
-// are in the array; what is beside it is read from its last row and column instead, without a branch for each.
-template <class T, int N> struct Values {
-  typedef typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type Bits;
-  Bits raw[4][N];
-  __device__ __forceinline__ void ask(const T *head, const Part &p, int rows, bool whole) {
-    const Bits *at = (const Bits *)head;
-    if (whole) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const unsigned off = (unsigned)(p.row + e) * p.step + p.col;
-#pragma unroll
-        for (int n = 0; n < N; ++n) raw[e][n] = (at + 16 * n)[off];
-      }
-    } else
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const unsigned off = (unsigned)min(p.row + e, rows - 1) * p.step;
-#pragma unroll
-        for (int n = 0; n < N; ++n) raw[e][n] = at[off + min(p.col + 16 * n, p.cols - 1)];
-      }
-  }
-  // zeros behind the sequence's `live` rows and beside the array
-  __device__ __forceinline__ tile get(int n, const Part &p, int live, bool whole) const {
-    tile v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(sizeof(T) == 2 ? (uint32_t)raw[e][n] << 16 : (uint32_t)raw[e][n]);
-    if (!whole)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = p.row + e < live && p.col + 16 * n < p.cols ? v[e] : 0.f;
-    return v;
-  }
-};
-template <class T, int N> __device__ __forceinline__ void values_to(T *head, const Part &p, int rows, int live, bool whole, const tile (&v)[N]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const unsigned off = (unsigned)(p.row + e) * p.step + p.col;
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-      if (whole) (head + 16 * n)[off] = (T)v[n][e];
-      else if (p.row + e < rows && p.col + 16 * n < p.cols) (head + 16 * n)[off] = (T)(p.row + e < live ? v[n][e] : 0.f);
-  }
-}
-// Waits for all loads, where the compiler would else wait for what comes from before a loop in each of its turns, and for all that was asked for since
-__device__ __forceinline__ void loaded() { __builtin_amdgcn_s_waitcnt(0x0f70); }
-// Tiles of a state between registers and memory: rows of the lane's wavefront from `row` on, RT tiles of them, every 16th column from col on
-template <int RT, int NT> __device__ __forceinline__ void state_from(const float *from, int row, int col, int rows, int cols, tile (&s)[RT][NT]) {
-#pragma unroll
-  for (int i = 0; i < RT; ++i)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        s[i][n][e] = element(from + (long long)(row + 16 * i + e) * cols + col + 16 * n, row + 16 * i + e < rows && col + 16 * n < cols);
-}
-template <int RT, int NT> __device__ __forceinline__ void state_to(float *to, int row, int col, int rows, int cols, bool whole, const tile (&s)[RT][NT]) {
-  const unsigned off = (unsigned)row * cols + col;
-#pragma unroll
-  for (int i = 0; i < RT; ++i)
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        if (whole || (row + 16 * i + e < rows && col + 16 * n < cols)) (to + (16 * i + e) * cols + 16 * n)[off] = s[i][n][e];
-}
-
 // Elements as they are in memory, asked for ahead of their use
 template <class T> struct Octet { // 8 of a row
   words4 raw[sizeof(T) / 2];
@@ -298,6 +227,87 @@ template <class T> struct Quad { // 4 of a row
         if (j < count) p[j] = (T)v[j];
   }
 };
+
+// A wavefront's 16 rows of a tile of BV columns between memory, 16 bytes a lane, and registers, four rows and every 16th column a lane, by way of LDS of its
+// own.  (Asked for element by element they are half of all requests to memory, and what the walks wait for.)  Rows are as far apart in LDS as the
+// lanes' four rows need to be in banks of their own.
+struct Place { int rows, live, cols; }; // from the tile's first row and column on: rows in the array, those before the sequence's end, columns
+template <class T, int BV> struct Strip {
+  static constexpr int STRIDE = BV * sizeof(T) + 16, BYTES = 16 * STRIDE, N = BV / 32, OF_ROW = BV / 8;
+  static __device__ __forceinline__ void turn() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+  }
+  Octet<T> raw[N];
+  // row0: the wavefront's first row of the tile
+  __device__ __forceinline__ void ask(const T *head, unsigned step, int row0, int lane, const Place &p) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = 64 * i + lane, row = min(row0 + at / OF_ROW, p.rows - 1), col = at % OF_ROW * 8;
+      raw[i].ask(head + ((unsigned)row * step + col), p.cols - col);
+    }
+  }
+  template <int NT> __device__ __forceinline__ void get(char *lds, int row0, int lane, const Place &p, bool whole, tile (&v)[NT]) const {
+    turn(); // (what was here before has been read)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = 64 * i + lane;
+      __builtin_memcpy(lds + at / OF_ROW * STRIDE + at % OF_ROW * (8 * sizeof(T)), raw[i].raw, sizeof raw[i].raw);
+    }
+    turn();
+    const int r = lane & 15, q4 = lane >> 4;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = (float)*(const T *)(lds + (4 * q4 + e) * STRIDE + (16 * n + r) * sizeof(T));
+        v[n][e] = whole || (row0 + 4 * q4 + e < p.live && 16 * n + r < p.cols) ? x : 0.f;
+      }
+  }
+  template <int NT> static __device__ __forceinline__ void put(char *lds, T *head, unsigned step, int row0, int lane, const Place &p, bool whole, const tile (&v)[NT]) {
+    const int r = lane & 15, q4 = lane >> 4;
+    turn();
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *(T *)(lds + (4 * q4 + e) * STRIDE + (16 * n + r) * sizeof(T)) = (T)(whole || row0 + 4 * q4 + e < p.live ? v[n][e] : 0.f);
+    turn();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = 64 * i + lane, row = row0 + at / OF_ROW, col = at % OF_ROW * 8;
+      const char *from = lds + at / OF_ROW * STRIDE + at % OF_ROW * (8 * sizeof(T));
+      T *to = head + ((unsigned)row * step + col);
+      if (whole || (row < p.rows && col + 8 <= p.cols)) {
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) *(words4_any *)((char *)to + 16 * k) = *(const words4 *)(from + 16 * k);
+      } else if (row < p.rows)
+        for (int j = 0; j < p.cols - col; ++j) to[j] = ((const T *)from)[j];
+    }
+  }
+};
+// Waits for all loads, where the compiler would else wait for what comes from before a loop in each of its turns, and for all that was asked for since
+__device__ __forceinline__ void loaded() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+// Tiles of a state between registers and memory: rows of the lane's wavefront from `row` on, RT tiles of them, every 16th column from col on
+template <int RT, int NT> __device__ __forceinline__ void state_from(const float *from, int row, int col, int rows, int cols, tile (&s)[RT][NT]) {
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        s[i][n][e] = element(from + (long long)(row + 16 * i + e) * cols + col + 16 * n, row + 16 * i + e < rows && col + 16 * n < cols);
+}
+template <int RT, int NT> __device__ __forceinline__ void state_to(float *to, int row, int col, int rows, int cols, bool whole, const tile (&s)[RT][NT]) {
+  const unsigned off = (unsigned)row * cols + col;
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        if (whole || (row + 16 * i + e < rows && col + 16 * n < cols)) (to + (16 * i + e) * cols + 16 * n)[off] = s[i][n][e];
+}
 
 // ---- a chunk by itself ------------------------------------------------------------------------
 // ONE: each head has queries and keys of its own.
@@ -531,6 +541,7 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
   constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
   __shared__ __align__(16) Planes<PC, BV, DK> st;
   __shared__ __align__(16) Planes<PC, BV, C> et, wt;
+  __shared__ __align__(16) char strips[4][REC && Strip<float, BV>::BYTES > Strip<T, BV>::BYTES ? Strip<float, BV>::BYTES : Strip<T, BV>::BYTES];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
   const int per = a.batch * a.heads;
   const Unit u = unit_of(blockIdx.x % (per * a.blocks), per, a.blocks);
@@ -547,7 +558,8 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
   // What the next chunk needs is on its way while this one is worked on: each part is asked for as soon as this chunk's has been used.
   Operand<PI> k[KK], q[REC ? 1 : KK], kt[RT][2];
   Operand<PC> am[2], bm[2];
-  Values<T, NT> v;
+  Strip<T, BV> v;
+  char *const strip = strips[w];
   tile gam, left; // left: gam_end / gam beta
   float end;
   auto of_keys = [&](int c) { return (((long long)c * a.batch + b) * a.key_heads + kh) * (DK * C * PI); };
@@ -559,10 +571,10 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
       if constexpr (!REC) q[i] = fetch<PI>(a.qf + of_keys(c), w * KK + i, lane);
     }
   };
-  const Part of_v = {(unsigned)(a.batch * a.ld_v), row0, col, a.dv}, of_o = {(unsigned)(a.batch * a.ld_o), row0, col, a.dv};
+  const unsigned step_v = (unsigned)(a.batch * a.ld_v), step_o = (unsigned)(a.batch * a.ld_o);
   auto ask_values = [&](int c) {
     const int t0 = (a.first + c) * C;
-    v.ask((const T *)a.v + ((long long)t0 * a.batch + b) * a.ld_v + h * a.dv, of_v, a.T - t0, cols && t0 + C <= a.T);
+    v.ask((const T *)a.v + ((long long)t0 * a.batch + b) * a.ld_v + h * a.dv + v0, step_v, 16 * w, lane, Place{a.T - t0, len - t0, a.dv - v0});
   };
   auto ask_squares = [&](const __bf16 *p, int c, Operand<PC> (&m)[2]) { // (lower triangular: the first two rows of blocks have zeros behind)
     m[0] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w, lane);
@@ -594,7 +606,10 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
     if constexpr (!REC) {
       if (a.kept && (a.first + c) % KEPT == 0)
         state_to(a.kept + ((long long)((a.first + c) / KEPT) * per + u.of) * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
-    } else state_to(a.before + of_head(c) * DK * a.dvp, srow, col, DK, a.dvp, true, s); // (dvp is a multiple of the 32 columns of a workgroup)
+    } else
+#pragma unroll
+      for (int i = 0; i < RT; ++i) // (dvp is a multiple of the 32 columns of a workgroup)
+        Strip<float, BV>::put(strip, a.before + of_head(c) * DK * a.dvp + v0, a.dvp, 16 * (w * RT + i), lane, Place{}, true, s[i]);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -609,11 +624,13 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
       if constexpr (!REC) multiply(o, q[i], y);
     }
     ask_rows(next);
+    const Place place = {a.T - t0, len - t0, a.dv - v0};
+    tile vn[NT];
+    v.get(strip, 16 * w, lane, place, whole, vn);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const tile vn = v.get(n, of_v, len - t0, whole);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e[n][i] = fmaf(-gam[i], e[n][i], vn[i]);
+      for (int i = 0; i < 4; ++i) e[n][i] = fmaf(-gam[i], e[n][i], vn[n][i]);
       et.put(16 * n + r, row0, e[n]);
     }
     ask_values(next);
@@ -632,10 +649,10 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
       }
     ask_squares(a.af, next, am);
     if constexpr (!REC) ask_squares(a.bf, next, bm);
-    if constexpr (REC) state_to(a.w + of_head(c) * C * a.dvp, row0, col, C, a.dvp, true, (const tile (&)[1][NT])x);
+    if constexpr (REC) Strip<float, BV>::put(strip, a.w + of_head(c) * C * a.dvp + v0, a.dvp, 16 * w, lane, Place{}, true, x);
 #pragma unroll
     for (int n = 0; n < NT; ++n) wt.put(16 * n + r, row0, REC ? x[n] * left : x[n]);
-    if constexpr (!REC) values_to<T, NT>((T *)a.o + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv, of_o, a.T - t0, len - t0, whole, o);
+    if constexpr (!REC) v.put(strip, (T *)a.o + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv + v0, step_o, 16 * w, lane, place, whole, o);
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -661,6 +678,7 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
   __shared__ __align__(16) Planes<PC, BV, DK> st;
   __shared__ __align__(16) Planes<PI, BV, C> ot;
   __shared__ __align__(16) Planes<PC, BV, C> got, ut, et; // scale gam dO, K dS', -gam dE
+  __shared__ __align__(16) char strips[4][Strip<float, BV>::BYTES];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
   const int per = a.batch * a.heads;
   const Unit u = unit_of(blockIdx.x, per, a.blocks);
@@ -675,7 +693,8 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
   // (as in k_walk)
   Operand<PI> k[KK], kt[RT][2], qt[RT][2];
   Operand<PC> am[2], bm[2];
-  Values<T, NT> raw; // of dO
+  Strip<T, BV> raw; // of dO
+  char *const strip = strips[w];
   tile gam;
   float end;
   auto of_keys = [&](int c) { return (((long long)c * a.batch + b) * a.key_heads + kh) * (DK * C * PI); };
@@ -684,10 +703,10 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
 #pragma unroll
     for (int i = 0; i < KK; ++i) k[i] = fetch<PI>(a.kf + of_keys(c), w * KK + i, lane);
   };
-  const Part of_o = {(unsigned)(a.batch * a.ld_o), row0, col, a.dv}, of_v = {(unsigned)(a.batch * a.ld_dv), row0, col, a.dv};
+  const unsigned step_o = (unsigned)(a.batch * a.ld_o), step_v = (unsigned)(a.batch * a.ld_dv);
   auto ask_values = [&](int c) {
     const int t0 = (a.first + c) * C;
-    raw.ask((const T *)a.dout + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv, of_o, a.T - t0, cols && t0 + C <= a.T);
+    raw.ask((const T *)a.dout + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv + v0, step_o, 16 * w, lane, Place{a.T - t0, len - t0, a.dv - v0});
   };
   auto ask_squares = [&](const __bf16 *p, int c, Operand<PC> (&m)[2]) { // (upper triangular: the last two rows of blocks begin with zeros)
     if (w < 2) m[0] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w, lane);
@@ -720,17 +739,17 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
     const int t0 = (a.first + c) * C, next = max(c - 1, 0);
     const long long of = of_head(c);
     const bool whole = cols && t0 + C <= len;
-    state_to(a.after + of * DK * a.dvp, srow, col, DK, a.dvp, true, s);
+    const Place place = {a.T - t0, len - t0, a.dv - v0};
+#pragma unroll
+    for (int i = 0; i < RT; ++i) Strip<float, BV>::put(strip, a.after + of * DK * a.dvp + v0, a.dvp, 16 * (w * RT + i), lane, place, true, s[i]);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
       for (int n = 0; n < NT; ++n) st.put(16 * n + r, srow + 16 * i, s[i][n]);
     tile given[NT];
+    raw.get(strip, 16 * w, lane, place, whole, given);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      given[n] = raw.get(n, of_o, len - t0, whole);
-      ot.put(16 * n + r, row0, given[n]);
-    }
+    for (int n = 0; n < NT; ++n) ot.put(16 * n + r, row0, given[n]);
     lds_barrier(); // (and every wavefront is through with the last chunk)
 #pragma unroll
     for (int n = 0; n < NT; ++n) got.put(16 * n + r, row0, given[n] * (gam * a.scale));
@@ -770,8 +789,8 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
         for (int e = 0; e < 4; ++e) x[n][e] = t0 + row0 + e < len ? x[n][e] : 0.f;
       et.put(16 * n + r, row0, x[n] * -gam);
     }
-    state_to(a.de + of * C * a.dvp, row0, col, C, a.dvp, true, (const tile (&)[1][NT])x);
-    values_to<T, NT>((T *)a.dv_ + ((long long)t0 * a.batch + b) * a.ld_dv + h * a.dv, of_v, a.T - t0, len - t0, whole, x);
+    Strip<float, BV>::put(strip, a.de + of * C * a.dvp + v0, a.dvp, 16 * w, lane, place, true, x);
+    raw.put(strip, (T *)a.dv_ + ((long long)t0 * a.batch + b) * a.ld_dv + h * a.dv + v0, step_v, 16 * w, lane, place, whole, x);
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < RT; ++i)
