@@ -1171,7 +1171,7 @@ template <class T, int DK, int LV> __global__ __launch_bounds__(256) void k_step
 
 // ---- launches -------------------------------------------------------------------------------------
 constexpr int STEPS_MOST = 16;            // steps that are taken one after the other
-constexpr size_t PIECE = (size_t)256 << 20; // bytes of a piece's intermediate arrays, at least 4 chunks
+constexpr size_t PIECE = (size_t)2 << 30; // bytes of a piece's intermediate arrays, at least 4 chunks
 
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
@@ -1217,6 +1217,8 @@ struct Plan {
     const size_t one = lay(KEPT) - lay(0);
     const long long most = (long long)(PIECE / one) * KEPT;
     chunks = (int)(most < KEPT ? KEPT : most > all ? all : most);
+    if (chunks < all) chunks = (all + (all + chunks - 1) / chunks - 1) / ((all + chunks - 1) / chunks); // as many pieces as it takes, of one length
+    chunks = (chunks + KEPT - 1) / KEPT * KEPT;
     if (chunks > all) chunks = all;
     bytes = lay(chunks);
     a.lengths = p.lengths;
