@@ -394,8 +394,8 @@ typedef struct {
                                 later steps hold does not matter; o and all gradients are zeros there */
 } snn_delta;
 
-/* Bytes of workspace for snn_delta_forward (gradients = 0; none for up to 16 steps) or snn_delta_backward; 0 for an invalid shape too.  Half a GB or what
- * four chunks of 64 steps need, whichever is more, however long the sequences are. */
+/* Bytes of workspace for snn_delta_forward (gradients = 0; none for a few steps) or snn_delta_backward; 0 for an invalid shape too.  About 2 GB or what four
+ * chunks of 64 steps need, whichever is more, however long the sequences are. */
 size_t snn_delta_workspace(const snn_delta *p, int32_t gradients);
 
 /* q, k [T][batch][key_heads][dk], v, o [T][batch][heads][dv], g, beta [T][batch][heads] fp32; s0 [batch][heads][dk][dv] fp32 or NULL (zeros); s_last of the same

@@ -233,7 +233,8 @@ template <class T> struct Quad { // 4 of a row
 // lanes' four rows need to be in banks of their own.
 struct Place { int rows, live, cols; }; // from the tile's first row and column on: rows in the array, those before the sequence's end, columns
 template <class T, int BV> struct Strip {
-  static constexpr int STRIDE = BV * sizeof(T) + 16, BYTES = 16 * STRIDE, N = BV / 32, OF_ROW = BV / 8;
+  static constexpr int STRIDE = BV * sizeof(T) + 16, BYTES = 16 * STRIDE, OF_ROW = BV / 8, N = (16 * OF_ROW + 63) / 64;
+  static __device__ __forceinline__ bool mine(int at) { return 16 * OF_ROW >= 64 || at < 16 * OF_ROW; } // (16 columns are 32 lanes')
   static __device__ __forceinline__ void turn() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
@@ -245,7 +246,7 @@ template <class T, int BV> struct Strip {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int at = 64 * i + lane, row = min(row0 + at / OF_ROW, p.rows - 1), col = at % OF_ROW * 8;
-      raw[i].ask(head + ((unsigned)row * step + col), p.cols - col);
+      if (mine(at)) raw[i].ask(head + ((unsigned)row * step + col), p.cols - col);
     }
   }
   template <int NT> __device__ __forceinline__ void get(char *lds, int row0, int lane, const Place &p, bool whole, tile (&v)[NT]) const {
@@ -253,7 +254,7 @@ template <class T, int BV> struct Strip {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int at = 64 * i + lane;
-      __builtin_memcpy(lds + at / OF_ROW * STRIDE + at % OF_ROW * (8 * sizeof(T)), raw[i].raw, sizeof raw[i].raw);
+      if (mine(at)) __builtin_memcpy(lds + at / OF_ROW * STRIDE + at % OF_ROW * (8 * sizeof(T)), raw[i].raw, sizeof raw[i].raw);
     }
     turn();
     const int r = lane & 15, q4 = lane >> 4;
@@ -276,6 +277,7 @@ template <class T, int BV> struct Strip {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int at = 64 * i + lane, row = row0 + at / OF_ROW, col = at % OF_ROW * 8;
+      if (!mine(at)) continue;
       const char *from = lds + at / OF_ROW * STRIDE + at % OF_ROW * (8 * sizeof(T));
       T *to = head + ((unsigned)row * step + col);
       if (whole || (row < p.rows && col + 8 <= p.cols)) {
@@ -1093,38 +1095,46 @@ template <class T, int DK, int LV> __global__ __launch_bounds__(256) void k_step
     }
   };
   if (a.kept && a.T) state_to(a.kept);
-  for (int t = 0; t < a.T; ++t) {
+  // a step's inputs, asked for while the one before is worked on
+  T q = (T)0.f, k = (T)0.f;
+  T v[4];
+  float g = 0.f, beta = 0.f;
+  auto ask = [&](int t) {
     const long long row = (long long)t * a.batch + b;
-    T *op = (T *)a.o + row * a.ld_o + h * a.dv + col;
-    if (t >= len) {
-      if (first == 0)
+    if ((int)threadIdx.x < a.dk) {
+      q = ((const T *)a.q)[row * a.ld_q + kh * a.dk + threadIdx.x];
+      k = ((const T *)a.k)[row * a.ld_k + kh * a.dk + threadIdx.x];
+    }
+    Quad<T> f;
+    f.ask((const T *)a.v + row * a.ld_v + h * a.dv + col, cols);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < cols) op[e] = (T)0.f;
+    for (int e = 0; e < 4; ++e) v[e] = f.x[e];
+    g = a.g[row * a.heads + h];
+    beta = a.beta[row * a.heads + h];
+  };
+  if (len) ask(0);
+  for (int t = 0; t < a.T; ++t) {
+    T *op = (T *)a.o + ((long long)t * a.batch + b) * a.ld_o + h * a.dv + col;
+    if (t >= len) {
+      if (first == 0) Quad<T>::put(op, cols, tile{});
       continue;
     }
     const int turn = t & 1; // (LDS of one step is read while that of the next is written)
     if ((int)threadIdx.x < DK) {
-      const bool on = (int)threadIdx.x < a.dk;
-      const float q = element((const T *)a.q + row * a.ld_q + kh * a.dk + threadIdx.x, on), k = element((const T *)a.k + row * a.ld_k + kh * a.dk + threadIdx.x, on);
-      qs[turn][threadIdx.x] = q;
-      ks[turn][threadIdx.x] = k;
-      float d = q * k;
-#pragma unroll
-      for (int x = 1; x < 64; x *= 2) d += __shfl_xor(d, x);
-      if (lane == 0) dots[turn][wave] = d;
+      qs[turn][threadIdx.x] = (float)q;
+      ks[turn][threadIdx.x] = (float)k;
     }
-    tile v = {};
-    const T *vp = (const T *)a.v + row * a.ld_v + h * a.dv + col;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = element(vp + e, e < cols);
-    const float hold = __builtin_amdgcn_exp2f(a.g[row * a.heads + h] * LOG2E), beta = a.beta[row * a.heads + h];
-    __syncthreads();
+    const tile vn = {(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+    const float hold = __builtin_amdgcn_exp2f(g * LOG2E), rate = beta;
+    if (t + 1 < len) ask(t + 1);
+    lds_barrier();
     tile of_k = {}, of_q = {};
+    float qk = 0.f;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
       const float k = ks[turn][first + GROUPS * i], q = qs[turn][first + GROUPS * i];
       s[i] *= hold;
+      qk = fmaf(q, k, qk);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         of_k[e] = fmaf(s[i][e], k, of_k[e]);
@@ -1132,48 +1142,61 @@ template <class T, int DK, int LV> __global__ __launch_bounds__(256) void k_step
       }
     }
 #pragma unroll
-    for (int x = LV; x < 64; x *= 2)
+    for (int x = LV; x < 64; x *= 2) {
+      qk += __shfl_xor(qk, x);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         of_k[e] += __shfl_xor(of_k[e], x);
         of_q[e] += __shfl_xor(of_q[e], x);
       }
+    }
+    if (lane == 0) dots[turn][wave] = qk;
     if (lane < LV) {
       *(tile *)(sums[turn][wave][0] + 4 * at) = of_k;
       *(tile *)(sums[turn][wave][1] + 4 * at) = of_q;
     }
-    __syncthreads();
+    lds_barrier();
     of_k = of_q = tile{};
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       of_k += *(const tile *)(sums[turn][x][0] + 4 * at);
       of_q += *(const tile *)(sums[turn][x][1] + 4 * at);
     }
-    float qk = 0.f;
-#pragma unroll
-    for (int x = 0; x < DK / 64; ++x) qk += dots[turn][x];
-    const tile un = (v - of_k) * beta;
+    qk = (dots[turn][0] + dots[turn][1]) + (dots[turn][2] + dots[turn][3]);
+    const tile un = (vn - of_k) * rate;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
       const float k = ks[turn][first + GROUPS * i];
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[i][e] = fmaf(k, un[e], s[i][e]);
     }
-    if (first == 0) {
-      const tile o = (of_q + un * qk) * a.scale;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < cols) op[e] = (T)o[e];
-    }
+    if (first == 0) Quad<T>::put(op, cols, (of_q + un * qk) * a.scale);
   }
   if (a.to) state_to(a.to);
 }
 
 // ---- launches -------------------------------------------------------------------------------------
-constexpr int STEPS_MOST = 16;            // steps that are taken one after the other
 constexpr size_t PIECE = (size_t)2 << 30; // bytes of a piece's intermediate arrays, at least 4 chunks
 
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Columns of the state that a workgroup walks with: fewer where there would be few workgroups, as a chunk then takes a shorter time.  4096 steps, 128 x 128, in us:
+// forward with 16 and 32 columns, 4 heads 207 and 269 in fp32, 112 and 152 in bf16; 32 heads 379 and 418, 160 and 188; 64 heads 725 and 517, 308 and
+// 241; backward 4 heads 327 and 389, 182 and 214; 16 heads 613 and 649, 329 and 335; 32 heads 933 and 926, 584 and 540.  In bf16 with 32 and 64 forward, 128
+// heads 440 and 412.
+int columns(const DeltaShape &p, bool back) {
+  const long long heads = (long long)p.batch * p.heads;
+  if (p.bf16 && !back && p.dv > 32 && heads * ((p.dv + 63) / 64) >= 256) return 64;
+  return heads * ((p.dv + 31) / 32) > (back ? 64 : 128) ? 32 : 16;
+}
+
+// Whether steps are taken one after the other.  dk and dv 128, in us, so and in chunks: 16 heads, 8 steps 19.6 and 22.5 in fp32, 19.9 and 20.7 in bf16, 12 steps
+// 25.2 and 22.5, 25.6 and 20.7; 128 heads, fp32 16 steps 34.6 and 35.2, 32 steps 59.7 and 35.4, bf16 8 steps 23.3 and 23.9, 12 steps 29.5 and
+// 24.1; 1024 heads, fp32 32 steps 150 and 229, bf16 12 steps 80.7 and 93.0, 16 steps 94.7 and 89.4.
+bool one_by_one(const DeltaShape &p) {
+  const long long heads = (long long)p.batch * p.heads;
+  return p.T <= (heads < 128 ? 8 : heads < 512 ? p.bf16 ? 8 : 16 : p.bf16 ? 12 : 32);
+}
 
 struct Plan {
   int dk, bv, blocks, dvp, all, chunks, per, units; // units: of key heads
@@ -1183,9 +1206,9 @@ struct Plan {
   Plan(const DeltaShape &p, bool back, char *work) {
     dk = p.dk <= 64 ? 64 : 128;
     per = p.batch * p.heads, units = p.batch * p.key_heads;
-    bv = p.bf16 && p.dv > 32 && !back ? 64 : 32;
-    blocks = (p.dv + bv - 1) / bv;
     dvp = (p.dv + 31) / 32 * 32;
+    bv = columns(p, back);
+    blocks = (dvp + bv - 1) / bv;
     all = (p.T + C - 1) / C;
     const size_t pi = p.bf16 ? 1 : 3, pc = p.bf16 ? 2 : 3;
     auto lay = [&](int n) {
@@ -1241,7 +1264,8 @@ template <class T, int DK> hipError_t forward(Plan &p, hipStream_t s) {
     else k_chunk<T, DK, false, false><<<a.chunks * p.units, 256, 0, s>>>(a);
     if (p.bv == 64) {
       if constexpr (sizeof(T) == 2) k_walk<T, DK, 64, false><<<p.per * p.blocks, 256, 0, s>>>(a);
-    } else k_walk<T, DK, 32, false><<<p.per * p.blocks, 256, 0, s>>>(a);
+    } else if (p.bv == 32) k_walk<T, DK, 32, false><<<p.per * p.blocks, 256, 0, s>>>(a);
+    else k_walk<T, DK, 16, false><<<p.per * p.blocks, 256, 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     from = carry;
   }
@@ -1254,7 +1278,8 @@ template <class T, int DK> hipError_t backward(Plan &p, const float *kept, const
   if (!p.all) {
     a.from = ds_last;
     a.to = p.last;
-    k_walk_back<T, DK, 32><<<p.per * p.blocks, 256, 0, s>>>(a);
+    if (p.bv == 32) k_walk_back<T, DK, 32><<<p.per * p.blocks, 256, 0, s>>>(a);
+    else k_walk_back<T, DK, 16><<<p.per * p.blocks, 256, 0, s>>>(a);
     return hipGetLastError();
   }
   // pieces of whole kept intervals, from the last one on
@@ -1265,10 +1290,13 @@ template <class T, int DK> hipError_t backward(Plan &p, const float *kept, const
     else k_chunk<T, DK, true, false><<<a.chunks * p.units, 256, 0, s>>>(a);
     a.from = kept;
     a.to = nullptr;
-    k_walk<T, DK, 32, true><<<(a.chunks + KEPT - 1) / KEPT * p.per * p.blocks, 256, 0, s>>>(a);
+    const unsigned walks = p.per * p.blocks, segments = (a.chunks + KEPT - 1) / KEPT;
+    if (p.bv == 32) k_walk<T, DK, 32, true><<<segments * walks, 256, 0, s>>>(a);
+    else k_walk<T, DK, 16, true><<<segments * walks, 256, 0, s>>>(a);
     a.from = from;
     a.to = first ? carry : p.last;
-    k_walk_back<T, DK, 32><<<p.per * p.blocks, 256, 0, s>>>(a);
+    if (p.bv == 32) k_walk_back<T, DK, 32><<<walks, 256, 0, s>>>(a);
+    else k_walk_back<T, DK, 16><<<walks, 256, 0, s>>>(a);
     if (a.heads == a.key_heads) k_grads<T, DK, true><<<a.chunks * p.units, 512, 0, s>>>(a);
     else k_grads<T, DK, false><<<a.chunks * p.units, 512, 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -1295,7 +1323,7 @@ template <class T> hipError_t steps(Plan &p, hipStream_t s) {
 } // namespace
 
 size_t delta_workspace(const DeltaShape &p, bool back) {
-  if (!p.T || (!back && p.T <= STEPS_MOST)) return 0;
+  if (!p.T || (!back && one_by_one(p))) return 0;
   return Plan(p, back, nullptr).bytes;
 }
 
@@ -1305,7 +1333,7 @@ hipError_t launch_delta_forward(const DeltaShape &p, const void *q, const void *
   Args &a = plan.a;
   a.q = q, a.k = k, a.v = v, a.g = g, a.beta = beta, a.from = s0, a.o = o, a.kept = kept;
   plan.last = s_last;
-  if (p.T <= STEPS_MOST) return p.bf16 ? steps<__bf16>(plan, s) : steps<float>(plan, s);
+  if (one_by_one(p)) return p.bf16 ? steps<__bf16>(plan, s) : steps<float>(plan, s);
   if (plan.dk == 64) return p.bf16 ? forward<__bf16, 64>(plan, s) : forward<float, 64>(plan, s);
   return p.bf16 ? forward<__bf16, 128>(plan, s) : forward<float, 128>(plan, s);
 }

@@ -469,7 +469,7 @@ def close(got, want, tol, what):
 DELTA = [(0, 2, 3, 3, 5, 7, False), (1, 2, 3, 3, 5, 7, False), (1, 64, 4, 2, 128, 128, False), (3, 2, 2, 1, 65, 130, True), (16, 2, 4, 4, 128, 64, True),
          (17, 1, 2, 2, 16, 16, False), (63, 2, 1, 1, 1, 1, False), (64, 2, 2, 2, 64, 64, False), (65, 3, 3, 1, 48, 75, True), (130, 3, 2, 2, 33, 31, True),
          (256, 1, 2, 2, 128, 128, False), (257, 3, 2, 1, 64, 100, True), (300, 5, 4, 2, 128, 40, True), (700, 1, 1, 1, 100, 256, False),
-         (200, 4, 6, 2, 72, 33, True), (128, 8, 8, 8, 32, 96, False)]
+         (200, 4, 6, 2, 72, 33, True), (128, 8, 8, 8, 32, 96, False), (8, 2, 3, 1, 100, 70, True), (12, 64, 4, 2, 24, 40, True), (32, 64, 4, 4, 70, 20, False)]
 
 
 @gpu
