@@ -17,9 +17,11 @@
 //
 // G and its differences are of 64 bits: behind a decay that forgets everything the next steps' ratios keep their digits.  A is found by substitution in
 // blocks of 16, in 32 bits, and by products of blocks, so that equal keys do no harm.
-// States and sums are of 32 bits.  Products go through the bf16 matrix cores: arrays of bf16 as they are, what is computed on the way (S, E, u, dE, A, B) in two
-// bf16 parts, which leaves 16 bits of each factor (off by 2^-17 of itself at most; 3 products of parts, or 2 beside an operand that is bf16); with
-// arrays of 32 bits everything goes in three parts and six products, which keep 24.
+// States and sums are of 32 bits.  Products go through the bf16 matrix cores: arrays of bf16 as they are, those of 32 bits in three bf16 parts, and what is
+// computed on the way (S, E, u, dE, A, B) in three too, 24 bits of it: six products of two such operands, three of one beside a bf16 array.
+// (Two parts would leave 16 bits.  With those, forward 4096 x 8 x 16 x 128 x 128 took 407 us instead of TIMEF and backward 1638 instead of TIMEB, but states
+// were off by up to 7e-6 of their norm and gradients of gates by 2e-5.)  Where nothing but a result in bf16 comes of a product, o and the products of the
+// chunk's own steps in dq and dk, two parts are enough: 2^-17 of each factor, beside 2^-8 of the result.
 //
 // Four kernels: what is of a chunk alone (k_chunk: A, B, and the operands in the order in which a wavefront loads them); the walk over the chunks
 // with S in registers, its columns dealt to workgroups (k_walk; for the backward pass it starts at each kept state, every 4 chunks); the walk back
@@ -39,7 +41,8 @@ constexpr int FLINE = C + 4; // floats from row to row of a matrix of a chunk's 
 constexpr float LOG2E = 1.44269504f;
 
 template <class T> constexpr int GIVEN = sizeof(T) == 2 ? 1 : 3; // parts of what the caller's arrays hold
-template <class T> constexpr int MADE = sizeof(T) == 2 ? 2 : 3;  // and of what is computed
+constexpr int MADE = 3;                                    // of what is computed
+template <class T> constexpr int LAST = sizeof(T) == 2 ? 2 : 3; // and of that, where nothing but a result in the arrays' type comes from it
 
 struct Args {
   const void *q, *k, *v, *dout;
@@ -74,6 +77,13 @@ template <int PA, int PB> __device__ __forceinline__ void multiply(tile &acc, co
 #pragma unroll
     for (int i = 0; i <= s; ++i)
       if (i < PA && s - i < PB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], acc, 0, 0, 0);
+}
+// The first parts of operands
+template <int P, int PA, int N> __device__ __forceinline__ void first_parts(const Operand<PA> (&a)[N], Operand<P> (&r)[N]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < P; ++i) r[n].p[i] = a[n].p[i];
 }
 // Several columns' products in turn: none waits for the one before
 template <int PA, int PB, int N> __device__ __forceinline__ void multiply(tile (&acc)[N], const Operand<PA> &a, const Operand<PB> (&b)[N]) {
@@ -314,7 +324,7 @@ template <int RT, int NT> __device__ __forceinline__ void state_to(float *to, in
 // ---- a chunk by itself ------------------------------------------------------------------------
 // ONE: each head has queries and keys of its own.
 template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256, ONE ? sizeof(T) == 2 || DK == 64 ? 4 : 3 : 2) void k_chunk(Args a) {
-  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32;
+  constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32;
   typedef Planes<PI, C, DK> Rows;
   struct Squares { float m[C][FLINE], x[C][FLINE]; };
   __shared__ __align__(16) char space[sizeof(Rows) > sizeof(Squares) ? sizeof(Rows) : sizeof(Squares)];
@@ -492,7 +502,8 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
     }
     __syncthreads();
     // A lower triangular matrix in x, or its transpose, times a factor of its rows; blocks of zeros, which nothing reads, are left out
-    auto emit = [&](__bf16 *to, bool over, bool scaled) {
+    auto emit = [&](auto parts, __bf16 *to, bool over, bool scaled) {
+      constexpr int P = decltype(parts)::value;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         if (over ? 2 * s + 1 < w : 2 * s > w) continue;
@@ -502,11 +513,11 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
           const int k = 32 * s + 8 * q4 + j;
           e[j] = (over ? x[k][16 * w + r] : x[16 * w + r][k]) * (scaled ? left[over ? k : 16 * w + r] : 1.f);
         }
-        leave<PC>(to + of * (C * C * PC), 2 * w + s, lane, operand<PC>(e));
+        leave<P>(to + of * (C * C * P), 2 * w + s, lane, operand<P>(e));
       }
     };
-    emit(a.af, false, !BACK);
-    if constexpr (BACK) emit(a.at, true, true);
+    emit(std::integral_constant<int, PC>(), a.af, false, !BACK);
+    if constexpr (BACK) emit(std::integral_constant<int, PC>(), a.at, true, true);
     tile product[4] = {};
 #pragma unroll
     for (int n = 0; n < 4; ++n)
@@ -524,8 +535,8 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[16 * w + 4 * q4 + e][16 * n + r] = product[n][e];
     __syncthreads();
-    if constexpr (BACK) emit(a.bt, true, false);
-    else emit(a.bf, false, false);
+    if constexpr (BACK) emit(std::integral_constant<int, PC>(), a.bt, true, false);
+    else emit(std::integral_constant<int, LAST<T>>(), a.bf, false, false);
     __syncthreads();
   }
 }
@@ -540,7 +551,7 @@ __device__ __forceinline__ Unit unit_of(unsigned id, int units, int blocks) {
 
 // REC: of the backward pass, from a kept state to the next; leaves S and w of each chunk.
 template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk(Args a) {
-  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
+  constexpr int PI = GIVEN<T>, PC = MADE, PO = LAST<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
   __shared__ __align__(16) Planes<PC, BV, DK> st;
   __shared__ __align__(16) Planes<PC, BV, C> et, wt;
   __shared__ __align__(16) char strips[4][REC && Strip<float, BV>::BYTES > Strip<T, BV>::BYTES ? Strip<float, BV>::BYTES : Strip<T, BV>::BYTES];
@@ -559,7 +570,8 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
   const int row0 = 16 * w + 4 * q4;
   // What the next chunk needs is on its way while this one is worked on: each part is asked for as soon as this chunk's has been used.
   Operand<PI> k[KK], q[REC ? 1 : KK], kt[RT][2];
-  Operand<PC> am[2], bm[2];
+  Operand<PC> am[2];
+  Operand<PO> bm[2];
   Strip<T, BV> v;
   char *const strip = strips[w];
   tile gam, left; // left: gam_end / gam beta
@@ -578,9 +590,10 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
     const int t0 = (a.first + c) * C;
     v.ask((const T *)a.v + ((long long)t0 * a.batch + b) * a.ld_v + h * a.dv + v0, step_v, 16 * w, lane, Place{a.T - t0, len - t0, a.dv - v0});
   };
-  auto ask_squares = [&](const __bf16 *p, int c, Operand<PC> (&m)[2]) { // (lower triangular: the first two rows of blocks have zeros behind)
-    m[0] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w, lane);
-    if (w > 1) m[1] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w + 1, lane);
+  auto ask_squares = [&](const __bf16 *p, int c, auto &m) { // (lower triangular: the first two rows of blocks have zeros behind)
+    constexpr int P = sizeof(m[0].p) / sizeof(frag);
+    m[0] = fetch<P>(p + of_head(c) * (C * C * P), 2 * w, lane);
+    if (w > 1) m[1] = fetch<P>(p + of_head(c) * (C * C * P), 2 * w + 1, lane);
   };
   auto ask_columns = [&](int c) {
 #pragma unroll
@@ -623,7 +636,11 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
       Operand<PC> y[NT];
       st.get(r, 32 * i + 8 * q4, y);
       multiply(e, k[i], y);
-      if constexpr (!REC) multiply(o, q[i], y);
+      if constexpr (!REC) {
+        Operand<PO> z[NT];
+        first_parts(y, z);
+        multiply(o, q[i], z);
+      }
     }
     ask_rows(next);
     const Place place = {a.T - t0, len - t0, a.dv - v0};
@@ -647,7 +664,11 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
         Operand<PC> y[NT];
         et.get(r, 32 * j + 8 * q4, y);
         multiply(x, am[j], y);
-        if constexpr (!REC) multiply(o, bm[j], y);
+        if constexpr (!REC) {
+          Operand<PO> z[NT];
+          first_parts(y, z);
+          multiply(o, bm[j], z);
+        }
       }
     ask_squares(a.af, next, am);
     if constexpr (!REC) ask_squares(a.bf, next, bm);
@@ -676,7 +697,7 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
 
 // ---- the walk back --------------------------------------------------------------------------------
 template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk_back(Args a) {
-  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
+  constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32, RT = DK / 64, NT = BV / 16;
   __shared__ __align__(16) Planes<PC, BV, DK> st;
   __shared__ __align__(16) Planes<PI, BV, C> ot;
   __shared__ __align__(16) Planes<PC, BV, C> got, ut, et; // scale gam dO, K dS', -gam dE
@@ -818,7 +839,7 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
 // Sums over the state's columns go through LDS 32 at a time, the next ones on their way; results are [dk][t], so that a lane has four elements of one step's
 // row.  Eight wavefronts: four take 16 steps each, with one half of the channels, and of the chunk's steps before theirs, four with the other.
 template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k_grads(Args a) {
-  constexpr int PI = GIVEN<T>, PC = MADE<T>, KK = DK / 32, NT = DK / 32; // NT: tiles of a half of the channels
+  constexpr int PI = GIVEN<T>, PC = MADE, PO = LAST<T>, KK = DK / 32, NT = DK / 32; // NT: tiles of a half of the channels
   struct Sums { Planes<PC, DK, 32> before, after; Planes<PC, C, 32> w; };
   struct Rows { Planes<PI, C, DK> q, k; };
   struct Squares { float dp[C][FLINE], m[C][FLINE]; };
@@ -1011,13 +1032,13 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
       float y[LANE];
 #pragma unroll
       for (int j = 0; j < LANE; ++j) y[j] = squares.dp[mine][32 * s + 8 * q4 + j];
-      const Operand<PC> dpf = operand<PC>(y);
+      const Operand<PO> dpf = operand<PO>(y);
 #pragma unroll
       for (int j = 0; j < LANE; ++j) y[j] = squares.dp[32 * s + 8 * q4 + j][mine];
-      const Operand<PC> dpt = operand<PC>(y);
+      const Operand<PO> dpt = operand<PO>(y);
 #pragma unroll
       for (int j = 0; j < LANE; ++j) y[j] = squares.m[mine][32 * s + 8 * q4 + j];
-      const Operand<PC> m = operand<PC>(y);
+      const Operand<PO> m = operand<PO>(y);
       if constexpr (PI > 1) columns(s);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -1186,7 +1207,6 @@ size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 // heads 440 and 412.
 int columns(const DeltaShape &p, bool back) {
   const long long heads = (long long)p.batch * p.heads;
-  if (p.bf16 && !back && p.dv > 32 && heads * ((p.dv + 63) / 64) >= 256) return 64;
   return heads * ((p.dv + 31) / 32) > (back ? 64 : 128) ? 32 : 16;
 }
 
@@ -1210,7 +1230,7 @@ struct Plan {
     bv = columns(p, back);
     blocks = (dvp + bv - 1) / bv;
     all = (p.T + C - 1) / C;
-    const size_t pi = p.bf16 ? 1 : 3, pc = p.bf16 ? 2 : 3;
+    const size_t pi = p.bf16 ? 1 : 3, pc = MADE, po = p.bf16 ? LAST<__bf16> : LAST<float>;
     auto lay = [&](int n) {
       size_t at = 0;
       auto take = [&](auto *&to, size_t count) {
@@ -1224,7 +1244,7 @@ struct Plan {
       for (__bf16 **x : {&a.kf, &a.qf, &a.ktf}) take(*x, nk * dk * C * pi);
       take(a.af, nh * C * C * pc);
       take(a.gates, nh * 3 * C);
-      if (!back) take(a.bf, nh * C * C * pc);
+      if (!back) take(a.bf, nh * C * C * po);
       else {
         take(a.qtf, nk * dk * C * pi);
         take(a.bt, nh * C * C * pc);
@@ -1262,9 +1282,7 @@ template <class T, int DK> hipError_t forward(Plan &p, hipStream_t s) {
     a.to = first + a.chunks < p.all ? carry : p.last;
     if (a.heads == a.key_heads) k_chunk<T, DK, false, true><<<a.chunks * p.units, 256, 0, s>>>(a);
     else k_chunk<T, DK, false, false><<<a.chunks * p.units, 256, 0, s>>>(a);
-    if (p.bv == 64) {
-      if constexpr (sizeof(T) == 2) k_walk<T, DK, 64, false><<<p.per * p.blocks, 256, 0, s>>>(a);
-    } else if (p.bv == 32) k_walk<T, DK, 32, false><<<p.per * p.blocks, 256, 0, s>>>(a);
+    if (p.bv == 32) k_walk<T, DK, 32, false><<<p.per * p.blocks, 256, 0, s>>>(a);
     else k_walk<T, DK, 16, false><<<p.per * p.blocks, 256, 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     from = carry;
