@@ -446,20 +446,22 @@ def clean(a, lengths):
     return torch.where((torch.arange(a.shape[0])[:, None] < lengths.cpu()[None, :]).view(*a.shape[:2], *[1] * (a.dim() - 2)), a, 0.0)
 
 
-def delta_tol(dtype, T, dk, times):
+def delta_tol(T, dk, times):
     """What results may be off by, to their 2-norm.  Roundings of either sign add up as the root of their number: sums over dk and over 64 steps, twice
-    each, and those of up to 16 chunks that a state remembers; with bf16 also what two parts leave of a factor (2^-17 at most), of up to eight
-    factors in each of the chunks.  Four times that, for what adds up in one direction; `times` as much where such results are factors again."""
-    chunks = min(T / 64 + 1, 16)
-    return times * 4 * (U * math.sqrt(2 * (dk + 64) * chunks) + (0 if dtype == torch.float32 else 2.0 ** -18 * math.sqrt(8 * chunks)))
+    each, and those of up to 16 chunks that a state remembers.  Four times that, for what adds up in one direction; `times` as much where such results
+    are factors again."""
+    return times * 4 * U * math.sqrt(2 * (dk + 64) * min(T / 64 + 1, 16))
 
 
 def close(got, want, tol, what):
-    """To the 2-norm, and each element to 30 times the root mean square besides its own rounding."""
+    """To the 2-norm, and each element to 30 times the root mean square besides its own rounding.  Results in bf16 come of factors in two parts, each off by
+    2^-17 at most, two of them."""
     got_, want = got.double().cpu(), want.double()
     assert got_.shape == want.shape, what
     if not want.numel():
         return
+    if got.dtype == torch.bfloat16:
+        tol += 2.0 ** -16
     off, norm = (got_ - want).norm().item(), want.norm().item()
     assert off <= (tol + HALF[got.dtype]) * norm, (what, off / max(norm, 1e-300), tol)
     rest = ((got_ - want).abs() - HALF[got.dtype] * want.abs()).max().item()
@@ -479,7 +481,7 @@ def test_delta_forward(T, B, H, K, dk, dv, ragged, dtype):
     x, s0, _, _, lengths = delta_inputs(T, B, H, K, dk, dv, dtype, ragged)
     given = lengths if ragged else None
     o, last, kept = snn.snn_delta_forward(*x, s0, lengths=given, keep=True)
-    c, tol = [clean(a, lengths) for a in x], delta_tol(dtype, T, dk, 1)
+    c, tol = [clean(a, lengths) for a in x], delta_tol(T, dk, 1)
     want = delta_plain(*c, s0.cpu().double(), lengths.cpu(), dk ** -0.5)
     for got, ref, what in zip((o, last, kept), want, ("o", "last", "kept")):
         close(got, ref, tol, what)
@@ -500,7 +502,7 @@ def test_delta_backward(T, B, H, K, dk, dv, ragged, dtype):
     f = (o * clean(do, lengths)).sum()
     got = snn.snn_delta_backward(*x, kept.detach().float().cuda(), do, ds, lengths=given)
     want = torch.autograd.grad(f + (last * ds.cpu().double()).sum(), (*c, S), retain_graph=True, allow_unused=True)
-    tol = delta_tol(dtype, T, dk, 3)
+    tol = delta_tol(T, dk, 3)
     for a, b, y, what in zip(got, want, (*c, S), ("dq", "dk", "dv", "dg", "dbeta", "ds0")):
         close(a, torch.zeros_like(y) if b is None else b, tol, what)
     behind = torch.arange(T, device="cuda")[:, None] >= lengths[None, :]
@@ -541,7 +543,7 @@ def test_delta_state_in_place_is_a_sequence_cut_anywhere(dtype):
     whole, last, _ = snn.snn_delta_forward(*x, s0)
     state = s0.clone()
     parts = [snn.snn_delta_forward(*[y[a:b].contiguous() for y in x], state, s_last=state)[0] for a, b in ((0, 1), (1, 2), (2, 20), (20, 100), (100, 300))]
-    tol = 2 * delta_tol(dtype, 300, 72, 1)
+    tol = 2 * delta_tol(300, 72, 1)
     close(torch.cat(parts), whole.cpu(), tol + HALF[dtype], "o")
     close(state, last.cpu(), tol, "state")
 
@@ -590,7 +592,7 @@ def test_delta_equal_keys(T, dtype):
     x[4].fill_(1.0)
     o, last, _ = snn.snn_delta_forward(*x, None, scale=1.0)
     # differences of neighbouring values, each off by a few roundings
-    near(o, x[2].cpu(), (16 * U if dtype == torch.float32 else 2.0 ** -15) * 2 * x[2].cpu().double().abs().max(), "o")
+    near(o, x[2].cpu(), (16 * U if dtype == torch.float32 else 16 * U + 2.0 ** -16) * 2 * x[2].cpu().double().abs().max(), "o")
 
 
 @gpu
@@ -606,7 +608,7 @@ def test_delta_gates_at_their_ends(dtype):
     beta[::3], beta[1::5] = 0.0, 1.0
     o, last, kept = snn.snn_delta_forward(*x, s0, keep=True)
     c = [clean(a, lengths) for a in x]
-    tol = delta_tol(dtype, T, 40, 1)
+    tol = delta_tol(T, 40, 1)
     want = delta_plain(*c, s0.cpu().double(), lengths.cpu(), 40 ** -0.5)
     close(o, want[0], tol, "o")
     close(last, want[1], tol, "last")
@@ -692,7 +694,7 @@ def test_delta_beyond_4_gb():
     first = [y[T - 516:T - 16] for y in x]
     state = snn.snn_delta_forward(*first)[1]
     end, state, _ = snn.snn_delta_forward(*[y[T - 16:] for y in x], state)
-    tol = 2 * delta_tol(torch.bfloat16, 500, 32, 1)
+    tol = 2 * delta_tol(500, 32, 1)
     close(o[T - 16:], end.cpu(), tol + HALF[torch.bfloat16], "o")
     close(last, state.cpu(), tol, "last")
 
@@ -793,7 +795,7 @@ def test_a_model_of_norms_delta_rule_and_vocabulary_takes_a_step():
     assert abs(loss.double().mean().item() - want.item()) <= 2e-5 * want.item()  # (the root mean square of its logits' errors is 1e-6)
     reference = torch.autograd.grad(want, double)
     for a, b, what in zip(grads, reference, ("table", "w1", "up", "down", "w2")):
-        close(a, b, 3 * delta_tol(torch.float32, T, d, 3), what)
+        close(a, b, 3 * delta_tol(T, d, 3), what)
     # and the step that they make
     plan = snn.snn_adamw_plan(params, *snn.snn_adamw_moments(params))
     before = [p.cpu().double() for p in params]
