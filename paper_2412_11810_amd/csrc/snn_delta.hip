@@ -64,6 +64,8 @@ struct Args {
 };
 
 __device__ __forceinline__ int length_of(const Args &a, int b) { return a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T; }
+// The chunks behind a sequence's end change nothing: they are left out, but for zeros in what they should give. Of c0..c1, those before that
+__device__ __forceinline__ int before_end(const Args &a, int len, int c0, int c1) { return min(c1, max(c0, (len + C - 1) / C - a.first)); }
 
 // ---- products ------------------------------------------------------------------------------
 // Matrix instructions of 16 x 16 with sums over 32.  Lane l has row (of B: column) l % 16 and sums 8 (l / 16) on of both operands, and elements 4 (l / 16) on of
@@ -335,6 +337,7 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
   const int unit = blockIdx.x, kh = unit % a.key_heads, b = unit / a.key_heads % a.batch, c = unit / a.key_heads / a.batch;
   const int t0 = (a.first + c) * C, len = length_of(a, b), group = ONE ? 1 : a.heads / a.key_heads;
+  if (t0 >= len) return;
   const int t = t0 + 16 * w + r;
   constexpr int SIZE = DK * C * PI; // elements of one operand array of a unit
   Octet<T> kr[KK], qr[KK];
@@ -566,7 +569,7 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
   tile s[RT][NT] = {};
   if (a.from) state_from(a.from + ((REC ? (long long)(a.first / KEPT + segment) * per : 0) + u.of) * a.dk * a.dv, srow, col, a.dk, a.dv, s);
   loaded();
-  const int c0 = REC ? segment * KEPT : 0, c1 = REC ? min(c0 + KEPT, a.chunks) : a.chunks;
+  const int c0 = REC ? segment * KEPT : 0, chunks = REC ? min(c0 + KEPT, a.chunks) : a.chunks, c1 = before_end(a, len, c0, chunks);
   const int row0 = 16 * w + 4 * q4;
   // What the next chunk needs is on its way while this one is worked on: each part is asked for as soon as this chunk's has been used.
   Operand<PI> k[KK], q[REC ? 1 : KK], kt[RT][2];
@@ -691,8 +694,16 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
     ask_columns(next);
     ask_gates(next);
   }
-  if constexpr (!REC)
+  if constexpr (!REC) {
+    for (int c = c1; c < chunks; ++c) {
+      const int t0 = (a.first + c) * C;
+      if (a.kept && (a.first + c) % KEPT == 0)
+        state_to(a.kept + ((long long)((a.first + c) / KEPT) * per + u.of) * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
+      const tile none[NT] = {};
+      v.put(strip, (T *)a.o + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv + v0, step_o, 16 * w, lane, Place{a.T - t0, len - t0, a.dv - v0}, false, none);
+    }
     if (a.to) state_to(a.to + (long long)u.of * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
+  }
 }
 
 // ---- the walk back --------------------------------------------------------------------------------
@@ -749,8 +760,14 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
     gam = *(const tile *)(gates + row0);
     end = gates[C - 1];
   };
-  if (a.chunks) {
-    const int c = a.chunks - 1;
+  const int chunks = before_end(a, len, 0, a.chunks);
+  for (int c = chunks; c < a.chunks; ++c) {
+    const int t0 = (a.first + c) * C;
+    const tile none[NT] = {};
+    raw.put(strip, (T *)a.dv_ + ((long long)t0 * a.batch + b) * a.ld_dv + h * a.dv + v0, step_v, 16 * w, lane, Place{a.T - t0, len - t0, a.dv - v0}, false, none);
+  }
+  if (chunks) {
+    const int c = chunks - 1;
     ask_values(c);
     ask_rows(c);
     ask_squares(a.bt, c, bm);
@@ -758,7 +775,7 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
     ask_columns(c);
     ask_gates(c);
   }
-  for (int c = a.chunks - 1; c >= 0; --c) {
+  for (int c = chunks - 1; c >= 0; --c) {
     const int t0 = (a.first + c) * C, next = max(c - 1, 0);
     const long long of = of_head(c);
     const bool whole = cols && t0 + C <= len;
@@ -855,7 +872,12 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
   const int t0 = (a.first + c) * C, len = length_of(a, b), group = ONE ? 1 : a.heads / a.key_heads, row0 = 16 * w + 4 * q4;
   const int mine = 16 * w + r, t = t0 + mine; // a lane's step
   tile gq[NT] = {}, gk[NT] = {};
-  for (int i = 0; i < group; ++i) {
+  if (t0 >= len && wave == 0 && t0 + lane < a.T)
+    for (int i = 0; i < group; ++i) {
+      const long long at = ((long long)(t0 + lane) * a.batch + b) * a.heads + kh * group + i;
+      a.dg[at] = a.dbeta[at] = 0.f;
+    }
+  for (int i = 0; i < group && t0 < len; ++i) {
     const int h = kh * group + i;
     const long long of = ((long long)c * a.batch + b) * a.heads + h;
     long long of_k = (long long)unit * (DK * C * PI);

@@ -681,6 +681,34 @@ def test_delta_pieces_of_long_sequences(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_delta_ends_in_any_piece(dtype):
+    # a sequence that ends long before the others: the same bits as if they all ended there, whatever piece that is in
+    T, B, H = 64 * 160, 2, 32
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rand = lambda *x: torch.randn(x, generator=g, device="cuda")  # noqa: E731
+    q, k = (torch.nn.functional.normalize(rand(T, B, H, 128), dim=-1).to(dtype) for _ in range(2))
+    x = [q, k, rand(T, B, H, 64).to(dtype), -0.1 * rand(T, B, H).abs(), torch.sigmoid(rand(T, B, H))]
+    do, ds = rand(T, B, H, 64).to(dtype), rand(B, H, 128, 64)
+    for n in (70, 64 * 128, 64 * 150 + 1):
+        lengths = torch.tensor([T, n], dtype=torch.int32, device="cuda")
+        for y in (*x, do):
+            y[n:, 1] = math.nan
+        o, last, kept = snn.snn_delta_forward(*x, lengths=lengths, keep=True)
+        grads = snn.snn_delta_backward(*x, kept, do, ds, lengths=lengths)
+        short = [y[:n] for y in x]
+        want = snn.snn_delta_forward(*short, keep=True)
+        back = snn.snn_delta_backward(*short, want[2], do[:n], ds)
+        of_one = lambda a: a[:, 1]  # noqa: E731
+        assert same(map(of_one, (o[:n], kept[:len(want[2])], *(y[:n] for y in grads[:5]))), map(of_one, (want[0], want[2], *back[:5]))), n
+        assert torch.equal(last[1], want[1][1]) and torch.equal(grads[5][1], back[5][1])
+        assert all((y[n:, 1] == 0).all() for y in (o, *grads[:5])) and (kept[len(want[2]):, 1] == last[1]).all()
+        assert all(torch.isfinite(y).all() for y in (o, last, *grads))
+        for y in (*x, do):  # (the next end is further on)
+            y[n:, 1] = y[n:, 0]
+
+
+@gpu
 def test_delta_beyond_4_gb():
     T, B, H, dv = 32768 + 16, 8, 64, 128  # 2^31 elements and more of v, of o
     g = torch.Generator(device="cuda").manual_seed(4)
