@@ -449,6 +449,9 @@ class AdamwPlan:
 
     def __init__(self, params, m, v, copies, tensors, device):
         self.params, self.m, self.v, self.copies, self.tensors, self.device = params, m, v, copies, tensors, device
+        # (the memory that `tensors` points at stays, also where a tensor is given other memory)
+        parts = (y for x in (*params, *m, *v, *copies) if x is not None for y in (x if isinstance(x, Packed) else (x,)))
+        self.memory = [x.detach() for x in parts]
 
 
 def snn_adamw_moments(params, bits=32):
@@ -476,7 +479,7 @@ def snn_adamw_moments(params, bits=32):
 def snn_adamw_plan(params, m, v, copies=None):
     """What snn_adamw_step needs of its tensors, once for all steps: params (float32 or bfloat16, contiguous), their moments (snn_adamw_moments,
     or tensors like those) and, if wanted, copies in bfloat16 of params in float32 (None in the list: no copy of that one).
-    The tensors are held, and changed in place by each step."""
+    The tensors are held, and changed in place by each step; params that have been given other memory since (x.data = ...) need a new plan."""
     import torch
     params, m, v = list(params), list(m), list(v)
     copies = [None] * len(params) if copies is None else list(copies)
@@ -512,7 +515,7 @@ def snn_adamw_plan(params, m, v, copies=None):
 def snn_adamw_step(plan, grads, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None):
     """One step of AdamW: params, moments and copies of the plan change in place.  grads: a gradient (float32 or bfloat16, contiguous) for each of
     params.  step: 1, 2, ..., or an int32 tensor [1] on the device with the number of steps taken, which the call counts up (a step in a
-    graph).  grad_scale: float32 [1] that the gradients are multiplied by first."""
+    graph).  grad_scale: float32 [1] that the gradients are multiplied by first.  A plan is for one call at a time."""
     import torch
     grads = list(grads)
     if len(grads) != len(plan.params):
@@ -527,6 +530,8 @@ def snn_adamw_step(plan, grads, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, wei
             t.dtype_g = SNN_F32
         else:
             raise TypeError(f"grads[{i}] must be float32 or bfloat16, got {g.dtype}")
+        if p.data_ptr() != (t.p or 0):
+            raise ValueError(f"params[{i}] has other memory than when the plan was made")
         if g.shape != p.shape or g.device != device or not g.is_contiguous():
             _packed_rows(_same(g, f"grads[{i}]", g.dtype, p.shape, device), f"grads[{i}]")
         t.g = g.data_ptr()

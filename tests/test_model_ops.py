@@ -920,6 +920,22 @@ def test_binding_of_norm_and_adamw_refuses_tensors_that_do_not_fit():
             call()
 
 
+def test_a_plan_is_of_the_memory_that_its_tensors_had():
+    import weakref
+    p = torch.nn.Parameter(torch.zeros(40))
+    m, v = snn.snn_adamw_moments([p])
+    plan = snn.snn_adamw_plan([p], m, v)
+    old = plan.memory[0]
+    assert old.data_ptr() == p.data_ptr() == plan.tensors[0].p
+    p.data = torch.ones(40)
+    assert (old == 0).all() and old.data_ptr() == plan.tensors[0].p
+    with pytest.raises(ValueError, match="other memory"):
+        snn.snn_adamw_step(plan, [torch.zeros(40)], 1)
+    held = weakref.ref(plan.memory[0])
+    del old, plan
+    assert held() is None
+
+
 def test_c_entry_points_of_the_delta_rule_refuse_what_they_cannot_run():
     L, at = snn.lib(), ops.snn_launch(0, None, None, 0)
     here = C.cast(C.create_string_buffer(4096), C.c_void_p).value
