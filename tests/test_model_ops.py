@@ -274,6 +274,35 @@ def test_adamw_steps(bits, many):
 
 
 @gpu
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_of_parts_of_arrays(bits):
+    # at any address, and nothing beside them is touched
+    shapes, kinds = [(37,), (8200,), (1,), (3, 50)], [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)] * 2
+    params, grads, copies, m, v = adamw_inputs(shapes, bits, kinds)
+    wide, at = [], 0
+
+    def part(x):
+        nonlocal at
+        at += 1
+        w = torch.full((x.numel() + 16,), 99, dtype=x.dtype, device="cuda")
+        first = 1 + at % 7
+        w[first:first + x.numel()] = x.flatten()
+        wide.append((w, first, x.numel()))
+        return w[first:first + x.numel()].view(x.shape)
+
+    of = lambda x: snn.Packed(*map(part, x)) if bits == 8 else part(x)  # noqa: E731
+    plans = [snn.snn_adamw_plan([part(x) for x in params], [of(x) for x in m], [of(x) for x in v], [x if x is None else part(x) for x in copies])]
+    theirs = [part(g) for g in grads]
+    plans.append(snn.snn_adamw_plan(params, m, v, copies))
+    for t in (1, 2, 3):
+        snn.snn_adamw_step(plans[0], theirs, t)
+        snn.snn_adamw_step(plans[1], grads, t)
+    assert same(plans[0].memory, plans[1].memory)
+    for w, first, n in wide:
+        assert (w[:first] == 99).all() and (w[first + n:] == 99).all()
+
+
+@gpu
 def test_adamw_in_8_bits_follows_moments_that_change_little_at_a_time():
     # gradients that stop: a root changes by 1/2000 of itself at a time, a twentieth of a code at most
     params = [torch.zeros(4096, device="cuda")]
@@ -471,7 +500,8 @@ def close(got, want, tol, what):
 DELTA = [(0, 2, 3, 3, 5, 7, False), (1, 2, 3, 3, 5, 7, False), (1, 64, 4, 2, 128, 128, False), (3, 2, 2, 1, 65, 130, True), (16, 2, 4, 4, 128, 64, True),
          (17, 1, 2, 2, 16, 16, False), (63, 2, 1, 1, 1, 1, False), (64, 2, 2, 2, 64, 64, False), (65, 3, 3, 1, 48, 75, True), (130, 3, 2, 2, 33, 31, True),
          (256, 1, 2, 2, 128, 128, False), (257, 3, 2, 1, 64, 100, True), (300, 5, 4, 2, 128, 40, True), (700, 1, 1, 1, 100, 256, False),
-         (200, 4, 6, 2, 72, 33, True), (128, 8, 8, 8, 32, 96, False), (8, 2, 3, 1, 100, 70, True), (12, 64, 4, 2, 24, 40, True), (32, 64, 4, 4, 70, 20, False)]
+         (200, 4, 6, 2, 72, 33, True), (128, 8, 8, 8, 32, 96, False), (8, 2, 3, 1, 100, 70, True), (12, 64, 4, 2, 24, 40, True), (32, 64, 4, 4, 70, 20, False),
+         (70, 1, 2, 1, 128, 1024, False), (2, 1, 3, 3, 17, 1000, False), (40, 300, 6, 2, 5, 3, True), (90, 2, 40, 5, 16, 33, True)]
 
 
 @gpu
