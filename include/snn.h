@@ -381,7 +381,7 @@ snn_status snn_vocab_loss_grad(const snn_launch *at, const snn_vocab *p, const v
  * beta 0..1 the state stays bounded; g <= 0 as a rule, minus infinity forgets all (as -10^4 does).  Computed in fp32, sums over a
  * sequence's gates in fp64; what goes through the matrix cores keeps 24 bits, but for 16 of the factors of a result in bf16.  Where a state, key,
  * value or gate is not finite, its head's results need not be from its chunk of 64 steps on, and no gradient of the head; other heads are not touched, but for the
- * gradients of queries and keys that they share with it. */
+ * gradients of queries and keys that they share with it.  The same holds where keys or gates would let a state grow beyond 32 bits, also if it is 0. */
 typedef struct {
   int32_t T, batch;          /* T >= 0 (0: s_last = s0), at most 2^30 */
   int32_t heads, key_heads;  /* heads a multiple of key_heads: head h has the queries and keys of h / (heads / key_heads).  batch * heads 2^20 at most */

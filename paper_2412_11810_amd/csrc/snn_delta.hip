@@ -23,9 +23,10 @@
 // were off by up to 7e-6 of their norm and gradients of gates by 2e-5.)  Where nothing but a result in bf16 comes of a product, o and the products of the
 // chunk's own steps in dq and dk, two parts are enough: 2^-17 of each factor, beside 2^-8 of the result.
 //
-// Four kernels: what is of a chunk alone (k_chunk: A, B, and the operands in the order in which a wavefront loads them); the walk over the chunks
+// The kernels: what is of a chunk alone (k_chunk: A, B, and the operands in the order in which a wavefront loads them); the walk over the chunks
 // with S in registers, its columns dealt to workgroups (k_walk; for the backward pass it starts at each kept state, every 4 chunks); the walk back
-// with dS (k_walk_back); and what needs S, dS', w and dE of a chunk (k_grads).  They go through the sequence in pieces whose intermediate arrays fit the caches
+// with dS (k_walk_back); and what needs S, dS', w and dE of a chunk (k_grads).  Where there are few heads the walks take segments of a long sequence side by side, from
+// states found by the segments' maps, S' = M S + c (k_join).  They go through the sequence in pieces whose intermediate arrays fit the caches
 // or nearly so.  Few steps are taken one after the other, by a kernel whose workgroup holds the whole state of a head (k_steps).
 //
 // At 4096 x 8 x 16 x 128 x 128 in bf16 forward takes 486 us and backward 1832 (memory alone would take 135 and 240): what a chunk's steps need of each other, and a chunk
@@ -49,7 +50,7 @@ template <class T> constexpr int LAST = sizeof(T) == 2 ? 2 : 3; // and of that, 
 
 struct Args {
   const void *q, *k, *v, *dout;
-  const float *g, *beta, *from; // from: s0, kept (k_walk in the backward pass), ds_last; NULL: zeros
+  const float *g, *beta, *from; // from: s0, kept (k_walk in the backward pass), ds_last, or the segments' states; NULL: zeros
   void *o, *dq, *dk_, *dv_;
   float *to, *kept, *dg, *dbeta; // to: s_last, ds0
   const int *lengths;
@@ -60,9 +61,11 @@ struct Args {
   double *sums;                // [64]: G, as exponents of two
   float *before, *after;       // S and dS' [dk padded][dvp]
   float *w, *de;               // [64][dvp]
+  float *maps, *bounds;        // of segments: [dk padded][dvp + dk padded], c and M; the states that they begin with
   long long ld_q, ld_k, ld_v, ld_o, ld_dq, ld_dk, ld_dv;
   int T, batch, heads, key_heads, dk, dv, dvp, blocks;
   int first, chunks; // the piece's first chunk, its chunks
+  int length, segments; // those of a segment of the piece
   float scale;
 };
 
@@ -557,30 +560,43 @@ __device__ __forceinline__ Unit unit_of(unsigned id, int units, int blocks) {
   return {(int)(id / blocks), (int)(id % blocks)};
 }
 
-// REC: of the backward pass, from a kept state to the next; leaves S and w of each chunk.
+// AGAIN: of the backward pass, from a kept state to the next; leaves S and w of each chunk.  MAPS: leaves what a segment makes of the state before it, M S + c:
+// c from no state, and M's columns from those of the identity, without values.
 // What bounds it: a chunk's three products after one another, with an exchange through LDS and a barrier after each, 5 us for 32 columns of 128 channels with two
 // workgroups in a compute unit; the matrix cores work in half of that.  322 us for 64 chunks of 128 heads.  Operands as k_chunk laid them out go from
 // memory to registers a chunk ahead; made here of rows of q and k they took 350 us instead of 279.
-template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk(Args a) {
+enum Walk { WALK, AGAIN, MAPS };
+template <int RT, int NT> __device__ __forceinline__ void identity(int row, int col, tile (&s)[RT][NT]) {
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[i][n][e] = row + 16 * i + e == col + 16 * n ? 1.f : 0.f;
+}
+template <class T, int DK, int BV, Walk HOW> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk(Args a) {
+  constexpr bool REC = HOW == AGAIN, OUT = HOW == WALK;
   constexpr int PI = GIVEN<T>, PC = MADE, PO = LAST<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
   __shared__ __align__(16) Planes<PC, BV, DK> st;
   __shared__ __align__(16) Planes<PC, BV, C> et, wt;
   __shared__ __align__(16) char strips[4][REC && Strip<float, BV>::BYTES > Strip<T, BV>::BYTES ? Strip<float, BV>::BYTES : Strip<T, BV>::BYTES];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
-  const int per = a.batch * a.heads;
-  const Unit u = unit_of(blockIdx.x % (per * a.blocks), per, a.blocks);
-  const int segment = blockIdx.x / (per * a.blocks); // REC: of KEPT chunks
-  const int h = u.of % a.heads, b = u.of / a.heads, kh = h / (a.heads / a.key_heads), v0 = u.block * BV;
+  const int per = a.batch * a.heads, blocks = a.blocks + (HOW == MAPS ? DK / BV : 0);
+  const Unit u = unit_of(blockIdx.x % (per * blocks), per, blocks);
+  const int segment = blockIdx.x / (per * blocks);
+  const bool of_map = HOW == MAPS && u.block >= a.blocks;
+  const int h = u.of % a.heads, b = u.of / a.heads, kh = h / (a.heads / a.key_heads), v0 = (of_map ? u.block - a.blocks : u.block) * BV;
   const int len = length_of(a, b);
   const int srow = 16 * w * RT + 4 * q4, col = v0 + r;
-  const bool cols = v0 + BV <= a.dv, all = cols && a.dk == DK; // the columns, the state are there
+  const bool cols = !of_map && v0 + BV <= a.dv, all = cols && a.dk == DK; // the columns, the state are there
   tile s[RT][NT] = {};
-  if (a.from) state_from(a.from + ((REC ? (long long)(a.first / KEPT + segment) * per : 0) + u.of) * a.dk * a.dv, srow, col, a.dk, a.dv, s);
+  if (HOW != MAPS && a.from) state_from(a.from + ((long long)((REC ? a.first / KEPT : 0) + segment) * per + u.of) * a.dk * a.dv, srow, col, a.dk, a.dv, s);
+  if (of_map) identity(srow, col, s);
   loaded();
-  const int c0 = REC ? segment * KEPT : 0, chunks = REC ? min(c0 + KEPT, a.chunks) : a.chunks, c1 = before_end(a, len, c0, chunks);
+  const int c0 = segment * a.length, chunks = min(c0 + a.length, a.chunks), c1 = before_end(a, len, c0, chunks);
   const int row0 = 16 * w + 4 * q4;
   // What the next chunk needs is on its way while this one is worked on: each part is asked for as soon as this chunk's has been used.
-  Operand<PI> k[KK], q[REC ? 1 : KK], kt[RT][2];
+  Operand<PI> k[KK], q[OUT ? KK : 1], kt[RT][2];
   Operand<PC> am[2];
   Operand<PO> bm[2];
   Strip<T, BV> v;
@@ -593,13 +609,14 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
 #pragma unroll
     for (int i = 0; i < KK; ++i) {
       k[i] = fetch<PI>(a.kf + of_keys(c), w * KK + i, lane);
-      if constexpr (!REC) q[i] = fetch<PI>(a.qf + of_keys(c), w * KK + i, lane);
+      if constexpr (OUT) q[i] = fetch<PI>(a.qf + of_keys(c), w * KK + i, lane);
     }
   };
   const unsigned step_v = (unsigned)(a.batch * a.ld_v), step_o = (unsigned)(a.batch * a.ld_o);
+  auto place_of = [&](int t0) { return Place{a.T - t0, len - t0, of_map ? 0 : a.dv - v0}; };
   auto ask_values = [&](int c) {
     const int t0 = (a.first + c) * C;
-    v.ask((const T *)a.v + ((long long)t0 * a.batch + b) * a.ld_v + h * a.dv + v0, step_v, 16 * w, lane, Place{a.T - t0, len - t0, a.dv - v0});
+    v.ask((const T *)a.v + ((long long)t0 * a.batch + b) * a.ld_v + h * a.dv + v0, step_v, 16 * w, lane, place_of(t0));
   };
   auto ask_squares = [&](const __bf16 *p, int c, auto &m) { // (lower triangular: the first two rows of blocks have zeros behind)
     constexpr int P = sizeof(m[0].p) / sizeof(frag);
@@ -622,17 +639,18 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
     ask_rows(c0);
     ask_values(c0);
     ask_squares(a.af, c0, am);
-    if constexpr (!REC) ask_squares(a.bf, c0, bm);
+    if constexpr (OUT) ask_squares(a.bf, c0, bm);
     ask_columns(c0);
     ask_gates(c0);
   }
   for (int c = c0; c < c1; ++c) {
     const int t0 = (a.first + c) * C, next = min(c + 1, c1 - 1);
     const bool whole = cols && t0 + C <= len;
-    if constexpr (!REC) {
+    if constexpr (OUT) {
       if (a.kept && (a.first + c) % KEPT == 0)
         state_to(a.kept + ((long long)((a.first + c) / KEPT) * per + u.of) * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
-    } else
+    }
+    if constexpr (REC)
 #pragma unroll
       for (int i = 0; i < RT; ++i) // (dvp is a multiple of the 32 columns of a workgroup)
         Strip<float, BV>::put(strip, a.before + of_head(c) * DK * a.dvp + v0, a.dvp, 16 * (w * RT + i), lane, Place{}, true, s[i]);
@@ -647,14 +665,14 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
       Operand<PC> y[NT];
       st.get(r, 32 * i + 8 * q4, y);
       multiply(e, k[i], y);
-      if constexpr (!REC) {
+      if constexpr (OUT) {
         Operand<PO> z[NT];
         first_parts(y, z);
         multiply(o, q[i], z);
       }
     }
     ask_rows(next);
-    const Place place = {a.T - t0, len - t0, a.dv - v0};
+    const Place place = place_of(t0);
     tile vn[NT];
     v.get(strip, 16 * w, lane, place, whole, vn);
 #pragma unroll
@@ -666,7 +684,7 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
     ask_values(next);
     lds_barrier();
     tile x[NT] = {};
-    if constexpr (!REC)
+    if constexpr (OUT)
 #pragma unroll
       for (int n = 0; n < NT; ++n) o[n] *= gam * a.scale;
 #pragma unroll
@@ -675,18 +693,18 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
         Operand<PC> y[NT];
         et.get(r, 32 * j + 8 * q4, y);
         multiply(x, am[j], y);
-        if constexpr (!REC) {
+        if constexpr (OUT) {
           Operand<PO> z[NT];
           first_parts(y, z);
           multiply(o, bm[j], z);
         }
       }
     ask_squares(a.af, next, am);
-    if constexpr (!REC) ask_squares(a.bf, next, bm);
+    if constexpr (OUT) ask_squares(a.bf, next, bm);
     if constexpr (REC) Strip<float, BV>::put(strip, a.w + of_head(c) * C * a.dvp + v0, a.dvp, 16 * w, lane, Place{}, true, x);
 #pragma unroll
     for (int n = 0; n < NT; ++n) wt.put(16 * n + r, row0, REC ? x[n] * left : x[n]);
-    if constexpr (!REC) v.put(strip, (T *)a.o + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv + v0, step_o, 16 * w, lane, place, whole, o);
+    if constexpr (OUT) v.put(strip, (T *)a.o + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv + v0, step_o, 16 * w, lane, place, whole, o);
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -702,35 +720,41 @@ template <class T, int DK, int BV, bool REC> __global__ __launch_bounds__(256, s
     ask_columns(next);
     ask_gates(next);
   }
-  if constexpr (!REC) {
+  if constexpr (HOW == MAPS)
+    state_to(a.maps + ((long long)segment * per + u.of) * DK * (a.dvp + DK) + (of_map ? a.dvp : 0), srow, col, DK, a.dvp + DK, true, s);
+  if constexpr (OUT) {
     for (int c = c1; c < chunks; ++c) {
       const int t0 = (a.first + c) * C;
       if (a.kept && (a.first + c) % KEPT == 0)
         state_to(a.kept + ((long long)((a.first + c) / KEPT) * per + u.of) * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
       const tile none[NT] = {};
-      v.put(strip, (T *)a.o + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv + v0, step_o, 16 * w, lane, Place{a.T - t0, len - t0, a.dv - v0}, false, none);
+      v.put(strip, (T *)a.o + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv + v0, step_o, 16 * w, lane, place_of(t0), false, none);
     }
-    if (a.to) state_to(a.to + (long long)u.of * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
+    if (a.to && segment == a.segments - 1) state_to(a.to + (long long)u.of * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
   }
 }
 
 // ---- the walk back --------------------------------------------------------------------------------
 // As the walk, with four products, two of them after one another: 228 us for 32 chunks of 128 heads of 128 channels in bf16.
-template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk_back(Args a) {
+template <class T, int DK, int BV, Walk HOW> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk_back(Args a) {
+  constexpr bool OUT = HOW == WALK;
   constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32, RT = DK / 64, NT = BV / 16;
   __shared__ __align__(16) Planes<PC, BV, DK> st;
   __shared__ __align__(16) Planes<PI, BV, C> ot;
   __shared__ __align__(16) Planes<PC, BV, C> got, ut, et; // scale gam dO, K dS', -gam dE
   __shared__ __align__(16) char strips[4][Strip<float, BV>::BYTES];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
-  const int per = a.batch * a.heads;
-  const Unit u = unit_of(blockIdx.x, per, a.blocks);
-  const int h = u.of % a.heads, b = u.of / a.heads, kh = h / (a.heads / a.key_heads), v0 = u.block * BV;
+  const int per = a.batch * a.heads, blocks = a.blocks + (HOW == MAPS ? DK / BV : 0);
+  const Unit u = unit_of(blockIdx.x % (per * blocks), per, blocks);
+  const int segment = blockIdx.x / (per * blocks) + (HOW == MAPS); // (nothing comes before the first)
+  const bool of_map = HOW == MAPS && u.block >= a.blocks;
+  const int h = u.of % a.heads, b = u.of / a.heads, kh = h / (a.heads / a.key_heads), v0 = (of_map ? u.block - a.blocks : u.block) * BV;
   const int len = length_of(a, b);
   const int srow = 16 * w * RT + 4 * q4, col = v0 + r;
-  const bool cols = v0 + BV <= a.dv, all = cols && a.dk == DK;
+  const bool cols = !of_map && v0 + BV <= a.dv, all = cols && a.dk == DK;
   tile s[RT][NT] = {};
-  if (a.from) state_from(a.from + (long long)u.of * a.dk * a.dv, srow, col, a.dk, a.dv, s);
+  if (HOW != MAPS && a.from) state_from(a.from + ((long long)segment * per + u.of) * a.dk * a.dv, srow, col, a.dk, a.dv, s);
+  if (of_map) identity(srow, col, s);
   loaded();
   const int row0 = 16 * w + 4 * q4;
   // (as in k_walk)
@@ -747,9 +771,10 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
     for (int i = 0; i < KK; ++i) k[i] = fetch<PI>(a.kf + of_keys(c), w * KK + i, lane);
   };
   const unsigned step_o = (unsigned)(a.batch * a.ld_o), step_v = (unsigned)(a.batch * a.ld_dv);
+  auto place_of = [&](int t0) { return Place{a.T - t0, len - t0, of_map ? 0 : a.dv - v0}; };
   auto ask_values = [&](int c) {
     const int t0 = (a.first + c) * C;
-    raw.ask((const T *)a.dout + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv + v0, step_o, 16 * w, lane, Place{a.T - t0, len - t0, a.dv - v0});
+    raw.ask((const T *)a.dout + ((long long)t0 * a.batch + b) * a.ld_o + h * a.dv + v0, step_o, 16 * w, lane, place_of(t0));
   };
   auto ask_squares = [&](const __bf16 *p, int c, Operand<PC> (&m)[2]) { // (upper triangular: the last two rows of blocks begin with zeros)
     if (w < 2) m[0] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w, lane);
@@ -769,14 +794,15 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
     gam = *(const tile *)(gates + row0);
     end = gates[C - 1];
   };
-  const int chunks = before_end(a, len, 0, a.chunks);
-  for (int c = chunks; c < a.chunks; ++c) {
-    const int t0 = (a.first + c) * C;
-    const tile none[NT] = {};
-    raw.put(strip, (T *)a.dv_ + ((long long)t0 * a.batch + b) * a.ld_dv + h * a.dv + v0, step_v, 16 * w, lane, Place{a.T - t0, len - t0, a.dv - v0}, false, none);
-  }
-  if (chunks) {
-    const int c = chunks - 1;
+  const int c0 = segment * a.length, chunks = min(c0 + a.length, a.chunks), c1 = before_end(a, len, c0, chunks);
+  if constexpr (OUT)
+    for (int c = c1; c < chunks; ++c) {
+      const int t0 = (a.first + c) * C;
+      const tile none[NT] = {};
+      raw.put(strip, (T *)a.dv_ + ((long long)t0 * a.batch + b) * a.ld_dv + h * a.dv + v0, step_v, 16 * w, lane, place_of(t0), false, none);
+    }
+  if (c0 < c1) {
+    const int c = c1 - 1;
     ask_values(c);
     ask_rows(c);
     ask_squares(a.bt, c, bm);
@@ -784,13 +810,14 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
     ask_columns(c);
     ask_gates(c);
   }
-  for (int c = chunks - 1; c >= 0; --c) {
-    const int t0 = (a.first + c) * C, next = max(c - 1, 0);
+  for (int c = c1 - 1; c >= c0; --c) {
+    const int t0 = (a.first + c) * C, next = max(c - 1, c0);
     const long long of = of_head(c);
     const bool whole = cols && t0 + C <= len;
-    const Place place = {a.T - t0, len - t0, a.dv - v0};
+    const Place place = place_of(t0);
+    if constexpr (OUT)
 #pragma unroll
-    for (int i = 0; i < RT; ++i) Strip<float, BV>::put(strip, a.after + of * DK * a.dvp + v0, a.dvp, 16 * (w * RT + i), lane, place, true, s[i]);
+      for (int i = 0; i < RT; ++i) Strip<float, BV>::put(strip, a.after + of * DK * a.dvp + v0, a.dvp, 16 * (w * RT + i), lane, place, true, s[i]);
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -838,8 +865,8 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
         for (int e = 0; e < 4; ++e) x[n][e] = t0 + row0 + e < len ? x[n][e] : 0.f;
       et.put(16 * n + r, row0, x[n] * -gam);
     }
-    Strip<float, BV>::put(strip, a.de + of * C * a.dvp + v0, a.dvp, 16 * w, lane, place, true, x);
-    raw.put(strip, (T *)a.dv_ + ((long long)t0 * a.batch + b) * a.ld_dv + h * a.dv + v0, step_v, 16 * w, lane, place, whole, x);
+    if constexpr (OUT) Strip<float, BV>::put(strip, a.de + of * C * a.dvp + v0, a.dvp, 16 * w, lane, place, true, x);
+    if constexpr (OUT) raw.put(strip, (T *)a.dv_ + ((long long)t0 * a.batch + b) * a.ld_dv + h * a.dv + v0, step_v, 16 * w, lane, place, whole, x);
     lds_barrier();
 #pragma unroll
     for (int i = 0; i < RT; ++i)
@@ -858,7 +885,51 @@ template <class T, int DK, int BV> __global__ __launch_bounds__(256, sizeof(T) =
     ask_columns(next);
     ask_gates(next);
   }
-  if (a.to) state_to(a.to + (long long)u.of * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
+  if constexpr (HOW == MAPS)
+    state_to(a.maps + ((long long)segment * per + u.of) * DK * (a.dvp + DK) + (of_map ? a.dvp : 0), srow, col, DK, a.dvp + DK, true, s);
+  else if (a.to && !segment) state_to(a.to + (long long)u.of * a.dk * a.dv, srow, col, a.dk, a.dv, all, s);
+}
+
+// ---- the states between segments ------------------------------------------------------------------
+// S' = M S + c, a segment after the other, by instructions of 32 bits; a workgroup has 16 columns.
+template <int DK, bool BACK> __global__ __launch_bounds__(256) void k_join(Args a) {
+  constexpr int RT = DK / 64, KT = DK / 16;
+  __shared__ __align__(16) float st[2][16][DK + 4];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
+  const int per = a.batch * a.heads, blocks = a.dvp / 16, of = blockIdx.x / blocks, col = blockIdx.x % blocks * 16 + r, row0 = 16 * w * RT + 4 * q4, ld = a.dvp + DK;
+  tile s[RT][1] = {};
+  if (a.from) state_from(a.from + (long long)of * a.dk * a.dv, row0, col, a.dk, a.dv, s);
+  tile m[RT][KT], c[RT];
+  auto ask = [&](int segment) {
+    const float *from = a.maps + ((long long)segment * per + of) * DK * ld;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+#pragma unroll
+      for (int j = 0; j < KT; ++j) m[i][j] = *(const tile *)(from + (16 * (w * RT + i) + r) * ld + a.dvp + 16 * j + 4 * q4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[i][e] = from[(row0 + 16 * i + e) * ld + col];
+    }
+  };
+  if (a.segments > 1) ask(BACK ? a.segments - 1 : 0);
+  for (int n = 0; n < a.segments; ++n) {
+    const int segment = BACK ? a.segments - 1 - n : n;
+    state_to(a.bounds + ((long long)segment * per + of) * a.dk * a.dv, row0, col, a.dk, a.dv, false, s);
+    if (n == a.segments - 1) break;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) *(tile *)&st[n & 1][r][row0 + 16 * i] = s[i][0];
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < RT; ++i) s[i][0] = c[i];
+#pragma unroll
+    for (int j = 0; j < KT; ++j) {
+      const tile f = *(const tile *)&st[n & 1][r][16 * j + 4 * q4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) s[i][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(m[i][j][e], f[e], s[i][0], 0, 0, 0);
+    }
+    if (n + 2 < a.segments) ask(BACK ? segment - 1 : segment + 1);
+  }
 }
 
 // ---- gradients of a chunk's queries, keys and gates -----------------------------------------------
@@ -1238,7 +1309,7 @@ size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // Columns of the state that a workgroup walks with: fewer where there would be few workgroups, as a chunk then takes a shorter time.  4096 steps, 128 x 128, in us,
 // with 16 and with 32 columns: forward in fp32 4 heads 207 and 269, 32 heads 379 and 418, 64 heads 725 and 517; in bf16 132 and 186, 176 and 224, 331 and 269;
-// backward in fp32 4 heads 327 and 389, 16 heads 613 and 649, 32 heads 933 and 926, 64 heads 1831 and 1460; in bf16 210 and 263, 366 and 396, 627 and 608, 1139
+// backward in fp32 4 heads 327 and 389 (in one segment each), 16 heads 613 and 649, 32 heads 933 and 926, 64 heads 1831 and 1460; in bf16 210 and 263, 366 and 396, 627 and 608, 1139
 // and 951.  64 columns to a workgroup are no faster than 32.
 int columns(const DeltaShape &p, bool back) {
   const long long heads = (long long)p.batch * p.heads;
@@ -1251,6 +1322,17 @@ int columns(const DeltaShape &p, bool back) {
 bool one_by_one(const DeltaShape &p) {
   const long long heads = (long long)p.batch * p.heads;
   return p.T <= (heads < 128 ? 8 : heads < 512 ? p.bf16 ? 8 : 16 : p.bf16 ? 12 : 32);
+}
+
+// Segments of a piece, walked side by side: one walk leaves their maps, k_join the states between them, and another walk the results.  That is 2.5 times the work, for
+// walks that would leave most of the chip idle, 512 workgroups in all, and at least 8 chunks for each of 3 segments.  In one segment and so, us, forward and backward:
+// 16384 steps, 8 heads of 64 x 128 in bf16 438 and 190, 859 and 530, in fp32 653 and 315, 1164 and 774; 4096 steps, 4 heads of 128 x 128 in bf16 134 and 88, 219 and
+// 154, in fp32 262 and 143, 354 and 258; 2048 steps, 2 heads of 64 x 64 in bf16 61 and 46, 98 and 78.  It does not pay with more workgroups (4096 steps, 12 heads
+// of 128 x 128, 96 of them: 152 and 180, 365 and 366; 16384 steps in fp32 1188 and 1289) nor with fewer chunks (1024 steps, 4 heads, 4 chunks each: 47 and 57).
+int segments_of(int bv, long long walks, int chunks) {
+  if (bv != 16 || walks > 64) return 1;
+  const int n = (int)(512 / walks < chunks / 8 ? 512 / walks : chunks / 8);
+  return n > 2 ? n : 1;
 }
 
 struct Plan {
@@ -1266,7 +1348,7 @@ struct Plan {
     blocks = (dvp + bv - 1) / bv;
     all = (p.T + C - 1) / C;
     const size_t pi = p.bf16 ? 1 : 3, pc = MADE, po = p.bf16 ? LAST<__bf16> : LAST<float>;
-    auto lay = [&](int n) {
+    auto lay = [&](int n, int segments) {
       size_t at = 0;
       auto take = [&](auto *&to, size_t count) {
         to = (std::remove_reference_t<decltype(to)>)(work ? work + at : nullptr);
@@ -1276,6 +1358,8 @@ struct Plan {
       float *carry;
       take(carry, (size_t)per * p.dk * p.dv);
       a.to = carry;
+      take(a.maps, segments > 1 ? (size_t)segments * per * dk * (dvp + dk) : 0);
+      take(a.bounds, segments > 1 ? (size_t)segments * per * p.dk * p.dv : 0);
       for (__bf16 **x : {&a.kf, &a.qf, &a.ktf}) take(*x, nk * dk * C * pi);
       take(a.af, nh * C * C * pc);
       take(a.gates, nh * 3 * C);
@@ -1292,19 +1376,26 @@ struct Plan {
       }
       return at;
     };
-    const size_t one = lay(KEPT) - lay(0);
+    const size_t one = lay(KEPT, 1) - lay(0, 1);
     const long long most = (long long)(PIECE / one) * KEPT;
     chunks = (int)(most < KEPT ? KEPT : most > all ? all : most);
     if (chunks < all) chunks = (all + (all + chunks - 1) / chunks - 1) / ((all + chunks - 1) / chunks); // as many pieces as it takes, of one length
     chunks = (chunks + KEPT - 1) / KEPT * KEPT;
     if (chunks > all) chunks = all;
-    bytes = lay(chunks);
+    bytes = lay(chunks, segments_of(bv, (long long)per * blocks, chunks));
     a.lengths = p.lengths;
     a.ld_q = p.ld_q, a.ld_k = p.ld_k, a.ld_v = p.ld_v, a.ld_o = p.ld_o, a.ld_dq = p.ld_dq, a.ld_dk = p.ld_dk, a.ld_dv = p.ld_dv;
     a.T = p.T, a.batch = p.batch, a.heads = p.heads, a.key_heads = p.key_heads, a.dk = p.dk, a.dv = p.dv, a.dvp = dvp, a.blocks = blocks;
     a.scale = p.scale;
   }
 };
+
+// Cuts a piece into segments.  The last one may be shorter than the others
+void cut(Args &a, const Plan &p) {
+  a.segments = segments_of(p.bv, (long long)p.per * p.blocks, a.chunks);
+  a.length = (a.chunks + a.segments - 1) / a.segments;
+  if (a.length) a.segments = (a.chunks + a.length - 1) / a.length;
+}
 
 template <class T, int DK> hipError_t forward(Plan &p, hipStream_t s) {
   Args a = p.a;
@@ -1317,8 +1408,14 @@ template <class T, int DK> hipError_t forward(Plan &p, hipStream_t s) {
     a.to = first + a.chunks < p.all ? carry : p.last;
     if (a.heads == a.key_heads) k_chunk<T, DK, false, true><<<a.chunks * p.units, 256, 0, s>>>(a);
     else k_chunk<T, DK, false, false><<<a.chunks * p.units, 256, 0, s>>>(a);
-    if (p.bv == 32) k_walk<T, DK, 32, false><<<p.per * p.blocks, 256, 0, s>>>(a);
-    else k_walk<T, DK, 16, false><<<p.per * p.blocks, 256, 0, s>>>(a);
+    cut(a, p);
+    if (a.segments > 1) {
+      k_walk<T, DK, 16, MAPS><<<(a.segments - 1) * p.per * (p.blocks + DK / 16), 256, 0, s>>>(a);
+      k_join<DK, false><<<p.per * (p.dvp / 16), 256, 0, s>>>(a);
+      a.from = a.bounds;
+    }
+    if (p.bv == 32) k_walk<T, DK, 32, WALK><<<a.segments * p.per * p.blocks, 256, 0, s>>>(a);
+    else k_walk<T, DK, 16, WALK><<<a.segments * p.per * p.blocks, 256, 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     from = carry;
   }
@@ -1331,8 +1428,8 @@ template <class T, int DK> hipError_t backward(Plan &p, const float *kept, const
   if (!p.all) {
     a.from = ds_last;
     a.to = p.last;
-    if (p.bv == 32) k_walk_back<T, DK, 32><<<p.per * p.blocks, 256, 0, s>>>(a);
-    else k_walk_back<T, DK, 16><<<p.per * p.blocks, 256, 0, s>>>(a);
+    if (p.bv == 32) k_walk_back<T, DK, 32, WALK><<<p.per * p.blocks, 256, 0, s>>>(a);
+    else k_walk_back<T, DK, 16, WALK><<<p.per * p.blocks, 256, 0, s>>>(a);
     return hipGetLastError();
   }
   // pieces of whole kept intervals, from the last one on
@@ -1343,13 +1440,21 @@ template <class T, int DK> hipError_t backward(Plan &p, const float *kept, const
     else k_chunk<T, DK, true, false><<<a.chunks * p.units, 256, 0, s>>>(a);
     a.from = kept;
     a.to = nullptr;
-    const unsigned walks = p.per * p.blocks, segments = (a.chunks + KEPT - 1) / KEPT;
-    if (p.bv == 32) k_walk<T, DK, 32, true><<<segments * walks, 256, 0, s>>>(a);
-    else k_walk<T, DK, 16, true><<<segments * walks, 256, 0, s>>>(a);
+    a.length = KEPT;
+    a.segments = (a.chunks + KEPT - 1) / KEPT;
+    const unsigned walks = p.per * p.blocks;
+    if (p.bv == 32) k_walk<T, DK, 32, AGAIN><<<a.segments * walks, 256, 0, s>>>(a);
+    else k_walk<T, DK, 16, AGAIN><<<a.segments * walks, 256, 0, s>>>(a);
     a.from = from;
     a.to = first ? carry : p.last;
-    if (p.bv == 32) k_walk_back<T, DK, 32><<<walks, 256, 0, s>>>(a);
-    else k_walk_back<T, DK, 16><<<walks, 256, 0, s>>>(a);
+    cut(a, p);
+    if (a.segments > 1) {
+      k_walk_back<T, DK, 16, MAPS><<<(a.segments - 1) * p.per * (p.blocks + DK / 16), 256, 0, s>>>(a);
+      k_join<DK, true><<<p.per * (p.dvp / 16), 256, 0, s>>>(a);
+      a.from = a.bounds;
+    }
+    if (p.bv == 32) k_walk_back<T, DK, 32, WALK><<<a.segments * walks, 256, 0, s>>>(a);
+    else k_walk_back<T, DK, 16, WALK><<<a.segments * walks, 256, 0, s>>>(a);
     if (a.heads == a.key_heads) k_grads<T, DK, true><<<a.chunks * p.units, 512, 0, s>>>(a);
     else k_grads<T, DK, false><<<a.chunks * p.units, 512, 0, s>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;

@@ -501,7 +501,8 @@ DELTA = [(0, 2, 3, 3, 5, 7, False), (1, 2, 3, 3, 5, 7, False), (1, 64, 4, 2, 128
          (17, 1, 2, 2, 16, 16, False), (63, 2, 1, 1, 1, 1, False), (64, 2, 2, 2, 64, 64, False), (65, 3, 3, 1, 48, 75, True), (130, 3, 2, 2, 33, 31, True),
          (256, 1, 2, 2, 128, 128, False), (257, 3, 2, 1, 64, 100, True), (300, 5, 4, 2, 128, 40, True), (700, 1, 1, 1, 100, 256, False),
          (200, 4, 6, 2, 72, 33, True), (128, 8, 8, 8, 32, 96, False), (8, 2, 3, 1, 100, 70, True), (12, 64, 4, 2, 24, 40, True), (32, 64, 4, 4, 70, 20, False),
-         (70, 1, 2, 1, 128, 1024, False), (2, 1, 3, 3, 17, 1000, False), (40, 300, 6, 2, 5, 3, True), (90, 2, 40, 5, 16, 33, True)]
+         (70, 1, 2, 1, 128, 1024, False), (2, 1, 3, 3, 17, 1000, False), (40, 300, 6, 2, 5, 3, True), (90, 2, 40, 5, 16, 33, True),
+         (1100, 3, 2, 1, 64, 40, True), (1500, 2, 2, 2, 100, 33, True), (2600, 1, 1, 1, 16, 16, False), (1030, 1, 4, 2, 128, 130, False)]
 
 
 @gpu
