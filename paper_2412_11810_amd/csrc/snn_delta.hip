@@ -26,8 +26,8 @@
 // The kernels: what is of a chunk alone (k_chunk: A, B, and the operands in the order in which a wavefront loads them); the walk over the chunks
 // with S in registers, its columns dealt to workgroups (k_walk; for the backward pass it starts at each kept state, every 4 chunks); the walk back
 // with dS (k_walk_back); and what needs S, dS', w and dE of a chunk (k_grads).  Where there are few heads the walks take segments of a long sequence side by side, from
-// states found by the segments' maps, S' = M S + c (k_join).  They go through the sequence in pieces whose intermediate arrays fit the caches
-// or nearly so.  Few steps are taken one after the other, by a kernel whose workgroup holds the whole state of a head (k_steps).
+// states found by the segments' maps, S' = M S + c (k_join).  They go through the sequence in pieces of 2 GB of
+// intermediate arrays.  Few steps are taken one after the other, by a kernel whose workgroup holds the whole state of a head (k_steps).
 //
 // At 4096 x 8 x 16 x 128 x 128 in bf16 forward takes 486 us and backward 1832 (memory alone would take 135 and 240): what a chunk's steps need of each other, and a chunk
 // of the one before, keeps the matrix cores waiting.
@@ -330,10 +330,11 @@ template <int RT, int NT> __device__ __forceinline__ void state_to(float *to, in
 }
 
 // ---- a chunk by itself ------------------------------------------------------------------------
-// ONE: each head has queries and keys of its own.
+// A workgroup has one head; heads that share queries and keys find the products of those each for itself: a workgroup for all of them, its registers full of
+// them, took longer at every size (333 x 5 x 6 of 2 x 48 x 75 in fp32 forward 49 us instead of 35, 2048 x 4 x 6 of 2 x 128 x 128 in bf16 90 instead of 81).
 // What bounds it: the substitution's chain of sums and the barriers between its parts, some 10 us for a workgroup of which four are in a compute unit, so that
-// registers count.  182 us for 8192 chunks of 128 channels, 0.8 GB of operands written; 131 us for 4096 in the backward pass.
-template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256, ONE ? sizeof(T) == 2 || DK == 64 ? 4 : 3 : 2) void k_chunk(Args a) {
+// registers count.  184 us for 8192 chunks of 128 channels, 0.8 GB of operands written; 132 us for 4096 in the backward pass.
+template <class T, int DK, bool BACK> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 4 : 3) void k_chunk(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32;
   typedef Planes<PI, C, DK> Rows;
   struct Squares { float m[C][FLINE], x[C][FLINE]; };
@@ -343,8 +344,10 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
   Rows &rows = *(Rows *)space;
   auto &m = ((Squares *)space)->m, &x = ((Squares *)space)->x;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q4 = lane >> 4;
-  const int unit = blockIdx.x, kh = unit % a.key_heads, b = unit / a.key_heads % a.batch, c = unit / a.key_heads / a.batch;
-  const int t0 = (a.first + c) * C, len = length_of(a, b), group = ONE ? 1 : a.heads / a.key_heads;
+  const int h = blockIdx.x % a.heads, b = blockIdx.x / a.heads % a.batch, c = blockIdx.x / a.heads / a.batch, sharing = a.heads / a.key_heads, kh = h / sharing;
+  const long long unit = ((long long)c * a.batch + b) * a.key_heads + kh, of = ((long long)c * a.batch + b) * a.heads + h;
+  const bool lays = h % sharing == 0; // the operands, for all heads that share them
+  const int t0 = (a.first + c) * C, len = length_of(a, b);
   if (t0 >= len) return;
   const int t = t0 + 16 * w + r;
   constexpr int SIZE = DK * C * PI; // elements of one operand array of a unit
@@ -356,12 +359,11 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
   };
   // a head's gates, in the first wavefront, whose lanes are the chunk's steps
   const bool on = t0 + lane < len;
-  auto gate = [&](const float *p, int h) { return on ? p[((long long)(t0 + lane) * a.batch + b) * a.heads + h] : 0.f; };
-  float g = w == 0 ? gate(a.g, kh * group) : 0.f, beta = w == 0 ? gate(a.beta, kh * group) : 0.f;
+  auto gate = [&](const float *p) { return on ? p[((long long)(t0 + lane) * a.batch + b) * a.heads + h] : 0.f; };
+  const float g = w == 0 ? gate(a.g) : 0.f, beta = w == 0 ? gate(a.beta) : 0.f;
   ask(a.k, a.ld_k, kr);
   ask(a.q, a.ld_q, qr);
-  auto gates = [&](int h, int lane) {
-    const long long of = ((long long)c * a.batch + b) * a.heads + h;
+  if (w == 0) {
     double G = (double)(g < -1e4f ? -1e4f : g) * 1.4426950408889634; // (minus infinity: forgotten all the same)
 #pragma unroll
     for (int s = 1; s < C; s *= 2) {
@@ -378,14 +380,13 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
     to[C + lane] = tail;
     to[2 * C + lane] = beta;
     if constexpr (BACK) a.sums[of * C + lane] = G;
-  };
-  if (w == 0) gates(kh * group, lane);
+  }
   // rows of steps: to memory as operands, and those of k to LDS
   auto give = [&](const Octet<T> (&o)[KK], Operand<PI> (&f)[KK], __bf16 *to) {
 #pragma unroll
     for (int i = 0; i < KK; ++i) {
       f[i] = o[i].get();
-      leave<PI>(to + (long long)unit * SIZE, w * KK + i, lane, f[i]);
+      if (lays) leave<PI>(to + unit * SIZE, w * KK + i, lane, f[i]);
     }
   };
   auto to_lds = [&](const Operand<PI> (&f)[KK]) {
@@ -400,7 +401,7 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
       for (int p = 0; p < PI; ++p)
 #pragma unroll
         for (int j = 0; j < LANE; ++j) y.p[p][j] = rows.e[p][Rows::place(32 * (f & 1) + 8 * q4 + j, 16 * (f >> 1) + r)];
-      leave<PI>(to + (long long)unit * SIZE, f, lane, y);
+      leave<PI>(to + unit * SIZE, f, lane, y);
     }
   };
   Operand<PI> kf[KK], qf[KK];
@@ -420,136 +421,122 @@ template <class T, int DK, bool BACK, bool ONE> __global__ __launch_bounds__(256
       }
     __builtin_amdgcn_sched_barrier(0);
   }
-  turned(a.ktf);
-  if constexpr (BACK) {
+  if (lays) turned(a.ktf);
+  if (BACK && lays) {
     __syncthreads();
     to_lds(qf);
     __syncthreads();
     turned(a.qtf);
   }
-  const int thread = lane;
-#pragma unroll 1
-  for (int i = 0; i < group; ++i) {
-    // (What depends on the lane alone would be kept for all heads, masks and addresses, in twice the registers: 84 of them without)
-    int lane = thread;
-    asm volatile("" : "+v"(lane));
-    const int r = lane & 15, q4 = lane >> 4, h = kh * group + i;
-    const long long of = ((long long)c * a.batch + b) * a.heads + h;
-    if (w == 0) {
-      if (i) gates(h, lane);
-      if (i + 1 < group) g = gate(a.g, h + 1), beta = gate(a.beta, h + 1);
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = 16 * w + 4 * q4 + e, col = 16 * j + r;
+      float d = 0.f;
+      if (j <= w && col <= row) d = __builtin_amdgcn_exp2f((float)(sum[row] - sum[col]));
+      m[row][col] = col < row ? kk[j][e] * d * rate[col] : 0.f;
+      x[row][col] = col <= row ? qk[j][e] * d * a.scale : 0.f;
     }
-    __syncthreads();
+  __syncthreads();
+  // P diag(beta): its rows of this wavefront's steps
+  Operand<PC> pm[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+  for (int s = 0; s < 2; ++s) {
+    float e[LANE];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = 16 * w + 4 * q4 + e, col = 16 * j + r;
-        float d = 0.f;
-        if (j <= w && col <= row) d = __builtin_amdgcn_exp2f((float)(sum[row] - sum[col]));
-        m[row][col] = col < row ? kk[j][e] * d * rate[col] : 0.f;
-        x[row][col] = col <= row ? qk[j][e] * d * a.scale : 0.f;
-      }
-    __syncthreads();
-    // P diag(beta): its rows of this wavefront's steps
-    Operand<PC> pm[2];
+    for (int j = 0; j < LANE; ++j) e[j] = x[16 * w + r][32 * s + 8 * q4 + j] * rate[32 * s + 8 * q4 + j];
+    pm[s] = operand<PC>(e);
+  }
+  // column r of the inverse of the diagonal's block w: a row of it after the other, the next row of m on its way
+  float y[16];
+  tile now[4] = {}, then[4];
+#pragma unroll
+  for (int n = 0; n < 16; ++n) {
+    if (n < 15)
+#pragma unroll
+      for (int j = 0; j <= n / 4; ++j) then[j] = *(const tile *)&m[16 * w + n + 1][16 * w + 4 * j];
+    float s[4] = {n == r ? 1.f : 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < n; ++j) s[j % 4] = fmaf(-now[j / 4][j % 4], y[j], s[j % 4]);
+    y[n] = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+    for (int j = 0; j <= n / 4; ++j) now[j] = then[j];
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j > w) x[16 * w + 4 * q4 + e][16 * j + r] = 0.f;
+#pragma unroll
+  for (int n = 0; n < 16; ++n)
+    if (n / 4 == q4) x[16 * w + n][16 * w + r] = y[n];
+  __syncthreads();
+  // column w of blocks, from the diagonal down: X_nw = -X_nn sum_j M_nj X_jw.  Four instructions of 16 x 16 with sums over 4 make a product; their sums
+  // are taken over elements e, 4 + e, .. of both operands, so that a result's registers are the next one's operand.
+  tile inv[4] = {};
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    if (n == w)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) inv[n][e] = x[16 * n + 4 * q4 + e][16 * w + r];
+    if (n > w) {
+      tile s = {}, z = {};
+#pragma unroll
+      for (int j = 0; j < n; ++j)
+        if (j >= w) {
+          const tile f = *(const tile *)&m[16 * n + r][16 * j + 4 * q4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(f[e], inv[j][e], s, 0, 0, 0);
+        }
+      const tile f = *(const tile *)&x[16 * n + r][16 * n + 4 * q4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z = __builtin_amdgcn_mfma_f32_16x16x4f32(-f[e], s[e], z, 0, 0, 0);
+      inv[n] = z;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[16 * n + 4 * q4 + e][16 * w + r] = z[e];
+    }
+  }
+  __syncthreads();
+  // A lower triangular matrix in x, or its transpose, times a factor of its rows; blocks of zeros, which nothing reads, are left out
+  auto emit = [&](auto parts, __bf16 *to, bool over, bool scaled) {
+    constexpr int P = decltype(parts)::value;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
+      if (over ? 2 * s + 1 < w : 2 * s > w) continue;
       float e[LANE];
 #pragma unroll
-      for (int j = 0; j < LANE; ++j) e[j] = x[16 * w + r][32 * s + 8 * q4 + j] * rate[32 * s + 8 * q4 + j];
-      pm[s] = operand<PC>(e);
-    }
-    // column r of the inverse of the diagonal's block w: a row of it after the other, the next row of m on its way
-    float y[16];
-    tile now[4] = {}, then[4];
-#pragma unroll
-    for (int n = 0; n < 16; ++n) {
-      if (n < 15)
-#pragma unroll
-        for (int j = 0; j <= n / 4; ++j) then[j] = *(const tile *)&m[16 * w + n + 1][16 * w + 4 * j];
-      float s[4] = {n == r ? 1.f : 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < n; ++j) s[j % 4] = fmaf(-now[j / 4][j % 4], y[j], s[j % 4]);
-      y[n] = (s[0] + s[1]) + (s[2] + s[3]);
-#pragma unroll
-      for (int j = 0; j <= n / 4; ++j) now[j] = then[j];
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (j > w) x[16 * w + 4 * q4 + e][16 * j + r] = 0.f;
-#pragma unroll
-    for (int n = 0; n < 16; ++n)
-      if (n / 4 == q4) x[16 * w + n][16 * w + r] = y[n];
-    __syncthreads();
-    // column w of blocks, from the diagonal down: X_nw = -X_nn sum_j M_nj X_jw.  Four instructions of 16 x 16 with sums over 4 make a product; their sums
-    // are taken over elements e, 4 + e, .. of both operands, so that a result's registers are the next one's operand.
-    tile inv[4] = {};
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      if (n == w)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) inv[n][e] = x[16 * n + 4 * q4 + e][16 * w + r];
-      if (n > w) {
-        tile s = {}, z = {};
-#pragma unroll
-        for (int j = 0; j < n; ++j)
-          if (j >= w) {
-            const tile f = *(const tile *)&m[16 * n + r][16 * j + 4 * q4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(f[e], inv[j][e], s, 0, 0, 0);
-          }
-        const tile f = *(const tile *)&x[16 * n + r][16 * n + 4 * q4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z = __builtin_amdgcn_mfma_f32_16x16x4f32(-f[e], s[e], z, 0, 0, 0);
-        inv[n] = z;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[16 * n + 4 * q4 + e][16 * w + r] = z[e];
+      for (int j = 0; j < LANE; ++j) {
+        const int k = 32 * s + 8 * q4 + j;
+        e[j] = (over ? x[k][16 * w + r] : x[16 * w + r][k]) * (scaled ? left[over ? k : 16 * w + r] : 1.f);
       }
+      leave<P>(to + of * (C * C * P), 2 * w + s, lane, operand<P>(e));
     }
-    __syncthreads();
-    // A lower triangular matrix in x, or its transpose, times a factor of its rows; blocks of zeros, which nothing reads, are left out
-    auto emit = [&](auto parts, __bf16 *to, bool over, bool scaled) {
-      constexpr int P = decltype(parts)::value;
+  };
+  emit(std::integral_constant<int, PC>(), a.af, false, !BACK);
+  if constexpr (BACK) emit(std::integral_constant<int, PC>(), a.at, true, true);
+  tile product[4] = {};
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        if (over ? 2 * s + 1 < w : 2 * s > w) continue;
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+      if (n <= w && 2 * s <= w && 2 * s + 1 >= n) {
         float e[LANE];
 #pragma unroll
-        for (int j = 0; j < LANE; ++j) {
-          const int k = 32 * s + 8 * q4 + j;
-          e[j] = (over ? x[k][16 * w + r] : x[16 * w + r][k]) * (scaled ? left[over ? k : 16 * w + r] : 1.f);
-        }
-        leave<P>(to + of * (C * C * P), 2 * w + s, lane, operand<P>(e));
+        for (int j = 0; j < LANE; ++j) e[j] = x[32 * s + 8 * q4 + j][16 * n + r];
+        multiply(product[n], pm[s], operand<PC>(e));
       }
-    };
-    emit(std::integral_constant<int, PC>(), a.af, false, !BACK);
-    if constexpr (BACK) emit(std::integral_constant<int, PC>(), a.at, true, true);
-    tile product[4] = {};
+  __syncthreads();
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+  for (int n = 0; n < 4; ++n)
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-        if (n <= w && 2 * s <= w && 2 * s + 1 >= n) {
-          float e[LANE];
-#pragma unroll
-          for (int j = 0; j < LANE; ++j) e[j] = x[32 * s + 8 * q4 + j][16 * n + r];
-          multiply(product[n], pm[s], operand<PC>(e));
-        }
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < 4; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[16 * w + 4 * q4 + e][16 * n + r] = product[n][e];
-    __syncthreads();
-    if constexpr (BACK) emit(std::integral_constant<int, PC>(), a.bt, true, false);
-    else emit(std::integral_constant<int, LAST<T>>(), a.bf, false, false);
-    __syncthreads();
-  }
+    for (int e = 0; e < 4; ++e) x[16 * w + 4 * q4 + e][16 * n + r] = product[n][e];
+  __syncthreads();
+  if constexpr (BACK) emit(std::integral_constant<int, PC>(), a.bt, true, false);
+  else emit(std::integral_constant<int, LAST<T>>(), a.bf, false, false);
 }
 
 // ---- the walk over the chunks -------------------------------------------------------------------
@@ -1406,8 +1393,7 @@ template <class T, int DK> hipError_t forward(Plan &p, hipStream_t s) {
     a.chunks = p.all - first < p.chunks ? p.all - first : p.chunks;
     a.from = from;
     a.to = first + a.chunks < p.all ? carry : p.last;
-    if (a.heads == a.key_heads) k_chunk<T, DK, false, true><<<a.chunks * p.units, 256, 0, s>>>(a);
-    else k_chunk<T, DK, false, false><<<a.chunks * p.units, 256, 0, s>>>(a);
+    k_chunk<T, DK, false><<<a.chunks * p.per, 256, 0, s>>>(a);
     cut(a, p);
     if (a.segments > 1) {
       k_walk<T, DK, 16, MAPS><<<(a.segments - 1) * p.per * (p.blocks + DK / 16), 256, 0, s>>>(a);
@@ -1436,8 +1422,7 @@ template <class T, int DK> hipError_t backward(Plan &p, const float *kept, const
   for (int first = (p.all - 1) / p.chunks * p.chunks; first >= 0; first -= p.chunks) {
     a.first = first;
     a.chunks = p.all - first < p.chunks ? p.all - first : p.chunks;
-    if (a.heads == a.key_heads) k_chunk<T, DK, true, true><<<a.chunks * p.units, 256, 0, s>>>(a);
-    else k_chunk<T, DK, true, false><<<a.chunks * p.units, 256, 0, s>>>(a);
+    k_chunk<T, DK, true><<<a.chunks * p.per, 256, 0, s>>>(a);
     a.from = kept;
     a.to = nullptr;
     a.length = KEPT;
