@@ -920,7 +920,7 @@ template <int DK, bool BACK> __global__ __launch_bounds__(256) void k_join(Args 
 }
 
 // ---- gradients of a chunk's queries, keys and gates -----------------------------------------------
-// Sums over the state's columns go through LDS 32 at a time, the next ones on their way; results are [dk][t], so that a lane has four elements of one step's
+// Sums over the state's columns go through LDS 32 at a time, in two places in turn, the next ones on their way; results are [dk][t], so that a lane has four elements of one step's
 // row.  Eight wavefronts: four take 16 steps each, with one half of the channels, and of the chunk's steps before theirs, four with the other.
 // What bounds it: 44 MFLOP a chunk of 128 x 128, six instructions to a product of what is computed on the way, at 0.48 PFLOP/s: one workgroup of 190 registers
 // to a compute unit, so that few wavefronts cover the time from LDS.  378 us for 4096 chunks; with 128 registers and two workgroups values spill, and it is slower.
@@ -929,11 +929,11 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
   struct Sums { Planes<PC, DK, 32> before, after; Planes<PC, C, 32> w; };
   struct Rows { Planes<PI, C, DK> q, k; };
   struct Squares { float dp[C][FLINE], m[C][FLINE]; };
-  constexpr size_t FIRST = sizeof(Sums) > sizeof(Squares) ? sizeof(Sums) : sizeof(Squares);
+  constexpr size_t FIRST = 2 * sizeof(Sums) > sizeof(Squares) ? 2 * sizeof(Sums) : sizeof(Squares);
   __shared__ __align__(16) char space[sizeof(Rows) > FIRST ? sizeof(Rows) : FIRST];
   __shared__ float of_col[4][C], of_row[3][2][C], of_all[8], gates[3][C];
   __shared__ double G[C];
-  Sums &sums = *(Sums *)space;
+  Sums *const sums = (Sums *)space; // two, one of which is read while the other is written
   Rows &rows = *(Rows *)space;
   Squares &squares = *(Squares *)space;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3, half = wave >> 2, r = lane & 15, q4 = lane >> 4;
@@ -971,39 +971,40 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
     ask(0);
     tile sq[NT] = {}, se[NT] = {}, su[NT] = {}, p[2] = {}, x[2] = {};
     float both = 0.f; // <S, dS'>
-    for (int v = 0; v < a.dvp; v += 32) {
-      lds_barrier();
-      if (v == 0) { // (every wavefront is through with the last head's)
-        if (threadIdx.x < 3 * C) gates[threadIdx.x / C][threadIdx.x % C] = gate;
-        if (threadIdx.x < C) G[threadIdx.x] = sum;
-      }
+    Operand<PI> d;
+    Operand<PC> e;
+    auto stage = [&](Sums &to) {
       float y[LANE], z[LANE];
-      auto to_lds = [&](const float (&from)[LANE], auto &planes, int row) {
-        planes.put(row, scol, operand<PC>(from));
-      };
       if (threadIdx.x < 4 * DK) {
         rb.get(y);
         ra.get(z);
 #pragma unroll
         for (int j = 0; j < LANE; ++j) both = fmaf(y[j], z[j], both);
-        to_lds(y, sums.before, srow);
-        to_lds(z, sums.after, srow);
+        to.before.put(srow, scol, operand<PC>(y));
+        to.after.put(srow, scol, operand<PC>(z));
       }
       if (threadIdx.x < 4 * C) {
         rw.get(y);
-        to_lds(y, sums.w, srow);
+        to.w.put(srow, scol, operand<PC>(y));
       }
       rd.get(y);
-      const Operand<PI> d = operand<PI>(y);
+      d = operand<PI>(y);
       re.get(y);
-      const Operand<PC> e = operand<PC>(y);
-      if (v + 32 < a.dvp) ask(v + 32);
+      e = operand<PC>(y);
+    };
+    lds_barrier(); // (every wavefront is through with the last head)
+    if (threadIdx.x < 3 * C) gates[threadIdx.x / C][threadIdx.x % C] = gate;
+    if (threadIdx.x < C) G[threadIdx.x] = sum;
+    stage(sums[0]);
+    if (32 < a.dvp) ask(32);
+    for (int v = 0, turn = 0; v < a.dvp; v += 32, turn ^= 1) {
       lds_barrier();
-      const Operand<PC> wm = sums.w.get(mine, 8 * q4);
+      const Sums &now = sums[turn];
+      const Operand<PC> wm = now.w.get(mine, 8 * q4);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const int row = 16 * (half * NT + n) + r;
-        const Operand<PC> s = sums.before.get(row, 8 * q4), s2 = sums.after.get(row, 8 * q4);
+        const Operand<PC> s = now.before.get(row, 8 * q4), s2 = now.after.get(row, 8 * q4);
         multiply(sq[n], s, d);
         multiply(se[n], s, e);
         multiply(su[n], s2, wm);
@@ -1011,10 +1012,14 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
 #pragma unroll
       for (int j = 0; j < 2; ++j)
         if (2 * half + j <= w) {
-          const Operand<PC> y = sums.w.get(16 * (2 * half + j) + r, 8 * q4);
+          const Operand<PC> y = now.w.get(16 * (2 * half + j) + r, 8 * q4);
           multiply(p[j], d, y);
           multiply(x[j], e, y);
         }
+      if (v + 32 < a.dvp) {
+        stage(sums[turn ^ 1]);
+        if (v + 64 < a.dvp) ask(v + 64);
+      }
     }
     // queries and keys of the chunk: what its steps are to each other, and each step's with what came from the states
     {
