@@ -19,7 +19,7 @@
 // blocks of 16, in 32 bits, and by products of blocks, so that equal keys do no harm.
 // States and sums are of 32 bits.  Products go through the bf16 matrix cores: arrays of bf16 as they are, those of 32 bits in three bf16 parts, and what is
 // computed on the way (S, E, u, dE, A, B) in three too, 24 bits of it: six products of two such operands, three of one beside a bf16 array.
-// (Two parts would leave 16 bits.  With those, forward 4096 x 8 x 16 x 128 x 128 took 407 us instead of 486 and backward 1638 instead of 1832, but states
+// (Two parts would leave 16 bits.  With those, forward 4096 x 8 x 16 x 128 x 128 took 407 us instead of 490 and backward 1638 instead of 1832, but states
 // were off by up to 7e-6 of their norm and gradients of gates by 2e-5.)  Where nothing but a result in bf16 comes of a product, o and the products of the
 // chunk's own steps in dq and dk, two parts are enough: 2^-17 of each factor, beside 2^-8 of the result.
 //
@@ -29,7 +29,7 @@
 // states found by the segments' maps, S' = M S + c (k_join).  They go through the sequence in pieces of 2 GB of
 // intermediate arrays.  Few steps are taken one after the other, by a kernel whose workgroup holds the whole state of a head (k_steps).
 //
-// At 4096 x 8 x 16 x 128 x 128 in bf16 forward takes 486 us and backward 1832 (memory alone would take 135 and 240): what a chunk's steps need of each other, and a chunk
+// At 4096 x 8 x 16 x 128 x 128 in bf16 forward takes 490 us and backward 1819 (memory alone would take 135 and 240): what a chunk's steps need of each other, and a chunk
 // of the one before, keeps the matrix cores waiting.
 #include "snn_rows.h"
 
@@ -922,8 +922,8 @@ template <int DK, bool BACK> __global__ __launch_bounds__(256) void k_join(Args 
 // ---- gradients of a chunk's queries, keys and gates -----------------------------------------------
 // Sums over the state's columns go through LDS 32 at a time, in two places in turn, the next ones on their way; results are [dk][t], so that a lane has four elements of one step's
 // row.  Eight wavefronts: four take 16 steps each, with one half of the channels, and of the chunk's steps before theirs, four with the other.
-// What bounds it: 44 MFLOP a chunk of 128 x 128, six instructions to a product of what is computed on the way, at 0.48 PFLOP/s: one workgroup of 190 registers
-// to a compute unit, so that few wavefronts cover the time from LDS.  378 us for 4096 chunks; with 128 registers and two workgroups values spill, and it is slower.
+// What bounds it: 44 MFLOP a chunk of 128 x 128, six instructions to a product of what is computed on the way, at 0.49 PFLOP/s: one workgroup of 210 registers
+// to a compute unit, so that few wavefronts cover the times from memory and LDS.  370 us for 4096 chunks; with 128 registers and two workgroups values spill, and it is slower.
 template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k_grads(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE, PO = LAST<T>, KK = DK / 32, NT = DK / 32; // NT: tiles of a half of the channels
   struct Sums { Planes<PC, DK, 32> before, after; Planes<PC, C, 32> w; };

@@ -580,6 +580,24 @@ def test_delta_state_in_place_is_a_sequence_cut_anywhere(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("T", [1, 100, 1800])
+def test_delta_states_in_place(T):
+    x, s0, do, ds, lengths = delta_inputs(T, 2, 4, 2, 40, 70, torch.float32, ragged=True, seed=6)
+    state = s0.clone()
+    got, want = snn.snn_delta_forward(*x, state, lengths=lengths, s_last=state), snn.snn_delta_forward(*x, s0, lengths=lengths, keep=True)
+    assert got[1] is state and same(got[:2], want[:2])
+    # ds0 in the place of ds_last, by the C entry point
+    grads = snn.snn_delta_backward(*x, want[2], do, ds, lengths=lengths)
+    p = ops.snn_delta(T, 2, 4, 2, 40, 70, ops.SNN_F32, 40 ** -0.5, lengths=lengths.data_ptr())
+    at, space = ops._launch(ds.device, snn.lib().snn_delta_workspace(C.byref(p), 1))
+    out, d = [torch.empty_like(y) for y in grads[:5]], ds.clone()
+    q, k, v, g, beta = (y.data_ptr() for y in x)
+    assert snn.lib().snn_delta_backward(C.byref(at), C.byref(p), q, k, v, g, beta, want[2].data_ptr(), do.data_ptr(), d.data_ptr(),
+                                        *[y.data_ptr() for y in out], d.data_ptr()) == 0
+    assert same([*out, d], grads)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T", [5, 150])
 def test_delta_parts_of_a_projection(T, dtype):
@@ -653,7 +671,7 @@ def test_delta_gates_at_their_ends(dtype):
 
 
 @gpu
-@pytest.mark.parametrize("T", [4, 90])
+@pytest.mark.parametrize("T", [4, 90, 2000])
 def test_delta_values_that_are_not_finite_stay_in_their_heads(T):
     x, s0, do, ds, _ = delta_inputs(T, 3, 4, 2, 20, 30, torch.float32, seed=9)
     want = snn.snn_delta_forward(*x, s0, keep=True)
@@ -759,7 +777,7 @@ def test_delta_beyond_4_gb():
 
 
 @gpu
-@pytest.mark.parametrize("T", [1, 100])
+@pytest.mark.parametrize("T", [1, 100, 1600])
 def test_delta_in_a_graph(T):
     x, s0, do, ds, lengths = delta_inputs(T, 3, 4, 2, 40, 50, torch.bfloat16, ragged=T > 1, seed=11)
     state = s0.clone()
