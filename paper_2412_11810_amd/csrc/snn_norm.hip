@@ -3,14 +3,14 @@
 //   s = x + residual (or x);  i = 1 / sqrt(mean(s^2) + eps);  y = w s i
 //   c = mean(w dy s i);  dx = i (w dy - s i c) + dtotal;  dw = sum over rows of dy s i
 //
-// A row is read once and stays in registers: lanes take 8 elements at a time, rows of up to 512 elements share a wavefront with others, those of up
-// to 2048 have one of their own, longer ones a workgroup of 4 or 16.  s is rounded to the arrays' type where it is written; y comes from the sum before that.
+// A row is read once and stays in registers: lanes take 8 elements at a time, rows of up to 256 elements share a wavefront with others, longer ones
+// have one of their own or a workgroup of 4 or 16.  s is rounded to the arrays' type where it is written; y comes from the sum before that.
 // Into 8 bits y goes without a rounding to bf16 first: its blocks are those of snn_pack (four lanes).
 // Sums of squares are of 32 bits; where one is too large or too small for that, the row is multiplied by a power of two first.
 // dw: a workgroup sums over its rows in registers and leaves one row of sums; a second kernel adds those up.  No atomics, so the same bits each time.
 //
 // What bounds it: memory.  32768 rows of 4096 in bf16: backward 200 us, 5.4 TB/s, and 11 us for dw's rows of sums; forward with residual and total into 8 bits
-// 182 us, 5.2 TB/s.  Few rows are bound by the call: 64 of 2048 take 11 us, 6 of them in the kernel.
+// 182 us, 5.2 TB/s.  Few rows are bound by the call: 64 of 2048 take 11 us, 3 of them in the kernel.
 #include "snn_rows.h"
 
 namespace {
@@ -259,32 +259,43 @@ template <class T> __global__ __launch_bounds__(256) void k_norm_dw(int count, i
 }
 
 // How rows of n elements are dealt to lanes
+constexpr long long MOST_FORWARD = 1 << 20, MOST_BACK = 1024; // workgroups
 struct Plan {
   int waves, vectors, lanes;
   unsigned groups; // workgroups
-  Plan(long long rows, int n, unsigned most) {
+  Plan(long long rows, int n, bool bf16, bool back) {
     const int need = (n + LANE - 1) / LANE;
-    waves = need <= 256 ? 1 : need <= 1024 ? 4 : 16; // (n is 2^15 at most: four vectors of a lane)
+    // A workgroup has a row of more than 2048 elements (n is 2^15 at most: four vectors of a lane), and a shorter one where a wavefront would need four vectors, which
+    // takes registers, or two and rows are few.  A wavefront and a workgroup to a row, us in a graph: 64 rows of 2048 in bf16 forward 5.1 and 2.8, 16384 rows
+    // 53 and 47, backward 87 and 53; 4329 rows of 1501 in fp32 19.6 and 18.3, 33.4 and 28.6; but many rows in bf16 that leave lanes without elements or
+    // begin between words, forward, 16384 of 1500 45 and 68, of 1930 53 and 62.  Of 1024 in bf16 64 rows forward 3.6 and 2.8, 4329 rows 8.3 and 9.7; backward
+    // 64 rows 6.4 and 5.1, 256 rows 6.6 and 7.4.
+    const bool wide = need > 128 ? back || !bf16 || rows <= 2048 || (need > 240 && n % LANE == 0) : need > 64 && rows <= (back ? 128 : 1024);
+    waves = need <= 256 && !wide ? 1 : need <= 1024 ? 4 : 16;
     lanes = 4;
     while (lanes < need && lanes < 64) lanes *= 2;
     const int of_row = waves == 1 ? lanes : 64 * waves;
     vectors = 1;
     while (vectors * of_row < need) vectors *= 2;
     const int at_once = waves == 1 ? 256 / lanes : 1;
-    const long long all = (rows + at_once - 1) / at_once;
+    // (Backward a workgroup has four rows at least, where that leaves one for each compute unit: dw's rows of sums are fewer.  1024 rows of 2048 in bf16 13 us instead
+    // of 20, of 4096 18 instead of 24)
+    const long long all = (rows + at_once - 1) / at_once, four = waves == 1 ? all : rows / 4 > 256 ? rows / 4 : 256;
+    const long long most = !back ? MOST_FORWARD : four < MOST_BACK ? four : MOST_BACK;
     groups = (unsigned)(all < most ? all : most);
     if (!groups) groups = 1;
   }
 };
-constexpr unsigned MOST_FORWARD = 1 << 20, MOST_BACK = 1024;
 
-template <class F> hipError_t with_plan(const Plan &p, F f) {
+// MOST: vectors of a lane where a row has a wavefront
+template <int MOST, class F> hipError_t with_plan(const Plan &p, F f) {
   auto v = [&](auto waves) {
-    switch (p.vectors) {
-    case 1: f(waves, std::integral_constant<int, 1>()); break;
-    case 2: f(waves, std::integral_constant<int, 2>()); break;
-    default: f(waves, std::integral_constant<int, 4>()); break;
-    }
+    constexpr int W = decltype(waves)::value;
+    if constexpr (W < 16)
+      if (p.vectors == 1) return f(waves, std::integral_constant<int, 1>());
+    if constexpr (W > 1 || MOST > 2)
+      if (p.vectors == 4) return f(waves, std::integral_constant<int, 4>());
+    f(waves, std::integral_constant<int, 2>());
   };
   if (p.waves == 1) v(std::integral_constant<int, 1>());
   else if (p.waves == 4) v(std::integral_constant<int, 4>());
@@ -293,20 +304,20 @@ template <class F> hipError_t with_plan(const Plan &p, F f) {
 }
 
 template <class T> hipError_t forward(const Args &a, hipStream_t s) {
-  const Plan p(a.rows, a.n, MOST_FORWARD);
+  const Plan p(a.rows, a.n, sizeof(T) == 2, false);
   Args b = a;
   b.lanes = p.lanes;
-  return with_plan(p, [&](auto waves, auto v) {
+  return with_plan<sizeof(T) == 2 ? 4 : 2>(p, [&](auto waves, auto v) {
     constexpr int W = decltype(waves)::value, V = decltype(v)::value;
     if (b.codes) k_norm<T, W, V, true><<<p.groups, W == 16 ? 1024 : 256, 0, s>>>(b);
     else k_norm<T, W, V, false><<<p.groups, W == 16 ? 1024 : 256, 0, s>>>(b);
   });
 }
 template <class T> hipError_t backward(const Args &a, void *dw, hipStream_t s) {
-  const Plan p(a.rows, a.n, MOST_BACK);
+  const Plan p(a.rows, a.n, sizeof(T) == 2, true);
   Args b = a;
   b.lanes = p.lanes;
-  const hipError_t e = with_plan(p, [&](auto waves, auto v) {
+  const hipError_t e = with_plan<2>(p, [&](auto waves, auto v) {
     constexpr int W = decltype(waves)::value, V = decltype(v)::value;
     k_norm_back<T, W, V><<<p.groups, W == 16 ? 1024 : 256, 0, s>>>(b);
   });
@@ -317,7 +328,7 @@ template <class T> hipError_t backward(const Args &a, void *dw, hipStream_t s) {
 
 } // namespace
 
-size_t norm_workspace(const NormShape &p) { return sizeof(float) * Plan(p.rows, p.n, MOST_BACK).groups * p.n; }
+size_t norm_workspace(const NormShape &p) { return sizeof(float) * Plan(p.rows, p.n, p.bf16, true).groups * p.n; }
 
 hipError_t launch_norm(const NormShape &p, const void *x, const void *residual, const void *w, void *total, void *y, int8_t *codes, uint8_t *exps,
                        hipStream_t s) {

@@ -43,7 +43,7 @@ def rows_of(shape, dtype, seed, wide=0, spread=0.5):
 
 
 # ---- norm ---------------------------------------------------------------------------------------
-NORM = [(1, 1), (3, 2), (5, 8), (70, 31), (64, 64), (9, 75), (1000, 128), (3, 500), (33, 513), (7, 1024), (5, 1501), (64, 2048), (3, 2049), (4, 4096),
+NORM = [(1, 1), (2200, 2000), (130, 1000), (1030, 600), (3, 2), (5, 8), (70, 31), (64, 64), (9, 75), (1000, 128), (3, 500), (33, 513), (7, 1024), (5, 1501), (64, 2048), (3, 2049), (4, 4096),
         (2, 8191), (3, 8200), (2, 16385), (1, 32768), (5000, 40), (2100, 1100)]
 ROUNDINGS = 64  # of a sum over a row: 32 elements in a lane, 6 exchanges, 16 wavefronts, and the square root, the quotient and three products
 
