@@ -379,8 +379,8 @@ snn_status snn_vocab_loss_grad(const snn_launch *at, const snn_vocab *p, const v
  *   S_t = a_t S_{t-1} + k_t u_t^T ,  u_t = beta_t (v_t - a_t S_{t-1}^T k_t) ,  o_t = scale S_t^T q_t ,  a_t = exp(g_t) ,  t = 1..T
  * (k_t reads what the state holds for it, and beta_t of the difference to v_t is written in its place.)  Keys are taken as they are: with |k| = 1 and
  * beta 0..1 the state stays bounded; g <= 0 as a rule, minus infinity forgets all (as -10^4 does).  Computed in fp32, sums over a
- * sequence's gates in fp64; what goes through the matrix cores keeps 24 bits, but for 16 of the factors of a result in bf16.  Where a state, key,
- * value or gate is not finite, its head's results need not be from its chunk of 64 steps on, and no gradient of the head; other heads are not touched, but for the
+ * sequence's gates in fp64; what goes through the matrix cores keeps 24 bits.  Where a state, key, value or gate is not
+ * finite, its head's results need not be from its chunk of 64 steps on, and no gradient of the head; other heads are not touched, but for the
  * gradients of queries and keys that they share with it.  The same holds where keys or gates would let a state grow beyond 32 bits, also if it is 0. */
 typedef struct {
   int32_t T, batch;          /* T >= 0 (0: s_last = s0), at most 2^30 */

@@ -19,9 +19,9 @@
 // blocks of 16, in 32 bits, and by products of blocks, so that equal keys do no harm.
 // States and sums are of 32 bits.  Products go through the bf16 matrix cores: arrays of bf16 as they are, those of 32 bits in three bf16 parts, and what is
 // computed on the way (S, E, u, dE, A, B) in three too, 24 bits of it: six products of two such operands, three of one beside a bf16 array.
-// (Two parts would leave 16 bits.  With those, forward 4096 x 8 x 16 x 128 x 128 took 407 us instead of 490 and backward 1638 instead of 1832, but states
-// were off by up to 7e-6 of their norm and gradients of gates by 2e-5.)  Where nothing but a result in bf16 comes of a product, o and the products of the
-// chunk's own steps in dq and dk, two parts are enough: 2^-17 of each factor, beside 2^-8 of the result.
+// (Two parts would leave 16 bits.  With those, forward 4096 x 8 x 16 x 128 x 128 took 407 us instead of 514 and backward 1638 instead of 1838, but states
+// were off by up to 7e-6 of their norm and gradients of gates by 2e-5.  Where nothing but a result in bf16 comes of a product they are not enough either:
+// o is the difference of what the state held and what is written in its place, each of which may be thousands of times as large.)
 //
 // The kernels: what is of a chunk alone (k_chunk: A, B, and the operands in the order in which a wavefront loads them); the walk over the chunks
 // with S in registers, its columns dealt to workgroups (k_walk; for the backward pass it starts at each kept state, every 4 chunks); the walk back
@@ -46,7 +46,6 @@ constexpr float LOG2E = 1.44269504f;
 
 template <class T> constexpr int GIVEN = sizeof(T) == 2 ? 1 : 3; // parts of what the caller's arrays hold
 constexpr int MADE = 3;                                    // of what is computed
-template <class T> constexpr int LAST = sizeof(T) == 2 ? 2 : 3; // and of that, where nothing but a result in the arrays' type comes from it
 
 struct Args {
   const void *q, *k, *v, *dout;
@@ -85,13 +84,6 @@ template <int PA, int PB> __device__ __forceinline__ void multiply(tile &acc, co
 #pragma unroll
     for (int i = 0; i <= s; ++i)
       if (i < PA && s - i < PB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], acc, 0, 0, 0);
-}
-// The first parts of operands
-template <int P, int PA, int N> __device__ __forceinline__ void first_parts(const Operand<PA> (&a)[N], Operand<P> (&r)[N]) {
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-#pragma unroll
-    for (int i = 0; i < P; ++i) r[n].p[i] = a[n].p[i];
 }
 // Several columns' products in turn: none waits for the one before
 template <int PA, int PB, int N> __device__ __forceinline__ void multiply(tile (&acc)[N], const Operand<PA> &a, const Operand<PB> (&b)[N]) {
@@ -502,8 +494,7 @@ template <class T, int DK, bool BACK> __global__ __launch_bounds__(256, sizeof(T
   }
   __syncthreads();
   // A lower triangular matrix in x, or its transpose, times a factor of its rows; blocks of zeros, which nothing reads, are left out
-  auto emit = [&](auto parts, __bf16 *to, bool over, bool scaled) {
-    constexpr int P = decltype(parts)::value;
+  auto emit = [&](__bf16 *to, bool over, bool scaled) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       if (over ? 2 * s + 1 < w : 2 * s > w) continue;
@@ -513,11 +504,11 @@ template <class T, int DK, bool BACK> __global__ __launch_bounds__(256, sizeof(T
         const int k = 32 * s + 8 * q4 + j;
         e[j] = (over ? x[k][16 * w + r] : x[16 * w + r][k]) * (scaled ? left[over ? k : 16 * w + r] : 1.f);
       }
-      leave<P>(to + of * (C * C * P), 2 * w + s, lane, operand<P>(e));
+      leave<PC>(to + of * (C * C * PC), 2 * w + s, lane, operand<PC>(e));
     }
   };
-  emit(std::integral_constant<int, PC>(), a.af, false, !BACK);
-  if constexpr (BACK) emit(std::integral_constant<int, PC>(), a.at, true, true);
+  emit(a.af, false, !BACK);
+  if constexpr (BACK) emit(a.at, true, true);
   tile product[4] = {};
 #pragma unroll
   for (int n = 0; n < 4; ++n)
@@ -535,8 +526,8 @@ template <class T, int DK, bool BACK> __global__ __launch_bounds__(256, sizeof(T
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[16 * w + 4 * q4 + e][16 * n + r] = product[n][e];
   __syncthreads();
-  if constexpr (BACK) emit(std::integral_constant<int, PC>(), a.bt, true, false);
-  else emit(std::integral_constant<int, LAST<T>>(), a.bf, false, false);
+  if constexpr (BACK) emit(a.bt, true, false);
+  else emit(a.bf, false, false);
 }
 
 // ---- the walk over the chunks -------------------------------------------------------------------
@@ -563,7 +554,7 @@ template <int RT, int NT> __device__ __forceinline__ void identity(int row, int 
 }
 template <class T, int DK, int BV, Walk HOW> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk(Args a) {
   constexpr bool REC = HOW == AGAIN, OUT = HOW == WALK;
-  constexpr int PI = GIVEN<T>, PC = MADE, PO = LAST<T>, KK = DK / 32, RT = DK / 64, NT = BV / 16;
+  constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32, RT = DK / 64, NT = BV / 16;
   __shared__ __align__(16) Planes<PC, BV, DK> st;
   __shared__ __align__(16) Planes<PC, BV, C> et, wt;
   __shared__ __align__(16) char strips[4][REC && Strip<float, BV>::BYTES > Strip<T, BV>::BYTES ? Strip<float, BV>::BYTES : Strip<T, BV>::BYTES];
@@ -584,8 +575,7 @@ template <class T, int DK, int BV, Walk HOW> __global__ __launch_bounds__(256, s
   const int row0 = 16 * w + 4 * q4;
   // What the next chunk needs is on its way while this one is worked on: each part is asked for as soon as this chunk's has been used.
   Operand<PI> k[KK], q[OUT ? KK : 1], kt[RT][2];
-  Operand<PC> am[2];
-  Operand<PO> bm[2];
+  Operand<PC> am[2], bm[2];
   Strip<T, BV> v;
   char *const strip = strips[w];
   tile gam, left; // left: gam_end / gam beta
@@ -605,10 +595,9 @@ template <class T, int DK, int BV, Walk HOW> __global__ __launch_bounds__(256, s
     const int t0 = (a.first + c) * C;
     v.ask((const T *)a.v + ((long long)t0 * a.batch + b) * a.ld_v + h * a.dv + v0, step_v, 16 * w, lane, place_of(t0));
   };
-  auto ask_squares = [&](const __bf16 *p, int c, auto &m) { // (lower triangular: the first two rows of blocks have zeros behind)
-    constexpr int P = sizeof(m[0].p) / sizeof(frag);
-    m[0] = fetch<P>(p + of_head(c) * (C * C * P), 2 * w, lane);
-    if (w > 1) m[1] = fetch<P>(p + of_head(c) * (C * C * P), 2 * w + 1, lane);
+  auto ask_squares = [&](const __bf16 *p, int c, Operand<PC> (&m)[2]) { // (lower triangular: the first two rows of blocks have zeros behind)
+    m[0] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w, lane);
+    if (w > 1) m[1] = fetch<PC>(p + of_head(c) * (C * C * PC), 2 * w + 1, lane);
   };
   auto ask_columns = [&](int c) {
 #pragma unroll
@@ -652,11 +641,7 @@ template <class T, int DK, int BV, Walk HOW> __global__ __launch_bounds__(256, s
       Operand<PC> y[NT];
       st.get(r, 32 * i + 8 * q4, y);
       multiply(e, k[i], y);
-      if constexpr (OUT) {
-        Operand<PO> z[NT];
-        first_parts(y, z);
-        multiply(o, q[i], z);
-      }
+      if constexpr (OUT) multiply(o, q[i], y);
     }
     ask_rows(next);
     const Place place = place_of(t0);
@@ -680,11 +665,7 @@ template <class T, int DK, int BV, Walk HOW> __global__ __launch_bounds__(256, s
         Operand<PC> y[NT];
         et.get(r, 32 * j + 8 * q4, y);
         multiply(x, am[j], y);
-        if constexpr (OUT) {
-          Operand<PO> z[NT];
-          first_parts(y, z);
-          multiply(o, bm[j], z);
-        }
+        if constexpr (OUT) multiply(o, bm[j], y);
       }
     ask_squares(a.af, next, am);
     if constexpr (OUT) ask_squares(a.bf, next, bm);
@@ -925,7 +906,7 @@ template <int DK, bool BACK> __global__ __launch_bounds__(256) void k_join(Args 
 // What bounds it: 44 MFLOP a chunk of 128 x 128, six instructions to a product of what is computed on the way, at 0.49 PFLOP/s: one workgroup of 210 registers
 // to a compute unit, so that few wavefronts cover the times from memory and LDS.  370 us for 4096 chunks; with 128 registers and two workgroups values spill, and it is slower.
 template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k_grads(Args a) {
-  constexpr int PI = GIVEN<T>, PC = MADE, PO = LAST<T>, KK = DK / 32, NT = DK / 32; // NT: tiles of a half of the channels
+  constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32, NT = DK / 32; // NT: tiles of a half of the channels
   struct Sums { Planes<PC, DK, 32> before, after; Planes<PC, C, 32> w; };
   struct Rows { Planes<PI, C, DK> q, k; };
   struct Squares { float dp[C][FLINE], m[C][FLINE]; };
@@ -1128,13 +1109,13 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
       float y[LANE];
 #pragma unroll
       for (int j = 0; j < LANE; ++j) y[j] = squares.dp[mine][32 * s + 8 * q4 + j];
-      const Operand<PO> dpf = operand<PO>(y);
+      const Operand<PC> dpf = operand<PC>(y);
 #pragma unroll
       for (int j = 0; j < LANE; ++j) y[j] = squares.dp[32 * s + 8 * q4 + j][mine];
-      const Operand<PO> dpt = operand<PO>(y);
+      const Operand<PC> dpt = operand<PC>(y);
 #pragma unroll
       for (int j = 0; j < LANE; ++j) y[j] = squares.m[mine][32 * s + 8 * q4 + j];
-      const Operand<PO> m = operand<PO>(y);
+      const Operand<PC> m = operand<PC>(y);
       if constexpr (PI > 1) columns(s);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -1339,7 +1320,7 @@ struct Plan {
     bv = columns(p, back);
     blocks = (dvp + bv - 1) / bv;
     all = (p.T + C - 1) / C;
-    const size_t pi = p.bf16 ? 1 : 3, pc = MADE, po = p.bf16 ? LAST<__bf16> : LAST<float>;
+    const size_t pi = p.bf16 ? 1 : 3, pc = MADE;
     auto lay = [&](int n, int segments) {
       size_t at = 0;
       auto take = [&](auto *&to, size_t count) {
@@ -1355,7 +1336,7 @@ struct Plan {
       for (__bf16 **x : {&a.kf, &a.qf, &a.ktf}) take(*x, nk * dk * C * pi);
       take(a.af, nh * C * C * pc);
       take(a.gates, nh * 3 * C);
-      if (!back) take(a.bf, nh * C * C * po);
+      if (!back) take(a.bf, nh * C * C * pc);
       else {
         take(a.qtf, nk * dk * C * pi);
         take(a.bt, nh * C * C * pc);

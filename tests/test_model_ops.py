@@ -646,6 +646,22 @@ def test_delta_equal_keys(T, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T", [20, 250])
+def test_delta_small_values_in_the_place_of_large_ones(T, dtype):
+    # beta = 1 and keys that do not meet: each step reads its own value, as the difference of what was held and what is taken from it
+    x, _, _, _, _ = delta_inputs(T, 2, 2, 2, 32, 48, dtype, seed=21)
+    x[0][:] = x[1][:] = torch.eye(32, device="cuda")[torch.arange(T) % 32][:, None, None]
+    x[3].zero_()
+    x[4].fill_(1.0)
+    s0 = 4096 * torch.randn((2, 2, 32, 48), generator=torch.Generator().manual_seed(22)).cuda()
+    x[2][:T // 2] *= 512
+    o = snn.snn_delta_forward(*x, s0, scale=1.0)[0]
+    held = max(s0.abs().max().item(), x[2].abs().max().item())
+    near(o, x[2].cpu(), 16 * U * held, "o")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
 def test_delta_gates_at_their_ends(dtype):
     # decays that forget all (minus infinity, and sums of them that 32 bits would round), none at all, beta 0 and 1
     T = 150
