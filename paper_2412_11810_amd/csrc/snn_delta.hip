@@ -183,6 +183,25 @@ __device__ __forceinline__ void lds_barrier() { // of the LDS alone: loads from 
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// What a lane some lanes on, some lanes back or some lanes round in the same 16 has (0: there is none)
+constexpr int NEXT = 0x100, BEFORE = 0x110, ROUND = 0x120;
+template <int FROM, class X> __device__ __forceinline__ X in_row(X x) {
+  uint32_t word[sizeof(X) / 4];
+  __builtin_memcpy(word, &x, sizeof x);
+#pragma unroll
+  for (uint32_t &v : word) v = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, FROM, 0xf, 0xf, true);
+  __builtin_memcpy(&x, word, sizeof x);
+  return x;
+}
+__device__ __forceinline__ double of_lane(double x, int lane) {
+  uint32_t word[2];
+  __builtin_memcpy(word, &x, sizeof x);
+#pragma unroll
+  for (uint32_t &v : word) v = (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+  __builtin_memcpy(&x, word, sizeof x);
+  return x;
+}
+
 template <class T> __device__ __forceinline__ float element(const T *p, bool on) { return on ? (float)*p : 0.f; }
 // Elements as they are in memory, asked for ahead of their use
 template <class T> struct Octet { // 8 of a row
@@ -1066,6 +1085,7 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
       const int at = 2 * half + j, col = 16 * at + r;
       const float beta_col = gates[2][col];
       float z_col = 0.f;
+      tile z_on;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int row = row0 + e;
@@ -1074,7 +1094,7 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
         const float dps = low ? p[j][e] * d * a.scale : 0.f, me = below ? x[j][e] * d : 0.f; // beta of the column is left out
         const float zq = low ? qk[j][e] * dps : 0.f, zk = below ? kk[j][e] * me : 0.f;
         const float z = zq - zk; // of both w . dU less that of what it was taken from; times beta, of what decays lie between
-        of_z[e] = fmaf(z, beta_col, of_z[e]);
+        z_on[e] = z * beta_col;
         z_col += z;
         squares.dp[row][col] = dps * beta_col;
         if (below) squares.m[row][col] = squares.m[col][row] = -me * beta_col;
@@ -1083,6 +1103,16 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
 #pragma unroll
       for (int s = 16; s < 64; s *= 2) z_col += __shfl_xor(z_col, s);
       if (q4 == 0) of_col[w][col] = z_col;
+      // Between column and row lies the decay of every step behind the column's up to the row's.  So far that of the row itself: the column's sums from it to the end of these 16
+#pragma unroll
+      for (int e = 2; e >= 0; --e) z_on[e] += z_on[e + 1];
+      float next = __shfl_down(z_on[0], 16);
+      if (q4 == 3) next = 0.f;
+      const float two_on = __shfl_down(z_on[0] + next, 32);
+      if (q4 < 2) next += two_on;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col < row0 + e) of_z[e] += z_on[e] + next;
     }
 #pragma unroll
     for (int s = 16; s < 64; s *= 2) {
@@ -1090,9 +1120,12 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
       wrote += __shfl_xor(wrote, s);
     }
 #pragma unroll
-    for (int s = 1; s < 16; s *= 2)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) of_z[e] += __shfl_xor(of_z[e], s);
+    for (int e = 0; e < 4; ++e) {
+      of_z[e] += in_row<ROUND + 8>(of_z[e]);
+      of_z[e] += in_row<ROUND + 4>(of_z[e]);
+      of_z[e] += in_row<ROUND + 2>(of_z[e]);
+      of_z[e] += in_row<ROUND + 1>(of_z[e]);
+    }
     if (r == 0) *(tile *)(of_row[0][half] + row0) = of_z;
     if (q4 == 0) {
       of_row[1][half][mine] = read_by;
@@ -1125,21 +1158,29 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (wave == 0) {
+    // A wavefront has the decays of its 16 steps, each a sum of what goes past it alone: behind strong decays that is all there is of it, and much less than
+    // what lies on either side
+    if (half == 0) {
       const float beta = gates[2][lane], of_w = (of_col[0][lane] + of_col[1][lane]) + (of_col[2][lane] + of_col[3][lane]), left = of_row[2][0][lane] + of_row[2][1][lane];
-      const float own = left * beta;
-      double on = ((double)of_row[0][0][lane] + of_row[0][1][lane]) + ((double)of_row[1][0][lane] + of_row[1][1][lane]) - (double)of_w * beta;
-      double up = own;
+      float further = 0.f; // read behind these 16 steps
 #pragma unroll
-      for (int s = 1; s < C; s *= 2) {
-        const double o = __shfl_down(on, s), y = __shfl_up(up, s);
-        if (lane + s < C) on += o;
-        if (lane >= s) up += y;
-      }
+      for (int x = 1; x < 4; ++x)
+        if (x > w) further += of_col[x][lane];
+      // sums from a step on, and of those before it
+      double on = (double)of_row[1][0][lane] + of_row[1][1][lane], up = ((double)left + further) * beta;
+      on += in_row<NEXT + 1>(on), up += in_row<BEFORE + 1>(up);
+      on += in_row<NEXT + 2>(on), up += in_row<BEFORE + 2>(up);
+      on += in_row<NEXT + 4>(on), up += in_row<BEFORE + 4>(up);
+      on += in_row<NEXT + 8>(on), up += in_row<BEFORE + 8>(up);
+      double rest = 0.;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (x != w) rest += x > w ? of_lane(on, 16 * x) : of_lane(up, 16 * x + 15);
+      up = in_row<BEFORE + 1>(up) + rest;
       const float all = end * (((of_all[0] + of_all[1]) + (of_all[2] + of_all[3])) + ((of_all[4] + of_all[5]) + (of_all[6] + of_all[7])));
-      if (t0 + lane < a.T) {
+      if (lane >> 4 == w && t0 + lane < a.T) {
         const long long at = ((long long)(t0 + lane) * a.batch + b) * a.heads + h;
-        a.dg[at] = t0 + lane < len ? (float)(all + on + (up - own)) : 0.f;
+        a.dg[at] = t0 + lane < len ? (float)(all + on + up + ((double)of_row[0][0][lane] + of_row[0][1][lane])) : 0.f;
         a.dbeta[at] = t0 + lane < len ? of_w + left : 0.f;
       }
     }

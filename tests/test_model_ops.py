@@ -687,6 +687,34 @@ def test_delta_gates_at_their_ends(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("K,dk,dv", [(7, 40, 40), (1, 40, 70), (7, 100, 33), (1, 128, 64)])
+def test_delta_gradients_of_gates_behind_strong_decays(K, dk, dv, dtype):
+    # What goes past a decay is all that its gate's gradient is made of, however little that is beside what was written before it and read after it: heads that
+    # forget nearly all at every step, and single strong decays among mild ones, each compared to its own size.
+    T, H = 200, 7
+    x, s0, do, ds, lengths = delta_inputs(T, 1, H, K, dk, dv, dtype, seed=20)
+    g, strong = x[3], [-5.0, -10.0, -20.0, -60.0, -20.0, -30.0]
+    for h in range(4):
+        g[:, 0, h] = strong[h]
+    g[::9, 0, 4] = strong[4]
+    g[[63, 64, 100, 101, 150], 0, 5] = strong[5]
+    kept = snn.snn_delta_forward(*x, s0, keep=True)[2]
+    c = [clean(a, lengths).requires_grad_() for a in x]
+    S = s0.cpu().double().requires_grad_()
+    o, last, _ = delta_plain(*c, S, lengths.cpu(), dk ** -0.5)
+    want = torch.autograd.grad((o * do.cpu().double()).sum() + (last * ds.cpu().double()).sum(), (c[3], c[4]))
+    got = snn.snn_delta_backward(*x, kept, do, ds)[3:5]
+    for a, b, what in zip(got, want, ("dg", "dbeta")):
+        for h in range(H):
+            # (the exponent of a decay has 24 bits: the decay is off by |g| U, and twice that by its multiplication with log2 e)
+            at = g[:, 0, h] < -4.9
+            for part in (at, ~at):
+                off = 2 * U * -strong[h] if h < 6 and part is at else 0
+                close(a[part, 0, h], b[part.cpu(), 0, h], delta_tol(T, dk, 3) + off, (what, h))
+
+
+@gpu
 @pytest.mark.parametrize("T", [4, 90, 2000])
 def test_delta_values_that_are_not_finite_stay_in_their_heads(T):
     x, s0, do, ds, _ = delta_inputs(T, 3, 4, 2, 20, 30, torch.float32, seed=9)
