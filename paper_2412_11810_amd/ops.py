@@ -449,9 +449,20 @@ class AdamwPlan:
 
     def __init__(self, params, m, v, copies, tensors, device):
         self.params, self.m, self.v, self.copies, self.tensors, self.device = params, m, v, copies, tensors, device
+        self.held = [y for x in (*params, *m, *v, *copies) if x is not None for y in (x if isinstance(x, Packed) else (x,))]
         # (the memory that `tensors` points at stays, also where a tensor is given other memory)
-        parts = (y for x in (*params, *m, *v, *copies) if x is not None for y in (x if isinstance(x, Packed) else (x,)))
-        self.memory = [x.detach() for x in parts]
+        self.memory = [x.detach() for x in self.held]
+        self.addresses = [x.data_ptr() for x in self.held]
+
+    def names(self):
+        """What each of `held` is called."""
+        for name, xs in (("params", self.params), ("m", self.m), ("v", self.v), ("copies", self.copies)):
+            for i, x in enumerate(xs):
+                if isinstance(x, Packed):
+                    yield f"the codes of {name}[{i}]"
+                    yield f"the exponents of {name}[{i}]"
+                elif x is not None:
+                    yield f"{name}[{i}]"
 
 
 def snn_adamw_moments(params, bits=32):
@@ -479,7 +490,8 @@ def snn_adamw_moments(params, bits=32):
 def snn_adamw_plan(params, m, v, copies=None):
     """What snn_adamw_step needs of its tensors, once for all steps: params (float32 or bfloat16, contiguous), their moments (snn_adamw_moments,
     or tensors like those) and, if wanted, copies in bfloat16 of params in float32 (None in the list: no copy of that one).
-    The tensors are held, and changed in place by each step; params that have been given other memory since (x.data = ...) need a new plan."""
+    The tensors are held, and changed in place by each step; where any of them has been given other memory since (x.data = ...), a step
+    raises: that needs a new plan."""
     import torch
     params, m, v = list(params), list(m), list(v)
     copies = [None] * len(params) if copies is None else list(copies)
@@ -523,6 +535,10 @@ def snn_adamw_step(plan, grads, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, wei
     if not grads:
         return
     device = plan.device
+    now = list(map(torch.Tensor.data_ptr, plan.held))
+    if now != plan.addresses:
+        name = next(name for name, a, b in zip(plan.names(), now, plan.addresses) if a != b)
+        raise ValueError(f"{name} has other memory than when the plan was made")
     for i, (g, p, t) in enumerate(zip(grads, plan.params, plan.tensors)):
         if g.dtype == torch.bfloat16:
             t.dtype_g = SNN_BF16
@@ -530,8 +546,6 @@ def snn_adamw_step(plan, grads, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, wei
             t.dtype_g = SNN_F32
         else:
             raise TypeError(f"grads[{i}] must be float32 or bfloat16, got {g.dtype}")
-        if p.data_ptr() != (t.p or 0):
-            raise ValueError(f"params[{i}] has other memory than when the plan was made")
         if g.shape != p.shape or g.device != device or not g.is_contiguous():
             _packed_rows(_same(g, f"grads[{i}]", g.dtype, p.shape, device), f"grads[{i}]")
         t.g = g.data_ptr()

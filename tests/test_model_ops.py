@@ -1029,6 +1029,26 @@ def test_a_plan_is_of_the_memory_that_its_tensors_had():
     assert held() is None
 
 
+@pytest.mark.parametrize("bits,which,name", [(32, "m", "m"), (32, "v", "v"), (8, "m.codes", "the codes of m"), (8, "m.exps", "the exponents of m"),
+                                             (8, "v.codes", "the codes of v"), (8, "v.exps", "the exponents of v"), (8, "copies", "copies"), (32, "params", "params")])
+def test_a_plan_is_of_the_memory_that_its_moments_and_copies_had(bits, which, name):
+    params = [torch.zeros(40), torch.zeros(0), torch.zeros(3, 50)]
+    m, v = snn.snn_adamw_moments(params, bits)
+    copies = [None, None, torch.zeros(3, 50, dtype=torch.bfloat16)]
+    plan = snn.snn_adamw_plan(params, m, v, copies)
+    x, part = dict(m=m, v=v, copies=copies, params=params)[which.split(".")[0]][2], which.split(".")[1:]
+    x = getattr(x, part[0]) if part else x
+    old, grads = x.detach(), [torch.zeros_like(p) for p in params]
+    with pytest.raises(ValueError, match="run on a GPU"):
+        snn.snn_adamw_step(plan, grads, 1)  # (as far as it comes here)
+    x.data = x.clone()  # moments that were loaded, say
+    with pytest.raises(ValueError, match=rf"^{name}\[2\] has other memory"):
+        snn.snn_adamw_step(plan, grads, 1)
+    x.data = old
+    with pytest.raises(ValueError, match="run on a GPU"):
+        snn.snn_adamw_step(plan, grads, 1)
+
+
 def test_c_entry_points_of_the_delta_rule_refuse_what_they_cannot_run():
     L, at = snn.lib(), ops.snn_launch(0, None, None, 0)
     here = C.cast(C.create_string_buffer(4096), C.c_void_p).value
