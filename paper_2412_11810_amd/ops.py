@@ -539,13 +539,12 @@ def snn_adamw_step(plan, grads, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, wei
     if now != plan.addresses:
         name = next(name for name, a, b in zip(plan.names(), now, plan.addresses) if a != b)
         raise ValueError(f"{name} has other memory than when the plan was made")
+    kinds = {torch.float32: SNN_F32, torch.bfloat16: SNN_BF16}
     for i, (g, p, t) in enumerate(zip(grads, plan.params, plan.tensors)):
-        if g.dtype == torch.bfloat16:
-            t.dtype_g = SNN_BF16
-        elif g.dtype == torch.float32:
-            t.dtype_g = SNN_F32
-        else:
+        kind = kinds.get(g.dtype)
+        if kind is None:
             raise TypeError(f"grads[{i}] must be float32 or bfloat16, got {g.dtype}")
+        t.dtype_g = kind
         if g.shape != p.shape or g.device != device or not g.is_contiguous():
             _packed_rows(_same(g, f"grads[{i}]", g.dtype, p.shape, device), f"grads[{i}]")
         t.g = g.data_ptr()
