@@ -401,11 +401,13 @@ size_t snn_delta_workspace(const snn_delta *p, int32_t gradients);
 
 /* q, k [T][batch][key_heads][dk], v, o [T][batch][heads][dv], g, beta [T][batch][heads] fp32; s0 [batch][heads][dk][dv] fp32 or NULL (zeros); s_last of the same
  * shape or NULL, may be s0 itself (serving: T = 1, state in and out); kept [ceil(T / 256)][batch][heads][dk][dv] fp32 or NULL: the states before the
- * steps 1, 257, 513, ..., which the backward pass recomputes the others from. */
+ * steps 1, 257, 513, ..., which the backward pass recomputes the others from.  No element of a result may be one of another array (SNN_E_INVAL), but
+ * s_last may be s0, and o may take the place of v (the same rows, equally far apart). */
 snn_status snn_delta_forward(const snn_launch *at, const snn_delta *p, const void *q, const void *k, const void *v, const float *g, const float *beta,
                              const float *s0, void *o, float *s_last, float *kept);
 
-/* Gradients of q, k, v, g, beta and s0 from those of o and, where ds_last is not NULL, of s_last.  ds0 may be NULL; it may be ds_last itself. */
+/* Gradients of q, k, v, g, beta and s0 from those of o and, where ds_last is not NULL, of s_last.  ds0 may be NULL; it may be ds_last itself, and dq, dk, dv, dg
+ * and dbeta may take the place of q, k, v, g and beta.  No other element of a result may be one of another array (SNN_E_INVAL). */
 snn_status snn_delta_backward(const snn_launch *at, const snn_delta *p, const void *q, const void *k, const void *v, const float *g, const float *beta,
                               const float *kept, const void *dout, const float *ds_last, void *dq, void *dk, void *dv, float *dg, float *dbeta, float *ds0);
 

@@ -2,6 +2,7 @@
 // They allocate nothing, wait for nothing and keep nothing but the text of a thread's last error.
 #include "../../include/snn.h"
 #include "snn_ops.h"
+#include "snn_share.h"
 
 #include <algorithm>
 #include <cmath>
@@ -70,6 +71,18 @@ snn_status check_workspace(const char *what, const snn_launch *at, size_t bytes)
     return refuse(SNN_E_INVAL, "%s: the workspace has %zu bytes, %zu are needed", what, at->workspace ? at->workspace_bytes : (size_t)0, bytes);
   const Array w[] = {{"the workspace", at->workspace, 256, true}};
   return check(what, at, w);
+}
+
+// An array of a call by the memory that it takes; a result may share none with another one, but that it may take the place of those whose numbers are in `of`.
+struct Part { const char *name; Rows at; bool result; unsigned of; };
+Rows in_one(const void *p, int64_t elements, size_t size) { return Rows{p, 1, elements * (int64_t)size, elements * (int64_t)size}; }
+template <int N> snn_status apart(const char *what, const Part (&parts)[N]) {
+  for (int i = 0; i < N; ++i)
+    for (int j = 0; j < N && parts[i].result; ++j) {
+      if (i == j || (parts[j].result && j < i) || ((parts[i].of >> j & 1) && same_place(parts[i].at, parts[j].at))) continue;
+      if (share(parts[i].at, parts[j].at)) return refuse(SNN_E_INVAL, "%s: %s and %s share elements", what, parts[i].name, parts[j].name);
+    }
+  return SNN_OK;
 }
 
 size_t size_of(int dtype) { return dtype == SNN_BF16 ? 2 : 4; }
@@ -163,6 +176,17 @@ snn_status delta_shape(const char *what, const snn_delta *p, DeltaShape *d) {
   }
   return SNN_OK;
 }
+
+struct DeltaParts {
+  const DeltaShape &d;
+  size_t size;
+  Rows rows(const void *p, long long ld, bool keys) const { // of the steps and sequences, with all heads
+    return Rows{p, (int64_t)d.T * d.batch, (int64_t)size * (keys ? d.key_heads * d.dk : d.heads * d.dv), ld * (int64_t)size};
+  }
+  Rows gates(const float *p) const { return in_one(p, (int64_t)d.T * d.batch * d.heads, 4); }
+  Rows states(const float *p, int64_t n) const { return in_one(p, n * d.batch * d.heads * d.dk * d.dv, 4); }
+  Rows kept(const float *p) const { return states(p, (d.T + SNN_DELTA_INTERVAL - 1) / SNN_DELTA_INTERVAL); }
+};
 
 snn_status norm_shape(const char *what, const snn_norm *p, NormShape *n) {
   if (!p) return refuse(SNN_E_INVAL, "%s: no shape", what);
@@ -357,6 +381,11 @@ snn_status snn_delta_forward(const snn_launch *at, const snn_delta *p, const voi
                           {"o", o, size, some}, {"s_last", s_last, 4, false}, {"kept", kept, 4, false}, {"lengths", d.lengths, 4, false}};
   CHECK(check(what, at, arrays));
   CHECK(check_workspace(what, at, delta_workspace(d, false)));
+  const DeltaParts part{d, size};
+  const Part parts[] = {{"q", part.rows(q, d.ld_q, true)}, {"k", part.rows(k, d.ld_k, true)}, {"v", part.rows(v, d.ld_v, false)}, {"g", part.gates(g)},
+                        {"beta", part.gates(beta)}, {"s0", part.states(s0, 1)}, {"lengths", in_one(d.lengths, d.batch, 4)},
+                        {"o", part.rows(o, d.ld_o, false), true, 1u << 2}, {"s_last", part.states(s_last, 1), true, 1u << 5}, {"kept", part.kept(kept), true}};
+  CHECK(apart(what, parts));
   const OnDevice on(at->device);
   if (on.error != hipSuccess) return queued(on.error, what);
   return queued(launch_delta_forward(d, q, k, v, g, beta, s0, o, s_last, kept, at->workspace, (hipStream_t)at->stream), what);
@@ -375,6 +404,13 @@ snn_status snn_delta_backward(const snn_launch *at, const snn_delta *p, const vo
                           {"dg", dg, 4, some}, {"dbeta", dbeta, 4, some}, {"ds0", ds0, 4, false}, {"lengths", d.lengths, 4, false}};
   CHECK(check(what, at, arrays));
   CHECK(check_workspace(what, at, delta_workspace(d, true)));
+  const DeltaParts part{d, size};
+  const Part parts[] = {{"q", part.rows(q, d.ld_q, true)}, {"k", part.rows(k, d.ld_k, true)}, {"v", part.rows(v, d.ld_v, false)}, {"g", part.gates(g)},
+                        {"beta", part.gates(beta)}, {"kept", part.kept(kept)}, {"do", part.rows(dout, d.ld_o, false)}, {"ds_last", part.states(ds_last, 1)},
+                        {"lengths", in_one(d.lengths, d.batch, 4)}, {"dq", part.rows(dq, d.ld_dq, true), true, 1u << 0},
+                        {"dk", part.rows(dk, d.ld_dk, true), true, 1u << 1}, {"dv", part.rows(dv, d.ld_dv, false), true, 1u << 2},
+                        {"dg", part.gates(dg), true, 1u << 3}, {"dbeta", part.gates(dbeta), true, 1u << 4}, {"ds0", part.states(ds0, 1), true, 1u << 7}};
+  CHECK(apart(what, parts));
   const OnDevice on(at->device);
   if (on.error != hipSuccess) return queued(on.error, what);
   return queued(launch_delta_backward(d, q, k, v, g, beta, kept, dout, ds_last, dq, dk, dv, dg, dbeta, ds0, at->workspace, (hipStream_t)at->stream), what);

@@ -348,7 +348,7 @@ def snn_delta_forward(q, k, v, g, beta, s0=None, lengths=None, scale=None, keep=
     scale: 1 / sqrt(dk) unless given; consecutive heads share queries and keys where there are more of them than of keys.
 
     Returns o, the last state and, with keep, the states that snn_delta_backward needs (else None).  o and s_last: tensors for the results;
-    s_last may be s0 itself, a state that is updated in place."""
+    s_last may be s0 itself, a state that is updated in place, and o may be v."""
     import torch
     p, state = _delta_shape(q, k, v, g, beta, lengths, scale)
     device = q.device
@@ -368,7 +368,7 @@ def snn_delta_forward(q, k, v, g, beta, s0=None, lengths=None, scale=None, keep=
 
 def snn_delta_backward(q, k, v, g, beta, kept, do, ds_last=None, lengths=None, scale=None, dq=None, dk=None, dv=None):
     """Gradients of q, k, v, g, beta and s0 from those of o (and of the last state); q to beta, lengths and scale as the forward pass had them.
-    dq, dk and dv: tensors for the results (the parts of a projection's gradient, say)."""
+    dq, dk and dv: tensors for the results (the parts of a projection's gradient, say), which may be q, k and v themselves."""
     import torch
     p, state = _delta_shape(q, k, v, g, beta, lengths, scale)
     device = q.device

@@ -599,6 +599,40 @@ def test_delta_states_in_place(T):
 
 @gpu
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,H,K,dk,dv", [(6, 3, 3, 40, 40), (150, 4, 2, 24, 40), (300, 2, 2, 128, 128), (1700, 2, 1, 40, 64)])
+def test_delta_results_in_the_place_of_inputs(T, H, K, dk, dv, dtype):
+    x, s0, do, ds, lengths = delta_inputs(T, 2, H, K, dk, dv, dtype, ragged=True, seed=23)
+    want = snn.snn_delta_forward(*x, s0, lengths=lengths, keep=True)
+    back = snn.snn_delta_backward(*x, want[2], do, ds, lengths=lengths)
+    q, k, v, g, beta = (a.clone() for a in x)
+    got = snn.snn_delta_forward(q, k, v, g, beta, s0, lengths=lengths, keep=True, o=v)
+    assert got[0] is v and same(got, want)
+    v.copy_(x[2])
+    got = snn.snn_delta_backward(q, k, v, g, beta, want[2], do, ds, lengths=lengths, dq=q, dk=k, dv=v)
+    assert got[0] is q and got[1] is k and got[2] is v and same(got, back)
+    # dg and dbeta by the C entry point
+    (q, k, v, g, beta), ds0 = (a.clone() for a in x), ds.clone()
+    p = ops.snn_delta(T, 2, H, K, dk, dv, ops._type(q, "q"), dk ** -0.5, lengths=lengths.data_ptr())
+    at, space = ops._launch(ds.device, snn.lib().snn_delta_workspace(C.byref(p), 1))
+    inputs = [a.data_ptr() for a in (q, k, v, g, beta)]
+    assert snn.lib().snn_delta_backward(C.byref(at), C.byref(p), *inputs, want[2].data_ptr(), do.data_ptr(), ds0.data_ptr(), *inputs, ds0.data_ptr()) == 0
+    assert same([q, k, v, g, beta, ds0], back)
+
+
+@gpu
+def test_delta_refuses_results_in_other_places():
+    x, s0, do, ds, _ = delta_inputs(100, 2, 2, 2, 40, 40, torch.float32, seed=24)
+    kept, before = snn.snn_delta_forward(*x, s0, keep=True)[2], do.clone()
+    wide = torch.zeros((101, 2, 2, 40), device="cuda")
+    for call in (lambda: snn.snn_delta_backward(*x, kept, do, ds, dv=do), lambda: snn.snn_delta_backward(*x, kept, do, ds, dq=do),
+                 lambda: snn.snn_delta_backward(*x, kept, do, ds, dq=x[1]), lambda: snn.snn_delta_backward(*x, kept, do, ds, dq=wide[1:], dk=wide[:-1]),
+                 lambda: snn.snn_delta_forward(*x, s0, o=x[0]), lambda: snn.snn_delta_forward(*x[:2], wide[1:], *x[3:], s0, o=wide[:-1])):
+        refused(call, "share elements")
+    assert torch.equal(do, before) and (wide == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T", [5, 150])
 def test_delta_parts_of_a_projection(T, dtype):
     B, H, K, dk, dv = 3, 4, 2, 24, 40
