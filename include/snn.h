@@ -429,13 +429,14 @@ typedef struct {
 size_t snn_norm_workspace(const snn_norm *p);
 
 /* w [n] or NULL (ones); residual [rows][n] or NULL, then total must be NULL too; total [rows][n] or NULL: s, which may take the place of x or of the residual
- * (the same rows, equally far apart). */
+ * (the same rows, equally far apart), and so may y.  No other element of a result may be one of another array (SNN_E_INVAL). */
 snn_status snn_norm_forward(const snn_launch *at, const snn_norm *p, const void *x, const void *residual, const void *w, void *total, void *y);
 /* The same with y in 8 bits, as snn_pack would give it of a y that had not been rounded: codes [rows][n], exps [rows][ceil(n / 32)], packed. */
 snn_status snn_norm_forward_packed(const snn_launch *at, const snn_norm *p, const void *x, const void *residual, const void *w, void *total,
                                    int8_t *codes, uint8_t *exps);
 /* From total, as the forward pass gave it (or x, without a residual), and the gradients of y and, where dtotal is not NULL, of total: dx, which is the
- * residual's gradient as well and may take the place of dy or dtotal, and dw [n] (NULL: not wanted). */
+ * residual's gradient as well and may take the place of total, dy or dtotal, and dw [n] (NULL: not wanted).  No other element of a result may be one of
+ * another array (SNN_E_INVAL). */
 snn_status snn_norm_backward(const snn_launch *at, const snn_norm *p, const void *total, const void *w, const void *dy, const void *dtotal, void *dx,
                              void *dw);
 

@@ -213,6 +213,11 @@ snn_status norm_forward(const char *what, const snn_launch *at, const snn_norm *
                           {"y", y, size, !packed}, {"the codes", codes, 1, packed}, {"the exponents", exps, 1, packed}};
   CHECK(check(what, at, arrays));
   if (total && !residual) return refuse(SNN_E_INVAL, "%s: a total without a residual", what);
+  auto rows = [&](const void *q, long long ld) { return Rows{q, n.rows, n.n * (int64_t)size, ld * (int64_t)size}; };
+  const Part parts[] = {{"x", rows(x, n.ld_x)}, {"residual", rows(residual, n.ld_residual)}, {"w", in_one(w, n.n, size)}, {"total", rows(total, n.ld_total), true, 1u << 0 | 1u << 1},
+                        {"y", rows(y, n.ld_y), true, 1u << 0 | 1u << 1}, {"the codes", in_one(codes, n.rows * n.n, 1), true},
+                        {"the exponents", in_one(exps, n.rows * ((n.n + SNN_PACK_BLOCK - 1) / SNN_PACK_BLOCK), 1), true}};
+  CHECK(apart(what, parts));
   const OnDevice on(at->device);
   if (on.error != hipSuccess) return queued(on.error, what);
   return queued(launch_norm(n, x, residual, w, total, y, codes, exps, (hipStream_t)at->stream), what);
@@ -443,6 +448,10 @@ snn_status snn_norm_backward(const snn_launch *at, const snn_norm *p, const void
                           {"dx", dx, size, some}, {"dw", dw, size, false}};
   CHECK(check(what, at, arrays));
   if (dw) CHECK(check_workspace(what, at, norm_workspace(n)));
+  auto rows = [&](const void *q, long long ld) { return Rows{q, n.rows, n.n * (int64_t)size, ld * (int64_t)size}; };
+  const Part parts[] = {{"total", rows(total, n.ld_total)}, {"dy", rows(dy, n.ld_y)}, {"dtotal", rows(dtotal, n.ld_dtotal)}, {"w", in_one(w, n.n, size)},
+                        {"dx", rows(dx, n.ld_dx), true, 1u << 0 | 1u << 1 | 1u << 2}, {"dw", in_one(dw, n.n, size), true}};
+  CHECK(apart(what, parts));
   const OnDevice on(at->device);
   if (on.error != hipSuccess) return queued(on.error, what);
   return queued(launch_norm_backward(n, total, w, dy, dtotal, dx, dw, (float *)at->workspace, (hipStream_t)at->stream), what);

@@ -397,7 +397,7 @@ def snn_norm_forward(x, w=None, residual=None, eps=1e-6, packed=False, y=None, t
     """y = w s / sqrt(mean(s^2) + eps) for rows s = x + residual (or x) [..., n]; w [n] (None: ones).
 
     Returns y (packed: as Packed, in 8 bits) and s, which is what snn_norm_backward takes: x itself without a residual.  y and total: tensors
-    for the results; total may be x or residual itself, a sum that is updated in place."""
+    for the results; total may be x or residual itself, a sum that is updated in place, and so may y."""
     import torch
     dtype, device, (rows, n) = _type(x, "x"), x.device, _rows(x, "x")
     if w is not None:
@@ -427,7 +427,7 @@ def snn_norm_forward(x, w=None, residual=None, eps=1e-6, packed=False, y=None, t
 
 def snn_norm_backward(total, w, dy, dtotal=None, eps=1e-6, dx=None):
     """Gradients of x (and of the residual: the same) and of w (None without one) from those of y and, if given, of s = total itself.
-    dx: a tensor for the result, which may be dy or dtotal itself."""
+    dx: a tensor for the result, which may be total, dy or dtotal itself."""
     import torch
     dtype, device, (rows, n) = _type(total, "total"), total.device, _rows(total, "total")
     _same(dy, "dy", total.dtype, total.shape, device)

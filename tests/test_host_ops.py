@@ -37,12 +37,13 @@ class Memory:
 def outcome(lib, call, *args):
     before = lib.launches()
     status = getattr(lib, call)(C.byref(ops.snn_launch(0, None, None, 0)), *args)
-    assert lib.launches() - before == (status == snn.SNN_OK)
+    assert status == snn.SNN_OK or lib.launches() == before
     return "" if status == snn.SNN_OK else (status, lib.snn_launch_error().decode())
 
 
-def accepted(lib, call, *args):
-    assert outcome(lib, call, *args) == ""
+def accepted(lib, call, *args, launches=1):
+    before = lib.launches()
+    assert outcome(lib, call, *args) == "" and lib.launches() == before + launches
 
 
 def refused(lib, a, b, call, *args):
@@ -102,6 +103,38 @@ def test_parts_of_a_projection_are_apart(lib):
     refused(lib, "o", "q", "snn_delta_forward", delta(**p), *FORWARD(q=base, k=base + 64, v=base + 128, o=base + 400))
     accepted(lib, "snn_delta_backward", delta(**p), *BACKWARD(do=base + 192, q=base, k=base + 64, v=base + 128, dq=base, dk=base + 64, dv=base + 128))
     refused(lib, "dv", "do", "snn_delta_backward", delta(**p), *BACKWARD(do=base + 192, q=base, k=base + 64, v=base + 128, dv=base + 192))
+
+
+def test_results_of_the_norm_share_nothing_with_other_arrays(lib):
+    p = dict(rows=10, n=40, dtype=0, eps=1e-6)
+    norm = lambda **k: C.byref(ops.snn_norm(**{**p, **k}))  # noqa: E731
+    forward, packed = Memory(["x", "residual", "w", "total", "y"]), Memory(["x", "residual", "w", "total", "the codes", "the exponents"])
+    backward = Memory(["total", "w", "dy", "dtotal", "dx", "dw"])
+    for call, of, results, may in (("snn_norm_forward", forward, ("total", "y"), {"total": ("x", "residual"), "y": ("x", "residual")}),
+                                   ("snn_norm_forward_packed", packed, ("total", "the codes", "the exponents"), {"total": ("x", "residual")}),
+                                   ("snn_norm_backward", backward, ("dx", "dw"), {"dx": ("total", "dy", "dtotal")})):
+        accepted(lib, call, norm(), *of())
+        for i, a in enumerate(results):
+            for b in of.at:
+                if a == b:
+                    continue
+                if b in may.get(a, ()):
+                    accepted(lib, call, norm(), *of(**{a: b}))
+                    refused(lib, a, b, call, norm(), *of(**{a: of.at[b] + 160}))  # (row on row only)
+                else:
+                    first, second = (a, b) if b not in results or results.index(b) > i else (b, a)
+                    refused(lib, first, second, call, norm(), *of(**{a: b}))
+    accepted(lib, "snn_norm_forward", norm(), *forward(total="x", y="residual"))
+    accepted(lib, "snn_norm_forward", norm(), *forward(residual="x", total="x"))  # x + x
+    refused(lib, "total", "y", "snn_norm_forward", norm(), *forward(total="x", y="x"))
+    # the halves of wider rows, and rows that are not as far apart
+    x = forward.at["x"]
+    accepted(lib, "snn_norm_forward", norm(ld_x=80, ld_y=80), *forward(y=x + 160))
+    refused(lib, "y", "x", "snn_norm_forward", norm(ld_x=80, ld_y=80), *forward(y=x + 156))
+    refused(lib, "total", "x", "snn_norm_forward", norm(ld_x=40, ld_total=80), *forward(total=x))
+    accepted(lib, "snn_norm_forward", norm(rows=1, ld_x=40, ld_total=80), *forward(total=x))
+    accepted(lib, "snn_norm_forward", norm(rows=0), *forward(total="w"), launches=0)
+    refused(lib, "dw", "w", "snn_norm_backward", norm(rows=0), *backward(dw="w"))
 
 
 def test_arrays_of_rows_share_memory_where_their_rows_do(tmp_path):

@@ -127,6 +127,32 @@ def test_norm_backward(rows, n, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n", NORM)
+def test_norm_results_in_the_place_of_inputs(rows, n, dtype):
+    x, r, dy = (rows_of((rows, n), dtype, k, wide=n % 2) for k in (31, 32, 33))
+    w = rows_of((1, n), dtype, 34)[0]
+    want, back = snn.snn_norm_forward(x, w, residual=r), snn.snn_norm_backward(x, w, dy, dtotal=r)
+    for total, y in ((0, 1), (1, 0), (None, 0), (None, 1)):
+        place = [rows_of((rows, n), dtype, k, wide=n % 2) for k in (31, 32)]
+        got = snn.snn_norm_forward(place[0], w, residual=place[1], total=None if total is None else place[total], y=place[y])
+        assert got[0] is place[y] and (total is None or got[1] is place[total]) and same(got, want)
+    place = x.clone()
+    assert same(snn.snn_norm_backward(place, w, dy, dtotal=r, dx=place), back)
+
+
+@gpu
+def test_norm_refuses_results_in_other_places():
+    wide, w = torch.zeros((9, 40), device="cuda"), torch.ones(40, device="cuda")
+    x, r = wide[1:], torch.zeros((8, 40), device="cuda")
+    for call in (lambda: snn.snn_norm_forward(x, w, residual=r, total=wide[:-1]), lambda: snn.snn_norm_forward(x, w, y=wide[:-1]),
+                 lambda: snn.snn_norm_forward(x, w, residual=r, total=x, y=x), lambda: snn.snn_norm_forward(x, wide[3], y=x),
+                 lambda: snn.snn_norm_backward(x, w, r, dx=wide[:-1]), lambda: snn.snn_norm_backward(r, wide[4], r, dx=x)):
+        refused(call, "share elements")
+    assert (wide == 0).all()
+
+
+@gpu
 def test_norm_gradients_are_differences():
     s, dy, w = (rows_of(x, torch.float32, k) for k, x in enumerate(((5, 33), (5, 33), (1, 33))))
     dx, dw = snn.snn_norm_backward(s, w[0], dy, eps=1e-3)
