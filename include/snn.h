@@ -464,8 +464,8 @@ typedef struct {
 
 /* Bytes of workspace: none unless the step's number is on the device. */
 size_t snn_adamw_workspace(const snn_adamw *how);
-/* tensors: `count` descriptions in host memory, which are read before the call returns.  No two arrays that are written may share elements, nor may a
- * gradient with one of them (SNN_E_INVAL). */
+/* tensors: `count` descriptions in host memory, which are read before the call returns.  No two arrays that are written may share elements, the step's number
+ * among them, nor may a gradient or the gradients' scale with one of them (SNN_E_INVAL). */
 snn_status snn_adamw_step(const snn_launch *at, const snn_adamw *how, const snn_adamw_tensor *tensors, int64_t count);
 
 /*

@@ -225,10 +225,11 @@ snn_status norm_forward(const char *what, const snn_launch *at, const snn_norm *
 
 // No two of the arrays that a step writes may share elements: it would change them twice, or at the same time.
 struct Written { uintptr_t from, to; };
-snn_status adamw_arrays(const char *what, const snn_launch *at, const snn_adamw_tensor *tensors, int64_t count, std::vector<AdamwTensor> &out) {
+snn_status adamw_arrays(const char *what, const snn_launch *at, const snn_adamw *how, const snn_adamw_tensor *tensors, int64_t count, std::vector<AdamwTensor> &out) {
   std::vector<Written> written;
   out.reserve(count);
-  written.reserve(6 * count);
+  written.reserve(6 * count + 1);
+  if (how->step_on_device) written.push_back({(uintptr_t)how->step_on_device, (uintptr_t)how->step_on_device + 4});
   for (int64_t k = 0; k < count; ++k) {
     const snn_adamw_tensor &x = tensors[k];
     if (!dtype_ok(x.dtype_p) || !dtype_ok(x.dtype_g)) return refuse(SNN_E_INVAL, "%s: tensor %lld: unknown type", what, (long long)k);
@@ -250,11 +251,13 @@ snn_status adamw_arrays(const char *what, const snn_launch *at, const snn_adamw_
   std::sort(written.begin(), written.end(), [](const Written &a, const Written &b) { return a.from < b.from; });
   for (size_t i = 1; i < written.size(); ++i)
     if (written[i].from < written[i - 1].to) return refuse(SNN_E_INVAL, "%s: two of the arrays that the step writes share elements", what);
-  for (const AdamwTensor &x : out) { // a gradient may be anywhere but in what is written
-    const uintptr_t from = (uintptr_t)x.g, to = from + x.n * (x.g16 ? 2 : 4);
-    const auto next = std::upper_bound(written.begin(), written.end(), from, [](uintptr_t v, const Written &w) { return v < w.to; });
-    if (next != written.end() && next->from < to) return refuse(SNN_E_INVAL, "%s: a gradient shares elements with an array that the step writes", what);
-  }
+  auto writes = [&](const void *p, int64_t bytes) { // any of these
+    const auto next = std::upper_bound(written.begin(), written.end(), (uintptr_t)p, [](uintptr_t v, const Written &w) { return v < w.to; });
+    return next != written.end() && next->from < (uintptr_t)p + bytes;
+  };
+  for (const AdamwTensor &x : out) // a gradient may be anywhere but in what is written
+    if (writes(x.g, x.n * (x.g16 ? 2 : 4))) return refuse(SNN_E_INVAL, "%s: a gradient shares elements with an array that the step writes", what);
+  if (how->grad_scale && writes(how->grad_scale, 4)) return refuse(SNN_E_INVAL, "%s: the gradients' scale shares elements with an array that the step writes", what);
   return SNN_OK;
 }
 
@@ -473,7 +476,7 @@ snn_status snn_adamw_step(const snn_launch *at, const snn_adamw *how, const snn_
   CHECK(check_workspace(what, at, snn_adamw_workspace(how)));
   try {
     std::vector<AdamwTensor> all;
-    CHECK(adamw_arrays(what, at, tensors, count, all));
+    CHECK(adamw_arrays(what, at, how, tensors, count, all));
     const OnDevice on(at->device);
     if (on.error != hipSuccess) return queued(on.error, what);
     const AdamwStep step = {how->lr, how->beta1, how->beta2, how->eps, how->weight_decay, how->step, how->step_on_device, how->grad_scale};

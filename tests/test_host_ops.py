@@ -137,6 +137,28 @@ def test_results_of_the_norm_share_nothing_with_other_arrays(lib):
     refused(lib, "dw", "w", "snn_norm_backward", norm(rows=0), *backward(dw="w"))
 
 
+def test_what_a_step_of_adamw_writes_shares_nothing_with_other_arrays(lib):
+    at = {name: (1 << 32) + (i << 20) for i, name in enumerate(("p", "g", "m", "v", "m_exps", "v_exps", "copy"))}
+    step, scale = 1 << 30, (1 << 30) + 4
+
+    def call(**k):
+        how = ops.snn_adamw(1e-3, 0.9, 0.99, 1e-8, 0.1, 0, k.pop("step", step), k.pop("scale", scale))
+        return "snn_adamw_step", C.byref(how), C.byref(ops.snn_adamw_tensor(**{**at, **dict(n=100), **k})), 1
+
+    accepted(lib, *call())
+    for a in at:
+        for b in at:
+            if a != b:
+                assert "share" in outcome(lib, *call(**{a: at[b]}))[1], (a, b)
+    size = dict(p=400, m=100, v=100, m_exps=4, v_exps=4, copy=200)
+    for b, n in size.items():
+        for one, what in (("step", "two of the arrays"), ("scale", "scale shares")):
+            assert what in outcome(lib, *call(**{one: at[b] + (n - 1) // 4 * 4}))[1], (one, b)
+            accepted(lib, *call(**{one: at[b] + (n + 3) // 4 * 4}))
+    assert "scale shares" in outcome(lib, *call(scale=step))[1]
+    accepted(lib, *call(scale=at["g"]))  # (which is only read)
+
+
 def test_arrays_of_rows_share_memory_where_their_rows_do(tmp_path):
     source, exe = tmp_path / "share.cpp", str(tmp_path / "share")
     source.write_text("""#include "snn_share.h"
