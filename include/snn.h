@@ -388,7 +388,8 @@ typedef struct {
   int32_t dk, dv;            /* 1..128, 1..1024; batch * heads * dv 2^28 at most */
   int32_t dtype;             /* snn_dtype of q, k, v, o and their gradients; gates and states are fp32 */
   float scale;               /* of the queries, 1 / sqrt(dk) say */
-  int64_t ld_q, ld_k, ld_v, ld_o;  /* elements between consecutive rows (t, b), each of all heads one after the other (0: packed; at most 2^25 bytes per step); ld_o: of o and do.
+  int64_t ld_q, ld_k, ld_v, ld_o;  /* elements between consecutive rows (t, b), each of all heads one after the other (0: packed; at most 2^25 bytes per step, but 2^40 elements
+                                      for a single step forward: a token of a large batch); ld_o: of o and do.
                                       q, k and v may be parts of one projection */
   int64_t ld_dq, ld_dk, ld_dv;
   const int32_t *lengths;    /* [batch] or NULL (T each): sequence b has steps 1..lengths[b]; a number outside 0..T counts as the nearer end.  What

@@ -154,7 +154,7 @@ snn_status vocab_shape(const char *what, const snn_vocab *p, VocabShape *v) {
   return SNN_OK;
 }
 
-snn_status delta_shape(const char *what, const snn_delta *p, DeltaShape *d) {
+snn_status delta_shape(const char *what, const snn_delta *p, bool back, DeltaShape *d) {
   if (!p) return refuse(SNN_E_INVAL, "%s: no shape", what);
   if (!dtype_ok(p->dtype)) return refuse(SNN_E_INVAL, "%s: unknown type %d", what, p->dtype);
   if (p->T < 0 || p->T > (1 << 30)) return refuse(SNN_E_INVAL, "%s: T = %d", what, p->T);
@@ -169,10 +169,12 @@ snn_status delta_shape(const char *what, const snn_delta *p, DeltaShape *d) {
   const int64_t of_keys = (int64_t)p->key_heads * p->dk, of_values = (int64_t)p->heads * p->dv;
   const std::pair<long long *, int64_t> lds[] = {{&d->ld_q, of_keys}, {&d->ld_k, of_keys}, {&d->ld_v, of_values}, {&d->ld_o, of_values},
                                                  {&d->ld_dq, of_keys}, {&d->ld_dk, of_keys}, {&d->ld_dv, of_values}};
+  // places in a chunk of 64 steps fit 32 bits; a step by itself has no chunk
+  const long long most = p->T == 1 && !back ? 1ll << 40 : (1 << 25) / p->batch / (long long)size_of(p->dtype);
   for (auto [ld, least] : lds) {
     if (!*ld) *ld = least;
-    if (*ld < least || *ld > (1 << 25) / p->batch / (long long)size_of(p->dtype)) // (places in a chunk of 64 steps fit 32 bits)
-      return refuse(SNN_E_INVAL, "%s: %lld elements from row to row: those of all heads or more, and 2^25 bytes per step at most", what, *ld);
+    if (*ld < least || *ld > most)
+      return refuse(SNN_E_INVAL, "%s: %lld elements from row to row: those of all heads or more, and 2^25 bytes per step at most (2^40 elements for one step forward)", what, *ld);
   }
   return SNN_OK;
 }
@@ -374,7 +376,7 @@ snn_status snn_vocab_loss_grad(const snn_launch *at, const snn_vocab *p, const v
 
 size_t snn_delta_workspace(const snn_delta *p, int32_t gradients) {
   DeltaShape d;
-  return delta_shape("snn_delta_workspace", p, &d) == SNN_OK ? delta_workspace(d, gradients != 0) : 0;
+  return delta_shape("snn_delta_workspace", p, gradients != 0, &d) == SNN_OK ? delta_workspace(d, gradients != 0) : 0;
 }
 
 snn_status snn_delta_forward(const snn_launch *at, const snn_delta *p, const void *q, const void *k, const void *v, const float *g, const float *beta,
@@ -382,7 +384,7 @@ snn_status snn_delta_forward(const snn_launch *at, const snn_delta *p, const voi
   static const char what[] = "snn_delta_forward";
   DeltaShape d;
   CHECK(launch_ok(what, at));
-  CHECK(delta_shape(what, p, &d));
+  CHECK(delta_shape(what, p, false, &d));
   const bool some = d.T > 0;
   const size_t size = size_of(p->dtype);
   const Array arrays[] = {{"q", q, size, some}, {"k", k, size, some}, {"v", v, size, some}, {"g", g, 4, some}, {"beta", beta, 4, some}, {"s0", s0, 4, false},
@@ -404,7 +406,7 @@ snn_status snn_delta_backward(const snn_launch *at, const snn_delta *p, const vo
   static const char what[] = "snn_delta_backward";
   DeltaShape d;
   CHECK(launch_ok(what, at));
-  CHECK(delta_shape(what, p, &d));
+  CHECK(delta_shape(what, p, true, &d));
   const bool some = d.T > 0;
   const size_t size = size_of(p->dtype);
   const Array arrays[] = {{"q", q, size, some}, {"k", k, size, some}, {"v", v, size, some}, {"g", g, 4, some}, {"beta", beta, 4, some}, {"kept", kept, 4, some},

@@ -105,6 +105,20 @@ def test_parts_of_a_projection_are_apart(lib):
     refused(lib, "dv", "do", "snn_delta_backward", delta(**p), *BACKWARD(do=base + 192, q=base, k=base + 64, v=base + 128, dv=base + 192))
 
 
+def test_a_step_by_itself_may_be_of_any_size(lib):
+    # 2^26 bytes of v and o: chunks of 64 such steps would have places beyond 32 bits, a step forward has none
+    for large in (dict(batch=1 << 18, dv=16), dict(ld_v=1 << 24), dict(ld_q=1 << 24), dict(ld_k=1 << 40)):
+        def far(names):
+            of = Memory(names)
+            of.at = {name: i << 56 for i, name in enumerate(names, 1)}
+            return of()
+        accepted(lib, "snn_delta_forward", delta(T=1, **large), *far(FORWARD.at))
+        for T, call, names in ((2, "snn_delta_forward", FORWARD.at), (0, "snn_delta_forward", FORWARD.at), (1, "snn_delta_backward", BACKWARD.at)):
+            assert "2^25 bytes" in outcome(lib, call, delta(T=T, **large), *far(names))[1]
+    assert "row to row" in outcome(lib, "snn_delta_forward", delta(T=1, ld_v=(1 << 40) + 1), *FORWARD())[1]
+    assert "2^28" in outcome(lib, "snn_delta_forward", delta(T=1, batch=1 << 18, dv=257), *FORWARD())[1]
+
+
 def test_results_of_the_norm_share_nothing_with_other_arrays(lib):
     p = dict(rows=10, n=40, dtype=0, eps=1e-6)
     norm = lambda **k: C.byref(ops.snn_norm(**{**p, **k}))  # noqa: E731

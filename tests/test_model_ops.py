@@ -881,6 +881,30 @@ def test_delta_beyond_4_gb():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_delta_token_of_a_large_batch(dtype):
+    # more than 2^25 bytes of v: the same bits as for parts of the batch
+    B, H, K, dk, dv = 1 << 15, 16, 2, 8, 64
+    g = torch.Generator(device="cuda").manual_seed(6)
+    rand = lambda *x: torch.randn(x, generator=g, device="cuda")  # noqa: E731
+    x = [rand(1, B, K, dk).to(dtype), rand(1, B, K, dk).to(dtype), rand(1, B, H, dv).to(dtype), -rand(1, B, H).abs(), torch.sigmoid(rand(1, B, H))]
+    state = rand(B, H, dk, dv)
+    o, last, _ = snn.snn_delta_forward(*x, state)
+    for at in range(0, B, B // 4):
+        at = slice(at, at + B // 4)
+        part = snn.snn_delta_forward(*[y[:, at] for y in x], state[at])
+        assert torch.equal(part[0], o[:, at]) and torch.equal(part[1], last[at])
+    # and rows that are far apart
+    wide = torch.full((1, 3, 1 << 24), 7.0, dtype=dtype, device="cuda")
+    n = H * dv
+    q, k, v, to = (wide[..., i * n:i * n + w * c].unflatten(-1, (w, c)) for i, (w, c) in enumerate(((K, dk), (K, dk), (H, dv), (H, dv))))
+    for y, z in zip((q, k, v), x):
+        y.copy_(z[:, :3])
+    got = snn.snn_delta_forward(q, k, v, x[3][:, :3], x[4][:, :3], state[:3], o=to)
+    assert torch.equal(to, o[:, :3]) and torch.equal(got[1], last[:3]) and (wide[..., 4 * n:] == 7).all()
+
+
+@gpu
 @pytest.mark.parametrize("T", [1, 100, 1600])
 def test_delta_in_a_graph(T):
     x, s0, do, ds, lengths = delta_inputs(T, 3, 4, 2, 40, 50, torch.bfloat16, ragged=T > 1, seed=11)
