@@ -862,6 +862,37 @@ def test_delta_ends_in_any_piece(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,chunks", [(torch.float32, 700), (torch.bfloat16, 1500)])
+def test_delta_segments_of_pieces(dtype, chunks):
+    # few heads and more steps than the workspace holds at once: pieces, whose walks take segments side by side.  Calls for parts of 20 chunks, which have one
+    # segment and one piece, sum in another order
+    T, H, dk, dv, part = 64 * chunks + 17, 16, 128, 64, 1280
+    g = torch.Generator(device="cuda").manual_seed(7)
+    rand = lambda *x: torch.randn(x, generator=g, device="cuda")  # noqa: E731
+    q, k = (torch.nn.functional.normalize(rand(T, 1, H, dk), dim=-1).to(dtype) for _ in range(2))
+    x = [q, k, rand(T, 1, H, dv).to(dtype), -0.02 * rand(T, 1, H).abs(), torch.sigmoid(rand(T, 1, H))]
+    do, s0, ds = rand(T, 1, H, dv).to(dtype), rand(1, H, dk, dv), rand(1, H, dk, dv)
+    size = lambda n, back: snn.lib().snn_delta_workspace(C.byref(ops.snn_delta(n, 1, H, H, dk, dv, ops._type(q, "q"), 1.0)), back)  # noqa: E731
+    assert all(size(T, back) < 0.8 * chunks / 100 * size(6400, back) for back in (0, 1))
+    o, last, kept = snn.snn_delta_forward(*x, s0, keep=True)
+    grads = snn.snn_delta_backward(*x, kept, do, ds)
+    tol = 2 * delta_tol(T, dk, 1)
+    off = lambda a: HALF[dtype] if a.dtype == dtype else 0  # noqa: E731  (both are rounded)
+    cuts, state = list(range(0, T, part)), s0
+    for a in cuts:
+        oo, state, kk = snn.snn_delta_forward(*[y[a:a + part] for y in x], state, keep=True)
+        close(o[a:a + part], oo.cpu(), tol + off(oo), ("o", a))
+        close(kept[a // 256:(a + part) // 256], kk.cpu(), tol, ("kept", a))
+    close(last, state.cpu(), tol, "last")
+    for a in reversed(cuts):
+        back = snn.snn_delta_backward(*[y[a:a + part] for y in x], kept[a // 256:(a + part) // 256].contiguous(), do[a:a + part], ds)
+        ds = back[5]
+        for y, z, what in zip(grads, back[:5], ("dq", "dk", "dv", "dg", "dbeta")):
+            close(y[a:a + part], z.cpu(), 3 * tol + off(z), (what, a))
+    close(grads[5], ds.cpu(), 3 * tol, "ds0")
+
+
+@gpu
 def test_delta_beyond_4_gb():
     T, B, H, dv = 32768 + 16, 8, 64, 128  # 2^31 elements and more of v, of o
     g = torch.Generator(device="cuda").manual_seed(4)
