@@ -1139,22 +1139,33 @@ template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k
     lds_barrier();
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      float y[LANE];
-#pragma unroll
-      for (int j = 0; j < LANE; ++j) y[j] = squares.dp[mine][32 * s + 8 * q4 + j];
-      const Operand<PC> dpf = operand<PC>(y);
-#pragma unroll
-      for (int j = 0; j < LANE; ++j) y[j] = squares.dp[32 * s + 8 * q4 + j][mine];
-      const Operand<PC> dpt = operand<PC>(y);
-#pragma unroll
-      for (int j = 0; j < LANE; ++j) y[j] = squares.m[mine][32 * s + 8 * q4 + j];
-      const Operand<PC> m = operand<PC>(y);
       if constexpr (PI > 1) columns(s);
+      // (where heads share keys, a matrix after the other: there are no registers for all three)
+      auto apart = [] {
+        if constexpr (!ONE) __builtin_amdgcn_sched_barrier(0);
+      };
+      auto matrix = [&](auto at) {
+        float y[LANE];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        if (2 * s <= w) multiply(gq[n], kt[s][n], dpf);
-        multiply(gk[n], kt[s][n], m);
-        if (2 * s + 1 >= w) multiply(gk[n], qt[s][n], dpt);
+        for (int j = 0; j < LANE; ++j) y[j] = at(32 * s + 8 * q4 + j);
+        return operand<PC>(y);
+      };
+      if (2 * s <= w) {
+        const Operand<PC> f = matrix([&](int j) { return squares.dp[mine][j]; });
+#pragma unroll
+        for (int n = 0; n < NT; ++n) multiply(gq[n], kt[s][n], f);
+      }
+      apart();
+      {
+        const Operand<PC> f = matrix([&](int j) { return squares.m[mine][j]; });
+#pragma unroll
+        for (int n = 0; n < NT; ++n) multiply(gk[n], kt[s][n], f);
+      }
+      apart();
+      if (2 * s + 1 >= w) {
+        const Operand<PC> f = matrix([&](int j) { return squares.dp[j][mine]; });
+#pragma unroll
+        for (int n = 0; n < NT; ++n) multiply(gk[n], qt[s][n], f);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
