@@ -448,7 +448,8 @@ snn_status snn_norm_backward(const snn_launch *at, const snn_norm *p, const void
 typedef struct {
   double lr, beta1, beta2, eps, weight_decay; /* 0 <= beta < 1, eps >= 0 */
   int64_t step;            /* t: 1, 2, ... */
-  int32_t *step_on_device; /* [1] or NULL: steps taken so far, which the call counts up, and then goes by in place of `step` (a step in a graph) */
+  int32_t *step_on_device; /* [1] or NULL: steps taken so far, which the call counts up, and then goes by in place of `step` (a step in a graph, which
+                              keeps the other numbers, lr among them, as they were when it was captured) */
   const float *grad_scale; /* [1] or NULL: what the gradients are multiplied by first (1 / a loss scale, a clipping of their norm) */
 } snn_adamw;
 typedef struct {

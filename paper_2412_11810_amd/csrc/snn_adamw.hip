@@ -13,8 +13,8 @@
 // block, roundings cancel.  The root of a v that is not 0 has a code of 1 at least, as a divisor of 0 would make a step of any size.
 //
 // One launch for 40 tensors: their descriptions go as its arguments, so that nothing needs to be kept or copied.  A workgroup takes 8192 elements of one, a
-// lane 8 at a time.  What bounds it: memory.  363 million elements in bf16 with moments of 32 bits take 1947 us, 5.2 TB/s; 152 million with moments of 8 bits 495,
-// 4.9 TB/s; 17 tensors of 0.2 million in all are bound by the call, 22 us, 8 of them in the kernel.
+// lane 8 at a time.  What bounds it: memory.  363 million elements in bf16 with moments of 32 bits take 1942 us, 5.2 TB/s; 152 million with moments of 8 bits 494,
+// 4.9 TB/s; 17 tensors of 0.2 million in all are bound by the call, 22 us, 8.4 of them in the kernel, whose 34 workgroups take up to four rounds one after the other.
 #include "snn_rows.h"
 #include <math.h>
 

@@ -19,9 +19,9 @@
 // blocks of 16, in 32 bits, and by products of blocks, so that equal keys do no harm.
 // States and sums are of 32 bits.  Products go through the bf16 matrix cores: arrays of bf16 as they are, those of 32 bits in three bf16 parts, and what is
 // computed on the way (S, E, u, dE, A, B) in three too, 24 bits of it: six products of two such operands, three of one beside a bf16 array.
-// (Two parts would leave 16 bits.  With those, forward 4096 x 8 x 16 x 128 x 128 took 407 us instead of 514 and backward 1638 instead of 1838, but states
-// were off by up to 7e-6 of their norm and gradients of gates by 2e-5.  Where nothing but a result in bf16 comes of a product they are not enough either:
-// o is the difference of what the state held and what is written in its place, each of which may be thousands of times as large.)
+// (Two parts would leave 16 bits.  With those, forward 4096 x 8 x 16 x 128 x 128 took 407 us instead of 508 and backward 1638 instead of 1820, but states
+// were off by up to 7e-6 of their norm and gradients of gates by 2e-5.  Where nothing but a result in bf16 comes of a product they are not enough either
+// (486 us forward): o is the difference of what the state held and what is written in its place, each of which may be thousands of times as large.)
 //
 // The kernels: what is of a chunk alone (k_chunk: A, B, and the operands in the order in which a wavefront loads them); the walk over the chunks
 // with S in registers, its columns dealt to workgroups (k_walk; for the backward pass it starts at each kept state, every 4 chunks); the walk back
@@ -29,8 +29,10 @@
 // states found by the segments' maps, S' = M S + c (k_join).  They go through the sequence in pieces of 2 GB of
 // intermediate arrays.  Few steps are taken one after the other, by a kernel whose workgroup holds the whole state of a head (k_steps).
 //
-// At 4096 x 8 x 16 x 128 x 128 in bf16 forward takes 490 us and backward 1819 (memory alone would take 135 and 240): what a chunk's steps need of each other, and a chunk
-// of the one before, keeps the matrix cores waiting.
+// At 4096 x 8 x 16 x 128 x 128 in bf16 forward takes 508 us and backward 1820; the arrays of the call alone would take 135 and 214.  What bounds them is mostly what the kernels
+// leave for each other: 2.8 GB between memory and caches forward, 7.2 GB backward, where the call's arrays have 0.7 and 1.1.  Forward that is 5.5 TB/s, a
+// copy's 5.2 and what the caches give; backward 4.0, as the walks and the gradients also wait for products that need one another.  Short sequences are bound by the chain
+// of a chunk's steps and of the chunks.
 #include "snn_rows.h"
 
 namespace {
@@ -343,8 +345,9 @@ template <int RT, int NT> __device__ __forceinline__ void state_to(float *to, in
 // ---- a chunk by itself ------------------------------------------------------------------------
 // A workgroup has one head; heads that share queries and keys find the products of those each for itself: a workgroup for all of them, its registers full of
 // them, took longer at every size (333 x 5 x 6 of 2 x 48 x 75 in fp32 forward 49 us instead of 35, 2048 x 4 x 6 of 2 x 128 x 128 in bf16 90 instead of 81).
-// What bounds it: the substitution's chain of sums and the barriers between its parts, some 10 us for a workgroup of which four are in a compute unit, so that
-// registers count.  184 us for 8192 chunks of 128 channels, 0.8 GB of operands written; 132 us for 4096 in the backward pass.
+// What bounds it: memory, where there are many chunks: 192 us for 8192 of 128 channels in bf16, 0.71 GB of operands written and 0.30 read, 5.3 TB/s; 131 us for 4096 in the
+// backward pass, 0.65 GB, 5.0 TB/s.  Four workgroups to a compute unit, so that registers count, cover the substitution's chain of sums and the barriers between its
+// parts; these are what 180 chunks of 64 channels in fp32, less than one to a compute unit, take 16 us for.
 template <class T, int DK, bool BACK> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 4 : 3) void k_chunk(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32;
   typedef Planes<PI, C, DK> Rows;
@@ -560,8 +563,9 @@ __device__ __forceinline__ Unit unit_of(unsigned id, int units, int blocks) {
 // AGAIN: of the backward pass, from a kept state to the next; leaves S and w of each chunk.  MAPS: leaves what a segment makes of the state before it, M S + c:
 // c from no state, and M's columns from those of the identity, without values.
 // What bounds it: a chunk's three products after one another, with an exchange through LDS and a barrier after each, 5 us for 32 columns of 128 channels with two
-// workgroups in a compute unit; the matrix cores work in half of that.  322 us for 64 chunks of 128 heads.  Operands as k_chunk laid them out go from
-// memory to registers a chunk ahead; made here of rows of q and k they took 350 us instead of 279.
+// workgroups in a compute unit, and what these load meanwhile.  337 us for 64 chunks of 128 heads in bf16: 0.69 PFLOP/s, and 1.49 GB read and 0.29 written, 5.3 TB/s.  (0.85 GB
+// of it are different ones: a head's workgroups meet in their L2 only in part.)  AGAIN: 179 us for half of the chunks, 0.75 GB, 4.2 TB/s.  Operands as k_chunk laid them out
+// go from memory to registers a chunk ahead; made here of rows of q and k they took a quarter longer.
 enum Walk { WALK, AGAIN, MAPS };
 template <int RT, int NT> __device__ __forceinline__ void identity(int row, int col, tile (&s)[RT][NT]) {
 #pragma unroll
@@ -722,7 +726,7 @@ template <class T, int DK, int BV, Walk HOW> __global__ __launch_bounds__(256, s
 }
 
 // ---- the walk back --------------------------------------------------------------------------------
-// As the walk, with four products, two of them after one another: 228 us for 32 chunks of 128 heads of 128 channels in bf16.
+// As the walk, with four products, two of them after one another: 226 us for 32 chunks of 128 heads of 128 channels in bf16, 0.91 GB, 4.0 TB/s.
 template <class T, int DK, int BV, Walk HOW> __global__ __launch_bounds__(256, sizeof(T) == 2 || DK == 64 ? 2 : 1) void k_walk_back(Args a) {
   constexpr bool OUT = HOW == WALK;
   constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32, RT = DK / 64, NT = BV / 16;
@@ -922,8 +926,10 @@ template <int DK, bool BACK> __global__ __launch_bounds__(256) void k_join(Args 
 // ---- gradients of a chunk's queries, keys and gates -----------------------------------------------
 // Sums over the state's columns go through LDS 32 at a time, in two places in turn, the next ones on their way; results are [dk][t], so that a lane has four elements of one step's
 // row.  Eight wavefronts: four take 16 steps each, with one half of the channels, and of the chunk's steps before theirs, four with the other.
-// What bounds it: 44 MFLOP a chunk of 128 x 128, six instructions to a product of what is computed on the way, at 0.49 PFLOP/s: one workgroup of 210 registers
-// to a compute unit, so that few wavefronts cover the times from memory and LDS.  370 us for 4096 chunks; with 128 registers and two workgroups values spill, and it is slower.
+// What bounds it: 46 MFLOP a chunk of 128 x 128, six instructions to a product of what is computed on the way, at 0.50 PFLOP/s, and 1.3 GB for 4096 chunks, 3.5 TB/s: one workgroup
+// to a compute unit, so that few wavefronts cover the times from memory and LDS.  373 us for 4096 chunks in bf16, own keys, 211 registers; with 128 registers and two
+// workgroups values spill, and it is slower.  Where heads share queries and keys, gq and gk live across the loop over the heads: at 128 channels 256 registers are not enough
+// then and 41 spill in bf16, 124 in fp32 (at 64 channels none and 2): 4096 x 8 x 6 heads of 128 x 128 in bf16 take 820 us backward in all with two of keys, 785 with six.
 template <class T, int DK, bool ONE> __global__ __launch_bounds__(512, 2) void k_grads(Args a) {
   constexpr int PI = GIVEN<T>, PC = MADE, KK = DK / 32, NT = DK / 32; // NT: tiles of a half of the channels
   struct Sums { Planes<PC, DK, 32> before, after; Planes<PC, C, 32> w; };
@@ -1332,18 +1338,20 @@ constexpr size_t PIECE = (size_t)2 << 30; // bytes of a piece's intermediate arr
 
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// Columns of the state that a workgroup walks with: fewer where there would be few workgroups, as a chunk then takes a shorter time.  4096 steps, 128 x 128, in us,
-// with 16 and with 32 columns: forward in fp32 4 heads 207 and 269, 32 heads 379 and 418, 64 heads 725 and 517; in bf16 132 and 186, 176 and 224, 331 and 269;
-// backward in fp32 4 heads 327 and 389 (in one segment each), 16 heads 613 and 649, 32 heads 933 and 926, 64 heads 1831 and 1460; in bf16 210 and 263, 366 and 396, 627 and 608, 1139
-// and 951.  64 columns to a workgroup are no faster than 32.
+// Columns of the state that a workgroup walks with: fewer where there would be few workgroups, as a chunk then takes a shorter time.  4096 steps in one segment, 128 x 128, in us,
+// with 16 and with 32 columns: forward in fp32 4 heads 260 and 314, 32 heads 363 and 410, 64 heads 710 and 519; in bf16 141 and 192, 191 and 237, 332 and 287;
+// backward in fp32 4 heads 351 and 413, 16 heads 587 and 627, 32 heads 907 and 904, 64 heads 1799 and 1434; in bf16 218 and 265, 382 and 408, 595 and 591, 1114
+// and 946.  Other sizes change sides at the same number of workgroups: 64 x 64 in bf16 forward 64 heads 199 and 226, 128 heads 346 and 298, backward 32 heads 353 and 366,
+// 64 heads 548 and 536; 128 x 256 forward 16 heads 163 and 206, 32 heads 275 and 243.  64 columns to a workgroup are no faster than 32.
 int columns(const DeltaShape &p, bool back) {
   const long long heads = (long long)p.batch * p.heads;
   return heads * ((p.dv + 31) / 32) > (back ? 64 : 128) ? 32 : 16;
 }
 
-// Whether steps are taken one after the other.  dk and dv 128, in us, so and in chunks: 16 heads, 8 steps 19.6 and 22.5 in fp32, 19.9 and 20.7 in bf16, 12 steps
-// 25.2 and 22.5, 25.6 and 20.7; 128 heads, fp32 16 steps 34.6 and 35.2, 32 steps 59.7 and 35.4, bf16 8 steps 23.3 and 23.9, 12 steps 29.5 and
-// 24.1; 1024 heads, fp32 32 steps 150 and 229, bf16 12 steps 80.7 and 93.0, 16 steps 94.7 and 89.4.
+// Whether steps are taken one after the other.  dk and dv 128, in us, so and in chunks: 16 heads, 8 steps 19.8 and 23.6 in fp32, 20.3 and 21.2 in bf16, 12 steps
+// 25.3 and 23.6, 25.9 and 21.3; 128 heads, fp32 16 steps 31.9 and 36.2, 32 steps 53.3 and 36.8, bf16 8 steps 21.1 and 24.3, 12 steps 26.6 and
+// 24.5; 1024 heads, fp32 32 steps 121 and 224, bf16 12 steps 58 and 100, 16 steps 69 and 101 (from no state; with one, 94.7 and 89.4).  The numbers are those of 128 channels:
+// with 64 steps one after the other would pay somewhat longer (16 heads, 12 steps 17.3 and 21.6 in fp32), which the rule does not use.
 bool one_by_one(const DeltaShape &p) {
   const long long heads = (long long)p.batch * p.heads;
   return p.T <= (heads < 128 ? 8 : heads < 512 ? p.bf16 ? 8 : 16 : p.bf16 ? 12 : 32);
@@ -1351,9 +1359,10 @@ bool one_by_one(const DeltaShape &p) {
 
 // Segments of a piece, walked side by side: one walk leaves their maps, k_join the states between them, and another walk the results.  That is 2.5 times the work, for
 // walks that would leave most of the chip idle, 512 workgroups in all, and at least 8 chunks for each of 3 segments.  In one segment and so, us, forward and backward:
-// 16384 steps, 8 heads of 64 x 128 in bf16 438 and 190, 859 and 530, in fp32 653 and 315, 1164 and 774; 4096 steps, 4 heads of 128 x 128 in bf16 134 and 88, 219 and
-// 154, in fp32 262 and 143, 354 and 258; 2048 steps, 2 heads of 64 x 64 in bf16 61 and 46, 98 and 78.  It does not pay with more workgroups (4096 steps, 12 heads
-// of 128 x 128, 96 of them: 152 and 180, 365 and 366; 16384 steps in fp32 1188 and 1289) nor with fewer chunks (1024 steps, 4 heads, 4 chunks each: 47 and 57).
+// 16384 steps, 8 heads of 64 x 128 in bf16 450 and 198, 848 and 521, in fp32 648 and 314, 1155 and 768; 4096 steps, 4 heads of 128 x 128 in bf16 140 and 90, 218 and
+// 154, in fp32 260 and 144, 351 and 257; 2048 steps, 2 heads of 64 x 64 in bf16 63 and 47, 98 and 78.  It does not pay with fewer chunks (1024 steps, 4 heads, 4 chunks
+// each: 47 and 57).  With more workgroups it goes both ways, and the rule leaves it: 96 of them, 12 heads of 128 x 128, 4096 steps in bf16 159 and 186, 363 and 364,
+// 16384 steps 620 and 703, 1433 and 1338, in fp32 1179 and 1305, 2341 and 2463; 128 of them, 16 heads, 16384 steps in bf16 602 and 507, 1485 and 1433, in fp32 1165 and 1069, 2302 and 2540.
 int segments_of(int bv, long long walks, int chunks) {
   if (bv != 16 || walks > 64) return 1;
   const int n = (int)(512 / walks < chunks / 8 ? 512 / walks : chunks / 8);

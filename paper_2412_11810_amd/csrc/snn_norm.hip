@@ -9,8 +9,10 @@
 // Sums of squares are of 32 bits; where one is too large or too small for that, the row is multiplied by a power of two first.
 // dw: a workgroup sums over its rows in registers and leaves one row of sums; a second kernel adds those up.  No atomics, so the same bits each time.
 //
-// What bounds it: memory.  32768 rows of 4096 in bf16: backward 200 us, 5.4 TB/s, and 11 us for dw's rows of sums; forward with residual and total into 8 bits
-// 182 us, 5.2 TB/s.  Few rows are bound by the call: 64 of 2048 take 11 us, 3 of them in the kernel.
+// What bounds it: memory.  32768 rows of 4096 in bf16: backward 202 us, 5.3 TB/s, and 11 us for dw's rows of sums; forward with residual and total into 8 bits
+// 181 us, 5.2 TB/s.  Few rows are bound by the call: 64 of 2048 take 11 us, 3 of them in the kernel.  Backward in bf16 two things are not at memory's rate.  Up to 1024 rows of sums
+// are read again by few workgroups (one for 32 columns): 11 of 27 us for 4329 rows of 2048, whose arrays take 10.  And rows of odd widths begin between words, and none is asked for
+// before the last one's sums: 161 us for 32768 of 1501, whose arrays take 57.
 #include "snn_rows.h"
 
 namespace {
@@ -268,7 +270,7 @@ struct Plan {
     // A workgroup has a row of more than 2048 elements (n is 2^15 at most: four vectors of a lane), and a shorter one where a wavefront would need four vectors, which
     // takes registers, or two and rows are few.  A wavefront and a workgroup to a row, us in a graph: 64 rows of 2048 in bf16 forward 5.1 and 2.8, 16384 rows
     // 53 and 47, backward 87 and 53; 4329 rows of 1501 in fp32 19.6 and 18.3, 33.4 and 28.6; but many rows in bf16 that leave lanes without elements or
-    // begin between words, forward, 16384 of 1500 45 and 68, of 1930 53 and 62.  Of 1024 in bf16 64 rows forward 3.6 and 2.8, 4329 rows 8.3 and 9.7; backward
+    // begin between words, forward, 16384 of 1500 45 and 68, of 1930 53 and 62 (whole words: 16384 of 1536 31.4 and 30.6, of 1920 37.8 and 38.0).  Of 1024 in bf16 64 rows forward 3.6 and 2.8, 4329 rows 8.3 and 9.7; backward
     // 64 rows 6.4 and 5.1, 256 rows 6.6 and 7.4.
     const bool wide = need > 128 ? back || !bf16 || rows <= 2048 || (need > 240 && n % LANE == 0) : need > 64 && rows <= (back ? 128 : 1024);
     waves = need <= 256 && !wide ? 1 : need <= 1024 ? 4 : 16;

@@ -527,7 +527,7 @@ def snn_adamw_plan(params, m, v, copies=None):
 def snn_adamw_step(plan, grads, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None):
     """One step of AdamW: params, moments and copies of the plan change in place.  grads: a gradient (float32 or bfloat16, contiguous) for each of
     params.  step: 1, 2, ..., or an int32 tensor [1] on the device with the number of steps taken, which the call counts up (a step in a
-    graph).  grad_scale: float32 [1] that the gradients are multiplied by first.  A plan is for one call at a time."""
+    graph, which keeps lr and the other numbers as they were when it was captured).  grad_scale: float32 [1] that the gradients are multiplied by first.  A plan is for one call at a time."""
     import torch
     grads = list(grads)
     if len(grads) != len(plan.params):
